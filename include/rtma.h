@@ -43,6 +43,8 @@ extern "C" {
 
 #define RTMA_MAX_PARTS 64
 #define RTMA_MAX_LAYERS 8
+#define RTMA_MAX_GROUPS 1024   /* parts of one call of the operators on rows (rtma_grouped_linear and below) */
+#define RTMA_MAX_WIDTH 16384   /* columns of one operand of rtma_grouped_linear */
 
 enum {
     RTMA_OK = 0,
@@ -331,6 +333,98 @@ int32_t rtma_sample_hop(rtma_ctx* ctx, int64_t n, const int64_t* rowptr, const i
                         int64_t frontier_size, const int32_t* frontier, int32_t fanout, uint64_t seed,
                         int32_t hop, int64_t* block_rowptr, int32_t* block_col, int32_t* next_frontier,
                         int64_t* next_size, void* stream);
+
+/* ---- operators on the rows of many parts --------------------------------------------------
+ * What a layer does to its rows, for programs that put a layer of their own between the partition
+ * (or the neighbour sampler) and the aggregation: the product with the part's matrix, group norm
+ * with an activation, dropout, and their gradients.  The paper's encoders use the first two in the
+ * forms that rtma_local_steps fixes (Sec. 4.1 "GNN Encoders"); these calls are not tied to a model.
+ *  - Rows of all parts lie behind one another; part g holds the rows offsets[g] .. offsets[g+1]-1.
+ *    offsets [G+1] is a DEVICE array, ascending, within [0, n] (rtma_partition's part_offsets); it is
+ *    never read back.  Parts may be empty.  Rows before offsets[0] and behind offsets[G] are neither
+ *    read nor written.  offsets == NULL (then G = 1): one part of all n rows.  1 <= G <=
+ *    RTMA_MAX_GROUPS.  Offsets that do not ascend or leave [0, n] are cut to it (the results of such
+ *    parts are not defined; no memory outside the n rows is touched); the checked build reports them.
+ *  - dtype is the type of the rows (and of W and b): RTMA_F32, RTMA_BF16 or RTMA_F16.  Sums are
+ *    fp32; results are rounded once.  Parameters of the norm, statistics and gradients of parameters
+ *    are float.  A row's values are adjacent; ld* is the distance between rows in elements.  Any
+ *    alignment of the element type works, rows on 16-byte boundaries are faster.
+ *  - Parameters of part g lie at p + g * stride (elements); stride 0: one for all parts, and the
+ *    gradient with stride 0 is then the sum over all parts.  So a replica's parameters can be used
+ *    where they lie in params [M][P] (stride P).
+ *  - Calls only enqueue.  Inside a stream capture they neither grow the scratch (make the call once
+ *    before, or reserve in rtma_create; else RTMA_ERR_WORKSPACE) nor wait for an earlier training
+ *    call's streams.  A replay uses the context's scratch like a call: order it with other calls on
+ *    the context.  Scratch that a captured graph uses is kept until rtma_destroy.
+ *  - Results are equal bit for bit from run to run.                                             */
+enum { RTMA_F32 = 0, RTMA_BF16 = 1, RTMA_F16 = 2 };
+
+/* Y[r] = X[r] W_g + b_g for the rows r of part g.  W_g [d_in][d_out] row-major at W + g * w_stride,
+ * b_g [d_out] at b + g * b_stride (b may be NULL).  X [n][ldx], Y [n][ldy]; they must not overlap.
+ * Of fp32 rows every product is exact to fp32 (no TF32); a value of X that is not finite makes its
+ * row of Y not finite, possibly NaN where fp32 arithmetic gives an infinity.
+ * 1 <= d_in, d_out <= RTMA_MAX_WIDTH.                                                          */
+int32_t rtma_grouped_linear(rtma_ctx* ctx, int32_t dtype, int64_t n, int32_t G, const int64_t* offsets,
+                            int32_t d_in, int32_t d_out, const void* X, int64_t ldx, const void* W,
+                            int64_t w_stride, const void* b, int64_t b_stride, void* Y, int64_t ldy,
+                            void* stream);
+/* dX[r] = dY[r] W_g^T.                                                                         */
+int32_t rtma_grouped_linear_dx(rtma_ctx* ctx, int32_t dtype, int64_t n, int32_t G,
+                               const int64_t* offsets, int32_t d_in, int32_t d_out, const void* dY,
+                               int64_t lddy, const void* W, int64_t w_stride, void* dX, int64_t lddx,
+                               void* stream);
+/* dW_g [d_in][d_out] = sum_r X[r]^T dY[r] at dW + g * dw_stride, db_g [d_out] = sum_r dY[r] at
+ * db + g * db_stride (db may be NULL); zeros for an empty part.  dw_stride = 0 with G > 1: one dW
+ * [d_in][d_out] (and one db, db_stride = 0) summed over all parts.                             */
+int32_t rtma_grouped_linear_dw(rtma_ctx* ctx, int32_t dtype, int64_t n, int32_t G,
+                               const int64_t* offsets, int32_t d_in, int32_t d_out, const void* X,
+                               int64_t ldx, const void* dY, int64_t lddy, float* dW, int64_t dw_stride,
+                               float* db, int64_t db_stride, void* stream);
+
+/* Group norm over channels that lie last, with an activation and dropout behind it:
+ *   xhat = (x - mean) / sqrt(var + eps), u = gamma_g xhat + beta_g, y = dropout(act(u))
+ * The C channels are cut into `groups` sets of C / groups neighbours.  scope RTMA_SCOPE_ROW: mean and
+ * (biased) variance of a set within its row (groups = 1 is Layer Normalization); RTMA_SCOPE_PART:
+ * within all rows of its part.  act: none, ReLU, PReLU (one slope per part, slope [G] with
+ * slope_stride), SiLU.  Dropout as rtma_dropout with p, seed and row_ids (NULL: the row's number).
+ *   gamma, beta  [C] per part or NULL (1 and 0).   C <= 2048.
+ *   stats        [n or G][groups][2] (mean, 1 / sqrt(var + eps)): kept for the gradient; NULL: not
+ *                kept.  An empty part's are (0, 1 / sqrt(eps)).
+ * Y may be X.                                                                                  */
+enum { RTMA_SCOPE_ROW = 0, RTMA_SCOPE_PART = 1 };
+enum { RTMA_ACT_NONE = 0, RTMA_ACT_RELU = 1, RTMA_ACT_PRELU = 2, RTMA_ACT_SILU = 3 };
+typedef struct {
+    int32_t dtype, C, groups, scope, act;
+    float eps;
+    double p;           /* dropout probability, 0: none                                          */
+    uint64_t seed;
+    int64_t gamma_stride, beta_stride, slope_stride;
+} rtma_norm_desc;
+int32_t rtma_group_norm(rtma_ctx* ctx, const rtma_norm_desc* desc, int64_t n, int32_t G,
+                        const int64_t* offsets, const void* X, int64_t ldx, const float* gamma,
+                        const float* beta, const float* slope, const int32_t* row_ids, void* Y,
+                        int64_t ldy, float* stats, void* stream);
+/* The gradient, from the forward call's X and stats: dX of dY, and (each may be NULL) dgamma, dbeta
+ * [C] and dslope [1] per part, with strides of their own; stride 0 with G > 1: summed over the parts.
+ * At u = 0 ReLU and PReLU take the derivative of the negative side.  dX may be dY or X.        */
+int32_t rtma_group_norm_grad(rtma_ctx* ctx, const rtma_norm_desc* desc, int64_t n, int32_t G,
+                             const int64_t* offsets, const void* X, int64_t ldx, const void* dY,
+                             int64_t lddy, const float* stats, const float* gamma, const float* beta,
+                             const float* slope, const int32_t* row_ids, void* dX, int64_t lddx,
+                             float* dgamma, int64_t dgamma_stride, float* dbeta, int64_t dbeta_stride,
+                             float* dslope, int64_t dslope_stride, void* stream);
+
+/* Y = residual + dropout(X) for n rows of d values (residual NULL: none).  The mask is never stored:
+ * element (row id v, column j) is dropped iff 16 bits of a hash are below t = floor(65536 p + 1/2),
+ *   h = S(S(seed) ^ ((uint64)(uint32)v << 32 | j / 4)), S = one SplitMix64 step, bits 16 (j mod 4) ..
+ * and kept values are multiplied by 65536 / (65536 - t), so the kept share is that of p rounded to
+ * 1/65536 and the expectation is exact.  A dropped value gives +0 whatever it was (NaN too).
+ * row_ids [n] int32 (device; NULL: the row's number) are the rows' ids, for instance rtma_partition's
+ * perm: a node then has the same mask in whatever part and place it is.  The gradient is the same call
+ * on dY without the residual.  0 <= p <= 1.  Y may be X or residual.                            */
+int32_t rtma_dropout(rtma_ctx* ctx, int32_t dtype, int64_t n, int32_t d, const void* X, int64_t ldx,
+                     const int32_t* row_ids, const void* residual, int64_t ldr, double p, uint64_t seed,
+                     void* Y, int64_t ldy, void* stream);
 
 /* ---- R2: aggregation (Algorithm 1, phi = plain average; Algorithm 2, overwrite) ---------
  * Wbar[j] = (1/M) sum_i params[i][j]; every replica is overwritten with Wbar; global_out

@@ -17,6 +17,7 @@ LIB_PATH = os.path.join(_PKG, "librtma.so")
 LIB_CHECKED_PATH = os.path.join(_PKG, "librtma_checked.so")   # built with -DRTMA_BOUNDS: every caller-supplied index checked
 MAX_PARTS = 64
 MAX_LAYERS = 8
+MAX_GROUPS = 1024
 
 EXPORTS = (
     "rtma_create", "rtma_destroy", "rtma_last_error", "rtma_workspace_bytes", "rtma_partition", "rtma_partition_grouped",
@@ -25,7 +26,8 @@ EXPORTS = (
     "rtma_kernel_class_name", "rtma_check", "rtma_partition_static", "rtma_partition_static_error",
     "rtma_local_steps_var", "rtma_aggregate_masked", "rtma_selftest_wait_timeout", "rtma_link_param_count",
     "rtma_link_steps", "rtma_set_workspace_limit", "rtma_local_steps_gathered", "rtma_bounds_checked", "rtma_sample_hop",
-    "rtma_set_dense_aggregation", "rtma_selftest_chunks",
+    "rtma_set_dense_aggregation", "rtma_selftest_chunks", "rtma_grouped_linear", "rtma_grouped_linear_dx",
+    "rtma_grouped_linear_dw", "rtma_group_norm", "rtma_group_norm_grad", "rtma_dropout",
 )
 KERNEL_CLASSES = 21
 
@@ -57,6 +59,17 @@ def decoder_desc(ddims) -> DecoderDesc:
     return dd
 
 
+class NormDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("C", ctypes.c_int32), ("groups", ctypes.c_int32), ("scope", ctypes.c_int32),
+                ("act", ctypes.c_int32), ("eps", ctypes.c_float), ("p", ctypes.c_double), ("seed", ctypes.c_uint64),
+                ("gamma_stride", ctypes.c_int64), ("beta_stride", ctypes.c_int64), ("slope_stride", ctypes.c_int64)]
+
+
+ROW_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+SCOPES = {"row": 0, "part": 1}
+ACTIVATIONS = {"none": 0, "relu": 1, "prelu": 2, "silu": 3}
+
+
 class Taps(ctypes.Structure):
     _fields_ = [("acts", ctypes.c_void_p), ("grads", ctypes.c_void_p), ("step", ctypes.c_int32)]
 
@@ -76,6 +89,15 @@ def load_library(checked: bool = False):
         lib.rtma_param_count.restype = ctypes.c_int64
         lib.rtma_kernel_class_name.restype = ctypes.c_char_p
         lib.rtma_partition_static_error.restype = ctypes.c_char_p
+        vp, i32, i64, u64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64
+        linear = [vp, i32, i64, i32, vp, i32, i32, vp, i64, vp, i64]
+        lib.rtma_grouped_linear.argtypes = linear + [vp, i64, vp, i64, vp]
+        lib.rtma_grouped_linear_dx.argtypes = linear + [vp, i64, vp]
+        lib.rtma_grouped_linear_dw.argtypes = linear + [vp, i64, vp, i64, vp]
+        norm = [vp, ctypes.POINTER(NormDesc), i64, i32, vp, vp, i64]
+        lib.rtma_group_norm.argtypes = norm + [vp, vp, vp, vp, vp, i64, vp, vp]
+        lib.rtma_group_norm_grad.argtypes = norm + [vp, i64, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+        lib.rtma_dropout.argtypes = [vp, i32, i64, i32, vp, i64, vp, vp, i64, ctypes.c_double, u64, vp, i64, vp]
         _libs[path] = lib
     return _libs[path]
 
@@ -387,6 +409,194 @@ class Context:
             _ptr(params), ctypes.c_int32(K), _ptr(loss_out), ctypes.c_int32(record_step), _ptr(grads_out),
             _ptr(emb_out), _ptr(score_out), sarr)
         self._check(st, "rtma_link_steps")
+
+    # ---- operators on the rows of many parts -----------------------------------------
+    def _rows(self, t, name, dtype=None, shape=None):
+        """(pointer, distance between rows) of a matrix whose rows are contiguous."""
+        if dtype is None:
+            if t.dtype not in ROW_TYPES:
+                raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+        elif t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+        if t.device != self.device:
+            raise ValueError(f"{name} must live on {self.device}, got {t.device}")
+        if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
+            raise ValueError(f"{name} must be a matrix{'' if shape is None else ' of ' + str(shape)}, got {tuple(t.shape)}")
+        n, d = t.shape
+        if d > 1 and t.stride(1) != 1:
+            raise ValueError(f"the values of a row of {name} must be adjacent")
+        ld = t.stride(0) if n > 1 else max(t.stride(0), d)
+        if ld < d:
+            raise ValueError(f"the rows of {name} overlap")
+        return t.data_ptr(), ld
+
+    def _parts(self, offsets):
+        """(pointer, number of parts) of the parts' row offsets; None: one part of all rows."""
+        if offsets is None:
+            return None, 1
+        _need(offsets, torch.int64, "offsets", self.device)
+        if offsets.dim() != 1 or offsets.numel() < 2 or not offsets.is_contiguous():
+            raise ValueError("offsets must be a contiguous vector of one more value than there are parts")
+        return offsets.data_ptr(), offsets.numel() - 1
+
+    def _of_parts(self, t, name, dtype, G, shape):
+        """(pointer, distance between parts) of a parameter: [G, *shape], or *shape for one that all parts share."""
+        if t is None:
+            return None, 0
+        _need(t, dtype, name, self.device)
+        stride = 0
+        if t.dim() == len(shape) + 1 and t.shape[0] == G:
+            if G > 1:
+                stride = t.stride(0)
+            t = t[0]
+        if tuple(t.shape) != shape or not t.is_contiguous():
+            raise ValueError(f"{name} must be [{G}, {', '.join(map(str, shape))}] or {list(shape)}, contiguous within a part")
+        return t.data_ptr(), stride
+
+    def _stream(self, stream):
+        return int(torch.cuda.current_stream(self.device).cuda_stream) if stream is None else _stream_handle(stream)
+
+    def grouped_linear(self, X, offsets, W, bias=None, out=None, stream=None):
+        """Y[r] = X[r] W_g + b_g for the rows r of part g: X [n, d_in], W [G, d_in, d_out] (or [d_in, d_out] for all parts),
+        bias [G, d_out] (or [d_out]), offsets [G + 1] int64 on the device (None: one part).  Returns Y [n, d_out]; rows of no
+        part are left as they are in `out` (undefined in a new one)."""
+        x, ldx = self._rows(X, "X")
+        off, G = self._parts(offsets)
+        n, d_in = X.shape
+        d_out = W.shape[-1]
+        w, ws = self._of_parts(W, "W", X.dtype, G, (d_in, d_out))
+        b, bs = self._of_parts(bias, "bias", X.dtype, G, (d_out,))
+        if out is None:
+            out = torch.empty(n, d_out, dtype=X.dtype, device=self.device)
+        y, ldy = self._rows(out, "out", X.dtype, (n, d_out))
+        self._check(self._lib.rtma_grouped_linear(self._h, ROW_TYPES[X.dtype], n, G, off, d_in, d_out, x, ldx, w, ws, b, bs, y, ldy,
+                                                  self._stream(stream)), "rtma_grouped_linear")
+        return out
+
+    def grouped_linear_dx(self, dY, offsets, W, out=None, stream=None):
+        """dX[r] = dY[r] W_g^T: the input gradient of grouped_linear."""
+        g, ldg = self._rows(dY, "dY")
+        off, G = self._parts(offsets)
+        n, d_out = dY.shape
+        d_in = W.shape[-2]
+        w, ws = self._of_parts(W, "W", dY.dtype, G, (d_in, d_out))
+        if out is None:
+            out = torch.empty(n, d_in, dtype=dY.dtype, device=self.device)
+        x, ldx = self._rows(out, "out", dY.dtype, (n, d_in))
+        self._check(self._lib.rtma_grouped_linear_dx(self._h, ROW_TYPES[dY.dtype], n, G, off, d_in, d_out, g, ldg, w, ws, x, ldx,
+                                                     self._stream(stream)), "rtma_grouped_linear_dx")
+        return out
+
+    def grouped_linear_dw(self, X, dY, offsets, shared=False, dw=None, db=None, bias=True, stream=None):
+        """(dW, db) of grouped_linear in float32: dW_g = sum_r X[r]^T dY[r], db_g = sum_r dY[r]; [G, d_in, d_out] and [G, d_out],
+        or summed over all parts without the leading G (shared).  dw, db: where to write them (views of a replica's gradients,
+        for instance).  bias=False: dW alone, db is None."""
+        x, ldx = self._rows(X, "X")
+        n, d_in = X.shape
+        g, ldg = self._rows(dY, "dY", X.dtype)
+        d_out = dY.shape[1]
+        if dY.shape[0] != n:
+            raise ValueError(f"X has {n} rows, dY {dY.shape[0]}")
+        off, G = self._parts(offsets)
+        lead = () if shared else (G,)
+        if dw is None:
+            dw = torch.empty(*lead, d_in, d_out, dtype=torch.float32, device=self.device)
+        if db is None and bias:
+            db = torch.empty(*lead, d_out, dtype=torch.float32, device=self.device)
+        for t, name, rank in ((dw, "dw", 2), (db, "db", 1)):
+            if t is not None and t.dim() != rank + len(lead):
+                raise ValueError(f"{name} has {t.dim()} dimensions with shared={shared}")
+        w, ws = self._of_parts(dw, "dw", torch.float32, G, (d_in, d_out))
+        b, bs = self._of_parts(db, "db", torch.float32, G, (d_out,))
+        self._check(self._lib.rtma_grouped_linear_dw(self._h, ROW_TYPES[X.dtype], n, G, off, d_in, d_out, x, ldx, g, ldg, w, ws, b, bs,
+                                                     self._stream(stream)), "rtma_grouped_linear_dw")
+        return dw, db
+
+    def _norm(self, X, offsets, groups, gamma, beta, slope, scope, act, eps, p, seed, row_ids):
+        if scope not in SCOPES or act not in ACTIVATIONS:
+            raise ValueError(f"scope={scope!r} (of {list(SCOPES)}), act={act!r} (of {list(ACTIVATIONS)})")
+        off, G = self._parts(offsets)
+        n, C = X.shape
+        gm, gs = self._of_parts(gamma, "gamma", torch.float32, G, (C,))
+        bt, bs = self._of_parts(beta, "beta", torch.float32, G, (C,))
+        sl, ss = None, 0
+        if slope is not None:
+            _need(slope, torch.float32, "slope", self.device)
+            if slope.dim() > 1 or slope.numel() not in (1, G):
+                raise ValueError(f"slope must be [{G}] or a single value")
+            sl, ss = slope.data_ptr(), slope.stride(0) if slope.dim() == 1 and slope.numel() > 1 else 0
+        desc = NormDesc(ROW_TYPES[X.dtype], C, int(groups), SCOPES[scope], ACTIVATIONS[act], float(eps), float(p), int(seed) & (2**64 - 1),
+                        gs, bs, ss)
+        return off, G, desc, gm, bt, sl, self._ids(row_ids, n)
+
+    def _ids(self, row_ids, n):
+        if row_ids is None:
+            return None
+        _need(row_ids, torch.int32, "row_ids", self.device)
+        if tuple(row_ids.shape) != (n,) or not row_ids.is_contiguous():
+            raise ValueError(f"row_ids must be {n} contiguous ids")
+        return row_ids.data_ptr()
+
+    def group_norm(self, X, offsets, groups, gamma=None, beta=None, scope="row", act="none", slope=None, eps=1e-5, p=0.0, seed=0,
+                   row_ids=None, out=None, stats=None, stream=None):
+        """dropout(act(gamma_g xhat + beta_g)) over X [n, C], xhat normalised within sets of C / groups neighbouring channels of a
+        row (scope "row") or of all rows of a part ("part").  gamma, beta [G, C] or [C] float32, slope [G] or one value (act
+        "prelu"); dropout as in `dropout`.  Returns (Y, stats [n or G, groups, 2] float32: mean, 1 / std); Y may be X (out=X)."""
+        x, ldx = self._rows(X, "X")
+        off, G, desc, gm, bt, sl, ids = self._norm(X, offsets, groups, gamma, beta, slope, scope, act, eps, p, seed, row_ids)
+        n = X.shape[0]
+        if out is None:
+            out = torch.empty(X.shape, dtype=X.dtype, device=self.device)
+        y, ldy = self._rows(out, "out", X.dtype, tuple(X.shape))
+        shape = (n if scope == "row" else G, int(groups), 2)
+        if stats is None:
+            stats = torch.empty(shape, dtype=torch.float32, device=self.device)
+        st = self._of_parts(stats, "stats", torch.float32, 1, shape)[0]
+        self._check(self._lib.rtma_group_norm(self._h, desc, n, G, off, x, ldx, gm, bt, sl, ids, y, ldy, st, self._stream(stream)),
+                    "rtma_group_norm")
+        return out, stats
+
+    def group_norm_grad(self, X, dY, stats, offsets, groups, gamma=None, beta=None, scope="row", act="none", slope=None, eps=1e-5, p=0.0,
+                        seed=0, row_ids=None, out=None, dgamma=None, dbeta=None, dslope=None, stream=None):
+        """(dX, dgamma, dbeta, dslope) of group_norm from its X, its stats and dY; the parameters' gradients in float32, in the
+        parameters' shape (summed over the parts for a shared one), None for a parameter that is None."""
+        x, ldx = self._rows(X, "X")
+        off, G, desc, gm, bt, sl, ids = self._norm(X, offsets, groups, gamma, beta, slope, scope, act, eps, p, seed, row_ids)
+        n, C = X.shape
+        g, ldg = self._rows(dY, "dY", X.dtype, (n, C))
+        st = self._of_parts(stats, "stats", torch.float32, 1, (n if scope == "row" else G, int(groups), 2))[0]
+        if out is None:
+            out = torch.empty(X.shape, dtype=X.dtype, device=self.device)
+        dx, lddx = self._rows(out, "out", X.dtype, (n, C))
+        new = lambda like: torch.empty(like.shape, dtype=torch.float32, device=self.device)  # noqa: E731
+        dgamma = new(gamma) if dgamma is None and gamma is not None else dgamma
+        dbeta = new(beta) if dbeta is None and beta is not None else dbeta
+        dslope = new(slope) if dslope is None and act == "prelu" else dslope
+        dg, dgs = self._of_parts(dgamma, "dgamma", torch.float32, G, (C,))
+        db, dbs = self._of_parts(dbeta, "dbeta", torch.float32, G, (C,))
+        ds, dss = None, 0
+        if dslope is not None:
+            _need(dslope, torch.float32, "dslope", self.device)
+            if dslope.dim() > 1 or dslope.numel() not in (1, G):
+                raise ValueError(f"dslope must be [{G}] or a single value")
+            ds, dss = dslope.data_ptr(), dslope.stride(0) if dslope.dim() == 1 and dslope.numel() > 1 else 0
+        self._check(self._lib.rtma_group_norm_grad(self._h, desc, n, G, off, x, ldx, g, ldg, st, gm, bt, sl, ids, dx, lddx, dg, dgs, db, dbs,
+                                                   ds, dss, self._stream(stream)), "rtma_group_norm_grad")
+        return out, dgamma, dbeta, dslope
+
+    def dropout(self, X, p, seed, row_ids=None, residual=None, out=None, stream=None):
+        """residual + X * mask / (1 - p) for X [n, d]; the mask is a hash of (seed, row id, column) and is not stored, so the
+        gradient is the same call on dY without the residual.  row_ids [n] int32: the rows' ids (None: their numbers)."""
+        x, ldx = self._rows(X, "X")
+        n, d = X.shape
+        r, ldr = (None, 0) if residual is None else self._rows(residual, "residual", X.dtype, (n, d))
+        ids = self._ids(row_ids, n)
+        if out is None:
+            out = torch.empty(n, d, dtype=X.dtype, device=self.device)
+        y, ldy = self._rows(out, "out", X.dtype, (n, d))
+        self._check(self._lib.rtma_dropout(self._h, ROW_TYPES[X.dtype], n, d, x, ldx, ids, r, ldr, float(p), int(seed) & (2**64 - 1), y, ldy,
+                                           self._stream(stream)), "rtma_dropout")
+        return out
 
     # ---- R2 -------------------------------------------------------------------------
     def aggregate(self, params, global_out=None, stream=None):

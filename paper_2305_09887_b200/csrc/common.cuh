@@ -40,6 +40,8 @@ struct rtma_ctx {
     char* arena = nullptr;        // device scratch
     size_t arena_bytes = 0;
     size_t arena_limit = 0;       // 0: none; else the arena never grows beyond this many bytes
+    bool arena_captured = false;  // a captured graph uses the arena: it is kept, not freed, when the arena grows
+    std::vector<char*> kept_arenas;
     // the streams of the last local-training call and an event recorded at the end of each
     std::vector<cudaStream_t> trained_streams;
     std::vector<cudaEvent_t> trained_events;
@@ -182,7 +184,7 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // (first offender: site, index, limit) in a word of the translation unit, the access is skipped, and
 // the next rtma_check returns RTMA_ERR_BOUNDS: nothing traps and nothing is read or written out of
 // range.  Sites: 1 column id of the input graph, 2 part id, 3 local id, 4 permutation entry, 5 column
-// id of an induced subgraph, 6 label, 7 pair end point.
+// id of an induced subgraph, 6 label, 7 pair end point, 8 part offset.
 #ifdef RTMA_BOUNDS
 #ifdef __CUDACC__
 static __device__ long long rtma_bounds_record[4];  // site (0: none), index, limit

@@ -2,7 +2,7 @@
 // partition and induced-subgraph stages.
 #include <cstdlib>
 
-#include "common.cuh"
+#include "rows.cuh"
 
 extern "C" int32_t rtma_create(rtma_ctx** out, int32_t device, size_t workspace_bytes) {
     if (!out) return RTMA_ERR_INVALID_ARG;
@@ -42,6 +42,7 @@ extern "C" int32_t rtma_destroy(rtma_ctx* ctx) {
     cudaSetDevice(ctx->device);
     cudaDeviceSynchronize();
     if (ctx->arena) cudaFree(ctx->arena);
+    for (char* a : ctx->kept_arenas) cudaFree(a);
     if (ctx->host_block) cudaFree(ctx->host_block);
     if (ctx->host_cols) cudaFree(ctx->host_cols);
     if (ctx->keep_bits) cudaFree(ctx->keep_bits);
@@ -92,7 +93,7 @@ extern "C" int32_t rtma_check(rtma_ctx* ctx) {
 #ifdef RTMA_BOUNDS
     {
         static const char* const site_names[] = {"", "column id of the input graph", "part id", "local id", "permutation entry",
-                                                 "column id of an induced subgraph", "label", "pair end point"};
+                                                 "column id of an induced subgraph", "label", "pair end point", "part offset"};
         long long first[3] = {0, 0, 0};
         bool any = false;
         for (rtma_bounds_reader r : bounds_readers()) {
@@ -104,7 +105,7 @@ extern "C" int32_t rtma_check(rtma_ctx* ctx) {
         }
         if (any)
             return rtma_fail(ctx, RTMA_ERR_BOUNDS, "index out of range in the caller's data: %s %lld outside [0, %lld)",
-                             first[0] >= 1 && first[0] <= 7 ? site_names[first[0]] : "index", first[1], first[2]);
+                             first[0] >= 1 && first[0] <= 8 ? site_names[first[0]] : "index", first[1], first[2]);
     }
 #endif
     int word[2] = {0, 0};
@@ -174,6 +175,34 @@ int32_t mark_trained(rtma_ctx* ctx, const std::vector<cudaStream_t>& streams) {
     return RTMA_OK;
 }
 
+int32_t stream_captures(rtma_ctx* ctx, cudaStream_t stream, bool* captures) {
+    cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
+    RTMA_CUDA(ctx, cudaStreamIsCapturing(stream, &st));
+    *captures = st != cudaStreamCaptureStatusNone;
+    return RTMA_OK;
+}
+
+int32_t prepare_row_call(rtma_ctx* ctx, size_t scratch_bytes, cudaStream_t stream) {
+    bool captures = false;
+    RTMA_TRY(stream_captures(ctx, stream, &captures));
+    if (!captures) {
+        RTMA_TRY(order_after_training(ctx, stream));
+        return scratch_bytes ? rtma_reserve(ctx, scratch_bytes) : RTMA_OK;
+    }
+    if (scratch_bytes > ctx->arena_bytes)
+        return rtma_fail(ctx, RTMA_ERR_WORKSPACE, "%zu bytes of scratch needed inside a stream capture, %zu reserved: make the call once before the capture",
+                         scratch_bytes, ctx->arena_bytes);
+    if (scratch_bytes) ctx->arena_captured = true;
+    return RTMA_OK;
+}
+
+int32_t check_parts(rtma_ctx* ctx, const char* who, int64_t n, int32_t G, const int64_t* offsets) {
+    if (n < 0 || n >= (int64_t(1) << 31)) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: n=%lld outside [0, 2^31)", who, (long long)n);
+    if (G < 1 || G > RTMA_MAX_GROUPS) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: G=%d outside [1,%d]", who, G, RTMA_MAX_GROUPS);
+    if (!offsets && G != 1) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: %d parts without offsets", who, G);
+    return RTMA_OK;
+}
+
 int32_t rtma_reserve(rtma_ctx* ctx, size_t bytes) {
     if (bytes <= ctx->arena_bytes) return RTMA_OK;
     if (ctx->arena_limit && bytes > ctx->arena_limit)
@@ -182,7 +211,16 @@ int32_t rtma_reserve(rtma_ctx* ctx, size_t bytes) {
     RTMA_CUDA(ctx, cudaSetDevice(ctx->device));
     RTMA_CUDA(ctx, cudaDeviceSynchronize());
     if (ctx->arena) {
-        RTMA_CUDA(ctx, cudaFree(ctx->arena));
+        if (ctx->arena_captured) {  // a graph replayed later still writes there
+            try {
+                ctx->kept_arenas.push_back(ctx->arena);
+            } catch (...) {
+                return rtma_fail(ctx, RTMA_ERR_WORKSPACE, "no host memory");
+            }
+        } else {
+            RTMA_CUDA(ctx, cudaFree(ctx->arena));
+        }
+        ctx->arena_captured = false;
         ctx->arena = nullptr;
         ctx->arena_bytes = 0;
     }

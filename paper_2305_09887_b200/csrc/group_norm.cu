@@ -1,0 +1,784 @@
+// Group norm over channels that lie last, with the activation and dropout behind it, and its gradient.
+//   xhat = (x - mean) * rstd, u = gamma xhat + beta, h = act(u), y = dropout(h)
+// mean and rstd = 1 / sqrt(var + eps) are those of a set of C / groups neighbouring channels, of one row (scope 0) or of all rows
+// of a part (scope 1); gamma, beta and the PReLU slope are the part's own (or shared).  Backward, with m values in a set:
+//   dh = dropout(dy), du = dh act'(u), dgamma = sum du xhat, dbeta = sum du, dslope = sum_{u <= 0} dh u,
+//   dx = rstd (gamma du - (S1 + xhat S2) / m),  S1 = sum gamma du, S2 = sum gamma du xhat over the set.
+// A thread keeps eight neighbouring channels and walks down the rows of a tile (a run of rows of one part); what is summed over
+// rows is left per tile and added up in a fixed order by a second kernel, so results do not depend on which block ran when.
+#include "rows.cuh"
+
+RTMA_BOUNDS_TU()
+
+namespace {
+
+constexpr int NORM_THREADS = 256;
+constexpr int NORM_MAX_CHANNELS = 8 * NORM_THREADS;
+
+struct NormArgs {
+    const int64_t* offsets;
+    int64_t n;
+    int G, C, groups, per_set, units, rows_at_once;  // per_set = C / groups; units of eight channels; rows a block works on at a time
+    int tile_rows;
+    int64_t tiles;  // at most so many
+    int act;
+    float eps;
+    const void *X, *dY;
+    void* Y;  // forward: y; backward: dx
+    int64_t ldx, lddy, ldy;
+    bool vx, vdy, vy;
+    const float *gamma, *beta, *slope;
+    int64_t gamma_stride, beta_stride, slope_stride;
+    DropArgs drop;
+    float* stats;    // [row or part][groups][2]
+    float2* pieces;  // part scope, forward: [tile][groups] (mean, sum of squared differences)
+    float* partial;  // backward: [tile][2 C + 1]: sums of du, of du xhat, of the slope's gradient
+    float* sums;     // backward: [part][2 C + 1]
+    float *dgamma, *dbeta, *dslope;
+    int64_t dgamma_stride, dbeta_stride, dslope_stride;
+};
+
+__device__ __forceinline__ float sigmoid(float u) { return __fdividef(1.f, 1.f + __expf(-u)); }
+
+__device__ __forceinline__ void activate_eight(int act, float slope, float (&u)[8]) {
+    if (act == RTMA_ACT_RELU || act == RTMA_ACT_PRELU) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) u[j] = u[j] <= 0.f ? (act == RTMA_ACT_PRELU ? slope * u[j] : 0.f) : u[j];  // NaN stays NaN
+    } else if (act == RTMA_ACT_SILU) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) u[j] = __fdividef(u[j], 1.f + __expf(-u[j]));
+    }
+}
+// d (holding dh) becomes du; returns the slope's gradient
+__device__ __forceinline__ float activate_back_eight(int act, float slope, const float (&u)[8], float (&d)[8]) {
+    float ds = 0.f;
+    if (act == RTMA_ACT_RELU) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) d[j] = u[j] > 0.f ? d[j] : 0.f;
+    } else if (act == RTMA_ACT_PRELU) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (!(u[j] > 0.f)) {
+                ds += d[j] * u[j];
+                d[j] *= slope;
+            }
+        }
+    } else if (act == RTMA_ACT_SILU) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float g = sigmoid(u[j]);
+            d[j] *= g * (1.f + u[j] * (1.f - g));
+        }
+    }
+    return ds;
+}
+
+// A thread's place in a block and its channels' parameters.
+struct Lane {
+    int u, y, valid;  // unit, row within those worked on at a time, channels that exist
+    bool active;
+    __device__ __forceinline__ explicit Lane(const NormArgs& a) {
+        y = threadIdx.x / a.units;
+        u = threadIdx.x - y * a.units;
+        active = y < a.rows_at_once;
+        valid = active ? min(8, a.C - 8 * u) : 0;
+    }
+};
+__device__ __forceinline__ void load_params(const float* p, int64_t stride, int part, int u, int valid, float missing, float (&v)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = p && j < valid ? __ldg(p + part * stride + 8 * u + j) : (j < valid ? missing : 0.f);
+}
+
+// The lanes that share one set's sum: a power of two, so many that a block's threads cover `sets` sets.
+__device__ __forceinline__ int lanes_per_set(int per_set, int sets) {
+    int l = 32;
+    while (l > 1 && (l > per_set || l * sets > NORM_THREADS)) l >>= 1;
+    return l;
+}
+__device__ __forceinline__ float lane_sum(float x, int lanes) {
+    for (int o = lanes >> 1; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
+
+// ---- statistics of a row ---------------------------------------------------------------------------
+__device__ __forceinline__ int row_pitch(const NormArgs& a) { return a.units * 8; }
+
+template <class T>
+__global__ void __launch_bounds__(NORM_THREADS) norm_rows_kernel(const NormArgs a) {
+    extern __shared__ float shared[];
+    __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
+    wait_for_kernel_before();
+    number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums);
+    const int pitch = row_pitch(a);
+    float* vals = shared;                                                        // [rows_at_once][pitch]
+    float2* stat = reinterpret_cast<float2*>(vals + a.rows_at_once * pitch);     // [rows_at_once][groups]
+    const Lane at(a);
+    const int pairs = a.rows_at_once * a.groups, L = lanes_per_set(a.per_set, pairs), sets_at_once = NORM_THREADS / L;
+    const T* X = static_cast<const T*>(a.X);
+    T* Y = static_cast<T*>(a.Y);
+    for (int tile = blockIdx.x; tile < tile_start[a.G]; tile += gridDim.x) {
+        const int part = part_of_tile(tile_start, a.G, tile);
+        int64_t begin, end;
+        part_rows(a.offsets, a.n, part, begin, end);
+        begin += (int64_t)(tile - tile_start[part]) * a.tile_rows;
+        end = min(end, begin + a.tile_rows);
+        float gam[8], bet[8];
+        load_params(a.gamma, a.gamma_stride, part, at.u, at.valid, 1.f, gam);
+        load_params(a.beta, a.beta_stride, part, at.u, at.valid, 0.f, bet);
+        const float slope = a.slope ? __ldg(a.slope + part * a.slope_stride) : 0.f;
+        for (int64_t r0 = begin; r0 < end; r0 += a.rows_at_once) {
+            const int64_t r = r0 + at.y;
+            const bool here = at.active && r < end;
+            float v[8];
+            if (here) {
+                Eight<T> x;
+                x.load(X + r * a.ldx + 8 * at.u, at.valid, a.vx);
+                x.values(v);
+                float4* to = reinterpret_cast<float4*>(vals + at.y * pitch + 8 * at.u);
+                to[0] = make_float4(v[0], v[1], v[2], v[3]);
+                to[1] = make_float4(v[4], v[5], v[6], v[7]);
+            }
+            __syncthreads();
+            for (int s0 = 0; s0 < pairs; s0 += sets_at_once) {  // pair = row, set
+                const int pair = s0 + threadIdx.x / L, l = threadIdx.x % L;
+                const int y = pair / a.groups, set = pair - y * a.groups;
+                const bool ok = pair < pairs && r0 + y < end;
+                const float* p = vals + y * pitch + set * a.per_set;
+                float s = 0.f;
+                if (ok) for (int i = l; i < a.per_set; i += L) s += p[i];
+                const float mean = lane_sum(s, L) / (float)a.per_set;
+                s = 0.f;
+                if (ok) for (int i = l; i < a.per_set; i += L) s += (p[i] - mean) * (p[i] - mean);
+                s = lane_sum(s, L);
+                if (ok && l == 0) {
+                    const float2 st = make_float2(mean, 1.f / sqrtf(s / (float)a.per_set + a.eps));
+                    stat[pair] = st;
+                    if (a.stats) *reinterpret_cast<float2*>(a.stats + 2 * ((r0 + y) * a.groups + set)) = st;
+                }
+            }
+            __syncthreads();
+            if (here) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if (j < at.valid) {
+                        const float2 st = stat[at.y * a.groups + (8 * at.u + j) / a.per_set];
+                        v[j] = fmaf((v[j] - st.x) * st.y, gam[j], bet[j]);
+                    }
+                }
+                activate_eight(a.act, slope, v);
+                if (a.drop.threshold) drop_eight(a.drop, a.drop.ids ? (uint32_t)__ldg(a.drop.ids + r) : (uint32_t)r, at.u, v);
+                store_eight(Y + r * a.ldy + 8 * at.u, v, at.valid, a.vy);
+            }
+        }
+    }
+}
+
+// dh -> du, xhat and u of eight channels; returns the slope's gradient
+template <class T>
+__device__ __forceinline__ float back_eight(const NormArgs& a, int64_t r, int u, int valid, const float (&mean)[8], const float (&rstd)[8],
+                                            const float (&gam)[8], const float (&bet)[8], float slope, float (&xhat)[8], float (&du)[8]) {
+    Eight<T> x, d;
+    x.load(static_cast<const T*>(a.X) + r * a.ldx + 8 * u, valid, a.vx);
+    d.load(static_cast<const T*>(a.dY) + r * a.lddy + 8 * u, valid, a.vdy);
+    x.values(xhat);
+    d.values(du);
+    if (a.drop.threshold) drop_eight(a.drop, a.drop.ids ? (uint32_t)__ldg(a.drop.ids + r) : (uint32_t)r, u, du);
+    float pre[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        xhat[j] = (xhat[j] - mean[j]) * rstd[j];
+        pre[j] = fmaf(xhat[j], gam[j], bet[j]);
+    }
+    return activate_back_eight(a.act, slope, pre, du);
+}
+
+// Sums over a block's rows of its channels' (du, du xhat) and of the slope's gradient, written to the tile's slot.
+__device__ __forceinline__ void leave_sums(const NormArgs& a, const Lane& at, int tile, float (&sb)[8], float (&sg)[8], float ds, float* shared) {
+    float* red = shared;  // [thread][8], one kind after the other
+    const int threads = a.rows_at_once * a.units;
+    int top = 1;
+    while (top < a.rows_at_once) top <<= 1;
+    float* out = a.partial + (int64_t)tile * (2 * a.C + 1);
+#pragma unroll
+    for (int kind = 0; kind < 2; ++kind) {
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) red[j * NORM_THREADS + threadIdx.x] = kind == 0 ? sb[j] : sg[j];
+        for (int h = top >> 1; h > 0; h >>= 1) {
+            __syncthreads();
+            if (at.active && at.y < h && at.y + h < a.rows_at_once) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) red[j * NORM_THREADS + threadIdx.x] += red[j * NORM_THREADS + threadIdx.x + h * a.units];
+            }
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < a.C; c += NORM_THREADS) out[kind * a.C + c] = red[(c & 7) * NORM_THREADS + (c >> 3)];
+    }
+    __syncthreads();
+    red[threadIdx.x] = (int)threadIdx.x < threads ? ds : 0.f;
+    for (int h = NORM_THREADS / 2; h > 0; h >>= 1) {
+        __syncthreads();
+        if ((int)threadIdx.x < h) red[threadIdx.x] += red[threadIdx.x + h];
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) out[2 * a.C] = red[0];
+    __syncthreads();
+}
+
+template <class T>
+__global__ void __launch_bounds__(NORM_THREADS) norm_rows_grad_kernel(const NormArgs a) {
+    extern __shared__ float shared[];
+    __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
+    wait_for_kernel_before();
+    number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums);
+    const int pitch = row_pitch(a);
+    float2* vals = reinterpret_cast<float2*>(shared);                    // [rows_at_once][pitch] (gamma du, gamma du xhat)
+    float2* stat = vals + (NORM_THREADS * 8);                            // [rows_at_once][groups]
+    const Lane at(a);
+    const int pairs = a.rows_at_once * a.groups, L = lanes_per_set(a.per_set, pairs), sets_at_once = NORM_THREADS / L;
+    T* Y = static_cast<T*>(a.Y);
+    for (int tile = blockIdx.x; tile < tile_start[a.G]; tile += gridDim.x) {
+        const int part = part_of_tile(tile_start, a.G, tile);
+        int64_t begin, end;
+        part_rows(a.offsets, a.n, part, begin, end);
+        begin += (int64_t)(tile - tile_start[part]) * a.tile_rows;
+        end = min(end, begin + a.tile_rows);
+        float gam[8], bet[8], sb[8], sg[8], ds = 0.f;
+        load_params(a.gamma, a.gamma_stride, part, at.u, at.valid, 1.f, gam);
+        load_params(a.beta, a.beta_stride, part, at.u, at.valid, 0.f, bet);
+        const float slope = a.slope ? __ldg(a.slope + part * a.slope_stride) : 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sb[j] = sg[j] = 0.f;
+        for (int64_t r0 = begin; r0 < end; r0 += a.rows_at_once) {
+            const int64_t r = r0 + at.y;
+            const bool here = at.active && r < end;
+            float xhat[8], du[8], rstd[8];
+            if (here) {
+                float mean[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float2 st = j < at.valid ? *reinterpret_cast<const float2*>(a.stats + 2 * (r * a.groups + (8 * at.u + j) / a.per_set)) : make_float2(0.f, 0.f);
+                    mean[j] = st.x;
+                    rstd[j] = st.y;
+                }
+                ds += back_eight<T>(a, r, at.u, at.valid, mean, rstd, gam, bet, slope, xhat, du);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    sb[j] += du[j];
+                    sg[j] = fmaf(du[j], xhat[j], sg[j]);
+                    du[j] *= gam[j];
+                    vals[at.y * pitch + 8 * at.u + j] = make_float2(du[j], du[j] * xhat[j]);
+                }
+            }
+            __syncthreads();
+            for (int s0 = 0; s0 < pairs; s0 += sets_at_once) {
+                const int pair = s0 + threadIdx.x / L, l = threadIdx.x % L;
+                const int y = pair / a.groups, set = pair - y * a.groups;
+                const bool ok = pair < pairs && r0 + y < end;
+                const float2* p = vals + y * pitch + set * a.per_set;
+                float s1 = 0.f, s2 = 0.f;
+                if (ok) {
+                    for (int i = l; i < a.per_set; i += L) {
+                        s1 += p[i].x;
+                        s2 += p[i].y;
+                    }
+                }
+                s1 = lane_sum(s1, L);
+                s2 = lane_sum(s2, L);
+                if (ok && l == 0) stat[pair] = make_float2(s1 / (float)a.per_set, s2 / (float)a.per_set);
+            }
+            __syncthreads();
+            if (here) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if (j < at.valid) {
+                        const float2 st = stat[at.y * a.groups + (8 * at.u + j) / a.per_set];
+                        du[j] = rstd[j] * (du[j] - st.x - xhat[j] * st.y);
+                    }
+                }
+                store_eight(Y + r * a.ldy + 8 * at.u, du, at.valid, a.vy);
+            }
+        }
+        leave_sums(a, at, tile, sb, sg, ds, shared);
+    }
+}
+
+// ---- statistics of a part --------------------------------------------------------------------------
+// (mean, sum of squared differences) of two disjoint samples joined (Chan, Golub and LeVeque)
+__device__ __forceinline__ void join_moments(float& mean, float& m2, float n, float mean_b, float m2_b, float n_b) {
+    const float d = mean_b - mean, share = n_b / (n + n_b);
+    mean += d * share;
+    m2 += m2_b + d * d * n * share;
+}
+
+// Mean and sum of squared differences of every set within a tile.
+template <class T>
+__global__ void __launch_bounds__(NORM_THREADS) norm_stats_kernel(const NormArgs a) {
+    __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
+    __shared__ float s_mean[8 * NORM_THREADS], s_m2[8 * NORM_THREADS], s_count[NORM_THREADS];
+    wait_for_kernel_before();
+    number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums);
+    const Lane at(a);
+    const T* X = static_cast<const T*>(a.X);
+    const int L = lanes_per_set(a.per_set, a.groups), sets_at_once = NORM_THREADS / L;
+    constexpr int BATCH = 4;  // rows in flight
+    for (int tile = blockIdx.x; tile < tile_start[a.G]; tile += gridDim.x) {
+        const int part = part_of_tile(tile_start, a.G, tile);
+        int64_t begin, end;
+        part_rows(a.offsets, a.n, part, begin, end);
+        begin += (int64_t)(tile - tile_start[part]) * a.tile_rows;
+        end = min(end, begin + a.tile_rows);
+        float mean[8], m2[8], count = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) mean[j] = m2[j] = 0.f;
+        if (at.active) {
+            for (int64_t r = begin + at.y; r < end; r += BATCH * a.rows_at_once) {
+                Eight<T> x[BATCH];
+                int rows = 0;
+#pragma unroll
+                for (int b = 0; b < BATCH; ++b) {
+                    const int64_t row = r + b * a.rows_at_once;
+                    const bool ok = row < end;
+                    x[b].load(X + (ok ? row : r) * a.ldx + 8 * at.u, at.valid, a.vx);
+                    rows += ok;
+                }
+                // moments of the batch about its own mean, then joined to the thread's
+                const float nb = (float)rows, inv = 1.f / nb, share = nb / (count + nb), weight = count * share;
+                float v[BATCH][8];
+#pragma unroll
+                for (int b = 0; b < BATCH; ++b) x[b].values(v[b]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    float s = v[0][j];
+#pragma unroll
+                    for (int b = 1; b < BATCH; ++b) s += b < rows ? v[b][j] : 0.f;
+                    s *= inv;
+                    float q = 0.f;
+#pragma unroll
+                    for (int b = 0; b < BATCH; ++b) {
+                        const float d = b < rows ? v[b][j] - s : 0.f;
+                        q = fmaf(d, d, q);
+                    }
+                    const float d = s - mean[j];
+                    mean[j] = fmaf(d, share, mean[j]);
+                    m2[j] += fmaf(d * d, weight, q);
+                }
+                count += nb;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            s_mean[j * NORM_THREADS + threadIdx.x] = mean[j];
+            s_m2[j * NORM_THREADS + threadIdx.x] = m2[j];
+        }
+        s_count[threadIdx.x] = count;
+        int top = 1;
+        while (top < a.rows_at_once) top <<= 1;
+        for (int h = top >> 1; h > 0; h >>= 1) {
+            __syncthreads();
+            const int other = threadIdx.x + h * a.units;
+            float n = 0.f, nb = 0.f;
+            if (at.active && at.y < h && at.y + h < a.rows_at_once) {
+                n = s_count[threadIdx.x];
+                nb = s_count[other];
+                if (nb > 0.f) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        join_moments(s_mean[j * NORM_THREADS + threadIdx.x], s_m2[j * NORM_THREADS + threadIdx.x], n,
+                                     s_mean[j * NORM_THREADS + other], s_m2[j * NORM_THREADS + other], nb);
+                }
+                s_count[threadIdx.x] = n + nb;
+            }
+        }
+        __syncthreads();
+        const float rows = (float)(end - begin);
+        for (int s0 = 0; s0 < a.groups; s0 += sets_at_once) {
+            const int set = s0 + threadIdx.x / L, l = threadIdx.x % L;
+            const bool ok = set < a.groups;
+            const int c0 = set * a.per_set;
+            const float first = ok ? s_mean[(c0 & 7) * NORM_THREADS + (c0 >> 3)] : 0.f;
+            float s = 0.f;
+            if (ok) for (int c = c0 + l; c < c0 + a.per_set; c += L) s += s_mean[(c & 7) * NORM_THREADS + (c >> 3)] - first;
+            const float m = first + lane_sum(s, L) / (float)a.per_set;
+            float q = 0.f;
+            if (ok) {
+                for (int c = c0 + l; c < c0 + a.per_set; c += L) {
+                    const float d = s_mean[(c & 7) * NORM_THREADS + (c >> 3)] - m;
+                    q += s_m2[(c & 7) * NORM_THREADS + (c >> 3)] + rows * d * d;
+                }
+            }
+            q = lane_sum(q, L);
+            if (ok && l == 0) a.pieces[(int64_t)tile * a.groups + set] = make_float2(m, q);
+        }
+        __syncthreads();
+    }
+}
+
+// The tiles' moments of every (part, set) joined: a warp each.
+__global__ void __launch_bounds__(NORM_THREADS) norm_join_kernel(const NormArgs a) {
+    __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
+    wait_for_kernel_before();
+    number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums);
+    const int lane = threadIdx.x & 31;
+    const int job = (int)(((int64_t)blockIdx.x * NORM_THREADS + threadIdx.x) >> 5);
+    if (job >= a.G * a.groups) return;
+    const int part = job / a.groups, set = job - part * a.groups;
+    int64_t begin, end;
+    part_rows(a.offsets, a.n, part, begin, end);
+    const int t0 = tile_start[part], t1 = tile_start[part + 1];
+    float2 st = make_float2(0.f, 1.f / sqrtf(a.eps));
+    if (t1 > t0) {
+        const float total = (float)(end - begin);
+        const float2* p = a.pieces + set;
+        const float first = p[(int64_t)t0 * a.groups].x;
+        float s = 0.f;
+        for (int t = t0 + lane; t < t1; t += 32) {
+            const float rows = (float)min((int64_t)a.tile_rows, end - begin - (int64_t)(t - t0) * a.tile_rows);
+            s += rows * (p[(int64_t)t * a.groups].x - first);
+        }
+        const float mean = first + lane_sum(s, 32) / total;
+        float q = 0.f;
+        for (int t = t0 + lane; t < t1; t += 32) {
+            const float rows = (float)min((int64_t)a.tile_rows, end - begin - (int64_t)(t - t0) * a.tile_rows);
+            const float2 v = p[(int64_t)t * a.groups];
+            const float d = v.x - mean;
+            q += v.y + rows * (float)a.per_set * d * d;
+        }
+        q = lane_sum(q, 32);
+        st = make_float2(mean, 1.f / sqrtf(q / (total * (float)a.per_set) + a.eps));
+    }
+    if (lane == 0) *reinterpret_cast<float2*>(a.stats + 2 * ((int64_t)part * a.groups + set)) = st;
+}
+
+__device__ __forceinline__ void load_part_stats(const NormArgs& a, int part, const Lane& at, float (&mean)[8], float (&rstd)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float2 st = j < at.valid ? *reinterpret_cast<const float2*>(a.stats + 2 * ((int64_t)part * a.groups + (8 * at.u + j) / a.per_set)) : make_float2(0.f, 0.f);
+        mean[j] = st.x;
+        rstd[j] = st.y;
+    }
+}
+
+template <class T>
+__global__ void __launch_bounds__(NORM_THREADS) norm_apply_kernel(const NormArgs a) {
+    __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
+    wait_for_kernel_before();
+    number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums);
+    const Lane at(a);
+    if (!at.active) return;
+    const T* X = static_cast<const T*>(a.X);
+    T* Y = static_cast<T*>(a.Y);
+    for (int tile = blockIdx.x; tile < tile_start[a.G]; tile += gridDim.x) {
+        const int part = part_of_tile(tile_start, a.G, tile);
+        int64_t begin, end;
+        part_rows(a.offsets, a.n, part, begin, end);
+        begin += (int64_t)(tile - tile_start[part]) * a.tile_rows;
+        end = min(end, begin + a.tile_rows);
+        float gam[8], bet[8], mean[8], rstd[8];
+        load_params(a.gamma, a.gamma_stride, part, at.u, at.valid, 1.f, gam);
+        load_params(a.beta, a.beta_stride, part, at.u, at.valid, 0.f, bet);
+        load_part_stats(a, part, at, mean, rstd);
+        const float slope = a.slope ? __ldg(a.slope + part * a.slope_stride) : 0.f;
+        for (int64_t r = begin + at.y; r < end; r += a.rows_at_once) {
+            Eight<T> x;
+            x.load(X + r * a.ldx + 8 * at.u, at.valid, a.vx);
+            float v[8];
+            x.values(v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = fmaf((v[j] - mean[j]) * rstd[j], gam[j], bet[j]);
+            activate_eight(a.act, slope, v);
+            if (a.drop.threshold) drop_eight(a.drop, a.drop.ids ? (uint32_t)__ldg(a.drop.ids + r) : (uint32_t)r, at.u, v);
+            store_eight(Y + r * a.ldy + 8 * at.u, v, at.valid, a.vy);
+        }
+    }
+}
+
+template <class T>
+__global__ void __launch_bounds__(NORM_THREADS) norm_grad_sums_kernel(const NormArgs a) {
+    __shared__ float shared[8 * NORM_THREADS];
+    __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
+    wait_for_kernel_before();
+    number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums);
+    const Lane at(a);
+    for (int tile = blockIdx.x; tile < tile_start[a.G]; tile += gridDim.x) {
+        const int part = part_of_tile(tile_start, a.G, tile);
+        int64_t begin, end;
+        part_rows(a.offsets, a.n, part, begin, end);
+        begin += (int64_t)(tile - tile_start[part]) * a.tile_rows;
+        end = min(end, begin + a.tile_rows);
+        float gam[8], bet[8], mean[8], rstd[8], sb[8], sg[8], ds = 0.f;
+        load_params(a.gamma, a.gamma_stride, part, at.u, at.valid, 1.f, gam);
+        load_params(a.beta, a.beta_stride, part, at.u, at.valid, 0.f, bet);
+        load_part_stats(a, part, at, mean, rstd);
+        const float slope = a.slope ? __ldg(a.slope + part * a.slope_stride) : 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sb[j] = sg[j] = 0.f;
+        if (at.active) {
+            for (int64_t r = begin + at.y; r < end; r += a.rows_at_once) {
+                float xhat[8], du[8];
+                ds += back_eight<T>(a, r, at.u, at.valid, mean, rstd, gam, bet, slope, xhat, du);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    sb[j] += du[j];
+                    sg[j] = fmaf(du[j], xhat[j], sg[j]);
+                }
+            }
+        }
+        leave_sums(a, at, tile, sb, sg, ds, shared);
+    }
+}
+
+template <class T>
+__global__ void __launch_bounds__(NORM_THREADS) norm_grad_apply_kernel(const NormArgs a) {
+    __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
+    __shared__ float2 of_set[NORM_MAX_CHANNELS];
+    wait_for_kernel_before();
+    number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums);
+    const Lane at(a);
+    T* Y = static_cast<T*>(a.Y);
+    const int L = lanes_per_set(a.per_set, a.groups), sets_at_once = NORM_THREADS / L;
+    for (int tile = blockIdx.x; tile < tile_start[a.G]; tile += gridDim.x) {
+        const int part = part_of_tile(tile_start, a.G, tile);
+        int64_t begin, end;
+        part_rows(a.offsets, a.n, part, begin, end);
+        const float inv = 1.f / ((float)(end - begin) * (float)a.per_set);
+        begin += (int64_t)(tile - tile_start[part]) * a.tile_rows;
+        end = min(end, begin + a.tile_rows);
+        const float* sums = a.sums + (int64_t)part * (2 * a.C + 1);
+        __syncthreads();
+        for (int s0 = 0; s0 < a.groups; s0 += sets_at_once) {
+            const int set = s0 + threadIdx.x / L, l = threadIdx.x % L;
+            float s1 = 0.f, s2 = 0.f;
+            if (set < a.groups) {
+                for (int c = set * a.per_set + l; c < (set + 1) * a.per_set; c += L) {
+                    const float g = a.gamma ? __ldg(a.gamma + part * a.gamma_stride + c) : 1.f;
+                    s1 += g * sums[c];
+                    s2 += g * sums[a.C + c];
+                }
+            }
+            s1 = lane_sum(s1, L);
+            s2 = lane_sum(s2, L);
+            if (set < a.groups && l == 0) of_set[set] = make_float2(s1 * inv, s2 * inv);
+        }
+        __syncthreads();
+        float gam[8], bet[8], mean[8], rstd[8], m1[8], m2[8];
+        load_params(a.gamma, a.gamma_stride, part, at.u, at.valid, 1.f, gam);
+        load_params(a.beta, a.beta_stride, part, at.u, at.valid, 0.f, bet);
+        load_part_stats(a, part, at, mean, rstd);
+        const float slope = a.slope ? __ldg(a.slope + part * a.slope_stride) : 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float2 s = j < at.valid ? of_set[(8 * at.u + j) / a.per_set] : make_float2(0.f, 0.f);
+            m1[j] = s.x;
+            m2[j] = s.y;
+        }
+        if (at.active) {
+            for (int64_t r = begin + at.y; r < end; r += a.rows_at_once) {
+                float xhat[8], du[8];
+                back_eight<T>(a, r, at.u, at.valid, mean, rstd, gam, bet, slope, xhat, du);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) du[j] = rstd[j] * (fmaf(gam[j], du[j], -m1[j]) - xhat[j] * m2[j]);
+                store_eight(Y + r * a.ldy + 8 * at.u, du, at.valid, a.vy);
+            }
+        }
+    }
+}
+
+// The tiles' sums of every part added up in order: a block of 32 columns by 8 shares of the tiles.
+__global__ void __launch_bounds__(NORM_THREADS) norm_reduce_kernel(const NormArgs a) {
+    __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
+    __shared__ float red[8][33];
+    wait_for_kernel_before();
+    number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums);
+    const int width = 2 * a.C + 1, lane = threadIdx.x & 31, share = threadIdx.x >> 5;
+    const int c = blockIdx.x * 32 + lane, part = blockIdx.y;
+    float s = 0.f;
+    if (c < width)
+        for (int t = tile_start[part] + share; t < tile_start[part + 1]; t += 8) s += a.partial[(int64_t)t * width + c];
+    red[share][lane] = s;
+    __syncthreads();
+    if (share == 0 && c < width) {
+        for (int k = 1; k < 8; ++k) s += red[k][lane];
+        a.sums[(int64_t)part * width + c] = s;
+        if (c < a.C) {
+            if (a.dbeta && (a.dbeta_stride || a.G == 1)) a.dbeta[part * a.dbeta_stride + c] = s;
+        } else if (c < 2 * a.C) {
+            if (a.dgamma && (a.dgamma_stride || a.G == 1)) a.dgamma[part * a.dgamma_stride + c - a.C] = s;
+        } else if (a.dslope && (a.dslope_stride || a.G == 1)) {
+            a.dslope[part * a.dslope_stride] = s;
+        }
+    }
+}
+
+// Gradients of parameters that all parts share: the parts' sums added up in order.
+__global__ void __launch_bounds__(NORM_THREADS) norm_reduce_parts_kernel(const NormArgs a) {
+    wait_for_kernel_before();
+    const int width = 2 * a.C + 1, c = blockIdx.x * NORM_THREADS + threadIdx.x;
+    if (c >= width) return;
+    float* to = c < a.C ? (a.dbeta && !a.dbeta_stride ? a.dbeta + c : nullptr)
+                : c < 2 * a.C ? (a.dgamma && !a.dgamma_stride ? a.dgamma + c - a.C : nullptr)
+                              : (a.dslope && !a.dslope_stride ? a.dslope : nullptr);
+    if (!to) return;
+    float s = 0.f;
+    for (int g = 0; g < a.G; ++g) s += a.sums[(int64_t)g * width + c];
+    *to = s;
+}
+
+template <class K>
+K by_type(int32_t dtype, K f32, K bf16, K f16) { return dtype == RTMA_F32 ? f32 : dtype == RTMA_BF16 ? bf16 : f16; }
+#define NORM_KERNEL(name) by_type(d->dtype, &name<float>, &name<__nv_bfloat16>, &name<__half>)
+
+int32_t check_norm(rtma_ctx* ctx, const char* who, const rtma_norm_desc* d, int64_t n, int32_t G, const int64_t* offsets, const float* slope) {
+    if (!d) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: null descriptor", who);
+    RTMA_TRY(check_parts(ctx, who, n, G, offsets));
+    if (d->dtype < RTMA_F32 || d->dtype > RTMA_F16) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: dtype=%d", who, d->dtype);
+    if (d->C < 1 || d->C > NORM_MAX_CHANNELS) return rtma_fail(ctx, RTMA_ERR_UNSUPPORTED, "%s: %d channels outside [1,%d]", who, d->C, NORM_MAX_CHANNELS);
+    if (d->groups < 1 || d->C % d->groups) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: %d channels in %d sets", who, d->C, d->groups);
+    if (d->scope != RTMA_SCOPE_ROW && d->scope != RTMA_SCOPE_PART) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: scope=%d", who, d->scope);
+    if (d->act < RTMA_ACT_NONE || d->act > RTMA_ACT_SILU) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: act=%d", who, d->act);
+    if (d->act == RTMA_ACT_PRELU && !slope) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: PReLU without a slope", who);
+    if (!(d->eps > 0.f) || std::isinf(d->eps)) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: eps=%g", who, (double)d->eps);
+    if (!(d->p >= 0.0 && d->p <= 1.0)) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: p=%g outside [0,1]", who, d->p);
+    return RTMA_OK;
+}
+
+NormArgs norm_args(const rtma_ctx* ctx, const rtma_norm_desc* d, int64_t n, int32_t G, const int64_t* offsets, const void* X, int64_t ldx,
+                   const float* gamma, const float* beta, const float* slope, const int32_t* row_ids) {
+    NormArgs a{};
+    a.offsets = offsets;
+    a.n = n;
+    a.G = G;
+    a.C = d->C;
+    a.groups = d->groups;
+    a.per_set = d->C / d->groups;
+    a.units = (d->C + 7) / 8;
+    a.rows_at_once = NORM_THREADS / a.units;
+    // four runs of rows per SM; a few rows per thread at least
+    const int64_t least = 4 * (int64_t)a.rows_at_once, even = ceil_div(n, 4 * (int64_t)ctx->sm_count);
+    a.tile_rows = (int)(even > least ? even : least);
+    a.tiles = n / a.tile_rows + G;
+    a.act = d->act;
+    a.eps = d->eps;
+    a.X = X;
+    a.ldx = ldx;
+    a.vx = aligned_rows(X, ldx, row_type_bytes(d->dtype));
+    a.gamma = gamma;
+    a.beta = beta;
+    a.slope = d->act == RTMA_ACT_PRELU ? slope : nullptr;
+    a.gamma_stride = d->gamma_stride;
+    a.beta_stride = d->beta_stride;
+    a.slope_stride = d->slope_stride;
+    a.drop = drop_args(d->p, d->seed, row_ids);
+    return a;
+}
+
+}  // namespace
+
+extern "C" int32_t rtma_group_norm(rtma_ctx* ctx, const rtma_norm_desc* d, int64_t n, int32_t G, const int64_t* offsets, const void* X, int64_t ldx,
+                                   const float* gamma, const float* beta, const float* slope, const int32_t* row_ids, void* Y, int64_t ldy,
+                                   float* stats, void* stream_) {
+    if (!ctx) return RTMA_ERR_INVALID_ARG;
+    RTMA_TRY(check_norm(ctx, "rtma_group_norm", d, n, G, offsets, slope));
+    if (n > 0 && (!X || !Y)) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "rtma_group_norm: null pointer");
+    if (ldx < d->C || ldy < d->C) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "rtma_group_norm: rows of %d channels lie closer than that", d->C);
+    const bool rows = d->scope == RTMA_SCOPE_ROW;
+    if (n == 0 && (rows || !stats)) return RTMA_OK;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    DeviceScope on(ctx->device);
+    RTMA_CUDA(ctx, on.status);
+    NormArgs a = norm_args(ctx, d, n, G, offsets, X, ldx, gamma, beta, slope, row_ids);
+    a.Y = Y;
+    a.ldy = ldy;
+    a.vy = aligned_rows(Y, ldy, row_type_bytes(d->dtype));
+    a.stats = stats;
+    const int64_t tiles = a.tiles;
+    const size_t piece_bytes = rows ? 0 : ArenaCursor::granule(sizeof(float2) * tiles * a.groups);
+    const size_t stat_bytes = rows || stats ? 0 : ArenaCursor::granule(sizeof(float2) * (size_t)G * a.groups);
+    RTMA_TRY(prepare_row_call(ctx, piece_bytes + stat_bytes, stream));
+    const unsigned grid = (unsigned)tiles;
+    if (rows) {
+        const size_t smem = sizeof(float) * a.rows_at_once * (8 * a.units + 2 * (size_t)a.groups);
+        auto kernel = NORM_KERNEL(norm_rows_kernel);
+        KernelScope ks(ctx, KC_POST, stream);
+        launch_kernel(kernel, grid, NORM_THREADS, smem, stream, a);
+    } else {
+        ArenaCursor cur(ctx->arena);
+        a.pieces = cur.take<float2>(tiles * a.groups);
+        if (!stats) a.stats = cur.take<float>(2 * (size_t)G * a.groups);
+        if (n > 0) {
+            KernelScope ks(ctx, KC_POST, stream);
+            launch_kernel(NORM_KERNEL(norm_stats_kernel), grid, NORM_THREADS, 0, stream, a);
+        }
+        RTMA_LAUNCH_CHECK(ctx);
+        {
+            KernelScope ks(ctx, KC_POST, stream);
+            launch_kernel(norm_join_kernel, (unsigned)ceil_div((int64_t)G * a.groups * 32, NORM_THREADS), NORM_THREADS, 0, stream, a);
+        }
+        RTMA_LAUNCH_CHECK(ctx);
+        if (n > 0) {
+            KernelScope ks(ctx, KC_POST, stream);
+            launch_kernel(NORM_KERNEL(norm_apply_kernel), grid, NORM_THREADS, 0, stream, a);
+        }
+    }
+    RTMA_LAUNCH_CHECK(ctx);
+    return RTMA_OK;
+}
+
+extern "C" int32_t rtma_group_norm_grad(rtma_ctx* ctx, const rtma_norm_desc* d, int64_t n, int32_t G, const int64_t* offsets, const void* X, int64_t ldx,
+                                        const void* dY, int64_t lddy, const float* stats, const float* gamma, const float* beta, const float* slope,
+                                        const int32_t* row_ids, void* dX, int64_t lddx, float* dgamma, int64_t dgamma_stride, float* dbeta,
+                                        int64_t dbeta_stride, float* dslope, int64_t dslope_stride, void* stream_) {
+    if (!ctx) return RTMA_ERR_INVALID_ARG;
+    RTMA_TRY(check_norm(ctx, "rtma_group_norm_grad", d, n, G, offsets, slope));
+    if (n > 0 && (!X || !dY || !stats || !dX)) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "rtma_group_norm_grad: null pointer");
+    if (ldx < d->C || lddy < d->C || lddx < d->C)
+        return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "rtma_group_norm_grad: rows of %d channels lie closer than that", d->C);
+    if (dslope && d->act != RTMA_ACT_PRELU) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "rtma_group_norm_grad: a slope's gradient without PReLU");
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    DeviceScope on(ctx->device);
+    RTMA_CUDA(ctx, on.status);
+    NormArgs a = norm_args(ctx, d, n, G, offsets, X, ldx, gamma, beta, slope, row_ids);
+    a.dY = dY;
+    a.lddy = lddy;
+    a.vdy = aligned_rows(dY, lddy, row_type_bytes(d->dtype));
+    a.Y = dX;
+    a.ldy = lddx;
+    a.vy = aligned_rows(dX, lddx, row_type_bytes(d->dtype));
+    a.stats = const_cast<float*>(stats);
+    a.dgamma = dgamma; a.dgamma_stride = dgamma_stride;
+    a.dbeta = dbeta; a.dbeta_stride = dbeta_stride;
+    a.dslope = dslope; a.dslope_stride = dslope_stride;
+    const int64_t tiles = a.tiles, width = 2 * (int64_t)a.C + 1;
+    RTMA_TRY(prepare_row_call(ctx, ArenaCursor::granule(sizeof(float) * tiles * width) + ArenaCursor::granule(sizeof(float) * G * width), stream));
+    ArenaCursor cur(ctx->arena);
+    a.partial = cur.take<float>(tiles * width);
+    a.sums = cur.take<float>(G * width);
+    const bool rows = d->scope == RTMA_SCOPE_ROW;
+    if (n > 0) {
+        KernelScope ks(ctx, KC_POST, stream);
+        if (rows) {
+            const size_t smem = sizeof(float2) * (8 * NORM_THREADS + (size_t)a.rows_at_once * a.groups);
+            auto kernel = NORM_KERNEL(norm_rows_grad_kernel);
+            launch_kernel(kernel, (unsigned)tiles, NORM_THREADS, smem, stream, a);
+        } else {
+            launch_kernel(NORM_KERNEL(norm_grad_sums_kernel), (unsigned)tiles, NORM_THREADS, 0, stream, a);
+        }
+    }
+    RTMA_LAUNCH_CHECK(ctx);
+    {
+        KernelScope ks(ctx, KC_POST, stream);
+        launch_kernel(norm_reduce_kernel, dim3((unsigned)ceil_div(width, 32), (unsigned)G), NORM_THREADS, 0, stream, a);
+    }
+    RTMA_LAUNCH_CHECK(ctx);
+    if (G > 1 && ((dgamma && !dgamma_stride) || (dbeta && !dbeta_stride) || (dslope && !dslope_stride))) {
+        KernelScope ks(ctx, KC_POST, stream);
+        launch_kernel(norm_reduce_parts_kernel, (unsigned)ceil_div(width, NORM_THREADS), NORM_THREADS, 0, stream, a);
+    }
+    RTMA_LAUNCH_CHECK(ctx);
+    if (n > 0 && !rows) {
+        KernelScope ks(ctx, KC_POST, stream);
+        launch_kernel(NORM_KERNEL(norm_grad_apply_kernel), (unsigned)tiles, NORM_THREADS, 0, stream, a);
+    }
+    RTMA_LAUNCH_CHECK(ctx);
+    return RTMA_OK;
+}
