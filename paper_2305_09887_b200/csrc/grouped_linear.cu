@@ -1,145 +1,651 @@
 // The product of every part's rows with the part's own matrix, and its gradients:
 //   forward  Y[r] = X[r] W_g + b_g        dx  dX[r] = dY[r] W_g^T        dw  dW_g = sum_r X[r]^T dY[r], db_g = sum_r dY[r]
-// for the rows r of part g.  Simple form: 64 x 64 tiles on the fp32 units.
+// for the rows r of part g, on the tensor cores (tcgen05, accumulators in tensor memory).
+//
+// One kernel body serves all three: a tile is 128 x BN results, its operands are staged 64 deep in the contraction, each as 32-row
+// slabs of 128 bytes per row in the 128-byte swizzle.  Rows that run along the contraction (X, dY; W in dx) make a K-major
+// operand, rows across it (W forward; X and dY in dw) an MN-major one: both come from memory as they lie, nothing is transposed.
+// fp32 values are split on their way into three bf16 numbers (8 + 8 + 8 bits, the whole significand) and a product is six MMAs;
+// what is left out is below 2^-24 of it.
+//
+// The tensor cores truncate when they accumulate, so a long sum drifts towards zero by half a step per addition.  Where the
+// result is fp32 the drain warps therefore take the accumulator after every 64 terms and add it up in registers, rounded to nearest;
+// inside 64 terms the five small products of fp32 operands come first.
+//
+// Warps: 0-7 drain (a quarter of the lanes, every second 32 columns each), 8-15 load, 16 issues the MMAs (17-19 complete its group
+// of four).
 #include "rows.cuh"
+#include "tc_common.cuh"
 
 RTMA_BOUNDS_TU()
 
 namespace {
 
-constexpr int BM = 64, BN = 64, BK = 16, THREADS = 256;
+enum Mode { FORWARD, INPUT_GRADIENT, WEIGHT_GRADIENT };
+
+constexpr int BM = 128, BK = 64;
+constexpr int DRAIN_WARPS = 8, LOAD_WARPS = 8, WARPS = DRAIN_WARPS + LOAD_WARPS + 4, THREADS = 32 * WARPS;
+// A block is launched with 96 registers a thread (640 of them); the four warps of the multiplier give theirs up to the others:
+// 256 x 120 + 256 x 104 + 128 x 24 = 60,416 of 61,440.
+constexpr int DRAIN_REGISTERS = 120, LOAD_REGISTERS = 104, MULTIPLY_REGISTERS = 24;
+constexpr int SLAB_BYTES = 32 * 128;       // 32 rows of 64 16-bit values
+constexpr int OUT_PITCH = 80, OUT_BYTES = 32 * OUT_PITCH;  // a drain warp's 32 rows of 64 bytes on their way out
+constexpr int RING_BYTES = 192 * 1024;
+constexpr int DYNAMIC_BYTES = RING_BYTES + 1024 + DRAIN_WARPS * OUT_BYTES;
+constexpr int BIAS_ROWS = LOAD_WARPS;      // partial sums of the bias gradient in a slot, one row per loading warp
+constexpr int MAX_STAGES = 6;
+
+template <class T, int MODE>
+struct Form {
+    static constexpr bool SPLIT = sizeof(T) == 4;
+    static constexpr int PLANES = SPLIT ? 3 : 1;
+    static constexpr bool IN_REGISTERS = SPLIT || MODE == WEIGHT_GRADIENT;  // accumulated there, 64 terms at a time
+    static constexpr int BN = IN_REGISTERS ? 128 : 256;                     // widest tile
+    static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128;            // of a plane
+    static constexpr int STAGE_BYTES = PLANES * (A_BYTES + B_BYTES);
+    static constexpr int STAGES = RING_BYTES / STAGE_BYTES;
+    static constexpr bool A_ACROSS = MODE == WEIGHT_GRADIENT, B_ACROSS = MODE != INPUT_GRADIENT;  // MN-major
+};
 
 struct LinearArgs {
     const int64_t* offsets;
     int64_t n;
     int G, span;
-    int64_t tile_rows, tiles;
+    int64_t tile_rows, tiles;  // rows of a row tile (forward, dx: 128; dw: of a chunk), row tiles at most
+    int m_tiles, n_tiles;      // tiles of one row tile: m_tiles (dw) x n_tiles
+    int BN;
     int d_in, d_out;
-    const void *A, *B;  // rows; matrices (forward, dx) or rows (dw)
+    const void *A, *B;         // rows; matrices (forward, dx) or rows (dw)
     int64_t lda, ldb, w_stride;
+    bool va, vb, vo;           // rows on 16-byte boundaries
     const void* bias;
     int64_t bias_stride;
-    void* out;
+    void* out;                 // dw: the slots, [row tile][(d_in + BIAS_ROWS) * d_out]
     int64_t ldo;
-    float* partial;  // dw: [tile][(d_in + 1) * d_out], the last row the bias's
     float *dW, *db;
     int64_t dw_stride, db_stride;
+    int* error_word;
 };
 
-template <class T, bool TRANSPOSED>
-__global__ void __launch_bounds__(THREADS) linear_rows_kernel(const LinearArgs a) {
-    __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
-    __shared__ float sa[BK][BM + 1], sb[BK][BN + 1];
-    wait_for_kernel_before();
-    number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums, a.span);
-    const int tile = blockIdx.x;
-    if (tile >= tile_start[a.G]) return;
-    const int part = part_of_tile(tile_start, a.G, tile);
-    int64_t begin, end;
-    part_rows(a.offsets, a.n, part, begin, end);
-    begin += (int64_t)(tile - tile_start[part]) * a.tile_rows;
-    const int rows = (int)min(end - begin, a.tile_rows);
-    const int K = TRANSPOSED ? a.d_out : a.d_in, N = TRANSPOSED ? a.d_in : a.d_out, n0 = blockIdx.y * BN;
-    const T* A = static_cast<const T*>(a.A) + begin * a.lda;
-    const T* W = static_cast<const T*>(a.B) + part * a.w_stride;
-    const T* bias = a.bias ? static_cast<const T*>(a.bias) + part * a.bias_stride : nullptr;
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    float acc[4][4] = {};
-    for (int k0 = 0; k0 < K; k0 += BK) {
-        for (int i = threadIdx.x; i < BM * BK; i += THREADS) {
-            const int k = i % BK, m = i / BK;
-            sa[k][m] = m < rows && k0 + k < K ? to_f32(A[m * a.lda + k0 + k]) : 0.f;
-        }
-        for (int i = threadIdx.x; i < BN * BK; i += THREADS) {
-            const int j = TRANSPOSED ? i / BK : i % BN, k = TRANSPOSED ? i % BK : i / BN;
-            const bool ok = k0 + k < K && n0 + j < N;
-            sb[k][j] = ok ? to_f32(TRANSPOSED ? W[(int64_t)(n0 + j) * a.d_out + k0 + k] : W[(int64_t)(k0 + k) * a.d_out + n0 + j]) : 0.f;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < BK; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(sa[k][ty + 16 * i], sb[k][tx + 16 * j], acc[i][j]);
-        __syncthreads();
+struct Shared {
+    uint64_t full[MAX_STAGES], empty[MAX_STAGES];
+    uint64_t acc_full[2], acc_empty[2];
+    uint32_t tmem_base;
+    int abort;
+    int32_t warp_sums[32];
+    int32_t tile_start[RTMA_MAX_GROUPS + 1], begin[RTMA_MAX_GROUPS], rows[RTMA_MAX_GROUPS];
+};
+
+__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, Shared& sh, int* error_word) {
+    for (uint32_t i = 0; i < tc::WAIT_POLLS; ++i) {
+        if (tc::mbar_try_wait(bar, parity)) return true;
+        if ((i & 1023u) == 1023u && *reinterpret_cast<volatile int*>(&sh.abort)) break;
     }
-    T* out = static_cast<T*>(a.out) + begin * a.ldo;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int m = ty + 16 * i, c = n0 + tx + 16 * j;
-            if (m < rows && c < N) out[m * a.ldo + c] = from_f32<T>(acc[i][j] + (bias ? to_f32(bias[c]) : 0.f));
-        }
+    *reinterpret_cast<volatile int*>(&sh.abort) = 1;
+    atomicExch(error_word, 1);
+    return false;
 }
 
-template <class T>
-__global__ void __launch_bounds__(THREADS) linear_weights_kernel(const LinearArgs a) {
-    __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
-    __shared__ float sa[BK][BM + 1], sb[BK][BN + 1];
-    wait_for_kernel_before();
-    number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums, a.span);
-    const int tile = blockIdx.x;
-    if (tile >= tile_start[a.G]) return;
-    const int part = part_of_tile(tile_start, a.G, tile);
-    int64_t begin, end;
-    part_rows(a.offsets, a.n, part, begin, end, a.span);
-    begin += (int64_t)(tile - tile_start[part]) * a.tile_rows;
-    end = min(end, begin + a.tile_rows);
-    const int m0 = blockIdx.z * BM, n0 = blockIdx.y * BN;
-    const T* X = static_cast<const T*>(a.A);
-    const T* dY = static_cast<const T*>(a.B);
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    float acc[4][4] = {}, sums[4] = {};
-    for (int64_t r0 = begin; r0 < end; r0 += BK) {
-        for (int i = threadIdx.x; i < BM * BK; i += THREADS) {
-            const int m = i % BM, k = i / BM;
-            sa[k][m] = r0 + k < end && m0 + m < a.d_in ? to_f32(X[(r0 + k) * a.lda + m0 + m]) : 0.f;
+// A role's walk over a block's tiles and their stages.
+template <int MODE>
+struct Walk {
+    int tile, part, row_tile, m0, n0;
+    int64_t row0;     // first row of the tile
+    int rows, k_end;  // rows of the tile; terms of the contraction
+    int k0;
+    __device__ __forceinline__ bool at(const LinearArgs& a, const Shared& sh) {
+        const int per = a.m_tiles * a.n_tiles;
+        row_tile = tile / per;
+        if (row_tile >= sh.tile_start[a.G]) return false;
+        const int rest = tile - row_tile * per;
+        m0 = rest / a.n_tiles * BM;
+        n0 = rest % a.n_tiles * a.BN;
+        part = part_of_tile(sh.tile_start, a.G, row_tile);
+        const int64_t inside = (int64_t)(row_tile - sh.tile_start[part]) * a.tile_rows;
+        row0 = sh.begin[part] + inside;
+        rows = (int)min((int64_t)sh.rows[part] - inside, a.tile_rows);
+        k_end = MODE == FORWARD ? a.d_in : MODE == INPUT_GRADIENT ? a.d_out : rows;
+        k0 = 0;
+        return true;
+    }
+    __device__ __forceinline__ bool first(const LinearArgs& a, const Shared& sh) {
+        tile = blockIdx.x;
+        return at(a, sh);
+    }
+    __device__ __forceinline__ bool last_stage() const { return k0 + BK >= k_end; }
+    __device__ __forceinline__ bool next(const LinearArgs& a, const Shared& sh) {  // the next stage
+        if (!last_stage()) {
+            k0 += BK;
+            return true;
         }
-        for (int i = threadIdx.x; i < BN * BK; i += THREADS) {
-            const int j = i % BN, k = i / BN;
-            sb[k][j] = r0 + k < end && n0 + j < a.d_out ? to_f32(dY[(r0 + k) * a.ldb + n0 + j]) : 0.f;
+        tile += gridDim.x;
+        return at(a, sh);
+    }
+    __device__ __forceinline__ bool next_tile(const LinearArgs& a, const Shared& sh) {
+        tile += gridDim.x;
+        return at(a, sh);
+    }
+};
+
+// Where the eight values of slab i that a loading thread (row 0..31 of the slab, unit 0..7 of the row) brings come from, and how
+// many of them exist.
+template <class T, int MODE>
+__device__ __forceinline__ const T* source_a(const LinearArgs& a, const Walk<MODE>& w, int i, int row, int unit, int& valid) {
+    const T* A = static_cast<const T*>(a.A);
+    if constexpr (MODE == WEIGHT_GRADIENT) {
+        const int k = w.k0 + 32 * (i & 1) + row, c = w.m0 + 64 * (i >> 1) + 8 * unit;
+        valid = k < w.k_end ? max(0, min(8, a.d_in - c)) : 0;
+        return valid ? A + (w.row0 + k) * a.lda + c : A;
+    } else {
+        const int r = 32 * i + row, c = w.k0 + 8 * unit;
+        valid = r < w.rows ? max(0, min(8, w.k_end - c)) : 0;
+        return valid ? A + (w.row0 + r) * a.lda + c : A;
+    }
+}
+template <class T, int MODE>
+__device__ __forceinline__ const T* source_b(const LinearArgs& a, const Walk<MODE>& w, int i, int row, int unit, int& valid) {
+    const T* B = static_cast<const T*>(a.B);
+    if constexpr (MODE == INPUT_GRADIENT) {
+        const int r = w.n0 + 32 * i + row, c = w.k0 + 8 * unit;
+        valid = r < a.d_in ? max(0, min(8, w.k_end - c)) : 0;
+        return valid ? B + w.part * a.w_stride + (int64_t)r * a.d_out + c : B;
+    } else {
+        const int k = w.k0 + 32 * (i & 1) + row, c = w.n0 + 64 * (i >> 1) + 8 * unit;
+        valid = k < w.k_end ? max(0, min(8, a.d_out - c)) : 0;
+        if constexpr (MODE == WEIGHT_GRADIENT) return valid ? B + (w.row0 + k) * a.ldb + c : B;
+        else return valid ? B + w.part * a.w_stride + (int64_t)k * a.d_out + c : B;
+    }
+}
+
+__device__ __forceinline__ void copy_16(uint32_t dst, const void* src, int bytes) {  // the rest of the 16 bytes becomes zero
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void store_16(uint32_t dst, uint4 v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ uint4 load_16(uint32_t src) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(src) : "memory");
+    return v;
+}
+
+// Eight fp32 values as three bf16 numbers each, x = h + m + l exactly (l rounds only where x has bits below the smallest bf16
+// number).  Values that round to an infinity are cut instead; what is not finite stays in h alone.
+__device__ __forceinline__ void split_eight(const float (&x)[8], uint4 (&planes)[3]) {
+    uint32_t big = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) big = max(big, __float_as_uint(x[j]) & 0x7FFFFFFFu);
+    uint32_t h[4], m[4], l[4];
+    if (big < 0x7F7F8000u) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 a = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+            h[i] = *reinterpret_cast<const uint32_t*>(&a);
+            const float r0 = x[2 * i] - __uint_as_float(h[i] << 16), r1 = x[2 * i + 1] - __uint_as_float(h[i] & 0xFFFF0000u);
+            const __nv_bfloat162 b = __floats2bfloat162_rn(r0, r1);
+            m[i] = *reinterpret_cast<const uint32_t*>(&b);
+            const __nv_bfloat162 c = __floats2bfloat162_rn(r0 - __uint_as_float(m[i] << 16), r1 - __uint_as_float(m[i] & 0xFFFF0000u));
+            l[i] = *reinterpret_cast<const uint32_t*>(&c);
         }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < BK; ++k)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                sums[j] += sb[k][tx + 16 * j];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[i][j] = fmaf(sa[k][ty + 16 * i], sb[k][tx + 16 * j], acc[i][j]);
+    } else {
+        for (int i = 0; i < 4; ++i) {
+            h[i] = m[i] = l[i] = 0;
+            for (int k = 0; k < 2; ++k) {
+                const float v = x[2 * i + k];
+                const uint32_t u = __float_as_uint(v), mag = u & 0x7FFFFFFFu;
+                uint32_t a = mag > 0x7F800000u ? 0x7FC0u : u >> 16, b = 0, c = 0;
+                if (mag < 0x7F7F8000u) a = __bfloat16_as_ushort(__float2bfloat16_rn(v));
+                if (mag < 0x7F800000u) {
+                    const float r = v - __uint_as_float(a << 16);
+                    b = __bfloat16_as_ushort(__float2bfloat16_rn(r));
+                    c = __bfloat16_as_ushort(__float2bfloat16_rn(r - __uint_as_float(b << 16)));
+                }
+                h[i] |= a << 16 * k;
+                m[i] |= b << 16 * k;
+                l[i] |= c << 16 * k;
             }
-        __syncthreads();
+        }
     }
-    float* out = a.partial + (int64_t)tile * (a.d_in + 1) * a.d_out;
+    planes[0] = make_uint4(h[0], h[1], h[2], h[3]);
+    planes[1] = make_uint4(m[0], m[1], m[2], m[3]);
+    planes[2] = make_uint4(l[0], l[1], l[2], l[3]);
+}
+
+// Sums over a loading warp's rows of the columns of dY that its lanes hold, written to the warp's row of the slot.
+__device__ __forceinline__ void leave_bias(const LinearArgs& a, const Walk<WEIGHT_GRADIENT>& w, float (&sums)[2][8], int warp, int lane) {
+    float* to = static_cast<float*>(a.out) + ((int64_t)w.row_tile * (a.d_in + BIAS_ROWS) + a.d_in + warp) * a.d_out;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int c = n0 + tx + 16 * j;
-        if (c >= a.d_out) continue;
-        if (ty == 0 && m0 == 0) out[(int64_t)a.d_in * a.d_out + c] = sums[j];
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (m0 + ty + 16 * i < a.d_in) out[(int64_t)(m0 + ty + 16 * i) * a.d_out + c] = acc[i][j];
+        for (int j = 0; j < 8; ++j) {
+            float s = sums[t][j];
+            s += __shfl_xor_sync(0xffffffffu, s, 8);
+            s += __shfl_xor_sync(0xffffffffu, s, 16);
+            const int c = 64 * t + 8 * lane + j;
+            if (lane < 8 && c < a.BN && w.n0 + c < a.d_out) to[w.n0 + c] = s;
+            sums[t][j] = 0.f;
+        }
+}
+
+template <class T, int MODE>
+__device__ __forceinline__ void load_role(const LinearArgs& a, Shared& sh, uint32_t ring) {
+    typedef Form<T, MODE> F;
+    const int t = threadIdx.x - 32 * DRAIN_WARPS, row = t >> 3, unit = t & 7, lane = t & 31, warp = t >> 5;
+    const uint32_t place = row * 128 + ((unit ^ (row & 7)) << 4);  // inside a slab; 32-row slabs do not change row mod 8
+    const int b_slabs = F::B_ACROSS ? 2 * ((a.BN + 63) / 64) : (a.BN + 31) / 32;
+    float sums[2][8];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sums[i][j] = 0.f;
+    Walk<MODE> w;
+    bool more = w.first(a, sh);
+    tc::RingAt at;
+    if constexpr (F::SPLIT) {
+        // Values wait in registers for their stage: while one operand's are split the other's are on their way.
+        Eight<T> ra[4], rb[4];
+        if (more) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                int valid;
+                const T* p = source_a<T, MODE>(a, w, i, row, unit, valid);
+                ra[i].load(p, valid, a.va);
+            }
+        }
+        while (more) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                int valid = 0;
+                const T* p = nullptr;
+                if (i < b_slabs) p = source_b<T, MODE>(a, w, i, row, unit, valid);
+                if (i < b_slabs) rb[i].load(p, valid, a.vb);
+            }
+            if (!wait_for(&sh.empty[at.s], at.phase ^ 1u, sh, a.error_word)) return;
+            const uint32_t stage = ring + at.s * F::STAGE_BYTES + place;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float v[8];
+                uint4 planes[3];
+                ra[i].values(v);
+                split_eight(v, planes);
+#pragma unroll
+                for (int k = 0; k < 3; ++k) store_16(stage + k * F::A_BYTES + i * SLAB_BYTES, planes[k]);
+            }
+            const bool sums_wanted = MODE == WEIGHT_GRADIENT && w.m0 == 0 && a.db;
+            const Walk<MODE> here = w;
+            more = w.next(a, sh);
+            if (more) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    int valid;
+                    const T* p = source_a<T, MODE>(a, w, i, row, unit, valid);
+                    ra[i].load(p, valid, a.va);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (i < b_slabs) {
+                    float v[8];
+                    uint4 planes[3];
+                    rb[i].values(v);
+                    if (sums_wanted) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) sums[i >> 1][j] += v[j];
+                    }
+                    split_eight(v, planes);
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) store_16(stage + 3 * F::A_BYTES + k * F::B_BYTES + i * SLAB_BYTES, planes[k]);
+                }
+            }
+            tc::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&sh.full[at.s]);
+            at.advance(F::STAGES);
+            if constexpr (MODE == WEIGHT_GRADIENT)
+                if (sums_wanted && here.last_stage()) leave_bias(a, here, sums, warp, lane);
+        }
+    } else {
+        // 16-byte copies straight into the stage; a stage is handed over once this thread's copies of it have landed, LAG stages later.
+        constexpr int LAG = F::STAGES - 2;  // stages whose copies are under way behind the newest
+        Walk<MODE> late = w;
+        tc::RingAt late_at;
+        int under_way = 0;
+        auto hand_over = [&]() {
+            if constexpr (MODE == WEIGHT_GRADIENT) {
+                if (late.m0 == 0 && a.db) {
+                    const uint32_t stage = ring + late_at.s * F::STAGE_BYTES + F::PLANES * F::A_BYTES + place;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (i < b_slabs) {
+                            Eight<T> e;
+                            e.w[0] = load_16(stage + i * SLAB_BYTES);
+                            float v[8];
+                            e.values(v);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) sums[i >> 1][j] += v[j];
+                        }
+                    }
+                    if (late.last_stage()) leave_bias(a, late, sums, warp, lane);
+                }
+                late.next(a, sh);
+            }
+            tc::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&sh.full[late_at.s]);
+            late_at.advance(F::STAGES);
+            --under_way;
+        };
+        bool ok = true;
+        while (more) {
+            ok = wait_for(&sh.empty[at.s], at.phase ^ 1u, sh, a.error_word);
+            if (!ok) break;
+            const uint32_t stage = ring + at.s * F::STAGE_BYTES + place;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                int valid;
+                const T* p = source_a<T, MODE>(a, w, i, row, unit, valid);
+                if (a.va) {
+                    copy_16(stage + i * SLAB_BYTES, p, valid * (int)sizeof(T));
+                } else {
+                    Eight<T> e;
+                    e.load(p, valid, false);
+                    store_16(stage + i * SLAB_BYTES, e.w[0]);
+                }
+            }
+#pragma unroll 4
+            for (int i = 0; i < b_slabs; ++i) {
+                int valid;
+                const T* p = source_b<T, MODE>(a, w, i, row, unit, valid);
+                if (a.vb) {
+                    copy_16(stage + F::A_BYTES + i * SLAB_BYTES, p, valid * (int)sizeof(T));
+                } else {
+                    Eight<T> e;
+                    e.load(p, valid, false);
+                    store_16(stage + F::A_BYTES + i * SLAB_BYTES, e.w[0]);
+                }
+            }
+            copies_commit();
+            at.advance(F::STAGES);
+            if (++under_way > LAG) {
+                copies_wait<LAG>();
+                hand_over();
+            }
+            more = w.next(a, sh);
+        }
+        copies_wait<0>();
+        if (ok)
+            while (under_way > 0) hand_over();
     }
 }
 
-// The tiles' sums of every part added up in order.
-__global__ void __launch_bounds__(THREADS) linear_reduce_kernel(const LinearArgs a) {
+template <class T, int MODE>
+__device__ __forceinline__ void multiply_role(const LinearArgs& a, Shared& sh, uint32_t ring) {
+    typedef Form<T, MODE> F;
+    const uint32_t format = std::is_same<T, __half>::value ? 0u : 1u;  // fp16 or bf16 operands, fp32 sums
+    const uint32_t idesc = (1u << 4) | (format << 7) | (format << 10) | ((F::A_ACROSS ? 1u : 0u) << 15) | ((F::B_ACROSS ? 1u : 0u) << 16) |
+                           ((uint32_t)(a.BN >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
+    const uint64_t desc = tc::smem_desc_sw128(0, 2 * SLAB_BYTES, 1024);  // atoms of 64 columns lie two slabs apart
+    constexpr uint32_t a_step = F::A_ACROSS ? 128 : 2, b_step = F::B_ACROSS ? 128 : 2;  // 16 terms further, in units of 16 bytes
+    constexpr uint32_t a_plane = F::A_BYTES >> 4, b_plane = F::B_BYTES >> 4;
+    Walk<MODE> w;
+    tc::RingAt at, acc;
+    bool more = w.first(a, sh);
+    while (more) {
+        if (F::IN_REGISTERS || w.k0 == 0) {
+            if (!wait_for(&sh.acc_empty[acc.s], acc.phase ^ 1u, sh, a.error_word)) return;
+        }
+        if (!wait_for(&sh.full[at.s], at.phase, sh, a.error_word)) return;
+        tc::tc_fence_after_sync();
+        const uint32_t d = sh.tmem_base + acc.s * F::BN;
+        const uint32_t sa = (ring + at.s * F::STAGE_BYTES) >> 4, sb = sa + F::PLANES * a_plane;
+        const int steps = (min(BK, w.k_end - w.k0) + 15) >> 4;
+        uint32_t accumulate = F::IN_REGISTERS || w.k0 == 0 ? 0u : 1u;
+        if constexpr (F::SPLIT) {
+            for (int k = 0; k < steps; ++k) {
+                const uint64_t da = desc + sa + k * a_step, db = desc + sb + k * b_step;
+                tc::mma_bf16(d, da + 2 * a_plane, db, idesc, accumulate);
+                tc::mma_bf16(d, da, db + 2 * b_plane, idesc, 1u);
+                tc::mma_bf16(d, da + a_plane, db + b_plane, idesc, 1u);
+                tc::mma_bf16(d, da + a_plane, db, idesc, 1u);
+                tc::mma_bf16(d, da, db + b_plane, idesc, 1u);
+                accumulate = 1u;
+            }
+        }
+        for (int k = 0; k < steps; ++k) {
+            tc::mma_bf16(d, desc + sa + k * a_step, desc + sb + k * b_step, idesc, accumulate);
+            accumulate = 1u;
+        }
+        tc::mma_commit(&sh.empty[at.s]);
+        at.advance(F::STAGES);
+        if (F::IN_REGISTERS || w.last_stage()) {
+            tc::mma_commit(&sh.acc_full[acc.s]);
+            acc.advance(2);
+        }
+        more = w.next(a, sh);
+    }
+}
+
+// 32 columns of a warp's 32 rows (a row per lane) on their way out, through shared memory so that lines are written whole.
+template <class O>
+__device__ __forceinline__ void write_out(O* out, int64_t ldo, bool vec, const float (&v)[32], uint32_t slab, int rows, int cols, int lane) {
+    constexpr int WIDE = 64 / sizeof(O), PIECE = 16 / sizeof(O);  // columns at a time, and of 16 bytes
+#pragma unroll
+    for (int c0 = 0; c0 < 32; c0 += WIDE) {
+        if (c0 >= cols) break;
+        __syncwarp();
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            uint4 x;
+            if constexpr (sizeof(O) == 4) {
+                x = make_uint4(__float_as_uint(v[c0 + 4 * q]), __float_as_uint(v[c0 + 4 * q + 1]), __float_as_uint(v[c0 + 4 * q + 2]), __float_as_uint(v[c0 + 4 * q + 3]));
+            } else {
+                const O* tag = nullptr;
+                x = make_uint4(narrow2(v[8 * q], v[8 * q + 1], tag), narrow2(v[8 * q + 2], v[8 * q + 3], tag),
+                               narrow2(v[8 * q + 4], v[8 * q + 5], tag), narrow2(v[8 * q + 6], v[8 * q + 7], tag));
+            }
+            store_16(slab + lane * OUT_PITCH + 16 * q, x);
+        }
+        __syncwarp();
+        if (vec && cols - c0 >= WIDE) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = 8 * i + (lane >> 2), q = lane & 3;
+                const uint4 x = load_16(slab + r * OUT_PITCH + 16 * q);
+                if (r < rows) *reinterpret_cast<uint4*>(out + r * ldo + c0 + q * PIECE) = x;
+            }
+        } else {
+            const int c = lane % WIDE;
+            for (int r = lane / WIDE; r < rows; r += 32 / WIDE) {
+                O x;
+                if constexpr (sizeof(O) == 4) {
+                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(slab + r * OUT_PITCH + 4 * c) : "memory");
+                } else {
+                    unsigned short bits;
+                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(bits) : "r"(slab + r * OUT_PITCH + 2 * c) : "memory");
+                    x = *reinterpret_cast<O*>(&bits);
+                }
+                if (c0 + c < cols) out[r * ldo + c0 + c] = x;
+            }
+        }
+    }
+}
+
+template <class T, int MODE>
+__device__ __forceinline__ void drain_role(const LinearArgs& a, Shared& sh, uint32_t slabs) {
+    typedef Form<T, MODE> F;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, half = warp >> 2;
+    const uint32_t slab = slabs + warp * OUT_BYTES, lanes = (uint32_t)(32 * quarter) << 16;
+    const int chunks = (a.BN + 31) / 32;
+    Walk<MODE> w;
+    tc::RingAt acc;
+    for (bool more = w.first(a, sh); more; more = w.next_tile(a, sh)) {
+        const int N = MODE == INPUT_GRADIENT ? a.d_in : a.d_out;
+        const int out_rows = max(0, (MODE == WEIGHT_GRADIENT ? min(BM, a.d_in - w.m0) : w.rows) - 32 * quarter);
+        auto put = [&](float (&v)[32], int chunk) {
+            const int c = w.n0 + 32 * chunk, cols = min(min(32, a.BN - 32 * chunk), N - c);
+            if (cols <= 0 || out_rows <= 0) return;
+            if constexpr (MODE == WEIGHT_GRADIENT) {
+                float* out = static_cast<float*>(a.out) + ((int64_t)w.row_tile * (a.d_in + BIAS_ROWS) + w.m0 + 32 * quarter) * a.d_out + c;
+                write_out<float>(out, a.d_out, a.vo, v, slab, min(32, out_rows), cols, lane);
+            } else {
+                if (MODE == FORWARD && a.bias) {
+                    const T* bias = static_cast<const T*>(a.bias) + w.part * a.bias_stride + c;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] += j < cols ? to_f32(bias[j]) : 0.f;
+                }
+                write_out<T>(static_cast<T*>(a.out) + (w.row0 + 32 * quarter) * a.ldo + c, a.ldo, a.vo, v, slab, min(32, out_rows), cols, lane);
+            }
+        };
+        if constexpr (F::IN_REGISTERS) {
+            float total[2][32];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 32; ++j) total[i][j] = 0.f;
+            for (int k0 = 0; k0 < w.k_end; k0 += BK) {
+                if (!wait_for(&sh.acc_full[acc.s], acc.phase, sh, a.error_word)) return;
+                __syncwarp();
+                tc::tc_fence_after_sync();
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if (half + 2 * i < chunks) {
+                        float v[32];
+                        tc::tmem_load_32x32(sh.tmem_base + lanes + acc.s * F::BN + 32 * (half + 2 * i), v);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) total[i][j] += v[j];
+                    }
+                }
+                tc::tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&sh.acc_empty[acc.s]);
+                acc.advance(2);
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (half + 2 * i < chunks) put(total[i], half + 2 * i);
+        } else {
+            if (!wait_for(&sh.acc_full[acc.s], acc.phase, sh, a.error_word)) return;
+            __syncwarp();
+            tc::tc_fence_after_sync();
+            for (int chunk = half; chunk < chunks; chunk += 2) {
+                float v[32];
+                tc::tmem_load_32x32(sh.tmem_base + lanes + acc.s * F::BN + 32 * chunk, v);
+                put(v, chunk);
+            }
+            tc::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&sh.acc_empty[acc.s]);
+            acc.advance(2);
+        }
+    }
+}
+
+template <class T, int MODE>
+__global__ void __launch_bounds__(THREADS, 1) linear_kernel(const __grid_constant__ LinearArgs a) {
+    typedef Form<T, MODE> F;
+    extern __shared__ uint8_t raw[];
+    __shared__ Shared sh;
+    const uint32_t ring = (tc::smem_u32(raw) + 1023u) & ~1023u, slabs = ring + RING_BYTES;
+    const int warp = threadIdx.x >> 5;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < F::STAGES; ++s) {
+            tc::mbar_init(&sh.full[s], LOAD_WARPS);
+            tc::mbar_init(&sh.empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            tc::mbar_init(&sh.acc_full[b], 1);
+            tc::mbar_init(&sh.acc_empty[b], DRAIN_WARPS);
+        }
+        sh.abort = 0;
+        tc::fence_barrier_init();
+    }
+    if (warp == WARPS - 1) {
+        tc::tmem_alloc(&sh.tmem_base, 2 * F::BN);
+        tc::tmem_relinquish();
+    }
+    wait_for_kernel_before();
+    for (int g = threadIdx.x; g < a.G; g += THREADS) {
+        int64_t begin, end;
+        part_rows(a.offsets, a.n, g, begin, end, a.span);
+        sh.begin[g] = (int32_t)begin;
+        sh.rows[g] = (int32_t)(end - begin);
+    }
+    number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, sh.tile_start, sh.warp_sums, a.span);
+    tc::tc_fence_before_sync();
+    __syncthreads();
+    tc::tc_fence_after_sync();
+    if (warp < DRAIN_WARPS) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(DRAIN_REGISTERS));
+        drain_role<T, MODE>(a, sh, slabs);
+    } else if (warp < DRAIN_WARPS + LOAD_WARPS) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(LOAD_REGISTERS));
+        load_role<T, MODE>(a, sh, ring);
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(MULTIPLY_REGISTERS));
+        if (warp == DRAIN_WARPS + LOAD_WARPS && (threadIdx.x & 31) == 0) multiply_role<T, MODE>(a, sh, ring);
+    }
+    __syncwarp();
+    tc::tc_fence_before_sync();
+    __syncthreads();
+    if (warp == WARPS - 1) {
+        tc::tc_fence_after_sync();
+        tc::tmem_dealloc(sh.tmem_base, 2 * F::BN);
+    }
+}
+
+// The slots of every part added up in order.
+constexpr int REDUCE_THREADS = 256;
+__global__ void __launch_bounds__(REDUCE_THREADS) linear_reduce_kernel(const __grid_constant__ LinearArgs a) {
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
     wait_for_kernel_before();
     number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums, a.span);
     const int part = blockIdx.y;
-    const int64_t weights = (int64_t)a.d_in * a.d_out, count = weights + a.d_out, i = (int64_t)blockIdx.x * THREADS + threadIdx.x;
-    if (i >= count) return;
+    const int64_t weights = (int64_t)a.d_in * a.d_out, slot = weights + BIAS_ROWS * (int64_t)a.d_out, i = (int64_t)blockIdx.x * REDUCE_THREADS + threadIdx.x;
+    if (i >= weights + a.d_out) return;
+    const float* p = static_cast<const float*>(a.out);
+    const int t1 = tile_start[part + 1];
     float s = 0.f;
-    for (int t = tile_start[part]; t < tile_start[part + 1]; ++t) s += a.partial[(int64_t)t * count + i];
-    if (i < weights) a.dW[part * a.dw_stride + i] = s;
-    else if (a.db) a.db[part * a.db_stride + i - weights] = s;
+    if (i < weights) {
+#pragma unroll 8
+        for (int t = tile_start[part]; t < t1; ++t) s += p[(int64_t)t * slot + i];
+        a.dW[part * a.dw_stride + i] = s;
+    } else if (a.db) {
+        for (int t = tile_start[part]; t < t1; ++t)
+#pragma unroll
+            for (int k = 0; k < BIAS_ROWS; ++k) s += p[(int64_t)t * slot + i + (int64_t)k * a.d_out];
+        a.db[part * a.db_stride + i - weights] = s;
+    }
 }
 
 template <class K>
 K by_type(int32_t dtype, K f32, K bf16, K f16) { return dtype == RTMA_F32 ? f32 : dtype == RTMA_BF16 ? bf16 : f16; }
+
+// Columns in equal tiles of a multiple of 16.
+void cut_columns(LinearArgs& a, int N, int widest) {
+    a.n_tiles = (int)ceil_div(N, widest);
+    a.BN = (int)ceil_div(ceil_div(N, a.n_tiles), 16) * 16;
+    a.n_tiles = (int)ceil_div(N, a.BN);
+}
+
+template <int MODE>
+int32_t launch_linear(rtma_ctx* ctx, int32_t dtype, LinearArgs& a, int cls, cudaStream_t stream) {
+    a.error_word = ctx->error_word;
+    const int64_t tiles = a.tiles * a.m_tiles * a.n_tiles;
+    if (tiles >= (int64_t(1) << 31)) return rtma_fail(ctx, RTMA_ERR_OVERFLOW, "grouped product: %lld tiles", (long long)tiles);
+    auto kernel = by_type(dtype, &linear_kernel<float, MODE>, &linear_kernel<__nv_bfloat16, MODE>, &linear_kernel<__half, MODE>);
+    bool& configured = ctx->linear_configured[MODE * 3 + dtype];
+    if (!configured) {
+        RTMA_CUDA(ctx, cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, DYNAMIC_BYTES));
+        configured = true;
+    }
+    KernelScope ks(ctx, cls, stream);
+    launch_kernel(kernel, (unsigned)(tiles < ctx->sm_count ? tiles : ctx->sm_count), THREADS, DYNAMIC_BYTES, stream, a);
+    RTMA_LAUNCH_CHECK(ctx);
+    return RTMA_OK;
+}
 
 int32_t check_linear(rtma_ctx* ctx, const char* who, int32_t dtype, int64_t n, int32_t G, const int64_t* offsets, int32_t d_in, int32_t d_out) {
     RTMA_TRY(check_parts(ctx, who, n, G, offsets));
@@ -162,21 +668,20 @@ int32_t run_rows(rtma_ctx* ctx, const char* who, bool transposed, int32_t dtype,
     DeviceScope on(ctx->device);
     RTMA_CUDA(ctx, on.status);
     RTMA_TRY(prepare_row_call(ctx, 0, stream));
+    const size_t es = row_type_bytes(dtype);
     LinearArgs a{};
     a.offsets = offsets; a.n = n; a.G = G; a.span = 1;
     a.tile_rows = BM;
     a.tiles = n / BM + G;
+    a.m_tiles = 1;
+    cut_columns(a, N, dtype == RTMA_F32 ? 128 : 256);
     a.d_in = d_in; a.d_out = d_out;
     a.A = A; a.lda = lda; a.B = W; a.w_stride = w_stride; a.bias = b; a.bias_stride = b_stride;
+    a.va = aligned_rows(A, lda, es);
+    a.vb = aligned_rows(W, d_out, es) && (w_stride * (int64_t)es) % 16 == 0;
     a.out = out; a.ldo = ldo;
-    auto kernel = transposed ? by_type(dtype, &linear_rows_kernel<float, true>, &linear_rows_kernel<__nv_bfloat16, true>, &linear_rows_kernel<__half, true>)
-                             : by_type(dtype, &linear_rows_kernel<float, false>, &linear_rows_kernel<__nv_bfloat16, false>, &linear_rows_kernel<__half, false>);
-    {
-        KernelScope ks(ctx, transposed ? KC_GEMM_DGRAD : KC_GEMM_FWD, stream);
-        launch_kernel(kernel, dim3((unsigned)a.tiles, (unsigned)ceil_div(N, BN)), THREADS, 0, stream, a);
-    }
-    RTMA_LAUNCH_CHECK(ctx);
-    return RTMA_OK;
+    a.vo = aligned_rows(out, ldo, es);
+    return transposed ? launch_linear<INPUT_GRADIENT>(ctx, dtype, a, KC_GEMM_DGRAD, stream) : launch_linear<FORWARD>(ctx, dtype, a, KC_GEMM_FWD, stream);
 }
 
 }  // namespace
@@ -212,23 +717,25 @@ extern "C" int32_t rtma_grouped_linear_dw(rtma_ctx* ctx, int32_t dtype, int64_t 
     a.offsets = offsets; a.n = n;
     a.G = shared ? 1 : G;
     a.span = shared ? G : 1;
-    const int64_t blocks = ceil_div(d_in, BM) * ceil_div(d_out, BN), chunk = ceil_div(n * blocks, 8 * (int64_t)ctx->sm_count);
-    a.tile_rows = chunk < 256 ? 256 : ceil_div(chunk, 64) * 64;
+    a.m_tiles = (int)ceil_div(d_in, BM);
+    cut_columns(a, d_out, 128);
+    // about four tiles per SM over the whole call; chunks of whole stages
+    const int64_t chunk = ceil_div(n * a.m_tiles * a.n_tiles, 4 * (int64_t)ctx->sm_count);
+    a.tile_rows = chunk < 256 ? 256 : ceil_div(chunk, BK) * BK;
     a.tiles = n / a.tile_rows + a.G;
+    const size_t es = row_type_bytes(dtype);
     a.d_in = d_in; a.d_out = d_out;
     a.A = X; a.lda = ldx; a.B = dY; a.ldb = lddy;
+    a.va = aligned_rows(X, ldx, es);
+    a.vb = aligned_rows(dY, lddy, es);
+    a.vo = d_out % 4 == 0;
     a.dW = dW; a.dw_stride = dw_stride; a.db = db; a.db_stride = db_stride;
-    RTMA_TRY(prepare_row_call(ctx, sizeof(float) * a.tiles * (weights + d_out), stream));
-    a.partial = reinterpret_cast<float*>(ctx->arena);
-    if (n > 0) {
-        auto kernel = by_type(dtype, &linear_weights_kernel<float>, &linear_weights_kernel<__nv_bfloat16>, &linear_weights_kernel<__half>);
-        KernelScope ks(ctx, KC_GEMM_WGRAD, stream);
-        launch_kernel(kernel, dim3((unsigned)a.tiles, (unsigned)ceil_div(d_out, BN), (unsigned)ceil_div(d_in, BM)), THREADS, 0, stream, a);
-    }
-    RTMA_LAUNCH_CHECK(ctx);
+    RTMA_TRY(prepare_row_call(ctx, sizeof(float) * a.tiles * (weights + BIAS_ROWS * (int64_t)d_out), stream));
+    a.out = ctx->arena;
+    if (n > 0) RTMA_TRY(launch_linear<WEIGHT_GRADIENT>(ctx, dtype, a, KC_GEMM_WGRAD, stream));
     {
         KernelScope ks(ctx, KC_REDUCE_SGD, stream);
-        launch_kernel(linear_reduce_kernel, dim3((unsigned)ceil_div(weights + d_out, THREADS), (unsigned)a.G), THREADS, 0, stream, a);
+        launch_kernel(linear_reduce_kernel, dim3((unsigned)ceil_div(weights + d_out, REDUCE_THREADS), (unsigned)a.G), REDUCE_THREADS, 0, stream, a);
     }
     RTMA_LAUNCH_CHECK(ctx);
     return RTMA_OK;
