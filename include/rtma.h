@@ -43,7 +43,7 @@ extern "C" {
 
 #define RTMA_MAX_PARTS 64
 #define RTMA_MAX_LAYERS 8
-#define RTMA_MAX_GROUPS 1024   /* parts of one call of the operators on rows (rtma_grouped_linear and below) */
+#define RTMA_MAX_GROUPS 512   /* parts of one call of the operators on rows (rtma_grouped_linear and below) */
 #define RTMA_MAX_WIDTH 16384   /* columns of one operand of rtma_grouped_linear */
 
 enum {

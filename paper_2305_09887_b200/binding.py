@@ -17,7 +17,7 @@ LIB_PATH = os.path.join(_PKG, "librtma.so")
 LIB_CHECKED_PATH = os.path.join(_PKG, "librtma_checked.so")   # built with -DRTMA_BOUNDS: every caller-supplied index checked
 MAX_PARTS = 64
 MAX_LAYERS = 8
-MAX_GROUPS = 1024
+MAX_GROUPS = 512
 
 EXPORTS = (
     "rtma_create", "rtma_destroy", "rtma_last_error", "rtma_workspace_bytes", "rtma_partition", "rtma_partition_grouped",

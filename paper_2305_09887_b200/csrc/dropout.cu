@@ -12,7 +12,7 @@ struct DropoutArgs {
     void* Y;
     int64_t n, ldx, ldr, ldy;
     int d, units;       // columns; groups of eight columns in a row
-    bool vx, vr, vy;    // rows on 16-byte boundaries
+    int vx, vr, vy;     // granules of the rows (bytes)
     DropArgs drop;
 };
 
@@ -68,8 +68,8 @@ extern "C" int32_t rtma_dropout(rtma_ctx* ctx, int32_t dtype, int64_t n, int32_t
     RTMA_CUDA(ctx, on.status);
     RTMA_TRY(prepare_row_call(ctx, 0, stream));
     const size_t es = row_type_bytes(dtype);
-    DropoutArgs a{X, residual, Y, n, ldx, ldr, ldy, d, (d + 7) / 8, aligned_rows(X, ldx, es), residual && aligned_rows(residual, ldr, es),
-                  aligned_rows(Y, ldy, es), drop_args(p, seed, row_ids)};
+    DropoutArgs a{X, residual, Y, n, ldx, ldr, ldy, d, (d + 7) / 8, row_granule(X, ldx, es), row_granule(residual, ldr, es),
+                  row_granule(Y, ldy, es), drop_args(p, seed, row_ids)};
     const int64_t blocks = ceil_div(n * a.units, 256);
     const unsigned grid = (unsigned)(blocks < (int64_t)ctx->sm_count * 32 ? blocks : (int64_t)ctx->sm_count * 32);
     auto kernel = dtype == RTMA_F32 ? dropout_kernel<float> : dtype == RTMA_BF16 ? dropout_kernel<__nv_bfloat16> : dropout_kernel<__half>;

@@ -26,7 +26,7 @@ struct NormArgs {
     const void *X, *dY;
     void* Y;  // forward: y; backward: dx
     int64_t ldx, lddy, ldy;
-    bool vx, vdy, vy;
+    int vx, vdy, vy;  // granules of the rows (bytes)
     const float *gamma, *beta, *slope;
     int64_t gamma_stride, beta_stride, slope_stride;
     DropArgs drop;
@@ -661,7 +661,7 @@ NormArgs norm_args(const rtma_ctx* ctx, const rtma_norm_desc* d, int64_t n, int3
     a.eps = d->eps;
     a.X = X;
     a.ldx = ldx;
-    a.vx = aligned_rows(X, ldx, row_type_bytes(d->dtype));
+    a.vx = row_granule(X, ldx, row_type_bytes(d->dtype));
     a.gamma = gamma;
     a.beta = beta;
     a.slope = d->act == RTMA_ACT_PRELU ? slope : nullptr;
@@ -689,7 +689,7 @@ extern "C" int32_t rtma_group_norm(rtma_ctx* ctx, const rtma_norm_desc* d, int64
     NormArgs a = norm_args(ctx, d, n, G, offsets, X, ldx, gamma, beta, slope, row_ids);
     a.Y = Y;
     a.ldy = ldy;
-    a.vy = aligned_rows(Y, ldy, row_type_bytes(d->dtype));
+    a.vy = row_granule(Y, ldy, row_type_bytes(d->dtype));
     a.stats = stats;
     const int64_t tiles = a.tiles;
     const size_t piece_bytes = rows ? 0 : ArenaCursor::granule(sizeof(float2) * tiles * a.groups);
@@ -740,10 +740,10 @@ extern "C" int32_t rtma_group_norm_grad(rtma_ctx* ctx, const rtma_norm_desc* d, 
     NormArgs a = norm_args(ctx, d, n, G, offsets, X, ldx, gamma, beta, slope, row_ids);
     a.dY = dY;
     a.lddy = lddy;
-    a.vdy = aligned_rows(dY, lddy, row_type_bytes(d->dtype));
+    a.vdy = row_granule(dY, lddy, row_type_bytes(d->dtype));
     a.Y = dX;
     a.ldy = lddx;
-    a.vy = aligned_rows(dX, lddx, row_type_bytes(d->dtype));
+    a.vy = row_granule(dX, lddx, row_type_bytes(d->dtype));
     a.stats = const_cast<float*>(stats);
     a.dgamma = dgamma; a.dgamma_stride = dgamma_stride;
     a.dbeta = dbeta; a.dbeta_stride = dbeta_stride;

@@ -12,8 +12,12 @@
 // result is fp32 the drain warps therefore take the accumulator after every 64 terms and add it up in registers, rounded to nearest;
 // inside 64 terms the five small products of fp32 operands come first.
 //
-// Warps: 0-7 drain (a quarter of the lanes, every second 32 columns each), 8-15 load, 16 issues the MMAs (17-19 complete its group
-// of four).
+// Three ways of loading (Loading below), and the warps that go with them:
+//   SPLIT   fp32: 8 warps per operand bring values through registers and split them; 8 drain warps; one warp multiplies
+//   COPIES  16-bit rows that do not all lie on 16-byte boundaries: the same warps with asynchronous copies of 16, 8 or 4 bytes
+//   BULK    16-bit rows on 16-byte boundaries: one thread with bulk-tensor loads; 8 drain warps; one warp multiplies
+#include <algorithm>
+
 #include "rows.cuh"
 #include "tc_common.cuh"
 
@@ -23,28 +27,32 @@ namespace {
 
 enum Mode { FORWARD, INPUT_GRADIENT, WEIGHT_GRADIENT };
 
+enum Loading { SPLIT, COPIES, BULK };
+
 constexpr int BM = 128, BK = 64;
-constexpr int DRAIN_WARPS = 8, LOAD_WARPS = 8, WARPS = DRAIN_WARPS + LOAD_WARPS + 4, THREADS = 32 * WARPS;
-// A block is launched with 96 registers a thread (640 of them); the four warps of the multiplier give theirs up to the others:
-// 256 x 120 + 256 x 104 + 128 x 24 = 60,416 of 61,440.
-constexpr int DRAIN_REGISTERS = 120, LOAD_REGISTERS = 104, MULTIPLY_REGISTERS = 24;
+constexpr int DRAIN_WARPS = 8, OPERAND_WARPS = 8;  // of each operand
+// A block of the first two ways is launched with 72 registers a thread (28 warps); the multiplier's four give theirs up to the
+// others: 256 x 104 + 512 x 64 + 128 x 24 = 62,464 of 64,512.
+constexpr int DRAIN_REGISTERS = 104, LOAD_REGISTERS = 64, MULTIPLY_REGISTERS = 24;
 constexpr int SLAB_BYTES = 32 * 128;       // 32 rows of 64 16-bit values
 constexpr int OUT_PITCH = 80, OUT_BYTES = 32 * OUT_PITCH;  // a drain warp's 32 rows of 64 bytes on their way out
 constexpr int RING_BYTES = 192 * 1024;
 constexpr int DYNAMIC_BYTES = RING_BYTES + 1024 + DRAIN_WARPS * OUT_BYTES;
-constexpr int BIAS_ROWS = LOAD_WARPS;      // partial sums of the bias gradient in a slot, one row per loading warp
+constexpr int BIAS_ROWS = 8;               // partial sums of the bias gradient in a slot, one row per warp that adds them up
 constexpr int MAX_STAGES = 6;
 
-template <class T, int MODE>
+template <class T, int MODE, int LOADING>
 struct Form {
-    static constexpr bool SPLIT = sizeof(T) == 4;
-    static constexpr int PLANES = SPLIT ? 3 : 1;
-    static constexpr bool IN_REGISTERS = SPLIT || MODE == WEIGHT_GRADIENT;  // accumulated there, 64 terms at a time
-    static constexpr int BN = IN_REGISTERS ? 128 : 256;                     // widest tile
-    static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128;            // of a plane
+    static constexpr int PLANES = LOADING == SPLIT ? 3 : 1;
+    static constexpr bool IN_REGISTERS = LOADING == SPLIT || MODE == WEIGHT_GRADIENT;  // accumulated there, 64 terms at a time
+    static constexpr int BN = IN_REGISTERS ? 128 : 256;                                // widest tile
+    static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128;                       // of a plane
     static constexpr int STAGE_BYTES = PLANES * (A_BYTES + B_BYTES);
     static constexpr int STAGES = RING_BYTES / STAGE_BYTES;
     static constexpr bool A_ACROSS = MODE == WEIGHT_GRADIENT, B_ACROSS = MODE != INPUT_GRADIENT;  // MN-major
+    static constexpr bool DRAIN_SUMS = LOADING == BULK && MODE == WEIGHT_GRADIENT;     // the drain warps add up the columns of dY
+    static constexpr int LOAD_WARPS = LOADING == BULK ? 0 : 2 * OPERAND_WARPS;
+    static constexpr int THREADS = 32 * (DRAIN_WARPS + LOAD_WARPS + 4);
 };
 
 struct LinearArgs {
@@ -57,7 +65,8 @@ struct LinearArgs {
     int d_in, d_out;
     const void *A, *B;         // rows; matrices (forward, dx) or rows (dw)
     int64_t lda, ldb, w_stride;
-    bool va, vb, vo;           // rows on 16-byte boundaries
+    int va, vb;                // granules of the rows (bytes)
+    bool vo;                   // rows of the result on 16-byte boundaries
     const void* bias;
     int64_t bias_stride;
     void* out;                 // dw: the slots, [row tile][(d_in + BIAS_ROWS) * d_out]
@@ -65,6 +74,7 @@ struct LinearArgs {
     float *dW, *db;
     int64_t dw_stride, db_stride;
     int* error_word;
+    CUtensorMap map_a, map_b;  // BULK
 };
 
 struct Shared {
@@ -74,6 +84,7 @@ struct Shared {
     int abort;
     int32_t warp_sums[32];
     int32_t tile_start[RTMA_MAX_GROUPS + 1], begin[RTMA_MAX_GROUPS], rows[RTMA_MAX_GROUPS];
+    float bias[DRAIN_WARPS][128];  // of a warp's columns
 };
 
 __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, Shared& sh, int* error_word) {
@@ -157,8 +168,19 @@ __device__ __forceinline__ const T* source_b(const LinearArgs& a, const Walk<MOD
     }
 }
 
-__device__ __forceinline__ void copy_16(uint32_t dst, const void* src, int bytes) {  // the rest of the 16 bytes becomes zero
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+template <int SIZE>
+__device__ __forceinline__ void copy(uint32_t dst, const void* src, int bytes) {  // the rest of the SIZE bytes becomes zero
+    if constexpr (SIZE == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(dst), "l"(src), "r"(bytes), "n"(SIZE) : "memory");
+}
+// 16 bytes of which `bytes` exist, from a multiple of SIZE
+template <int SIZE>
+__device__ __forceinline__ void copy_pieces(uint32_t dst, const void* src, int bytes) {
+#pragma unroll
+    for (int i = 0; i < 16 / SIZE; ++i) {
+        const int here = max(0, min(SIZE, bytes - i * SIZE));
+        copy<SIZE>(dst + i * SIZE, here ? static_cast<const char*>(src) + i * SIZE : src, here);
+    }
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -172,49 +194,26 @@ __device__ __forceinline__ uint4 load_16(uint32_t src) {
     return v;
 }
 
-// Eight fp32 values as three bf16 numbers each, x = h + m + l exactly (l rounds only where x has bits below the smallest bf16
-// number).  Values that round to an infinity are cut instead; what is not finite stays in h alone.
-__device__ __forceinline__ void split_eight(const float (&x)[8], uint4 (&planes)[3]) {
-    uint32_t big = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) big = max(big, __float_as_uint(x[j]) & 0x7FFFFFFFu);
+// Eight fp32 values as three bf16 numbers each, x = h + m + l exactly (but for bits below the smallest bf16 number).  h is cut off
+// so that no finite value becomes an infinity, m is rounded to nearest so that the products left out (m l, l m, l l: below 2^-22 of
+// the product) have no preferred sign.  An infinity or NaN leaves NaN in m.
+__device__ __forceinline__ void split_eight(const uint32_t (&x)[8], uint4 (&planes)[3]) {
     uint32_t h[4], m[4], l[4];
-    if (big < 0x7F7F8000u) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 a = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-            h[i] = *reinterpret_cast<const uint32_t*>(&a);
-            const float r0 = x[2 * i] - __uint_as_float(h[i] << 16), r1 = x[2 * i + 1] - __uint_as_float(h[i] & 0xFFFF0000u);
-            const __nv_bfloat162 b = __floats2bfloat162_rn(r0, r1);
-            m[i] = *reinterpret_cast<const uint32_t*>(&b);
-            const __nv_bfloat162 c = __floats2bfloat162_rn(r0 - __uint_as_float(m[i] << 16), r1 - __uint_as_float(m[i] & 0xFFFF0000u));
-            l[i] = *reinterpret_cast<const uint32_t*>(&c);
-        }
-    } else {
-        for (int i = 0; i < 4; ++i) {
-            h[i] = m[i] = l[i] = 0;
-            for (int k = 0; k < 2; ++k) {
-                const float v = x[2 * i + k];
-                const uint32_t u = __float_as_uint(v), mag = u & 0x7FFFFFFFu;
-                uint32_t a = mag > 0x7F800000u ? 0x7FC0u : u >> 16, b = 0, c = 0;
-                if (mag < 0x7F7F8000u) a = __bfloat16_as_ushort(__float2bfloat16_rn(v));
-                if (mag < 0x7F800000u) {
-                    const float r = v - __uint_as_float(a << 16);
-                    b = __bfloat16_as_ushort(__float2bfloat16_rn(r));
-                    c = __bfloat16_as_ushort(__float2bfloat16_rn(r - __uint_as_float(b << 16)));
-                }
-                h[i] |= a << 16 * k;
-                m[i] |= b << 16 * k;
-                l[i] |= c << 16 * k;
-            }
-        }
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t a = x[2 * i], b = x[2 * i + 1];
+        h[i] = __byte_perm(a, b, 0x7632);
+        const float r0 = __uint_as_float(a) - __uint_as_float(a & 0xFFFF0000u), r1 = __uint_as_float(b) - __uint_as_float(b & 0xFFFF0000u);
+        const __nv_bfloat162 t = __floats2bfloat162_rn(r0, r1);
+        m[i] = *reinterpret_cast<const uint32_t*>(&t);
+        l[i] = __byte_perm(__float_as_uint(r0 - __uint_as_float(m[i] << 16)), __float_as_uint(r1 - __uint_as_float(m[i] & 0xFFFF0000u)), 0x7632);
     }
     planes[0] = make_uint4(h[0], h[1], h[2], h[3]);
     planes[1] = make_uint4(m[0], m[1], m[2], m[3]);
     planes[2] = make_uint4(l[0], l[1], l[2], l[3]);
 }
 
-// Sums over a loading warp's rows of the columns of dY that its lanes hold, written to the warp's row of the slot.
+// Sums over a warp's rows of the columns of dY that its lanes hold, written to the warp's row of the slot.
 __device__ __forceinline__ void leave_bias(const LinearArgs& a, const Walk<WEIGHT_GRADIENT>& w, float (&sums)[2][8], int warp, int lane) {
     float* to = static_cast<float*>(a.out) + ((int64_t)w.row_tile * (a.d_in + BIAS_ROWS) + a.d_in + warp) * a.d_out;
 #pragma unroll
@@ -230,102 +229,101 @@ __device__ __forceinline__ void leave_bias(const LinearArgs& a, const Walk<WEIGH
         }
 }
 
-template <class T, int MODE>
-__device__ __forceinline__ void load_role(const LinearArgs& a, Shared& sh, uint32_t ring) {
-    typedef Form<T, MODE> F;
-    const int t = threadIdx.x - 32 * DRAIN_WARPS, row = t >> 3, unit = t & 7, lane = t & 31, warp = t >> 5;
-    const uint32_t place = row * 128 + ((unit ^ (row & 7)) << 4);  // inside a slab; 32-row slabs do not change row mod 8
-    const int b_slabs = F::B_ACROSS ? 2 * ((a.BN + 63) / 64) : (a.BN + 31) / 32;
-    float sums[2][8];
+__device__ __forceinline__ void add_eight(float (&sums)[8], const float (&v)[8]) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 8; ++j) sums[j] += v[j];
+}
+
+// The warps of one operand (t: 0..255).
+template <class T, int MODE, int LOADING, bool IS_B>
+__device__ __forceinline__ void load_role(const LinearArgs& a, Shared& sh, uint32_t ring, int t) {
+    typedef Form<T, MODE, LOADING> F;
+    const int row = t >> 3, unit = t & 7, lane = t & 31, warp = t >> 5;
+    // a thread's 16 bytes inside a slab (32-row slabs do not change row mod 8)
+    const uint32_t place = (IS_B ? F::PLANES * F::A_BYTES : 0) + row * 128 + ((unit ^ (row & 7)) << 4);
+    constexpr int MOST = (IS_B ? F::BN : BM) / 32;
+    const int slabs = !IS_B ? MOST : F::B_ACROSS ? 2 * ((a.BN + 63) / 64) : (a.BN + 31) / 32;
+    const int granule = IS_B ? a.vb : a.va;
+    auto source = [&](const Walk<MODE>& w, int i, int& valid) {
+        if constexpr (IS_B) return source_b<T, MODE>(a, w, i, row, unit, valid);
+        else return source_a<T, MODE>(a, w, i, row, unit, valid);
+    };
+    constexpr bool SUMS = IS_B && MODE == WEIGHT_GRADIENT;
+    float sums[SUMS ? 2 : 1][8];
+    if constexpr (SUMS) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sums[i][j] = 0.f;
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sums[i][j] = 0.f;
+    }
     Walk<MODE> w;
     bool more = w.first(a, sh);
     tc::RingAt at;
-    if constexpr (F::SPLIT) {
-        // Values wait in registers for their stage: while one operand's are split the other's are on their way.
-        Eight<T> ra[4], rb[4];
+    if constexpr (LOADING == SPLIT) {
+        // A stage's values wait in registers; as soon as one piece is split, the next stage's is on its way.
+        Eight<T> held[MOST];
         if (more) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < MOST; ++i) {
                 int valid;
-                const T* p = source_a<T, MODE>(a, w, i, row, unit, valid);
-                ra[i].load(p, valid, a.va);
+                if (i < slabs) {
+                    const T* p = source(w, i, valid);
+                    held[i].load(p, valid, granule);
+                }
             }
         }
         while (more) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                int valid = 0;
-                const T* p = nullptr;
-                if (i < b_slabs) p = source_b<T, MODE>(a, w, i, row, unit, valid);
-                if (i < b_slabs) rb[i].load(p, valid, a.vb);
-            }
+            const bool wanted = SUMS && w.m0 == 0 && a.db, last = w.last_stage();
+            const Walk<MODE> here = w;
+            more = w.next(a, sh);
             if (!wait_for(&sh.empty[at.s], at.phase ^ 1u, sh, a.error_word)) return;
             const uint32_t stage = ring + at.s * F::STAGE_BYTES + place;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float v[8];
-                uint4 planes[3];
-                ra[i].values(v);
-                split_eight(v, planes);
-#pragma unroll
-                for (int k = 0; k < 3; ++k) store_16(stage + k * F::A_BYTES + i * SLAB_BYTES, planes[k]);
-            }
-            const bool sums_wanted = MODE == WEIGHT_GRADIENT && w.m0 == 0 && a.db;
-            const Walk<MODE> here = w;
-            more = w.next(a, sh);
-            if (more) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    int valid;
-                    const T* p = source_a<T, MODE>(a, w, i, row, unit, valid);
-                    ra[i].load(p, valid, a.va);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (i < b_slabs) {
-                    float v[8];
+            for (int i = 0; i < MOST; ++i) {
+                if (i < slabs) {
                     uint4 planes[3];
-                    rb[i].values(v);
-                    if (sums_wanted) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) sums[i >> 1][j] += v[j];
+                    if constexpr (SUMS) {
+                        if (wanted) {
+                            float v[8];
+                            held[i].values(v);
+                            add_eight(sums[i >> 1], v);
+                        }
                     }
-                    split_eight(v, planes);
+                    split_eight(reinterpret_cast<const uint32_t(&)[8]>(held[i].w), planes);
 #pragma unroll
-                    for (int k = 0; k < 3; ++k) store_16(stage + 3 * F::A_BYTES + k * F::B_BYTES + i * SLAB_BYTES, planes[k]);
+                    for (int k = 0; k < 3; ++k) store_16(stage + k * (IS_B ? F::B_BYTES : F::A_BYTES) + i * SLAB_BYTES, planes[k]);
+                    if (more) {
+                        int valid;
+                        const T* p = source(w, i, valid);
+                        held[i].load(p, valid, granule);
+                    }
                 }
             }
             tc::fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(&sh.full[at.s]);
             at.advance(F::STAGES);
-            if constexpr (MODE == WEIGHT_GRADIENT)
-                if (sums_wanted && here.last_stage()) leave_bias(a, here, sums, warp, lane);
+            if constexpr (SUMS)
+                if (wanted && last) leave_bias(a, here, sums, warp, lane);
         }
     } else {
-        // 16-byte copies straight into the stage; a stage is handed over once this thread's copies of it have landed, LAG stages later.
-        constexpr int LAG = F::STAGES - 2;  // stages whose copies are under way behind the newest
+        // Copies straight into the stage; it is handed over once this thread's copies have landed, LAG stages later.
+        constexpr int LAG = F::STAGES - 2;
         Walk<MODE> late = w;
         tc::RingAt late_at;
         int under_way = 0;
         auto hand_over = [&]() {
-            if constexpr (MODE == WEIGHT_GRADIENT) {
+            if constexpr (SUMS) {
                 if (late.m0 == 0 && a.db) {
-                    const uint32_t stage = ring + late_at.s * F::STAGE_BYTES + F::PLANES * F::A_BYTES + place;
+                    const uint32_t stage = ring + late_at.s * F::STAGE_BYTES + place;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (i < b_slabs) {
+                    for (int i = 0; i < MOST; ++i) {
+                        if (i < slabs) {
                             Eight<T> e;
                             e.w[0] = load_16(stage + i * SLAB_BYTES);
                             float v[8];
                             e.values(v);
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) sums[i >> 1][j] += v[j];
+                            add_eight(sums[i >> 1], v);
                         }
                     }
                     if (late.last_stage()) leave_bias(a, late, sums, warp, lane);
@@ -343,28 +341,18 @@ __device__ __forceinline__ void load_role(const LinearArgs& a, Shared& sh, uint3
             ok = wait_for(&sh.empty[at.s], at.phase ^ 1u, sh, a.error_word);
             if (!ok) break;
             const uint32_t stage = ring + at.s * F::STAGE_BYTES + place;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                int valid;
-                const T* p = source_a<T, MODE>(a, w, i, row, unit, valid);
-                if (a.va) {
-                    copy_16(stage + i * SLAB_BYTES, p, valid * (int)sizeof(T));
-                } else {
-                    Eight<T> e;
-                    e.load(p, valid, false);
-                    store_16(stage + i * SLAB_BYTES, e.w[0]);
-                }
-            }
 #pragma unroll 4
-            for (int i = 0; i < b_slabs; ++i) {
+            for (int i = 0; i < slabs; ++i) {
                 int valid;
-                const T* p = source_b<T, MODE>(a, w, i, row, unit, valid);
-                if (a.vb) {
-                    copy_16(stage + F::A_BYTES + i * SLAB_BYTES, p, valid * (int)sizeof(T));
-                } else {
+                const T* p = source(w, i, valid);
+                const uint32_t to = stage + i * SLAB_BYTES;
+                if (granule == 16) copy_pieces<16>(to, p, valid * (int)sizeof(T));
+                else if (granule == 8) copy_pieces<8>(to, p, valid * (int)sizeof(T));
+                else if (granule == 4) copy_pieces<4>(to, p, valid * (int)sizeof(T));
+                else {
                     Eight<T> e;
-                    e.load(p, valid, false);
-                    store_16(stage + F::A_BYTES + i * SLAB_BYTES, e.w[0]);
+                    e.load(p, valid, granule);
+                    store_16(to, e.w[0]);
                 }
             }
             copies_commit();
@@ -381,9 +369,60 @@ __device__ __forceinline__ void load_role(const LinearArgs& a, Shared& sh, uint3
     }
 }
 
+// One warp with bulk-tensor loads.  Rows behind the end of a tile belong to the next part: they only reach results that are not
+// written, but in the weight gradient they would be summed, so the last rows of a part are copied by the warp's lanes, with zeros
+// behind them.
 template <class T, int MODE>
+__device__ __forceinline__ void bulk_role(const LinearArgs& a, Shared& sh, uint8_t* ring, int lane) {
+    typedef Form<T, MODE, BULK> F;
+    const uint32_t b_bytes = F::B_ACROSS ? (uint32_t)((a.BN + 63) / 64) * 2 * SLAB_BYTES : (uint32_t)a.BN * 128u;
+    if (lane == 0) {
+        tc::prefetch_tensormap(&a.map_a);
+        tc::prefetch_tensormap(&a.map_b);
+    }
+    Walk<MODE> w;
+    tc::RingAt at;
+    for (bool more = w.first(a, sh); more; more = w.next(a, sh), at.advance(F::STAGES)) {
+        if (!wait_for(&sh.empty[at.s], at.phase ^ 1u, sh, a.error_word)) return;
+        uint8_t* stage = ring + at.s * F::STAGE_BYTES;
+        uint64_t* bar = &sh.full[at.s];
+        if (MODE == WEIGHT_GRADIENT && w.k0 + BK > w.k_end) {
+            const int slabs = 2 * ((a.BN + 63) / 64);
+            for (int j = lane; j < (4 + slabs) * 256; j += 32) {
+                const int i = j >> 8, row = (j >> 3) & 31, unit = j & 7;
+                int valid;
+                const T* p = i < 4 ? source_a<T, MODE>(a, w, i, row, unit, valid) : source_b<T, MODE>(a, w, i - 4, row, unit, valid);
+                copy<16>(tc::smem_u32(stage) + i * SLAB_BYTES + row * 128 + ((unit ^ (row & 7)) << 4), p, valid * (int)sizeof(T));
+            }
+            copies_commit();
+            copies_wait<0>();
+            tc::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(bar);
+        } else if (lane == 0) {
+            tc::mbar_arrive_expect_tx(bar, F::A_BYTES + b_bytes);
+            uint8_t* b = stage + F::A_BYTES;
+            if constexpr (MODE == WEIGHT_GRADIENT) {
+                const int r = (int)w.row0 + w.k0;
+                for (int i = 0; i < 2; ++i) tc::tma_load_3d(stage + 2 * i * SLAB_BYTES, &a.map_a, bar, w.m0 + 64 * i, r, 0);
+                for (int i = 0; 64 * i < a.BN; ++i) tc::tma_load_3d(b + 2 * i * SLAB_BYTES, &a.map_b, bar, w.n0 + 64 * i, r, 0);
+            } else {
+                const int z = a.w_stride ? w.part : 0;
+                tc::tma_load_3d(stage, &a.map_a, bar, w.k0, (int)w.row0, 0);
+                if constexpr (MODE == FORWARD) {
+                    for (int i = 0; 64 * i < a.BN; ++i) tc::tma_load_3d(b + 2 * i * SLAB_BYTES, &a.map_b, bar, w.n0 + 64 * i, w.k0, z);
+                } else {
+                    tc::tma_load_3d(b, &a.map_b, bar, w.k0, w.n0, z);
+                }
+            }
+        }
+        __syncwarp();
+    }
+}
+
+template <class T, int MODE, int LOADING>
 __device__ __forceinline__ void multiply_role(const LinearArgs& a, Shared& sh, uint32_t ring) {
-    typedef Form<T, MODE> F;
+    typedef Form<T, MODE, LOADING> F;
     const uint32_t format = std::is_same<T, __half>::value ? 0u : 1u;  // fp16 or bf16 operands, fp32 sums
     const uint32_t idesc = (1u << 4) | (format << 7) | (format << 10) | ((F::A_ACROSS ? 1u : 0u) << 15) | ((F::B_ACROSS ? 1u : 0u) << 16) |
                            ((uint32_t)(a.BN >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
@@ -403,7 +442,7 @@ __device__ __forceinline__ void multiply_role(const LinearArgs& a, Shared& sh, u
         const uint32_t sa = (ring + at.s * F::STAGE_BYTES) >> 4, sb = sa + F::PLANES * a_plane;
         const int steps = (min(BK, w.k_end - w.k0) + 15) >> 4;
         uint32_t accumulate = F::IN_REGISTERS || w.k0 == 0 ? 0u : 1u;
-        if constexpr (F::SPLIT) {
+        if constexpr (LOADING == SPLIT) {
             for (int k = 0; k < steps; ++k) {
                 const uint64_t da = desc + sa + k * a_step, db = desc + sb + k * b_step;
                 tc::mma_bf16(d, da + 2 * a_plane, db, idesc, accumulate);
@@ -473,14 +512,22 @@ __device__ __forceinline__ void write_out(O* out, int64_t ldo, bool vec, const f
     }
 }
 
-template <class T, int MODE>
-__device__ __forceinline__ void drain_role(const LinearArgs& a, Shared& sh, uint32_t slabs) {
-    typedef Form<T, MODE> F;
+template <class T, int MODE, int LOADING>
+__device__ __forceinline__ void drain_role(const LinearArgs& a, Shared& sh, uint32_t slabs, uint32_t ring) {
+    typedef Form<T, MODE, LOADING> F;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, half = warp >> 2;
     const uint32_t slab = slabs + warp * OUT_BYTES, lanes = (uint32_t)(32 * quarter) << 16;
     const int chunks = (a.BN + 31) / 32;
     Walk<MODE> w;
-    tc::RingAt acc;
+    tc::RingAt acc, at;
+    int bias_part = -1, bias_n0 = -1;
+    float sums[F::DRAIN_SUMS ? 2 : 1][8];
+    if constexpr (F::DRAIN_SUMS) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sums[i][j] = 0.f;
+    }
     for (bool more = w.first(a, sh); more; more = w.next_tile(a, sh)) {
         const int N = MODE == INPUT_GRADIENT ? a.d_in : a.d_out;
         const int out_rows = max(0, (MODE == WEIGHT_GRADIENT ? min(BM, a.d_in - w.m0) : w.rows) - 32 * quarter);
@@ -492,13 +539,23 @@ __device__ __forceinline__ void drain_role(const LinearArgs& a, Shared& sh, uint
                 write_out<float>(out, a.d_out, a.vo, v, slab, min(32, out_rows), cols, lane);
             } else {
                 if (MODE == FORWARD && a.bias) {
-                    const T* bias = static_cast<const T*>(a.bias) + w.part * a.bias_stride + c;
+                    const float* bias = &sh.bias[warp][32 * (chunk >> 1)];
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] += j < cols ? to_f32(bias[j]) : 0.f;
+                    for (int j = 0; j < 32; ++j) v[j] += bias[j];
                 }
                 write_out<T>(static_cast<T*>(a.out) + (w.row0 + 32 * quarter) * a.ldo + c, a.ldo, a.vo, v, slab, min(32, out_rows), cols, lane);
             }
         };
+        if (MODE == FORWARD && a.bias && (w.part != bias_part || w.n0 != bias_n0)) {
+            const T* bias = static_cast<const T*>(a.bias) + w.part * a.bias_stride + w.n0;
+            for (int chunk = half; chunk < chunks; chunk += 2) {
+                const int c = 32 * chunk + lane;
+                sh.bias[warp][32 * (chunk >> 1) + lane] = c < a.BN && w.n0 + c < N ? to_f32(bias[c]) : 0.f;
+            }
+            bias_part = w.part;
+            bias_n0 = w.n0;
+            __syncwarp();
+        }
         if constexpr (F::IN_REGISTERS) {
             float total[2][32];
 #pragma unroll
@@ -522,7 +579,31 @@ __device__ __forceinline__ void drain_role(const LinearArgs& a, Shared& sh, uint
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(&sh.acc_empty[acc.s]);
                 acc.advance(2);
+                if constexpr (F::DRAIN_SUMS) {
+                    if (a.db) {  // the stage is given back by the warps that add up its columns as well
+                        if (w.m0 == 0) {
+                            if (!wait_for(&sh.full[at.s], at.phase, sh, a.error_word)) return;
+                            const int t = threadIdx.x, row = t >> 3, unit = t & 7;
+                            const uint32_t stage = ring + at.s * F::STAGE_BYTES + F::A_BYTES + row * 128 + ((unit ^ (row & 7)) << 4);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                if (i < 2 * ((a.BN + 63) / 64)) {
+                                    Eight<T> e;
+                                    e.w[0] = load_16(stage + i * SLAB_BYTES);
+                                    float v[8];
+                                    e.values(v);
+                                    add_eight(sums[i >> 1], v);
+                                }
+                            }
+                            __syncwarp();
+                        }
+                        if (lane == 0) tc::mbar_arrive(&sh.empty[at.s]);
+                        at.advance(F::STAGES);
+                    }
+                }
             }
+            if constexpr (F::DRAIN_SUMS)
+                if (a.db && w.m0 == 0) leave_bias(a, w, sums, warp, lane);
 #pragma unroll
             for (int i = 0; i < 2; ++i)
                 if (half + 2 * i < chunks) put(total[i], half + 2 * i);
@@ -543,17 +624,19 @@ __device__ __forceinline__ void drain_role(const LinearArgs& a, Shared& sh, uint
     }
 }
 
-template <class T, int MODE>
-__global__ void __launch_bounds__(THREADS, 1) linear_kernel(const __grid_constant__ LinearArgs a) {
-    typedef Form<T, MODE> F;
+template <class T, int MODE, int LOADING>
+__global__ void __launch_bounds__(Form<T, MODE, LOADING>::THREADS, 1) linear_kernel(const __grid_constant__ LinearArgs a) {
+    typedef Form<T, MODE, LOADING> F;
     extern __shared__ uint8_t raw[];
     __shared__ Shared sh;
-    const uint32_t ring = (tc::smem_u32(raw) + 1023u) & ~1023u, slabs = ring + RING_BYTES;
-    const int warp = threadIdx.x >> 5;
+    uint8_t* ring_bytes = raw + ((1024u - (tc::smem_u32(raw) & 1023u)) & 1023u);
+    const uint32_t ring = tc::smem_u32(ring_bytes), slabs = ring + RING_BYTES;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr int MULTIPLIER = DRAIN_WARPS + F::LOAD_WARPS;
     if (threadIdx.x == 0) {
         for (int s = 0; s < F::STAGES; ++s) {
-            tc::mbar_init(&sh.full[s], LOAD_WARPS);
-            tc::mbar_init(&sh.empty[s], 1);
+            tc::mbar_init(&sh.full[s], LOADING == BULK ? 1 : F::LOAD_WARPS);
+            tc::mbar_init(&sh.empty[s], 1 + (F::DRAIN_SUMS && a.db ? DRAIN_WARPS : 0));
         }
         for (int b = 0; b < 2; ++b) {
             tc::mbar_init(&sh.acc_full[b], 1);
@@ -562,12 +645,12 @@ __global__ void __launch_bounds__(THREADS, 1) linear_kernel(const __grid_constan
         sh.abort = 0;
         tc::fence_barrier_init();
     }
-    if (warp == WARPS - 1) {
+    if (warp == MULTIPLIER) {
         tc::tmem_alloc(&sh.tmem_base, 2 * F::BN);
         tc::tmem_relinquish();
     }
     wait_for_kernel_before();
-    for (int g = threadIdx.x; g < a.G; g += THREADS) {
+    for (int g = threadIdx.x; g < a.G; g += F::THREADS) {
         int64_t begin, end;
         part_rows(a.offsets, a.n, g, begin, end, a.span);
         sh.begin[g] = (int32_t)begin;
@@ -578,19 +661,24 @@ __global__ void __launch_bounds__(THREADS, 1) linear_kernel(const __grid_constan
     __syncthreads();
     tc::tc_fence_after_sync();
     if (warp < DRAIN_WARPS) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(DRAIN_REGISTERS));
-        drain_role<T, MODE>(a, sh, slabs);
-    } else if (warp < DRAIN_WARPS + LOAD_WARPS) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(LOAD_REGISTERS));
-        load_role<T, MODE>(a, sh, ring);
+        if constexpr (LOADING != BULK) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(DRAIN_REGISTERS));
+        drain_role<T, MODE, LOADING>(a, sh, slabs, ring);
+    } else if (warp < MULTIPLIER) {
+        if constexpr (LOADING != BULK) {
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(LOAD_REGISTERS));
+            if (warp < DRAIN_WARPS + OPERAND_WARPS) load_role<T, MODE, LOADING, false>(a, sh, ring, threadIdx.x - 32 * DRAIN_WARPS);
+            else load_role<T, MODE, LOADING, true>(a, sh, ring, threadIdx.x - 32 * (DRAIN_WARPS + OPERAND_WARPS));
+        }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(MULTIPLY_REGISTERS));
-        if (warp == DRAIN_WARPS + LOAD_WARPS && (threadIdx.x & 31) == 0) multiply_role<T, MODE>(a, sh, ring);
+        if constexpr (LOADING != BULK) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(MULTIPLY_REGISTERS));
+        if (warp == MULTIPLIER && lane == 0) multiply_role<T, MODE, LOADING>(a, sh, ring);
+        if constexpr (LOADING == BULK)
+            if (warp == MULTIPLIER + 1) bulk_role<T, MODE>(a, sh, ring_bytes, lane);
     }
     __syncwarp();
     tc::tc_fence_before_sync();
     __syncthreads();
-    if (warp == WARPS - 1) {
+    if (warp == MULTIPLIER) {
         tc::tc_fence_after_sync();
         tc::tmem_dealloc(sh.tmem_base, 2 * F::BN);
     }
@@ -620,9 +708,6 @@ __global__ void __launch_bounds__(REDUCE_THREADS) linear_reduce_kernel(const __g
     }
 }
 
-template <class K>
-K by_type(int32_t dtype, K f32, K bf16, K f16) { return dtype == RTMA_F32 ? f32 : dtype == RTMA_BF16 ? bf16 : f16; }
-
 // Columns in equal tiles of a multiple of 16.
 void cut_columns(LinearArgs& a, int N, int widest) {
     a.n_tiles = (int)ceil_div(N, widest);
@@ -630,21 +715,45 @@ void cut_columns(LinearArgs& a, int N, int widest) {
     a.n_tiles = (int)ceil_div(N, a.BN);
 }
 
+template <class T, int MODE, int LOADING>
+int32_t launch_form(rtma_ctx* ctx, const LinearArgs& a, unsigned grid, bool& configured, cudaStream_t stream) {
+    if (!configured) {
+        RTMA_CUDA(ctx, cudaFuncSetAttribute(linear_kernel<T, MODE, LOADING>, cudaFuncAttributeMaxDynamicSharedMemorySize, DYNAMIC_BYTES));
+        configured = true;
+    }
+    launch_kernel(linear_kernel<T, MODE, LOADING>, grid, Form<T, MODE, LOADING>::THREADS, DYNAMIC_BYTES, stream, a);
+    RTMA_LAUNCH_CHECK(ctx);
+    return RTMA_OK;
+}
+
+// Whether both operands can be fetched by bulk-tensor loads; sets up their maps.
+template <int MODE>
+bool bulk_maps(LinearArgs& a, bool bf16) {
+    if (a.va != 16 || a.vb != 16) return false;
+    if (MODE == WEIGHT_GRADIENT)
+        return make_tensor_map_16bit(&a.map_a, bf16, a.A, 1, a.n, a.d_in, a.lda, a.n * a.lda, BK) &&
+               make_tensor_map_16bit(&a.map_b, bf16, a.B, 1, a.n, a.d_out, a.ldb, a.n * a.ldb, BK);
+    const int K = MODE == FORWARD ? a.d_in : a.d_out;
+    const int64_t matrix = (int64_t)a.d_in * a.d_out;
+    if (a.w_stride < 0) return false;
+    return make_tensor_map_16bit(&a.map_a, bf16, a.A, 1, a.n, K, a.lda, a.n * a.lda, BM) &&
+           make_tensor_map_16bit(&a.map_b, bf16, a.B, a.w_stride ? a.G : 1, a.d_in, a.d_out, a.d_out, a.w_stride ? a.w_stride : matrix,
+                                 MODE == FORWARD ? BK : a.BN);
+}
+
 template <int MODE>
 int32_t launch_linear(rtma_ctx* ctx, int32_t dtype, LinearArgs& a, int cls, cudaStream_t stream) {
     a.error_word = ctx->error_word;
     const int64_t tiles = a.tiles * a.m_tiles * a.n_tiles;
-    if (tiles >= (int64_t(1) << 31)) return rtma_fail(ctx, RTMA_ERR_OVERFLOW, "grouped product: %lld tiles", (long long)tiles);
-    auto kernel = by_type(dtype, &linear_kernel<float, MODE>, &linear_kernel<__nv_bfloat16, MODE>, &linear_kernel<__half, MODE>);
-    bool& configured = ctx->linear_configured[MODE * 3 + dtype];
-    if (!configured) {
-        RTMA_CUDA(ctx, cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, DYNAMIC_BYTES));
-        configured = true;
-    }
+    if (tiles >= (int64_t(1) << 30)) return rtma_fail(ctx, RTMA_ERR_OVERFLOW, "grouped product: %lld tiles", (long long)tiles);
+    const unsigned grid = (unsigned)(tiles < ctx->sm_count ? tiles : ctx->sm_count);
+    bool* configured = ctx->linear_configured + MODE * 5;
     KernelScope ks(ctx, cls, stream);
-    launch_kernel(kernel, (unsigned)(tiles < ctx->sm_count ? tiles : ctx->sm_count), THREADS, DYNAMIC_BYTES, stream, a);
-    RTMA_LAUNCH_CHECK(ctx);
-    return RTMA_OK;
+    if (dtype == RTMA_F32) return launch_form<float, MODE, SPLIT>(ctx, a, grid, configured[0], stream);
+    const bool bf16 = dtype == RTMA_BF16;
+    if (bulk_maps<MODE>(a, bf16))
+        return bf16 ? launch_form<__nv_bfloat16, MODE, BULK>(ctx, a, grid, configured[1], stream) : launch_form<__half, MODE, BULK>(ctx, a, grid, configured[2], stream);
+    return bf16 ? launch_form<__nv_bfloat16, MODE, COPIES>(ctx, a, grid, configured[3], stream) : launch_form<__half, MODE, COPIES>(ctx, a, grid, configured[4], stream);
 }
 
 int32_t check_linear(rtma_ctx* ctx, const char* who, int32_t dtype, int64_t n, int32_t G, const int64_t* offsets, int32_t d_in, int32_t d_out) {
@@ -677,10 +786,10 @@ int32_t run_rows(rtma_ctx* ctx, const char* who, bool transposed, int32_t dtype,
     cut_columns(a, N, dtype == RTMA_F32 ? 128 : 256);
     a.d_in = d_in; a.d_out = d_out;
     a.A = A; a.lda = lda; a.B = W; a.w_stride = w_stride; a.bias = b; a.bias_stride = b_stride;
-    a.va = aligned_rows(A, lda, es);
-    a.vb = aligned_rows(W, d_out, es) && (w_stride * (int64_t)es) % 16 == 0;
+    a.va = row_granule(A, lda, es);
+    a.vb = std::min(row_granule(W, d_out, es), row_granule(nullptr, w_stride, es));
     a.out = out; a.ldo = ldo;
-    a.vo = aligned_rows(out, ldo, es);
+    a.vo = row_granule(out, ldo, es) == 16;
     return transposed ? launch_linear<INPUT_GRADIENT>(ctx, dtype, a, KC_GEMM_DGRAD, stream) : launch_linear<FORWARD>(ctx, dtype, a, KC_GEMM_FWD, stream);
 }
 
@@ -726,8 +835,8 @@ extern "C" int32_t rtma_grouped_linear_dw(rtma_ctx* ctx, int32_t dtype, int64_t 
     const size_t es = row_type_bytes(dtype);
     a.d_in = d_in; a.d_out = d_out;
     a.A = X; a.lda = ldx; a.B = dY; a.ldb = lddy;
-    a.va = aligned_rows(X, ldx, es);
-    a.vb = aligned_rows(dY, lddy, es);
+    a.va = row_granule(X, ldx, es);
+    a.vb = row_granule(dY, lddy, es);
     a.vo = d_out % 4 == 0;
     a.dW = dW; a.dw_stride = dw_stride; a.db = db; a.db_stride = db_stride;
     RTMA_TRY(prepare_row_call(ctx, sizeof(float) * a.tiles * (weights + BIAS_ROWS * (int64_t)d_out), stream));

@@ -26,8 +26,10 @@ struct DeviceScope {
 };
 
 inline size_t row_type_bytes(int32_t dtype) { return dtype == RTMA_F32 ? 4 : 2; }
-inline bool aligned_rows(const void* p, int64_t ld, size_t element) {
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (ld * (int64_t)element) % 16 == 0;
+// The largest power of two, up to 16 bytes, on whose multiples all rows lie.
+inline int row_granule(const void* p, int64_t ld, size_t element) {
+    const uintptr_t both = reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * (int64_t)element) | 16;
+    return (int)(both & (~both + 1));
 }
 // Whether `stream` is being captured into a graph: such a call neither grows the scratch nor waits for other streams.
 int32_t stream_captures(rtma_ctx* ctx, cudaStream_t stream, bool* captures);
@@ -87,14 +89,27 @@ __device__ __forceinline__ uint32_t narrow2(float a, float b, const __half*) {
     return *reinterpret_cast<const uint32_t*>(&t);
 }
 
-// Eight consecutive values as they are stored; `valid` of them exist (the others read as zero).  vec: p is on a 16-byte boundary.
+// Eight consecutive values as they are stored; `valid` of them exist (the others read as zero).  p lies on a multiple of
+// `granule` bytes.
 template <class T>
 struct Eight {
     uint4 w[sizeof(T) / 2];
-    __device__ __forceinline__ void load(const T* p, int valid, bool vec) {
-        if (vec && valid == 8) {
+    __device__ __forceinline__ void load(const T* p, int valid, int granule) {
+        uint32_t* q = reinterpret_cast<uint32_t*>(w);
+        constexpr int WORDS = 2 * sizeof(T);
+        if (valid == 8 && granule == 16) {
 #pragma unroll
-            for (int i = 0; i < (int)(sizeof(T) / 2); ++i) w[i] = reinterpret_cast<const uint4*>(p)[i];
+            for (int i = 0; i < WORDS / 4; ++i) w[i] = reinterpret_cast<const uint4*>(p)[i];
+        } else if (valid == 8 && granule == 8) {
+#pragma unroll
+            for (int i = 0; i < WORDS / 2; ++i) {
+                const uint2 x = reinterpret_cast<const uint2*>(p)[i];
+                q[2 * i] = x.x;
+                q[2 * i + 1] = x.y;
+            }
+        } else if (sizeof(T) == 2 && valid == 8 && granule == 4) {
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) q[i] = reinterpret_cast<const uint32_t*>(p)[i];
         } else {
             T e[8];
 #pragma unroll
@@ -125,9 +140,10 @@ struct Eight {
     }
 };
 template <class T>
-__device__ __forceinline__ void store_eight(T* p, const float (&v)[8], int valid, bool vec) {
-    if (vec && valid == 8) {
-        uint32_t q[2 * sizeof(T)];
+__device__ __forceinline__ void store_eight(T* p, const float (&v)[8], int valid, int granule) {
+    constexpr int WORDS = 2 * sizeof(T);
+    if (valid == 8 && granule > (int)sizeof(T)) {
+        uint32_t q[WORDS];
         if constexpr (sizeof(T) == 4) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) q[j] = __float_as_uint(v[j]);
@@ -135,9 +151,17 @@ __device__ __forceinline__ void store_eight(T* p, const float (&v)[8], int valid
 #pragma unroll
             for (int j = 0; j < 4; ++j) q[j] = narrow2(v[2 * j], v[2 * j + 1], static_cast<const T*>(nullptr));
         }
+        if (granule == 16) {
 #pragma unroll
-        for (int i = 0; i < (int)(sizeof(T) / 2); ++i)
-            reinterpret_cast<uint4*>(p)[i] = make_uint4(q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]);
+            for (int i = 0; i < WORDS / 4; ++i)
+                reinterpret_cast<uint4*>(p)[i] = make_uint4(q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]);
+        } else if (granule == 8) {
+#pragma unroll
+            for (int i = 0; i < WORDS / 2; ++i) reinterpret_cast<uint2*>(p)[i] = make_uint2(q[2 * i], q[2 * i + 1]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) reinterpret_cast<uint32_t*>(p)[i] = q[i];
+        }
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)

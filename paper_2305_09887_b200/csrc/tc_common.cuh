@@ -78,6 +78,14 @@ __device__ __forceinline__ void tma_load_2d(void* smem_dst, const CUtensorMap* m
         : "memory");
 }
 
+// The same of a 3-D tensor: the box of matrix z.
+__device__ __forceinline__ void tma_load_3d(void* smem_dst, const CUtensorMap* map, uint64_t* bar, int32_t x, int32_t y, int32_t z) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
+        : "memory");
+}
+
 // ---- bulk-tensor stores -----------------------------------------------------------------
 // The box at (x, y) from shared memory to the matrix; what lies outside the matrix is not written.  x and y not negative.
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, const void* smem_src, int32_t x, int32_t y) {
@@ -251,3 +259,7 @@ __device__ __forceinline__ void mma_commit_pair(uint64_t* bar) {
 // read as zero.  Returns false if the driver refuses.
 bool make_tensor_map_bf16(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint64_t ld,
                           uint32_t box_cols, uint32_t box_rows);
+// `count` row-major matrices [rows x cols] of 16-bit values, ld elements between rows and `stride` between matrices; boxes of 64
+// columns x box_rows (up to 256) of one matrix, 128-byte swizzle, zeros outside a matrix.
+bool make_tensor_map_16bit(CUtensorMap* out, bool bf16, const void* base, uint64_t count, uint64_t rows, uint64_t cols, uint64_t ld, uint64_t stride,
+                           uint32_t box_rows);
