@@ -13,9 +13,10 @@
 // inside 64 terms the five small products of fp32 operands come first.
 //
 // Three ways of loading (Loading below), and the warps that go with them:
-//   SPLIT   fp32: 8 warps per operand bring values through registers and split them; 8 drain warps; one warp multiplies
-//   COPIES  16-bit rows that do not all lie on 16-byte boundaries: the same warps with asynchronous copies of 16, 8 or 4 bytes
-//   BULK    16-bit rows on 16-byte boundaries: one thread with bulk-tensor loads; 8 drain warps; one warp multiplies
+//   SPLIT   fp32: 16 warps, 8 per operand, bring values through registers, split them, and drain the stage before; they take turns
+//           at issuing a stage's MMAs
+//   COPIES  16-bit rows that do not all lie on 16-byte boundaries: 8 warps with asynchronous copies of 16, 8 or 4 bytes, 8 drain
+//   BULK    16-bit rows on 16-byte boundaries: one thread with bulk-tensor loads, 8 warps drain
 #include <algorithm>
 
 #include "rows.cuh"
@@ -30,14 +31,11 @@ enum Mode { FORWARD, INPUT_GRADIENT, WEIGHT_GRADIENT };
 enum Loading { SPLIT, COPIES, BULK };
 
 constexpr int BM = 128, BK = 64;
-constexpr int DRAIN_WARPS = 8, OPERAND_WARPS = 8;  // of each operand
-// A block of the first two ways is launched with 72 registers a thread (28 warps); the multiplier's four give theirs up to the
-// others: 256 x 104 + 512 x 64 + 128 x 24 = 62,464 of 64,512.
-constexpr int DRAIN_REGISTERS = 104, LOAD_REGISTERS = 64, MULTIPLY_REGISTERS = 24;
+constexpr int OPERAND_THREADS = 256;       // that load one operand: 8 per row of a slab
+// Registers a thread.  COPIES is launched with 96 (20 warps); the multiplier's four warps and the loading ones give some up to those
+// that drain: 256 x 112 + 256 x 96 + 128 x 64 = 61,440 = 640 x 96.
+constexpr int DRAIN_REGISTERS = 112, MULTIPLY_REGISTERS = 64;
 constexpr int SLAB_BYTES = 32 * 128;       // 32 rows of 64 16-bit values
-constexpr int OUT_PITCH = 80, OUT_BYTES = 32 * OUT_PITCH;  // a drain warp's 32 rows of 64 bytes on their way out
-constexpr int RING_BYTES = 192 * 1024;
-constexpr int DYNAMIC_BYTES = RING_BYTES + 1024 + DRAIN_WARPS * OUT_BYTES;
 constexpr int BIAS_ROWS = 8;               // partial sums of the bias gradient in a slot, one row per warp that adds them up
 constexpr int MAX_STAGES = 6;
 
@@ -48,11 +46,18 @@ struct Form {
     static constexpr int BN = IN_REGISTERS ? 128 : 256;                                // widest tile
     static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128;                       // of a plane
     static constexpr int STAGE_BYTES = PLANES * (A_BYTES + B_BYTES);
+    // BULK: the results of a tile leave while the next is drained, which is worth more than a fourth stage
+    static constexpr int RING_BYTES = (LOADING == BULK ? (MODE == WEIGHT_GRADIENT ? 160 : 144) : 192) * 1024;
     static constexpr int STAGES = RING_BYTES / STAGE_BYTES;
+    static constexpr int DRAIN_WARPS = LOADING == SPLIT ? 16 : 8;
+    static constexpr int OUT_SLABS = LOADING != BULK ? 1 : MODE == WEIGHT_GRADIENT ? 2 : 4;  // of a drain warp: 32 rows of OUT_ROW bytes on
+    static constexpr int OUT_ROW = LOADING == SPLIT ? 32 : 64;                         // their way out
+    static constexpr int OUT_BYTES = OUT_SLABS * 32 * OUT_ROW;
+    static constexpr int DYNAMIC_BYTES = RING_BYTES + 1024 + DRAIN_WARPS * OUT_BYTES;
     static constexpr bool A_ACROSS = MODE == WEIGHT_GRADIENT, B_ACROSS = MODE != INPUT_GRADIENT;  // MN-major
     static constexpr bool DRAIN_SUMS = LOADING == BULK && MODE == WEIGHT_GRADIENT;     // the drain warps add up the columns of dY
-    static constexpr int LOAD_WARPS = LOADING == BULK ? 0 : 2 * OPERAND_WARPS;
-    static constexpr int THREADS = 32 * (DRAIN_WARPS + LOAD_WARPS + 4);
+    static constexpr int LOAD_WARPS = LOADING == COPIES ? 8 : 0;                       // that do nothing else
+    static constexpr int THREADS = 32 * (DRAIN_WARPS + LOAD_WARPS + (LOADING == SPLIT ? 0 : 4));
 };
 
 struct LinearArgs {
@@ -66,7 +71,7 @@ struct LinearArgs {
     const void *A, *B;         // rows; matrices (forward, dx) or rows (dw)
     int64_t lda, ldb, w_stride;
     int va, vb;                // granules of the rows (bytes)
-    bool vo;                   // rows of the result on 16-byte boundaries
+    bool vo;                   // rows of the result on 16-byte boundaries: map_o holds
     const void* bias;
     int64_t bias_stride;
     void* out;                 // dw: the slots, [row tile][(d_in + BIAS_ROWS) * d_out]
@@ -75,6 +80,7 @@ struct LinearArgs {
     int64_t dw_stride, db_stride;
     int* error_word;
     CUtensorMap map_a, map_b;  // BULK
+    CUtensorMap map_o;         // the result (dw: the slots, one below the other)
 };
 
 struct Shared {
@@ -84,7 +90,7 @@ struct Shared {
     int abort;
     int32_t warp_sums[32];
     int32_t tile_start[RTMA_MAX_GROUPS + 1], begin[RTMA_MAX_GROUPS], rows[RTMA_MAX_GROUPS];
-    float bias[DRAIN_WARPS][128];  // of a warp's columns
+    alignas(16) float bias[8 * 128];  // of every drain warp's columns
 };
 
 __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, Shared& sh, int* error_word) {
@@ -214,8 +220,8 @@ __device__ __forceinline__ void split_eight(const uint32_t (&x)[8], uint4 (&plan
 }
 
 // Sums over a warp's rows of the columns of dY that its lanes hold, written to the warp's row of the slot.
-__device__ __forceinline__ void leave_bias(const LinearArgs& a, const Walk<WEIGHT_GRADIENT>& w, float (&sums)[2][8], int warp, int lane) {
-    float* to = static_cast<float*>(a.out) + ((int64_t)w.row_tile * (a.d_in + BIAS_ROWS) + a.d_in + warp) * a.d_out;
+__device__ __forceinline__ void leave_bias(const LinearArgs& a, int row_tile, int n0, float (&sums)[2][8], int warp, int lane) {
+    float* to = static_cast<float*>(a.out) + ((int64_t)row_tile * (a.d_in + BIAS_ROWS) + a.d_in + warp) * a.d_out;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -224,149 +230,161 @@ __device__ __forceinline__ void leave_bias(const LinearArgs& a, const Walk<WEIGH
             s += __shfl_xor_sync(0xffffffffu, s, 8);
             s += __shfl_xor_sync(0xffffffffu, s, 16);
             const int c = 64 * t + 8 * lane + j;
-            if (lane < 8 && c < a.BN && w.n0 + c < a.d_out) to[w.n0 + c] = s;
+            if (lane < 8 && c < a.BN && n0 + c < a.d_out) to[n0 + c] = s;
             sums[t][j] = 0.f;
         }
 }
+
+// The same source for a thread that walks down one operand stage by stage: an address per tile, steps from there.
+template <class T, int MODE, bool IS_B>
+struct Cursor {
+    static constexpr bool ACROSS = IS_B ? MODE != INPUT_GRADIENT : MODE == WEIGHT_GRADIENT;
+    const T* p;         // this thread's first value of the tile
+    int tile, k0, k_end;
+    int near, cols;     // along: rows from this thread's on, terms;  across: terms from this thread's row on, columns from its unit on
+    int row_tile, m0, n0;
+    __device__ __forceinline__ bool open(const LinearArgs& a, const Shared& sh, int row, int unit) {
+        Walk<MODE> w;
+        w.tile = tile;
+        if (!w.at(a, sh)) return false;
+        k0 = 0;
+        k_end = w.k_end;
+        row_tile = w.row_tile;
+        m0 = w.m0;
+        n0 = w.n0;
+        const T* base = static_cast<const T*>(IS_B ? a.B : a.A);
+        if constexpr (ACROSS) {
+            const int c = (IS_B ? n0 : m0) + 8 * unit;
+            near = k_end - row;
+            cols = (IS_B ? a.d_out : a.d_in) - c;
+            p = base + (MODE == WEIGHT_GRADIENT ? (w.row0 + row) * (IS_B ? a.ldb : a.lda) : w.part * a.w_stride + (int64_t)row * a.d_out) + c;
+        } else {
+            near = (IS_B ? a.d_in - n0 : w.rows) - row;
+            cols = k_end - 8 * unit;
+            p = base + (IS_B ? w.part * a.w_stride + (int64_t)(n0 + row) * a.d_out : (w.row0 + row) * a.lda) + 8 * unit;
+        }
+        return true;
+    }
+    __device__ __forceinline__ bool first(const LinearArgs& a, const Shared& sh, int row, int unit) {
+        tile = blockIdx.x;
+        return open(a, sh, row, unit);
+    }
+    __device__ __forceinline__ bool last_stage() const { return k0 + BK >= k_end; }
+    __device__ __forceinline__ bool next(const LinearArgs& a, const Shared& sh, int row, int unit) {
+        if (!last_stage()) {
+            k0 += BK;
+            return true;
+        }
+        tile += gridDim.x;
+        return open(a, sh, row, unit);
+    }
+    __device__ __forceinline__ void load(const LinearArgs& a, int i, Eight<T>& to, int granule) const {
+        const int64_t ld = MODE == WEIGHT_GRADIENT ? (IS_B ? a.ldb : a.lda) : IS_B ? (int64_t)a.d_out : a.lda;
+        if constexpr (ACROSS) {
+            const int k = k0 + 32 * (i & 1);
+            to.load(p + k * ld + 64 * (i >> 1), k < near ? min(8, cols - 64 * (i >> 1)) : 0, granule);
+        } else {
+            to.load(p + 32 * i * ld + k0, 32 * i < near ? min(8, cols - k0) : 0, granule);
+        }
+    }
+};
 
 __device__ __forceinline__ void add_eight(float (&sums)[8], const float (&v)[8]) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) sums[j] += v[j];
 }
 
-// The warps of one operand (t: 0..255).
-template <class T, int MODE, int LOADING, bool IS_B>
-__device__ __forceinline__ void load_role(const LinearArgs& a, Shared& sh, uint32_t ring, int t) {
-    typedef Form<T, MODE, LOADING> F;
-    const int row = t >> 3, unit = t & 7, lane = t & 31, warp = t >> 5;
-    // a thread's 16 bytes inside a slab (32-row slabs do not change row mod 8)
-    const uint32_t place = (IS_B ? F::PLANES * F::A_BYTES : 0) + row * 128 + ((unit ^ (row & 7)) << 4);
-    constexpr int MOST = (IS_B ? F::BN : BM) / 32;
-    const int slabs = !IS_B ? MOST : F::B_ACROSS ? 2 * ((a.BN + 63) / 64) : (a.BN + 31) / 32;
-    const int granule = IS_B ? a.vb : a.va;
-    auto source = [&](const Walk<MODE>& w, int i, int& valid) {
-        if constexpr (IS_B) return source_b<T, MODE>(a, w, i, row, unit, valid);
-        else return source_a<T, MODE>(a, w, i, row, unit, valid);
-    };
-    constexpr bool SUMS = IS_B && MODE == WEIGHT_GRADIENT;
-    float sums[SUMS ? 2 : 1][8];
-    if constexpr (SUMS) {
+template <int N>
+__device__ __forceinline__ void clear(float (&v)[N][8]) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < N; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sums[i][j] = 0.f;
+        for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+}
+// Adds the pieces that a thread holds of a stage's dY (slabs two by two below one another) to its columns' sums.
+template <class T>
+__device__ __forceinline__ void add_columns(uint32_t from, int slabs, float (&sums)[2][8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (i < slabs) {
+            Eight<T> e;
+            e.w[0] = load_16(from + i * SLAB_BYTES);
+            float v[8];
+            e.values(v);
+            add_eight(sums[i >> 1], v);
+        }
     }
+}
+
+// 16-byte pieces of both operands straight into the stage (t: 0..255); it is handed over once this thread's copies have landed, LAG
+// stages later.
+template <class T, int MODE>
+__device__ __forceinline__ void copy_role(const LinearArgs& a, Shared& sh, uint32_t ring, int t) {
+    typedef Form<T, MODE, COPIES> F;
+    constexpr int LAG = F::STAGES - 2;
+    constexpr bool SUMS = MODE == WEIGHT_GRADIENT;
+    const int row = t >> 3, unit = t & 7, lane = t & 31, warp = t >> 5;
+    const uint32_t place = row * 128 + ((unit ^ (row & 7)) << 4);  // inside a slab (32-row slabs do not change row mod 8)
+    const int b_slabs = F::B_ACROSS ? 2 * ((a.BN + 63) / 64) : (a.BN + 31) / 32;
+    float sums[SUMS ? 2 : 1][8];
+    if constexpr (SUMS) clear(sums);
     Walk<MODE> w;
     bool more = w.first(a, sh);
-    tc::RingAt at;
-    if constexpr (LOADING == SPLIT) {
-        // A stage's values wait in registers; as soon as one piece is split, the next stage's is on its way.
-        Eight<T> held[MOST];
-        if (more) {
-#pragma unroll
-            for (int i = 0; i < MOST; ++i) {
-                int valid;
-                if (i < slabs) {
-                    const T* p = source(w, i, valid);
-                    held[i].load(p, valid, granule);
-                }
+    Walk<MODE> late = w;
+    tc::RingAt at, late_at;
+    int under_way = 0;
+    auto hand_over = [&]() {
+        if constexpr (SUMS) {
+            if (late.m0 == 0 && a.db) {
+                add_columns<T>(ring + late_at.s * F::STAGE_BYTES + F::A_BYTES + place, b_slabs, sums);
+                if (late.last_stage()) leave_bias(a, late.row_tile, late.n0, sums, warp, lane);
             }
+            late.next(a, sh);
         }
-        while (more) {
-            const bool wanted = SUMS && w.m0 == 0 && a.db, last = w.last_stage();
-            const Walk<MODE> here = w;
-            more = w.next(a, sh);
-            if (!wait_for(&sh.empty[at.s], at.phase ^ 1u, sh, a.error_word)) return;
-            const uint32_t stage = ring + at.s * F::STAGE_BYTES + place;
-#pragma unroll
-            for (int i = 0; i < MOST; ++i) {
-                if (i < slabs) {
-                    uint4 planes[3];
-                    if constexpr (SUMS) {
-                        if (wanted) {
-                            float v[8];
-                            held[i].values(v);
-                            add_eight(sums[i >> 1], v);
-                        }
-                    }
-                    split_eight(reinterpret_cast<const uint32_t(&)[8]>(held[i].w), planes);
-#pragma unroll
-                    for (int k = 0; k < 3; ++k) store_16(stage + k * (IS_B ? F::B_BYTES : F::A_BYTES) + i * SLAB_BYTES, planes[k]);
-                    if (more) {
-                        int valid;
-                        const T* p = source(w, i, valid);
-                        held[i].load(p, valid, granule);
-                    }
-                }
-            }
-            tc::fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) tc::mbar_arrive(&sh.full[at.s]);
-            at.advance(F::STAGES);
-            if constexpr (SUMS)
-                if (wanted && last) leave_bias(a, here, sums, warp, lane);
+        tc::fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&sh.full[late_at.s]);
+        late_at.advance(F::STAGES);
+        --under_way;
+    };
+    auto bring = [&](uint32_t to, const T* p, int valid, int granule) {
+        if (granule >= 16) copy_pieces<16>(to, p, valid * (int)sizeof(T));
+        else if (granule == 8) copy_pieces<8>(to, p, valid * (int)sizeof(T));
+        else if (granule == 4) copy_pieces<4>(to, p, valid * (int)sizeof(T));
+        else {
+            Eight<T> e;
+            e.load(p, valid, granule);
+            store_16(to, e.w[0]);
         }
-    } else {
-        // Copies straight into the stage; it is handed over once this thread's copies have landed, LAG stages later.
-        constexpr int LAG = F::STAGES - 2;
-        Walk<MODE> late = w;
-        tc::RingAt late_at;
-        int under_way = 0;
-        auto hand_over = [&]() {
-            if constexpr (SUMS) {
-                if (late.m0 == 0 && a.db) {
-                    const uint32_t stage = ring + late_at.s * F::STAGE_BYTES + place;
+    };
+    bool ok = true;
+    while (more) {
+        ok = wait_for(&sh.empty[at.s], at.phase ^ 1u, sh, a.error_word);
+        if (!ok) break;
+        const uint32_t stage = ring + at.s * F::STAGE_BYTES + place;
 #pragma unroll
-                    for (int i = 0; i < MOST; ++i) {
-                        if (i < slabs) {
-                            Eight<T> e;
-                            e.w[0] = load_16(stage + i * SLAB_BYTES);
-                            float v[8];
-                            e.values(v);
-                            add_eight(sums[i >> 1], v);
-                        }
-                    }
-                    if (late.last_stage()) leave_bias(a, late, sums, warp, lane);
-                }
-                late.next(a, sh);
-            }
-            tc::fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) tc::mbar_arrive(&sh.full[late_at.s]);
-            late_at.advance(F::STAGES);
-            --under_way;
-        };
-        bool ok = true;
-        while (more) {
-            ok = wait_for(&sh.empty[at.s], at.phase ^ 1u, sh, a.error_word);
-            if (!ok) break;
-            const uint32_t stage = ring + at.s * F::STAGE_BYTES + place;
+        for (int i = 0; i < 4; ++i) {
+            int valid;
+            const T* p = source_a<T, MODE>(a, w, i, row, unit, valid);
+            bring(stage + i * SLAB_BYTES, p, valid, a.va);
+        }
 #pragma unroll 4
-            for (int i = 0; i < slabs; ++i) {
-                int valid;
-                const T* p = source(w, i, valid);
-                const uint32_t to = stage + i * SLAB_BYTES;
-                if (granule == 16) copy_pieces<16>(to, p, valid * (int)sizeof(T));
-                else if (granule == 8) copy_pieces<8>(to, p, valid * (int)sizeof(T));
-                else if (granule == 4) copy_pieces<4>(to, p, valid * (int)sizeof(T));
-                else {
-                    Eight<T> e;
-                    e.load(p, valid, granule);
-                    store_16(to, e.w[0]);
-                }
-            }
-            copies_commit();
-            at.advance(F::STAGES);
-            if (++under_way > LAG) {
-                copies_wait<LAG>();
-                hand_over();
-            }
-            more = w.next(a, sh);
+        for (int i = 0; i < b_slabs; ++i) {
+            int valid;
+            const T* p = source_b<T, MODE>(a, w, i, row, unit, valid);
+            bring(stage + F::A_BYTES + i * SLAB_BYTES, p, valid, a.vb);
         }
-        copies_wait<0>();
-        if (ok)
-            while (under_way > 0) hand_over();
+        copies_commit();
+        at.advance(F::STAGES);
+        if (++under_way > LAG) {
+            copies_wait<LAG>();
+            hand_over();
+        }
+        more = w.next(a, sh);
     }
+    copies_wait<0>();
+    if (ok)
+        while (under_way > 0) hand_over();
 }
 
 // One warp with bulk-tensor loads.  Rows behind the end of a tile belong to the next part: they only reach results that are not
@@ -420,8 +438,9 @@ __device__ __forceinline__ void bulk_role(const LinearArgs& a, Shared& sh, uint8
     }
 }
 
+// A stage's MMAs, by one thread.
 template <class T, int MODE, int LOADING>
-__device__ __forceinline__ void multiply_role(const LinearArgs& a, Shared& sh, uint32_t ring) {
+__device__ __forceinline__ void multiply_stage(const LinearArgs& a, uint32_t d, uint32_t stage, int terms, uint32_t accumulate) {
     typedef Form<T, MODE, LOADING> F;
     const uint32_t format = std::is_same<T, __half>::value ? 0u : 1u;  // fp16 or bf16 operands, fp32 sums
     const uint32_t idesc = (1u << 4) | (format << 7) | (format << 10) | ((F::A_ACROSS ? 1u : 0u) << 15) | ((F::B_ACROSS ? 1u : 0u) << 16) |
@@ -429,133 +448,166 @@ __device__ __forceinline__ void multiply_role(const LinearArgs& a, Shared& sh, u
     const uint64_t desc = tc::smem_desc_sw128(0, 2 * SLAB_BYTES, 1024);  // atoms of 64 columns lie two slabs apart
     constexpr uint32_t a_step = F::A_ACROSS ? 128 : 2, b_step = F::B_ACROSS ? 128 : 2;  // 16 terms further, in units of 16 bytes
     constexpr uint32_t a_plane = F::A_BYTES >> 4, b_plane = F::B_BYTES >> 4;
+    uint64_t da = desc + (stage >> 4), db = da + F::PLANES * a_plane;
+    const int steps = (terms + 15) >> 4;
+    if constexpr (LOADING == SPLIT) {
+        uint64_t sa = da, sb = db;
+        for (int k = 0; k < steps; ++k, sa += a_step, sb += b_step) {
+            tc::mma_bf16(d, sa + 2 * a_plane, sb, idesc, accumulate);
+            accumulate = 1u;
+            tc::mma_bf16(d, sa, sb + 2 * b_plane, idesc, 1u);
+            tc::mma_bf16(d, sa + a_plane, sb + b_plane, idesc, 1u);
+            tc::mma_bf16(d, sa + a_plane, sb, idesc, 1u);
+            tc::mma_bf16(d, sa, sb + b_plane, idesc, 1u);
+        }
+    }
+    for (int k = 0; k < steps; ++k, da += a_step, db += b_step) {
+        tc::mma_bf16(d, da, db, idesc, accumulate);
+        accumulate = 1u;
+    }
+}
+
+template <class T, int MODE, int LOADING>
+__device__ __forceinline__ void multiply_role(const LinearArgs& a, Shared& sh, uint32_t ring) {
+    typedef Form<T, MODE, LOADING> F;
     Walk<MODE> w;
     tc::RingAt at, acc;
-    bool more = w.first(a, sh);
-    while (more) {
+    for (bool more = w.first(a, sh); more; more = w.next(a, sh)) {
         if (F::IN_REGISTERS || w.k0 == 0) {
             if (!wait_for(&sh.acc_empty[acc.s], acc.phase ^ 1u, sh, a.error_word)) return;
         }
         if (!wait_for(&sh.full[at.s], at.phase, sh, a.error_word)) return;
         tc::tc_fence_after_sync();
-        const uint32_t d = sh.tmem_base + acc.s * F::BN;
-        const uint32_t sa = (ring + at.s * F::STAGE_BYTES) >> 4, sb = sa + F::PLANES * a_plane;
-        const int steps = (min(BK, w.k_end - w.k0) + 15) >> 4;
-        uint32_t accumulate = F::IN_REGISTERS || w.k0 == 0 ? 0u : 1u;
-        if constexpr (LOADING == SPLIT) {
-            for (int k = 0; k < steps; ++k) {
-                const uint64_t da = desc + sa + k * a_step, db = desc + sb + k * b_step;
-                tc::mma_bf16(d, da + 2 * a_plane, db, idesc, accumulate);
-                tc::mma_bf16(d, da, db + 2 * b_plane, idesc, 1u);
-                tc::mma_bf16(d, da + a_plane, db + b_plane, idesc, 1u);
-                tc::mma_bf16(d, da + a_plane, db, idesc, 1u);
-                tc::mma_bf16(d, da, db + b_plane, idesc, 1u);
-                accumulate = 1u;
-            }
-        }
-        for (int k = 0; k < steps; ++k) {
-            tc::mma_bf16(d, desc + sa + k * a_step, desc + sb + k * b_step, idesc, accumulate);
-            accumulate = 1u;
-        }
+        multiply_stage<T, MODE, LOADING>(a, sh.tmem_base + acc.s * F::BN, ring + at.s * F::STAGE_BYTES, min(BK, w.k_end - w.k0), F::IN_REGISTERS || w.k0 == 0 ? 0u : 1u);
         tc::mma_commit(&sh.empty[at.s]);
         at.advance(F::STAGES);
         if (F::IN_REGISTERS || w.last_stage()) {
             tc::mma_commit(&sh.acc_full[acc.s]);
             acc.advance(2);
         }
-        more = w.next(a, sh);
     }
 }
 
-// 32 columns of a warp's 32 rows (a row per lane) on their way out, through shared memory so that lines are written whole.
-template <class O>
-__device__ __forceinline__ void write_out(O* out, int64_t ldo, bool vec, const float (&v)[32], uint32_t slab, int rows, int cols, int lane) {
-    constexpr int WIDE = 64 / sizeof(O), PIECE = 16 / sizeof(O);  // columns at a time, and of 16 bytes
+// A drain warp's results on their way out: ROW bytes of each of its 32 rows (a row per lane) at a time go through one of its slabs,
+// in the map's swizzle of ROW bytes, so that they leave as one bulk-tensor store; boxes that would reach rows or columns that are
+// not this tile's, and rows off the 16-byte boundaries, are written by the lanes.
+template <class O, int SLABS, int ROW>
+struct Outlet {
+    uint32_t slabs;
+    int at = 0;
+    __device__ __forceinline__ static int swizzle(int row) { return ROW == 64 ? (row >> 1) & 3 : (row >> 2) & 1; }
+    // row0, c: place in the map; rows, cols: how much is this tile's; whole: all columns of the matrix from c on are, and end on a
+    // 16-byte boundary (a store's box is cut off at the edge of the matrix only in steps of 16 bytes)
+    __device__ __forceinline__ void put(const LinearArgs& a, const float (&v)[32], int64_t row0, int c, int rows, int cols, bool whole, O* out, int64_t ldo, int lane) {
+        constexpr int WIDE = ROW / sizeof(O), PIECE = 16 / sizeof(O);
 #pragma unroll
-    for (int c0 = 0; c0 < 32; c0 += WIDE) {
-        if (c0 >= cols) break;
-        __syncwarp();
+        for (int c0 = 0; c0 < 32; c0 += WIDE) {
+            if (c0 >= cols) break;
+            const uint32_t slab = slabs + at * 32 * ROW;
+            if (lane == 0) tc::tma_store_wait_read_but<SLABS - 1>();  // the slab's last store has read it
+            __syncwarp();
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            uint4 x;
-            if constexpr (sizeof(O) == 4) {
-                x = make_uint4(__float_as_uint(v[c0 + 4 * q]), __float_as_uint(v[c0 + 4 * q + 1]), __float_as_uint(v[c0 + 4 * q + 2]), __float_as_uint(v[c0 + 4 * q + 3]));
-            } else {
-                const O* tag = nullptr;
-                x = make_uint4(narrow2(v[8 * q], v[8 * q + 1], tag), narrow2(v[8 * q + 2], v[8 * q + 3], tag),
-                               narrow2(v[8 * q + 4], v[8 * q + 5], tag), narrow2(v[8 * q + 6], v[8 * q + 7], tag));
-            }
-            store_16(slab + lane * OUT_PITCH + 16 * q, x);
-        }
-        __syncwarp();
-        if (vec && cols - c0 >= WIDE) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = 8 * i + (lane >> 2), q = lane & 3;
-                const uint4 x = load_16(slab + r * OUT_PITCH + 16 * q);
-                if (r < rows) *reinterpret_cast<uint4*>(out + r * ldo + c0 + q * PIECE) = x;
-            }
-        } else {
-            const int c = lane % WIDE;
-            for (int r = lane / WIDE; r < rows; r += 32 / WIDE) {
-                O x;
+            for (int q = 0; q < ROW / 16; ++q) {
+                const int e = c0 + q * PIECE;
+                uint4 x;
                 if constexpr (sizeof(O) == 4) {
-                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(slab + r * OUT_PITCH + 4 * c) : "memory");
+                    x = make_uint4(__float_as_uint(v[e]), __float_as_uint(v[e + 1]), __float_as_uint(v[e + 2]), __float_as_uint(v[e + 3]));
                 } else {
-                    unsigned short bits;
-                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(bits) : "r"(slab + r * OUT_PITCH + 2 * c) : "memory");
-                    x = *reinterpret_cast<O*>(&bits);
+                    const O* tag = nullptr;
+                    x = make_uint4(narrow2(v[e], v[e + 1], tag), narrow2(v[e + 2], v[e + 3], tag), narrow2(v[e + 4], v[e + 5], tag), narrow2(v[e + 6], v[e + 7], tag));
                 }
-                if (c0 + c < cols) out[r * ldo + c0 + c] = x;
+                store_16(slab + lane * ROW + ((q ^ swizzle(lane)) << 4), x);
             }
+            const bool bulk = a.vo && rows == 32 && (cols - c0 >= WIDE || whole);
+            if (bulk) tc::fence_proxy_async_smem();
+            __syncwarp();
+            if (bulk) {
+                if (lane == 0) {
+                    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
+                                 ::"l"(reinterpret_cast<uint64_t>(&a.map_o)), "r"(slab), "r"(c + c0), "r"((int32_t)row0)
+                                 : "memory");
+                }
+            } else {
+                const int x = lane % WIDE;
+                for (int r = lane / WIDE; r < rows; r += 32 / WIDE) {
+                    const uint32_t from = slab + r * ROW + (((x / PIECE) ^ swizzle(r)) << 4) + (x % PIECE) * (int)sizeof(O);
+                    O y;
+                    if constexpr (sizeof(O) == 4) {
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(y) : "r"(from) : "memory");
+                    } else {
+                        unsigned short bits;
+                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(bits) : "r"(from) : "memory");
+                        y = *reinterpret_cast<O*>(&bits);
+                    }
+                    if (c0 + x < cols) out[r * ldo + c0 + x] = y;
+                }
+            }
+            if (lane == 0) tc::tma_store_commit();  // a group for every slab, empty or not
+            at = at + 1 == SLABS ? 0 : at + 1;
         }
     }
+    __device__ __forceinline__ void finish(int lane) const {
+        if (lane == 0) tc::tma_store_wait_all();
+    }
+};
+
+// The bias of a warp's `count` columns from column c of the tile, kept in shared memory until the part or the columns change.
+template <class T, int MODE>
+struct BiasHolder {
+    float* at;  // 16-byte boundary
+    int part = -1, n0 = -1;
+    __device__ __forceinline__ void fetch(const LinearArgs& a, const Walk<MODE>& w, int c, int step, int chunks, int lane) {
+        if (w.part == part && w.n0 == n0) return;
+        part = w.part;
+        n0 = w.n0;
+        const T* bias = static_cast<const T*>(a.bias) + part * a.bias_stride + n0;
+        __syncwarp();
+        for (int chunk = c, i = 0; chunk < chunks; chunk += step, ++i) {
+            const int col = 32 * chunk + lane;
+            at[32 * i + lane] = col < a.BN && n0 + col < a.d_out ? to_f32(bias[col]) : 0.f;
+        }
+        __syncwarp();
+    }
+    __device__ __forceinline__ void add(float (&v)[32], int i) const {
+        const float4* b = reinterpret_cast<const float4*>(at + 32 * i);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float4 x = b[j];
+            v[4 * j] += x.x;
+            v[4 * j + 1] += x.y;
+            v[4 * j + 2] += x.z;
+            v[4 * j + 3] += x.w;
+        }
+    }
+};
+
+// 32 columns (chunk `chunk` of the tile) of a warp's 32 rows (its quarter of the tile's) to the result.
+template <class T, int MODE, class OUT>
+__device__ __forceinline__ void put_chunk(const LinearArgs& a, const Walk<MODE>& w, OUT& outlet, const float (&v)[32], int quarter, int chunk, int lane) {
+    typedef typename std::conditional<MODE == WEIGHT_GRADIENT, float, T>::type O;
+    const int N = MODE == INPUT_GRADIENT ? a.d_in : a.d_out;
+    const int c = w.n0 + 32 * chunk, cols = min(min(32, a.BN - 32 * chunk), N - c);
+    const int rows = min(32, (MODE == WEIGHT_GRADIENT ? min(BM, a.d_in - w.m0) : w.rows) - 32 * quarter);
+    if (cols <= 0 || rows <= 0) return;
+    const int64_t row0 = (MODE == WEIGHT_GRADIENT ? (int64_t)w.row_tile * (a.d_in + BIAS_ROWS) + w.m0 : w.row0) + 32 * quarter;
+    const int64_t ldo = MODE == WEIGHT_GRADIENT ? a.d_out : a.ldo;
+    outlet.put(a, v, row0, c, rows, cols, c + cols == N && N % (16 / (int)sizeof(O)) == 0, static_cast<O*>(a.out) + row0 * ldo + c, ldo, lane);
 }
 
 template <class T, int MODE, int LOADING>
 __device__ __forceinline__ void drain_role(const LinearArgs& a, Shared& sh, uint32_t slabs, uint32_t ring) {
     typedef Form<T, MODE, LOADING> F;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, half = warp >> 2;
-    const uint32_t slab = slabs + warp * OUT_BYTES, lanes = (uint32_t)(32 * quarter) << 16;
+    typedef typename std::conditional<MODE == WEIGHT_GRADIENT, float, T>::type O;
+    Outlet<O, F::OUT_SLABS, F::OUT_ROW> outlet{slabs + warp * F::OUT_BYTES};
+    BiasHolder<T, MODE> bias{sh.bias + 128 * warp};
+    const uint32_t lanes = (uint32_t)(32 * quarter) << 16;
     const int chunks = (a.BN + 31) / 32;
     Walk<MODE> w;
     tc::RingAt acc, at;
-    int bias_part = -1, bias_n0 = -1;
     float sums[F::DRAIN_SUMS ? 2 : 1][8];
-    if constexpr (F::DRAIN_SUMS) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sums[i][j] = 0.f;
-    }
+    if constexpr (F::DRAIN_SUMS) clear(sums);
     for (bool more = w.first(a, sh); more; more = w.next_tile(a, sh)) {
-        const int N = MODE == INPUT_GRADIENT ? a.d_in : a.d_out;
-        const int out_rows = max(0, (MODE == WEIGHT_GRADIENT ? min(BM, a.d_in - w.m0) : w.rows) - 32 * quarter);
-        auto put = [&](float (&v)[32], int chunk) {
-            const int c = w.n0 + 32 * chunk, cols = min(min(32, a.BN - 32 * chunk), N - c);
-            if (cols <= 0 || out_rows <= 0) return;
-            if constexpr (MODE == WEIGHT_GRADIENT) {
-                float* out = static_cast<float*>(a.out) + ((int64_t)w.row_tile * (a.d_in + BIAS_ROWS) + w.m0 + 32 * quarter) * a.d_out + c;
-                write_out<float>(out, a.d_out, a.vo, v, slab, min(32, out_rows), cols, lane);
-            } else {
-                if (MODE == FORWARD && a.bias) {
-                    const float* bias = &sh.bias[warp][32 * (chunk >> 1)];
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] += bias[j];
-                }
-                write_out<T>(static_cast<T*>(a.out) + (w.row0 + 32 * quarter) * a.ldo + c, a.ldo, a.vo, v, slab, min(32, out_rows), cols, lane);
-            }
-        };
-        if (MODE == FORWARD && a.bias && (w.part != bias_part || w.n0 != bias_n0)) {
-            const T* bias = static_cast<const T*>(a.bias) + w.part * a.bias_stride + w.n0;
-            for (int chunk = half; chunk < chunks; chunk += 2) {
-                const int c = 32 * chunk + lane;
-                sh.bias[warp][32 * (chunk >> 1) + lane] = c < a.BN && w.n0 + c < N ? to_f32(bias[c]) : 0.f;
-            }
-            bias_part = w.part;
-            bias_n0 = w.n0;
-            __syncwarp();
-        }
         if constexpr (F::IN_REGISTERS) {
             float total[2][32];
 #pragma unroll
@@ -584,17 +636,7 @@ __device__ __forceinline__ void drain_role(const LinearArgs& a, Shared& sh, uint
                         if (w.m0 == 0) {
                             if (!wait_for(&sh.full[at.s], at.phase, sh, a.error_word)) return;
                             const int t = threadIdx.x, row = t >> 3, unit = t & 7;
-                            const uint32_t stage = ring + at.s * F::STAGE_BYTES + F::A_BYTES + row * 128 + ((unit ^ (row & 7)) << 4);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                if (i < 2 * ((a.BN + 63) / 64)) {
-                                    Eight<T> e;
-                                    e.w[0] = load_16(stage + i * SLAB_BYTES);
-                                    float v[8];
-                                    e.values(v);
-                                    add_eight(sums[i >> 1], v);
-                                }
-                            }
+                            add_columns<T>(ring + at.s * F::STAGE_BYTES + F::A_BYTES + row * 128 + ((unit ^ (row & 7)) << 4), 2 * ((a.BN + 63) / 64), sums);
                             __syncwarp();
                         }
                         if (lane == 0) tc::mbar_arrive(&sh.empty[at.s]);
@@ -603,18 +645,23 @@ __device__ __forceinline__ void drain_role(const LinearArgs& a, Shared& sh, uint
                 }
             }
             if constexpr (F::DRAIN_SUMS)
-                if (a.db && w.m0 == 0) leave_bias(a, w, sums, warp, lane);
+                if (a.db && w.m0 == 0) {
+                    leave_bias(a, w.row_tile, w.n0, sums, warp, lane);
+                    clear(sums);
+                }
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                if (half + 2 * i < chunks) put(total[i], half + 2 * i);
+                if (half + 2 * i < chunks) put_chunk<T, MODE>(a, w, outlet, total[i], quarter, half + 2 * i, lane);
         } else {
+            if (MODE == FORWARD && a.bias) bias.fetch(a, w, half, 2, chunks, lane);
             if (!wait_for(&sh.acc_full[acc.s], acc.phase, sh, a.error_word)) return;
             __syncwarp();
             tc::tc_fence_after_sync();
             for (int chunk = half; chunk < chunks; chunk += 2) {
                 float v[32];
                 tc::tmem_load_32x32(sh.tmem_base + lanes + acc.s * F::BN + 32 * chunk, v);
-                put(v, chunk);
+                if (MODE == FORWARD && a.bias) bias.add(v, chunk >> 1);
+                put_chunk<T, MODE>(a, w, outlet, v, quarter, chunk, lane);
             }
             tc::tc_fence_before_sync();
             __syncwarp();
@@ -622,30 +669,132 @@ __device__ __forceinline__ void drain_role(const LinearArgs& a, Shared& sh, uint
             acc.advance(2);
         }
     }
+    outlet.finish(lane);
+}
+
+// fp32 rows: a warp of one operand (t: 0..255 of its threads).  A stage's values wait in registers; as soon as one piece is split
+// and stored, the same piece of the next stage is on its way.  Then the warp takes its 32 columns of the stage before from tensor
+// memory: when that has been multiplied, its place in the ring and its accumulator are free, so the next
+// stage needs no other leave, and the tensor cores work on one while the warps split the next.
+template <int MODE, bool IS_B>
+__device__ __forceinline__ void split_role(const LinearArgs& a, Shared& sh, uint32_t slabs, uint32_t ring, int t) {
+    typedef Form<float, MODE, SPLIT> F;
+    const int row = t >> 3, unit = t & 7, lane = t & 31, warp = threadIdx.x >> 5, quarter = warp & 3, chunk = warp >> 2;
+    const uint32_t place = (IS_B ? F::PLANES * F::A_BYTES : 0) + row * 128 + ((unit ^ (row & 7)) << 4);
+    constexpr bool SUMS = IS_B && MODE == WEIGHT_GRADIENT;
+    const int pieces = !IS_B ? 4 : F::B_ACROSS ? 2 * ((a.BN + 63) / 64) : (a.BN + 31) / 32, granule = IS_B ? a.vb : a.va;
+    const bool drains = chunk < (a.BN + 31) / 32;
+    const uint32_t tmem = sh.tmem_base + ((uint32_t)(32 * quarter) << 16) + 32 * chunk;
+    Outlet<float, F::OUT_SLABS, F::OUT_ROW> outlet{slabs + warp * F::OUT_BYTES};
+    BiasHolder<float, MODE> bias{sh.bias + 32 * warp};
+    float sums[SUMS ? 2 : 1][8], total[32];
+    if constexpr (SUMS) clear(sums);
+    Eight<float> held[4];
+    Cursor<float, MODE, IS_B> c;
+    Walk<MODE> out;  // the tile that is drained
+    bool more = c.first(a, sh, row, unit);
+    out.first(a, sh);
+    if (more) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < pieces) c.load(a, i, held[i], granule);
+    }
+    auto drain = [&](const tc::RingAt& stage) {
+        if (!wait_for(&sh.acc_full[stage.s], stage.phase, sh, a.error_word)) return false;
+        __syncwarp();
+        tc::tc_fence_after_sync();
+        if (drains) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                float v[8];
+                tc::tmem_load_32x8(tmem + stage.s * F::BN + 8 * q, v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) total[8 * q + j] = out.k0 ? total[8 * q + j] + v[j] : v[j];
+            }
+            if (out.last_stage()) {
+                if (MODE == FORWARD && a.bias) {
+                    bias.fetch(a, out, chunk, 4, min(chunk + 1, (a.BN + 31) / 32), lane);
+                    bias.add(total, 0);
+                }
+                put_chunk<float, MODE>(a, out, outlet, total, quarter, chunk, lane);
+            }
+        }
+        out.next(a, sh);
+        tc::tc_fence_before_sync();
+        return true;
+    };
+    tc::RingAt at, before;
+    bool pending = false;
+    int turn = 0;
+    while (more) {
+        const bool wanted = SUMS && c.m0 == 0 && a.db, last = c.last_stage();
+        const int row_tile = c.row_tile, n0 = c.n0, terms = min(BK, c.k_end - c.k0);
+        more = c.next(a, sh, row, unit);
+        const uint32_t stage = ring + at.s * F::STAGE_BYTES + place;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (i < pieces) {
+                uint4 planes[3];
+                if constexpr (SUMS) {
+                    if (wanted) {
+                        float v[8];
+                        held[i].values(v);
+                        add_eight(sums[i >> 1], v);
+                    }
+                }
+                split_eight(reinterpret_cast<const uint32_t(&)[8]>(held[i].w), planes);
+#pragma unroll
+                for (int k = 0; k < 3; ++k) store_16(stage + k * (IS_B ? F::B_BYTES : F::A_BYTES) + i * SLAB_BYTES, planes[k]);
+                if (more) c.load(a, i, held[i], granule);
+            }
+        }
+        tc::fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&sh.full[at.s]);
+        if constexpr (SUMS)
+            if (wanted && last) leave_bias(a, row_tile, n0, sums, t >> 5, lane);
+        if (warp == turn) {
+            if (!wait_for(&sh.full[at.s], at.phase, sh, a.error_word)) return;
+            tc::tc_fence_after_sync();
+            if (lane == 0) {
+                multiply_stage<float, MODE, SPLIT>(a, sh.tmem_base + at.s * F::BN, ring + at.s * F::STAGE_BYTES, terms, 0u);
+                tc::mma_commit(&sh.acc_full[at.s]);
+            }
+            __syncwarp();
+        }
+        turn = (turn + 1) & 15;
+        if (pending && !drain(before)) return;
+        pending = true;
+        before = at;
+        at.advance(2);
+    }
+    if (pending && !drain(before)) return;
+    outlet.finish(lane);
 }
 
 template <class T, int MODE, int LOADING>
 __global__ void __launch_bounds__(Form<T, MODE, LOADING>::THREADS, 1) linear_kernel(const __grid_constant__ LinearArgs a) {
     typedef Form<T, MODE, LOADING> F;
+    static_assert(F::DYNAMIC_BYTES + sizeof(Shared) <= 232448 && F::STAGES <= MAX_STAGES, "shared memory of a block");
     extern __shared__ uint8_t raw[];
     __shared__ Shared sh;
     uint8_t* ring_bytes = raw + ((1024u - (tc::smem_u32(raw) & 1023u)) & 1023u);
-    const uint32_t ring = tc::smem_u32(ring_bytes), slabs = ring + RING_BYTES;
+    const uint32_t ring = tc::smem_u32(ring_bytes), slabs = ring + F::RING_BYTES;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr int MULTIPLIER = DRAIN_WARPS + F::LOAD_WARPS;
+    constexpr int MULTIPLIER = F::DRAIN_WARPS + F::LOAD_WARPS, OWNER = LOADING == SPLIT ? 0 : MULTIPLIER;  // OWNER: of tensor memory
     if (threadIdx.x == 0) {
         for (int s = 0; s < F::STAGES; ++s) {
-            tc::mbar_init(&sh.full[s], LOADING == BULK ? 1 : F::LOAD_WARPS);
-            tc::mbar_init(&sh.empty[s], 1 + (F::DRAIN_SUMS && a.db ? DRAIN_WARPS : 0));
+            tc::mbar_init(&sh.full[s], LOADING == BULK ? 1 : LOADING == SPLIT ? F::DRAIN_WARPS : F::LOAD_WARPS);
+            tc::mbar_init(&sh.empty[s], 1 + (F::DRAIN_SUMS && a.db ? F::DRAIN_WARPS : 0));
         }
         for (int b = 0; b < 2; ++b) {
             tc::mbar_init(&sh.acc_full[b], 1);
-            tc::mbar_init(&sh.acc_empty[b], DRAIN_WARPS);
+            tc::mbar_init(&sh.acc_empty[b], F::DRAIN_WARPS);
         }
         sh.abort = 0;
         tc::fence_barrier_init();
     }
-    if (warp == MULTIPLIER) {
+    if (warp == OWNER) {
         tc::tmem_alloc(&sh.tmem_base, 2 * F::BN);
         tc::tmem_relinquish();
     }
@@ -660,25 +809,29 @@ __global__ void __launch_bounds__(Form<T, MODE, LOADING>::THREADS, 1) linear_ker
     tc::tc_fence_before_sync();
     __syncthreads();
     tc::tc_fence_after_sync();
-    if (warp < DRAIN_WARPS) {
-        if constexpr (LOADING != BULK) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(DRAIN_REGISTERS));
-        drain_role<T, MODE, LOADING>(a, sh, slabs, ring);
+    if (warp < F::DRAIN_WARPS) {
+        if constexpr (LOADING == SPLIT) {
+            if (threadIdx.x < OPERAND_THREADS) split_role<MODE, false>(a, sh, slabs, ring, threadIdx.x);
+            else split_role<MODE, true>(a, sh, slabs, ring, threadIdx.x - OPERAND_THREADS);
+        } else {
+            if constexpr (LOADING == COPIES) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(DRAIN_REGISTERS));
+            drain_role<T, MODE, LOADING>(a, sh, slabs, ring);
+        }
     } else if (warp < MULTIPLIER) {
-        if constexpr (LOADING != BULK) {
-            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(LOAD_REGISTERS));
-            if (warp < DRAIN_WARPS + OPERAND_WARPS) load_role<T, MODE, LOADING, false>(a, sh, ring, threadIdx.x - 32 * DRAIN_WARPS);
-            else load_role<T, MODE, LOADING, true>(a, sh, ring, threadIdx.x - 32 * (DRAIN_WARPS + OPERAND_WARPS));
+        if constexpr (LOADING == COPIES) {
+            copy_role<T, MODE>(a, sh, ring, threadIdx.x - 32 * F::DRAIN_WARPS);
         }
     } else {
-        if constexpr (LOADING != BULK) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(MULTIPLY_REGISTERS));
-        if (warp == MULTIPLIER && lane == 0) multiply_role<T, MODE, LOADING>(a, sh, ring);
+        if constexpr (LOADING == COPIES) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(MULTIPLY_REGISTERS));
+        if constexpr (LOADING != SPLIT)
+            if (warp == MULTIPLIER && lane == 0) multiply_role<T, MODE, LOADING>(a, sh, ring);
         if constexpr (LOADING == BULK)
             if (warp == MULTIPLIER + 1) bulk_role<T, MODE>(a, sh, ring_bytes, lane);
     }
     __syncwarp();
     tc::tc_fence_before_sync();
     __syncthreads();
-    if (warp == MULTIPLIER) {
+    if (warp == OWNER) {
         tc::tc_fence_after_sync();
         tc::tmem_dealloc(sh.tmem_base, 2 * F::BN);
     }
@@ -718,10 +871,10 @@ void cut_columns(LinearArgs& a, int N, int widest) {
 template <class T, int MODE, int LOADING>
 int32_t launch_form(rtma_ctx* ctx, const LinearArgs& a, unsigned grid, bool& configured, cudaStream_t stream) {
     if (!configured) {
-        RTMA_CUDA(ctx, cudaFuncSetAttribute(linear_kernel<T, MODE, LOADING>, cudaFuncAttributeMaxDynamicSharedMemorySize, DYNAMIC_BYTES));
+        RTMA_CUDA(ctx, cudaFuncSetAttribute(linear_kernel<T, MODE, LOADING>, cudaFuncAttributeMaxDynamicSharedMemorySize, Form<T, MODE, LOADING>::DYNAMIC_BYTES));
         configured = true;
     }
-    launch_kernel(linear_kernel<T, MODE, LOADING>, grid, Form<T, MODE, LOADING>::THREADS, DYNAMIC_BYTES, stream, a);
+    launch_kernel(linear_kernel<T, MODE, LOADING>, grid, Form<T, MODE, LOADING>::THREADS, Form<T, MODE, LOADING>::DYNAMIC_BYTES, stream, a);
     RTMA_LAUNCH_CHECK(ctx);
     return RTMA_OK;
 }
@@ -729,7 +882,7 @@ int32_t launch_form(rtma_ctx* ctx, const LinearArgs& a, unsigned grid, bool& con
 // Whether both operands can be fetched by bulk-tensor loads; sets up their maps.
 template <int MODE>
 bool bulk_maps(LinearArgs& a, bool bf16) {
-    if (a.va != 16 || a.vb != 16) return false;
+    if (a.va < 16 || a.vb < 16) return false;
     if (MODE == WEIGHT_GRADIENT)
         return make_tensor_map_16bit(&a.map_a, bf16, a.A, 1, a.n, a.d_in, a.lda, a.n * a.lda, BK) &&
                make_tensor_map_16bit(&a.map_b, bf16, a.B, 1, a.n, a.d_out, a.ldb, a.n * a.ldb, BK);
@@ -789,7 +942,7 @@ int32_t run_rows(rtma_ctx* ctx, const char* who, bool transposed, int32_t dtype,
     a.va = row_granule(A, lda, es);
     a.vb = std::min(row_granule(W, d_out, es), row_granule(nullptr, w_stride, es));
     a.out = out; a.ldo = ldo;
-    a.vo = row_granule(out, ldo, es) == 16;
+    a.vo = row_granule(out, ldo, es) >= 16 && make_store_map(&a.map_o, dtype, out, n, N, ldo, dtype == RTMA_F32 ? 32 : 64);
     return transposed ? launch_linear<INPUT_GRADIENT>(ctx, dtype, a, KC_GEMM_DGRAD, stream) : launch_linear<FORWARD>(ctx, dtype, a, KC_GEMM_FWD, stream);
 }
 
@@ -837,10 +990,11 @@ extern "C" int32_t rtma_grouped_linear_dw(rtma_ctx* ctx, int32_t dtype, int64_t 
     a.A = X; a.lda = ldx; a.B = dY; a.ldb = lddy;
     a.va = row_granule(X, ldx, es);
     a.vb = row_granule(dY, lddy, es);
-    a.vo = d_out % 4 == 0;
     a.dW = dW; a.dw_stride = dw_stride; a.db = db; a.db_stride = db_stride;
     RTMA_TRY(prepare_row_call(ctx, sizeof(float) * a.tiles * (weights + BIAS_ROWS * (int64_t)d_out), stream));
     a.out = ctx->arena;
+    a.vo = d_out % 4 == 0 && a.tiles * (d_in + BIAS_ROWS) < (int64_t(1) << 31) &&
+           make_store_map(&a.map_o, RTMA_F32, a.out, a.tiles * (d_in + BIAS_ROWS), d_out, d_out, dtype == RTMA_F32 ? 32 : 64);
     if (n > 0) RTMA_TRY(launch_linear<WEIGHT_GRADIENT>(ctx, dtype, a, KC_GEMM_WGRAD, stream));
     {
         KernelScope ks(ctx, KC_REDUCE_SGD, stream);

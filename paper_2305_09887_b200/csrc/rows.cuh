@@ -26,9 +26,9 @@ struct DeviceScope {
 };
 
 inline size_t row_type_bytes(int32_t dtype) { return dtype == RTMA_F32 ? 4 : 2; }
-// The largest power of two, up to 16 bytes, on whose multiples all rows lie.
+// The largest power of two, up to 32 bytes, on whose multiples all rows lie.
 inline int row_granule(const void* p, int64_t ld, size_t element) {
-    const uintptr_t both = reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * (int64_t)element) | 16;
+    const uintptr_t both = reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * (int64_t)element) | 32;
     return (int)(both & (~both + 1));
 }
 // Whether `stream` is being captured into a graph: such a call neither grows the scratch nor waits for other streams.
@@ -97,7 +97,11 @@ struct Eight {
     __device__ __forceinline__ void load(const T* p, int valid, int granule) {
         uint32_t* q = reinterpret_cast<uint32_t*>(w);
         constexpr int WORDS = 2 * sizeof(T);
-        if (valid == 8 && granule == 16) {
+        if (sizeof(T) == 4 && valid == 8 && granule == 32) {
+            asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3]), "=r"(q[WORDS - 4]), "=r"(q[WORDS - 3]), "=r"(q[WORDS - 2]), "=r"(q[WORDS - 1])
+                         : "l"(p));
+        } else if (valid == 8 && granule >= 16) {
 #pragma unroll
             for (int i = 0; i < WORDS / 4; ++i) w[i] = reinterpret_cast<const uint4*>(p)[i];
         } else if (valid == 8 && granule == 8) {
@@ -151,7 +155,11 @@ __device__ __forceinline__ void store_eight(T* p, const float (&v)[8], int valid
 #pragma unroll
             for (int j = 0; j < 4; ++j) q[j] = narrow2(v[2 * j], v[2 * j + 1], static_cast<const T*>(nullptr));
         }
-        if (granule == 16) {
+        if (sizeof(T) == 4 && granule == 32) {
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(q[0]), "r"(q[1]), "r"(q[2]), "r"(q[3]),
+                         "r"(q[WORDS - 4]), "r"(q[WORDS - 3]), "r"(q[WORDS - 2]), "r"(q[WORDS - 1])
+                         : "memory");
+        } else if (granule >= 16) {
 #pragma unroll
             for (int i = 0; i < WORDS / 4; ++i)
                 reinterpret_cast<uint4*>(p)[i] = make_uint4(q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]);
