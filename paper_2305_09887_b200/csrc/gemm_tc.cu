@@ -961,15 +961,15 @@ bool make_store_map(CUtensorMap* out, int type, const void* base, uint64_t rows,
 }
 
 bool make_tensor_map_16bit(CUtensorMap* out, bool bf16, const void* base, uint64_t count, uint64_t rows, uint64_t cols, uint64_t ld, uint64_t stride,
-                           uint32_t box_rows) {
+                           uint32_t box_rows, uint32_t box_cols, uint32_t box_matrices) {
     EncodeTiledFn fn = encode_tiled();
     if (!fn || count == 0 || rows == 0 || cols == 0) return false;
     const cuuint64_t gdim[3] = {cols, rows, count};
     const cuuint64_t gstride[2] = {ld * 2, stride * 2};
-    const cuuint32_t box[3] = {64, box_rows, 1};
+    const cuuint32_t box[3] = {box_cols, box_rows, box_matrices};
     const cuuint32_t estride[3] = {1, 1, 1};
     return fn(out, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(base), gdim, gstride, box, estride,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 

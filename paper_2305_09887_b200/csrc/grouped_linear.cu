@@ -5,149 +5,58 @@
 // One kernel body serves all three: a tile is 128 x BN results, its operands are staged 64 deep in the contraction, each as 32-row
 // slabs of 128 bytes per row in the 128-byte swizzle.  Rows that run along the contraction (X, dY; W in dx) make a K-major
 // operand, rows across it (W forward; X and dY in dw) an MN-major one: both come from memory as they lie, nothing is transposed.
-// fp32 values are split on their way into three bf16 numbers (8 + 8 + 8 bits, the whole significand) and a product is six MMAs;
-// what is left out is below 2^-24 of it.
 //
-// The tensor cores truncate when they accumulate, so a long sum drifts towards zero by half a step per addition.  Where the
-// result is fp32 the drain warps therefore take the accumulator after every 64 terms and add it up in registers, rounded to nearest;
-// inside 64 terms the five small products of fp32 operands come first.
+// The tensor cores truncate when they accumulate, so a long sum drifts towards zero by half a step per addition.  The weight
+// gradient, whose result is fp32, therefore has its drain warps take the accumulator after every 64 rows and add it up in
+// registers, rounded to nearest.
 //
-// Three ways of loading (Loading below), and the warps that go with them:
-//   SPLIT   fp32: 16 warps, 8 per operand, bring values through registers, split them, and drain the stage before; they take turns
-//           at issuing a stage's MMAs
-//   COPIES  16-bit rows that do not all lie on 16-byte boundaries: 8 warps with asynchronous copies of 16, 8 or 4 bytes, 8 drain
-//   BULK    16-bit rows on 16-byte boundaries: one thread with bulk-tensor loads, 8 warps drain
+// This file: 16-bit rows (fp32 ones are in grouped_split.cu).  Two ways of loading:
+//   COPIES  rows that do not all lie on 16-byte boundaries: 8 warps with asynchronous copies of 16, 8 or 4 bytes
+//   BULK    rows on 16-byte boundaries: one thread with bulk-tensor loads
+// then 8 drain warps (a quarter of the lanes, every second 32 columns each) and one warp that issues the MMAs.
 #include <algorithm>
 
-#include "rows.cuh"
-#include "tc_common.cuh"
+#include "grouped_linear.cuh"
 
 RTMA_BOUNDS_TU()
 
 namespace {
 
-enum Mode { FORWARD, INPUT_GRADIENT, WEIGHT_GRADIENT };
+using namespace grouped;
 
-enum Loading { SPLIT, COPIES, BULK };
+enum Loading { COPIES, BULK };
 
 constexpr int BM = 128, BK = 64;
-constexpr int OPERAND_THREADS = 256;       // that load one operand: 8 per row of a slab
 // Registers a thread.  COPIES is launched with 96 (20 warps); the multiplier's four warps and the loading ones give some up to those
 // that drain: 256 x 112 + 256 x 96 + 128 x 64 = 61,440 = 640 x 96.
 constexpr int DRAIN_REGISTERS = 112, MULTIPLY_REGISTERS = 64;
 constexpr int SLAB_BYTES = 32 * 128;       // 32 rows of 64 16-bit values
 constexpr int BIAS_ROWS = 8;               // partial sums of the bias gradient in a slot, one row per warp that adds them up
-constexpr int MAX_STAGES = 6;
 
 template <class T, int MODE, int LOADING>
 struct Form {
-    static constexpr int PLANES = LOADING == SPLIT ? 3 : 1;
-    static constexpr bool IN_REGISTERS = LOADING == SPLIT || MODE == WEIGHT_GRADIENT;  // accumulated there, 64 terms at a time
+    static constexpr bool IN_REGISTERS = MODE == WEIGHT_GRADIENT;  // accumulated there, 64 terms at a time
     static constexpr int BN = IN_REGISTERS ? 128 : 256;                                // widest tile
-    static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128;                       // of a plane
-    static constexpr int STAGE_BYTES = PLANES * (A_BYTES + B_BYTES);
-    // BULK: the results of a tile leave while the next is drained, which is worth more than a fourth stage
-    static constexpr int RING_BYTES = (LOADING == BULK ? (MODE == WEIGHT_GRADIENT ? 160 : 144) : 192) * 1024;
+    static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128;
+    static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
+    // the results of a tile leave while the next is drained, which is worth more than another stage
+    static constexpr int RING_BYTES = (MODE == WEIGHT_GRADIENT ? 160 : 144) * 1024;
     static constexpr int STAGES = RING_BYTES / STAGE_BYTES;
-    static constexpr int DRAIN_WARPS = LOADING == SPLIT ? 16 : 8;
-    static constexpr int OUT_SLABS = LOADING != BULK ? 1 : MODE == WEIGHT_GRADIENT ? 2 : 4;  // of a drain warp: 32 rows of OUT_ROW bytes on
-    static constexpr int OUT_ROW = LOADING == SPLIT ? 32 : 64;                         // their way out
+    static constexpr int DRAIN_WARPS = 8;
+    static constexpr int OUT_SLABS = MODE == WEIGHT_GRADIENT ? 2 : 4;                  // of a drain warp: 32 rows of OUT_ROW bytes on
+    static constexpr int OUT_ROW = 64;                                                 // their way out
     static constexpr int OUT_BYTES = OUT_SLABS * 32 * OUT_ROW;
     static constexpr int DYNAMIC_BYTES = RING_BYTES + 1024 + DRAIN_WARPS * OUT_BYTES;
     static constexpr bool A_ACROSS = MODE == WEIGHT_GRADIENT, B_ACROSS = MODE != INPUT_GRADIENT;  // MN-major
     static constexpr bool DRAIN_SUMS = LOADING == BULK && MODE == WEIGHT_GRADIENT;     // the drain warps add up the columns of dY
     static constexpr int LOAD_WARPS = LOADING == COPIES ? 8 : 0;                       // that do nothing else
-    static constexpr int THREADS = 32 * (DRAIN_WARPS + LOAD_WARPS + (LOADING == SPLIT ? 0 : 4));
-};
-
-struct LinearArgs {
-    const int64_t* offsets;
-    int64_t n;
-    int G, span;
-    int64_t tile_rows, tiles;  // rows of a row tile (forward, dx: 128; dw: of a chunk), row tiles at most
-    int m_tiles, n_tiles;      // tiles of one row tile: m_tiles (dw) x n_tiles
-    int BN;
-    int d_in, d_out;
-    const void *A, *B;         // rows; matrices (forward, dx) or rows (dw)
-    int64_t lda, ldb, w_stride;
-    int va, vb;                // granules of the rows (bytes)
-    bool vo;                   // rows of the result on 16-byte boundaries: map_o holds
-    const void* bias;
-    int64_t bias_stride;
-    void* out;                 // dw: the slots, [row tile][(d_in + BIAS_ROWS) * d_out]
-    int64_t ldo;
-    float *dW, *db;
-    int64_t dw_stride, db_stride;
-    int* error_word;
-    CUtensorMap map_a, map_b;  // BULK
-    CUtensorMap map_o;         // the result (dw: the slots, one below the other)
-};
-
-struct Shared {
-    uint64_t full[MAX_STAGES], empty[MAX_STAGES];
-    uint64_t acc_full[2], acc_empty[2];
-    uint32_t tmem_base;
-    int abort;
-    int32_t warp_sums[32];
-    int32_t tile_start[RTMA_MAX_GROUPS + 1], begin[RTMA_MAX_GROUPS], rows[RTMA_MAX_GROUPS];
-    alignas(16) float bias[8 * 128];  // of every drain warp's columns
-};
-
-__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, Shared& sh, int* error_word) {
-    for (uint32_t i = 0; i < tc::WAIT_POLLS; ++i) {
-        if (tc::mbar_try_wait(bar, parity)) return true;
-        if ((i & 1023u) == 1023u && *reinterpret_cast<volatile int*>(&sh.abort)) break;
-    }
-    *reinterpret_cast<volatile int*>(&sh.abort) = 1;
-    atomicExch(error_word, 1);
-    return false;
-}
-
-// A role's walk over a block's tiles and their stages.
-template <int MODE>
-struct Walk {
-    int tile, part, row_tile, m0, n0;
-    int64_t row0;     // first row of the tile
-    int rows, k_end;  // rows of the tile; terms of the contraction
-    int k0;
-    __device__ __forceinline__ bool at(const LinearArgs& a, const Shared& sh) {
-        const int per = a.m_tiles * a.n_tiles;
-        row_tile = tile / per;
-        if (row_tile >= sh.tile_start[a.G]) return false;
-        const int rest = tile - row_tile * per;
-        m0 = rest / a.n_tiles * BM;
-        n0 = rest % a.n_tiles * a.BN;
-        part = part_of_tile(sh.tile_start, a.G, row_tile);
-        const int64_t inside = (int64_t)(row_tile - sh.tile_start[part]) * a.tile_rows;
-        row0 = sh.begin[part] + inside;
-        rows = (int)min((int64_t)sh.rows[part] - inside, a.tile_rows);
-        k_end = MODE == FORWARD ? a.d_in : MODE == INPUT_GRADIENT ? a.d_out : rows;
-        k0 = 0;
-        return true;
-    }
-    __device__ __forceinline__ bool first(const LinearArgs& a, const Shared& sh) {
-        tile = blockIdx.x;
-        return at(a, sh);
-    }
-    __device__ __forceinline__ bool last_stage() const { return k0 + BK >= k_end; }
-    __device__ __forceinline__ bool next(const LinearArgs& a, const Shared& sh) {  // the next stage
-        if (!last_stage()) {
-            k0 += BK;
-            return true;
-        }
-        tile += gridDim.x;
-        return at(a, sh);
-    }
-    __device__ __forceinline__ bool next_tile(const LinearArgs& a, const Shared& sh) {
-        tile += gridDim.x;
-        return at(a, sh);
-    }
+    static constexpr int THREADS = 32 * (DRAIN_WARPS + LOAD_WARPS + 4);
 };
 
 // Where the eight values of slab i that a loading thread (row 0..31 of the slab, unit 0..7 of the row) brings come from, and how
 // many of them exist.
 template <class T, int MODE>
-__device__ __forceinline__ const T* source_a(const LinearArgs& a, const Walk<MODE>& w, int i, int row, int unit, int& valid) {
+__device__ __forceinline__ const T* source_a(const LinearArgs& a, const Walk<MODE, BM, BK>& w, int i, int row, int unit, int& valid) {
     const T* A = static_cast<const T*>(a.A);
     if constexpr (MODE == WEIGHT_GRADIENT) {
         const int k = w.k0 + 32 * (i & 1) + row, c = w.m0 + 64 * (i >> 1) + 8 * unit;
@@ -160,7 +69,7 @@ __device__ __forceinline__ const T* source_a(const LinearArgs& a, const Walk<MOD
     }
 }
 template <class T, int MODE>
-__device__ __forceinline__ const T* source_b(const LinearArgs& a, const Walk<MODE>& w, int i, int row, int unit, int& valid) {
+__device__ __forceinline__ const T* source_b(const LinearArgs& a, const Walk<MODE, BM, BK>& w, int i, int row, int unit, int& valid) {
     const T* B = static_cast<const T*>(a.B);
     if constexpr (MODE == INPUT_GRADIENT) {
         const int r = w.n0 + 32 * i + row, c = w.k0 + 8 * unit;
@@ -191,37 +100,9 @@ __device__ __forceinline__ void copy_pieces(uint32_t dst, const void* src, int b
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ void store_16(uint32_t dst, uint4 v) {
-    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-}
-__device__ __forceinline__ uint4 load_16(uint32_t src) {
-    uint4 v;
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(src) : "memory");
-    return v;
-}
-
-// Eight fp32 values as three bf16 numbers each, x = h + m + l exactly (but for bits below the smallest bf16 number).  h is cut off
-// so that no finite value becomes an infinity, m is rounded to nearest so that the products left out (m l, l m, l l: below 2^-22 of
-// the product) have no preferred sign.  An infinity or NaN leaves NaN in m.
-__device__ __forceinline__ void split_eight(const uint32_t (&x)[8], uint4 (&planes)[3]) {
-    uint32_t h[4], m[4], l[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t a = x[2 * i], b = x[2 * i + 1];
-        h[i] = __byte_perm(a, b, 0x7632);
-        const float r0 = __uint_as_float(a) - __uint_as_float(a & 0xFFFF0000u), r1 = __uint_as_float(b) - __uint_as_float(b & 0xFFFF0000u);
-        const __nv_bfloat162 t = __floats2bfloat162_rn(r0, r1);
-        m[i] = *reinterpret_cast<const uint32_t*>(&t);
-        l[i] = __byte_perm(__float_as_uint(r0 - __uint_as_float(m[i] << 16)), __float_as_uint(r1 - __uint_as_float(m[i] & 0xFFFF0000u)), 0x7632);
-    }
-    planes[0] = make_uint4(h[0], h[1], h[2], h[3]);
-    planes[1] = make_uint4(m[0], m[1], m[2], m[3]);
-    planes[2] = make_uint4(l[0], l[1], l[2], l[3]);
-}
-
 // Sums over a warp's rows of the columns of dY that its lanes hold, written to the warp's row of the slot.
 __device__ __forceinline__ void leave_bias(const LinearArgs& a, int row_tile, int n0, float (&sums)[2][8], int warp, int lane) {
-    float* to = static_cast<float*>(a.out) + ((int64_t)row_tile * (a.d_in + BIAS_ROWS) + a.d_in + warp) * a.d_out;
+    float* to = static_cast<float*>(a.out) + ((int64_t)row_tile * (a.d_in + BIAS_ROWS) + a.d_in + warp) * a.ldo;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -233,65 +114,6 @@ __device__ __forceinline__ void leave_bias(const LinearArgs& a, int row_tile, in
             if (lane < 8 && c < a.BN && n0 + c < a.d_out) to[n0 + c] = s;
             sums[t][j] = 0.f;
         }
-}
-
-// The same source for a thread that walks down one operand stage by stage: an address per tile, steps from there.
-template <class T, int MODE, bool IS_B>
-struct Cursor {
-    static constexpr bool ACROSS = IS_B ? MODE != INPUT_GRADIENT : MODE == WEIGHT_GRADIENT;
-    const T* p;         // this thread's first value of the tile
-    int tile, k0, k_end;
-    int near, cols;     // along: rows from this thread's on, terms;  across: terms from this thread's row on, columns from its unit on
-    int row_tile, m0, n0;
-    __device__ __forceinline__ bool open(const LinearArgs& a, const Shared& sh, int row, int unit) {
-        Walk<MODE> w;
-        w.tile = tile;
-        if (!w.at(a, sh)) return false;
-        k0 = 0;
-        k_end = w.k_end;
-        row_tile = w.row_tile;
-        m0 = w.m0;
-        n0 = w.n0;
-        const T* base = static_cast<const T*>(IS_B ? a.B : a.A);
-        if constexpr (ACROSS) {
-            const int c = (IS_B ? n0 : m0) + 8 * unit;
-            near = k_end - row;
-            cols = (IS_B ? a.d_out : a.d_in) - c;
-            p = base + (MODE == WEIGHT_GRADIENT ? (w.row0 + row) * (IS_B ? a.ldb : a.lda) : w.part * a.w_stride + (int64_t)row * a.d_out) + c;
-        } else {
-            near = (IS_B ? a.d_in - n0 : w.rows) - row;
-            cols = k_end - 8 * unit;
-            p = base + (IS_B ? w.part * a.w_stride + (int64_t)(n0 + row) * a.d_out : (w.row0 + row) * a.lda) + 8 * unit;
-        }
-        return true;
-    }
-    __device__ __forceinline__ bool first(const LinearArgs& a, const Shared& sh, int row, int unit) {
-        tile = blockIdx.x;
-        return open(a, sh, row, unit);
-    }
-    __device__ __forceinline__ bool last_stage() const { return k0 + BK >= k_end; }
-    __device__ __forceinline__ bool next(const LinearArgs& a, const Shared& sh, int row, int unit) {
-        if (!last_stage()) {
-            k0 += BK;
-            return true;
-        }
-        tile += gridDim.x;
-        return open(a, sh, row, unit);
-    }
-    __device__ __forceinline__ void load(const LinearArgs& a, int i, Eight<T>& to, int granule) const {
-        const int64_t ld = MODE == WEIGHT_GRADIENT ? (IS_B ? a.ldb : a.lda) : IS_B ? (int64_t)a.d_out : a.lda;
-        if constexpr (ACROSS) {
-            const int k = k0 + 32 * (i & 1);
-            to.load(p + k * ld + 64 * (i >> 1), k < near ? min(8, cols - 64 * (i >> 1)) : 0, granule);
-        } else {
-            to.load(p + 32 * i * ld + k0, 32 * i < near ? min(8, cols - k0) : 0, granule);
-        }
-    }
-};
-
-__device__ __forceinline__ void add_eight(float (&sums)[8], const float (&v)[8]) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sums[j] += v[j];
 }
 
 template <int N>
@@ -328,9 +150,9 @@ __device__ __forceinline__ void copy_role(const LinearArgs& a, Shared& sh, uint3
     const int b_slabs = F::B_ACROSS ? 2 * ((a.BN + 63) / 64) : (a.BN + 31) / 32;
     float sums[SUMS ? 2 : 1][8];
     if constexpr (SUMS) clear(sums);
-    Walk<MODE> w;
+    Walk<MODE, BM, BK> w;
     bool more = w.first(a, sh);
-    Walk<MODE> late = w;
+    Walk<MODE, BM, BK> late = w;
     tc::RingAt at, late_at;
     int under_way = 0;
     auto hand_over = [&]() {
@@ -398,7 +220,7 @@ __device__ __forceinline__ void bulk_role(const LinearArgs& a, Shared& sh, uint8
         tc::prefetch_tensormap(&a.map_a);
         tc::prefetch_tensormap(&a.map_b);
     }
-    Walk<MODE> w;
+    Walk<MODE, BM, BK> w;
     tc::RingAt at;
     for (bool more = w.first(a, sh); more; more = w.next(a, sh), at.advance(F::STAGES)) {
         if (!wait_for(&sh.empty[at.s], at.phase ^ 1u, sh, a.error_word)) return;
@@ -447,20 +269,9 @@ __device__ __forceinline__ void multiply_stage(const LinearArgs& a, uint32_t d, 
                            ((uint32_t)(a.BN >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
     const uint64_t desc = tc::smem_desc_sw128(0, 2 * SLAB_BYTES, 1024);  // atoms of 64 columns lie two slabs apart
     constexpr uint32_t a_step = F::A_ACROSS ? 128 : 2, b_step = F::B_ACROSS ? 128 : 2;  // 16 terms further, in units of 16 bytes
-    constexpr uint32_t a_plane = F::A_BYTES >> 4, b_plane = F::B_BYTES >> 4;
-    uint64_t da = desc + (stage >> 4), db = da + F::PLANES * a_plane;
+    constexpr uint32_t a_plane = F::A_BYTES >> 4;
+    uint64_t da = desc + (stage >> 4), db = da + a_plane;
     const int steps = (terms + 15) >> 4;
-    if constexpr (LOADING == SPLIT) {
-        uint64_t sa = da, sb = db;
-        for (int k = 0; k < steps; ++k, sa += a_step, sb += b_step) {
-            tc::mma_bf16(d, sa + 2 * a_plane, sb, idesc, accumulate);
-            accumulate = 1u;
-            tc::mma_bf16(d, sa, sb + 2 * b_plane, idesc, 1u);
-            tc::mma_bf16(d, sa + a_plane, sb + b_plane, idesc, 1u);
-            tc::mma_bf16(d, sa + a_plane, sb, idesc, 1u);
-            tc::mma_bf16(d, sa, sb + b_plane, idesc, 1u);
-        }
-    }
     for (int k = 0; k < steps; ++k, da += a_step, db += b_step) {
         tc::mma_bf16(d, da, db, idesc, accumulate);
         accumulate = 1u;
@@ -470,7 +281,7 @@ __device__ __forceinline__ void multiply_stage(const LinearArgs& a, uint32_t d, 
 template <class T, int MODE, int LOADING>
 __device__ __forceinline__ void multiply_role(const LinearArgs& a, Shared& sh, uint32_t ring) {
     typedef Form<T, MODE, LOADING> F;
-    Walk<MODE> w;
+    Walk<MODE, BM, BK> w;
     tc::RingAt at, acc;
     for (bool more = w.first(a, sh); more; more = w.next(a, sh)) {
         if (F::IN_REGISTERS || w.k0 == 0) {
@@ -488,110 +299,16 @@ __device__ __forceinline__ void multiply_role(const LinearArgs& a, Shared& sh, u
     }
 }
 
-// A drain warp's results on their way out: ROW bytes of each of its 32 rows (a row per lane) at a time go through one of its slabs,
-// in the map's swizzle of ROW bytes, so that they leave as one bulk-tensor store; boxes that would reach rows or columns that are
-// not this tile's, and rows off the 16-byte boundaries, are written by the lanes.
-template <class O, int SLABS, int ROW>
-struct Outlet {
-    uint32_t slabs;
-    int at = 0;
-    __device__ __forceinline__ static int swizzle(int row) { return ROW == 64 ? (row >> 1) & 3 : (row >> 2) & 1; }
-    // row0, c: place in the map; rows, cols: how much is this tile's; whole: all columns of the matrix from c on are, and end on a
-    // 16-byte boundary (a store's box is cut off at the edge of the matrix only in steps of 16 bytes)
-    __device__ __forceinline__ void put(const LinearArgs& a, const float (&v)[32], int64_t row0, int c, int rows, int cols, bool whole, O* out, int64_t ldo, int lane) {
-        constexpr int WIDE = ROW / sizeof(O), PIECE = 16 / sizeof(O);
-#pragma unroll
-        for (int c0 = 0; c0 < 32; c0 += WIDE) {
-            if (c0 >= cols) break;
-            const uint32_t slab = slabs + at * 32 * ROW;
-            if (lane == 0) tc::tma_store_wait_read_but<SLABS - 1>();  // the slab's last store has read it
-            __syncwarp();
-#pragma unroll
-            for (int q = 0; q < ROW / 16; ++q) {
-                const int e = c0 + q * PIECE;
-                uint4 x;
-                if constexpr (sizeof(O) == 4) {
-                    x = make_uint4(__float_as_uint(v[e]), __float_as_uint(v[e + 1]), __float_as_uint(v[e + 2]), __float_as_uint(v[e + 3]));
-                } else {
-                    const O* tag = nullptr;
-                    x = make_uint4(narrow2(v[e], v[e + 1], tag), narrow2(v[e + 2], v[e + 3], tag), narrow2(v[e + 4], v[e + 5], tag), narrow2(v[e + 6], v[e + 7], tag));
-                }
-                store_16(slab + lane * ROW + ((q ^ swizzle(lane)) << 4), x);
-            }
-            const bool bulk = a.vo && rows == 32 && (cols - c0 >= WIDE || whole);
-            if (bulk) tc::fence_proxy_async_smem();
-            __syncwarp();
-            if (bulk) {
-                if (lane == 0) {
-                    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
-                                 ::"l"(reinterpret_cast<uint64_t>(&a.map_o)), "r"(slab), "r"(c + c0), "r"((int32_t)row0)
-                                 : "memory");
-                }
-            } else {
-                const int x = lane % WIDE;
-                for (int r = lane / WIDE; r < rows; r += 32 / WIDE) {
-                    const uint32_t from = slab + r * ROW + (((x / PIECE) ^ swizzle(r)) << 4) + (x % PIECE) * (int)sizeof(O);
-                    O y;
-                    if constexpr (sizeof(O) == 4) {
-                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(y) : "r"(from) : "memory");
-                    } else {
-                        unsigned short bits;
-                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(bits) : "r"(from) : "memory");
-                        y = *reinterpret_cast<O*>(&bits);
-                    }
-                    if (c0 + x < cols) out[r * ldo + c0 + x] = y;
-                }
-            }
-            if (lane == 0) tc::tma_store_commit();  // a group for every slab, empty or not
-            at = at + 1 == SLABS ? 0 : at + 1;
-        }
-    }
-    __device__ __forceinline__ void finish(int lane) const {
-        if (lane == 0) tc::tma_store_wait_all();
-    }
-};
-
-// The bias of a warp's `count` columns from column c of the tile, kept in shared memory until the part or the columns change.
-template <class T, int MODE>
-struct BiasHolder {
-    float* at;  // 16-byte boundary
-    int part = -1, n0 = -1;
-    __device__ __forceinline__ void fetch(const LinearArgs& a, const Walk<MODE>& w, int c, int step, int chunks, int lane) {
-        if (w.part == part && w.n0 == n0) return;
-        part = w.part;
-        n0 = w.n0;
-        const T* bias = static_cast<const T*>(a.bias) + part * a.bias_stride + n0;
-        __syncwarp();
-        for (int chunk = c, i = 0; chunk < chunks; chunk += step, ++i) {
-            const int col = 32 * chunk + lane;
-            at[32 * i + lane] = col < a.BN && n0 + col < a.d_out ? to_f32(bias[col]) : 0.f;
-        }
-        __syncwarp();
-    }
-    __device__ __forceinline__ void add(float (&v)[32], int i) const {
-        const float4* b = reinterpret_cast<const float4*>(at + 32 * i);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float4 x = b[j];
-            v[4 * j] += x.x;
-            v[4 * j + 1] += x.y;
-            v[4 * j + 2] += x.z;
-            v[4 * j + 3] += x.w;
-        }
-    }
-};
-
 // 32 columns (chunk `chunk` of the tile) of a warp's 32 rows (its quarter of the tile's) to the result.
 template <class T, int MODE, class OUT>
-__device__ __forceinline__ void put_chunk(const LinearArgs& a, const Walk<MODE>& w, OUT& outlet, const float (&v)[32], int quarter, int chunk, int lane) {
+__device__ __forceinline__ void put_chunk(const LinearArgs& a, const Walk<MODE, BM, BK>& w, OUT& outlet, const float (&v)[32], int quarter, int chunk, int lane) {
     typedef typename std::conditional<MODE == WEIGHT_GRADIENT, float, T>::type O;
-    const int N = MODE == INPUT_GRADIENT ? a.d_in : a.d_out;
+    const int N = MODE == INPUT_GRADIENT ? a.d_in : MODE == FORWARD ? a.d_out : (int)a.ldo;  // (dw: the slots' rows are padded)
     const int c = w.n0 + 32 * chunk, cols = min(min(32, a.BN - 32 * chunk), N - c);
     const int rows = min(32, (MODE == WEIGHT_GRADIENT ? min(BM, a.d_in - w.m0) : w.rows) - 32 * quarter);
     if (cols <= 0 || rows <= 0) return;
     const int64_t row0 = (MODE == WEIGHT_GRADIENT ? (int64_t)w.row_tile * (a.d_in + BIAS_ROWS) + w.m0 : w.row0) + 32 * quarter;
-    const int64_t ldo = MODE == WEIGHT_GRADIENT ? a.d_out : a.ldo;
-    outlet.put(a, v, row0, c, rows, cols, c + cols == N && N % (16 / (int)sizeof(O)) == 0, static_cast<O*>(a.out) + row0 * ldo + c, ldo, lane);
+    outlet.put(a, v, row0, c, rows, cols, c + cols == N && N % (16 / (int)sizeof(O)) == 0, static_cast<O*>(a.out) + row0 * a.ldo + c, a.ldo, lane);
 }
 
 template <class T, int MODE, int LOADING>
@@ -600,10 +317,10 @@ __device__ __forceinline__ void drain_role(const LinearArgs& a, Shared& sh, uint
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, half = warp >> 2;
     typedef typename std::conditional<MODE == WEIGHT_GRADIENT, float, T>::type O;
     Outlet<O, F::OUT_SLABS, F::OUT_ROW> outlet{slabs + warp * F::OUT_BYTES};
-    BiasHolder<T, MODE> bias{sh.bias + 128 * warp};
+    BiasHolder<T> bias{sh.bias + 128 * warp};
     const uint32_t lanes = (uint32_t)(32 * quarter) << 16;
     const int chunks = (a.BN + 31) / 32;
-    Walk<MODE> w;
+    Walk<MODE, BM, BK> w;
     tc::RingAt acc, at;
     float sums[F::DRAIN_SUMS ? 2 : 1][8];
     if constexpr (F::DRAIN_SUMS) clear(sums);
@@ -653,7 +370,7 @@ __device__ __forceinline__ void drain_role(const LinearArgs& a, Shared& sh, uint
             for (int i = 0; i < 2; ++i)
                 if (half + 2 * i < chunks) put_chunk<T, MODE>(a, w, outlet, total[i], quarter, half + 2 * i, lane);
         } else {
-            if (MODE == FORWARD && a.bias) bias.fetch(a, w, half, 2, chunks, lane);
+            if (MODE == FORWARD && a.bias) bias.fetch(a, w.part, w.n0, half, 2, chunks, lane);
             if (!wait_for(&sh.acc_full[acc.s], acc.phase, sh, a.error_word)) return;
             __syncwarp();
             tc::tc_fence_after_sync();
@@ -672,119 +389,19 @@ __device__ __forceinline__ void drain_role(const LinearArgs& a, Shared& sh, uint
     outlet.finish(lane);
 }
 
-// fp32 rows: a warp of one operand (t: 0..255 of its threads).  A stage's values wait in registers; as soon as one piece is split
-// and stored, the same piece of the next stage is on its way.  Then the warp takes its 32 columns of the stage before from tensor
-// memory: when that has been multiplied, its place in the ring and its accumulator are free, so the next
-// stage needs no other leave, and the tensor cores work on one while the warps split the next.
-template <int MODE, bool IS_B>
-__device__ __forceinline__ void split_role(const LinearArgs& a, Shared& sh, uint32_t slabs, uint32_t ring, int t) {
-    typedef Form<float, MODE, SPLIT> F;
-    const int row = t >> 3, unit = t & 7, lane = t & 31, warp = threadIdx.x >> 5, quarter = warp & 3, chunk = warp >> 2;
-    const uint32_t place = (IS_B ? F::PLANES * F::A_BYTES : 0) + row * 128 + ((unit ^ (row & 7)) << 4);
-    constexpr bool SUMS = IS_B && MODE == WEIGHT_GRADIENT;
-    const int pieces = !IS_B ? 4 : F::B_ACROSS ? 2 * ((a.BN + 63) / 64) : (a.BN + 31) / 32, granule = IS_B ? a.vb : a.va;
-    const bool drains = chunk < (a.BN + 31) / 32;
-    const uint32_t tmem = sh.tmem_base + ((uint32_t)(32 * quarter) << 16) + 32 * chunk;
-    Outlet<float, F::OUT_SLABS, F::OUT_ROW> outlet{slabs + warp * F::OUT_BYTES};
-    BiasHolder<float, MODE> bias{sh.bias + 32 * warp};
-    float sums[SUMS ? 2 : 1][8], total[32];
-    if constexpr (SUMS) clear(sums);
-    Eight<float> held[4];
-    Cursor<float, MODE, IS_B> c;
-    Walk<MODE> out;  // the tile that is drained
-    bool more = c.first(a, sh, row, unit);
-    out.first(a, sh);
-    if (more) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < pieces) c.load(a, i, held[i], granule);
-    }
-    auto drain = [&](const tc::RingAt& stage) {
-        if (!wait_for(&sh.acc_full[stage.s], stage.phase, sh, a.error_word)) return false;
-        __syncwarp();
-        tc::tc_fence_after_sync();
-        if (drains) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                float v[8];
-                tc::tmem_load_32x8(tmem + stage.s * F::BN + 8 * q, v);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) total[8 * q + j] = out.k0 ? total[8 * q + j] + v[j] : v[j];
-            }
-            if (out.last_stage()) {
-                if (MODE == FORWARD && a.bias) {
-                    bias.fetch(a, out, chunk, 4, min(chunk + 1, (a.BN + 31) / 32), lane);
-                    bias.add(total, 0);
-                }
-                put_chunk<float, MODE>(a, out, outlet, total, quarter, chunk, lane);
-            }
-        }
-        out.next(a, sh);
-        tc::tc_fence_before_sync();
-        return true;
-    };
-    tc::RingAt at, before;
-    bool pending = false;
-    int turn = 0;
-    while (more) {
-        const bool wanted = SUMS && c.m0 == 0 && a.db, last = c.last_stage();
-        const int row_tile = c.row_tile, n0 = c.n0, terms = min(BK, c.k_end - c.k0);
-        more = c.next(a, sh, row, unit);
-        const uint32_t stage = ring + at.s * F::STAGE_BYTES + place;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (i < pieces) {
-                uint4 planes[3];
-                if constexpr (SUMS) {
-                    if (wanted) {
-                        float v[8];
-                        held[i].values(v);
-                        add_eight(sums[i >> 1], v);
-                    }
-                }
-                split_eight(reinterpret_cast<const uint32_t(&)[8]>(held[i].w), planes);
-#pragma unroll
-                for (int k = 0; k < 3; ++k) store_16(stage + k * (IS_B ? F::B_BYTES : F::A_BYTES) + i * SLAB_BYTES, planes[k]);
-                if (more) c.load(a, i, held[i], granule);
-            }
-        }
-        tc::fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&sh.full[at.s]);
-        if constexpr (SUMS)
-            if (wanted && last) leave_bias(a, row_tile, n0, sums, t >> 5, lane);
-        if (warp == turn) {
-            if (!wait_for(&sh.full[at.s], at.phase, sh, a.error_word)) return;
-            tc::tc_fence_after_sync();
-            if (lane == 0) {
-                multiply_stage<float, MODE, SPLIT>(a, sh.tmem_base + at.s * F::BN, ring + at.s * F::STAGE_BYTES, terms, 0u);
-                tc::mma_commit(&sh.acc_full[at.s]);
-            }
-            __syncwarp();
-        }
-        turn = (turn + 1) & 15;
-        if (pending && !drain(before)) return;
-        pending = true;
-        before = at;
-        at.advance(2);
-    }
-    if (pending && !drain(before)) return;
-    outlet.finish(lane);
-}
-
 template <class T, int MODE, int LOADING>
 __global__ void __launch_bounds__(Form<T, MODE, LOADING>::THREADS, 1) linear_kernel(const __grid_constant__ LinearArgs a) {
     typedef Form<T, MODE, LOADING> F;
-    static_assert(F::DYNAMIC_BYTES + sizeof(Shared) <= 232448 && F::STAGES <= MAX_STAGES, "shared memory of a block");
+    static_assert(F::DYNAMIC_BYTES + sizeof(Shared) <= SMEM_MOST && F::STAGES <= MAX_STAGES, "shared memory of a block");
     extern __shared__ uint8_t raw[];
     __shared__ Shared sh;
     uint8_t* ring_bytes = raw + ((1024u - (tc::smem_u32(raw) & 1023u)) & 1023u);
     const uint32_t ring = tc::smem_u32(ring_bytes), slabs = ring + F::RING_BYTES;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr int MULTIPLIER = F::DRAIN_WARPS + F::LOAD_WARPS, OWNER = LOADING == SPLIT ? 0 : MULTIPLIER;  // OWNER: of tensor memory
+    constexpr int MULTIPLIER = F::DRAIN_WARPS + F::LOAD_WARPS;
     if (threadIdx.x == 0) {
         for (int s = 0; s < F::STAGES; ++s) {
-            tc::mbar_init(&sh.full[s], LOADING == BULK ? 1 : LOADING == SPLIT ? F::DRAIN_WARPS : F::LOAD_WARPS);
+            tc::mbar_init(&sh.full[s], LOADING == BULK ? 1 : F::LOAD_WARPS);
             tc::mbar_init(&sh.empty[s], 1 + (F::DRAIN_SUMS && a.db ? F::DRAIN_WARPS : 0));
         }
         for (int b = 0; b < 2; ++b) {
@@ -794,7 +411,7 @@ __global__ void __launch_bounds__(Form<T, MODE, LOADING>::THREADS, 1) linear_ker
         sh.abort = 0;
         tc::fence_barrier_init();
     }
-    if (warp == OWNER) {
+    if (warp == MULTIPLIER) {
         tc::tmem_alloc(&sh.tmem_base, 2 * F::BN);
         tc::tmem_relinquish();
     }
@@ -810,28 +427,23 @@ __global__ void __launch_bounds__(Form<T, MODE, LOADING>::THREADS, 1) linear_ker
     __syncthreads();
     tc::tc_fence_after_sync();
     if (warp < F::DRAIN_WARPS) {
-        if constexpr (LOADING == SPLIT) {
-            if (threadIdx.x < OPERAND_THREADS) split_role<MODE, false>(a, sh, slabs, ring, threadIdx.x);
-            else split_role<MODE, true>(a, sh, slabs, ring, threadIdx.x - OPERAND_THREADS);
-        } else {
-            if constexpr (LOADING == COPIES) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(DRAIN_REGISTERS));
-            drain_role<T, MODE, LOADING>(a, sh, slabs, ring);
-        }
+        if constexpr (LOADING == COPIES) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(DRAIN_REGISTERS));
+        drain_role<T, MODE, LOADING>(a, sh, slabs, ring);
     } else if (warp < MULTIPLIER) {
         if constexpr (LOADING == COPIES) {
             copy_role<T, MODE>(a, sh, ring, threadIdx.x - 32 * F::DRAIN_WARPS);
         }
     } else {
         if constexpr (LOADING == COPIES) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(MULTIPLY_REGISTERS));
-        if constexpr (LOADING != SPLIT)
-            if (warp == MULTIPLIER && lane == 0) multiply_role<T, MODE, LOADING>(a, sh, ring);
+        if (warp == MULTIPLIER && lane == 0) multiply_role<T, MODE, LOADING>(a, sh, ring);
         if constexpr (LOADING == BULK)
             if (warp == MULTIPLIER + 1) bulk_role<T, MODE>(a, sh, ring_bytes, lane);
     }
     __syncwarp();
+    if (*reinterpret_cast<volatile int*>(&sh.abort)) __nanosleep(1000000);  // a wait ran out: copies and MMAs under way land before the block ends
     tc::tc_fence_before_sync();
     __syncthreads();
-    if (warp == OWNER) {
+    if (warp == MULTIPLIER) {
         tc::tc_fence_after_sync();
         tc::tmem_dealloc(sh.tmem_base, 2 * F::BN);
     }
@@ -844,19 +456,19 @@ __global__ void __launch_bounds__(REDUCE_THREADS) linear_reduce_kernel(const __g
     wait_for_kernel_before();
     number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums, a.span);
     const int part = blockIdx.y;
-    const int64_t weights = (int64_t)a.d_in * a.d_out, slot = weights + BIAS_ROWS * (int64_t)a.d_out, i = (int64_t)blockIdx.x * REDUCE_THREADS + threadIdx.x;
+    const int64_t weights = (int64_t)a.d_in * a.d_out, slot = (a.d_in + a.bias_rows) * a.ldo, i = (int64_t)blockIdx.x * REDUCE_THREADS + threadIdx.x;
     if (i >= weights + a.d_out) return;
+    const int64_t row = i / a.d_out, from = row * a.ldo + (i - row * a.d_out);
     const float* p = static_cast<const float*>(a.out);
     const int t1 = tile_start[part + 1];
     float s = 0.f;
     if (i < weights) {
 #pragma unroll 8
-        for (int t = tile_start[part]; t < t1; ++t) s += p[(int64_t)t * slot + i];
+        for (int t = tile_start[part]; t < t1; ++t) s += p[(int64_t)t * slot + from];
         a.dW[part * a.dw_stride + i] = s;
     } else if (a.db) {
         for (int t = tile_start[part]; t < t1; ++t)
-#pragma unroll
-            for (int k = 0; k < BIAS_ROWS; ++k) s += p[(int64_t)t * slot + i + (int64_t)k * a.d_out];
+            for (int k = 0; k < a.bias_rows; ++k) s += p[(int64_t)t * slot + from + k * a.ldo];
         a.db[part * a.db_stride + i - weights] = s;
     }
 }
@@ -897,16 +509,16 @@ bool bulk_maps(LinearArgs& a, bool bf16) {
 template <int MODE>
 int32_t launch_linear(rtma_ctx* ctx, int32_t dtype, LinearArgs& a, int cls, cudaStream_t stream) {
     a.error_word = ctx->error_word;
+    if (dtype == RTMA_F32) return launch_split(ctx, MODE, a, MODE == WEIGHT_GRADIENT ? nullptr : ctx->arena, cls, stream);
     const int64_t tiles = a.tiles * a.m_tiles * a.n_tiles;
     if (tiles >= (int64_t(1) << 30)) return rtma_fail(ctx, RTMA_ERR_OVERFLOW, "grouped product: %lld tiles", (long long)tiles);
     const unsigned grid = (unsigned)(tiles < ctx->sm_count ? tiles : ctx->sm_count);
-    bool* configured = ctx->linear_configured + MODE * 5;
+    bool* configured = ctx->linear_configured + MODE * 4;
     KernelScope ks(ctx, cls, stream);
-    if (dtype == RTMA_F32) return launch_form<float, MODE, SPLIT>(ctx, a, grid, configured[0], stream);
     const bool bf16 = dtype == RTMA_BF16;
     if (bulk_maps<MODE>(a, bf16))
-        return bf16 ? launch_form<__nv_bfloat16, MODE, BULK>(ctx, a, grid, configured[1], stream) : launch_form<__half, MODE, BULK>(ctx, a, grid, configured[2], stream);
-    return bf16 ? launch_form<__nv_bfloat16, MODE, COPIES>(ctx, a, grid, configured[3], stream) : launch_form<__half, MODE, COPIES>(ctx, a, grid, configured[4], stream);
+        return bf16 ? launch_form<__nv_bfloat16, MODE, BULK>(ctx, a, grid, configured[0], stream) : launch_form<__half, MODE, BULK>(ctx, a, grid, configured[1], stream);
+    return bf16 ? launch_form<__nv_bfloat16, MODE, COPIES>(ctx, a, grid, configured[2], stream) : launch_form<__half, MODE, COPIES>(ctx, a, grid, configured[3], stream);
 }
 
 int32_t check_linear(rtma_ctx* ctx, const char* who, int32_t dtype, int64_t n, int32_t G, const int64_t* offsets, int32_t d_in, int32_t d_out) {
@@ -929,20 +541,21 @@ int32_t run_rows(rtma_ctx* ctx, const char* who, bool transposed, int32_t dtype,
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     DeviceScope on(ctx->device);
     RTMA_CUDA(ctx, on.status);
-    RTMA_TRY(prepare_row_call(ctx, 0, stream));
     const size_t es = row_type_bytes(dtype);
     LinearArgs a{};
     a.offsets = offsets; a.n = n; a.G = G; a.span = 1;
     a.tile_rows = BM;
     a.tiles = n / BM + G;
     a.m_tiles = 1;
-    cut_columns(a, N, dtype == RTMA_F32 ? 128 : 256);
+    cut_columns(a, N, 256);
     a.d_in = d_in; a.d_out = d_out;
     a.A = A; a.lda = lda; a.B = W; a.w_stride = w_stride; a.bias = b; a.bias_stride = b_stride;
     a.va = row_granule(A, lda, es);
     a.vb = std::min(row_granule(W, d_out, es), row_granule(nullptr, w_stride, es));
     a.out = out; a.ldo = ldo;
-    a.vo = row_granule(out, ldo, es) >= 16 && make_store_map(&a.map_o, dtype, out, n, N, ldo, dtype == RTMA_F32 ? 32 : 64);
+    a.go = row_granule(out, ldo, es);
+    a.vo = dtype != RTMA_F32 && a.go >= 16 && make_store_map(&a.map_o, dtype, out, n, N, ldo, 64);
+    RTMA_TRY(prepare_row_call(ctx, dtype == RTMA_F32 ? split_planes_bytes(a) : 0, stream));
     return transposed ? launch_linear<INPUT_GRADIENT>(ctx, dtype, a, KC_GEMM_DGRAD, stream) : launch_linear<FORWARD>(ctx, dtype, a, KC_GEMM_FWD, stream);
 }
 
@@ -979,7 +592,8 @@ extern "C" int32_t rtma_grouped_linear_dw(rtma_ctx* ctx, int32_t dtype, int64_t 
     a.offsets = offsets; a.n = n;
     a.G = shared ? 1 : G;
     a.span = shared ? G : 1;
-    a.m_tiles = (int)ceil_div(d_in, BM);
+    a.m_tiles = (int)ceil_div(d_in, dtype == RTMA_F32 ? SPLIT_DW_ROWS : BM);
+    a.bias_rows = dtype == RTMA_F32 ? SPLIT_BIAS_ROWS : BIAS_ROWS;
     cut_columns(a, d_out, 128);
     // about four tiles per SM over the whole call; chunks of whole stages
     const int64_t chunk = ceil_div(n * a.m_tiles * a.n_tiles, 4 * (int64_t)ctx->sm_count);
@@ -991,10 +605,12 @@ extern "C" int32_t rtma_grouped_linear_dw(rtma_ctx* ctx, int32_t dtype, int64_t 
     a.va = row_granule(X, ldx, es);
     a.vb = row_granule(dY, lddy, es);
     a.dW = dW; a.dw_stride = dw_stride; a.db = db; a.db_stride = db_stride;
-    RTMA_TRY(prepare_row_call(ctx, sizeof(float) * a.tiles * (weights + BIAS_ROWS * (int64_t)d_out), stream));
+    a.ldo = ceil_div(d_out, 8) * 8;
+    a.go = 32;
+    const int64_t slot_rows = a.tiles * (d_in + a.bias_rows);
+    RTMA_TRY(prepare_row_call(ctx, sizeof(float) * slot_rows * a.ldo, stream));
     a.out = ctx->arena;
-    a.vo = d_out % 4 == 0 && a.tiles * (d_in + BIAS_ROWS) < (int64_t(1) << 31) &&
-           make_store_map(&a.map_o, RTMA_F32, a.out, a.tiles * (d_in + BIAS_ROWS), d_out, d_out, dtype == RTMA_F32 ? 32 : 64);
+    a.vo = dtype != RTMA_F32 && slot_rows < (int64_t(1) << 31) && make_store_map(&a.map_o, RTMA_F32, a.out, slot_rows, a.ldo, a.ldo, 64);
     if (n > 0) RTMA_TRY(launch_linear<WEIGHT_GRADIENT>(ctx, dtype, a, KC_GEMM_WGRAD, stream));
     {
         KernelScope ks(ctx, KC_REDUCE_SGD, stream);

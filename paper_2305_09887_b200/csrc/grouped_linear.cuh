@@ -1,0 +1,223 @@
+// What the kernels of the grouped products share: their arguments, a block's walk over its tiles, and the way of the results out.
+#pragma once
+
+#include <type_traits>
+
+#include "rows.cuh"
+#include "tc_common.cuh"
+
+namespace grouped {
+
+enum Mode { FORWARD, INPUT_GRADIENT, WEIGHT_GRADIENT };
+constexpr int MAX_STAGES = 6;
+constexpr int SMEM_MOST = 232448;  // bytes a block can have
+
+struct LinearArgs {
+    const int64_t* offsets;
+    int64_t n;
+    int G, span;
+    int64_t tile_rows, tiles;  // rows of a row tile (forward, dx: 128; dw: of a chunk), row tiles at most
+    int m_tiles, n_tiles;      // tiles of one row tile: m_tiles (dw) x n_tiles
+    int BN;
+    int d_in, d_out;
+    const void *A, *B;         // rows; matrices (forward, dx) or rows (dw)
+    int64_t lda, ldb, w_stride;
+    int va, vb;                // granules of the rows (bytes)
+    int go;                    // granule of the result's rows
+    bool vo;                   // the result can leave by bulk-tensor stores: map_o holds
+    const void* bias;
+    int64_t bias_stride;
+    int bias_rows;             // dw: partial sums of the bias gradient in a slot, one row per warp that adds them up
+    void* out;                 // dw: the slots, [row tile][d_in + bias_rows][ldo]
+    int64_t ldo;
+    float *dW, *db;
+    int64_t dw_stride, db_stride;
+    int* error_word;
+    CUtensorMap map_a, map_b;  // operands that are fetched by bulk-tensor loads
+    CUtensorMap map_o;         // the result (dw: the slots, one below the other)
+};
+
+#ifdef __CUDACC__
+struct Shared {
+    uint64_t full[MAX_STAGES], empty[MAX_STAGES];
+    uint64_t acc_full[2], acc_empty[2];
+    uint32_t tmem_base;
+    int abort;
+    int32_t warp_sums[32];
+    int32_t tile_start[RTMA_MAX_GROUPS + 1], begin[RTMA_MAX_GROUPS], rows[RTMA_MAX_GROUPS];
+    alignas(16) float bias[8 * 128];  // of every drain warp's columns
+};
+
+__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, Shared& sh, int* error_word) {
+    for (uint32_t i = 0; i < tc::WAIT_POLLS; ++i) {
+        if (tc::mbar_try_wait(bar, parity)) return true;
+        if ((i & 1023u) == 1023u && *reinterpret_cast<volatile int*>(&sh.abort)) break;
+    }
+    *reinterpret_cast<volatile int*>(&sh.abort) = 1;
+    atomicExch(error_word, 1);
+    return false;
+}
+
+// A role's walk over a block's tiles and their stages.
+template <int MODE, int BM, int BK>
+struct Walk {
+    int tile, part, row_tile, m0, n0;  // part: set before `at`, to one that is not behind the tile's
+    int64_t row0;     // first row of the tile
+    int rows, k_end;  // rows of the tile; terms of the contraction
+    int k0;
+    __device__ __forceinline__ bool at(const LinearArgs& a, const Shared& sh) {
+        const int per = a.m_tiles * a.n_tiles;
+        int rest = 0;
+        row_tile = tile;
+        if (per > 1) {
+            row_tile = tile / per;
+            rest = tile - row_tile * per;
+        }
+        if (row_tile >= sh.tile_start[a.G]) return false;
+        m0 = 0;
+        if (MODE == WEIGHT_GRADIENT && a.m_tiles > 1) {
+            m0 = rest / a.n_tiles;
+            rest -= m0 * a.n_tiles;
+            m0 *= BM;
+        }
+        n0 = rest * a.BN;
+        while (row_tile >= sh.tile_start[part + 1]) ++part;  // tiles come in ascending order
+        const int64_t inside = (int64_t)(row_tile - sh.tile_start[part]) * a.tile_rows;
+        row0 = sh.begin[part] + inside;
+        rows = (int)min((int64_t)sh.rows[part] - inside, a.tile_rows);
+        k_end = MODE == FORWARD ? a.d_in : MODE == INPUT_GRADIENT ? a.d_out : rows;
+        k0 = 0;
+        return true;
+    }
+    __device__ __forceinline__ bool first(const LinearArgs& a, const Shared& sh) {
+        tile = blockIdx.x;
+        part = 0;
+        return at(a, sh);
+    }
+    __device__ __forceinline__ bool last_stage() const { return k0 + BK >= k_end; }
+    __device__ __forceinline__ bool next(const LinearArgs& a, const Shared& sh) {  // the next stage
+        if (!last_stage()) {
+            k0 += BK;
+            return true;
+        }
+        tile += gridDim.x;
+        return at(a, sh);
+    }
+    __device__ __forceinline__ bool next_tile(const LinearArgs& a, const Shared& sh) {
+        tile += gridDim.x;
+        return at(a, sh);
+    }
+};
+
+__device__ __forceinline__ void store_16(uint32_t dst, uint4 v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ uint4 load_16(uint32_t src) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(src) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ void add_eight(float (&sums)[8], const float (&v)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sums[j] += v[j];
+}
+
+// A drain warp's results on their way out: ROW bytes of each of its 32 rows (a row per lane) at a time go through one of its slabs,
+// in the map's swizzle of ROW bytes, so that they leave as one bulk-tensor store; boxes that would reach rows or columns that are
+// not this tile's, and rows off the 16-byte boundaries, are written by the lanes.
+template <class O, int SLABS, int ROW>
+struct Outlet {
+    uint32_t slabs;
+    int at = 0;
+    __device__ __forceinline__ static int swizzle(int row) { return ROW == 64 ? (row >> 1) & 3 : (row >> 2) & 1; }
+    // row0, c: place in the map; rows, cols: how much is this tile's; whole: all columns of the matrix from c on are, and end on a
+    // 16-byte boundary (a store's box is cut off at the edge of the matrix only in steps of 16 bytes)
+    __device__ __forceinline__ void put(const LinearArgs& a, const float (&v)[32], int64_t row0, int c, int rows, int cols, bool whole, O* out, int64_t ldo, int lane) {
+        constexpr int WIDE = ROW / sizeof(O), PIECE = 16 / sizeof(O);
+#pragma unroll
+        for (int c0 = 0; c0 < 32; c0 += WIDE) {
+            if (c0 >= cols) break;
+            const uint32_t slab = slabs + at * 32 * ROW;
+            if (lane == 0) tc::tma_store_wait_read_but<SLABS - 1>();  // the slab's last store has read it
+            __syncwarp();
+#pragma unroll
+            for (int q = 0; q < ROW / 16; ++q) {
+                const int e = c0 + q * PIECE;
+                uint4 x;
+                if constexpr (sizeof(O) == 4) {
+                    x = make_uint4(__float_as_uint(v[e]), __float_as_uint(v[e + 1]), __float_as_uint(v[e + 2]), __float_as_uint(v[e + 3]));
+                } else {
+                    const O* tag = nullptr;
+                    x = make_uint4(narrow2(v[e], v[e + 1], tag), narrow2(v[e + 2], v[e + 3], tag), narrow2(v[e + 4], v[e + 5], tag), narrow2(v[e + 6], v[e + 7], tag));
+                }
+                store_16(slab + lane * ROW + ((q ^ swizzle(lane)) << 4), x);
+            }
+            const bool bulk = a.vo && rows == 32 && (cols - c0 >= WIDE || whole);
+            if (bulk) tc::fence_proxy_async_smem();
+            __syncwarp();
+            if (bulk) {
+                if (lane == 0) {
+                    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
+                                 ::"l"(reinterpret_cast<uint64_t>(&a.map_o)), "r"(slab), "r"(c + c0), "r"((int32_t)row0)
+                                 : "memory");
+                }
+            } else {
+                const int x = lane % WIDE;
+                for (int r = lane / WIDE; r < rows; r += 32 / WIDE) {
+                    const uint32_t from = slab + r * ROW + (((x / PIECE) ^ swizzle(r)) << 4) + (x % PIECE) * (int)sizeof(O);
+                    O y;
+                    if constexpr (sizeof(O) == 4) {
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(y) : "r"(from) : "memory");
+                    } else {
+                        unsigned short bits;
+                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(bits) : "r"(from) : "memory");
+                        y = *reinterpret_cast<O*>(&bits);
+                    }
+                    if (c0 + x < cols) out[r * ldo + c0 + x] = y;
+                }
+            }
+            if (lane == 0) tc::tma_store_commit();  // a group for every slab, empty or not
+            at = at + 1 == SLABS ? 0 : at + 1;
+        }
+    }
+    __device__ __forceinline__ void finish(int lane) const {
+        if (lane == 0) tc::tma_store_wait_all();
+    }
+};
+
+// The bias of a warp's columns (chunks c, c + step, ... of 32), in shared memory.
+template <class T>
+struct BiasHolder {
+    float* at;  // 16-byte boundary
+    __device__ __forceinline__ void fetch(const LinearArgs& a, int part, int n0, int c, int step, int chunks, int lane) const {
+        const T* bias = static_cast<const T*>(a.bias) + part * a.bias_stride + n0;
+        __syncwarp();
+        for (int chunk = c, i = 0; chunk < chunks; chunk += step, ++i) {
+            const int col = 32 * chunk + lane;
+            at[32 * i + lane] = col < a.BN && n0 + col < a.d_out ? to_f32(bias[col]) : 0.f;
+        }
+        __syncwarp();
+    }
+    __device__ __forceinline__ void add(float (&v)[32], int i) const {
+        const float4* b = reinterpret_cast<const float4*>(at + 32 * i);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float4 x = b[j];
+            v[4 * j] += x.x;
+            v[4 * j + 1] += x.y;
+            v[4 * j + 2] += x.z;
+            v[4 * j + 3] += x.w;
+        }
+    }
+};
+
+#endif
+
+}  // namespace grouped
+
+// Products of fp32 rows (grouped_split.cu): rows of a dw tile and the partial bias sums it leaves, the scratch that the matrices'
+// planes take in forward and dx, and the launch.
+constexpr int SPLIT_DW_ROWS = 256, SPLIT_BIAS_ROWS = 16;
+size_t split_planes_bytes(const grouped::LinearArgs& a);
+int32_t launch_split(rtma_ctx* ctx, int mode, grouped::LinearArgs& a, void* planes, int cls, cudaStream_t stream);

@@ -275,7 +275,7 @@ bool make_tensor_map_bf16(CUtensorMap* out, const void* base, uint64_t rows, uin
 // For results: a row-major matrix whose rows leave in boxes of row_bytes (32 or 64) x 32 rows, swizzled over row_bytes.  type:
 // RTMA_F32, _BF16, _F16.
 bool make_store_map(CUtensorMap* out, int type, const void* base, uint64_t rows, uint64_t cols, uint64_t ld, int row_bytes);
-// `count` row-major matrices [rows x cols] of 16-bit values, ld elements between rows and `stride` between matrices; boxes of 64
-// columns x box_rows (up to 256) of one matrix, 128-byte swizzle, zeros outside a matrix.
+// `count` row-major matrices [rows x cols] of 16-bit values, ld elements between rows and `stride` between matrices; boxes of
+// box_cols (64: 128-byte swizzle, 32: 64-byte swizzle) x box_rows (up to 256) of box_matrices, zeros outside a matrix.
 bool make_tensor_map_16bit(CUtensorMap* out, bool bf16, const void* base, uint64_t count, uint64_t rows, uint64_t cols, uint64_t ld, uint64_t stride,
-                           uint32_t box_rows);
+                           uint32_t box_rows, uint32_t box_cols = 64, uint32_t box_matrices = 1);
