@@ -450,27 +450,33 @@ __global__ void __launch_bounds__(Form<T, MODE, LOADING>::THREADS, 1) linear_ker
 }
 
 // The slots of every part added up in order.
+// A block takes 32 neighbouring values, its warps every eighth slot each (of a bias, of the slots' rows of partial sums).
 constexpr int REDUCE_THREADS = 256;
 __global__ void __launch_bounds__(REDUCE_THREADS) linear_reduce_kernel(const __grid_constant__ LinearArgs a) {
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
+    __shared__ float red[8][32];
     wait_for_kernel_before();
     number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums, a.span);
-    const int part = blockIdx.y;
-    const int64_t weights = (int64_t)a.d_in * a.d_out, slot = (a.d_in + a.bias_rows) * a.ldo, i = (int64_t)blockIdx.x * REDUCE_THREADS + threadIdx.x;
-    if (i >= weights + a.d_out) return;
+    const int part = blockIdx.y, lane = threadIdx.x & 31, share = threadIdx.x >> 5;
+    const int64_t weights = (int64_t)a.d_in * a.d_out, slot = (a.d_in + a.bias_rows) * a.ldo, i = (int64_t)blockIdx.x * 32 + lane;
     const int64_t row = i / a.d_out, from = row * a.ldo + (i - row * a.d_out);
-    const float* p = static_cast<const float*>(a.out);
-    const int t1 = tile_start[part + 1];
+    const int t0 = tile_start[part], t1 = tile_start[part + 1];
+    const float* p = static_cast<const float*>(a.out) + t0 * slot + from;
     float s = 0.f;
     if (i < weights) {
-#pragma unroll 8
-        for (int t = tile_start[part]; t < t1; ++t) s += p[(int64_t)t * slot + from];
-        a.dW[part * a.dw_stride + i] = s;
-    } else if (a.db) {
-        for (int t = tile_start[part]; t < t1; ++t)
-            for (int k = 0; k < a.bias_rows; ++k) s += p[(int64_t)t * slot + from + k * a.ldo];
-        a.db[part * a.db_stride + i - weights] = s;
+#pragma unroll 4
+        for (int t = share; t < t1 - t0; t += 8) s += p[t * slot];
+    } else if (i < weights + a.d_out) {
+#pragma unroll 4
+        for (int j = share; j < (t1 - t0) * a.bias_rows; j += 8) s += p[j / a.bias_rows * slot + j % a.bias_rows * a.ldo];
     }
+    red[share][lane] = s;
+    __syncthreads();
+    if (share || i >= weights + a.d_out) return;
+#pragma unroll
+    for (int k = 1; k < 8; ++k) s += red[k][lane];
+    if (i < weights) a.dW[part * a.dw_stride + i] = s;
+    else if (a.db) a.db[part * a.db_stride + i - weights] = s;
 }
 
 // Columns in equal tiles of a multiple of 16.
@@ -547,7 +553,7 @@ int32_t run_rows(rtma_ctx* ctx, const char* who, bool transposed, int32_t dtype,
     a.tile_rows = BM;
     a.tiles = n / BM + G;
     a.m_tiles = 1;
-    cut_columns(a, N, 256);
+    cut_columns(a, N, dtype == RTMA_F32 ? SPLIT_COLUMNS : 256);
     a.d_in = d_in; a.d_out = d_out;
     a.A = A; a.lda = lda; a.B = W; a.w_stride = w_stride; a.bias = b; a.bias_stride = b_stride;
     a.va = row_granule(A, lda, es);
@@ -592,9 +598,9 @@ extern "C" int32_t rtma_grouped_linear_dw(rtma_ctx* ctx, int32_t dtype, int64_t 
     a.offsets = offsets; a.n = n;
     a.G = shared ? 1 : G;
     a.span = shared ? G : 1;
-    a.m_tiles = (int)ceil_div(d_in, dtype == RTMA_F32 ? SPLIT_DW_ROWS : BM);
+    a.m_tiles = (int)ceil_div(d_in, BM);
     a.bias_rows = dtype == RTMA_F32 ? SPLIT_BIAS_ROWS : BIAS_ROWS;
-    cut_columns(a, d_out, 128);
+    cut_columns(a, d_out, dtype == RTMA_F32 ? SPLIT_DW_COLUMNS : 128);
     // about four tiles per SM over the whole call; chunks of whole stages
     const int64_t chunk = ceil_div(n * a.m_tiles * a.n_tiles, 4 * (int64_t)ctx->sm_count);
     a.tile_rows = chunk < 256 ? 256 : ceil_div(chunk, BK) * BK;
@@ -614,7 +620,7 @@ extern "C" int32_t rtma_grouped_linear_dw(rtma_ctx* ctx, int32_t dtype, int64_t 
     if (n > 0) RTMA_TRY(launch_linear<WEIGHT_GRADIENT>(ctx, dtype, a, KC_GEMM_WGRAD, stream));
     {
         KernelScope ks(ctx, KC_REDUCE_SGD, stream);
-        launch_kernel(linear_reduce_kernel, dim3((unsigned)ceil_div(weights + d_out, REDUCE_THREADS), (unsigned)a.G), REDUCE_THREADS, 0, stream, a);
+        launch_kernel(linear_reduce_kernel, dim3((unsigned)ceil_div(weights + d_out, 32), (unsigned)a.G), REDUCE_THREADS, 0, stream, a);
     }
     RTMA_LAUNCH_CHECK(ctx);
     return RTMA_OK;

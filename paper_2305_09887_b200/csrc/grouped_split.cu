@@ -4,13 +4,13 @@
 // below 2^-22 of it.  The tensor cores truncate when they accumulate: a stage of 32 terms starts a fresh accumulator, the five small
 // products first, and is then added up in registers, rounded to nearest.
 //
-// Splitting costs as many instructions as a block can issue beside the MMAs, so every split value should meet as many others as the
-// accumulators have room for: a tile is 128 rows x 256 columns in forward and dx, where the matrices are split beforehand, once a
-// call, into planes in the scratch and come by bulk-tensor loads; 256 x 128 in dw, where both operands are rows.
-//
-// 16 warps do everything in turn: split the next stage's values (which wait in registers) into shared memory, request the ones
-// after, take their 64 columns of the stage before from tensor memory.  When those are there, that stage's place in the ring and
-// its accumulator are free again; warp 0 issues the MMAs, warp 1 the loads of W.
+// The matrices are split beforehand, once a call, into planes in the scratch, and come by bulk-tensor loads in forward and dx; in dw
+// both operands are rows.  The rows' values are split by the warps, which do everything in turn: split the next stage's values
+// (which wait in registers) into shared memory, request the ones after, take their columns of the stage before from tensor memory
+// and add them up.  When those are there, that stage's place in the ring and its accumulator are free again; warp 0 issues the MMAs,
+// warp 1 the loads of W.  All these steps are short and wait for one another, so two blocks share an SM, each on tiles of 128 x 128
+// (dw: 128 x 64): one block of twice the width on the SM, which splits less, took 127 us for 200,000 x 128 -> 256 and 220 for the
+// 256 x 47 gradient of as many rows.
 #include "grouped_linear.cuh"
 
 RTMA_BOUNDS_TU()
@@ -19,17 +19,17 @@ namespace {
 
 using namespace grouped;
 
-constexpr int BK = 32, WARPS = 16, THREADS = 32 * WARPS;
-constexpr int A_STAGES = 2, W_STAGES = 3;
-constexpr int OUT_ROW = 32, OUT_BYTES = 32 * OUT_ROW;   // a warp's 32 rows of 8 values on their way out
+constexpr int BM = 128, BK = 32, WARPS = 8, THREADS = 32 * WARPS, BLOCKS_PER_SM = 2;
+constexpr int A_STAGES = 2, W_STAGES = 2;
 
 template <int MODE>
 struct Form {
     static constexpr bool W_BULK = MODE != WEIGHT_GRADIENT;           // the right operand is W and comes as planes
-    static constexpr int BM = W_BULK ? 128 : SPLIT_DW_ROWS, BN = W_BULK ? 256 : 128;
+    static constexpr int BN = W_BULK ? 128 : SPLIT_DW_COLUMNS;
+    static constexpr int COLUMNS = BN / 2, HALVES = COLUMNS / 32;      // of the accumulator that a warp drains, 32 at a time
     static constexpr int A_PLANE = BM * BK * 2, B_PLANE = BN * BK * 2;
     static constexpr int RING_BYTES = A_STAGES * 3 * A_PLANE + (W_BULK ? W_STAGES : A_STAGES) * 3 * B_PLANE;
-    static constexpr int DYNAMIC_BYTES = RING_BYTES + 1024 + WARPS * OUT_BYTES;
+    static constexpr int DYNAMIC_BYTES = RING_BYTES + 1024;
 };
 
 // Eight fp32 values as three bf16 numbers each, x = h + m + l exactly (but for bits below the smallest bf16 number).  h is cut off
@@ -71,16 +71,16 @@ __global__ void __launch_bounds__(256) split_planes_kernel(const float* __restri
 }
 
 // One operand's values of a thread: PIECES units of eight, where they come from and where in a plane they go.
-//   ALONG (K-major, 64-byte rows of 32 terms, 64-byte swizzle): thread t holds unit t % 4 of row t / 4
+//   ALONG (K-major, 64-byte rows of 32 terms, 64-byte swizzle): unit t % 4 of rows t / 4 + (THREADS / 4) i
 //   across (MN-major, atoms of 64 columns x 32 terms, 128-byte swizzle): unit t % U of terms t / U + (THREADS / U) i, U = columns / 8
 template <bool ALONG, int COLUMNS>
 struct Place {
-    static constexpr int U = ALONG ? 4 : COLUMNS / 8, STEP = THREADS / U, PIECES = ALONG ? 1 : BK / STEP;
+    static constexpr int U = ALONG ? 4 : COLUMNS / 8, STEP = THREADS / U, PIECES = (ALONG ? BM : BK) / STEP;
     int row, unit;
     __device__ __forceinline__ explicit Place(int t) : row(t / U), unit(t % U) {}
     __device__ __forceinline__ uint32_t in_plane(int i) const {
-        if constexpr (ALONG) return row * 64 + ((unit ^ ((row >> 1) & 3)) << 4);
         const int r = row + STEP * i;
+        if constexpr (ALONG) return r * 64 + ((unit ^ ((r >> 1) & 3)) << 4);
         return (unit >> 3) * 4096 + r * 128 + (((unit & 7) ^ (r & 7)) << 4);
     }
 };
@@ -89,10 +89,10 @@ struct Place {
 template <int MODE, bool IS_B>
 struct Rows {
     static constexpr bool ALONG = MODE != WEIGHT_GRADIENT;
-    typedef Place<ALONG, IS_B ? Form<MODE>::BN : Form<MODE>::BM> P;
+    typedef Place<ALONG, IS_B ? Form<MODE>::BN : BM> P;
     const float* p;  // this thread's first value of the tile
-    int near, cols;  // along: rows from this one on (one is enough), terms;  across: terms from this thread's first on, columns
-    __device__ __forceinline__ void open(const LinearArgs& a, const Walk<MODE, Form<MODE>::BM, BK>& w, const P& at) {
+    int near, cols;  // along: rows from this thread's first on, terms;  across: terms from this thread's first on, columns
+    __device__ __forceinline__ void open(const LinearArgs& a, const Walk<MODE, BM, BK>& w, const P& at) {
         const float* base = static_cast<const float*>(IS_B ? a.B : a.A);
         const int64_t ld = IS_B ? a.ldb : a.lda;
         p = base + (w.row0 + at.row) * ld + 8 * at.unit;
@@ -111,18 +111,24 @@ struct Rows {
         const float* from;
         int valid;
         if constexpr (ALONG) {
-            from = p + k0;
-            valid = near > 0 ? cols - k0 : 0;
+            from = p + P::STEP * i * (IS_B ? a.ldb : a.lda) + k0;
+            valid = P::STEP * i < near ? cols - k0 : 0;
         } else {
             const int k = k0 + P::STEP * i;
             from = p + k * (IS_B ? a.ldb : a.lda);
             valid = k < near ? cols : 0;
         }
         if constexpr (EASY) {  // 16-byte boundaries, widths of whole 16 bytes
-            const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-            to.w[0] = to.w[1] = zero;
-            if (valid > 0) to.w[0] = *reinterpret_cast<const uint4*>(from);
-            if (valid > 4) to.w[1] = *reinterpret_cast<const uint4*>(from + 4);
+            uint32_t* q = reinterpret_cast<uint32_t*>(to.w);
+            if (valid >= 8 && (IS_B ? a.vb : a.va) == 32) {
+                asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                             : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3]), "=r"(q[4]), "=r"(q[5]), "=r"(q[6]), "=r"(q[7])
+                             : "l"(from));
+            } else {
+                to.w[0] = to.w[1] = make_uint4(0u, 0u, 0u, 0u);
+                if (valid > 0) to.w[0] = *reinterpret_cast<const uint4*>(from);
+                if (valid > 4) to.w[1] = *reinterpret_cast<const uint4*>(from + 4);
+            }
         } else {
             to.load(from, max(0, min(8, valid)), IS_B ? a.vb : a.va);
         }
@@ -132,14 +138,14 @@ struct Rows {
 template <int MODE>
 struct SplitShared : Shared {
     uint64_t w_full[W_STAGES];
-    Walk<MODE, Form<MODE>::BM, BK> ahead;  // the stage of W that is fetched next, and its place: one thread's
+    Walk<MODE, BM, BK> ahead;  // the stage of W that is fetched next, and its place: one thread's
     int ahead_slot;
     bool ahead_left;
 };
 
 // The stage's matrix by one thread, into its place in the ring.
 template <int MODE>
-__device__ __forceinline__ void load_w(const LinearArgs& a, SplitShared<MODE>& sh, uint8_t* to, int slot, const Walk<MODE, Form<MODE>::BM, BK>& w) {
+__device__ __forceinline__ void load_w(const LinearArgs& a, SplitShared<MODE>& sh, uint8_t* to, int slot, const Walk<MODE, BM, BK>& w) {
     uint64_t* bar = &sh.w_full[slot];
     uint8_t* dst = to + slot * 3 * Form<MODE>::B_PLANE;
     const int z = a.w_stride ? 3 * w.part : 0;
@@ -162,77 +168,56 @@ __device__ __forceinline__ void multiply(const LinearArgs& a, uint32_t d, uint32
     typedef Form<MODE> F;
     constexpr bool A_ACROSS = MODE == WEIGHT_GRADIENT, B_ACROSS = MODE != INPUT_GRADIENT;
     const uint32_t idesc = tc::idesc_bf16(128, a.BN, A_ACROSS, B_ACROSS);
-    uint64_t da = (A_ACROSS ? describe(4096, 1024, false) : describe(16, 512, true)) + (sa >> 4);
-    uint64_t db = (MODE == INPUT_GRADIENT ? describe(16, 512, true) : describe(MODE == FORWARD ? 3 * 4096 : 4096, 1024, false)) + (sb >> 4);
+    const uint64_t da = (A_ACROSS ? describe(4096, 1024, false) : describe(16, 512, true)) + (sa >> 4);
+    const uint64_t db = (MODE == INPUT_GRADIENT ? describe(16, 512, true) : describe(MODE == FORWARD ? 3 * 4096 : 4096, 1024, false)) + (sb >> 4);
     constexpr uint32_t a_step = A_ACROSS ? 128 : 2, b_step = B_ACROSS ? 128 : 2;  // 16 terms further
     constexpr uint32_t ap = F::A_PLANE >> 4;
     const uint32_t bp = MODE == FORWARD ? 4096 >> 4 : MODE == INPUT_GRADIENT ? (uint32_t)a.BN * 4 : F::B_PLANE >> 4;
     const int steps = (terms + 15) >> 4;
+    uint32_t accumulate = 0u;
+#pragma unroll 1  // (the warps share the instruction cache)
+    for (int k = 0; k < steps; ++k) {
+        const uint64_t x = da + k * a_step, y = db + k * b_step;
+        tc::mma_bf16(d, x + 2 * ap, y, idesc, accumulate);
+        tc::mma_bf16(d, x, y + 2 * bp, idesc, 1u);
+        tc::mma_bf16(d, x + ap, y + bp, idesc, 1u);
+        tc::mma_bf16(d, x + ap, y, idesc, 1u);
+        tc::mma_bf16(d, x, y + bp, idesc, 1u);
+        accumulate = 1u;
+    }
+#pragma unroll 1
+    for (int k = 0; k < steps; ++k) tc::mma_bf16(d, da + k * a_step, db + k * b_step, idesc, 1u);
+}
+
+// 32 columns of a warp's rows (one per lane).  A lane writes its own row, as many bytes at a time as lie on a boundary: nothing is
+// waited for, where bulk stores through the little shared memory there is left held the warps up (248 -> 129 us for 200,000 x 128 ->
+// 256).
+__device__ __forceinline__ void put_rows(float* out, int64_t ldo, int granule, const float (&v)[32], int rows, int cols, int lane) {
+    if (lane >= rows) return;
+    out += lane * ldo;
+    if (granule == 32 && cols % 8 == 0) {
 #pragma unroll
-    for (int m = 0; m < F::BM / 128; ++m) {
-        uint32_t accumulate = 0u;
-        for (int k = 0; k < steps; ++k) {
-            const uint64_t x = da + k * a_step, y = db + k * b_step;
-            tc::mma_bf16(d, x + 2 * ap, y, idesc, accumulate);
-            tc::mma_bf16(d, x, y + 2 * bp, idesc, 1u);
-            tc::mma_bf16(d, x + ap, y + bp, idesc, 1u);
-            tc::mma_bf16(d, x + ap, y, idesc, 1u);
-            tc::mma_bf16(d, x, y + bp, idesc, 1u);
-            accumulate = 1u;
+        for (int q = 0; q < 4; ++q) {
+            if (8 * q < cols)
+                asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + 8 * q), "f"(v[8 * q]), "f"(v[8 * q + 1]), "f"(v[8 * q + 2]),
+                             "f"(v[8 * q + 3]), "f"(v[8 * q + 4]), "f"(v[8 * q + 5]), "f"(v[8 * q + 6]), "f"(v[8 * q + 7])
+                             : "memory");
         }
-        for (int k = 0; k < steps; ++k) tc::mma_bf16(d, da + k * a_step, db + k * b_step, idesc, 1u);
-        d += 128;                   // the next 128 rows (dw): their columns of the accumulator,
-        da += 2 * 4096 >> 4;        // their two atoms
+    } else if (granule >= 16 && cols % 4 == 0) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (4 * q < cols) *reinterpret_cast<float4*>(out + 4 * q) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (j < cols) out[j] = v[j];
     }
 }
 
-// 32 columns of a warp's rows (one per lane).  A lane writes its own row, 32 or 16 bytes at a time: nothing is waited for, where
-// bulk stores through the little shared memory there is left held the warps up (248 -> 118 us for 200,000 x 128 -> 256).  Rows off
-// the 16-byte boundaries go through shared memory, so that neighbouring lanes write neighbouring values.
-__device__ __forceinline__ void put_rows(float* out, int64_t ldo, int granule, const float (&v)[32], uint32_t slab, int rows, int cols, int lane) {
-    if (granule >= 16 && cols % 4 == 0) {
-        float* mine = out + lane * ldo;
-        if (lane < rows) {
-            if (granule == 32 && cols % 8 == 0) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    if (8 * q < cols)
-                        asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(mine + 8 * q), "f"(v[8 * q]), "f"(v[8 * q + 1]), "f"(v[8 * q + 2]),
-                                     "f"(v[8 * q + 3]), "f"(v[8 * q + 4]), "f"(v[8 * q + 5]), "f"(v[8 * q + 6]), "f"(v[8 * q + 7])
-                                     : "memory");
-                }
-            } else {
-#pragma unroll
-                for (int q = 0; q < 8; ++q)
-                    if (4 * q < cols) *reinterpret_cast<float4*>(mine + 4 * q) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
-            }
-        }
-        return;
-    }
-#pragma unroll
-    for (int c0 = 0; c0 < 32; c0 += 8) {
-        if (c0 < cols) {
-            __syncwarp();
-#pragma unroll
-            for (int q = 0; q < 2; ++q)
-                store_16(slab + lane * 32 + ((q ^ ((lane >> 2) & 1)) << 4),
-                         make_uint4(__float_as_uint(v[c0 + 4 * q]), __float_as_uint(v[c0 + 4 * q + 1]), __float_as_uint(v[c0 + 4 * q + 2]), __float_as_uint(v[c0 + 4 * q + 3])));
-            __syncwarp();
-            const int x = lane & 7;
-#pragma unroll 2
-            for (int r = lane >> 3; r < rows; r += 4) {
-                float y;
-                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(y) : "r"(slab + r * 32 + (((x >> 2) ^ ((r >> 2) & 1)) << 4) + (x & 3) * 4) : "memory");
-                if (c0 + x < cols) out[r * ldo + c0 + x] = y;
-            }
-        }
-    }
-}
-
-template <int MODE, bool EASY>
-__device__ __forceinline__ void work(const LinearArgs& a, SplitShared<MODE>& sh, uint8_t* ring_bytes, uint32_t slabs) {
+template <int MODE, int EASY>
+__device__ __forceinline__ void work(const LinearArgs& a, SplitShared<MODE>& sh, uint8_t* ring_bytes) {
     typedef Form<MODE> F;
-    typedef Walk<MODE, F::BM, BK> W;
+    typedef Walk<MODE, BM, BK> W;
     constexpr bool DW = MODE == WEIGHT_GRADIENT;
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5, quarter = warp & 3, group = warp >> 2;
     const uint32_t ring = tc::smem_u32(ring_bytes);
@@ -245,15 +230,15 @@ __device__ __forceinline__ void work(const LinearArgs& a, SplitShared<MODE>& sh,
     Rows<MODE, true> rows_b;
     Eight<float> held_a[Rows<MODE, false>::P::PIECES], held_b[1];
     static_assert(!DW || Rows<MODE, true>::P::PIECES == 1, "one piece of dY a thread");
-    // this warp's 64 columns of the accumulator, and where they go in the result
-    const uint32_t tmem = sh.tmem_base + ((uint32_t)(32 * quarter) << 16) + 64 * group;
-    const int out_m = (DW ? 128 * (group >> 1) : 0) + 32 * quarter, out_c = 64 * (DW ? group & 1 : group);
+    // this warp's rows and columns of the accumulator
+    const int out_m = 32 * quarter, out_c = F::COLUMNS * group;
+    const uint32_t tmem = sh.tmem_base + ((uint32_t)out_m << 16) + out_c;
     const bool drains = out_c < a.BN;
     BiasHolder<float> bias{sh.bias + 64 * warp};
-    float total[2][32], sums[8];
+    float total[F::HALVES][32], sums[8];
     auto clear_total = [&]() {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < F::HALVES; ++h)
 #pragma unroll
             for (int j = 0; j < 32; ++j) total[h][j] = 0.f;
     };
@@ -272,8 +257,8 @@ __device__ __forceinline__ void work(const LinearArgs& a, SplitShared<MODE>& sh,
         if constexpr (DW) rows_b.open(a, w, place_b);
     }
 #pragma unroll
-    for (int i = 0; i < Rows<MODE, false>::P::PIECES; ++i) rows_a.template load<EASY>(a, 0, i, held_a[i]);
-    if constexpr (DW) rows_b.template load<EASY>(a, 0, 0, held_b[0]);
+    for (int i = 0; i < Rows<MODE, false>::P::PIECES; ++i) rows_a.template load<(EASY & 1) != 0>(a, 0, i, held_a[i]);
+    if constexpr (DW) rows_b.template load<(EASY & 2) != 0>(a, 0, 0, held_b[0]);
     if (F::W_BULK && t == 32) {
         bool some = sh.ahead.first(a, sh);
         for (int s = 0; s < W_STAGES && some; ++s) {
@@ -291,11 +276,11 @@ __device__ __forceinline__ void work(const LinearArgs& a, SplitShared<MODE>& sh,
         __syncwarp();
         tc::tc_fence_after_sync();
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < F::HALVES; ++h) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 float v[8];
-                tc::tmem_load_32x8(tmem + (before & 1) * 256 + 32 * h + 8 * q, v);
+                tc::tmem_load_32x8(tmem + (before & 1) * F::BN + 32 * h + 8 * q, v);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) total[h][8 * q + j] += v[j];
             }
@@ -315,15 +300,15 @@ __device__ __forceinline__ void work(const LinearArgs& a, SplitShared<MODE>& sh,
             out.at(a, sh);
             part = out.part;
             const int N = MODE == INPUT_GRADIENT ? a.d_in : MODE == FORWARD ? a.d_out : (int)a.ldo;  // (dw: the slots' rows are padded)
-            const int rows = min(32, (DW ? min(F::BM, a.d_in - out.m0) : out.rows) - out_m);
+            const int rows = min(32, (DW ? min(BM, a.d_in - out.m0) : out.rows) - out_m);
             const int64_t row0 = (DW ? (int64_t)out.row_tile * (a.d_in + a.bias_rows) + out.m0 : out.row0) + out_m;
-            if (MODE == FORWARD && a.bias) bias.fetch(a, out.part, out.n0, 2 * group, 1, min(2 * group + 2, (a.BN + 31) / 32), lane);
+            if (MODE == FORWARD && a.bias) bias.fetch(a, out.part, out.n0, F::HALVES * group, 1, min(F::HALVES * (group + 1), (a.BN + 31) / 32), lane);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < F::HALVES; ++h) {
                 const int c = out.n0 + out_c + 32 * h, cols = min(min(32, a.BN - out_c - 32 * h), N - c);
                 if (rows > 0 && cols > 0) {
                     if (MODE == FORWARD && a.bias) bias.add(total[h], h);
-                    put_rows(static_cast<float*>(a.out) + row0 * a.ldo + c, a.ldo, a.go, total[h], slabs + warp * OUT_BYTES, rows, cols, lane);
+                    put_rows(static_cast<float*>(a.out) + row0 * a.ldo + c, a.ldo, a.go, total[h], rows, cols, lane);
                 }
             }
         }
@@ -375,24 +360,24 @@ __device__ __forceinline__ void work(const LinearArgs& a, SplitShared<MODE>& sh,
         tc::fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(&sh.full[slot]);
-        if (more) {  // (before the fence they would be waited for there)
-#pragma unroll
-            for (int i = 0; i < Rows<MODE, false>::P::PIECES; ++i) rows_a.template load<EASY>(a, k0, i, held_a[i]);
-            if constexpr (DW) rows_b.template load<EASY>(a, k0, 0, held_b[0]);
-        }
         if (warp == 0) {
             const uint32_t round = stage / W_STAGES, w_slot = stage - round * W_STAGES;
             if (!wait_for(&sh.full[slot], stage >> 1 & 1, sh, a.error_word)) return;
             if (F::W_BULK && !wait_for(&sh.w_full[w_slot], round & 1, sh, a.error_word)) return;
             tc::tc_fence_after_sync();
             if (lane == 0) {
-                multiply<MODE>(a, sh.tmem_base + slot * 256, sa, b_ring + (F::W_BULK ? w_slot : slot) * B_STAGE, terms);
+                multiply<MODE>(a, sh.tmem_base + slot * F::BN, sa, b_ring + (F::W_BULK ? w_slot : slot) * B_STAGE, terms);
                 tc::mma_commit(&sh.acc_full[slot]);
             }
             __syncwarp();
         }
+        if (more) {  // (before the fence they would be waited for there)
+#pragma unroll
+            for (int i = 0; i < Rows<MODE, false>::P::PIECES; ++i) rows_a.template load<(EASY & 1) != 0>(a, k0, i, held_a[i]);
+            if constexpr (DW) rows_b.template load<(EASY & 2) != 0>(a, k0, 0, held_b[0]);
+        }
         if constexpr (DW) {
-            if (tile_ends) {  // two terms' threads a warp hold the same columns
+            if (tile_ends) {  // four terms' threads of a warp hold the same columns
                 W w;
                 w.tile = this_tile;
                 w.part = part;
@@ -400,9 +385,10 @@ __device__ __forceinline__ void work(const LinearArgs& a, SplitShared<MODE>& sh,
                 float* to = static_cast<float*>(a.out) + ((int64_t)w.row_tile * (a.d_in + a.bias_rows) + a.d_in + warp) * a.ldo;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float s = sums[j] + __shfl_xor_sync(0xffffffffu, sums[j], 16);
+                    float s = sums[j] + __shfl_xor_sync(0xffffffffu, sums[j], 8);
+                    s += __shfl_xor_sync(0xffffffffu, s, 16);
                     const int c = 8 * place_b.unit + j;
-                    if (w.m0 == 0 && lane < 16 && c < a.BN && w.n0 + c < a.d_out) to[w.n0 + c] = s;
+                    if (w.m0 == 0 && lane < 8 && c < a.BN && w.n0 + c < a.d_out) to[w.n0 + c] = s;
                     sums[j] = 0.f;
                 }
             }
@@ -413,10 +399,10 @@ __device__ __forceinline__ void work(const LinearArgs& a, SplitShared<MODE>& sh,
     drain();
 }
 
-template <int MODE, bool EASY>
-__global__ void __launch_bounds__(THREADS, 1) split_kernel(const __grid_constant__ LinearArgs a) {
+template <int MODE, int EASY>
+__global__ void __launch_bounds__(THREADS, BLOCKS_PER_SM) split_kernel(const __grid_constant__ LinearArgs a) {
     typedef Form<MODE> F;
-    static_assert(F::DYNAMIC_BYTES + sizeof(SplitShared<MODE>) <= SMEM_MOST, "shared memory of a block");
+    static_assert(BLOCKS_PER_SM * (F::DYNAMIC_BYTES + sizeof(SplitShared<MODE>) + 1024) <= SMEM_MOST + 1024, "shared memory of a block");
     extern __shared__ uint8_t raw[];
     __shared__ SplitShared<MODE> sh;
     uint8_t* ring = raw + ((1024u - (tc::smem_u32(raw) & 1023u)) & 1023u);
@@ -432,7 +418,7 @@ __global__ void __launch_bounds__(THREADS, 1) split_kernel(const __grid_constant
         if (F::W_BULK) tc::prefetch_tensormap(&a.map_b);
     }
     if (warp == 0) {
-        tc::tmem_alloc(&sh.tmem_base, 512);
+        tc::tmem_alloc(&sh.tmem_base, 2 * F::BN);
         tc::tmem_relinquish();
     }
     wait_for_kernel_before();
@@ -446,18 +432,18 @@ __global__ void __launch_bounds__(THREADS, 1) split_kernel(const __grid_constant
     tc::tc_fence_before_sync();
     __syncthreads();
     tc::tc_fence_after_sync();
-    work<MODE, EASY>(a, sh, ring, tc::smem_u32(ring) + F::RING_BYTES);
+    work<MODE, EASY>(a, sh, ring);
     __syncwarp();
     if (*reinterpret_cast<volatile int*>(&sh.abort)) __nanosleep(1000000);  // a wait ran out: copies and MMAs under way land before the block ends
     tc::tc_fence_before_sync();
     __syncthreads();
     if (warp == 0) {
         tc::tc_fence_after_sync();
-        tc::tmem_dealloc(sh.tmem_base, 512);
+        tc::tmem_dealloc(sh.tmem_base, 2 * F::BN);
     }
 }
 
-template <int MODE, bool EASY>
+template <int MODE, int EASY>
 int32_t launch_form(rtma_ctx* ctx, const LinearArgs& a, unsigned grid, bool& configured, cudaStream_t stream) {
     if (!configured) {
         RTMA_CUDA(ctx, cudaFuncSetAttribute(split_kernel<MODE, EASY>, cudaFuncAttributeMaxDynamicSharedMemorySize, Form<MODE>::DYNAMIC_BYTES));
@@ -482,11 +468,16 @@ int32_t launch_mode(rtma_ctx* ctx, LinearArgs& a, void* planes, int cls, cudaStr
         RTMA_LAUNCH_CHECK(ctx);
     }
     const int64_t tiles = a.tiles * a.m_tiles * a.n_tiles;
-    const unsigned grid = (unsigned)(tiles < ctx->sm_count ? tiles : ctx->sm_count);
-    const bool easy = a.va >= 16 && (MODE == FORWARD ? a.d_in % 4 == 0 : a.d_out % 4 == 0) && (MODE != WEIGHT_GRADIENT || (a.vb >= 16 && a.d_in % 4 == 0));
-    bool* configured = ctx->split_configured + 2 * MODE;
+    const int64_t places = (int64_t)BLOCKS_PER_SM * ctx->sm_count;
+    const unsigned grid = (unsigned)(tiles < places ? tiles : places);
+    // operands on 16-byte boundaries with widths of whole 16 bytes are loaded without a case for every value
+    const bool easy_a = a.va >= 16 && (MODE == INPUT_GRADIENT ? a.d_out : a.d_in) % 4 == 0, easy_b = a.vb >= 16 && a.d_out % 4 == 0;
+    bool* configured = ctx->split_configured + 4 * MODE;
     KernelScope ks(ctx, cls, stream);
-    return easy ? launch_form<MODE, true>(ctx, a, grid, configured[1], stream) : launch_form<MODE, false>(ctx, a, grid, configured[0], stream);
+    if constexpr (MODE == WEIGHT_GRADIENT) {
+        if (easy_b) return easy_a ? launch_form<MODE, 3>(ctx, a, grid, configured[3], stream) : launch_form<MODE, 2>(ctx, a, grid, configured[2], stream);
+    }
+    return easy_a ? launch_form<MODE, 1>(ctx, a, grid, configured[1], stream) : launch_form<MODE, 0>(ctx, a, grid, configured[0], stream);
 }
 
 }  // namespace
