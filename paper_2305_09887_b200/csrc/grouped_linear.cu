@@ -260,7 +260,7 @@ __device__ __forceinline__ void bulk_role(const LinearArgs& a, Shared& sh, uint8
     }
 }
 
-// A stage's MMAs, by one thread.
+// A stage's MMAs, by one warp.
 template <class T, int MODE, int LOADING>
 __device__ __forceinline__ void multiply_stage(const LinearArgs& a, uint32_t d, uint32_t stage, int terms, uint32_t accumulate) {
     typedef Form<T, MODE, LOADING> F;
@@ -270,12 +270,11 @@ __device__ __forceinline__ void multiply_stage(const LinearArgs& a, uint32_t d, 
     const uint64_t desc = tc::smem_desc_sw128(0, 2 * SLAB_BYTES, 1024);  // atoms of 64 columns lie two slabs apart
     constexpr uint32_t a_step = F::A_ACROSS ? 128 : 2, b_step = F::B_ACROSS ? 128 : 2;  // 16 terms further, in units of 16 bytes
     constexpr uint32_t a_plane = F::A_BYTES >> 4;
-    uint64_t da = desc + (stage >> 4), db = da + a_plane;
+    const uint64_t da = desc + (stage >> 4), db = da + a_plane;
     const int steps = (terms + 15) >> 4;
-    for (int k = 0; k < steps; ++k, da += a_step, db += b_step) {
-        tc::mma_bf16(d, da, db, idesc, accumulate);
-        accumulate = 1u;
-    }
+#pragma unroll
+    for (int k = 0; k < BK / 16; ++k)
+        if (k < steps) tc::mma_by_warp(d, da + k * a_step, db + k * b_step, idesc, k ? 1u : accumulate);
 }
 
 template <class T, int MODE, int LOADING>
@@ -289,11 +288,12 @@ __device__ __forceinline__ void multiply_role(const LinearArgs& a, Shared& sh, u
         }
         if (!wait_for(&sh.full[at.s], at.phase, sh, a.error_word)) return;
         tc::tc_fence_after_sync();
+        __syncwarp();
         multiply_stage<T, MODE, LOADING>(a, sh.tmem_base + acc.s * F::BN, ring + at.s * F::STAGE_BYTES, min(BK, w.k_end - w.k0), F::IN_REGISTERS || w.k0 == 0 ? 0u : 1u);
-        tc::mma_commit(&sh.empty[at.s]);
+        tc::commit_by_warp(&sh.empty[at.s]);
         at.advance(F::STAGES);
         if (F::IN_REGISTERS || w.last_stage()) {
-            tc::mma_commit(&sh.acc_full[acc.s]);
+            tc::commit_by_warp(&sh.acc_full[acc.s]);
             acc.advance(2);
         }
     }
@@ -435,7 +435,7 @@ __global__ void __launch_bounds__(Form<T, MODE, LOADING>::THREADS, 1) linear_ker
         }
     } else {
         if constexpr (LOADING == COPIES) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(MULTIPLY_REGISTERS));
-        if (warp == MULTIPLIER && lane == 0) multiply_role<T, MODE, LOADING>(a, sh, ring);
+        if (warp == MULTIPLIER) multiply_role<T, MODE, LOADING>(a, sh, ring);
         if constexpr (LOADING == BULK)
             if (warp == MULTIPLIER + 1) bulk_role<T, MODE>(a, sh, ring_bytes, lane);
     }

@@ -173,20 +173,22 @@ __device__ __forceinline__ void multiply(const LinearArgs& a, uint32_t d, uint32
     constexpr uint32_t a_step = A_ACROSS ? 128 : 2, b_step = B_ACROSS ? 128 : 2;  // 16 terms further
     constexpr uint32_t ap = F::A_PLANE >> 4;
     const uint32_t bp = MODE == FORWARD ? 4096 >> 4 : MODE == INPUT_GRADIENT ? (uint32_t)a.BN * 4 : F::B_PLANE >> 4;
-    const int steps = (terms + 15) >> 4;
-    uint32_t accumulate = 0u;
-#pragma unroll 1  // (the warps share the instruction cache)
-    for (int k = 0; k < steps; ++k) {
-        const uint64_t x = da + k * a_step, y = db + k * b_step;
-        tc::mma_bf16(d, x + 2 * ap, y, idesc, accumulate);
-        tc::mma_bf16(d, x, y + 2 * bp, idesc, 1u);
-        tc::mma_bf16(d, x + ap, y + bp, idesc, 1u);
-        tc::mma_bf16(d, x + ap, y, idesc, 1u);
-        tc::mma_bf16(d, x, y + bp, idesc, 1u);
-        accumulate = 1u;
+    const bool two = terms > 16;
+    tc::mma_by_warp(d, da + 2 * ap, db, idesc, 0u);
+    tc::mma_by_warp(d, da, db + 2 * bp, idesc, 1u);
+    tc::mma_by_warp(d, da + ap, db + bp, idesc, 1u);
+    tc::mma_by_warp(d, da + ap, db, idesc, 1u);
+    tc::mma_by_warp(d, da, db + bp, idesc, 1u);
+    if (two) {
+        const uint64_t x = da + a_step, y = db + b_step;
+        tc::mma_by_warp(d, x + 2 * ap, y, idesc, 1u);
+        tc::mma_by_warp(d, x, y + 2 * bp, idesc, 1u);
+        tc::mma_by_warp(d, x + ap, y + bp, idesc, 1u);
+        tc::mma_by_warp(d, x + ap, y, idesc, 1u);
+        tc::mma_by_warp(d, x, y + bp, idesc, 1u);
+        tc::mma_by_warp(d, x, y, idesc, 1u);
     }
-#pragma unroll 1
-    for (int k = 0; k < steps; ++k) tc::mma_bf16(d, da + k * a_step, db + k * b_step, idesc, 1u);
+    tc::mma_by_warp(d, da, db, idesc, 1u);
 }
 
 // 32 columns of a warp's rows (one per lane).  A lane writes its own row, as many bytes at a time as lie on a boundary: nothing is
@@ -365,11 +367,9 @@ __device__ __forceinline__ void work(const LinearArgs& a, SplitShared<MODE>& sh,
             if (!wait_for(&sh.full[slot], stage >> 1 & 1, sh, a.error_word)) return;
             if (F::W_BULK && !wait_for(&sh.w_full[w_slot], round & 1, sh, a.error_word)) return;
             tc::tc_fence_after_sync();
-            if (lane == 0) {
-                multiply<MODE>(a, sh.tmem_base + slot * F::BN, sa, b_ring + (F::W_BULK ? w_slot : slot) * B_STAGE, terms);
-                tc::mma_commit(&sh.acc_full[slot]);
-            }
             __syncwarp();
+            multiply<MODE>(a, sh.tmem_base + slot * F::BN, sa, b_ring + (F::W_BULK ? w_slot : slot) * B_STAGE, terms);
+            tc::commit_by_warp(&sh.acc_full[slot]);
         }
         if (more) {  // (before the fence they would be waited for there)
 #pragma unroll
