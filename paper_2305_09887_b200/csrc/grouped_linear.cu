@@ -7,8 +7,9 @@
 // operand, rows across it (W forward; X and dY in dw) an MN-major one: both come from memory as they lie, nothing is transposed.
 //
 // The tensor cores truncate when they accumulate, so a long sum drifts towards zero by half a step per addition.  The weight
-// gradient, whose result is fp32, therefore has its drain warps take the accumulator after every 64 rows and add it up in
-// registers, rounded to nearest.
+// gradient, whose result is fp32, therefore has its drain warps take the accumulator after every 128 rows and add it up in
+// registers, rounded to nearest.  The column sums of dY are a product as well, with a left operand of ones: added up by the drain
+// warps from shared memory they cost more than all else that these do (239 -> XX us for 1M x 128 x 256 in fp16).
 //
 // This file: 16-bit rows (fp32 ones are in grouped_split.cu).  Two ways of loading:
 //   COPIES  rows that do not all lie on 16-byte boundaries: 8 warps with asynchronous copies of 16, 8 or 4 bytes
@@ -31,12 +32,11 @@ constexpr int BM = 128, BK = 64;
 // that drain: 256 x 112 + 256 x 96 + 128 x 64 = 61,440 = 640 x 96.
 constexpr int DRAIN_REGISTERS = 112, MULTIPLY_REGISTERS = 64;
 constexpr int SLAB_BYTES = 32 * 128;       // 32 rows of 64 16-bit values
-constexpr int BIAS_ROWS = 8;               // partial sums of the bias gradient in a slot, one row per warp that adds them up
+constexpr int BIAS_ROWS = 1;               // of a slot: column sums of dY
 
 template <class T, int MODE, int LOADING>
 struct Form {
-    static constexpr bool IN_REGISTERS = MODE == WEIGHT_GRADIENT;  // accumulated there, 64 terms at a time
-    static constexpr int BN = IN_REGISTERS ? 128 : 256;                                // widest tile
+    static constexpr int BN = MODE == WEIGHT_GRADIENT ? 128 : 256;                                // widest tile
     static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128;
     static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
     // the results of a tile leave while the next is drained, which is worth more than another stage
@@ -46,9 +46,11 @@ struct Form {
     static constexpr int OUT_SLABS = MODE == WEIGHT_GRADIENT ? 2 : 4;                  // of a drain warp: 32 rows of OUT_ROW bytes on
     static constexpr int OUT_ROW = 64;                                                 // their way out
     static constexpr int OUT_BYTES = OUT_SLABS * 32 * OUT_ROW;
-    static constexpr int DYNAMIC_BYTES = RING_BYTES + 1024 + DRAIN_WARPS * OUT_BYTES;
+    static constexpr int ACC_STAGES = MODE == WEIGHT_GRADIENT ? 2 : 1 << 20;           // after so many the accumulator is drained (or at a tile's end)
+    static constexpr int ACC_COLUMNS = 256;                                            // dw: 128 of the product, 128 of the column sums
+    static constexpr int ONES_BYTES = MODE == WEIGHT_GRADIENT ? 1024 : 0;
+    static constexpr int DYNAMIC_BYTES = RING_BYTES + 1024 + DRAIN_WARPS * OUT_BYTES + ONES_BYTES;
     static constexpr bool A_ACROSS = MODE == WEIGHT_GRADIENT, B_ACROSS = MODE != INPUT_GRADIENT;  // MN-major
-    static constexpr bool DRAIN_SUMS = LOADING == BULK && MODE == WEIGHT_GRADIENT;     // the drain warps add up the columns of dY
     static constexpr int LOAD_WARPS = LOADING == COPIES ? 8 : 0;                       // that do nothing else
     static constexpr int THREADS = 32 * (DRAIN_WARPS + LOAD_WARPS + 4);
 };
@@ -100,69 +102,20 @@ __device__ __forceinline__ void copy_pieces(uint32_t dst, const void* src, int b
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-// Sums over a warp's rows of the columns of dY that its lanes hold, written to the warp's row of the slot.
-__device__ __forceinline__ void leave_bias(const LinearArgs& a, int row_tile, int n0, float (&sums)[2][8], int warp, int lane) {
-    float* to = static_cast<float*>(a.out) + ((int64_t)row_tile * (a.d_in + BIAS_ROWS) + a.d_in + warp) * a.ldo;
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float s = sums[t][j];
-            s += __shfl_xor_sync(0xffffffffu, s, 8);
-            s += __shfl_xor_sync(0xffffffffu, s, 16);
-            const int c = 64 * t + 8 * lane + j;
-            if (lane < 8 && c < a.BN && n0 + c < a.d_out) to[n0 + c] = s;
-            sums[t][j] = 0.f;
-        }
-}
-
-template <int N>
-__device__ __forceinline__ void clear(float (&v)[N][8]) {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
-}
-// Adds the pieces that a thread holds of a stage's dY (slabs two by two below one another) to its columns' sums.
-template <class T>
-__device__ __forceinline__ void add_columns(uint32_t from, int slabs, float (&sums)[2][8]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (i < slabs) {
-            Eight<T> e;
-            e.w[0] = load_16(from + i * SLAB_BYTES);
-            float v[8];
-            e.values(v);
-            add_eight(sums[i >> 1], v);
-        }
-    }
-}
-
 // 16-byte pieces of both operands straight into the stage (t: 0..255); it is handed over once this thread's copies have landed, LAG
 // stages later.
 template <class T, int MODE>
 __device__ __forceinline__ void copy_role(const LinearArgs& a, Shared& sh, uint32_t ring, int t) {
     typedef Form<T, MODE, COPIES> F;
     constexpr int LAG = F::STAGES - 2;
-    constexpr bool SUMS = MODE == WEIGHT_GRADIENT;
-    const int row = t >> 3, unit = t & 7, lane = t & 31, warp = t >> 5;
+    const int row = t >> 3, unit = t & 7, lane = t & 31;
     const uint32_t place = row * 128 + ((unit ^ (row & 7)) << 4);  // inside a slab (32-row slabs do not change row mod 8)
     const int b_slabs = F::B_ACROSS ? 2 * ((a.BN + 63) / 64) : (a.BN + 31) / 32;
-    float sums[SUMS ? 2 : 1][8];
-    if constexpr (SUMS) clear(sums);
     Walk<MODE, BM, BK> w;
     bool more = w.first(a, sh);
-    Walk<MODE, BM, BK> late = w;
     tc::RingAt at, late_at;
     int under_way = 0;
     auto hand_over = [&]() {
-        if constexpr (SUMS) {
-            if (late.m0 == 0 && a.db) {
-                add_columns<T>(ring + late_at.s * F::STAGE_BYTES + F::A_BYTES + place, b_slabs, sums);
-                if (late.last_stage()) leave_bias(a, late.row_tile, late.n0, sums, warp, lane);
-            }
-            late.next(a, sh);
-        }
         tc::fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(&sh.full[late_at.s]);
@@ -262,7 +215,7 @@ __device__ __forceinline__ void bulk_role(const LinearArgs& a, Shared& sh, uint8
 
 // A stage's MMAs, by one warp.
 template <class T, int MODE, int LOADING>
-__device__ __forceinline__ void multiply_stage(const LinearArgs& a, uint32_t d, uint32_t stage, int terms, uint32_t accumulate) {
+__device__ __forceinline__ void multiply_stage(const LinearArgs& a, uint32_t d, uint32_t stage, int terms, uint32_t accumulate, uint32_t ones) {
     typedef Form<T, MODE, LOADING> F;
     const uint32_t format = std::is_same<T, __half>::value ? 0u : 1u;  // fp16 or bf16 operands, fp32 sums
     const uint32_t idesc = (1u << 4) | (format << 7) | (format << 10) | ((F::A_ACROSS ? 1u : 0u) << 15) | ((F::B_ACROSS ? 1u : 0u) << 16) |
@@ -275,24 +228,31 @@ __device__ __forceinline__ void multiply_stage(const LinearArgs& a, uint32_t d, 
 #pragma unroll
     for (int k = 0; k < BK / 16; ++k)
         if (k < steps) tc::mma_by_warp(d, da + k * a_step, db + k * b_step, idesc, k ? 1u : accumulate);
+    if (MODE == WEIGHT_GRADIENT && ones) {  // 128 rows of ones, all from the same 1024 bytes
+        const uint64_t one = tc::smem_desc_sw128(ones, 0, 0);
+#pragma unroll
+        for (int k = 0; k < BK / 16; ++k)
+            if (k < steps) tc::mma_by_warp(d + 128, one, db + k * b_step, idesc, k ? 1u : accumulate);
+    }
 }
 
 template <class T, int MODE, int LOADING>
-__device__ __forceinline__ void multiply_role(const LinearArgs& a, Shared& sh, uint32_t ring) {
+__device__ __forceinline__ void multiply_role(const LinearArgs& a, Shared& sh, uint32_t ring, uint32_t ones) {
     typedef Form<T, MODE, LOADING> F;
     Walk<MODE, BM, BK> w;
     tc::RingAt at, acc;
+    int held = 0;  // stages in the accumulator
     for (bool more = w.first(a, sh); more; more = w.next(a, sh)) {
-        if (F::IN_REGISTERS || w.k0 == 0) {
-            if (!wait_for(&sh.acc_empty[acc.s], acc.phase ^ 1u, sh, a.error_word)) return;
-        }
+        if (held == 0 && !wait_for(&sh.acc_empty[acc.s], acc.phase ^ 1u, sh, a.error_word)) return;
         if (!wait_for(&sh.full[at.s], at.phase, sh, a.error_word)) return;
         tc::tc_fence_after_sync();
         __syncwarp();
-        multiply_stage<T, MODE, LOADING>(a, sh.tmem_base + acc.s * F::BN, ring + at.s * F::STAGE_BYTES, min(BK, w.k_end - w.k0), F::IN_REGISTERS || w.k0 == 0 ? 0u : 1u);
+        multiply_stage<T, MODE, LOADING>(a, sh.tmem_base + acc.s * F::ACC_COLUMNS, ring + at.s * F::STAGE_BYTES, min(BK, w.k_end - w.k0), held ? 1u : 0u,
+                                         a.db && w.m0 == 0 ? ones : 0u);
         tc::commit_by_warp(&sh.empty[at.s]);
         at.advance(F::STAGES);
-        if (F::IN_REGISTERS || w.last_stage()) {
+        if (++held == F::ACC_STAGES || w.last_stage()) {
+            held = 0;
             tc::commit_by_warp(&sh.acc_full[acc.s]);
             acc.advance(2);
         }
@@ -312,60 +272,60 @@ __device__ __forceinline__ void put_chunk(const LinearArgs& a, const Walk<MODE, 
 }
 
 template <class T, int MODE, int LOADING>
-__device__ __forceinline__ void drain_role(const LinearArgs& a, Shared& sh, uint32_t slabs, uint32_t ring) {
+__device__ __forceinline__ void drain_role(const LinearArgs& a, Shared& sh, uint32_t slabs) {
     typedef Form<T, MODE, LOADING> F;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, half = warp >> 2;
     typedef typename std::conditional<MODE == WEIGHT_GRADIENT, float, T>::type O;
     Outlet<O, F::OUT_SLABS, F::OUT_ROW> outlet{slabs + warp * F::OUT_BYTES};
     BiasHolder<T> bias{sh.bias + 128 * warp};
-    const uint32_t lanes = (uint32_t)(32 * quarter) << 16;
+    const uint32_t tmem = sh.tmem_base + ((uint32_t)(32 * quarter) << 16);
     const int chunks = (a.BN + 31) / 32;
     Walk<MODE, BM, BK> w;
-    tc::RingAt acc, at;
-    float sums[F::DRAIN_SUMS ? 2 : 1][8];
-    if constexpr (F::DRAIN_SUMS) clear(sums);
+    tc::RingAt acc;
     for (bool more = w.first(a, sh); more; more = w.next_tile(a, sh)) {
-        if constexpr (F::IN_REGISTERS) {
-            float total[2][32];
+        if constexpr (MODE == WEIGHT_GRADIENT) {
+            float total[2][32], sums[16];  // sums: of 16 columns, the same in every lane
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int j = 0; j < 32; ++j) total[i][j] = 0.f;
-            for (int k0 = 0; k0 < w.k_end; k0 += BK) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) sums[j] = 0.f;
+            const bool sums_wanted = a.db && w.m0 == 0 && 16 * warp < a.BN;
+            for (int k0 = 0; k0 < w.k_end; k0 += F::ACC_STAGES * BK) {
                 if (!wait_for(&sh.acc_full[acc.s], acc.phase, sh, a.error_word)) return;
                 __syncwarp();
                 tc::tc_fence_after_sync();
+                const uint32_t from = tmem + acc.s * F::ACC_COLUMNS;
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     if (half + 2 * i < chunks) {
                         float v[32];
-                        tc::tmem_load_32x32(sh.tmem_base + lanes + acc.s * F::BN + 32 * (half + 2 * i), v);
+                        tc::tmem_load_32x32(from + 32 * (half + 2 * i), v);
 #pragma unroll
                         for (int j = 0; j < 32; ++j) total[i][j] += v[j];
+                    }
+                }
+                if (sums_wanted) {
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        float v[8];
+                        tc::tmem_load_32x8(from + 128 + 16 * warp + 8 * q, v);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) sums[8 * q + j] += v[j];
                     }
                 }
                 tc::tc_fence_before_sync();
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(&sh.acc_empty[acc.s]);
                 acc.advance(2);
-                if constexpr (F::DRAIN_SUMS) {
-                    if (a.db) {  // the stage is given back by the warps that add up its columns as well
-                        if (w.m0 == 0) {
-                            if (!wait_for(&sh.full[at.s], at.phase, sh, a.error_word)) return;
-                            const int t = threadIdx.x, row = t >> 3, unit = t & 7;
-                            add_columns<T>(ring + at.s * F::STAGE_BYTES + F::A_BYTES + row * 128 + ((unit ^ (row & 7)) << 4), 2 * ((a.BN + 63) / 64), sums);
-                            __syncwarp();
-                        }
-                        if (lane == 0) tc::mbar_arrive(&sh.empty[at.s]);
-                        at.advance(F::STAGES);
-                    }
-                }
             }
-            if constexpr (F::DRAIN_SUMS)
-                if (a.db && w.m0 == 0) {
-                    leave_bias(a, w.row_tile, w.n0, sums, warp, lane);
-                    clear(sums);
-                }
+            if (sums_wanted && lane == 0) {
+                float* to = static_cast<float*>(a.out) + ((int64_t)w.row_tile * (a.d_in + BIAS_ROWS) + a.d_in) * a.ldo + w.n0 + 16 * warp;
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (w.n0 + 16 * warp + j < a.d_out) to[j] = sums[j];
+            }
 #pragma unroll
             for (int i = 0; i < 2; ++i)
                 if (half + 2 * i < chunks) put_chunk<T, MODE>(a, w, outlet, total[i], quarter, half + 2 * i, lane);
@@ -376,7 +336,7 @@ __device__ __forceinline__ void drain_role(const LinearArgs& a, Shared& sh, uint
             tc::tc_fence_after_sync();
             for (int chunk = half; chunk < chunks; chunk += 2) {
                 float v[32];
-                tc::tmem_load_32x32(sh.tmem_base + lanes + acc.s * F::BN + 32 * chunk, v);
+                tc::tmem_load_32x32(tmem + acc.s * F::ACC_COLUMNS + 32 * chunk, v);
                 if (MODE == FORWARD && a.bias) bias.add(v, chunk >> 1);
                 put_chunk<T, MODE>(a, w, outlet, v, quarter, chunk, lane);
             }
@@ -396,13 +356,13 @@ __global__ void __launch_bounds__(Form<T, MODE, LOADING>::THREADS, 1) linear_ker
     extern __shared__ uint8_t raw[];
     __shared__ Shared sh;
     uint8_t* ring_bytes = raw + ((1024u - (tc::smem_u32(raw) & 1023u)) & 1023u);
-    const uint32_t ring = tc::smem_u32(ring_bytes), slabs = ring + F::RING_BYTES;
+    const uint32_t ring = tc::smem_u32(ring_bytes), slabs = ring + F::RING_BYTES, ones = slabs + F::DRAIN_WARPS * F::OUT_BYTES;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     constexpr int MULTIPLIER = F::DRAIN_WARPS + F::LOAD_WARPS;
     if (threadIdx.x == 0) {
         for (int s = 0; s < F::STAGES; ++s) {
             tc::mbar_init(&sh.full[s], LOADING == BULK ? 1 : F::LOAD_WARPS);
-            tc::mbar_init(&sh.empty[s], 1 + (F::DRAIN_SUMS && a.db ? F::DRAIN_WARPS : 0));
+            tc::mbar_init(&sh.empty[s], 1);
         }
         for (int b = 0; b < 2; ++b) {
             tc::mbar_init(&sh.acc_full[b], 1);
@@ -412,8 +372,13 @@ __global__ void __launch_bounds__(Form<T, MODE, LOADING>::THREADS, 1) linear_ker
         tc::fence_barrier_init();
     }
     if (warp == MULTIPLIER) {
-        tc::tmem_alloc(&sh.tmem_base, 2 * F::BN);
+        tc::tmem_alloc(&sh.tmem_base, 2 * F::ACC_COLUMNS);
         tc::tmem_relinquish();
+    }
+    if (MODE == WEIGHT_GRADIENT && threadIdx.x < 64) {
+        const uint32_t one = std::is_same<T, __half>::value ? 0x3C003C00u : 0x3F803F80u;
+        store_16(ones + 16 * threadIdx.x, make_uint4(one, one, one, one));
+        tc::fence_proxy_async_smem();
     }
     wait_for_kernel_before();
     for (int g = threadIdx.x; g < a.G; g += F::THREADS) {
@@ -428,14 +393,14 @@ __global__ void __launch_bounds__(Form<T, MODE, LOADING>::THREADS, 1) linear_ker
     tc::tc_fence_after_sync();
     if (warp < F::DRAIN_WARPS) {
         if constexpr (LOADING == COPIES) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(DRAIN_REGISTERS));
-        drain_role<T, MODE, LOADING>(a, sh, slabs, ring);
+        drain_role<T, MODE, LOADING>(a, sh, slabs);
     } else if (warp < MULTIPLIER) {
         if constexpr (LOADING == COPIES) {
             copy_role<T, MODE>(a, sh, ring, threadIdx.x - 32 * F::DRAIN_WARPS);
         }
     } else {
         if constexpr (LOADING == COPIES) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(MULTIPLY_REGISTERS));
-        if (warp == MULTIPLIER) multiply_role<T, MODE, LOADING>(a, sh, ring);
+        if (warp == MULTIPLIER) multiply_role<T, MODE, LOADING>(a, sh, ring, ones);
         if constexpr (LOADING == BULK)
             if (warp == MULTIPLIER + 1) bulk_role<T, MODE>(a, sh, ring_bytes, lane);
     }
@@ -445,38 +410,47 @@ __global__ void __launch_bounds__(Form<T, MODE, LOADING>::THREADS, 1) linear_ker
     __syncthreads();
     if (warp == MULTIPLIER) {
         tc::tc_fence_after_sync();
-        tc::tmem_dealloc(sh.tmem_base, 2 * F::BN);
+        tc::tmem_dealloc(sh.tmem_base, 2 * F::ACC_COLUMNS);
     }
 }
 
-// The slots of every part added up in order.
-// A block takes 32 neighbouring values, its warps every eighth slot each (of a bias, of the slots' rows of partial sums).
+// The slots of every part added up in order.  A block takes 128 neighbouring places of a slot, its warps every eighth slot each; the
+// row behind the weights is the bias's, whose partial sums lie in bias_rows rows.
 constexpr int REDUCE_THREADS = 256;
 __global__ void __launch_bounds__(REDUCE_THREADS) linear_reduce_kernel(const __grid_constant__ LinearArgs a) {
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
-    __shared__ float red[8][32];
+    __shared__ float4 red[8][32];
     wait_for_kernel_before();
     number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums, a.span);
     const int part = blockIdx.y, lane = threadIdx.x & 31, share = threadIdx.x >> 5;
-    const int64_t weights = (int64_t)a.d_in * a.d_out, slot = (a.d_in + a.bias_rows) * a.ldo, i = (int64_t)blockIdx.x * 32 + lane;
-    const int64_t row = i / a.d_out, from = row * a.ldo + (i - row * a.d_out);
+    const int64_t slot = (a.d_in + a.bias_rows) * a.ldo, i = ((int64_t)blockIdx.x * 32 + lane) * 4;
+    const int row = (int)(i / a.ldo), col = (int)(i - row * a.ldo);
     const int t0 = tile_start[part], t1 = tile_start[part + 1];
-    const float* p = static_cast<const float*>(a.out) + t0 * slot + from;
-    float s = 0.f;
-    if (i < weights) {
+    const float* p = static_cast<const float*>(a.out) + t0 * slot + i;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](const float4 v) {
+        s.x += v.x;
+        s.y += v.y;
+        s.z += v.z;
+        s.w += v.w;
+    };
+    if (row < a.d_in) {
 #pragma unroll 4
-        for (int t = share; t < t1 - t0; t += 8) s += p[t * slot];
-    } else if (i < weights + a.d_out) {
+        for (int t = share; t < t1 - t0; t += 8) add(*reinterpret_cast<const float4*>(p + t * slot));
+    } else if (row == a.d_in) {
 #pragma unroll 4
-        for (int j = share; j < (t1 - t0) * a.bias_rows; j += 8) s += p[j / a.bias_rows * slot + j % a.bias_rows * a.ldo];
+        for (int j = share; j < (t1 - t0) * a.bias_rows; j += 8) add(*reinterpret_cast<const float4*>(p + j / a.bias_rows * slot + j % a.bias_rows * a.ldo));
     }
     red[share][lane] = s;
     __syncthreads();
-    if (share || i >= weights + a.d_out) return;
+    if (share || row > a.d_in || (row == a.d_in && !a.db)) return;
 #pragma unroll
-    for (int k = 1; k < 8; ++k) s += red[k][lane];
-    if (i < weights) a.dW[part * a.dw_stride + i] = s;
-    else if (a.db) a.db[part * a.db_stride + i - weights] = s;
+    for (int k = 1; k < 8; ++k) add(red[k][lane]);
+    float* to = row < a.d_in ? a.dW + part * a.dw_stride + (int64_t)row * a.d_out + col : a.db + part * a.db_stride + col;
+    if (col < a.d_out) to[0] = s.x;
+    if (col + 1 < a.d_out) to[1] = s.y;
+    if (col + 2 < a.d_out) to[2] = s.z;
+    if (col + 3 < a.d_out) to[3] = s.w;
 }
 
 // Columns in equal tiles of a multiple of 16.
@@ -601,9 +575,11 @@ extern "C" int32_t rtma_grouped_linear_dw(rtma_ctx* ctx, int32_t dtype, int64_t 
     a.m_tiles = (int)ceil_div(d_in, BM);
     a.bias_rows = dtype == RTMA_F32 ? SPLIT_BIAS_ROWS : BIAS_ROWS;
     cut_columns(a, d_out, dtype == RTMA_F32 ? SPLIT_DW_COLUMNS : 128);
-    // about four tiles per SM over the whole call; chunks of whole stages
-    const int64_t chunk = ceil_div(n * a.m_tiles * a.n_tiles, 4 * (int64_t)ctx->sm_count);
-    a.tile_rows = chunk < 256 ? 256 : ceil_div(chunk, BK) * BK;
+    // Chunks of whole stages, so many that parts of equal size make two tiles for every block that runs at a time and no third (a few
+    // blocks with one tile more than the others cost all of them the time of a tile).
+    const int64_t places = (int64_t)ctx->sm_count * (dtype == RTMA_F32 ? SPLIT_BLOCKS_PER_SM : 1);
+    const int64_t per_part = std::max<int64_t>(1, 2 * places / ((int64_t)a.m_tiles * a.n_tiles * a.G));
+    a.tile_rows = std::max<int64_t>(256, ceil_div(ceil_div(ceil_div(n, a.G), per_part), BK) * BK);
     a.tiles = n / a.tile_rows + a.G;
     const size_t es = row_type_bytes(dtype);
     a.d_in = d_in; a.d_out = d_out;
@@ -620,7 +596,7 @@ extern "C" int32_t rtma_grouped_linear_dw(rtma_ctx* ctx, int32_t dtype, int64_t 
     if (n > 0) RTMA_TRY(launch_linear<WEIGHT_GRADIENT>(ctx, dtype, a, KC_GEMM_WGRAD, stream));
     {
         KernelScope ks(ctx, KC_REDUCE_SGD, stream);
-        launch_kernel(linear_reduce_kernel, dim3((unsigned)ceil_div(weights + d_out, 32), (unsigned)a.G), REDUCE_THREADS, 0, stream, a);
+        launch_kernel(linear_reduce_kernel, dim3((unsigned)ceil_div((d_in + 1) * a.ldo, 128), (unsigned)a.G), REDUCE_THREADS, 0, stream, a);
     }
     RTMA_LAUNCH_CHECK(ctx);
     return RTMA_OK;

@@ -218,6 +218,6 @@ struct BiasHolder {
 
 // Products of fp32 rows (grouped_split.cu): widest tiles, the partial bias sums that a dw tile leaves, the scratch that the matrices'
 // planes take in forward and dx, and the launch.
-constexpr int SPLIT_COLUMNS = 128, SPLIT_DW_COLUMNS = 64, SPLIT_BIAS_ROWS = 8;
+constexpr int SPLIT_COLUMNS = 128, SPLIT_DW_COLUMNS = 64, SPLIT_BIAS_ROWS = 8, SPLIT_BLOCKS_PER_SM = 2;
 size_t split_planes_bytes(const grouped::LinearArgs& a);
 int32_t launch_split(rtma_ctx* ctx, int mode, grouped::LinearArgs& a, void* planes, int cls, cudaStream_t stream);

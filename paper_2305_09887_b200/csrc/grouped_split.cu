@@ -19,7 +19,7 @@ namespace {
 
 using namespace grouped;
 
-constexpr int BM = 128, BK = 32, WARPS = 8, THREADS = 32 * WARPS, BLOCKS_PER_SM = 2;
+constexpr int BM = 128, BK = 32, WARPS = 8, THREADS = 32 * WARPS, BLOCKS_PER_SM = SPLIT_BLOCKS_PER_SM;
 constexpr int A_STAGES = 2, W_STAGES = 2;
 
 template <int MODE>
