@@ -32,6 +32,7 @@ constexpr int BM = 128, BK = 64;
 // that drain: 256 x 112 + 256 x 96 + 128 x 64 = 61,440 = 640 x 96.
 constexpr int DRAIN_REGISTERS = 112, MULTIPLY_REGISTERS = 64;
 constexpr int SLAB_BYTES = 32 * 128;       // 32 rows of 64 16-bit values
+constexpr int DW_WAVES = 2;                // tiles of a weight gradient for every block that runs at a time
 constexpr int BIAS_ROWS = 1;               // of a slot: column sums of dY
 
 template <class T, int MODE, int LOADING>
@@ -381,13 +382,7 @@ __global__ void __launch_bounds__(Form<T, MODE, LOADING>::THREADS, 1) linear_ker
         tc::fence_proxy_async_smem();
     }
     wait_for_kernel_before();
-    for (int g = threadIdx.x; g < a.G; g += F::THREADS) {
-        int64_t begin, end;
-        part_rows(a.offsets, a.n, g, begin, end, a.span);
-        sh.begin[g] = (int32_t)begin;
-        sh.rows[g] = (int32_t)(end - begin);
-    }
-    number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, sh.tile_start, sh.warp_sums, a.span);
+    lay_out<MODE, F::THREADS, BK>(a, sh);
     tc::tc_fence_before_sync();
     __syncthreads();
     tc::tc_fence_after_sync();
@@ -421,7 +416,7 @@ __global__ void __launch_bounds__(REDUCE_THREADS) linear_reduce_kernel(const __g
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
     __shared__ float4 red[8][32];
     wait_for_kernel_before();
-    number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums, a.span);
+    number_tiles(a.offsets, a.n, a.G, a.n ? *a.chunk_rows : 1, a.tiles, tile_start, warp_sums, a.span);
     const int part = blockIdx.y, lane = threadIdx.x & 31, share = threadIdx.x >> 5;
     const int64_t slot = (a.d_in + a.bias_rows) * a.ldo, i = ((int64_t)blockIdx.x * 32 + lane) * 4;
     const int row = (int)(i / a.ldo), col = (int)(i - row * a.ldo);
@@ -575,12 +570,10 @@ extern "C" int32_t rtma_grouped_linear_dw(rtma_ctx* ctx, int32_t dtype, int64_t 
     a.m_tiles = (int)ceil_div(d_in, BM);
     a.bias_rows = dtype == RTMA_F32 ? SPLIT_BIAS_ROWS : BIAS_ROWS;
     cut_columns(a, d_out, dtype == RTMA_F32 ? SPLIT_DW_COLUMNS : 128);
-    // Chunks of whole stages, so many that parts of equal size make two tiles for every block that runs at a time and no third (a few
-    // blocks with one tile more than the others cost all of them the time of a tile).
+    // DW_WAVES tiles for every block that runs at a time (a chunk per part at least), of 256 rows or more
     const int64_t places = (int64_t)ctx->sm_count * (dtype == RTMA_F32 ? SPLIT_BLOCKS_PER_SM : 1);
-    const int64_t per_part = std::max<int64_t>(1, 2 * places / ((int64_t)a.m_tiles * a.n_tiles * a.G));
-    a.tile_rows = std::max<int64_t>(256, ceil_div(ceil_div(ceil_div(n, a.G), per_part), BK) * BK);
-    a.tiles = n / a.tile_rows + a.G;
+    a.tile_rows = 256;
+    a.tiles = std::min(std::max<int64_t>(a.G, DW_WAVES * places / ((int64_t)a.m_tiles * a.n_tiles)), n / a.tile_rows + a.G);
     const size_t es = row_type_bytes(dtype);
     a.d_in = d_in; a.d_out = d_out;
     a.A = X; a.lda = ldx; a.B = dY; a.ldb = lddy;
@@ -590,8 +583,9 @@ extern "C" int32_t rtma_grouped_linear_dw(rtma_ctx* ctx, int32_t dtype, int64_t 
     a.ldo = ceil_div(d_out, 8) * 8;
     a.go = 32;
     const int64_t slot_rows = a.tiles * (d_in + a.bias_rows);
-    RTMA_TRY(prepare_row_call(ctx, sizeof(float) * slot_rows * a.ldo, stream));
-    a.out = ctx->arena;
+    RTMA_TRY(prepare_row_call(ctx, 256 + sizeof(float) * slot_rows * a.ldo, stream));
+    a.chunk_rows = reinterpret_cast<int32_t*>(ctx->arena);
+    a.out = ctx->arena + 256;
     a.vo = dtype != RTMA_F32 && slot_rows < (int64_t(1) << 31) && make_store_map(&a.map_o, RTMA_F32, a.out, slot_rows, a.ldo, a.ldo, 64);
     if (n > 0) RTMA_TRY(launch_linear<WEIGHT_GRADIENT>(ctx, dtype, a, KC_GEMM_WGRAD, stream));
     {

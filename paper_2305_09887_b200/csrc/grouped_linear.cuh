@@ -16,7 +16,7 @@ struct LinearArgs {
     const int64_t* offsets;
     int64_t n;
     int G, span;
-    int64_t tile_rows, tiles;  // rows of a row tile (forward, dx: 128; dw: of a chunk), row tiles at most
+    int64_t tile_rows, tiles;  // rows of a row tile (forward, dx: 128; dw: at least, see fit_chunks), row tiles at most
     int m_tiles, n_tiles;      // tiles of one row tile: m_tiles (dw) x n_tiles
     int BN;
     int d_in, d_out;
@@ -32,6 +32,7 @@ struct LinearArgs {
     int64_t ldo;
     float *dW, *db;
     int64_t dw_stride, db_stride;
+    int32_t* chunk_rows;       // dw: where the rows of a row tile are left for the reduction
     int* error_word;
     CUtensorMap map_a, map_b;  // operands that are fetched by bulk-tensor loads
     CUtensorMap map_o;         // the result (dw: the slots, one below the other)
@@ -44,6 +45,7 @@ struct Shared {
     uint32_t tmem_base;
     int abort;
     int32_t warp_sums[32];
+    int32_t tile_rows;
     int32_t tile_start[RTMA_MAX_GROUPS + 1], begin[RTMA_MAX_GROUPS], rows[RTMA_MAX_GROUPS];
     alignas(16) float bias[8 * 128];  // of every drain warp's columns
 };
@@ -82,9 +84,9 @@ struct Walk {
         }
         n0 = rest * a.BN;
         while (row_tile >= sh.tile_start[part + 1]) ++part;  // tiles come in ascending order
-        const int64_t inside = (int64_t)(row_tile - sh.tile_start[part]) * a.tile_rows;
+        const int64_t inside = (int64_t)(row_tile - sh.tile_start[part]) * sh.tile_rows;
         row0 = sh.begin[part] + inside;
-        rows = (int)min((int64_t)sh.rows[part] - inside, a.tile_rows);
+        rows = (int)min((int64_t)sh.rows[part] - inside, (int64_t)sh.tile_rows);
         k_end = MODE == FORWARD ? a.d_in : MODE == INPUT_GRADIENT ? a.d_out : rows;
         k0 = 0;
         return true;
@@ -108,6 +110,45 @@ struct Walk {
         return at(a, sh);
     }
 };
+
+// The parts' rows and the numbers of their tiles; every thread of the block.
+template <int MODE, int THREADS, int STEP>
+__device__ __forceinline__ void lay_out(const LinearArgs& a, Shared& sh) {
+    for (int g = threadIdx.x; g < a.G; g += THREADS) {
+        int64_t begin, end;
+        part_rows(a.offsets, a.n, g, begin, end, a.span);
+        sh.begin[g] = (int32_t)begin;
+        sh.rows[g] = (int32_t)(end - begin);
+    }
+    if (MODE == WEIGHT_GRADIENT) {
+        __syncthreads();
+        if (threadIdx.x < 32) {
+            // The smallest chunks (multiples of STEP rows) of which there are not more than `tiles`, which fills the blocks that run at
+            // a time evenly, whatever the parts' sizes; by bisection.
+            const int lane = threadIdx.x;
+            int most = 1;
+            for (int g = lane; g < a.G; g += 32) most = max(most, sh.rows[g]);
+            for (int o = 16; o > 0; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+            int lo = (int)min(a.tile_rows, (int64_t)1 << 30) / STEP, hi = max((most + STEP - 1) / STEP, lo);  // hi fits: a tile a part
+            while (lo < hi) {
+                const int mid = (lo + hi) / 2, rows = mid * STEP;
+                int64_t count = 0;
+                for (int g = lane; g < a.G; g += 32) count += (sh.rows[g] + rows - 1) / rows;
+                for (int o = 16; o > 0; o >>= 1) count += __shfl_xor_sync(0xffffffffu, count, o);
+                if (count <= a.tiles) hi = mid;
+                else lo = mid + 1;
+            }
+            if (lane == 0) {
+                sh.tile_rows = lo * STEP;
+                if (blockIdx.x == 0) *a.chunk_rows = lo * STEP;
+            }
+        }
+    } else if (threadIdx.x == 0) {
+        sh.tile_rows = (int32_t)a.tile_rows;
+    }
+    __syncthreads();
+    number_tiles(a.offsets, a.n, a.G, sh.tile_rows, a.tiles, sh.tile_start, sh.warp_sums, a.span);
+}
 
 __device__ __forceinline__ void store_16(uint32_t dst, uint4 v) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");

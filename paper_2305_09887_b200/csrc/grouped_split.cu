@@ -422,13 +422,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS_PER_SM) split_kernel(const __g
         tc::tmem_relinquish();
     }
     wait_for_kernel_before();
-    for (int g = threadIdx.x; g < a.G; g += THREADS) {
-        int64_t begin, end;
-        part_rows(a.offsets, a.n, g, begin, end, a.span);
-        sh.begin[g] = (int32_t)begin;
-        sh.rows[g] = (int32_t)(end - begin);
-    }
-    number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, sh.tile_start, sh.warp_sums, a.span);
+    lay_out<MODE, THREADS, BK>(a, sh);
     tc::tc_fence_before_sync();
     __syncthreads();
     tc::tc_fence_after_sync();
