@@ -6,6 +6,8 @@
 //   dx = rstd (gamma du - (S1 + xhat S2) / m),  S1 = sum gamma du, S2 = sum gamma du xhat over the set.
 // A thread keeps eight neighbouring channels and walks down the rows of a tile (a run of rows of one part); what is summed over
 // rows is left per tile and added up in a fixed order by a second kernel, so results do not depend on which block ran when.
+#include <algorithm>
+
 #include "rows.cuh"
 
 RTMA_BOUNDS_TU()
@@ -18,7 +20,8 @@ constexpr int NORM_MAX_CHANNELS = 8 * NORM_THREADS;
 struct NormArgs {
     const int64_t* offsets;
     int64_t n;
-    int G, C, groups, per_set, units, rows_at_once;  // per_set = C / groups; units of eight channels; rows a block works on at a time
+    int G, C, groups, per_set, units, rows_at_once, pitch;  // per_set = C / groups; units of eight channels; rows a block works on at a time;
+                                                           // lanes of a row where warps keep rows to themselves (0: they do not)
     int tile_rows;
     int64_t tiles;  // at most so many
     int act;
@@ -71,6 +74,10 @@ __device__ __forceinline__ float activate_back_eight(int act, float slope, const
         }
     }
     return ds;
+}
+
+__device__ __forceinline__ uint32_t id_of(const NormArgs& a, int64_t r) {
+    return a.drop.ids ? (uint32_t)__ldg(a.drop.ids + r) : (uint32_t)r;
 }
 
 // A thread's place in a block and its channels' parameters.
@@ -173,16 +180,10 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_rows_kernel(const NormArgs 
     }
 }
 
-// dh -> du, xhat and u of eight channels; returns the slope's gradient
-template <class T>
-__device__ __forceinline__ float back_eight(const NormArgs& a, int64_t r, int u, int valid, const float (&mean)[8], const float (&rstd)[8],
-                                            const float (&gam)[8], const float (&bet)[8], float slope, float (&xhat)[8], float (&du)[8]) {
-    Eight<T> x, d;
-    x.load(static_cast<const T*>(a.X) + r * a.ldx + 8 * u, valid, a.vx);
-    d.load(static_cast<const T*>(a.dY) + r * a.lddy + 8 * u, valid, a.vdy);
-    x.values(xhat);
-    d.values(du);
-    if (a.drop.threshold) drop_eight(a.drop, a.drop.ids ? (uint32_t)__ldg(a.drop.ids + r) : (uint32_t)r, u, du);
+// dh (in du) -> du and x (in xhat) -> xhat of eight channels; returns the slope's gradient
+__device__ __forceinline__ float back_values(const NormArgs& a, int64_t r, int u, const float (&mean)[8], const float (&rstd)[8], const float (&gam)[8],
+                                             const float (&bet)[8], float slope, float (&xhat)[8], float (&du)[8]) {
+    if (a.drop.threshold) drop_eight(a.drop, id_of(a, r), u, du);
     float pre[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -191,13 +192,22 @@ __device__ __forceinline__ float back_eight(const NormArgs& a, int64_t r, int u,
     }
     return activate_back_eight(a.act, slope, pre, du);
 }
+template <class T>
+__device__ __forceinline__ float back_eight(const NormArgs& a, int64_t r, int u, int valid, const float (&mean)[8], const float (&rstd)[8],
+                                            const float (&gam)[8], const float (&bet)[8], float slope, float (&xhat)[8], float (&du)[8]) {
+    Eight<T> x, d;
+    x.load(static_cast<const T*>(a.X) + r * a.ldx + 8 * u, valid, a.vx);
+    d.load(static_cast<const T*>(a.dY) + r * a.lddy + 8 * u, valid, a.vdy);
+    x.values(xhat);
+    d.values(du);
+    return back_values(a, r, u, mean, rstd, gam, bet, slope, xhat, du);
+}
 
-// Sums over a block's rows of its channels' (du, du xhat) and of the slope's gradient, written to the tile's slot.
-__device__ __forceinline__ void leave_sums(const NormArgs& a, const Lane& at, int tile, float (&sb)[8], float (&sg)[8], float ds, float* shared) {
-    float* red = shared;  // [thread][8], one kind after the other
-    const int threads = a.rows_at_once * a.units;
+// Sums over a block's rows of (du, du xhat) of a thread's eight channels from c0 on, written to the tile's slot.  Threads pitch apart
+// hold the same channels, rows_at_once of them.
+__device__ __forceinline__ void leave_sums(const NormArgs& a, int tile, int c0, int y, int pitch, int rows_at_once, float (&sb)[8], float (&sg)[8], float* red) {
     int top = 1;
-    while (top < a.rows_at_once) top <<= 1;
+    while (top < rows_at_once) top <<= 1;
     float* out = a.partial + (int64_t)tile * (2 * a.C + 1);
 #pragma unroll
     for (int kind = 0; kind < 2; ++kind) {
@@ -206,23 +216,256 @@ __device__ __forceinline__ void leave_sums(const NormArgs& a, const Lane& at, in
         for (int j = 0; j < 8; ++j) red[j * NORM_THREADS + threadIdx.x] = kind == 0 ? sb[j] : sg[j];
         for (int h = top >> 1; h > 0; h >>= 1) {
             __syncthreads();
-            if (at.active && at.y < h && at.y + h < a.rows_at_once) {
+            if (y < h && y + h < rows_at_once) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) red[j * NORM_THREADS + threadIdx.x] += red[j * NORM_THREADS + threadIdx.x + h * a.units];
+                for (int j = 0; j < 8; ++j) red[j * NORM_THREADS + threadIdx.x] += red[j * NORM_THREADS + threadIdx.x + h * pitch];
             }
         }
         __syncthreads();
-        for (int c = threadIdx.x; c < a.C; c += NORM_THREADS) out[kind * a.C + c] = red[(c & 7) * NORM_THREADS + (c >> 3)];
+        if (y == 0) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (c0 + j < a.C) out[kind * a.C + c0 + j] = red[j * NORM_THREADS + threadIdx.x];
+        }
     }
     __syncthreads();
-    red[threadIdx.x] = (int)threadIdx.x < threads ? ds : 0.f;
+}
+__device__ __forceinline__ void leave_slope(const NormArgs& a, int tile, float ds, float* red) {
+    red[threadIdx.x] = ds;
     for (int h = NORM_THREADS / 2; h > 0; h >>= 1) {
         __syncthreads();
         if ((int)threadIdx.x < h) red[threadIdx.x] += red[threadIdx.x + h];
     }
     __syncthreads();
-    if (threadIdx.x == 0) out[2 * a.C] = red[0];
+    if (threadIdx.x == 0) a.partial[(int64_t)tile * (2 * a.C + 1) + 2 * a.C] = red[0];
     __syncthreads();
+}
+
+// A run of rows of one part.
+struct Run {
+    int part;
+    int64_t begin, end;
+    __device__ __forceinline__ Run(const NormArgs& a, const int32_t* tile_start, int tile) {
+        part = part_of_tile(tile_start, a.G, tile);
+        part_rows(a.offsets, a.n, part, begin, end);
+        begin += (int64_t)(tile - tile_start[part]) * a.tile_rows;
+        end = min(end, begin + a.tile_rows);
+    }
+};
+
+// ---- rows of up to 512 channels whose sets are runs of lanes ---------------------------------------
+// A row lies in `pitch` lanes (a power of two), eight channels each (NP times: channels 8 (lane + 32 p) ..); a set is the whole row or
+// a power of two of neighbouring lanes, so its sums are exchanged within a warp and nothing goes through shared memory.  RB rows
+// side by side hide one another's loads and shuffles.
+__device__ __forceinline__ float set_sum(float x, int lanes) {
+    for (int o = lanes >> 1; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
+
+template <class T, int NP, int RB>
+__global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_kernel(const NormArgs a) {
+    __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
+    wait_for_kernel_before();
+    number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums);
+    const int pitch = a.pitch, u = threadIdx.x & (pitch - 1), y = threadIdx.x / pitch, rows_at_once = NORM_THREADS / pitch;
+    const bool whole = a.groups == 1;
+    const int lanes = whole ? pitch : a.per_set / 8;  // of a set
+    const float inv = 1.f / (float)a.per_set;
+    const T* X = static_cast<const T*>(a.X);
+    T* Y = static_cast<T*>(a.Y);
+    int valid[NP];
+#pragma unroll
+    for (int p = 0; p < NP; ++p) valid[p] = max(0, min(8, a.C - 8 * (u + 32 * p)));
+    for (int tile = blockIdx.x; tile < tile_start[a.G]; tile += gridDim.x) {
+        const Run run(a, tile_start, tile);
+        float gam[NP][8], bet[NP][8];
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            load_params(a.gamma, a.gamma_stride, run.part, u + 32 * p, valid[p], 1.f, gam[p]);
+            load_params(a.beta, a.beta_stride, run.part, u + 32 * p, valid[p], 0.f, bet[p]);
+        }
+        const float slope = a.slope ? __ldg(a.slope + run.part * a.slope_stride) : 0.f;
+        Eight<T> raw[RB][NP];  // the next rows are on their way while these are worked on
+        auto request = [&](int64_t r0) {
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {
+                const int64_t r = r0 + y + b * rows_at_once;
+#pragma unroll
+                for (int p = 0; p < NP; ++p) raw[b][p].load(X + r * a.ldx + 8 * (u + 32 * p), r < run.end ? valid[p] : 0, a.vx);
+            }
+        };
+        request(run.begin);
+        for (int64_t r0 = run.begin; r0 < run.end; r0 += RB * rows_at_once) {  // the same number of times in every lane
+            float v[RB][NP][8], mean[RB][NP], rstd[RB][NP];
+#pragma unroll
+            for (int b = 0; b < RB; ++b)
+#pragma unroll
+                for (int p = 0; p < NP; ++p) raw[b][p].values(v[b][p]);
+            request(r0 + RB * rows_at_once);
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+                    float s = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) s += v[b][p][j];  // what is not there reads as zero
+                    mean[b][p] = s;
+                }
+                if (NP == 2 && whole) mean[b][0] += mean[b][NP - 1];
+            }
+#pragma unroll
+            for (int b = 0; b < RB; ++b)
+#pragma unroll
+                for (int p = 0; p < NP; ++p) mean[b][p] = p && whole ? mean[b][0] : set_sum(mean[b][p], lanes) * inv;
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+                    float s = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        v[b][p][j] = j < valid[p] ? v[b][p][j] - mean[b][p] : 0.f;
+                        s = fmaf(v[b][p][j], v[b][p][j], s);
+                    }
+                    rstd[b][p] = s;
+                }
+                if (NP == 2 && whole) rstd[b][0] += rstd[b][NP - 1];
+            }
+#pragma unroll
+            for (int b = 0; b < RB; ++b)
+#pragma unroll
+                for (int p = 0; p < NP; ++p) rstd[b][p] = p && whole ? rstd[b][0] : 1.f / sqrtf(set_sum(rstd[b][p], lanes) * inv + a.eps);
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {
+                const int64_t r = r0 + y + b * rows_at_once;
+                if (r >= run.end) continue;
+                const uint32_t id = a.drop.threshold ? id_of(a, r) : 0u;
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+                    const int unit = u + 32 * p;
+                    if (valid[p] == 0) continue;
+                    if (a.stats && (whole ? unit == 0 : (unit & (lanes - 1)) == 0))
+                        *reinterpret_cast<float2*>(a.stats + 2 * (r * a.groups + (whole ? 0 : unit / lanes))) = make_float2(mean[b][p], rstd[b][p]);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[b][p][j] = fmaf(v[b][p][j] * rstd[b][p], gam[p][j], bet[p][j]);
+                    activate_eight(a.act, slope, v[b][p]);
+                    if (a.drop.threshold) drop_eight(a.drop, id, unit, v[b][p]);
+                    store_eight(Y + r * a.ldy + 8 * unit, v[b][p], valid[p], a.vy);
+                }
+            }
+        }
+    }
+}
+
+template <class T, int NP, int RB>
+__global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_grad_kernel(const NormArgs a) {
+    __shared__ float shared[8 * NORM_THREADS];
+    __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
+    wait_for_kernel_before();
+    number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums);
+    const int pitch = a.pitch, u = threadIdx.x & (pitch - 1), y = threadIdx.x / pitch, rows_at_once = NORM_THREADS / pitch;
+    const bool whole = a.groups == 1;
+    const int lanes = whole ? pitch : a.per_set / 8;
+    const float inv = 1.f / (float)a.per_set;
+    const T* X = static_cast<const T*>(a.X);
+    const T* dY = static_cast<const T*>(a.dY);
+    T* Y = static_cast<T*>(a.Y);
+    int valid[NP];
+#pragma unroll
+    for (int p = 0; p < NP; ++p) valid[p] = max(0, min(8, a.C - 8 * (u + 32 * p)));
+    for (int tile = blockIdx.x; tile < tile_start[a.G]; tile += gridDim.x) {
+        const Run run(a, tile_start, tile);
+        float gam[NP][8], bet[NP][8], sb[NP][8], sg[NP][8], ds = 0.f;
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            load_params(a.gamma, a.gamma_stride, run.part, u + 32 * p, valid[p], 1.f, gam[p]);
+            load_params(a.beta, a.beta_stride, run.part, u + 32 * p, valid[p], 0.f, bet[p]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sb[p][j] = sg[p][j] = 0.f;
+        }
+        const float slope = a.slope ? __ldg(a.slope + run.part * a.slope_stride) : 0.f;
+        Eight<T> rx[RB][NP], rd[RB][NP];
+        float2 rs[RB][NP];
+        auto request = [&](int64_t r0) {
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {
+                const int64_t r = r0 + y + b * rows_at_once;
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+                    const int here = r < run.end ? valid[p] : 0;
+                    rx[b][p].load(X + r * a.ldx + 8 * (u + 32 * p), here, a.vx);
+                    rd[b][p].load(dY + r * a.lddy + 8 * (u + 32 * p), here, a.vdy);
+                    rs[b][p] = here ? *reinterpret_cast<const float2*>(a.stats + 2 * (r * a.groups + (whole ? 0 : (u + 32 * p) / lanes))) : make_float2(0.f, 0.f);
+                }
+            }
+        };
+        request(run.begin);
+        for (int64_t r0 = run.begin; r0 < run.end; r0 += RB * rows_at_once) {
+            float xh[RB][NP][8], du[RB][NP][8], s1[RB][NP], s2[RB][NP];
+            float2 st[RB][NP];
+#pragma unroll
+            for (int b = 0; b < RB; ++b)
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+                    rx[b][p].values(xh[b][p]);
+                    rd[b][p].values(du[b][p]);
+                    st[b][p] = rs[b][p];
+                }
+            request(r0 + RB * rows_at_once);
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {
+                const int64_t r = r0 + y + b * rows_at_once;
+                const uint32_t id = a.drop.threshold && r < run.end ? id_of(a, r) : 0u;
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+                    if (a.drop.threshold) drop_eight(a.drop, id, u + 32 * p, du[b][p]);
+                    float pre[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        xh[b][p][j] = (xh[b][p][j] - st[b][p].x) * st[b][p].y;
+                        pre[j] = fmaf(xh[b][p][j], gam[p][j], bet[p][j]);
+                    }
+                    ds += activate_back_eight(a.act, slope, pre, du[b][p]);
+                    float t1 = 0.f, t2 = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        sb[p][j] += du[b][p][j];
+                        sg[p][j] = fmaf(du[b][p][j], xh[b][p][j], sg[p][j]);
+                        du[b][p][j] *= gam[p][j];
+                        t1 += du[b][p][j];
+                        t2 = fmaf(du[b][p][j], xh[b][p][j], t2);
+                    }
+                    s1[b][p] = t1;
+                    s2[b][p] = t2;
+                }
+                if (NP == 2 && whole) {
+                    s1[b][0] += s1[b][NP - 1];
+                    s2[b][0] += s2[b][NP - 1];
+                }
+            }
+#pragma unroll
+            for (int b = 0; b < RB; ++b)
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+                    s1[b][p] = p && whole ? s1[b][0] : set_sum(s1[b][p], lanes) * inv;
+                    s2[b][p] = p && whole ? s2[b][0] : set_sum(s2[b][p], lanes) * inv;
+                }
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {
+                const int64_t r = r0 + y + b * rows_at_once;
+                if (r >= run.end) continue;
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) du[b][p][j] = st[b][p].y * (du[b][p][j] - s1[b][p] - xh[b][p][j] * s2[b][p]);
+                    if (valid[p]) store_eight(Y + r * a.ldy + 8 * (u + 32 * p), du[b][p], valid[p], a.vy);
+                }
+            }
+        }
+#pragma unroll
+        for (int p = 0; p < NP; ++p) leave_sums(a, tile, 8 * (u + 32 * p), y, pitch, rows_at_once, sb[p], sg[p], shared);
+        leave_slope(a, tile, ds, shared);
+    }
 }
 
 template <class T>
@@ -299,7 +542,8 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_rows_grad_kernel(const Norm
                 store_eight(Y + r * a.ldy + 8 * at.u, du, at.valid, a.vy);
             }
         }
-        leave_sums(a, at, tile, sb, sg, ds, shared);
+        leave_sums(a, tile, 8 * at.u, at.active ? at.y : NORM_THREADS, a.units, a.rows_at_once, sb, sg, shared);
+        leave_slope(a, tile, ds, shared);
     }
 }
 
@@ -313,7 +557,7 @@ __device__ __forceinline__ void join_moments(float& mean, float& m2, float n, fl
 
 // Mean and sum of squared differences of every set within a tile.
 template <class T>
-__global__ void __launch_bounds__(NORM_THREADS) norm_stats_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(NORM_THREADS, 2) norm_stats_kernel(const NormArgs a) {
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
     __shared__ float s_mean[8 * NORM_THREADS], s_m2[8 * NORM_THREADS], s_count[NORM_THREADS];
     wait_for_kernel_before();
@@ -332,38 +576,50 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_stats_kernel(const NormArgs
 #pragma unroll
         for (int j = 0; j < 8; ++j) mean[j] = m2[j] = 0.f;
         if (at.active) {
-            for (int64_t r = begin + at.y; r < end; r += BATCH * a.rows_at_once) {
-                Eight<T> x[BATCH];
-                int rows = 0;
+            int64_t r = begin + at.y;
+            const int64_t step = BATCH * (int64_t)a.rows_at_once;
+            Eight<T> x[BATCH];
+            auto request = [&](int64_t from) {  // rows behind the last are not there
 #pragma unroll
-                for (int b = 0; b < BATCH; ++b) {
-                    const int64_t row = r + b * a.rows_at_once;
-                    const bool ok = row < end;
-                    x[b].load(X + (ok ? row : r) * a.ldx + 8 * at.u, at.valid, a.vx);
-                    rows += ok;
-                }
+                for (int b = 0; b < BATCH; ++b)
+                    x[b].load(X + (from + b * a.rows_at_once) * a.ldx + 8 * at.u, from + b * a.rows_at_once < end ? at.valid : 0, a.vx);
+            };
+            request(r);
+            for (; r + step - a.rows_at_once < end; r += step) {
                 // moments of the batch about its own mean, then joined to the thread's
-                const float nb = (float)rows, inv = 1.f / nb, share = nb / (count + nb), weight = count * share;
+                const float share = BATCH / (count + BATCH), weight = count * share;
                 float v[BATCH][8];
 #pragma unroll
                 for (int b = 0; b < BATCH; ++b) x[b].values(v[b]);
+                request(r + step);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     float s = v[0][j];
 #pragma unroll
-                    for (int b = 1; b < BATCH; ++b) s += b < rows ? v[b][j] : 0.f;
-                    s *= inv;
+                    for (int b = 1; b < BATCH; ++b) s += v[b][j];
+                    s *= 1.f / BATCH;
                     float q = 0.f;
 #pragma unroll
-                    for (int b = 0; b < BATCH; ++b) {
-                        const float d = b < rows ? v[b][j] - s : 0.f;
-                        q = fmaf(d, d, q);
-                    }
+                    for (int b = 0; b < BATCH; ++b) q = fmaf(v[b][j] - s, v[b][j] - s, q);
                     const float d = s - mean[j];
                     mean[j] = fmaf(d, share, mean[j]);
                     m2[j] += fmaf(d * d, weight, q);
                 }
-                count += nb;
+                count += BATCH;
+            }
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b) {
+                if (r + b * a.rows_at_once >= end) break;
+                float v[8];
+                x[b].values(v);
+                const float share = 1.f / (count + 1.f), weight = count * share;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float d = v[j] - mean[j];
+                    mean[j] = fmaf(d, share, mean[j]);
+                    m2[j] = fmaf(d * d, weight, m2[j]);
+                }
+                count += 1.f;
             }
         }
 #pragma unroll
@@ -460,7 +716,8 @@ __device__ __forceinline__ void load_part_stats(const NormArgs& a, int part, con
 }
 
 template <class T>
-__global__ void __launch_bounds__(NORM_THREADS) norm_apply_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(NORM_THREADS, 2) norm_apply_kernel(const NormArgs a) {
+    constexpr int RB = 4;  // rows in flight
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
     wait_for_kernel_before();
     number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums);
@@ -479,22 +736,34 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_apply_kernel(const NormArgs
         load_params(a.beta, a.beta_stride, part, at.u, at.valid, 0.f, bet);
         load_part_stats(a, part, at, mean, rstd);
         const float slope = a.slope ? __ldg(a.slope + part * a.slope_stride) : 0.f;
-        for (int64_t r = begin + at.y; r < end; r += a.rows_at_once) {
-            Eight<T> x;
-            x.load(X + r * a.ldx + 8 * at.u, at.valid, a.vx);
-            float v[8];
-            x.values(v);
+        Eight<T> x[RB];
+        auto request = [&](int64_t from, int b) {
+            const int64_t row = from + b * a.rows_at_once;
+            x[b].load(X + row * a.ldx + 8 * at.u, row < end ? at.valid : 0, a.vx);
+        };
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = fmaf((v[j] - mean[j]) * rstd[j], gam[j], bet[j]);
-            activate_eight(a.act, slope, v);
-            if (a.drop.threshold) drop_eight(a.drop, a.drop.ids ? (uint32_t)__ldg(a.drop.ids + r) : (uint32_t)r, at.u, v);
-            store_eight(Y + r * a.ldy + 8 * at.u, v, at.valid, a.vy);
+        for (int b = 0; b < RB; ++b) request(begin + at.y, b);
+        for (int64_t r = begin + at.y; r < end; r += RB * a.rows_at_once) {
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {
+                const int64_t row = r + b * a.rows_at_once;
+                if (row >= end) break;
+                float v[8];
+                x[b].values(v);
+                request(r + RB * a.rows_at_once, b);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = fmaf((v[j] - mean[j]) * rstd[j], gam[j], bet[j]);
+                activate_eight(a.act, slope, v);
+                if (a.drop.threshold) drop_eight(a.drop, id_of(a, row), at.u, v);
+                store_eight(Y + row * a.ldy + 8 * at.u, v, at.valid, a.vy);
+            }
         }
     }
 }
 
 template <class T>
-__global__ void __launch_bounds__(NORM_THREADS) norm_grad_sums_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(NORM_THREADS, 2) norm_grad_sums_kernel(const NormArgs a) {
+    constexpr int RB = 8 / sizeof(T);  // rows in flight
     __shared__ float shared[8 * NORM_THREADS];
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
     wait_for_kernel_before();
@@ -514,22 +783,40 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_grad_sums_kernel(const Norm
 #pragma unroll
         for (int j = 0; j < 8; ++j) sb[j] = sg[j] = 0.f;
         if (at.active) {
-            for (int64_t r = begin + at.y; r < end; r += a.rows_at_once) {
-                float xhat[8], du[8];
-                ds += back_eight<T>(a, r, at.u, at.valid, mean, rstd, gam, bet, slope, xhat, du);
+            Eight<T> x[RB], d[RB];
+            auto request = [&](int64_t from, int b) {
+                const int64_t row = from + b * a.rows_at_once;
+                x[b].load(static_cast<const T*>(a.X) + row * a.ldx + 8 * at.u, row < end ? at.valid : 0, a.vx);
+                d[b].load(static_cast<const T*>(a.dY) + row * a.lddy + 8 * at.u, row < end ? at.valid : 0, a.vdy);
+            };
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    sb[j] += du[j];
-                    sg[j] = fmaf(du[j], xhat[j], sg[j]);
+            for (int b = 0; b < RB; ++b) request(begin + at.y, b);
+            for (int64_t r = begin + at.y; r < end; r += RB * a.rows_at_once) {
+#pragma unroll
+                for (int b = 0; b < RB; ++b) {
+                    const int64_t row = r + b * a.rows_at_once;
+                    if (row >= end) break;
+                    float xhat[8], du[8];
+                    x[b].values(xhat);
+                    d[b].values(du);
+                    request(r + RB * a.rows_at_once, b);
+                    ds += back_values(a, row, at.u, mean, rstd, gam, bet, slope, xhat, du);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        sb[j] += du[j];
+                        sg[j] = fmaf(du[j], xhat[j], sg[j]);
+                    }
                 }
             }
         }
-        leave_sums(a, at, tile, sb, sg, ds, shared);
+        leave_sums(a, tile, 8 * at.u, at.active ? at.y : NORM_THREADS, a.units, a.rows_at_once, sb, sg, shared);
+        leave_slope(a, tile, ds, shared);
     }
 }
 
 template <class T>
-__global__ void __launch_bounds__(NORM_THREADS) norm_grad_apply_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(NORM_THREADS, 2) norm_grad_apply_kernel(const NormArgs a) {
+    constexpr int RB = 8 / sizeof(T);
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
     __shared__ float2 of_set[NORM_MAX_CHANNELS];
     wait_for_kernel_before();
@@ -573,12 +860,28 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_grad_apply_kernel(const Nor
             m2[j] = s.y;
         }
         if (at.active) {
-            for (int64_t r = begin + at.y; r < end; r += a.rows_at_once) {
-                float xhat[8], du[8];
-                back_eight<T>(a, r, at.u, at.valid, mean, rstd, gam, bet, slope, xhat, du);
+            Eight<T> x[RB], d[RB];
+            auto request = [&](int64_t from, int b) {
+                const int64_t row = from + b * a.rows_at_once;
+                x[b].load(static_cast<const T*>(a.X) + row * a.ldx + 8 * at.u, row < end ? at.valid : 0, a.vx);
+                d[b].load(static_cast<const T*>(a.dY) + row * a.lddy + 8 * at.u, row < end ? at.valid : 0, a.vdy);
+            };
 #pragma unroll
-                for (int j = 0; j < 8; ++j) du[j] = rstd[j] * (fmaf(gam[j], du[j], -m1[j]) - xhat[j] * m2[j]);
-                store_eight(Y + r * a.ldy + 8 * at.u, du, at.valid, a.vy);
+            for (int b = 0; b < RB; ++b) request(begin + at.y, b);
+            for (int64_t r = begin + at.y; r < end; r += RB * a.rows_at_once) {
+#pragma unroll
+                for (int b = 0; b < RB; ++b) {
+                    const int64_t row = r + b * a.rows_at_once;
+                    if (row >= end) break;
+                    float xhat[8], du[8];
+                    x[b].values(xhat);
+                    d[b].values(du);
+                    request(r + RB * a.rows_at_once, b);
+                    back_values(a, row, at.u, mean, rstd, gam, bet, slope, xhat, du);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) du[j] = rstd[j] * (fmaf(gam[j], du[j], -m1[j]) - xhat[j] * m2[j]);
+                    store_eight(Y + row * a.ldy + 8 * at.u, du, at.valid, a.vy);
+                }
             }
         }
     }
@@ -653,6 +956,10 @@ NormArgs norm_args(const rtma_ctx* ctx, const rtma_norm_desc* d, int64_t n, int3
     a.per_set = d->C / d->groups;
     a.units = (d->C + 7) / 8;
     a.rows_at_once = NORM_THREADS / a.units;
+    // warps keep rows to themselves where a set is a power of two of lanes, or the whole row
+    const int lanes = a.per_set / 8;
+    if (d->C <= 512 && (d->groups == 1 || (a.per_set % 8 == 0 && lanes <= 32 && (lanes & (lanes - 1)) == 0)))
+        for (a.pitch = 1; a.pitch < std::min(a.units, 32);) a.pitch *= 2;
     // four runs of rows per SM; a few rows per thread at least
     const int64_t least = 4 * (int64_t)a.rows_at_once, even = ceil_div(n, 4 * (int64_t)ctx->sm_count);
     a.tile_rows = (int)(even > least ? even : least);
@@ -698,9 +1005,11 @@ extern "C" int32_t rtma_group_norm(rtma_ctx* ctx, const rtma_norm_desc* d, int64
     const unsigned grid = (unsigned)tiles;
     if (rows) {
         const size_t smem = sizeof(float) * a.rows_at_once * (8 * a.units + 2 * (size_t)a.groups);
-        auto kernel = NORM_KERNEL(norm_rows_kernel);
+        auto kernel = a.pitch && a.units <= 32 ? by_type(d->dtype, &norm_warp_rows_kernel<float, 1, 4>, &norm_warp_rows_kernel<__nv_bfloat16, 1, 4>, &norm_warp_rows_kernel<__half, 1, 4>)
+                      : a.pitch ? by_type(d->dtype, &norm_warp_rows_kernel<float, 2, 2>, &norm_warp_rows_kernel<__nv_bfloat16, 2, 2>, &norm_warp_rows_kernel<__half, 2, 2>)
+                                : NORM_KERNEL(norm_rows_kernel);
         KernelScope ks(ctx, KC_POST, stream);
-        launch_kernel(kernel, grid, NORM_THREADS, smem, stream, a);
+        launch_kernel(kernel, grid, NORM_THREADS, a.pitch ? 0 : smem, stream, a);
     } else {
         ArenaCursor cur(ctx->arena);
         a.pieces = cur.take<float2>(tiles * a.groups);
@@ -758,8 +1067,10 @@ extern "C" int32_t rtma_group_norm_grad(rtma_ctx* ctx, const rtma_norm_desc* d, 
         KernelScope ks(ctx, KC_POST, stream);
         if (rows) {
             const size_t smem = sizeof(float2) * (8 * NORM_THREADS + (size_t)a.rows_at_once * a.groups);
-            auto kernel = NORM_KERNEL(norm_rows_grad_kernel);
-            launch_kernel(kernel, (unsigned)tiles, NORM_THREADS, smem, stream, a);
+            auto kernel = a.pitch && a.units <= 32 ? by_type(d->dtype, &norm_warp_rows_grad_kernel<float, 1, 2>, &norm_warp_rows_grad_kernel<__nv_bfloat16, 1, 2>, &norm_warp_rows_grad_kernel<__half, 1, 2>)
+                          : a.pitch ? by_type(d->dtype, &norm_warp_rows_grad_kernel<float, 2, 1>, &norm_warp_rows_grad_kernel<__nv_bfloat16, 2, 1>, &norm_warp_rows_grad_kernel<__half, 2, 1>)
+                                    : NORM_KERNEL(norm_rows_grad_kernel);
+            launch_kernel(kernel, (unsigned)tiles, NORM_THREADS, a.pitch ? 0 : smem, stream, a);
         } else {
             launch_kernel(NORM_KERNEL(norm_grad_sums_kernel), (unsigned)tiles, NORM_THREADS, 0, stream, a);
         }
