@@ -41,40 +41,75 @@ struct NormArgs {
     int64_t dgamma_stride, dbeta_stride, dslope_stride;
 };
 
-__device__ __forceinline__ float sigmoid(float u) { return __fdividef(1.f, 1.f + __expf(-u)); }
+// 1 / (1 + exp(-u)): two special-function instructions, relative error a few 2^-23 (1 + |u|)
+__device__ __forceinline__ f2 sigmoid2(f2 u) {
+    const float log2e = 1.4426950408889634f;
+    float a, b;
+    unpack2(mul2(u, pack2(-log2e, -log2e)), a, b);
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(a));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(b));
+    unpack2(add2(pack2(a, b), pack2(1.f, 1.f)), a, b);
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(a));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(b));
+    return pack2(a, b);
+}
 
-__device__ __forceinline__ void activate_eight(int act, float slope, float (&u)[8]) {
-    if (act == RTMA_ACT_RELU || act == RTMA_ACT_PRELU) {
+__device__ __forceinline__ void activate(int act, float slope, f2 (&u)[4]) {
+    if (act == RTMA_ACT_SILU) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) u[j] = u[j] <= 0.f ? (act == RTMA_ACT_PRELU ? slope * u[j] : 0.f) : u[j];  // NaN stays NaN
-    } else if (act == RTMA_ACT_SILU) {
+        for (int i = 0; i < 4; ++i) u[i] = mul2(u[i], sigmoid2(u[i]));
+    } else if (act != RTMA_ACT_NONE) {  // slope: 0 for ReLU, and then 0 comes from a choice, so that -inf gives 0
 #pragma unroll
-        for (int j = 0; j < 8; ++j) u[j] = __fdividef(u[j], 1.f + __expf(-u[j]));
+        for (int i = 0; i < 4; ++i) {
+            float a, b;
+            unpack2(u[i], a, b);
+            a = a <= 0.f ? (act == RTMA_ACT_RELU ? 0.f : slope * a) : a;  // NaN stays NaN
+            b = b <= 0.f ? (act == RTMA_ACT_RELU ? 0.f : slope * b) : b;
+            u[i] = pack2(a, b);
+        }
     }
 }
 // d (holding dh) becomes du; returns the slope's gradient
-__device__ __forceinline__ float activate_back_eight(int act, float slope, const float (&u)[8], float (&d)[8]) {
+__device__ __forceinline__ float activate_back(int act, float slope, const f2 (&u)[4], f2 (&d)[4]) {
     float ds = 0.f;
-    if (act == RTMA_ACT_RELU) {
+    if (act == RTMA_ACT_SILU) {
+        const f2 one = pack2(1.f, 1.f), minus = pack2(-1.f, -1.f);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) d[j] = u[j] > 0.f ? d[j] : 0.f;
-    } else if (act == RTMA_ACT_PRELU) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if (!(u[j] > 0.f)) {
-                ds += d[j] * u[j];
-                d[j] *= slope;
-            }
+        for (int i = 0; i < 4; ++i) {
+            const f2 g = sigmoid2(u[i]);
+            d[i] = mul2(d[i], mul2(g, fma2(u[i], fma2(g, minus, one), one)));
         }
-    } else if (act == RTMA_ACT_SILU) {
+    } else if (act != RTMA_ACT_NONE) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float g = sigmoid(u[j]);
-            d[j] *= g * (1.f + u[j] * (1.f - g));
+        for (int i = 0; i < 4; ++i) {
+            float a, b, x, y;
+            unpack2(u[i], a, b);
+            unpack2(d[i], x, y);
+            if (!(a > 0.f)) {
+                ds = fmaf(x, act == RTMA_ACT_PRELU ? a : 0.f, ds);
+                x = act == RTMA_ACT_RELU ? 0.f : x * slope;
+            }
+            if (!(b > 0.f)) {
+                ds = fmaf(y, act == RTMA_ACT_PRELU ? b : 0.f, ds);
+                y = act == RTMA_ACT_RELU ? 0.f : y * slope;
+            }
+            d[i] = pack2(x, y);
         }
     }
     return ds;
 }
+
+// (x - mean) * rstd of a pair.  Rows of half the size: one multiplication and addition with -mean * rstd, whose rounding is far
+// below theirs; fp32 rows: the difference first, so that a mean much larger than the deviation costs no digits.
+template <class T>
+struct Standard {
+    f2 r, m;
+    __device__ __forceinline__ void set(float mean0, float rstd0, float mean1, float rstd1) {
+        r = pack2(rstd0, rstd1);
+        m = sizeof(T) == 2 ? pack2(-mean0 * rstd0, -mean1 * rstd1) : pack2(-mean0, -mean1);
+    }
+    __device__ __forceinline__ f2 operator()(f2 x) const { return sizeof(T) == 2 ? fma2(x, r, m) : mul2(add2(x, m), r); }
+};
 
 __device__ __forceinline__ uint32_t id_of(const NormArgs& a, int64_t r) {
     return a.drop.ids ? (uint32_t)__ldg(a.drop.ids + r) : (uint32_t)r;
@@ -94,6 +129,12 @@ struct Lane {
 __device__ __forceinline__ void load_params(const float* p, int64_t stride, int part, int u, int valid, float missing, float (&v)[8]) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = p && j < valid ? __ldg(p + part * stride + 8 * u + j) : (j < valid ? missing : 0.f);
+}
+__device__ __forceinline__ void load_params(const float* p, int64_t stride, int part, int u, int valid, float missing, f2 (&v)[4]) {
+    float x[8];
+    load_params(p, stride, part, u, valid, missing, x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = pack2(x[2 * i], x[2 * i + 1]);
 }
 
 // The lanes that share one set's sum: a power of two, so many that a block's threads cover `sets` sets.
@@ -172,40 +213,34 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_rows_kernel(const NormArgs 
                         v[j] = fmaf((v[j] - st.x) * st.y, gam[j], bet[j]);
                     }
                 }
-                activate_eight(a.act, slope, v);
-                if (a.drop.threshold) drop_eight(a.drop, a.drop.ids ? (uint32_t)__ldg(a.drop.ids + r) : (uint32_t)r, at.u, v);
-                store_eight(Y + r * a.ldy + 8 * at.u, v, at.valid, a.vy);
+                f2 w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1]);
+                activate(a.act, slope, w);
+                if (a.drop.threshold) drop_pairs(a.drop, id_of(a, r), at.u, w);
+                store_pairs(Y + r * a.ldy + 8 * at.u, w, at.valid, a.vy);
             }
         }
     }
 }
 
 // dh (in du) -> du and x (in xhat) -> xhat of eight channels; returns the slope's gradient
-__device__ __forceinline__ float back_values(const NormArgs& a, int64_t r, int u, const float (&mean)[8], const float (&rstd)[8], const float (&gam)[8],
-                                             const float (&bet)[8], float slope, float (&xhat)[8], float (&du)[8]) {
-    if (a.drop.threshold) drop_eight(a.drop, id_of(a, r), u, du);
-    float pre[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        xhat[j] = (xhat[j] - mean[j]) * rstd[j];
-        pre[j] = fmaf(xhat[j], gam[j], bet[j]);
-    }
-    return activate_back_eight(a.act, slope, pre, du);
-}
 template <class T>
-__device__ __forceinline__ float back_eight(const NormArgs& a, int64_t r, int u, int valid, const float (&mean)[8], const float (&rstd)[8],
-                                            const float (&gam)[8], const float (&bet)[8], float slope, float (&xhat)[8], float (&du)[8]) {
-    Eight<T> x, d;
-    x.load(static_cast<const T*>(a.X) + r * a.ldx + 8 * u, valid, a.vx);
-    d.load(static_cast<const T*>(a.dY) + r * a.lddy + 8 * u, valid, a.vdy);
-    x.values(xhat);
-    d.values(du);
-    return back_values(a, r, u, mean, rstd, gam, bet, slope, xhat, du);
+__device__ __forceinline__ float back(const NormArgs& a, int64_t r, int u, const Standard<T> (&st)[4], const f2 (&gam)[4], const f2 (&bet)[4],
+                                      float slope, f2 (&xhat)[4], f2 (&du)[4]) {
+    if (a.drop.threshold) drop_pairs(a.drop, id_of(a, r), u, du);
+    f2 pre[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        xhat[i] = st[i](xhat[i]);
+        pre[i] = fma2(xhat[i], gam[i], bet[i]);
+    }
+    return activate_back(a.act, slope, pre, du);
 }
 
 // Sums over a block's rows of (du, du xhat) of a thread's eight channels from c0 on, written to the tile's slot.  Threads pitch apart
 // hold the same channels, rows_at_once of them.
-__device__ __forceinline__ void leave_sums(const NormArgs& a, int tile, int c0, int y, int pitch, int rows_at_once, float (&sb)[8], float (&sg)[8], float* red) {
+__device__ __forceinline__ void leave_sums(const NormArgs& a, int tile, int c0, int y, int pitch, int rows_at_once, const f2 (&sb)[4], const f2 (&sg)[4], float* red) {
     int top = 1;
     while (top < rows_at_once) top <<= 1;
     float* out = a.partial + (int64_t)tile * (2 * a.C + 1);
@@ -213,7 +248,7 @@ __device__ __forceinline__ void leave_sums(const NormArgs& a, int tile, int c0, 
     for (int kind = 0; kind < 2; ++kind) {
         __syncthreads();
 #pragma unroll
-        for (int j = 0; j < 8; ++j) red[j * NORM_THREADS + threadIdx.x] = kind == 0 ? sb[j] : sg[j];
+        for (int i = 0; i < 4; ++i) unpack2(kind == 0 ? sb[i] : sg[i], red[2 * i * NORM_THREADS + threadIdx.x], red[(2 * i + 1) * NORM_THREADS + threadIdx.x]);
         for (int h = top >> 1; h > 0; h >>= 1) {
             __syncthreads();
             if (y < h && y + h < rows_at_once) {
@@ -278,7 +313,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_kernel(const N
     for (int p = 0; p < NP; ++p) valid[p] = max(0, min(8, a.C - 8 * (u + 32 * p)));
     for (int tile = blockIdx.x; tile < tile_start[a.G]; tile += gridDim.x) {
         const Run run(a, tile_start, tile);
-        float gam[NP][8], bet[NP][8];
+        f2 gam[NP][4], bet[NP][4];
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
             load_params(a.gamma, a.gamma_stride, run.part, u + 32 * p, valid[p], 1.f, gam[p]);
@@ -296,21 +331,18 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_kernel(const N
         };
         request(run.begin);
         for (int64_t r0 = run.begin; r0 < run.end; r0 += RB * rows_at_once) {  // the same number of times in every lane
-            float v[RB][NP][8], mean[RB][NP], rstd[RB][NP];
+            f2 v[RB][NP][4];
+            float mean[RB][NP], rstd[RB][NP];
 #pragma unroll
             for (int b = 0; b < RB; ++b)
 #pragma unroll
-                for (int p = 0; p < NP; ++p) raw[b][p].values(v[b][p]);
+                for (int p = 0; p < NP; ++p) pairs_of(raw[b][p], v[b][p]);
             request(r0 + RB * rows_at_once);
 #pragma unroll
             for (int b = 0; b < RB; ++b) {
 #pragma unroll
-                for (int p = 0; p < NP; ++p) {
-                    float s = 0.f;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) s += v[b][p][j];  // what is not there reads as zero
-                    mean[b][p] = s;
-                }
+                for (int p = 0; p < NP; ++p)  // what is not there reads as zero
+                    mean[b][p] = halves_sum(add2(add2(v[b][p][0], v[b][p][1]), add2(v[b][p][2], v[b][p][3])));
                 if (NP == 2 && whole) mean[b][0] += mean[b][NP - 1];
             }
 #pragma unroll
@@ -321,13 +353,20 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_kernel(const N
             for (int b = 0; b < RB; ++b) {
 #pragma unroll
                 for (int p = 0; p < NP; ++p) {
-                    float s = 0.f;
+                    const f2 minus = pack2(-mean[b][p], -mean[b][p]);
+                    f2 q = 0ull;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        v[b][p][j] = j < valid[p] ? v[b][p][j] - mean[b][p] : 0.f;
-                        s = fmaf(v[b][p][j], v[b][p][j], s);
+                    for (int i = 0; i < 4; ++i) {
+                        v[b][p][i] = add2(v[b][p][i], minus);
+                        f2 t = v[b][p][i];
+                        if (valid[p] < 8) {  // channels that are not there do not count
+                            float t0, t1;
+                            unpack2(t, t0, t1);
+                            t = pack2(2 * i < valid[p] ? t0 : 0.f, 2 * i + 1 < valid[p] ? t1 : 0.f);
+                        }
+                        q = fma2(t, t, q);
                     }
-                    rstd[b][p] = s;
+                    rstd[b][p] = halves_sum(q);
                 }
                 if (NP == 2 && whole) rstd[b][0] += rstd[b][NP - 1];
             }
@@ -346,11 +385,12 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_kernel(const N
                     if (valid[p] == 0) continue;
                     if (a.stats && (whole ? unit == 0 : (unit & (lanes - 1)) == 0))
                         *reinterpret_cast<float2*>(a.stats + 2 * (r * a.groups + (whole ? 0 : unit / lanes))) = make_float2(mean[b][p], rstd[b][p]);
+                    const f2 r2 = pack2(rstd[b][p], rstd[b][p]);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[b][p][j] = fmaf(v[b][p][j] * rstd[b][p], gam[p][j], bet[p][j]);
-                    activate_eight(a.act, slope, v[b][p]);
-                    if (a.drop.threshold) drop_eight(a.drop, id, unit, v[b][p]);
-                    store_eight(Y + r * a.ldy + 8 * unit, v[b][p], valid[p], a.vy);
+                    for (int i = 0; i < 4; ++i) v[b][p][i] = fma2(mul2(v[b][p][i], r2), gam[p][i], bet[p][i]);
+                    activate(a.act, slope, v[b][p]);
+                    if (a.drop.threshold) drop_pairs(a.drop, id, unit, v[b][p]);
+                    store_pairs(Y + r * a.ldy + 8 * unit, v[b][p], valid[p], a.vy);
                 }
             }
         }
@@ -375,13 +415,14 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_grad_kernel(co
     for (int p = 0; p < NP; ++p) valid[p] = max(0, min(8, a.C - 8 * (u + 32 * p)));
     for (int tile = blockIdx.x; tile < tile_start[a.G]; tile += gridDim.x) {
         const Run run(a, tile_start, tile);
-        float gam[NP][8], bet[NP][8], sb[NP][8], sg[NP][8], ds = 0.f;
+        f2 gam[NP][4], bet[NP][4], sb[NP][4], sg[NP][4];
+        float ds = 0.f;
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
             load_params(a.gamma, a.gamma_stride, run.part, u + 32 * p, valid[p], 1.f, gam[p]);
             load_params(a.beta, a.beta_stride, run.part, u + 32 * p, valid[p], 0.f, bet[p]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sb[p][j] = sg[p][j] = 0.f;
+            for (int i = 0; i < 4; ++i) sb[p][i] = sg[p][i] = 0ull;
         }
         const float slope = a.slope ? __ldg(a.slope + run.part * a.slope_stride) : 0.f;
         Eight<T> rx[RB][NP], rd[RB][NP];
@@ -401,15 +442,17 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_grad_kernel(co
         };
         request(run.begin);
         for (int64_t r0 = run.begin; r0 < run.end; r0 += RB * rows_at_once) {
-            float xh[RB][NP][8], du[RB][NP][8], s1[RB][NP], s2[RB][NP];
-            float2 st[RB][NP];
+            f2 xh[RB][NP][4], du[RB][NP][4];
+            float s1[RB][NP], s2[RB][NP], rstd[RB][NP];
+            Standard<T> st[RB][NP];
 #pragma unroll
             for (int b = 0; b < RB; ++b)
 #pragma unroll
                 for (int p = 0; p < NP; ++p) {
-                    rx[b][p].values(xh[b][p]);
-                    rd[b][p].values(du[b][p]);
-                    st[b][p] = rs[b][p];
+                    pairs_of(rx[b][p], xh[b][p]);
+                    pairs_of(rd[b][p], du[b][p]);
+                    st[b][p].set(rs[b][p].x, rs[b][p].y, rs[b][p].x, rs[b][p].y);
+                    rstd[b][p] = rs[b][p].y;
                 }
             request(r0 + RB * rows_at_once);
 #pragma unroll
@@ -418,25 +461,25 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_grad_kernel(co
                 const uint32_t id = a.drop.threshold && r < run.end ? id_of(a, r) : 0u;
 #pragma unroll
                 for (int p = 0; p < NP; ++p) {
-                    if (a.drop.threshold) drop_eight(a.drop, id, u + 32 * p, du[b][p]);
-                    float pre[8];
+                    if (a.drop.threshold) drop_pairs(a.drop, id, u + 32 * p, du[b][p]);
+                    f2 pre[4];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        xh[b][p][j] = (xh[b][p][j] - st[b][p].x) * st[b][p].y;
-                        pre[j] = fmaf(xh[b][p][j], gam[p][j], bet[p][j]);
+                    for (int i = 0; i < 4; ++i) {
+                        xh[b][p][i] = st[b][p](xh[b][p][i]);
+                        pre[i] = fma2(xh[b][p][i], gam[p][i], bet[p][i]);
                     }
-                    ds += activate_back_eight(a.act, slope, pre, du[b][p]);
-                    float t1 = 0.f, t2 = 0.f;
+                    ds += activate_back(a.act, slope, pre, du[b][p]);
+                    f2 t1 = 0ull, t2 = 0ull;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        sb[p][j] += du[b][p][j];
-                        sg[p][j] = fmaf(du[b][p][j], xh[b][p][j], sg[p][j]);
-                        du[b][p][j] *= gam[p][j];
-                        t1 += du[b][p][j];
-                        t2 = fmaf(du[b][p][j], xh[b][p][j], t2);
+                    for (int i = 0; i < 4; ++i) {
+                        sb[p][i] = add2(sb[p][i], du[b][p][i]);
+                        sg[p][i] = fma2(du[b][p][i], xh[b][p][i], sg[p][i]);
+                        du[b][p][i] = mul2(du[b][p][i], gam[p][i]);
+                        t1 = add2(t1, du[b][p][i]);
+                        t2 = fma2(du[b][p][i], xh[b][p][i], t2);
                     }
-                    s1[b][p] = t1;
-                    s2[b][p] = t2;
+                    s1[b][p] = halves_sum(t1);
+                    s2[b][p] = halves_sum(t2);
                 }
                 if (NP == 2 && whole) {
                     s1[b][0] += s1[b][NP - 1];
@@ -456,9 +499,10 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_grad_kernel(co
                 if (r >= run.end) continue;
 #pragma unroll
                 for (int p = 0; p < NP; ++p) {
+                    const f2 m1 = pack2(-s1[b][p], -s1[b][p]), m2 = pack2(-s2[b][p], -s2[b][p]), r2 = pack2(rstd[b][p], rstd[b][p]);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) du[b][p][j] = st[b][p].y * (du[b][p][j] - s1[b][p] - xh[b][p][j] * s2[b][p]);
-                    if (valid[p]) store_eight(Y + r * a.ldy + 8 * (u + 32 * p), du[b][p], valid[p], a.vy);
+                    for (int i = 0; i < 4; ++i) du[b][p][i] = mul2(r2, fma2(xh[b][p][i], m2, add2(du[b][p][i], m1)));
+                    if (valid[p]) store_pairs(Y + r * a.ldy + 8 * (u + 32 * p), du[b][p], valid[p], a.vy);
                 }
             }
         }
@@ -486,16 +530,18 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_rows_grad_kernel(const Norm
         part_rows(a.offsets, a.n, part, begin, end);
         begin += (int64_t)(tile - tile_start[part]) * a.tile_rows;
         end = min(end, begin + a.tile_rows);
-        float gam[8], bet[8], sb[8], sg[8], ds = 0.f;
+        f2 gam[4], bet[4], sb[4], sg[4];
+        float ds = 0.f;
         load_params(a.gamma, a.gamma_stride, part, at.u, at.valid, 1.f, gam);
         load_params(a.beta, a.beta_stride, part, at.u, at.valid, 0.f, bet);
         const float slope = a.slope ? __ldg(a.slope + part * a.slope_stride) : 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sb[j] = sg[j] = 0.f;
+        for (int i = 0; i < 4; ++i) sb[i] = sg[i] = 0ull;
         for (int64_t r0 = begin; r0 < end; r0 += a.rows_at_once) {
             const int64_t r = r0 + at.y;
             const bool here = at.active && r < end;
-            float xhat[8], du[8], rstd[8];
+            f2 xhat[4], du[4];
+            float rstd[8];
             if (here) {
                 float mean[8];
 #pragma unroll
@@ -504,13 +550,24 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_rows_grad_kernel(const Norm
                     mean[j] = st.x;
                     rstd[j] = st.y;
                 }
-                ds += back_eight<T>(a, r, at.u, at.valid, mean, rstd, gam, bet, slope, xhat, du);
+                Standard<T> st[4];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    sb[j] += du[j];
-                    sg[j] = fmaf(du[j], xhat[j], sg[j]);
-                    du[j] *= gam[j];
-                    vals[at.y * pitch + 8 * at.u + j] = make_float2(du[j], du[j] * xhat[j]);
+                for (int i = 0; i < 4; ++i) st[i].set(mean[2 * i], rstd[2 * i], mean[2 * i + 1], rstd[2 * i + 1]);
+                Eight<T> x, d;
+                x.load(static_cast<const T*>(a.X) + r * a.ldx + 8 * at.u, at.valid, a.vx);
+                d.load(static_cast<const T*>(a.dY) + r * a.lddy + 8 * at.u, at.valid, a.vdy);
+                pairs_of(x, xhat);
+                pairs_of(d, du);
+                ds += back<T>(a, r, at.u, st, gam, bet, slope, xhat, du);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    sb[i] = add2(sb[i], du[i]);
+                    sg[i] = fma2(du[i], xhat[i], sg[i]);
+                    du[i] = mul2(du[i], gam[i]);
+                    float t0, t1, q0, q1;
+                    unpack2(du[i], t0, t1);
+                    unpack2(mul2(du[i], xhat[i]), q0, q1);
+                    *reinterpret_cast<float4*>(&vals[at.y * pitch + 8 * at.u + 2 * i]) = make_float4(t0, q0, t1, q1);
                 }
             }
             __syncthreads();
@@ -532,14 +589,20 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_rows_grad_kernel(const Norm
             }
             __syncthreads();
             if (here) {
+                float t[8], x[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    unpack2(du[i], t[2 * i], t[2 * i + 1]);
+                    unpack2(xhat[i], x[2 * i], x[2 * i + 1]);
+                }
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     if (j < at.valid) {
                         const float2 st = stat[at.y * a.groups + (8 * at.u + j) / a.per_set];
-                        du[j] = rstd[j] * (du[j] - st.x - xhat[j] * st.y);
+                        t[j] = rstd[j] * (t[j] - st.x - x[j] * st.y);
                     }
                 }
-                store_eight(Y + r * a.ldy + 8 * at.u, du, at.valid, a.vy);
+                store_eight(Y + r * a.ldy + 8 * at.u, t, at.valid, a.vy);
             }
         }
         leave_sums(a, tile, 8 * at.u, at.active ? at.y : NORM_THREADS, a.units, a.rows_at_once, sb, sg, shared);
@@ -572,12 +635,14 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_stats_kernel(const NormA
         part_rows(a.offsets, a.n, part, begin, end);
         begin += (int64_t)(tile - tile_start[part]) * a.tile_rows;
         end = min(end, begin + a.tile_rows);
-        float mean[8], m2[8], count = 0.f;
+        f2 mean[4], m2[4];
+        float count = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) mean[j] = m2[j] = 0.f;
+        for (int i = 0; i < 4; ++i) mean[i] = m2[i] = 0ull;
         if (at.active) {
             int64_t r = begin + at.y;
             const int64_t step = BATCH * (int64_t)a.rows_at_once;
+            const f2 minus = pack2(-1.f, -1.f), part_of_batch = pack2(1.f / BATCH, 1.f / BATCH);
             Eight<T> x[BATCH];
             auto request = [&](int64_t from) {  // rows behind the last are not there
 #pragma unroll
@@ -588,44 +653,49 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_stats_kernel(const NormA
             for (; r + step - a.rows_at_once < end; r += step) {
                 // moments of the batch about its own mean, then joined to the thread's
                 const float share = BATCH / (count + BATCH), weight = count * share;
-                float v[BATCH][8];
+                const f2 share2 = pack2(share, share), weight2 = pack2(weight, weight);
+                f2 v[BATCH][4];
 #pragma unroll
-                for (int b = 0; b < BATCH; ++b) x[b].values(v[b]);
+                for (int b = 0; b < BATCH; ++b) pairs_of(x[b], v[b]);
                 request(r + step);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    float s = v[0][j];
+                for (int i = 0; i < 4; ++i) {
+                    f2 s = v[0][i];
 #pragma unroll
-                    for (int b = 1; b < BATCH; ++b) s += v[b][j];
-                    s *= 1.f / BATCH;
-                    float q = 0.f;
+                    for (int b = 1; b < BATCH; ++b) s = add2(s, v[b][i]);
+                    s = mul2(s, part_of_batch);
+                    f2 q = m2[i];
 #pragma unroll
-                    for (int b = 0; b < BATCH; ++b) q = fmaf(v[b][j] - s, v[b][j] - s, q);
-                    const float d = s - mean[j];
-                    mean[j] = fmaf(d, share, mean[j]);
-                    m2[j] += fmaf(d * d, weight, q);
+                    for (int b = 0; b < BATCH; ++b) {
+                        const f2 d = fma2(s, minus, v[b][i]);
+                        q = fma2(d, d, q);
+                    }
+                    const f2 d = fma2(mean[i], minus, s);
+                    mean[i] = fma2(d, share2, mean[i]);
+                    m2[i] = fma2(mul2(d, d), weight2, q);
                 }
                 count += BATCH;
             }
 #pragma unroll
             for (int b = 0; b < BATCH; ++b) {
                 if (r + b * a.rows_at_once >= end) break;
-                float v[8];
-                x[b].values(v);
+                f2 v[4];
+                pairs_of(x[b], v);
                 const float share = 1.f / (count + 1.f), weight = count * share;
+                const f2 share2 = pack2(share, share), weight2 = pack2(weight, weight);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float d = v[j] - mean[j];
-                    mean[j] = fmaf(d, share, mean[j]);
-                    m2[j] = fmaf(d * d, weight, m2[j]);
+                for (int i = 0; i < 4; ++i) {
+                    const f2 d = fma2(mean[i], minus, v[i]);
+                    mean[i] = fma2(d, share2, mean[i]);
+                    m2[i] = fma2(mul2(d, d), weight2, m2[i]);
                 }
                 count += 1.f;
             }
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            s_mean[j * NORM_THREADS + threadIdx.x] = mean[j];
-            s_m2[j * NORM_THREADS + threadIdx.x] = m2[j];
+        for (int i = 0; i < 4; ++i) {
+            unpack2(mean[i], s_mean[2 * i * NORM_THREADS + threadIdx.x], s_mean[(2 * i + 1) * NORM_THREADS + threadIdx.x]);
+            unpack2(m2[i], s_m2[2 * i * NORM_THREADS + threadIdx.x], s_m2[(2 * i + 1) * NORM_THREADS + threadIdx.x]);
         }
         s_count[threadIdx.x] = count;
         int top = 1;
@@ -715,6 +785,31 @@ __device__ __forceinline__ void load_part_stats(const NormArgs& a, int part, con
     }
 }
 
+// minus the mean, rstd gamma and beta of a thread's channels
+__device__ __forceinline__ void load_coefficients(const NormArgs& a, int part, const Lane& at, f2 (&minus_mean)[4], f2 (&scale)[4], f2 (&bet)[4], float (&rstd)[8]) {
+    float gam[8], mean[8];
+    load_params(a.gamma, a.gamma_stride, part, at.u, at.valid, 1.f, gam);
+    load_params(a.beta, a.beta_stride, part, at.u, at.valid, 0.f, bet);
+    load_part_stats(a, part, at, mean, rstd);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        minus_mean[i] = pack2(-mean[2 * i], -mean[2 * i + 1]);
+        scale[i] = pack2(rstd[2 * i] * gam[2 * i], rstd[2 * i + 1] * gam[2 * i + 1]);
+    }
+}
+// x (in t) -> x - mean, dh (in du) -> du; returns the slope's gradient
+__device__ __forceinline__ float back_centred(const NormArgs& a, int64_t r, int u, const f2 (&minus_mean)[4], const f2 (&scale)[4], const f2 (&bet)[4],
+                                              float slope, f2 (&t)[4], f2 (&du)[4]) {
+    if (a.drop.threshold) drop_pairs(a.drop, id_of(a, r), u, du);
+    f2 pre[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        t[i] = add2(t[i], minus_mean[i]);
+        pre[i] = fma2(t[i], scale[i], bet[i]);
+    }
+    return activate_back(a.act, slope, pre, du);
+}
+
 template <class T>
 __global__ void __launch_bounds__(NORM_THREADS, 2) norm_apply_kernel(const NormArgs a) {
     constexpr int RB = 4;  // rows in flight
@@ -731,10 +826,20 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_apply_kernel(const NormA
         part_rows(a.offsets, a.n, part, begin, end);
         begin += (int64_t)(tile - tile_start[part]) * a.tile_rows;
         end = min(end, begin + a.tile_rows);
-        float gam[8], bet[8], mean[8], rstd[8];
-        load_params(a.gamma, a.gamma_stride, part, at.u, at.valid, 1.f, gam);
-        load_params(a.beta, a.beta_stride, part, at.u, at.valid, 0.f, bet);
-        load_part_stats(a, part, at, mean, rstd);
+        f2 scale[4], shift[4], bias[4];  // u = x scale + shift (rows of half the size) or (x + shift) scale + bias: see Standard
+        {
+            float gam[8], bet[8], mean[8], rstd[8];
+            load_params(a.gamma, a.gamma_stride, part, at.u, at.valid, 1.f, gam);
+            load_params(a.beta, a.beta_stride, part, at.u, at.valid, 0.f, bet);
+            load_part_stats(a, part, at, mean, rstd);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float s0 = rstd[2 * i] * gam[2 * i], s1 = rstd[2 * i + 1] * gam[2 * i + 1];
+                scale[i] = pack2(s0, s1);
+                bias[i] = pack2(bet[2 * i], bet[2 * i + 1]);
+                shift[i] = sizeof(T) == 2 ? pack2(fmaf(-mean[2 * i], s0, bet[2 * i]), fmaf(-mean[2 * i + 1], s1, bet[2 * i + 1])) : pack2(-mean[2 * i], -mean[2 * i + 1]);
+            }
+        }
         const float slope = a.slope ? __ldg(a.slope + part * a.slope_stride) : 0.f;
         Eight<T> x[RB];
         auto request = [&](int64_t from, int b) {
@@ -748,14 +853,14 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_apply_kernel(const NormA
             for (int b = 0; b < RB; ++b) {
                 const int64_t row = r + b * a.rows_at_once;
                 if (row >= end) break;
-                float v[8];
-                x[b].values(v);
+                f2 v[4];
+                pairs_of(x[b], v);
                 request(r + RB * a.rows_at_once, b);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = fmaf((v[j] - mean[j]) * rstd[j], gam[j], bet[j]);
-                activate_eight(a.act, slope, v);
-                if (a.drop.threshold) drop_eight(a.drop, id_of(a, row), at.u, v);
-                store_eight(Y + row * a.ldy + 8 * at.u, v, at.valid, a.vy);
+                for (int i = 0; i < 4; ++i) v[i] = sizeof(T) == 2 ? fma2(v[i], scale[i], shift[i]) : fma2(add2(v[i], shift[i]), scale[i], bias[i]);
+                activate(a.act, slope, v);
+                if (a.drop.threshold) drop_pairs(a.drop, id_of(a, row), at.u, v);
+                store_pairs(Y + row * a.ldy + 8 * at.u, v, at.valid, a.vy);
             }
         }
     }
@@ -763,7 +868,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_apply_kernel(const NormA
 
 template <class T>
 __global__ void __launch_bounds__(NORM_THREADS, 2) norm_grad_sums_kernel(const NormArgs a) {
-    constexpr int RB = 8 / sizeof(T);  // rows in flight
+    constexpr int RB = 2;  // rows in flight
     __shared__ float shared[8 * NORM_THREADS];
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
     wait_for_kernel_before();
@@ -775,13 +880,13 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_grad_sums_kernel(const N
         part_rows(a.offsets, a.n, part, begin, end);
         begin += (int64_t)(tile - tile_start[part]) * a.tile_rows;
         end = min(end, begin + a.tile_rows);
-        float gam[8], bet[8], mean[8], rstd[8], sb[8], sg[8], ds = 0.f;
-        load_params(a.gamma, a.gamma_stride, part, at.u, at.valid, 1.f, gam);
-        load_params(a.beta, a.beta_stride, part, at.u, at.valid, 0.f, bet);
-        load_part_stats(a, part, at, mean, rstd);
+        // u = (x - mean) scale + beta; the sum of du xhat is rstd times that of du (x - mean)
+        f2 minus_mean[4], scale[4], bet[4], sb[4], sg[4];
+        float rstd[8], ds = 0.f;
+        load_coefficients(a, part, at, minus_mean, scale, bet, rstd);
         const float slope = a.slope ? __ldg(a.slope + part * a.slope_stride) : 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sb[j] = sg[j] = 0.f;
+        for (int i = 0; i < 4; ++i) sb[i] = sg[i] = 0ull;
         if (at.active) {
             Eight<T> x[RB], d[RB];
             auto request = [&](int64_t from, int b) {
@@ -796,19 +901,21 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_grad_sums_kernel(const N
                 for (int b = 0; b < RB; ++b) {
                     const int64_t row = r + b * a.rows_at_once;
                     if (row >= end) break;
-                    float xhat[8], du[8];
-                    x[b].values(xhat);
-                    d[b].values(du);
+                    f2 t[4], du[4];
+                    pairs_of(x[b], t);
+                    pairs_of(d[b], du);
                     request(r + RB * a.rows_at_once, b);
-                    ds += back_values(a, row, at.u, mean, rstd, gam, bet, slope, xhat, du);
+                    ds += back_centred(a, row, at.u, minus_mean, scale, bet, slope, t, du);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        sb[j] += du[j];
-                        sg[j] = fmaf(du[j], xhat[j], sg[j]);
+                    for (int i = 0; i < 4; ++i) {
+                        sb[i] = add2(sb[i], du[i]);
+                        sg[i] = fma2(du[i], t[i], sg[i]);
                     }
                 }
             }
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sg[i] = mul2(sg[i], pack2(rstd[2 * i], rstd[2 * i + 1]));
         leave_sums(a, tile, 8 * at.u, at.active ? at.y : NORM_THREADS, a.units, a.rows_at_once, sb, sg, shared);
         leave_slope(a, tile, ds, shared);
     }
@@ -816,7 +923,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_grad_sums_kernel(const N
 
 template <class T>
 __global__ void __launch_bounds__(NORM_THREADS, 2) norm_grad_apply_kernel(const NormArgs a) {
-    constexpr int RB = 8 / sizeof(T);
+    constexpr int RB = 2;
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
     __shared__ float2 of_set[NORM_MAX_CHANNELS];
     wait_for_kernel_before();
@@ -848,17 +955,20 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_grad_apply_kernel(const 
             if (set < a.groups && l == 0) of_set[set] = make_float2(s1 * inv, s2 * inv);
         }
         __syncthreads();
-        float gam[8], bet[8], mean[8], rstd[8], m1[8], m2[8];
-        load_params(a.gamma, a.gamma_stride, part, at.u, at.valid, 1.f, gam);
-        load_params(a.beta, a.beta_stride, part, at.u, at.valid, 0.f, bet);
-        load_part_stats(a, part, at, mean, rstd);
-        const float slope = a.slope ? __ldg(a.slope + part * a.slope_stride) : 0.f;
+        // dx = rstd (gamma du - S1 / m) - (x - mean) rstd^2 S2 / m
+        f2 minus_mean[4], scale[4], bet[4], m1[4], m2[4];
+        {
+            float rstd[8];
+            load_coefficients(a, part, at, minus_mean, scale, bet, rstd);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float2 s = j < at.valid ? of_set[(8 * at.u + j) / a.per_set] : make_float2(0.f, 0.f);
-            m1[j] = s.x;
-            m2[j] = s.y;
+            for (int i = 0; i < 4; ++i) {
+                const float2 s0 = 2 * i < at.valid ? of_set[(8 * at.u + 2 * i) / a.per_set] : make_float2(0.f, 0.f);
+                const float2 s1 = 2 * i + 1 < at.valid ? of_set[(8 * at.u + 2 * i + 1) / a.per_set] : make_float2(0.f, 0.f);
+                m1[i] = pack2(-rstd[2 * i] * s0.x, -rstd[2 * i + 1] * s1.x);
+                m2[i] = pack2(-rstd[2 * i] * rstd[2 * i] * s0.y, -rstd[2 * i + 1] * rstd[2 * i + 1] * s1.y);
+            }
         }
+        const float slope = a.slope ? __ldg(a.slope + part * a.slope_stride) : 0.f;
         if (at.active) {
             Eight<T> x[RB], d[RB];
             auto request = [&](int64_t from, int b) {
@@ -873,14 +983,14 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_grad_apply_kernel(const 
                 for (int b = 0; b < RB; ++b) {
                     const int64_t row = r + b * a.rows_at_once;
                     if (row >= end) break;
-                    float xhat[8], du[8];
-                    x[b].values(xhat);
-                    d[b].values(du);
+                    f2 t[4], du[4];
+                    pairs_of(x[b], t);
+                    pairs_of(d[b], du);
                     request(r + RB * a.rows_at_once, b);
-                    back_values(a, row, at.u, mean, rstd, gam, bet, slope, xhat, du);
+                    back_centred(a, row, at.u, minus_mean, scale, bet, slope, t, du);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) du[j] = rstd[j] * (fmaf(gam[j], du[j], -m1[j]) - xhat[j] * m2[j]);
-                    store_eight(Y + row * a.ldy + 8 * at.u, du, at.valid, a.vy);
+                    for (int i = 0; i < 4; ++i) du[i] = fma2(t[i], m2[i], fma2(du[i], scale[i], m1[i]));
+                    store_pairs(Y + row * a.ldy + 8 * at.u, du, at.valid, a.vy);
                 }
             }
         }

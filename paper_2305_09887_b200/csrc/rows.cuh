@@ -177,6 +177,51 @@ __device__ __forceinline__ void store_eight(T* p, const float (&v)[8], int valid
     }
 }
 
+// ---- two fp32 numbers per instruction -------------------------------------------------------------
+typedef unsigned long long f2;  // the lower half first
+__device__ __forceinline__ f2 pack2(float a, float b) {
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(f2 x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+    f2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+    f2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+    f2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ float halves_sum(f2 x) {
+    float a, b;
+    unpack2(x, a, b);
+    return a + b;
+}
+
+// Eight values as four pairs.
+template <class T>
+__device__ __forceinline__ void pairs_of(const Eight<T>& e, f2 (&v)[4]) {
+    float x[8];
+    e.values(x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = pack2(x[2 * i], x[2 * i + 1]);
+}
+template <class T>
+__device__ __forceinline__ void store_pairs(T* p, const f2 (&v)[4], int valid, int granule) {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpack2(v[i], x[2 * i], x[2 * i + 1]);
+    store_eight(p, x, valid, granule);
+}
+
 // ---- parts ----------------------------------------------------------------------------------------
 // Rows of part g: [offsets[g], offsets[g + 1]) cut to [0, n), so that offsets that are no offsets reach no memory outside the
 // rows.  offsets == NULL: one part of all rows.  span: that many parts as one.
@@ -260,5 +305,13 @@ __device__ __forceinline__ void drop_eight(const DropArgs& d, uint32_t id, uint3
         v[4 * q + 2] = (hi & 0xFFFFu) >= d.threshold ? v[4 * q + 2] * d.scale : 0.f;
         v[4 * q + 3] = (hi >> 16) >= d.threshold ? v[4 * q + 3] * d.scale : 0.f;
     }
+}
+__device__ __forceinline__ void drop_pairs(const DropArgs& d, uint32_t id, uint32_t unit, f2 (&v)[4]) {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpack2(v[i], x[2 * i], x[2 * i + 1]);
+    drop_eight(d, id, unit, x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = pack2(x[2 * i], x[2 * i + 1]);
 }
 #endif
