@@ -276,6 +276,12 @@ __device__ __forceinline__ void leave_slope(const NormArgs& a, int tile, float d
     __syncthreads();
 }
 
+// 1 / sqrt(x) for x >= eps > 0: the approximation and a Newton step, within a unit in the last place
+__device__ __forceinline__ float inverse_root(float x) {
+    const float y = rsqrtf(x);
+    return y * fmaf(-0.5f * x * y, y, 1.5f);
+}
+
 // A run of rows of one part.
 struct Run {
     int part;
@@ -297,14 +303,14 @@ __device__ __forceinline__ float set_sum(float x, int lanes) {
     return x;
 }
 
-template <class T, int NP, int RB>
+template <class T, int NP, int RB, bool FULL>
 __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_kernel(const NormArgs a) {
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
     wait_for_kernel_before();
     number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums);
     const int pitch = a.pitch, u = threadIdx.x & (pitch - 1), y = threadIdx.x / pitch, rows_at_once = NORM_THREADS / pitch;
     const bool whole = a.groups == 1;
-    const int lanes = whole ? pitch : a.per_set / 8;  // of a set
+    const int lanes = whole ? pitch : a.per_set / 8, lanes_log = 31 - __clz(lanes);  // of a set
     const float inv = 1.f / (float)a.per_set;
     const T* X = static_cast<const T*>(a.X);
     T* Y = static_cast<T*>(a.Y);
@@ -321,23 +327,29 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_kernel(const N
         }
         const float slope = a.slope ? __ldg(a.slope + run.part * a.slope_stride) : 0.f;
         Eight<T> raw[RB][NP];  // the next rows are on their way while these are worked on
-        auto request = [&](int64_t r0) {
+        int left = (int)(run.end - run.begin), asked = left - y;  // rows from this step's first on; from this lane's next request on
+        const T* x = X + (run.begin + y) * a.ldx + 8 * u;
+        T* out = Y + (run.begin + y) * a.ldy + 8 * u;
+        int64_t r = run.begin + y;
+        const int64_t x_step = rows_at_once * a.ldx, out_step = rows_at_once * a.ldy;
+        auto request = [&]() {
 #pragma unroll
             for (int b = 0; b < RB; ++b) {
-                const int64_t r = r0 + y + b * rows_at_once;
 #pragma unroll
-                for (int p = 0; p < NP; ++p) raw[b][p].load(X + r * a.ldx + 8 * (u + 32 * p), r < run.end ? valid[p] : 0, a.vx);
+                for (int p = 0; p < NP; ++p) load_unit<FULL>(raw[b][p], x + 256 * p, b * rows_at_once < asked, valid[p], a.vx);
+                x += x_step;
             }
+            asked -= RB * rows_at_once;
         };
-        request(run.begin);
-        for (int64_t r0 = run.begin; r0 < run.end; r0 += RB * rows_at_once) {  // the same number of times in every lane
+        request();
+        for (; left > 0; left -= RB * rows_at_once) {  // the same number of times in every lane
             f2 v[RB][NP][4];
             float mean[RB][NP], rstd[RB][NP];
 #pragma unroll
             for (int b = 0; b < RB; ++b)
 #pragma unroll
                 for (int p = 0; p < NP; ++p) pairs_of(raw[b][p], v[b][p]);
-            request(r0 + RB * rows_at_once);
+            request();
 #pragma unroll
             for (int b = 0; b < RB; ++b) {
 #pragma unroll
@@ -359,7 +371,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_kernel(const N
                     for (int i = 0; i < 4; ++i) {
                         v[b][p][i] = add2(v[b][p][i], minus);
                         f2 t = v[b][p][i];
-                        if (valid[p] < 8) {  // channels that are not there do not count
+                        if (!FULL && valid[p] < 8) {  // channels that are not there do not count
                             float t0, t1;
                             unpack2(t, t0, t1);
                             t = pack2(2 * i < valid[p] ? t0 : 0.f, 2 * i + 1 < valid[p] ? t1 : 0.f);
@@ -373,31 +385,30 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_kernel(const N
 #pragma unroll
             for (int b = 0; b < RB; ++b)
 #pragma unroll
-                for (int p = 0; p < NP; ++p) rstd[b][p] = p && whole ? rstd[b][0] : 1.f / sqrtf(set_sum(rstd[b][p], lanes) * inv + a.eps);
+                for (int p = 0; p < NP; ++p) rstd[b][p] = p && whole ? rstd[b][0] : inverse_root(set_sum(rstd[b][p], lanes) * inv + a.eps);
 #pragma unroll
-            for (int b = 0; b < RB; ++b) {
-                const int64_t r = r0 + y + b * rows_at_once;
-                if (r >= run.end) continue;
+            for (int b = 0; b < RB; ++b, out += out_step, r += rows_at_once) {
+                if (y + b * rows_at_once >= left) continue;
                 const uint32_t id = a.drop.threshold ? id_of(a, r) : 0u;
 #pragma unroll
                 for (int p = 0; p < NP; ++p) {
                     const int unit = u + 32 * p;
-                    if (valid[p] == 0) continue;
+                    if (!FULL && valid[p] == 0) continue;
                     if (a.stats && (whole ? unit == 0 : (unit & (lanes - 1)) == 0))
-                        *reinterpret_cast<float2*>(a.stats + 2 * (r * a.groups + (whole ? 0 : unit / lanes))) = make_float2(mean[b][p], rstd[b][p]);
+                        *reinterpret_cast<float2*>(a.stats + 2 * (r * a.groups + (whole ? 0 : unit >> lanes_log))) = make_float2(mean[b][p], rstd[b][p]);
                     const f2 r2 = pack2(rstd[b][p], rstd[b][p]);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) v[b][p][i] = fma2(mul2(v[b][p][i], r2), gam[p][i], bet[p][i]);
                     activate(a.act, slope, v[b][p]);
                     if (a.drop.threshold) drop_pairs(a.drop, id, unit, v[b][p]);
-                    store_pairs(Y + r * a.ldy + 8 * unit, v[b][p], valid[p], a.vy);
+                    store_unit<FULL>(out + 256 * p, v[b][p], valid[p], a.vy);
                 }
             }
         }
     }
 }
 
-template <class T, int NP, int RB>
+template <class T, int NP, int RB, bool FULL>
 __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_grad_kernel(const NormArgs a) {
     __shared__ float shared[8 * NORM_THREADS];
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
@@ -405,7 +416,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_grad_kernel(co
     number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums);
     const int pitch = a.pitch, u = threadIdx.x & (pitch - 1), y = threadIdx.x / pitch, rows_at_once = NORM_THREADS / pitch;
     const bool whole = a.groups == 1;
-    const int lanes = whole ? pitch : a.per_set / 8;
+    const int lanes = whole ? pitch : a.per_set / 8, lanes_log = 31 - __clz(lanes);
     const float inv = 1.f / (float)a.per_set;
     const T* X = static_cast<const T*>(a.X);
     const T* dY = static_cast<const T*>(a.dY);
@@ -427,21 +438,32 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_grad_kernel(co
         const float slope = a.slope ? __ldg(a.slope + run.part * a.slope_stride) : 0.f;
         Eight<T> rx[RB][NP], rd[RB][NP];
         float2 rs[RB][NP];
-        auto request = [&](int64_t r0) {
+        int left = (int)(run.end - run.begin), asked = left - y;
+        const T* x = X + (run.begin + y) * a.ldx + 8 * u;
+        const T* dy = dY + (run.begin + y) * a.lddy + 8 * u;
+        const float* stat = a.stats + 2 * ((run.begin + y) * a.groups + (whole ? 0 : u >> lanes_log));
+        T* out = Y + (run.begin + y) * a.ldy + 8 * u;
+        int64_t r = run.begin + y;
+        const int64_t x_step = rows_at_once * a.ldx, dy_step = rows_at_once * a.lddy, out_step = rows_at_once * a.ldy;
+        const int stat_step = 2 * rows_at_once * a.groups;
+        auto request = [&]() {
 #pragma unroll
             for (int b = 0; b < RB; ++b) {
-                const int64_t r = r0 + y + b * rows_at_once;
+                const bool here = b * rows_at_once < asked;
 #pragma unroll
                 for (int p = 0; p < NP; ++p) {
-                    const int here = r < run.end ? valid[p] : 0;
-                    rx[b][p].load(X + r * a.ldx + 8 * (u + 32 * p), here, a.vx);
-                    rd[b][p].load(dY + r * a.lddy + 8 * (u + 32 * p), here, a.vdy);
-                    rs[b][p] = here ? *reinterpret_cast<const float2*>(a.stats + 2 * (r * a.groups + (whole ? 0 : (u + 32 * p) / lanes))) : make_float2(0.f, 0.f);
+                    load_unit<FULL>(rx[b][p], x + 256 * p, here, valid[p], a.vx);
+                    load_unit<FULL>(rd[b][p], dy + 256 * p, here, valid[p], a.vdy);
+                    rs[b][p] = here && (FULL || valid[p]) ? *reinterpret_cast<const float2*>(stat + (whole ? 0 : 2 * (32 >> lanes_log) * p)) : make_float2(0.f, 0.f);
                 }
+                x += x_step;
+                dy += dy_step;
+                stat += stat_step;
             }
+            asked -= RB * rows_at_once;
         };
-        request(run.begin);
-        for (int64_t r0 = run.begin; r0 < run.end; r0 += RB * rows_at_once) {
+        request();
+        for (; left > 0; left -= RB * rows_at_once) {
             f2 xh[RB][NP][4], du[RB][NP][4];
             float s1[RB][NP], s2[RB][NP], rstd[RB][NP];
             Standard<T> st[RB][NP];
@@ -454,11 +476,10 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_grad_kernel(co
                     st[b][p].set(rs[b][p].x, rs[b][p].y, rs[b][p].x, rs[b][p].y);
                     rstd[b][p] = rs[b][p].y;
                 }
-            request(r0 + RB * rows_at_once);
+            request();
 #pragma unroll
             for (int b = 0; b < RB; ++b) {
-                const int64_t r = r0 + y + b * rows_at_once;
-                const uint32_t id = a.drop.threshold && r < run.end ? id_of(a, r) : 0u;
+                const uint32_t id = a.drop.threshold && y + b * rows_at_once < left ? id_of(a, r + b * rows_at_once) : 0u;
 #pragma unroll
                 for (int p = 0; p < NP; ++p) {
                     if (a.drop.threshold) drop_pairs(a.drop, id, u + 32 * p, du[b][p]);
@@ -494,15 +515,14 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_grad_kernel(co
                     s2[b][p] = p && whole ? s2[b][0] : set_sum(s2[b][p], lanes) * inv;
                 }
 #pragma unroll
-            for (int b = 0; b < RB; ++b) {
-                const int64_t r = r0 + y + b * rows_at_once;
-                if (r >= run.end) continue;
+            for (int b = 0; b < RB; ++b, out += out_step, r += rows_at_once) {
+                if (y + b * rows_at_once >= left) continue;
 #pragma unroll
                 for (int p = 0; p < NP; ++p) {
                     const f2 m1 = pack2(-s1[b][p], -s1[b][p]), m2 = pack2(-s2[b][p], -s2[b][p]), r2 = pack2(rstd[b][p], rstd[b][p]);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) du[b][p][i] = mul2(r2, fma2(xh[b][p][i], m2, add2(du[b][p][i], m1)));
-                    if (valid[p]) store_pairs(Y + r * a.ldy + 8 * (u + 32 * p), du[b][p], valid[p], a.vy);
+                    if (FULL || valid[p]) store_unit<FULL>(out + 256 * p, du[b][p], valid[p], a.vy);
                 }
             }
         }
@@ -619,8 +639,8 @@ __device__ __forceinline__ void join_moments(float& mean, float& m2, float n, fl
 }
 
 // Mean and sum of squared differences of every set within a tile.
-template <class T>
-__global__ void __launch_bounds__(NORM_THREADS, 2) norm_stats_kernel(const NormArgs a) {
+template <class T, bool FULL>
+__global__ void __launch_bounds__(NORM_THREADS, FULL ? 3 : 2) norm_stats_kernel(const NormArgs a) {
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
     __shared__ float s_mean[8 * NORM_THREADS], s_m2[8 * NORM_THREADS], s_count[NORM_THREADS];
     wait_for_kernel_before();
@@ -644,12 +664,15 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_stats_kernel(const NormA
             const int64_t step = BATCH * (int64_t)a.rows_at_once;
             const f2 minus = pack2(-1.f, -1.f), part_of_batch = pack2(1.f / BATCH, 1.f / BATCH);
             Eight<T> x[BATCH];
-            auto request = [&](int64_t from) {  // rows behind the last are not there
+            int asked = (int)(end - r);
+            const T* from = X + r * a.ldx + 8 * at.u;
+            const int64_t x_step = a.rows_at_once * a.ldx;
+            auto request = [&]() {  // rows behind the last are not there
 #pragma unroll
-                for (int b = 0; b < BATCH; ++b)
-                    x[b].load(X + (from + b * a.rows_at_once) * a.ldx + 8 * at.u, from + b * a.rows_at_once < end ? at.valid : 0, a.vx);
+                for (int b = 0; b < BATCH; ++b, from += x_step) load_unit<FULL>(x[b], from, b * a.rows_at_once < asked, at.valid, a.vx);
+                asked -= BATCH * a.rows_at_once;
             };
-            request(r);
+            request();
             for (; r + step - a.rows_at_once < end; r += step) {
                 // moments of the batch about its own mean, then joined to the thread's
                 const float share = BATCH / (count + BATCH), weight = count * share;
@@ -657,7 +680,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_stats_kernel(const NormA
                 f2 v[BATCH][4];
 #pragma unroll
                 for (int b = 0; b < BATCH; ++b) pairs_of(x[b], v[b]);
-                request(r + step);
+                request();
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     f2 s = v[0][i];
@@ -810,9 +833,9 @@ __device__ __forceinline__ float back_centred(const NormArgs& a, int64_t r, int 
     return activate_back(a.act, slope, pre, du);
 }
 
-template <class T>
-__global__ void __launch_bounds__(NORM_THREADS, 2) norm_apply_kernel(const NormArgs a) {
-    constexpr int RB = 4;  // rows in flight
+template <class T, bool FULL>
+__global__ void __launch_bounds__(NORM_THREADS, FULL ? 3 : 2) norm_apply_kernel(const NormArgs a) {
+    constexpr int RB = 8 / sizeof(T);  // rows in flight
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
     wait_for_kernel_before();
     number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums);
@@ -842,31 +865,37 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_apply_kernel(const NormA
         }
         const float slope = a.slope ? __ldg(a.slope + part * a.slope_stride) : 0.f;
         Eight<T> x[RB];
-        auto request = [&](int64_t from, int b) {
-            const int64_t row = from + b * a.rows_at_once;
-            x[b].load(X + row * a.ldx + 8 * at.u, row < end ? at.valid : 0, a.vx);
+        int64_t row = begin + at.y;
+        int left = (int)(end - row), asked = left;
+        const T* from = X + row * a.ldx + 8 * at.u;
+        T* out = Y + row * a.ldy + 8 * at.u;
+        const int64_t x_step = a.rows_at_once * a.ldx, out_step = a.rows_at_once * a.ldy;
+        auto request = [&](int b) {
+            load_unit<FULL>(x[b], from, asked > 0, at.valid, a.vx);
+            from += x_step;
+            asked -= a.rows_at_once;
         };
 #pragma unroll
-        for (int b = 0; b < RB; ++b) request(begin + at.y, b);
-        for (int64_t r = begin + at.y; r < end; r += RB * a.rows_at_once) {
+        for (int b = 0; b < RB; ++b) request(b);
+        while (left > 0) {
 #pragma unroll
-            for (int b = 0; b < RB; ++b) {
-                const int64_t row = r + b * a.rows_at_once;
-                if (row >= end) break;
+            for (int b = 0; b < RB; ++b, row += a.rows_at_once, out += out_step) {
+                if (left <= 0) break;
+                left -= a.rows_at_once;
                 f2 v[4];
                 pairs_of(x[b], v);
-                request(r + RB * a.rows_at_once, b);
+                request(b);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[i] = sizeof(T) == 2 ? fma2(v[i], scale[i], shift[i]) : fma2(add2(v[i], shift[i]), scale[i], bias[i]);
                 activate(a.act, slope, v);
                 if (a.drop.threshold) drop_pairs(a.drop, id_of(a, row), at.u, v);
-                store_pairs(Y + row * a.ldy + 8 * at.u, v, at.valid, a.vy);
+                store_unit<FULL>(out, v, at.valid, a.vy);
             }
         }
     }
 }
 
-template <class T>
+template <class T, bool FULL>
 __global__ void __launch_bounds__(NORM_THREADS, 2) norm_grad_sums_kernel(const NormArgs a) {
     constexpr int RB = 2;  // rows in flight
     __shared__ float shared[8 * NORM_THREADS];
@@ -889,22 +918,29 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_grad_sums_kernel(const N
         for (int i = 0; i < 4; ++i) sb[i] = sg[i] = 0ull;
         if (at.active) {
             Eight<T> x[RB], d[RB];
-            auto request = [&](int64_t from, int b) {
-                const int64_t row = from + b * a.rows_at_once;
-                x[b].load(static_cast<const T*>(a.X) + row * a.ldx + 8 * at.u, row < end ? at.valid : 0, a.vx);
-                d[b].load(static_cast<const T*>(a.dY) + row * a.lddy + 8 * at.u, row < end ? at.valid : 0, a.vdy);
+            int64_t row = begin + at.y;
+            int left = (int)(end - row), asked = left;
+            const T* from = static_cast<const T*>(a.X) + row * a.ldx + 8 * at.u;
+            const T* d_from = static_cast<const T*>(a.dY) + row * a.lddy + 8 * at.u;
+            const int64_t x_step = a.rows_at_once * a.ldx, d_step = a.rows_at_once * a.lddy;
+            auto request = [&](int b) {
+                load_unit<FULL>(x[b], from, asked > 0, at.valid, a.vx);
+                load_unit<FULL>(d[b], d_from, asked > 0, at.valid, a.vdy);
+                from += x_step;
+                d_from += d_step;
+                asked -= a.rows_at_once;
             };
 #pragma unroll
-            for (int b = 0; b < RB; ++b) request(begin + at.y, b);
-            for (int64_t r = begin + at.y; r < end; r += RB * a.rows_at_once) {
+            for (int b = 0; b < RB; ++b) request(b);
+            while (left > 0) {
 #pragma unroll
-                for (int b = 0; b < RB; ++b) {
-                    const int64_t row = r + b * a.rows_at_once;
-                    if (row >= end) break;
+                for (int b = 0; b < RB; ++b, row += a.rows_at_once) {
+                    if (left <= 0) break;
+                    left -= a.rows_at_once;
                     f2 t[4], du[4];
                     pairs_of(x[b], t);
                     pairs_of(d[b], du);
-                    request(r + RB * a.rows_at_once, b);
+                    request(b);
                     ds += back_centred(a, row, at.u, minus_mean, scale, bet, slope, t, du);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -921,7 +957,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_grad_sums_kernel(const N
     }
 }
 
-template <class T>
+template <class T, bool FULL>
 __global__ void __launch_bounds__(NORM_THREADS, 2) norm_grad_apply_kernel(const NormArgs a) {
     constexpr int RB = 2;
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
@@ -971,26 +1007,34 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_grad_apply_kernel(const 
         const float slope = a.slope ? __ldg(a.slope + part * a.slope_stride) : 0.f;
         if (at.active) {
             Eight<T> x[RB], d[RB];
-            auto request = [&](int64_t from, int b) {
-                const int64_t row = from + b * a.rows_at_once;
-                x[b].load(static_cast<const T*>(a.X) + row * a.ldx + 8 * at.u, row < end ? at.valid : 0, a.vx);
-                d[b].load(static_cast<const T*>(a.dY) + row * a.lddy + 8 * at.u, row < end ? at.valid : 0, a.vdy);
+            int64_t row = begin + at.y;
+            int left = (int)(end - row), asked = left;
+            const T* from = static_cast<const T*>(a.X) + row * a.ldx + 8 * at.u;
+            const T* d_from = static_cast<const T*>(a.dY) + row * a.lddy + 8 * at.u;
+            T* out = Y + row * a.ldy + 8 * at.u;
+            const int64_t x_step = a.rows_at_once * a.ldx, d_step = a.rows_at_once * a.lddy, out_step = a.rows_at_once * a.ldy;
+            auto request = [&](int b) {
+                load_unit<FULL>(x[b], from, asked > 0, at.valid, a.vx);
+                load_unit<FULL>(d[b], d_from, asked > 0, at.valid, a.vdy);
+                from += x_step;
+                d_from += d_step;
+                asked -= a.rows_at_once;
             };
 #pragma unroll
-            for (int b = 0; b < RB; ++b) request(begin + at.y, b);
-            for (int64_t r = begin + at.y; r < end; r += RB * a.rows_at_once) {
+            for (int b = 0; b < RB; ++b) request(b);
+            while (left > 0) {
 #pragma unroll
-                for (int b = 0; b < RB; ++b) {
-                    const int64_t row = r + b * a.rows_at_once;
-                    if (row >= end) break;
+                for (int b = 0; b < RB; ++b, row += a.rows_at_once, out += out_step) {
+                    if (left <= 0) break;
+                    left -= a.rows_at_once;
                     f2 t[4], du[4];
                     pairs_of(x[b], t);
                     pairs_of(d[b], du);
-                    request(r + RB * a.rows_at_once, b);
+                    request(b);
                     back_centred(a, row, at.u, minus_mean, scale, bet, slope, t, du);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) du[i] = fma2(t[i], m2[i], fma2(du[i], scale[i], m1[i]));
-                    store_pairs(Y + row * a.ldy + 8 * at.u, du, at.valid, a.vy);
+                    store_unit<FULL>(out, du, at.valid, a.vy);
                 }
             }
         }
@@ -1039,7 +1083,14 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_reduce_parts_kernel(const N
 
 template <class K>
 K by_type(int32_t dtype, K f32, K bf16, K f16) { return dtype == RTMA_F32 ? f32 : dtype == RTMA_BF16 ? bf16 : f16; }
-#define NORM_KERNEL(name) by_type(d->dtype, &name<float>, &name<__nv_bfloat16>, &name<__half>)
+#define NORM_KERNEL(name, ...) by_type(d->dtype, &name<float __VA_ARGS__>, &name<__nv_bfloat16 __VA_ARGS__>, &name<__half __VA_ARGS__>)
+
+// Whether every unit of eight channels is there in full, on the boundary of one load: then no load or store asks.
+bool full_units(const NormArgs& a, int32_t dtype, bool gradient) {
+    const int most = dtype == RTMA_F32 ? 32 : 16;
+    const bool pieces = a.pitch == 0 || (a.units & (a.units - 1)) == 0;  // no lane of a row is idle
+    return a.C % 8 == 0 && pieces && a.vx >= most && a.vy >= most && (!gradient || a.vdy >= most);
+}
 
 int32_t check_norm(rtma_ctx* ctx, const char* who, const rtma_norm_desc* d, int64_t n, int32_t G, const int64_t* offsets, const float* slope) {
     if (!d) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: null descriptor", who);
@@ -1115,9 +1166,10 @@ extern "C" int32_t rtma_group_norm(rtma_ctx* ctx, const rtma_norm_desc* d, int64
     const unsigned grid = (unsigned)tiles;
     if (rows) {
         const size_t smem = sizeof(float) * a.rows_at_once * (8 * a.units + 2 * (size_t)a.groups);
-        auto kernel = a.pitch && a.units <= 32 ? by_type(d->dtype, &norm_warp_rows_kernel<float, 1, 4>, &norm_warp_rows_kernel<__nv_bfloat16, 1, 4>, &norm_warp_rows_kernel<__half, 1, 4>)
-                      : a.pitch ? by_type(d->dtype, &norm_warp_rows_kernel<float, 2, 2>, &norm_warp_rows_kernel<__nv_bfloat16, 2, 2>, &norm_warp_rows_kernel<__half, 2, 2>)
-                                : NORM_KERNEL(norm_rows_kernel);
+        const bool full = full_units(a, d->dtype, false);
+        auto kernel = !a.pitch ? NORM_KERNEL(norm_rows_kernel)
+                      : a.units <= 32 ? (full ? NORM_KERNEL(norm_warp_rows_kernel, , 1, 4, true) : NORM_KERNEL(norm_warp_rows_kernel, , 1, 4, false))
+                                      : (full ? NORM_KERNEL(norm_warp_rows_kernel, , 2, 2, true) : NORM_KERNEL(norm_warp_rows_kernel, , 2, 2, false));
         KernelScope ks(ctx, KC_POST, stream);
         launch_kernel(kernel, grid, NORM_THREADS, a.pitch ? 0 : smem, stream, a);
     } else {
@@ -1126,7 +1178,7 @@ extern "C" int32_t rtma_group_norm(rtma_ctx* ctx, const rtma_norm_desc* d, int64
         if (!stats) a.stats = cur.take<float>(2 * (size_t)G * a.groups);
         if (n > 0) {
             KernelScope ks(ctx, KC_POST, stream);
-            launch_kernel(NORM_KERNEL(norm_stats_kernel), grid, NORM_THREADS, 0, stream, a);
+            launch_kernel(full_units(a, d->dtype, false) ? NORM_KERNEL(norm_stats_kernel, , true) : NORM_KERNEL(norm_stats_kernel, , false), grid, NORM_THREADS, 0, stream, a);
         }
         RTMA_LAUNCH_CHECK(ctx);
         {
@@ -1136,7 +1188,7 @@ extern "C" int32_t rtma_group_norm(rtma_ctx* ctx, const rtma_norm_desc* d, int64
         RTMA_LAUNCH_CHECK(ctx);
         if (n > 0) {
             KernelScope ks(ctx, KC_POST, stream);
-            launch_kernel(NORM_KERNEL(norm_apply_kernel), grid, NORM_THREADS, 0, stream, a);
+            launch_kernel(full_units(a, d->dtype, false) ? NORM_KERNEL(norm_apply_kernel, , true) : NORM_KERNEL(norm_apply_kernel, , false), grid, NORM_THREADS, 0, stream, a);
         }
     }
     RTMA_LAUNCH_CHECK(ctx);
@@ -1177,12 +1229,13 @@ extern "C" int32_t rtma_group_norm_grad(rtma_ctx* ctx, const rtma_norm_desc* d, 
         KernelScope ks(ctx, KC_POST, stream);
         if (rows) {
             const size_t smem = sizeof(float2) * (8 * NORM_THREADS + (size_t)a.rows_at_once * a.groups);
-            auto kernel = a.pitch && a.units <= 32 ? by_type(d->dtype, &norm_warp_rows_grad_kernel<float, 1, 2>, &norm_warp_rows_grad_kernel<__nv_bfloat16, 1, 2>, &norm_warp_rows_grad_kernel<__half, 1, 2>)
-                          : a.pitch ? by_type(d->dtype, &norm_warp_rows_grad_kernel<float, 2, 1>, &norm_warp_rows_grad_kernel<__nv_bfloat16, 2, 1>, &norm_warp_rows_grad_kernel<__half, 2, 1>)
-                                    : NORM_KERNEL(norm_rows_grad_kernel);
+            const bool full = full_units(a, d->dtype, true);
+            auto kernel = !a.pitch ? NORM_KERNEL(norm_rows_grad_kernel)
+                          : a.units <= 32 ? (full ? NORM_KERNEL(norm_warp_rows_grad_kernel, , 1, 2, true) : NORM_KERNEL(norm_warp_rows_grad_kernel, , 1, 2, false))
+                                          : (full ? NORM_KERNEL(norm_warp_rows_grad_kernel, , 2, 1, true) : NORM_KERNEL(norm_warp_rows_grad_kernel, , 2, 1, false));
             launch_kernel(kernel, (unsigned)tiles, NORM_THREADS, a.pitch ? 0 : smem, stream, a);
         } else {
-            launch_kernel(NORM_KERNEL(norm_grad_sums_kernel), (unsigned)tiles, NORM_THREADS, 0, stream, a);
+            launch_kernel(full_units(a, d->dtype, true) ? NORM_KERNEL(norm_grad_sums_kernel, , true) : NORM_KERNEL(norm_grad_sums_kernel, , false), (unsigned)tiles, NORM_THREADS, 0, stream, a);
         }
     }
     RTMA_LAUNCH_CHECK(ctx);
@@ -1198,7 +1251,7 @@ extern "C" int32_t rtma_group_norm_grad(rtma_ctx* ctx, const rtma_norm_desc* d, 
     RTMA_LAUNCH_CHECK(ctx);
     if (n > 0 && !rows) {
         KernelScope ks(ctx, KC_POST, stream);
-        launch_kernel(NORM_KERNEL(norm_grad_apply_kernel), (unsigned)tiles, NORM_THREADS, 0, stream, a);
+        launch_kernel(full_units(a, d->dtype, true) ? NORM_KERNEL(norm_grad_apply_kernel, , true) : NORM_KERNEL(norm_grad_apply_kernel, , false), (unsigned)tiles, NORM_THREADS, 0, stream, a);
     }
     RTMA_LAUNCH_CHECK(ctx);
     return RTMA_OK;

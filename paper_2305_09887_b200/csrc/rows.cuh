@@ -143,6 +143,26 @@ struct Eight {
         }
     }
 };
+// FULL: all eight exist and lie on 16 bytes (fp32: 32); then one instruction, and none for rows that are not there.
+template <bool FULL, class T>
+__device__ __forceinline__ void load_unit(Eight<T>& e, const T* p, bool here, int valid, int granule) {
+    if constexpr (FULL) {
+        if (!here) {
+#pragma unroll
+            for (int i = 0; i < (int)(sizeof(T) / 2); ++i) e.w[i] = make_uint4(0u, 0u, 0u, 0u);
+        } else if constexpr (sizeof(T) == 4) {
+            uint32_t* q = reinterpret_cast<uint32_t*>(e.w);
+            asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3]), "=r"(q[4]), "=r"(q[5]), "=r"(q[6]), "=r"(q[7])
+                         : "l"(p));
+        } else {
+            e.w[0] = *reinterpret_cast<const uint4*>(p);
+        }
+    } else {
+        e.load(p, here ? valid : 0, granule);
+    }
+}
+
 template <class T>
 __device__ __forceinline__ void store_eight(T* p, const float (&v)[8], int valid, int granule) {
     constexpr int WORDS = 2 * sizeof(T);
@@ -213,6 +233,13 @@ __device__ __forceinline__ void pairs_of(const Eight<T>& e, f2 (&v)[4]) {
     e.values(x);
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = pack2(x[2 * i], x[2 * i + 1]);
+}
+template <bool FULL, class T>
+__device__ __forceinline__ void store_unit(T* p, const f2 (&v)[4], int valid, int granule) {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpack2(v[i], x[2 * i], x[2 * i + 1]);
+    store_eight(p, x, FULL ? 8 : valid, FULL ? (sizeof(T) == 4 ? 32 : 16) : granule);
 }
 template <class T>
 __device__ __forceinline__ void store_pairs(T* p, const f2 (&v)[4], int valid, int granule) {
