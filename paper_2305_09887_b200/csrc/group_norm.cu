@@ -58,14 +58,23 @@ __device__ __forceinline__ void activate(int act, float slope, f2 (&u)[4]) {
     if (act == RTMA_ACT_SILU) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) u[i] = mul2(u[i], sigmoid2(u[i]));
-    } else if (act != RTMA_ACT_NONE) {  // slope: 0 for ReLU, and then 0 comes from a choice, so that -inf gives 0
+    } else if (act == RTMA_ACT_RELU) {  // NaN stays NaN
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             float a, b;
             unpack2(u[i], a, b);
-            a = a <= 0.f ? (act == RTMA_ACT_RELU ? 0.f : slope * a) : a;  // NaN stays NaN
-            b = b <= 0.f ? (act == RTMA_ACT_RELU ? 0.f : slope * b) : b;
+            asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(a));
+            asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(b));
             u[i] = pack2(a, b);
+        }
+    } else if (act == RTMA_ACT_PRELU) {
+        const f2 slopes = pack2(slope, slope);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float a, b, x, y;
+            unpack2(u[i], a, b);
+            unpack2(mul2(u[i], slopes), x, y);
+            u[i] = pack2(a > 0.f ? a : x, b > 0.f ? b : y);
         }
     }
 }
@@ -79,21 +88,23 @@ __device__ __forceinline__ float activate_back(int act, float slope, const f2 (&
             const f2 g = sigmoid2(u[i]);
             d[i] = mul2(d[i], mul2(g, fma2(u[i], fma2(g, minus, one), one)));
         }
-    } else if (act != RTMA_ACT_NONE) {
+    } else if (act == RTMA_ACT_RELU) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             float a, b, x, y;
             unpack2(u[i], a, b);
             unpack2(d[i], x, y);
-            if (!(a > 0.f)) {
-                ds = fmaf(x, act == RTMA_ACT_PRELU ? a : 0.f, ds);
-                x = act == RTMA_ACT_RELU ? 0.f : x * slope;
-            }
-            if (!(b > 0.f)) {
-                ds = fmaf(y, act == RTMA_ACT_PRELU ? b : 0.f, ds);
-                y = act == RTMA_ACT_RELU ? 0.f : y * slope;
-            }
-            d[i] = pack2(x, y);
+            d[i] = pack2(a > 0.f ? x : 0.f, b > 0.f ? y : 0.f);
+        }
+    } else if (act == RTMA_ACT_PRELU) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float a, b, x, y;
+            unpack2(u[i], a, b);
+            unpack2(d[i], x, y);
+            ds = fmaf(x, a > 0.f ? 0.f : a, ds);
+            ds = fmaf(y, b > 0.f ? 0.f : b, ds);
+            d[i] = pack2(a > 0.f ? x : x * slope, b > 0.f ? y : y * slope);
         }
     }
     return ds;
@@ -298,9 +309,12 @@ struct Run {
 // A row lies in `pitch` lanes (a power of two), eight channels each (NP times: channels 8 (lane + 32 p) ..); a set is the whole row or
 // a power of two of neighbouring lanes, so its sums are exchanged within a warp and nothing goes through shared memory.  RB rows
 // side by side hide one another's loads and shuffles.
-__device__ __forceinline__ float set_sum(float x, int lanes) {
-    for (int o = lanes >> 1; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    return x;
+template <int N>
+__device__ __forceinline__ void set_sums(float (&x)[N], int lanes) {
+    for (int o = lanes >> 1; o > 0; o >>= 1) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] += __shfl_xor_sync(0xffffffffu, x[i], o);
+    }
 }
 
 template <class T, int NP, int RB, bool FULL>
@@ -344,7 +358,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_kernel(const N
         request();
         for (; left > 0; left -= RB * rows_at_once) {  // the same number of times in every lane
             f2 v[RB][NP][4];
-            float mean[RB][NP], rstd[RB][NP];
+            float mean[RB * NP], rstd[RB * NP];
 #pragma unroll
             for (int b = 0; b < RB; ++b)
 #pragma unroll
@@ -354,18 +368,16 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_kernel(const N
             for (int b = 0; b < RB; ++b) {
 #pragma unroll
                 for (int p = 0; p < NP; ++p)  // what is not there reads as zero
-                    mean[b][p] = halves_sum(add2(add2(v[b][p][0], v[b][p][1]), add2(v[b][p][2], v[b][p][3])));
-                if (NP == 2 && whole) mean[b][0] += mean[b][NP - 1];
+                    mean[b * NP + p] = halves_sum(add2(add2(v[b][p][0], v[b][p][1]), add2(v[b][p][2], v[b][p][3])));
+                if (NP == 2 && whole) mean[b * NP] = mean[b * NP + NP - 1] = mean[b * NP] + mean[b * NP + NP - 1];
             }
-#pragma unroll
-            for (int b = 0; b < RB; ++b)
-#pragma unroll
-                for (int p = 0; p < NP; ++p) mean[b][p] = p && whole ? mean[b][0] : set_sum(mean[b][p], lanes) * inv;
+            set_sums(mean, lanes);
 #pragma unroll
             for (int b = 0; b < RB; ++b) {
 #pragma unroll
                 for (int p = 0; p < NP; ++p) {
-                    const f2 minus = pack2(-mean[b][p], -mean[b][p]);
+                    mean[b * NP + p] *= inv;
+                    const f2 minus = pack2(-mean[b * NP + p], -mean[b * NP + p]);
                     f2 q = 0ull;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -378,14 +390,13 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_kernel(const N
                         }
                         q = fma2(t, t, q);
                     }
-                    rstd[b][p] = halves_sum(q);
+                    rstd[b * NP + p] = halves_sum(q);
                 }
-                if (NP == 2 && whole) rstd[b][0] += rstd[b][NP - 1];
+                if (NP == 2 && whole) rstd[b * NP] = rstd[b * NP + NP - 1] = rstd[b * NP] + rstd[b * NP + NP - 1];
             }
+            set_sums(rstd, lanes);
 #pragma unroll
-            for (int b = 0; b < RB; ++b)
-#pragma unroll
-                for (int p = 0; p < NP; ++p) rstd[b][p] = p && whole ? rstd[b][0] : inverse_root(set_sum(rstd[b][p], lanes) * inv + a.eps);
+            for (int i = 0; i < RB * NP; ++i) rstd[i] = inverse_root(fmaf(rstd[i], inv, a.eps));
 #pragma unroll
             for (int b = 0; b < RB; ++b, out += out_step, r += rows_at_once) {
                 if (y + b * rows_at_once >= left) continue;
@@ -395,8 +406,8 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_kernel(const N
                     const int unit = u + 32 * p;
                     if (!FULL && valid[p] == 0) continue;
                     if (a.stats && (whole ? unit == 0 : (unit & (lanes - 1)) == 0))
-                        *reinterpret_cast<float2*>(a.stats + 2 * (r * a.groups + (whole ? 0 : unit >> lanes_log))) = make_float2(mean[b][p], rstd[b][p]);
-                    const f2 r2 = pack2(rstd[b][p], rstd[b][p]);
+                        *reinterpret_cast<float2*>(a.stats + 2 * (r * a.groups + (whole ? 0 : unit >> lanes_log))) = make_float2(mean[b * NP + p], rstd[b * NP + p]);
+                    const f2 r2 = pack2(rstd[b * NP + p], rstd[b * NP + p]);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) v[b][p][i] = fma2(mul2(v[b][p][i], r2), gam[p][i], bet[p][i]);
                     activate(a.act, slope, v[b][p]);
@@ -465,7 +476,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_grad_kernel(co
         request();
         for (; left > 0; left -= RB * rows_at_once) {
             f2 xh[RB][NP][4], du[RB][NP][4];
-            float s1[RB][NP], s2[RB][NP], rstd[RB][NP];
+            float s12[2 * RB * NP], rstd[RB][NP];  // sums over the set of gamma du, and of gamma du xhat
             Standard<T> st[RB][NP];
 #pragma unroll
             for (int b = 0; b < RB; ++b)
@@ -499,27 +510,22 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_grad_kernel(co
                         t1 = add2(t1, du[b][p][i]);
                         t2 = fma2(du[b][p][i], xh[b][p][i], t2);
                     }
-                    s1[b][p] = halves_sum(t1);
-                    s2[b][p] = halves_sum(t2);
+                    s12[2 * (b * NP + p)] = halves_sum(t1);
+                    s12[2 * (b * NP + p) + 1] = halves_sum(t2);
                 }
                 if (NP == 2 && whole) {
-                    s1[b][0] += s1[b][NP - 1];
-                    s2[b][0] += s2[b][NP - 1];
+                    s12[2 * b * NP] = s12[2 * b * NP + 2 * (NP - 1)] = s12[2 * b * NP] + s12[2 * b * NP + 2 * (NP - 1)];
+                    s12[2 * b * NP + 1] = s12[2 * b * NP + 2 * NP - 1] = s12[2 * b * NP + 1] + s12[2 * b * NP + 2 * NP - 1];
                 }
             }
-#pragma unroll
-            for (int b = 0; b < RB; ++b)
-#pragma unroll
-                for (int p = 0; p < NP; ++p) {
-                    s1[b][p] = p && whole ? s1[b][0] : set_sum(s1[b][p], lanes) * inv;
-                    s2[b][p] = p && whole ? s2[b][0] : set_sum(s2[b][p], lanes) * inv;
-                }
+            set_sums(s12, lanes);
 #pragma unroll
             for (int b = 0; b < RB; ++b, out += out_step, r += rows_at_once) {
                 if (y + b * rows_at_once >= left) continue;
 #pragma unroll
                 for (int p = 0; p < NP; ++p) {
-                    const f2 m1 = pack2(-s1[b][p], -s1[b][p]), m2 = pack2(-s2[b][p], -s2[b][p]), r2 = pack2(rstd[b][p], rstd[b][p]);
+                    const float n1 = -inv * s12[2 * (b * NP + p)], n2 = -inv * s12[2 * (b * NP + p) + 1];
+                    const f2 m1 = pack2(n1, n1), m2 = pack2(n2, n2), r2 = pack2(rstd[b][p], rstd[b][p]);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) du[b][p][i] = mul2(r2, fma2(xh[b][p][i], m2, add2(du[b][p][i], m1)));
                     if (FULL || valid[p]) store_unit<FULL>(out + 256 * p, du[b][p], valid[p], a.vy);
@@ -1085,6 +1091,13 @@ template <class K>
 K by_type(int32_t dtype, K f32, K bf16, K f16) { return dtype == RTMA_F32 ? f32 : dtype == RTMA_BF16 ? bf16 : f16; }
 #define NORM_KERNEL(name, ...) by_type(d->dtype, &name<float __VA_ARGS__>, &name<__nv_bfloat16 __VA_ARGS__>, &name<__half __VA_ARGS__>)
 
+// Runs of rows, per_sm for every SM: twice as many as run at a time, so that all SMs end together.  A few rows per thread at least.
+void cut_rows(NormArgs& a, const rtma_ctx* ctx, int per_sm) {
+    const int64_t runs = (int64_t)per_sm * ctx->sm_count, least = 4 * (int64_t)a.rows_at_once, even = ceil_div(a.n, runs > 2 * a.G ? runs - a.G : a.G);
+    a.tile_rows = (int)(even > least ? even : least);
+    a.tiles = a.n / a.tile_rows + a.G;
+}
+
 // Whether every unit of eight channels is there in full, on the boundary of one load: then no load or store asks.
 bool full_units(const NormArgs& a, int32_t dtype, bool gradient) {
     const int most = dtype == RTMA_F32 ? 32 : 16;
@@ -1121,10 +1134,7 @@ NormArgs norm_args(const rtma_ctx* ctx, const rtma_norm_desc* d, int64_t n, int3
     const int lanes = a.per_set / 8;
     if (d->C <= 512 && (d->groups == 1 || (a.per_set % 8 == 0 && lanes <= 32 && (lanes & (lanes - 1)) == 0)))
         for (a.pitch = 1; a.pitch < std::min(a.units, 32);) a.pitch *= 2;
-    // four runs of rows per SM; a few rows per thread at least
-    const int64_t least = 4 * (int64_t)a.rows_at_once, even = ceil_div(n, 4 * (int64_t)ctx->sm_count);
-    a.tile_rows = (int)(even > least ? even : least);
-    a.tiles = n / a.tile_rows + G;
+    cut_rows(a, ctx, 4);
     a.act = d->act;
     a.eps = d->eps;
     a.X = X;
@@ -1159,6 +1169,7 @@ extern "C" int32_t rtma_group_norm(rtma_ctx* ctx, const rtma_norm_desc* d, int64
     a.ldy = ldy;
     a.vy = row_granule(Y, ldy, row_type_bytes(d->dtype));
     a.stats = stats;
+    if (!rows) cut_rows(a, ctx, 6);
     const int64_t tiles = a.tiles;
     const size_t piece_bytes = rows ? 0 : ArenaCursor::granule(sizeof(float2) * tiles * a.groups);
     const size_t stat_bytes = rows || stats ? 0 : ArenaCursor::granule(sizeof(float2) * (size_t)G * a.groups);
