@@ -196,6 +196,7 @@ class Context:
             raise RtmaError("no CUDA device: this library has no CPU path")
         self._lib = load_library(checked)
         self.device = torch.device("cuda", device)
+        self._index = self.device.index
         torch.cuda.init()
         with torch.cuda.device(self.device):
             torch.zeros(1, device=self.device)  # make sure the primary context exists
@@ -411,6 +412,12 @@ class Context:
         self._check(st, "rtma_link_steps")
 
     # ---- operators on the rows of many parts -----------------------------------------
+    # (These checks are most of what a small call costs on the host: integers instead of device objects, shapes and strides
+    # instead of views.)
+    def _here(self, t, name):
+        if t.get_device() != self._index:
+            raise ValueError(f"{name} must live on {self.device}, got {t.device}")
+
     def _rows(self, t, name, dtype=None, shape=None):
         """(pointer, distance between rows) of a matrix whose rows are contiguous."""
         if dtype is None:
@@ -418,43 +425,56 @@ class Context:
                 raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
         elif t.dtype != dtype:
             raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-        if t.device != self.device:
-            raise ValueError(f"{name} must live on {self.device}, got {t.device}")
-        if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
-            raise ValueError(f"{name} must be a matrix{'' if shape is None else ' of ' + str(shape)}, got {tuple(t.shape)}")
-        n, d = t.shape
-        if d > 1 and t.stride(1) != 1:
+        self._here(t, name)
+        size = t.shape
+        if len(size) != 2 or (shape is not None and size != shape):
+            raise ValueError(f"{name} must be a matrix{'' if shape is None else ' of ' + str(tuple(shape))}, got {tuple(size)}")
+        n, d = size
+        ld, inner = t.stride()
+        if inner != 1 and d > 1:
             raise ValueError(f"the values of a row of {name} must be adjacent")
-        ld = t.stride(0) if n > 1 else max(t.stride(0), d)
         if ld < d:
-            raise ValueError(f"the rows of {name} overlap")
+            if n > 1:
+                raise ValueError(f"the rows of {name} overlap")
+            ld = d
         return t.data_ptr(), ld
 
     def _parts(self, offsets):
         """(pointer, number of parts) of the parts' row offsets; None: one part of all rows."""
         if offsets is None:
             return None, 1
-        _need(offsets, torch.int64, "offsets", self.device)
-        if offsets.dim() != 1 or offsets.numel() < 2 or not offsets.is_contiguous():
+        if offsets.dtype != torch.int64:
+            raise TypeError(f"offsets must be {torch.int64}, got {offsets.dtype}")
+        self._here(offsets, "offsets")
+        size = offsets.shape
+        if len(size) != 1 or size[0] < 2 or not offsets.is_contiguous():
             raise ValueError("offsets must be a contiguous vector of one more value than there are parts")
-        return offsets.data_ptr(), offsets.numel() - 1
+        return offsets.data_ptr(), size[0] - 1
 
     def _of_parts(self, t, name, dtype, G, shape):
         """(pointer, distance between parts) of a parameter: [G, *shape], or *shape for one that all parts share."""
         if t is None:
             return None, 0
-        _need(t, dtype, name, self.device)
-        stride = 0
-        if t.dim() == len(shape) + 1 and t.shape[0] == G:
+        if t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+        self._here(t, name)
+        size, steps, between = tuple(t.shape), t.stride(), 0
+        if len(size) == len(shape) + 1 and size[0] == G:
             if G > 1:
-                stride = t.stride(0)
-            t = t[0]
-        if tuple(t.shape) != shape or not t.is_contiguous():
+                between = steps[0]
+            size, steps = size[1:], steps[1:]
+        step, packed = 1, size == shape
+        for k in range(len(shape) - 1, -1, -1):
+            if not packed:
+                break
+            packed = steps[k] == step or shape[k] == 1
+            step *= shape[k]
+        if not packed and 0 not in shape:
             raise ValueError(f"{name} must be [{G}, {', '.join(map(str, shape))}] or {list(shape)}, contiguous within a part")
-        return t.data_ptr(), stride
+        return t.data_ptr(), between
 
     def _stream(self, stream):
-        return int(torch.cuda.current_stream(self.device).cuda_stream) if stream is None else _stream_handle(stream)
+        return torch._C._cuda_getCurrentRawStream(self._index) if stream is None else _stream_handle(stream)
 
     def grouped_linear(self, X, offsets, W, bias=None, out=None, stream=None):
         """Y[r] = X[r] W_g + b_g for the rows r of part g: X [n, d_in], W [G, d_in, d_out] (or [d_in, d_out] for all parts),
@@ -521,18 +541,26 @@ class Context:
         bt, bs = self._of_parts(beta, "beta", torch.float32, G, (C,))
         sl, ss = None, 0
         if slope is not None:
-            _need(slope, torch.float32, "slope", self.device)
-            if slope.dim() > 1 or slope.numel() not in (1, G):
-                raise ValueError(f"slope must be [{G}] or a single value")
-            sl, ss = slope.data_ptr(), slope.stride(0) if slope.dim() == 1 and slope.numel() > 1 else 0
+            sl, ss = self._slope(slope, "slope", G)
         desc = NormDesc(ROW_TYPES[X.dtype], C, int(groups), SCOPES[scope], ACTIVATIONS[act], float(eps), float(p), int(seed) & (2**64 - 1),
                         gs, bs, ss)
         return off, G, desc, gm, bt, sl, self._ids(row_ids, n)
 
+    def _slope(self, t, name, G):
+        if t.dtype != torch.float32:
+            raise TypeError(f"{name} must be {torch.float32}, got {t.dtype}")
+        self._here(t, name)
+        size = tuple(t.shape)
+        if size not in ((), (1,), (G,)):
+            raise ValueError(f"{name} must be [{G}] or a single value")
+        return t.data_ptr(), t.stride(0) if size == (G,) and G > 1 else 0
+
     def _ids(self, row_ids, n):
         if row_ids is None:
             return None
-        _need(row_ids, torch.int32, "row_ids", self.device)
+        if row_ids.dtype != torch.int32:
+            raise TypeError(f"row_ids must be {torch.int32}, got {row_ids.dtype}")
+        self._here(row_ids, "row_ids")
         if tuple(row_ids.shape) != (n,) or not row_ids.is_contiguous():
             raise ValueError(f"row_ids must be {n} contiguous ids")
         return row_ids.data_ptr()
@@ -546,12 +574,14 @@ class Context:
         off, G, desc, gm, bt, sl, ids = self._norm(X, offsets, groups, gamma, beta, slope, scope, act, eps, p, seed, row_ids)
         n = X.shape[0]
         if out is None:
-            out = torch.empty(X.shape, dtype=X.dtype, device=self.device)
-        y, ldy = self._rows(out, "out", X.dtype, tuple(X.shape))
+            out = torch.empty_like(X, memory_format=torch.contiguous_format)
+        y, ldy = self._rows(out, "out", X.dtype, X.shape)
         shape = (n if scope == "row" else G, int(groups), 2)
         if stats is None:
             stats = torch.empty(shape, dtype=torch.float32, device=self.device)
-        st = self._of_parts(stats, "stats", torch.float32, 1, shape)[0]
+            st = stats.data_ptr()
+        else:
+            st = self._of_parts(stats, "stats", torch.float32, 1, shape)[0]
         self._check(self._lib.rtma_group_norm(self._h, desc, n, G, off, x, ldx, gm, bt, sl, ids, y, ldy, st, self._stream(stream)),
                     "rtma_group_norm")
         return out, stats
@@ -566,7 +596,7 @@ class Context:
         g, ldg = self._rows(dY, "dY", X.dtype, (n, C))
         st = self._of_parts(stats, "stats", torch.float32, 1, (n if scope == "row" else G, int(groups), 2))[0]
         if out is None:
-            out = torch.empty(X.shape, dtype=X.dtype, device=self.device)
+            out = torch.empty_like(X, memory_format=torch.contiguous_format)
         dx, lddx = self._rows(out, "out", X.dtype, (n, C))
         new = lambda like: torch.empty(like.shape, dtype=torch.float32, device=self.device)  # noqa: E731
         dgamma = new(gamma) if dgamma is None and gamma is not None else dgamma
@@ -576,10 +606,7 @@ class Context:
         db, dbs = self._of_parts(dbeta, "dbeta", torch.float32, G, (C,))
         ds, dss = None, 0
         if dslope is not None:
-            _need(dslope, torch.float32, "dslope", self.device)
-            if dslope.dim() > 1 or dslope.numel() not in (1, G):
-                raise ValueError(f"dslope must be [{G}] or a single value")
-            ds, dss = dslope.data_ptr(), dslope.stride(0) if dslope.dim() == 1 and dslope.numel() > 1 else 0
+            ds, dss = self._slope(dslope, "dslope", G)
         self._check(self._lib.rtma_group_norm_grad(self._h, desc, n, G, off, x, ldx, g, ldg, st, gm, bt, sl, ids, dx, lddx, dg, dgs, db, dbs,
                                                    ds, dss, self._stream(stream)), "rtma_group_norm_grad")
         return out, dgamma, dbeta, dslope
@@ -592,8 +619,8 @@ class Context:
         r, ldr = (None, 0) if residual is None else self._rows(residual, "residual", X.dtype, (n, d))
         ids = self._ids(row_ids, n)
         if out is None:
-            out = torch.empty(n, d, dtype=X.dtype, device=self.device)
-        y, ldy = self._rows(out, "out", X.dtype, (n, d))
+            out = torch.empty_like(X, memory_format=torch.contiguous_format)
+        y, ldy = self._rows(out, "out", X.dtype, X.shape)
         self._check(self._lib.rtma_dropout(self._h, ROW_TYPES[X.dtype], n, d, x, ldx, ids, r, ldr, float(p), int(seed) & (2**64 - 1), y, ldy,
                                            self._stream(stream)), "rtma_dropout")
         return out
