@@ -12,7 +12,7 @@
 // warps from shared memory they cost more than all else that these do (239 -> XX us for 1M x 128 x 256 in fp16).
 //
 // This file: 16-bit rows (fp32 ones are in grouped_split.cu).  Two ways of loading:
-//   COPIES  rows that do not all lie on 16-byte boundaries: 8 warps with asynchronous copies of 16, 8 or 4 bytes
+//   COPIES  rows that do not all lie on 16-byte boundaries: 8 warps for each operand with asynchronous copies of 16, 8 or 4 bytes
 //   BULK    rows on 16-byte boundaries: one thread with bulk-tensor loads
 // then 8 drain warps (a quarter of the lanes, every second 32 columns each) and one warp that issues the MMAs.
 #include <algorithm>
@@ -28,9 +28,9 @@ using namespace grouped;
 enum Loading { COPIES, BULK };
 
 constexpr int BM = 128, BK = 64;
-// Registers a thread.  COPIES is launched with 96 (20 warps); the multiplier's four warps and the loading ones give some up to those
-// that drain: 256 x 112 + 256 x 96 + 128 x 64 = 61,440 = 640 x 96.
-constexpr int DRAIN_REGISTERS = 112, MULTIPLY_REGISTERS = 64;
+// Registers a thread.  COPIES is launched with 72 (28 warps); the multiplier's four warps and the loading ones give some up to those
+// that drain: 256 x 112 + 512 x 56 + 128 x 48 = 63,488 of 64,512.
+constexpr int DRAIN_REGISTERS = 112, LOAD_REGISTERS = 56, MULTIPLY_REGISTERS = 48;
 constexpr int SLAB_BYTES = 32 * 128;       // 32 rows of 64 16-bit values
 constexpr int DW_WAVES = 2;                // tiles of a weight gradient for every block that runs at a time
 constexpr int BIAS_ROWS = 1;               // of a slot: column sums of dY
@@ -52,7 +52,7 @@ struct Form {
     static constexpr int ONES_BYTES = MODE == WEIGHT_GRADIENT ? 1024 : 0;
     static constexpr int DYNAMIC_BYTES = RING_BYTES + 1024 + DRAIN_WARPS * OUT_BYTES + ONES_BYTES;
     static constexpr bool A_ACROSS = MODE == WEIGHT_GRADIENT, B_ACROSS = MODE != INPUT_GRADIENT;  // MN-major
-    static constexpr int LOAD_WARPS = LOADING == COPIES ? 8 : 0;                       // that do nothing else
+    static constexpr int LOAD_WARPS = LOADING == COPIES ? 16 : 0;                      // that do nothing else
     static constexpr int THREADS = 32 * (DRAIN_WARPS + LOAD_WARPS + 4);
 };
 
@@ -103,64 +103,78 @@ __device__ __forceinline__ void copy_pieces(uint32_t dst, const void* src, int b
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-// 16-byte pieces of both operands straight into the stage (t: 0..255); it is handed over once this thread's copies have landed, LAG
-// stages later.
-template <class T, int MODE>
+// What one thread brings of an operand (row 0..31, unit 0..7 of every slab): an address per tile, steps from there.
+template <class T, int MODE, bool IS_B>
+struct Source {
+    static constexpr bool ACROSS = IS_B ? MODE != INPUT_GRADIENT : MODE == WEIGHT_GRADIENT;
+    const T* p;      // the tile's first
+    int near, cols;  // along: rows from this thread's on, terms;  across: terms from this thread's row on, columns from its unit on
+    int64_t slab;    // elements between 32 rows
+    __device__ __forceinline__ void open(const LinearArgs& a, const Walk<MODE, BM, BK>& w, int row, int unit) {
+        const T* base = static_cast<const T*>(IS_B ? a.B : a.A);
+        const int64_t ld = MODE == WEIGHT_GRADIENT ? (IS_B ? a.ldb : a.lda) : IS_B ? (int64_t)a.d_out : a.lda;
+        slab = 32 * ld;
+        if constexpr (ACROSS) {
+            const int c = (IS_B ? w.n0 : w.m0) + 8 * unit;
+            near = w.k_end - row;
+            cols = (IS_B ? a.d_out : a.d_in) - c;
+            p = base + (MODE == WEIGHT_GRADIENT ? (w.row0 + row) * ld : w.part * a.w_stride + row * ld) + c;
+        } else {
+            near = (IS_B ? a.d_in - w.n0 : w.rows) - row;
+            cols = w.k_end - 8 * unit;
+            p = base + (IS_B ? w.part * a.w_stride + (w.n0 + row) * ld : (w.row0 + row) * ld) + 8 * unit;
+        }
+    }
+    // slab i of the stage that starts with term k0; valid: how many of the eight exist (the address is the tile's first if none does)
+    __device__ __forceinline__ const T* at(int i, int k0, int& valid) const {
+        if constexpr (ACROSS) {
+            const int k = k0 + 32 * (i & 1), c = 64 * (i >> 1);
+            valid = k < near ? max(0, min(8, cols - c)) : 0;
+            return valid ? p + (k >> 5) * slab + c : p;
+        } else {
+            valid = 32 * i < near ? max(0, min(8, cols - k0)) : 0;
+            return valid ? p + i * slab + k0 : p;
+        }
+    }
+};
+
+// 16-byte pieces of an operand straight into the stage (t: 0..255 of the operand's threads).  A stage's barrier counts every thread
+// twice: what it wrote itself, and its copies, whenever they land; the fence between ordinary and asynchronous accesses to shared
+// memory is the multiplier's.
+template <class T, int MODE, bool IS_B>
 __device__ __forceinline__ void copy_role(const LinearArgs& a, Shared& sh, uint32_t ring, int t) {
     typedef Form<T, MODE, COPIES> F;
-    constexpr int LAG = F::STAGES - 2;
-    const int row = t >> 3, unit = t & 7, lane = t & 31;
-    const uint32_t place = row * 128 + ((unit ^ (row & 7)) << 4);  // inside a slab (32-row slabs do not change row mod 8)
-    const int b_slabs = F::B_ACROSS ? 2 * ((a.BN + 63) / 64) : (a.BN + 31) / 32;
+    const int row = t >> 3, unit = t & 7, granule = IS_B ? a.vb : a.va;
+    const uint32_t place = (IS_B ? F::A_BYTES : 0) + row * 128 + ((unit ^ (row & 7)) << 4);  // (32-row slabs do not change row mod 8)
+    const int slabs = !IS_B ? 4 : F::B_ACROSS ? 2 * ((a.BN + 63) / 64) : (a.BN + 31) / 32;
     Walk<MODE, BM, BK> w;
+    Source<T, MODE, IS_B> from;
+    tc::RingAt at;
     bool more = w.first(a, sh);
-    tc::RingAt at, late_at;
-    int under_way = 0;
-    auto hand_over = [&]() {
-        tc::fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&sh.full[late_at.s]);
-        late_at.advance(F::STAGES);
-        --under_way;
-    };
-    auto bring = [&](uint32_t to, const T* p, int valid, int granule) {
-        if (granule >= 16) copy_pieces<16>(to, p, valid * (int)sizeof(T));
-        else if (granule == 8) copy_pieces<8>(to, p, valid * (int)sizeof(T));
-        else if (granule == 4) copy_pieces<4>(to, p, valid * (int)sizeof(T));
-        else {
-            Eight<T> e;
-            e.load(p, valid, granule);
-            store_16(to, e.w[0]);
-        }
-    };
-    bool ok = true;
-    while (more) {
-        ok = wait_for(&sh.empty[at.s], at.phase ^ 1u, sh, a.error_word);
-        if (!ok) break;
+    if (!more) return;
+    for (; more; more = w.next(a, sh), at.advance(F::STAGES)) {
+        if (w.k0 == 0) from.open(a, w, row, unit);
+        if (!wait_for(&sh.empty[at.s], at.phase ^ 1u, sh, a.error_word)) break;
         const uint32_t stage = ring + at.s * F::STAGE_BYTES + place;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            int valid;
-            const T* p = source_a<T, MODE>(a, w, i, row, unit, valid);
-            bring(stage + i * SLAB_BYTES, p, valid, a.va);
-        }
 #pragma unroll 4
-        for (int i = 0; i < b_slabs; ++i) {
+        for (int i = 0; i < slabs; ++i) {
             int valid;
-            const T* p = source_b<T, MODE>(a, w, i, row, unit, valid);
-            bring(stage + F::A_BYTES + i * SLAB_BYTES, p, valid, a.vb);
+            const T* p = from.at(i, w.k0, valid);
+            const uint32_t to = stage + i * SLAB_BYTES;
+            if (granule >= 16) copy_pieces<16>(to, p, valid * (int)sizeof(T));
+            else if (granule == 8) copy_pieces<8>(to, p, valid * (int)sizeof(T));
+            else if (granule == 4) copy_pieces<4>(to, p, valid * (int)sizeof(T));
+            else {
+                Eight<T> e;
+                e.load(p, valid, granule);
+                store_16(to, e.w[0]);
+            }
         }
-        copies_commit();
-        at.advance(F::STAGES);
-        if (++under_way > LAG) {
-            copies_wait<LAG>();
-            hand_over();
-        }
-        more = w.next(a, sh);
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(tc::smem_u32(&sh.full[at.s])) : "memory");
+        tc::mbar_arrive(&sh.full[at.s]);
     }
+    copies_commit();
     copies_wait<0>();
-    if (ok)
-        while (under_way > 0) hand_over();
 }
 
 // One warp with bulk-tensor loads.  Rows behind the end of a tile belong to the next part: they only reach results that are not
@@ -246,6 +260,7 @@ __device__ __forceinline__ void multiply_role(const LinearArgs& a, Shared& sh, u
     for (bool more = w.first(a, sh); more; more = w.next(a, sh)) {
         if (held == 0 && !wait_for(&sh.acc_empty[acc.s], acc.phase ^ 1u, sh, a.error_word)) return;
         if (!wait_for(&sh.full[at.s], at.phase, sh, a.error_word)) return;
+        if (LOADING == COPIES || MODE == WEIGHT_GRADIENT) tc::fence_proxy_async_smem();  // for what ordinary copies brought
         tc::tc_fence_after_sync();
         __syncwarp();
         multiply_stage<T, MODE, LOADING>(a, sh.tmem_base + acc.s * F::ACC_COLUMNS, ring + at.s * F::STAGE_BYTES, min(BK, w.k_end - w.k0), held ? 1u : 0u,
@@ -362,7 +377,7 @@ __global__ void __launch_bounds__(Form<T, MODE, LOADING>::THREADS, 1) linear_ker
     constexpr int MULTIPLIER = F::DRAIN_WARPS + F::LOAD_WARPS;
     if (threadIdx.x == 0) {
         for (int s = 0; s < F::STAGES; ++s) {
-            tc::mbar_init(&sh.full[s], LOADING == BULK ? 1 : F::LOAD_WARPS);
+            tc::mbar_init(&sh.full[s], LOADING == BULK ? 1 : 2 * 32 * F::LOAD_WARPS);
             tc::mbar_init(&sh.empty[s], 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -391,7 +406,10 @@ __global__ void __launch_bounds__(Form<T, MODE, LOADING>::THREADS, 1) linear_ker
         drain_role<T, MODE, LOADING>(a, sh, slabs);
     } else if (warp < MULTIPLIER) {
         if constexpr (LOADING == COPIES) {
-            copy_role<T, MODE>(a, sh, ring, threadIdx.x - 32 * F::DRAIN_WARPS);
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(LOAD_REGISTERS));
+            const int t = threadIdx.x - 32 * F::DRAIN_WARPS;
+            if (t < 256) copy_role<T, MODE, false>(a, sh, ring, t);
+            else copy_role<T, MODE, true>(a, sh, ring, t - 256);
         }
     } else {
         if constexpr (LOADING == COPIES) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(MULTIPLY_REGISTERS));
