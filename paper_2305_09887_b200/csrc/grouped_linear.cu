@@ -29,8 +29,8 @@ enum Loading { COPIES, BULK };
 
 constexpr int BM = 128, BK = 64;
 // Registers a thread.  COPIES is launched with 72 (28 warps); the multiplier's four warps and the loading ones give some up to those
-// that drain: 256 x 112 + 512 x 56 + 128 x 48 = 63,488 of 64,512.
-constexpr int DRAIN_REGISTERS = 112, LOAD_REGISTERS = 56, MULTIPLY_REGISTERS = 48;
+// that drain: 256 x 104 + 512 x 64 + 128 x 40 = 64,512.
+constexpr int DRAIN_REGISTERS = 104, LOAD_REGISTERS = 64, MULTIPLY_REGISTERS = 40;
 constexpr int SLAB_BYTES = 32 * 128;       // 32 rows of 64 16-bit values
 constexpr int DW_WAVES = 2;                // tiles of a weight gradient for every block that runs at a time
 constexpr int BIAS_ROWS = 1;               // of a slot: column sums of dY
@@ -316,10 +316,13 @@ __device__ __forceinline__ void drain_role(const LinearArgs& a, Shared& sh, uint
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     if (half + 2 * i < chunks) {
-                        float v[32];
-                        tc::tmem_load_32x32(from + 32 * (half + 2 * i), v);
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) total[i][j] += v[j];
+                        for (int q = 0; q < 4; ++q) {
+                            float v[8];
+                            tc::tmem_load_32x8(from + 32 * (half + 2 * i) + 8 * q, v);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) total[i][8 * q + j] += v[j];
+                        }
                     }
                 }
                 if (sums_wanted) {

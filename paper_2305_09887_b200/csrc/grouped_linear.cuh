@@ -204,18 +204,27 @@ struct Outlet {
                                  : "memory");
                 }
             } else {
+                // single values, eight rows (16 in fp32) under way: one at a time, this took longer than all else
                 const int x = lane % WIDE;
-                for (int r = lane / WIDE; r < rows; r += 32 / WIDE) {
-                    const uint32_t from = slab + r * ROW + (((x / PIECE) ^ swizzle(r)) << 4) + (x % PIECE) * (int)sizeof(O);
-                    O y;
-                    if constexpr (sizeof(O) == 4) {
-                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(y) : "r"(from) : "memory");
-                    } else {
-                        unsigned short bits;
-                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(bits) : "r"(from) : "memory");
-                        y = *reinterpret_cast<O*>(&bits);
+                constexpr int TOGETHER = 8;
+                for (int r0 = lane / WIDE; r0 < rows; r0 += TOGETHER * (32 / WIDE)) {
+                    O y[TOGETHER];
+#pragma unroll
+                    for (int i = 0; i < TOGETHER; ++i) {
+                        const int r = r0 + i * (32 / WIDE);
+                        const uint32_t from = slab + r * ROW + (((x / PIECE) ^ swizzle(r)) << 4) + (x % PIECE) * (int)sizeof(O);
+                        if constexpr (sizeof(O) == 4) {
+                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(y[i]) : "r"(from) : "memory");
+                        } else {
+                            unsigned short bits;
+                            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(bits) : "r"(from) : "memory");
+                            y[i] = *reinterpret_cast<O*>(&bits);
+                        }
                     }
-                    if (c0 + x < cols) out[r * ldo + c0 + x] = y;
+                    O* to = out + r0 * ldo + c0 + x;
+#pragma unroll
+                    for (int i = 0; i < TOGETHER; ++i, to += (32 / WIDE) * ldo)
+                        if (r0 + i * (32 / WIDE) < rows && c0 + x < cols) *to = y[i];
                 }
             }
             if (lane == 0) tc::tma_store_commit();  // a group for every slab, empty or not
