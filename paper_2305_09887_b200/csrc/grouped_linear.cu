@@ -28,8 +28,9 @@ using namespace grouped;
 enum Loading { COPIES, BULK };
 
 constexpr int BM = 128, BK = 64;
-// Registers a thread.  COPIES is launched with 72 (28 warps); the multiplier's four warps and the loading ones give some up to those
-// that drain: 256 x 104 + 512 x 64 + 128 x 40 = 64,512.
+// Registers a thread.  COPIES is launched with 72 in the weight gradient (28 warps), otherwise with 80 (24 warps); the multiplier's
+// four warps and the loading ones give some up to those that drain: 256 x 104 + 512 x 64 + 128 x 40 = 64,512 = 896 x 72, and with
+// 384 loading threads 56,320 of 768 x 80.
 constexpr int DRAIN_REGISTERS = 104, LOAD_REGISTERS = 64, MULTIPLY_REGISTERS = 40;
 constexpr int SLAB_BYTES = 32 * 128;       // 32 rows of 64 16-bit values
 constexpr int DW_WAVES = 2;                // tiles of a weight gradient for every block that runs at a time
@@ -52,7 +53,10 @@ struct Form {
     static constexpr int ONES_BYTES = MODE == WEIGHT_GRADIENT ? 1024 : 0;
     static constexpr int DYNAMIC_BYTES = RING_BYTES + 1024 + DRAIN_WARPS * OUT_BYTES + ONES_BYTES;
     static constexpr bool A_ACROSS = MODE == WEIGHT_GRADIENT, B_ACROSS = MODE != INPUT_GRADIENT;  // MN-major
-    static constexpr int LOAD_WARPS = LOADING == COPIES ? 16 : 0;                      // that do nothing else
+    // Of four warps that do nothing else.  Not more than stages: a group could be two rounds of the ring ahead of the multiplier, where
+    // the parity of a barrier's phase says nothing.
+    static constexpr int LOAD_GROUPS = LOADING == BULK ? 0 : STAGES < 4 ? STAGES : 4;
+    static constexpr int LOAD_WARPS = 4 * LOAD_GROUPS;
     static constexpr int THREADS = 32 * (DRAIN_WARPS + LOAD_WARPS + 4);
 };
 
@@ -103,17 +107,17 @@ __device__ __forceinline__ void copy_pieces(uint32_t dst, const void* src, int b
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-// What one thread brings of an operand (row 0..31, unit 0..7 of every slab): an address per tile, steps from there.
+// What one thread brings of an operand (rows 0..15 and 16 more, unit 0..7 of every slab): an address, steps from there.
 template <class T, int MODE, bool IS_B>
 struct Source {
     static constexpr bool ACROSS = IS_B ? MODE != INPUT_GRADIENT : MODE == WEIGHT_GRADIENT;
     const T* p;      // the tile's first
     int near, cols;  // along: rows from this thread's on, terms;  across: terms from this thread's row on, columns from its unit on
-    int64_t slab;    // elements between 32 rows
+    int64_t half;    // elements between 16 rows
     __device__ __forceinline__ void open(const LinearArgs& a, const Walk<MODE, BM, BK>& w, int row, int unit) {
         const T* base = static_cast<const T*>(IS_B ? a.B : a.A);
         const int64_t ld = MODE == WEIGHT_GRADIENT ? (IS_B ? a.ldb : a.lda) : IS_B ? (int64_t)a.d_out : a.lda;
-        slab = 32 * ld;
+        half = 16 * ld;
         if constexpr (ACROSS) {
             const int c = (IS_B ? w.n0 : w.m0) + 8 * unit;
             near = w.k_end - row;
@@ -125,56 +129,69 @@ struct Source {
             p = base + (IS_B ? w.part * a.w_stride + (w.n0 + row) * ld : (w.row0 + row) * ld) + 8 * unit;
         }
     }
-    // slab i of the stage that starts with term k0; valid: how many of the eight exist (the address is the tile's first if none does)
-    __device__ __forceinline__ const T* at(int i, int k0, int& valid) const {
+    // half h of slab i of the stage that starts with term k0; valid: how many of the eight exist (the tile's first address if none does)
+    __device__ __forceinline__ const T* at(int i, int h, int k0, int& valid) const {
         if constexpr (ACROSS) {
-            const int k = k0 + 32 * (i & 1), c = 64 * (i >> 1);
+            const int k = k0 + 32 * (i & 1) + 16 * h, c = 64 * (i >> 1);
             valid = k < near ? max(0, min(8, cols - c)) : 0;
-            return valid ? p + (k >> 5) * slab + c : p;
+            return valid ? p + (k >> 4) * half + c : p;
         } else {
-            valid = 32 * i < near ? max(0, min(8, cols - k0)) : 0;
-            return valid ? p + i * slab + k0 : p;
+            valid = 32 * i + 16 * h < near ? max(0, min(8, cols - k0)) : 0;
+            return valid ? p + (2 * i + h) * half + k0 : p;
         }
     }
 };
 
-// 16-byte pieces of an operand straight into the stage (t: 0..255 of the operand's threads).  A stage's barrier counts every thread
-// twice: what it wrote itself, and its copies, whenever they land; the fence between ordinary and asynchronous accesses to shared
-// memory is the multiplier's.
+// `slabs` slabs of an operand into a stage, by 128 threads (t).
 template <class T, int MODE, bool IS_B>
-__device__ __forceinline__ void copy_role(const LinearArgs& a, Shared& sh, uint32_t ring, int t) {
-    typedef Form<T, MODE, COPIES> F;
-    const int row = t >> 3, unit = t & 7, granule = IS_B ? a.vb : a.va;
-    const uint32_t place = (IS_B ? F::A_BYTES : 0) + row * 128 + ((unit ^ (row & 7)) << 4);  // (32-row slabs do not change row mod 8)
-    const int slabs = !IS_B ? 4 : F::B_ACROSS ? 2 * ((a.BN + 63) / 64) : (a.BN + 31) / 32;
-    Walk<MODE, BM, BK> w;
+__device__ __forceinline__ void copy_operand(const LinearArgs& a, const Walk<MODE, BM, BK>& w, uint32_t to, int slabs, int granule, int t) {
+    const int row = t >> 3, unit = t & 7;
     Source<T, MODE, IS_B> from;
-    tc::RingAt at;
-    bool more = w.first(a, sh);
-    if (!more) return;
-    for (; more; more = w.next(a, sh), at.advance(F::STAGES)) {
-        if (w.k0 == 0) from.open(a, w, row, unit);
-        if (!wait_for(&sh.empty[at.s], at.phase ^ 1u, sh, a.error_word)) break;
-        const uint32_t stage = ring + at.s * F::STAGE_BYTES + place;
-#pragma unroll 4
-        for (int i = 0; i < slabs; ++i) {
+    from.open(a, w, row, unit);
+    to += row * 128 + ((unit ^ (row & 7)) << 4);  // (16 rows do not change row mod 8)
+#pragma unroll 2
+    for (int i = 0; i < slabs; ++i, to += SLAB_BYTES) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
             int valid;
-            const T* p = from.at(i, w.k0, valid);
-            const uint32_t to = stage + i * SLAB_BYTES;
-            if (granule >= 16) copy_pieces<16>(to, p, valid * (int)sizeof(T));
-            else if (granule == 8) copy_pieces<8>(to, p, valid * (int)sizeof(T));
-            else if (granule == 4) copy_pieces<4>(to, p, valid * (int)sizeof(T));
+            const T* p = from.at(i, h, w.k0, valid);
+            const uint32_t dst = to + h * (SLAB_BYTES / 2);
+            if (granule >= 16) copy_pieces<16>(dst, p, valid * (int)sizeof(T));
+            else if (granule == 8) copy_pieces<8>(dst, p, valid * (int)sizeof(T));
+            else if (granule == 4) copy_pieces<4>(dst, p, valid * (int)sizeof(T));
             else {
                 Eight<T> e;
                 e.load(p, valid, granule);
-                store_16(to, e.w[0]);
+                store_16(dst, e.w[0]);
             }
         }
-        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(tc::smem_u32(&sh.full[at.s])) : "memory");
-        tc::mbar_arrive(&sh.full[at.s]);
     }
-    copies_commit();
-    copies_wait<0>();
+}
+
+// Both operands' pieces straight into the stages, which groups of four warps fill in turn.  A group waits for its own
+// copies and makes them visible to the tensor cores itself: a fence in the multiplier's warp waits for everything that the block
+// has on its way (XXTIME).
+template <class T, int MODE>
+__device__ __forceinline__ void copy_role(const LinearArgs& a, Shared& sh, uint32_t ring, int t, int group) {
+    typedef Form<T, MODE, COPIES> F;
+    const int slabs = F::B_ACROSS ? 2 * ((a.BN + 63) / 64) : (a.BN + 31) / 32;
+    Walk<MODE, BM, BK> w;
+    tc::RingAt at;
+    int turn = 0;
+    for (bool more = w.first(a, sh); more; more = w.next(a, sh), at.advance(F::STAGES)) {
+        const bool mine = turn == group;
+        turn = turn + 1 == F::LOAD_GROUPS ? 0 : turn + 1;
+        if (!mine) continue;
+        if (!wait_for(&sh.empty[at.s], at.phase ^ 1u, sh, a.error_word)) break;
+        const uint32_t stage = ring + at.s * F::STAGE_BYTES;
+        copy_operand<T, MODE, false>(a, w, stage, 4, a.va, t);
+        copy_operand<T, MODE, true>(a, w, stage + F::A_BYTES, slabs, a.vb, t);
+        copies_commit();
+        copies_wait<0>();
+        tc::fence_proxy_async_smem();
+        __syncwarp();
+        if ((t & 31) == 0) tc::mbar_arrive(&sh.full[at.s]);
+    }
 }
 
 // One warp with bulk-tensor loads.  Rows behind the end of a tile belong to the next part: they only reach results that are not
@@ -260,7 +277,6 @@ __device__ __forceinline__ void multiply_role(const LinearArgs& a, Shared& sh, u
     for (bool more = w.first(a, sh); more; more = w.next(a, sh)) {
         if (held == 0 && !wait_for(&sh.acc_empty[acc.s], acc.phase ^ 1u, sh, a.error_word)) return;
         if (!wait_for(&sh.full[at.s], at.phase, sh, a.error_word)) return;
-        if (LOADING == COPIES || MODE == WEIGHT_GRADIENT) tc::fence_proxy_async_smem();  // for what ordinary copies brought
         tc::tc_fence_after_sync();
         __syncwarp();
         multiply_stage<T, MODE, LOADING>(a, sh.tmem_base + acc.s * F::ACC_COLUMNS, ring + at.s * F::STAGE_BYTES, min(BK, w.k_end - w.k0), held ? 1u : 0u,
@@ -380,7 +396,7 @@ __global__ void __launch_bounds__(Form<T, MODE, LOADING>::THREADS, 1) linear_ker
     constexpr int MULTIPLIER = F::DRAIN_WARPS + F::LOAD_WARPS;
     if (threadIdx.x == 0) {
         for (int s = 0; s < F::STAGES; ++s) {
-            tc::mbar_init(&sh.full[s], LOADING == BULK ? 1 : 2 * 32 * F::LOAD_WARPS);
+            tc::mbar_init(&sh.full[s], LOADING == BULK ? 1 : 4);
             tc::mbar_init(&sh.empty[s], 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -411,8 +427,7 @@ __global__ void __launch_bounds__(Form<T, MODE, LOADING>::THREADS, 1) linear_ker
         if constexpr (LOADING == COPIES) {
             asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(LOAD_REGISTERS));
             const int t = threadIdx.x - 32 * F::DRAIN_WARPS;
-            if (t < 256) copy_role<T, MODE, false>(a, sh, ring, t);
-            else copy_role<T, MODE, true>(a, sh, ring, t - 256);
+            copy_role<T, MODE>(a, sh, ring, t & 127, t >> 7);
         }
     } else {
         if constexpr (LOADING == COPIES) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(MULTIPLY_REGISTERS));
