@@ -12,7 +12,8 @@
 // warps from shared memory they cost more than all else that these do (239 -> XX us for 1M x 128 x 256 in fp16).
 //
 // This file: 16-bit rows (fp32 ones are in grouped_split.cu).  Two ways of loading:
-//   COPIES  rows that do not all lie on 16-byte boundaries: 8 warps for each operand with asynchronous copies of 16, 8 or 4 bytes
+//   COPIES  rows of an operand do not all lie on 16-byte boundaries: three or four groups of 4 warps with asynchronous copies of 8 or 4
+//           bytes (or plain loads of 2), bulk-tensor loads for the other operand
 //   BULK    rows on 16-byte boundaries: one thread with bulk-tensor loads
 // then 8 drain warps (a quarter of the lanes, every second 32 columns each) and one warp that issues the MMAs.
 #include <algorithm>
@@ -168,11 +169,36 @@ __device__ __forceinline__ void copy_operand(const LinearArgs& a, const Walk<MOD
     }
 }
 
-// Both operands' pieces straight into the stages, which groups of four warps fill in turn.  A group waits for its own
-// copies and makes them visible to the tensor cores itself: a fence in the multiplier's warp waits for everything that the block
-// has on its way (XXTIME).
+// The bulk-tensor loads of a stage's operand, by one thread.
+template <class T, int MODE, int LOADING>
+__device__ __forceinline__ uint32_t bulk_bytes_b(const LinearArgs& a) {
+    return Form<T, MODE, LOADING>::B_ACROSS ? (uint32_t)((a.BN + 63) / 64) * 2 * SLAB_BYTES : (uint32_t)a.BN * 128u;
+}
+template <int MODE>
+__device__ __forceinline__ void bulk_a(const LinearArgs& a, const Walk<MODE, BM, BK>& w, uint8_t* to, uint64_t* bar) {
+    if constexpr (MODE == WEIGHT_GRADIENT) {
+        for (int i = 0; i < 2; ++i) tc::tma_load_3d(to + 2 * i * SLAB_BYTES, &a.map_a, bar, w.m0 + 64 * i, (int)w.row0 + w.k0, 0);
+    } else {
+        tc::tma_load_3d(to, &a.map_a, bar, w.k0, (int)w.row0, 0);
+    }
+}
+template <int MODE>
+__device__ __forceinline__ void bulk_b(const LinearArgs& a, const Walk<MODE, BM, BK>& w, uint8_t* to, uint64_t* bar) {
+    const int z = MODE != WEIGHT_GRADIENT && a.w_stride ? w.part : 0;
+    if constexpr (MODE == INPUT_GRADIENT) {
+        tc::tma_load_3d(to, &a.map_b, bar, w.k0, w.n0, z);
+    } else {
+        const int r = MODE == FORWARD ? w.k0 : (int)w.row0 + w.k0;
+        for (int i = 0; 64 * i < a.BN; ++i) tc::tma_load_3d(to + 2 * i * SLAB_BYTES, &a.map_b, bar, w.n0 + 64 * i, r, z);
+    }
+}
+
+// Stages by copies, which groups of four warps fill in turn.  A group waits for its own copies and makes them visible to the tensor
+// cores itself: a fence in the multiplier's warp waits for everything that the block has on its way, which made a stage of
+// the weight gradient of 1M x 256 x 47 in fp16 cost 2700 cycles (375 us; with groups 256 us).  An operand whose rows do lie on 16-byte
+// boundaries still comes in bulk.
 template <class T, int MODE>
-__device__ __forceinline__ void copy_role(const LinearArgs& a, Shared& sh, uint32_t ring, int t, int group) {
+__device__ __forceinline__ void copy_role(const LinearArgs& a, Shared& sh, uint8_t* ring, int t, int group) {
     typedef Form<T, MODE, COPIES> F;
     const int slabs = F::B_ACROSS ? 2 * ((a.BN + 63) / 64) : (a.BN + 31) / 32;
     Walk<MODE, BM, BK> w;
@@ -183,14 +209,22 @@ __device__ __forceinline__ void copy_role(const LinearArgs& a, Shared& sh, uint3
         turn = turn + 1 == F::LOAD_GROUPS ? 0 : turn + 1;
         if (!mine) continue;
         if (!wait_for(&sh.empty[at.s], at.phase ^ 1u, sh, a.error_word)) break;
-        const uint32_t stage = ring + at.s * F::STAGE_BYTES;
-        copy_operand<T, MODE, false>(a, w, stage, 4, a.va, t);
-        copy_operand<T, MODE, true>(a, w, stage + F::A_BYTES, slabs, a.vb, t);
+        uint8_t* stage = ring + at.s * F::STAGE_BYTES;
+        uint64_t* bar = &sh.full[at.s];
+        const bool cut = MODE == WEIGHT_GRADIENT && w.k0 + BK > w.k_end;  // rows of the next part must not be summed
+        const bool a_whole = a.in_bulk & 1 && !cut, b_whole = a.in_bulk & 2 && !cut;
+        if (t == 0 && (a_whole || b_whole)) {  // (announced before this warp's arrival)
+            tc::mbar_expect_tx(bar, (a_whole ? F::A_BYTES : 0u) + (b_whole ? bulk_bytes_b<T, MODE, COPIES>(a) : 0u));
+            if (a_whole) bulk_a<MODE>(a, w, stage, bar);
+            if (b_whole) bulk_b<MODE>(a, w, stage + F::A_BYTES, bar);
+        }
+        if (!a_whole) copy_operand<T, MODE, false>(a, w, tc::smem_u32(stage), 4, a.va, t);
+        if (!b_whole) copy_operand<T, MODE, true>(a, w, tc::smem_u32(stage) + F::A_BYTES, slabs, a.vb, t);
         copies_commit();
         copies_wait<0>();
         tc::fence_proxy_async_smem();
         __syncwarp();
-        if ((t & 31) == 0) tc::mbar_arrive(&sh.full[at.s]);
+        if ((t & 31) == 0) tc::mbar_arrive(bar);
     }
 }
 
@@ -200,7 +234,7 @@ __device__ __forceinline__ void copy_role(const LinearArgs& a, Shared& sh, uint3
 template <class T, int MODE>
 __device__ __forceinline__ void bulk_role(const LinearArgs& a, Shared& sh, uint8_t* ring, int lane) {
     typedef Form<T, MODE, BULK> F;
-    const uint32_t b_bytes = F::B_ACROSS ? (uint32_t)((a.BN + 63) / 64) * 2 * SLAB_BYTES : (uint32_t)a.BN * 128u;
+    const uint32_t b_bytes = bulk_bytes_b<T, MODE, BULK>(a);
     if (lane == 0) {
         tc::prefetch_tensormap(&a.map_a);
         tc::prefetch_tensormap(&a.map_b);
@@ -226,20 +260,8 @@ __device__ __forceinline__ void bulk_role(const LinearArgs& a, Shared& sh, uint8
             if (lane == 0) tc::mbar_arrive(bar);
         } else if (lane == 0) {
             tc::mbar_arrive_expect_tx(bar, F::A_BYTES + b_bytes);
-            uint8_t* b = stage + F::A_BYTES;
-            if constexpr (MODE == WEIGHT_GRADIENT) {
-                const int r = (int)w.row0 + w.k0;
-                for (int i = 0; i < 2; ++i) tc::tma_load_3d(stage + 2 * i * SLAB_BYTES, &a.map_a, bar, w.m0 + 64 * i, r, 0);
-                for (int i = 0; 64 * i < a.BN; ++i) tc::tma_load_3d(b + 2 * i * SLAB_BYTES, &a.map_b, bar, w.n0 + 64 * i, r, 0);
-            } else {
-                const int z = a.w_stride ? w.part : 0;
-                tc::tma_load_3d(stage, &a.map_a, bar, w.k0, (int)w.row0, 0);
-                if constexpr (MODE == FORWARD) {
-                    for (int i = 0; 64 * i < a.BN; ++i) tc::tma_load_3d(b + 2 * i * SLAB_BYTES, &a.map_b, bar, w.n0 + 64 * i, w.k0, z);
-                } else {
-                    tc::tma_load_3d(b, &a.map_b, bar, w.k0, w.n0, z);
-                }
-            }
+            bulk_a<MODE>(a, w, stage, bar);
+            bulk_b<MODE>(a, w, stage + F::A_BYTES, bar);
         }
         __syncwarp();
     }
@@ -427,7 +449,7 @@ __global__ void __launch_bounds__(Form<T, MODE, LOADING>::THREADS, 1) linear_ker
         if constexpr (LOADING == COPIES) {
             asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(LOAD_REGISTERS));
             const int t = threadIdx.x - 32 * F::DRAIN_WARPS;
-            copy_role<T, MODE>(a, sh, ring, t & 127, t >> 7);
+            copy_role<T, MODE>(a, sh, ring_bytes, t & 127, t >> 7);
         }
     } else {
         if constexpr (LOADING == COPIES) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(MULTIPLY_REGISTERS));
@@ -504,17 +526,21 @@ int32_t launch_form(rtma_ctx* ctx, const LinearArgs& a, unsigned grid, bool& con
 
 // Whether both operands can be fetched by bulk-tensor loads; sets up their maps.
 template <int MODE>
-bool bulk_maps(LinearArgs& a, bool bf16) {
-    if (a.va < 16 || a.vb < 16) return false;
-    if (MODE == WEIGHT_GRADIENT)
-        return make_tensor_map_16bit(&a.map_a, bf16, a.A, 1, a.n, a.d_in, a.lda, a.n * a.lda, BK) &&
-               make_tensor_map_16bit(&a.map_b, bf16, a.B, 1, a.n, a.d_out, a.ldb, a.n * a.ldb, BK);
-    const int K = MODE == FORWARD ? a.d_in : a.d_out;
-    const int64_t matrix = (int64_t)a.d_in * a.d_out;
-    if (a.w_stride < 0) return false;
-    return make_tensor_map_16bit(&a.map_a, bf16, a.A, 1, a.n, K, a.lda, a.n * a.lda, BM) &&
-           make_tensor_map_16bit(&a.map_b, bf16, a.B, a.w_stride ? a.G : 1, a.d_in, a.d_out, a.d_out, a.w_stride ? a.w_stride : matrix,
-                                 MODE == FORWARD ? BK : a.BN);
+int bulk_maps(LinearArgs& a, bool bf16) {  // 1: the left operand, 2: the right one
+    int in_bulk = 0;
+    if (a.va >= 16) {
+        const bool ok = MODE == WEIGHT_GRADIENT ? make_tensor_map_16bit(&a.map_a, bf16, a.A, 1, a.n, a.d_in, a.lda, a.n * a.lda, BK)
+                                                : make_tensor_map_16bit(&a.map_a, bf16, a.A, 1, a.n, MODE == FORWARD ? a.d_in : a.d_out, a.lda, a.n * a.lda, BM);
+        in_bulk |= ok ? 1 : 0;
+    }
+    if (a.vb >= 16 && a.w_stride >= 0) {
+        const int64_t matrix = (int64_t)a.d_in * a.d_out;
+        const bool ok = MODE == WEIGHT_GRADIENT ? make_tensor_map_16bit(&a.map_b, bf16, a.B, 1, a.n, a.d_out, a.ldb, a.n * a.ldb, BK)
+                                                : make_tensor_map_16bit(&a.map_b, bf16, a.B, a.w_stride ? a.G : 1, a.d_in, a.d_out, a.d_out,
+                                                                        a.w_stride ? a.w_stride : matrix, MODE == FORWARD ? BK : a.BN);
+        in_bulk |= ok ? 2 : 0;
+    }
+    return in_bulk;
 }
 
 template <int MODE>
@@ -527,7 +553,8 @@ int32_t launch_linear(rtma_ctx* ctx, int32_t dtype, LinearArgs& a, int cls, cuda
     bool* configured = ctx->linear_configured + MODE * 4;
     KernelScope ks(ctx, cls, stream);
     const bool bf16 = dtype == RTMA_BF16;
-    if (bulk_maps<MODE>(a, bf16))
+    a.in_bulk = bulk_maps<MODE>(a, bf16);
+    if (a.in_bulk == 3)
         return bf16 ? launch_form<__nv_bfloat16, MODE, BULK>(ctx, a, grid, configured[0], stream) : launch_form<__half, MODE, BULK>(ctx, a, grid, configured[1], stream);
     return bf16 ? launch_form<__nv_bfloat16, MODE, COPIES>(ctx, a, grid, configured[2], stream) : launch_form<__half, MODE, COPIES>(ctx, a, grid, configured[3], stream);
 }

@@ -24,6 +24,7 @@ struct LinearArgs {
     int64_t lda, ldb, w_stride;
     int va, vb;                // granules of the rows (bytes)
     int go;                    // granule of the result's rows
+    int in_bulk;               // operands that bulk-tensor loads fetch: 1 the left one, 2 the right one
     bool vo;                   // the result can leave by bulk-tensor stores: map_o holds
     const void* bias;
     int64_t bias_stride;
