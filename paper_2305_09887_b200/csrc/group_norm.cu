@@ -22,8 +22,9 @@ struct NormArgs {
     int64_t n;
     int G, C, groups, per_set, units, rows_at_once, pitch;  // per_set = C / groups; units of eight channels; rows a block works on at a time;
                                                            // lanes of a row where warps keep rows to themselves (0: they do not)
+    bool straddles;  // sets share units, two at most
     int tile_rows;
-    int64_t tiles;  // at most so many
+    int64_t tiles;   // at most so many
     int act;
     float eps;
     const void *X, *dY;
@@ -534,6 +535,226 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_grad_kernel(co
         }
 #pragma unroll
         for (int p = 0; p < NP; ++p) leave_sums(a, tile, 8 * (u + 32 * p), y, pitch, rows_at_once, sb[p], sg[p], shared);
+        leave_slope(a, tile, ds, shared);
+    }
+}
+
+// ---- rows of up to 256 channels whose sets share units ---------------------------------------------
+// Sets of eight channels or more that do not end with a unit: a unit's channels belong to one set or to two.  A row lies in `pitch`
+// lanes as above; a set's sum grows from lane to lane in a scan that starts anew where a set begins, is complete in the lane with the
+// set's last channel and fetched from there.
+struct Straddle {
+    int set, first;   // set of the unit's first channel, how many of its channels are in it
+    bool begins, two; // the set begins with the unit; another one begins within it
+    int back;         // lanes from where the unit's last set begins
+    int end0, end1;   // lanes where the two sums are complete
+    __device__ __forceinline__ Straddle(const NormArgs& a, int u) {
+        const int c = 8 * u;
+        const bool there = c < a.C;
+        set = there ? c / a.per_set : 0;
+        const int c0 = set * a.per_set;
+        first = there ? min(8, c0 + a.per_set - c) : 8;
+        begins = !there || c == c0;
+        two = first < 8 && c + first < a.C;
+        back = begins || first < 8 ? 0 : u - (c0 >> 3);
+        end0 = there ? (c0 + a.per_set - 1) >> 3 : u;
+        end1 = two ? (c0 + 2 * a.per_set - 1) >> 3 : end0;
+    }
+    __device__ __forceinline__ f2 choose(int i, float in_first, float in_second) const {  // for channels 2 i and 2 i + 1
+        return pack2(2 * i < first ? in_first : in_second, 2 * i + 1 < first ? in_first : in_second);
+    }
+    // a unit's sums over the channels of its two sets
+    __device__ __forceinline__ void part(const f2 (&v)[4], float& lo, float& hi) const {
+        lo = hi = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float x, y;
+            unpack2(v[i], x, y);
+            lo += (2 * i < first ? x : 0.f) + (2 * i + 1 < first ? y : 0.f);
+            hi += (2 * i < first ? 0.f : x) + (2 * i + 1 < first ? 0.f : y);
+        }
+    }
+    // ... become the sets' sums
+    template <int N>
+    __device__ __forceinline__ void join(float (&lo)[N], float (&hi)[N], int pitch, int far) const {
+        float open[N];  // of the set that goes on behind the unit
+#pragma unroll
+        for (int i = 0; i < N; ++i) open[i] = first < 8 ? hi[i] : lo[i];
+        for (int o = 1; o <= far; o <<= 1) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float x = __shfl_up_sync(0xffffffffu, open[i], o, pitch);
+                if (o <= back) open[i] += x;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float before = __shfl_up_sync(0xffffffffu, open[i], 1, pitch), all = begins ? lo[i] : before + lo[i];
+            lo[i] = __shfl_sync(0xffffffffu, all, end0, pitch);
+            hi[i] = __shfl_sync(0xffffffffu, all, end1, pitch);
+        }
+    }
+};
+
+template <class T>
+__global__ void __launch_bounds__(NORM_THREADS, 2) norm_straddle_rows_kernel(const NormArgs a) {
+    constexpr int RB = sizeof(T) == 4 ? 2 : 4;  // rows in flight
+    __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
+    wait_for_kernel_before();
+    number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums);
+    const int pitch = a.pitch, u = threadIdx.x & (pitch - 1), y = threadIdx.x / pitch, rows_at_once = NORM_THREADS / pitch;
+    const int valid = max(0, min(8, a.C - 8 * u)), far = (a.per_set + 7) / 8;
+    const Straddle sets(a, u);
+    const float inv = 1.f / (float)a.per_set;
+    for (int tile = blockIdx.x; tile < tile_start[a.G]; tile += gridDim.x) {
+        const Run run(a, tile_start, tile);
+        f2 gam[4], bet[4];
+        load_params(a.gamma, a.gamma_stride, run.part, u, valid, 1.f, gam);
+        load_params(a.beta, a.beta_stride, run.part, u, valid, 0.f, bet);
+        const float slope = a.slope ? __ldg(a.slope + run.part * a.slope_stride) : 0.f;
+        Eight<T> raw[RB];
+        int left = (int)(run.end - run.begin), asked = left - y;
+        const T* x = static_cast<const T*>(a.X) + (run.begin + y) * a.ldx + 8 * u;
+        T* out = static_cast<T*>(a.Y) + (run.begin + y) * a.ldy + 8 * u;
+        int64_t r = run.begin + y;
+        const int64_t x_step = rows_at_once * a.ldx, out_step = rows_at_once * a.ldy;
+        auto request = [&]() {
+#pragma unroll
+            for (int b = 0; b < RB; ++b, x += x_step) load_unit<false>(raw[b], x, b * rows_at_once < asked, valid, a.vx);
+            asked -= RB * rows_at_once;
+        };
+        request();
+        for (; left > 0; left -= RB * rows_at_once) {  // the same number of times in every lane
+            f2 v[RB][4];
+            float mean0[RB], mean1[RB], rstd0[RB], rstd1[RB];
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {
+                pairs_of(raw[b], v[b]);
+                sets.part(v[b], mean0[b], mean1[b]);  // (what is not there reads as zero)
+            }
+            request();
+            sets.join(mean0, mean1, pitch, far);
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {
+                mean0[b] *= inv;
+                mean1[b] *= inv;
+                f2 q[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v[b][i] = add2(v[b][i], sets.choose(i, -mean0[b], -mean1[b]));
+                    float q0, q1;
+                    unpack2(mul2(v[b][i], v[b][i]), q0, q1);
+                    q[i] = pack2(2 * i < valid ? q0 : 0.f, 2 * i + 1 < valid ? q1 : 0.f);
+                }
+                sets.part(q, rstd0[b], rstd1[b]);
+            }
+            sets.join(rstd0, rstd1, pitch, far);
+#pragma unroll
+            for (int b = 0; b < RB; ++b, out += out_step, r += rows_at_once) {
+                rstd0[b] = inverse_root(fmaf(rstd0[b], inv, a.eps));
+                rstd1[b] = inverse_root(fmaf(rstd1[b], inv, a.eps));
+                if (y + b * rows_at_once >= left || valid == 0) continue;
+                if (a.stats) {
+                    float2* st = reinterpret_cast<float2*>(a.stats) + r * a.groups + sets.set;
+                    if (sets.begins) st[0] = make_float2(mean0[b], rstd0[b]);
+                    if (sets.two) st[1] = make_float2(mean1[b], rstd1[b]);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[b][i] = fma2(mul2(v[b][i], sets.choose(i, rstd0[b], rstd1[b])), gam[i], bet[i]);
+                activate(a.act, slope, v[b]);
+                if (a.drop.threshold) drop_pairs(a.drop, id_of(a, r), u, v[b]);
+                store_unit<false>(out, v[b], valid, a.vy);
+            }
+        }
+    }
+}
+
+template <class T>
+__global__ void __launch_bounds__(NORM_THREADS, 2) norm_straddle_rows_grad_kernel(const NormArgs a) {
+    constexpr int RB = sizeof(T) == 4 ? 1 : 2;
+    __shared__ float shared[8 * NORM_THREADS];
+    __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
+    wait_for_kernel_before();
+    number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums);
+    const int pitch = a.pitch, u = threadIdx.x & (pitch - 1), y = threadIdx.x / pitch, rows_at_once = NORM_THREADS / pitch;
+    const int valid = max(0, min(8, a.C - 8 * u)), far = (a.per_set + 7) / 8;
+    const Straddle sets(a, u);
+    const float inv = 1.f / (float)a.per_set;
+    for (int tile = blockIdx.x; tile < tile_start[a.G]; tile += gridDim.x) {
+        const Run run(a, tile_start, tile);
+        f2 gam[4], bet[4], sb[4], sg[4];
+        float ds = 0.f;
+        load_params(a.gamma, a.gamma_stride, run.part, u, valid, 1.f, gam);
+        load_params(a.beta, a.beta_stride, run.part, u, valid, 0.f, bet);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sb[i] = sg[i] = 0ull;
+        const float slope = a.slope ? __ldg(a.slope + run.part * a.slope_stride) : 0.f;
+        Eight<T> rx[RB], rd[RB];
+        float2 s0[RB], s1[RB];
+        int left = (int)(run.end - run.begin), asked = left - y;
+        const T* x = static_cast<const T*>(a.X) + (run.begin + y) * a.ldx + 8 * u;
+        const T* dy = static_cast<const T*>(a.dY) + (run.begin + y) * a.lddy + 8 * u;
+        const float2* stat = reinterpret_cast<const float2*>(a.stats) + (run.begin + y) * a.groups + sets.set;
+        T* out = static_cast<T*>(a.Y) + (run.begin + y) * a.ldy + 8 * u;
+        int64_t r = run.begin + y;
+        const int64_t x_step = rows_at_once * a.ldx, dy_step = rows_at_once * a.lddy, out_step = rows_at_once * a.ldy;
+        auto request = [&]() {
+#pragma unroll
+            for (int b = 0; b < RB; ++b, x += x_step, dy += dy_step, stat += rows_at_once * a.groups) {
+                const bool here = b * rows_at_once < asked;
+                load_unit<false>(rx[b], x, here, valid, a.vx);
+                load_unit<false>(rd[b], dy, here, valid, a.vdy);
+                s0[b] = here && valid ? stat[0] : make_float2(0.f, 0.f);
+                s1[b] = here && sets.two ? stat[1] : make_float2(0.f, 0.f);
+            }
+            asked -= RB * rows_at_once;
+        };
+        request();
+        for (; left > 0; left -= RB * rows_at_once) {
+            f2 xh[RB][4], du[RB][4];
+            float lo[2 * RB], hi[2 * RB], rstd0[RB], rstd1[RB];  // sums over the sets of gamma du, and of gamma du xhat
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {
+                pairs_of(rx[b], xh[b]);
+                pairs_of(rd[b], du[b]);
+                const uint32_t id = a.drop.threshold && y + b * rows_at_once < left ? id_of(a, r + b * rows_at_once) : 0u;
+                if (a.drop.threshold) drop_pairs(a.drop, id, u, du[b]);
+                f2 pre[4], t[4];
+                rstd0[b] = s0[b].y;
+                rstd1[b] = s1[b].y;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f2 r2 = sets.choose(i, rstd0[b], rstd1[b]);
+                    // (as in Standard)
+                    xh[b][i] = sizeof(T) == 2 ? fma2(xh[b][i], r2, sets.choose(i, -s0[b].x * s0[b].y, -s1[b].x * s1[b].y))
+                                              : mul2(add2(xh[b][i], sets.choose(i, -s0[b].x, -s1[b].x)), r2);
+                    pre[i] = fma2(xh[b][i], gam[i], bet[i]);
+                }
+                ds += activate_back(a.act, slope, pre, du[b]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    sb[i] = add2(sb[i], du[b][i]);
+                    sg[i] = fma2(du[b][i], xh[b][i], sg[i]);
+                    du[b][i] = mul2(du[b][i], gam[i]);
+                    t[i] = mul2(du[b][i], xh[b][i]);
+                }
+                sets.part(du[b], lo[2 * b], hi[2 * b]);
+                sets.part(t, lo[2 * b + 1], hi[2 * b + 1]);
+            }
+            request();
+            sets.join(lo, hi, pitch, far);
+#pragma unroll
+            for (int b = 0; b < RB; ++b, out += out_step, r += rows_at_once) {
+                if (y + b * rows_at_once >= left || valid == 0) continue;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f2 m1 = sets.choose(i, -inv * lo[2 * b], -inv * hi[2 * b]), m2 = sets.choose(i, -inv * lo[2 * b + 1], -inv * hi[2 * b + 1]);
+                    du[b][i] = mul2(sets.choose(i, rstd0[b], rstd1[b]), fma2(xh[b][i], m2, add2(du[b][i], m1)));
+                }
+                store_unit<false>(out, du[b], valid, a.vy);
+            }
+        }
+        leave_sums(a, tile, 8 * u, y, pitch, rows_at_once, sb, sg, shared);
         leave_slope(a, tile, ds, shared);
     }
 }
@@ -1130,9 +1351,11 @@ NormArgs norm_args(const rtma_ctx* ctx, const rtma_norm_desc* d, int64_t n, int3
     a.per_set = d->C / d->groups;
     a.units = (d->C + 7) / 8;
     a.rows_at_once = NORM_THREADS / a.units;
-    // warps keep rows to themselves where a set is a power of two of lanes, or the whole row
+    // warps keep rows to themselves where a set is a power of two of lanes or the whole row, or two sets at most share a unit
     const int lanes = a.per_set / 8;
-    if (d->C <= 512 && (d->groups == 1 || (a.per_set % 8 == 0 && lanes <= 32 && (lanes & (lanes - 1)) == 0)))
+    const bool of_lanes = d->groups == 1 || (a.per_set % 8 == 0 && lanes <= 32 && (lanes & (lanes - 1)) == 0);
+    a.straddles = !of_lanes && a.per_set >= 8 && d->C <= 256;
+    if (d->scope == RTMA_SCOPE_ROW && d->C <= 512 && (of_lanes || a.straddles))
         for (a.pitch = 1; a.pitch < std::min(a.units, 32);) a.pitch *= 2;
     cut_rows(a, ctx, 4);
     a.act = d->act;
@@ -1179,6 +1402,7 @@ extern "C" int32_t rtma_group_norm(rtma_ctx* ctx, const rtma_norm_desc* d, int64
         const size_t smem = sizeof(float) * a.rows_at_once * (8 * a.units + 2 * (size_t)a.groups);
         const bool full = full_units(a, d->dtype, false);
         auto kernel = !a.pitch ? NORM_KERNEL(norm_rows_kernel)
+                      : a.straddles ? NORM_KERNEL(norm_straddle_rows_kernel)
                       : a.units <= 32 ? (full ? NORM_KERNEL(norm_warp_rows_kernel, , 1, 4, true) : NORM_KERNEL(norm_warp_rows_kernel, , 1, 4, false))
                                       : (full ? NORM_KERNEL(norm_warp_rows_kernel, , 2, 2, true) : NORM_KERNEL(norm_warp_rows_kernel, , 2, 2, false));
         KernelScope ks(ctx, KC_POST, stream);
@@ -1242,6 +1466,7 @@ extern "C" int32_t rtma_group_norm_grad(rtma_ctx* ctx, const rtma_norm_desc* d, 
             const size_t smem = sizeof(float2) * (8 * NORM_THREADS + (size_t)a.rows_at_once * a.groups);
             const bool full = full_units(a, d->dtype, true);
             auto kernel = !a.pitch ? NORM_KERNEL(norm_rows_grad_kernel)
+                          : a.straddles ? NORM_KERNEL(norm_straddle_rows_grad_kernel)
                           : a.units <= 32 ? (full ? NORM_KERNEL(norm_warp_rows_grad_kernel, , 1, 2, true) : NORM_KERNEL(norm_warp_rows_grad_kernel, , 1, 2, false))
                                           : (full ? NORM_KERNEL(norm_warp_rows_grad_kernel, , 2, 1, true) : NORM_KERNEL(norm_warp_rows_grad_kernel, , 2, 1, false));
             launch_kernel(kernel, (unsigned)tiles, NORM_THREADS, a.pitch ? 0 : smem, stream, a);

@@ -115,6 +115,7 @@ def test_a_node_has_the_same_mask_in_every_partition(ctx):
 NORM_CASES = [
     # sizes of the parts, C, groups
     ([1], 8, 1), ([1], 2, 1), ([7, 0, 1, 30], 64, 8), ([130, 3], 47, 47), ([130, 3], 47, 1), ([64, 200], 100, 4), ([33, 0], 90, 9),
+    ([37, 0, 90], 240, 10), ([61, 5], 250, 2), ([3, 300], 54, 6), ([40, 1], 27, 3), ([200], 144, 16), ([9, 50], 300, 3), ([20, 30], 12, 3),
     ([50, 60], 256, 32), ([70], 512, 1), ([9, 12], 1024, 8), ([5, 9], 2048, 2), ([0, 0], 32, 4), ([2500], 24, 3), ([40, 50], 384, 1),
 ]
 
