@@ -104,29 +104,23 @@ struct Eight {
         } else if (valid == 8 && granule >= 16) {
 #pragma unroll
             for (int i = 0; i < WORDS / 4; ++i) w[i] = reinterpret_cast<const uint4*>(p)[i];
-        } else if (valid == 8 && granule == 8) {
+        } else if (granule >= 8 && valid % (8 / (int)sizeof(T)) == 0) {
+            // By pieces that are there or not: nothing is put together from loaded values, so that nothing waits for them here (which
+            // tails by single 16-bit values do: they made the rows of a warp wait for one another's).
 #pragma unroll
             for (int i = 0; i < WORDS / 2; ++i) {
-                const uint2 x = reinterpret_cast<const uint2*>(p)[i];
+                uint2 x = make_uint2(0u, 0u);
+                if ((i + 1) * (8 / (int)sizeof(T)) <= valid) x = reinterpret_cast<const uint2*>(p)[i];
                 q[2 * i] = x.x;
                 q[2 * i + 1] = x.y;
             }
-        } else if (sizeof(T) == 2 && valid == 8 && granule == 4) {
+        } else if (granule >= 4 && valid % (4 / (int)sizeof(T)) == 0) {
 #pragma unroll
-            for (int i = 0; i < WORDS; ++i) q[i] = reinterpret_cast<const uint32_t*>(p)[i];
-        } else {
+            for (int i = 0; i < WORDS; ++i) q[i] = (i + 1) * (4 / (int)sizeof(T)) <= valid ? reinterpret_cast<const uint32_t*>(p)[i] : 0u;
+        } else if constexpr (sizeof(T) == 2) {
             T e[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) e[j] = j < valid ? p[j] : from_f32<T>(0.f);
-            pack(e);
-        }
-    }
-    __device__ __forceinline__ void pack(const T (&e)[8]) {
-        uint32_t* q = reinterpret_cast<uint32_t*>(w);
-        if constexpr (sizeof(T) == 4) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) q[j] = __float_as_uint(e[j]);
-        } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 q[j] = (uint32_t)*reinterpret_cast<const unsigned short*>(&e[2 * j]) | (uint32_t)*reinterpret_cast<const unsigned short*>(&e[2 * j + 1]) << 16;
@@ -166,34 +160,33 @@ __device__ __forceinline__ void load_unit(Eight<T>& e, const T* p, bool here, in
 template <class T>
 __device__ __forceinline__ void store_eight(T* p, const float (&v)[8], int valid, int granule) {
     constexpr int WORDS = 2 * sizeof(T);
-    if (valid == 8 && granule > (int)sizeof(T)) {
-        uint32_t q[WORDS];
-        if constexpr (sizeof(T) == 4) {
+    uint32_t q[WORDS];
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) q[j] = __float_as_uint(v[j]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) q[j] = narrow2(v[2 * j], v[2 * j + 1], static_cast<const T*>(nullptr));
-        }
-        if (sizeof(T) == 4 && granule == 32) {
-            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(q[0]), "r"(q[1]), "r"(q[2]), "r"(q[3]),
-                         "r"(q[WORDS - 4]), "r"(q[WORDS - 3]), "r"(q[WORDS - 2]), "r"(q[WORDS - 1])
-                         : "memory");
-        } else if (granule >= 16) {
-#pragma unroll
-            for (int i = 0; i < WORDS / 4; ++i)
-                reinterpret_cast<uint4*>(p)[i] = make_uint4(q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]);
-        } else if (granule == 8) {
-#pragma unroll
-            for (int i = 0; i < WORDS / 2; ++i) reinterpret_cast<uint2*>(p)[i] = make_uint2(q[2 * i], q[2 * i + 1]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < WORDS; ++i) reinterpret_cast<uint32_t*>(p)[i] = q[i];
-        }
+        for (int j = 0; j < 8; ++j) q[j] = __float_as_uint(v[j]);
     } else {
 #pragma unroll
+        for (int j = 0; j < 4; ++j) q[j] = narrow2(v[2 * j], v[2 * j + 1], static_cast<const T*>(nullptr));
+    }
+    if (sizeof(T) == 4 && valid == 8 && granule == 32) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(q[0]), "r"(q[1]), "r"(q[2]), "r"(q[3]),
+                     "r"(q[WORDS - 4]), "r"(q[WORDS - 3]), "r"(q[WORDS - 2]), "r"(q[WORDS - 1])
+                     : "memory");
+    } else if (valid == 8 && granule >= 16) {
+#pragma unroll
+        for (int i = 0; i < WORDS / 4; ++i) reinterpret_cast<uint4*>(p)[i] = make_uint4(q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]);
+    } else if (granule >= 8 && valid % (8 / (int)sizeof(T)) == 0) {
+#pragma unroll
+        for (int i = 0; i < WORDS / 2; ++i)
+            if ((i + 1) * (8 / (int)sizeof(T)) <= valid) reinterpret_cast<uint2*>(p)[i] = make_uint2(q[2 * i], q[2 * i + 1]);
+    } else if (granule >= 4 && valid % (4 / (int)sizeof(T)) == 0) {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i)
+            if ((i + 1) * (4 / (int)sizeof(T)) <= valid) reinterpret_cast<uint32_t*>(p)[i] = q[i];
+    } else if constexpr (sizeof(T) == 2) {
+#pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (j < valid) p[j] = from_f32<T>(v[j]);
+            if (j < valid) reinterpret_cast<unsigned short*>(p)[j] = (unsigned short)(j & 1 ? q[j >> 1] >> 16 : q[j >> 1]);
     }
 }
 
