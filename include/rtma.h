@@ -341,8 +341,8 @@ int32_t rtma_sample_hop(rtma_ctx* ctx, int64_t n, const int64_t* rowptr, const i
  * forms that rtma_local_steps fixes (Sec. 4.1 "GNN Encoders"); these calls are not tied to a model.
  *  - Rows of all parts lie behind one another; part g holds the rows offsets[g] .. offsets[g+1]-1.
  *    offsets [G+1] is a DEVICE array, ascending, within [0, n] (rtma_partition's part_offsets); it is
- *    never read back.  Parts may be empty.  Rows before offsets[0] and behind offsets[G] are neither
- *    read nor written.  offsets == NULL (then G = 1): one part of all n rows.  1 <= G <=
+ *    never read back.  Parts may be empty.  Rows before offsets[0] and behind offsets[G] are not
+ *    written and no result depends on them.  offsets == NULL (then G = 1): one part of all n rows.  1 <= G <=
  *    RTMA_MAX_GROUPS.  Offsets that do not ascend or leave [0, n] are cut to it (the results of such
  *    parts are not defined; no memory outside the n rows is touched); the checked build reports them.
  *  - dtype is the type of the rows (and of W and b): RTMA_F32, RTMA_BF16 or RTMA_F16.  Sums are
@@ -361,8 +361,9 @@ enum { RTMA_F32 = 0, RTMA_BF16 = 1, RTMA_F16 = 2 };
 
 /* Y[r] = X[r] W_g + b_g for the rows r of part g.  W_g [d_in][d_out] row-major at W + g * w_stride,
  * b_g [d_out] at b + g * b_stride (b may be NULL).  X [n][ldx], Y [n][ldy]; they must not overlap.
- * Of fp32 rows every product is exact to fp32 (no TF32); a value of X that is not finite makes its
- * row of Y not finite, possibly NaN where fp32 arithmetic gives an infinity.
+ * Of fp32 rows the products are fp32 ones (no TF32): each factor is used as three bf16 numbers that
+ * add up to it, and only what is below 2^-22 of a product is left out; a value of X that is not
+ * finite makes its row of Y not finite, possibly NaN where fp32 arithmetic gives an infinity.
  * 1 <= d_in, d_out <= RTMA_MAX_WIDTH.                                                          */
 int32_t rtma_grouped_linear(rtma_ctx* ctx, int32_t dtype, int64_t n, int32_t G, const int64_t* offsets,
                             int32_t d_in, int32_t d_out, const void* X, int64_t ldx, const void* W,

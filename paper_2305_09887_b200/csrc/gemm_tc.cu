@@ -947,16 +947,16 @@ bool make_tensor_map_bf16(CUtensorMap* out, const void* base, uint64_t rows, uin
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-bool make_store_map(CUtensorMap* out, int type, const void* base, uint64_t rows, uint64_t cols, uint64_t ld, int row_bytes) {
+bool make_store_map(CUtensorMap* out, int type, const void* base, uint64_t rows, uint64_t cols, uint64_t ld) {
     EncodeTiledFn fn = encode_tiled();
     if (!fn || rows == 0 || cols == 0) return false;
     const cuuint32_t size = type == RTMA_F32 ? 4 : 2;
     const cuuint64_t gdim[2] = {cols, rows};
     const cuuint64_t gstride[1] = {ld * size};
-    const cuuint32_t box[2] = {row_bytes / size, 32};
+    const cuuint32_t box[2] = {64 / size, 32};
     const cuuint32_t estride[2] = {1, 1};
     const CUtensorMapDataType kind = type == RTMA_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : type == RTMA_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    return fn(out, kind, 2, const_cast<void*>(base), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE, row_bytes == 32 ? CU_TENSOR_MAP_SWIZZLE_32B : CU_TENSOR_MAP_SWIZZLE_64B,
+    return fn(out, kind, 2, const_cast<void*>(base), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
               CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 

@@ -9,7 +9,7 @@
 // The tensor cores truncate when they accumulate, so a long sum drifts towards zero by half a step per addition.  The weight
 // gradient, whose result is fp32, therefore has its drain warps take the accumulator after every 128 rows and add it up in
 // registers, rounded to nearest.  The column sums of dY are a product as well, with a left operand of ones: added up by the drain
-// warps from shared memory they cost more than all else that these do (239 -> XX us for 1M x 128 x 256 in fp16).
+// warps from shared memory they cost more than all else that these do (1M x 128 x 256 in fp16: 239 us then, 164 like this and with what came after).
 //
 // This file: 16-bit rows (fp32 ones are in grouped_split.cu).  Two ways of loading:
 //   COPIES  rows of an operand do not all lie on 16-byte boundaries: three or four groups of 4 warps with asynchronous copies of 8 or 4
@@ -46,9 +46,8 @@ struct Form {
     static constexpr int RING_BYTES = (MODE == WEIGHT_GRADIENT ? 160 : 144) * 1024;
     static constexpr int STAGES = RING_BYTES / STAGE_BYTES;
     static constexpr int DRAIN_WARPS = 8;
-    static constexpr int OUT_SLABS = MODE == WEIGHT_GRADIENT ? 2 : 4;                  // of a drain warp: 32 rows of OUT_ROW bytes on
-    static constexpr int OUT_ROW = 64;                                                 // their way out
-    static constexpr int OUT_BYTES = OUT_SLABS * 32 * OUT_ROW;
+    static constexpr int OUT_SLABS = MODE == WEIGHT_GRADIENT ? 2 : 4;                  // of a drain warp: 32 rows of 64 bytes on their way out
+    static constexpr int OUT_BYTES = OUT_SLABS * 32 * 64;
     static constexpr int ACC_STAGES = MODE == WEIGHT_GRADIENT ? 2 : 1 << 20;           // after so many the accumulator is drained (or at a tile's end)
     static constexpr int ACC_COLUMNS = 256;                                            // dw: 128 of the product, 128 of the column sums
     static constexpr int ONES_BYTES = MODE == WEIGHT_GRADIENT ? 1024 : 0;
@@ -105,9 +104,12 @@ __device__ __forceinline__ void copy_pieces(uint32_t dst, const void* src, int b
         copy<SIZE>(dst + i * SIZE, here ? static_cast<const char*>(src) + i * SIZE : src, here);
     }
 }
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+// this thread's copies have landed and the tensor cores may read them
+__device__ __forceinline__ void copies_done() {
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    tc::fence_proxy_async_smem();
+}
+
 // What one thread brings of an operand (rows 0..15 and 16 more, unit 0..7 of every slab): an address, steps from there.
 template <class T, int MODE, bool IS_B>
 struct Source {
@@ -220,9 +222,7 @@ __device__ __forceinline__ void copy_role(const LinearArgs& a, Shared& sh, uint8
         }
         if (!a_whole) copy_operand<T, MODE, false>(a, w, tc::smem_u32(stage), 4, a.va, t);
         if (!b_whole) copy_operand<T, MODE, true>(a, w, tc::smem_u32(stage) + F::A_BYTES, slabs, a.vb, t);
-        copies_commit();
-        copies_wait<0>();
-        tc::fence_proxy_async_smem();
+        copies_done();
         __syncwarp();
         if ((t & 31) == 0) tc::mbar_arrive(bar);
     }
@@ -253,9 +253,7 @@ __device__ __forceinline__ void bulk_role(const LinearArgs& a, Shared& sh, uint8
                 const T* p = i < 4 ? source_a<T, MODE>(a, w, i, row, unit, valid) : source_b<T, MODE>(a, w, i - 4, row, unit, valid);
                 copy<16>(tc::smem_u32(stage) + i * SLAB_BYTES + row * 128 + ((unit ^ (row & 7)) << 4), p, valid * (int)sizeof(T));
             }
-            copies_commit();
-            copies_wait<0>();
-            tc::fence_proxy_async_smem();
+            copies_done();
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(bar);
         } else if (lane == 0) {
@@ -330,7 +328,7 @@ __device__ __forceinline__ void drain_role(const LinearArgs& a, Shared& sh, uint
     typedef Form<T, MODE, LOADING> F;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, half = warp >> 2;
     typedef typename std::conditional<MODE == WEIGHT_GRADIENT, float, T>::type O;
-    Outlet<O, F::OUT_SLABS, F::OUT_ROW> outlet{slabs + warp * F::OUT_BYTES};
+    Outlet<O, F::OUT_SLABS> outlet{slabs + warp * F::OUT_BYTES};
     BiasHolder<T> bias{sh.bias + 128 * warp};
     const uint32_t tmem = sh.tmem_base + ((uint32_t)(32 * quarter) << 16);
     const int chunks = (a.BN + 31) / 32;
@@ -620,7 +618,7 @@ int32_t run_rows(rtma_ctx* ctx, const char* who, bool transposed, int32_t dtype,
     a.vb = std::min(row_granule(W, d_out, es), row_granule(nullptr, w_stride, es));
     a.out = out; a.ldo = ldo;
     a.go = row_granule(out, ldo, es);
-    a.vo = dtype != RTMA_F32 && a.go >= 16 && make_store_map(&a.map_o, dtype, out, n, N, ldo, 64);
+    a.vo = dtype != RTMA_F32 && a.go >= 16 && make_store_map(&a.map_o, dtype, out, n, N, ldo);
     // Matrices with rows on other boundaries are laid out on 16-byte ones first if a block would copy them more than once: 1M x 256 -> 47
     // in bf16 208 -> 126 us, its dx 261 -> 175; 32,000 rows 16.5 -> 15.1 and 17.9 -> 14.9; for a tile or less per block it is a launch more.
     const bool pad = dtype != RTMA_F32 && a.vb < 16 && a.tiles > ctx->sm_count;
@@ -682,7 +680,7 @@ extern "C" int32_t rtma_grouped_linear_dw(rtma_ctx* ctx, int32_t dtype, int64_t 
     RTMA_TRY(prepare_row_call(ctx, 256 + sizeof(float) * slot_rows * a.ldo, stream));
     a.chunk_rows = reinterpret_cast<int32_t*>(ctx->arena);
     a.out = ctx->arena + 256;
-    a.vo = dtype != RTMA_F32 && slot_rows < (int64_t(1) << 31) && make_store_map(&a.map_o, RTMA_F32, a.out, slot_rows, a.ldo, a.ldo, 64);
+    a.vo = dtype != RTMA_F32 && slot_rows < (int64_t(1) << 31) && make_store_map(&a.map_o, RTMA_F32, a.out, slot_rows, a.ldo, a.ldo);
     if (n > 0) RTMA_TRY(launch_linear<WEIGHT_GRADIENT>(ctx, dtype, a, KC_GEMM_WGRAD, stream));
     {
         KernelScope ks(ctx, KC_REDUCE_SGD, stream);

@@ -165,14 +165,15 @@ __device__ __forceinline__ void add_eight(float (&sums)[8], const float (&v)[8])
     for (int j = 0; j < 8; ++j) sums[j] += v[j];
 }
 
-// A drain warp's results on their way out: ROW bytes of each of its 32 rows (a row per lane) at a time go through one of its slabs,
-// in the map's swizzle of ROW bytes, so that they leave as one bulk-tensor store; boxes that would reach rows or columns that are
+// A drain warp's results on their way out: 64 bytes of each of its 32 rows (a row per lane) at a time go through one of its slabs,
+// in the map's 64-byte swizzle, so that they leave as one bulk-tensor store; boxes that would reach rows or columns that are
 // not this tile's, and rows off the 16-byte boundaries, are written by the lanes.
-template <class O, int SLABS, int ROW>
+template <class O, int SLABS>
 struct Outlet {
+    static constexpr int ROW = 64;
     uint32_t slabs;
     int at = 0;
-    __device__ __forceinline__ static int swizzle(int row) { return ROW == 64 ? (row >> 1) & 3 : (row >> 2) & 1; }
+    __device__ __forceinline__ static int swizzle(int row) { return (row >> 1) & 3; }
     // row0, c: place in the map; rows, cols: how much is this tile's; whole: all columns of the matrix from c on are, and end on a
     // 16-byte boundary (a store's box is cut off at the edge of the matrix only in steps of 16 bytes)
     __device__ __forceinline__ void put(const LinearArgs& a, const float (&v)[32], int64_t row0, int c, int rows, int cols, bool whole, O* out, int64_t ldo, int lane) {

@@ -445,6 +445,94 @@ def test_products_of_fp32_rows_are_fp32_products(ctx, K):
     assert off.mean().abs() < 8 * U and off.abs().max() < (n + 16) * 2 * U
 
 
+# Enough rows that every block works on several tiles and chunks, and that unaligned 16-bit matrices are laid out first.
+# d_in, d_out, elements between the rows of X and of dY: rows on 16-byte boundaries with a width that does not end on one, off them, ...
+MANY_CASES = [(256, 47, 0, 0), (47, 90, 0, 6), (100, 256, 4, 0), (101, 256, 3, 8), (512, 512, 0, 0), (33, 300, 0, 4), (130, 62, 6, 2)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d_in,d_out,pad,pad_out", MANY_CASES)
+def test_grouped_products_of_many_rows(ctx, dtype, d_in, d_out, pad, pad_out):
+    sizes = [21_000, 0, 17, 33_333, 128, 6_000]
+    o, off = offsets_of(sizes, 3)
+    n, G = o[-1] + 5, len(sizes)
+    host, x, _ = make_rows(n, d_in, dtype, 1, pad)
+    dhost, dy, _ = make_rows(n, d_out, dtype, 2, pad_out)
+    W = (torch.randn(G, d_in, d_out, generator=gen(3)) / math.sqrt(d_in)).to(dtype).cuda()
+    b = torch.randn(G, d_out, generator=gen(4)).to(dtype).cuda()
+    X, D, W64, b64 = host.cuda().to(F64), dhost.cuda().to(F64), W.to(F64), b.to(F64)
+    y = torch.full((n, d_out), 7.0, dtype=dtype, device="cuda")
+    dx = torch.full((n, d_in), 7.0, dtype=dtype, device="cuda")
+    ctx.grouped_linear(x, off, W, b, out=y)
+    ctx.grouped_linear_dx(dy, off, W, out=dx)
+    dw, db = ctx.grouped_linear_dw(x, dy, off)
+    for t in (y, dx):
+        assert (t[:o[0]] == 7).all() and (t[o[-1]:] == 7).all()
+
+    def close(got, want, size, steps, what, rounded):
+        tol = steps * 2 * U * size + (rounding(want, dtype) if rounded else 0)
+        worst = ((got.to(F64) - want).abs() / tol.clamp_min(1e-300)).max() if got.numel() else torch.zeros(())
+        assert worst <= 1, f"{what}: {worst.item():.3g} tolerances"
+
+    for g, (lo, hi) in enumerate(zip(o, o[1:])):
+        xs, ds = X[lo:hi], D[lo:hi]
+        close(y[lo:hi], xs @ W64[g] + b64[g], xs.abs() @ W64[g].abs() + b64[g].abs(), d_in + 16, f"y {g}", True)
+        close(dx[lo:hi], ds @ W64[g].T, ds.abs() @ W64[g].T.abs(), d_out + 16, f"dx {g}", True)
+        close(dw[g], xs.T @ ds, xs.T.abs() @ ds.abs(), hi - lo + 16, f"dW {g}", False)
+        close(db[g], ds.sum(0), ds.abs().sum(0), hi - lo + 16, f"db {g}", False)
+    ctx.check()
+
+
+def test_a_captured_product_keeps_its_laid_out_matrices():
+    """A matrix that is laid out first lies in the scratch: a capture without it is refused, a replay follows the matrix."""
+    ctx = binding.Context(0)
+    x = torch.randn(40_000, 64, generator=gen(1)).half().cuda()
+    W = torch.randn(64, 47, generator=gen(2)).half().cuda()
+    with pytest.raises(binding.RtmaError, match="before the capture"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            ctx.grouped_linear(x, None, W)
+    ctx.grouped_linear(x, None, W)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = ctx.grouped_linear(x, None, W)
+    W.mul_(2)
+    ctx.grouped_linear_dw(x, x, None)  # other contents, and more of them
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(y, ctx.grouped_linear(x, None, W))
+    ctx.check()
+
+
+def test_more_than_two_to_the_31_elements(ctx):
+    """The rows of the last part lie behind 2^31 elements and give what they give alone."""
+    d, few = 512, 700
+    n = 2 ** 31 // d + 300 + few
+    last = torch.randn(few, d, generator=gen(1)).half().cuda()
+    x = torch.zeros(n, d, dtype=torch.float16, device="cuda")
+    x[-few:] = last
+    off = torch.tensor([0, n - few, n], dtype=torch.int64, device="cuda")
+    W = torch.randn(2, d, 24, generator=gen(2)).half().cuda()
+    y = ctx.grouped_linear(x, off, W)
+    assert torch.equal(y[-few:], ctx.grouped_linear(last, None, W[1])) and not y[:-few].any()
+    ones = torch.ones_like(y)
+    dw, _ = ctx.grouped_linear_dw(x, ones, off)
+    alone, _ = ctx.grouped_linear_dw(last, ones[-few:], None)
+    assert not dw[0].any() and (dw[1] - alone[0]).abs().max() <= (few + 16) * 2 * U * last.abs().float().sum(0).max()
+    out = ctx.grouped_linear_dx(y, off, W)
+    assert torch.equal(out[-few:], ctx.grouped_linear_dx(y[-few:].contiguous(), None, W[1])) and not out[:-few].any()
+    ids = torch.zeros(n, dtype=torch.int32, device="cuda")  # one id many times: one mask
+    ids[-few:] = torch.arange(few, dtype=torch.int32, device="cuda")
+    ctx.dropout(x, 0.5, 9, row_ids=ids, out=out)
+    assert torch.equal(out[-few:], ctx.dropout(last, 0.5, 9)) and not out[:-few].any()
+    ctx.group_norm(x, off, 4, act="silu", out=out)
+    assert torch.equal(out[-few:], ctx.group_norm(last, None, 4, act="silu")[0]) and not out[:-few].any()
+    ctx.group_norm(x, off, 4, scope="part", out=out)
+    want = ctx.group_norm(last, None, 4, scope="part")[0]
+    assert (out[-few:].float() - want.float()).abs().max() <= 2 * half_step(torch.float16) * want.abs().max() and not out[:-few].any()
+    ctx.check()
+
+
 # ---- all of them ----------------------------------------------------------------------------------------
 
 
