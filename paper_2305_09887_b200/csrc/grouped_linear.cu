@@ -11,10 +11,11 @@
 // registers, rounded to nearest.  The column sums of dY are a product as well, with a left operand of ones: added up by the drain
 // warps from shared memory they cost more than all else that these do (1M x 128 x 256 in fp16: 239 us then, 164 like this and with what came after).
 //
-// This file: 16-bit rows (fp32 ones are in grouped_split.cu).  Two ways of loading:
+// This file: 16-bit rows (fp32 ones are in grouped_split.cu).  Three ways of loading:
 //   COPIES  rows of an operand do not all lie on 16-byte boundaries: three or four groups of 4 warps with asynchronous copies of 8 or 4
 //           bytes (or plain loads of 2), bulk-tensor loads for the other operand
 //   BULK    rows on 16-byte boundaries: one thread with bulk-tensor loads
+//   PAIR    the same on pairs of blocks (a cluster of two, MMAs of 256 rows) that bring half of the right operand each
 // then 8 drain warps (a quarter of the lanes, every second 32 columns each) and one warp that issues the MMAs.
 #include <algorithm>
 
@@ -26,7 +27,7 @@ namespace {
 
 using namespace grouped;
 
-enum Loading { COPIES, BULK };
+enum Loading { COPIES, BULK, PAIR };
 
 constexpr int BM = 128, BK = 64;
 // Registers a thread.  COPIES is launched with 72 in the weight gradient (28 warps), otherwise with 80 (24 warps); the multiplier's
@@ -40,7 +41,8 @@ constexpr int BIAS_ROWS = 1;               // of a slot: column sums of dY
 template <class T, int MODE, int LOADING>
 struct Form {
     static constexpr int BN = MODE == WEIGHT_GRADIENT ? 128 : 256;                                // widest tile
-    static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128;
+    static constexpr bool PAIRED = LOADING == PAIR;
+    static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128 / (PAIRED ? 2 : 1);               // in one block
     static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
     // the results of a tile leave while the next is drained, which is worth more than another stage
     static constexpr int RING_BYTES = (MODE == WEIGHT_GRADIENT ? 160 : 144) * 1024;
@@ -55,8 +57,9 @@ struct Form {
     static constexpr bool A_ACROSS = MODE == WEIGHT_GRADIENT, B_ACROSS = MODE != INPUT_GRADIENT;  // MN-major
     // Of four warps that do nothing else.  Not more than stages: a group could be two rounds of the ring ahead of the multiplier, where
     // the parity of a barrier's phase says nothing.
-    static constexpr int LOAD_GROUPS = LOADING == BULK ? 0 : STAGES < 4 ? STAGES : 4;
+    static constexpr int LOAD_GROUPS = LOADING != COPIES ? 0 : STAGES < 4 ? STAGES : 4;
     static constexpr int LOAD_WARPS = 4 * LOAD_GROUPS;
+    using Walks = Walk<MODE, BM, BK, PAIRED>;
     static constexpr int THREADS = 32 * (DRAIN_WARPS + LOAD_WARPS + 4);
 };
 
@@ -265,13 +268,55 @@ __device__ __forceinline__ void bulk_role(const LinearArgs& a, Shared& sh, uint8
     }
 }
 
+// A pair of blocks: each loads its own rows and its half of the right operand's columns, announced and counted on the first block's
+// barrier (the other's bytes may land before the announcement: the phase still lacks its arrival).
+template <class T, int MODE>
+__device__ __forceinline__ void pair_role(const LinearArgs& a, Shared& sh, uint8_t* ring, int rank) {
+    typedef Form<T, MODE, PAIR> F;
+    tc::prefetch_tensormap(&a.map_a);
+    tc::prefetch_tensormap(&a.map_b);
+    typename F::Walks w;
+    tc::RingAt at;
+    int filled = 0;  // stages, F::STAGES at most
+    bool ok = true;
+    for (bool more = w.first(a, sh); more; more = w.next(a, sh), at.advance(F::STAGES)) {
+        if (!wait_for<true>(&sh.empty[at.s], at.phase ^ 1u, sh, a.error_word)) {
+            ok = false;
+            break;
+        }
+        filled = min(filled + 1, F::STAGES);
+        uint8_t* stage = ring + at.s * F::STAGE_BYTES;
+        if (rank == 0) tc::mbar_arrive_expect_tx(&sh.full[at.s], 2 * F::STAGE_BYTES);
+        const uint32_t bar = tc::leader_addr(&sh.full[at.s]);
+        const int z = a.w_stride ? w.part : 0, n0 = w.n0 + rank * (F::BN / 2);
+        tc::tma_load_3d_pair(stage, &a.map_a, bar, w.k0, (int)w.row0, 0);
+        if constexpr (MODE == FORWARD) {
+            for (int i = 0; i < 2; ++i) tc::tma_load_3d_pair(stage + F::A_BYTES + 2 * i * SLAB_BYTES, &a.map_b, bar, n0 + 64 * i, w.k0, z);
+        } else {
+            tc::tma_load_3d_pair(stage + F::A_BYTES, &a.map_b, bar, w.k0, n0, z);
+        }
+    }
+    // No signal stays under way: every stage filled is waited for until both blocks have it back or, after a give-up, until its loads
+    // have landed (the first block, for both).
+    for (int n = 0; n < filled; ++n) {
+        // the oldest first: `filled` stages back, of the round before where that is behind the ring's start
+        const int back = filled - n, s = (at.s - back + F::STAGES) % F::STAGES;
+        const uint32_t parity = s < at.s ? at.phase : at.phase ^ 1u;
+        if (!ok || !wait_for<true>(&sh.empty[s], parity, sh, a.error_word)) {
+            ok = false;
+            if (rank == 0)
+                for (uint32_t i = 0; i < (1u << 14) && !tc::mbar_try_wait_cluster(&sh.full[s], parity); ++i) {}
+        }
+    }
+}
+
 // A stage's MMAs, by one warp.
 template <class T, int MODE, int LOADING>
 __device__ __forceinline__ void multiply_stage(const LinearArgs& a, uint32_t d, uint32_t stage, int terms, uint32_t accumulate, uint32_t ones) {
     typedef Form<T, MODE, LOADING> F;
     const uint32_t format = std::is_same<T, __half>::value ? 0u : 1u;  // fp16 or bf16 operands, fp32 sums
     const uint32_t idesc = (1u << 4) | (format << 7) | (format << 10) | ((F::A_ACROSS ? 1u : 0u) << 15) | ((F::B_ACROSS ? 1u : 0u) << 16) |
-                           ((uint32_t)(a.BN >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
+                           ((uint32_t)(a.BN >> 3) << 17) | ((uint32_t)((F::PAIRED ? 2 * BM : BM) >> 4) << 24);
     const uint64_t desc = tc::smem_desc_sw128(0, 2 * SLAB_BYTES, 1024);  // atoms of 64 columns lie two slabs apart
     constexpr uint32_t a_step = F::A_ACROSS ? 128 : 2, b_step = F::B_ACROSS ? 128 : 2;  // 16 terms further, in units of 16 bytes
     constexpr uint32_t a_plane = F::A_BYTES >> 4;
@@ -279,7 +324,10 @@ __device__ __forceinline__ void multiply_stage(const LinearArgs& a, uint32_t d, 
     const int steps = (terms + 15) >> 4;
 #pragma unroll
     for (int k = 0; k < BK / 16; ++k)
-        if (k < steps) tc::mma_by_warp(d, da + k * a_step, db + k * b_step, idesc, k ? 1u : accumulate);
+        if (k < steps) {
+            if constexpr (F::PAIRED) tc::mma_pair_by_warp(d, da + k * a_step, db + k * b_step, idesc, k ? 1u : accumulate);
+            else tc::mma_by_warp(d, da + k * a_step, db + k * b_step, idesc, k ? 1u : accumulate);
+        }
     if (MODE == WEIGHT_GRADIENT && ones) {  // 128 rows of ones, all from the same 1024 bytes
         const uint64_t one = tc::smem_desc_sw128(ones, 0, 0);
 #pragma unroll
@@ -291,29 +339,33 @@ __device__ __forceinline__ void multiply_stage(const LinearArgs& a, uint32_t d, 
 template <class T, int MODE, int LOADING>
 __device__ __forceinline__ void multiply_role(const LinearArgs& a, Shared& sh, uint32_t ring, uint32_t ones) {
     typedef Form<T, MODE, LOADING> F;
-    Walk<MODE, BM, BK> w;
+    typename F::Walks w;
     tc::RingAt at, acc;
     int held = 0;  // stages in the accumulator
+    auto commit = [](uint64_t* bar) {
+        if constexpr (F::PAIRED) tc::commit_pair_by_warp(bar);
+        else tc::commit_by_warp(bar);
+    };
     for (bool more = w.first(a, sh); more; more = w.next(a, sh)) {
-        if (held == 0 && !wait_for(&sh.acc_empty[acc.s], acc.phase ^ 1u, sh, a.error_word)) return;
-        if (!wait_for(&sh.full[at.s], at.phase, sh, a.error_word)) return;
+        if (held == 0 && !wait_for<F::PAIRED>(&sh.acc_empty[acc.s], acc.phase ^ 1u, sh, a.error_word)) return;
+        if (!wait_for<F::PAIRED>(&sh.full[at.s], at.phase, sh, a.error_word)) return;
         tc::tc_fence_after_sync();
         __syncwarp();
         multiply_stage<T, MODE, LOADING>(a, sh.tmem_base + acc.s * F::ACC_COLUMNS, ring + at.s * F::STAGE_BYTES, min(BK, w.k_end - w.k0), held ? 1u : 0u,
                                          a.db && w.m0 == 0 ? ones : 0u);
-        tc::commit_by_warp(&sh.empty[at.s]);
+        commit(&sh.empty[at.s]);
         at.advance(F::STAGES);
         if (++held == F::ACC_STAGES || w.last_stage()) {
             held = 0;
-            tc::commit_by_warp(&sh.acc_full[acc.s]);
+            commit(&sh.acc_full[acc.s]);
             acc.advance(2);
         }
     }
 }
 
 // 32 columns (chunk `chunk` of the tile) of a warp's 32 rows (its quarter of the tile's) to the result.
-template <class T, int MODE, class OUT>
-__device__ __forceinline__ void put_chunk(const LinearArgs& a, const Walk<MODE, BM, BK>& w, OUT& outlet, const float (&v)[32], int quarter, int chunk, int lane) {
+template <class T, int MODE, class W, class OUT>
+__device__ __forceinline__ void put_chunk(const LinearArgs& a, const W& w, OUT& outlet, const float (&v)[32], int quarter, int chunk, int lane) {
     typedef typename std::conditional<MODE == WEIGHT_GRADIENT, float, T>::type O;
     const int N = MODE == INPUT_GRADIENT ? a.d_in : MODE == FORWARD ? a.d_out : (int)a.ldo;  // (dw: the slots' rows are padded)
     const int c = w.n0 + 32 * chunk, cols = min(min(32, a.BN - 32 * chunk), N - c);
@@ -332,7 +384,7 @@ __device__ __forceinline__ void drain_role(const LinearArgs& a, Shared& sh, uint
     BiasHolder<T> bias{sh.bias + 128 * warp};
     const uint32_t tmem = sh.tmem_base + ((uint32_t)(32 * quarter) << 16);
     const int chunks = (a.BN + 31) / 32;
-    Walk<MODE, BM, BK> w;
+    typename F::Walks w;
     tc::RingAt acc;
     for (bool more = w.first(a, sh); more; more = w.next_tile(a, sh)) {
         if constexpr (MODE == WEIGHT_GRADIENT) {
@@ -345,7 +397,7 @@ __device__ __forceinline__ void drain_role(const LinearArgs& a, Shared& sh, uint
             for (int j = 0; j < 16; ++j) sums[j] = 0.f;
             const bool sums_wanted = a.db && w.m0 == 0 && 16 * warp < a.BN;
             for (int k0 = 0; k0 < w.k_end; k0 += F::ACC_STAGES * BK) {
-                if (!wait_for(&sh.acc_full[acc.s], acc.phase, sh, a.error_word)) return;
+                if (!wait_for<F::PAIRED>(&sh.acc_full[acc.s], acc.phase, sh, a.error_word)) return;
                 __syncwarp();
                 tc::tc_fence_after_sync();
                 const uint32_t from = tmem + acc.s * F::ACC_COLUMNS;
@@ -386,7 +438,7 @@ __device__ __forceinline__ void drain_role(const LinearArgs& a, Shared& sh, uint
                 if (half + 2 * i < chunks) put_chunk<T, MODE>(a, w, outlet, total[i], quarter, half + 2 * i, lane);
         } else {
             if (MODE == FORWARD && a.bias) bias.fetch(a, w.part, w.n0, half, 2, chunks, lane);
-            if (!wait_for(&sh.acc_full[acc.s], acc.phase, sh, a.error_word)) return;
+            if (!wait_for<F::PAIRED>(&sh.acc_full[acc.s], acc.phase, sh, a.error_word)) return;
             __syncwarp();
             tc::tc_fence_after_sync();
             for (int chunk = half; chunk < chunks; chunk += 2) {
@@ -397,7 +449,10 @@ __device__ __forceinline__ void drain_role(const LinearArgs& a, Shared& sh, uint
             }
             tc::tc_fence_before_sync();
             __syncwarp();
-            if (lane == 0) tc::mbar_arrive(&sh.acc_empty[acc.s]);
+            if (lane == 0) {  // (a pair's warps all report to the first block)
+                if constexpr (F::PAIRED) tc::mbar_arrive_remote(tc::leader_addr(&sh.acc_empty[acc.s]));
+                else tc::mbar_arrive(&sh.acc_empty[acc.s]);
+            }
             acc.advance(2);
         }
     }
@@ -405,7 +460,7 @@ __device__ __forceinline__ void drain_role(const LinearArgs& a, Shared& sh, uint
 }
 
 template <class T, int MODE, int LOADING>
-__global__ void __launch_bounds__(Form<T, MODE, LOADING>::THREADS, 1) linear_kernel(const __grid_constant__ LinearArgs a) {
+__device__ __forceinline__ void linear_body(const LinearArgs& a) {
     typedef Form<T, MODE, LOADING> F;
     static_assert(F::DYNAMIC_BYTES + sizeof(Shared) <= SMEM_MOST && F::STAGES <= MAX_STAGES, "shared memory of a block");
     extern __shared__ uint8_t raw[];
@@ -416,19 +471,24 @@ __global__ void __launch_bounds__(Form<T, MODE, LOADING>::THREADS, 1) linear_ker
     constexpr int MULTIPLIER = F::DRAIN_WARPS + F::LOAD_WARPS;
     if (threadIdx.x == 0) {
         for (int s = 0; s < F::STAGES; ++s) {
-            tc::mbar_init(&sh.full[s], LOADING == BULK ? 1 : 4);
+            tc::mbar_init(&sh.full[s], LOADING == COPIES ? 4 : 1);
             tc::mbar_init(&sh.empty[s], 1);
         }
         for (int b = 0; b < 2; ++b) {
             tc::mbar_init(&sh.acc_full[b], 1);
-            tc::mbar_init(&sh.acc_empty[b], F::DRAIN_WARPS);
+            tc::mbar_init(&sh.acc_empty[b], (F::PAIRED ? 2 : 1) * F::DRAIN_WARPS);  // a pair's first block counts the warps of both
         }
         sh.abort = 0;
         tc::fence_barrier_init();
     }
     if (warp == MULTIPLIER) {
-        tc::tmem_alloc(&sh.tmem_base, 2 * F::ACC_COLUMNS);
-        tc::tmem_relinquish();
+        if constexpr (F::PAIRED) {
+            tc::tmem_alloc_pair(&sh.tmem_base, 2 * F::ACC_COLUMNS);
+            tc::tmem_relinquish_pair();
+        } else {
+            tc::tmem_alloc(&sh.tmem_base, 2 * F::ACC_COLUMNS);
+            tc::tmem_relinquish();
+        }
     }
     if (MODE == WEIGHT_GRADIENT && threadIdx.x < 64) {
         const uint32_t one = std::is_same<T, __half>::value ? 0x3C003C00u : 0x3F803F80u;
@@ -439,7 +499,9 @@ __global__ void __launch_bounds__(Form<T, MODE, LOADING>::THREADS, 1) linear_ker
     lay_out<MODE, F::THREADS, BK>(a, sh);
     tc::tc_fence_before_sync();
     __syncthreads();
+    if constexpr (F::PAIRED) tc::cluster_sync();  // both blocks' barriers and tensor memory exist before either is signalled
     tc::tc_fence_after_sync();
+    const int rank = F::PAIRED ? (int)tc::cluster_rank() : 0;
     if (warp < F::DRAIN_WARPS) {
         if constexpr (LOADING == COPIES) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(DRAIN_REGISTERS));
         drain_role<T, MODE, LOADING>(a, sh, slabs);
@@ -451,18 +513,31 @@ __global__ void __launch_bounds__(Form<T, MODE, LOADING>::THREADS, 1) linear_ker
         }
     } else {
         if constexpr (LOADING == COPIES) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(MULTIPLY_REGISTERS));
-        if (warp == MULTIPLIER) multiply_role<T, MODE, LOADING>(a, sh, ring, ones);
+        if (warp == MULTIPLIER && rank == 0) multiply_role<T, MODE, LOADING>(a, sh, ring, ones);
         if constexpr (LOADING == BULK)
             if (warp == MULTIPLIER + 1) bulk_role<T, MODE>(a, sh, ring_bytes, lane);
+        if constexpr (F::PAIRED)
+            if (warp == MULTIPLIER + 1 && lane == 0) pair_role<T, MODE>(a, sh, ring_bytes, rank);
     }
     __syncwarp();
     if (*reinterpret_cast<volatile int*>(&sh.abort)) __nanosleep(1000000);  // a wait ran out: copies and MMAs under way land before the block ends
     tc::tc_fence_before_sync();
     __syncthreads();
+    if constexpr (F::PAIRED) tc::cluster_sync();  // neither block leaves while the other may still signal it or read its operands
     if (warp == MULTIPLIER) {
         tc::tc_fence_after_sync();
-        tc::tmem_dealloc(sh.tmem_base, 2 * F::ACC_COLUMNS);
+        if constexpr (F::PAIRED) tc::tmem_dealloc_pair(sh.tmem_base, 2 * F::ACC_COLUMNS);
+        else tc::tmem_dealloc(sh.tmem_base, 2 * F::ACC_COLUMNS);
     }
+}
+
+template <class T, int MODE, int LOADING>
+__global__ void __launch_bounds__(Form<T, MODE, LOADING>::THREADS, 1) linear_kernel(const __grid_constant__ LinearArgs a) {
+    linear_body<T, MODE, LOADING>(a);
+}
+template <class T, int MODE>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Form<T, MODE, PAIR>::THREADS, 1) linear_pair_kernel(const __grid_constant__ LinearArgs a) {
+    linear_body<T, MODE, PAIR>(a);
 }
 
 // The slots of every part added up in order.  A block takes 128 neighbouring places of a slot, its warps every eighth slot each; the
@@ -542,18 +617,21 @@ int32_t pad_matrices(rtma_ctx* ctx, LinearArgs& a, cudaStream_t stream) {
 
 template <class T, int MODE, int LOADING>
 int32_t launch_form(rtma_ctx* ctx, const LinearArgs& a, unsigned grid, bool& configured, cudaStream_t stream) {
+    void (*kernel)(LinearArgs);
+    if constexpr (LOADING == PAIR) kernel = linear_pair_kernel<T, MODE>;
+    else kernel = linear_kernel<T, MODE, LOADING>;
     if (!configured) {
-        RTMA_CUDA(ctx, cudaFuncSetAttribute(linear_kernel<T, MODE, LOADING>, cudaFuncAttributeMaxDynamicSharedMemorySize, Form<T, MODE, LOADING>::DYNAMIC_BYTES));
+        RTMA_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Form<T, MODE, LOADING>::DYNAMIC_BYTES));
         configured = true;
     }
-    launch_kernel(linear_kernel<T, MODE, LOADING>, grid, Form<T, MODE, LOADING>::THREADS, Form<T, MODE, LOADING>::DYNAMIC_BYTES, stream, a);
+    launch_kernel(kernel, grid, Form<T, MODE, LOADING>::THREADS, Form<T, MODE, LOADING>::DYNAMIC_BYTES, stream, a);
     RTMA_LAUNCH_CHECK(ctx);
     return RTMA_OK;
 }
 
-// Whether both operands can be fetched by bulk-tensor loads; sets up their maps.
+// Which operands bulk-tensor loads can fetch (1: the left one, 2: the right one); sets up their maps.
 template <int MODE>
-int bulk_maps(LinearArgs& a, bool bf16) {  // 1: the left operand, 2: the right one
+int bulk_maps(LinearArgs& a, bool bf16, bool pair) {
     int in_bulk = 0;
     if (a.va >= 16) {
         const bool ok = MODE == WEIGHT_GRADIENT ? make_tensor_map_16bit(&a.map_a, bf16, a.A, 1, a.n, a.d_in, a.lda, a.n * a.lda, BK)
@@ -563,7 +641,7 @@ int bulk_maps(LinearArgs& a, bool bf16) {  // 1: the left operand, 2: the right 
     if (a.vb >= 16 && a.w_stride >= 0) {
         const bool ok = MODE == WEIGHT_GRADIENT ? make_tensor_map_16bit(&a.map_b, bf16, a.B, 1, a.n, a.d_out, a.ldb, a.n * a.ldb, BK)
                                                 : make_tensor_map_16bit(&a.map_b, bf16, a.B, a.w_stride ? a.G : 1, a.d_in, a.d_out, a.ldb,
-                                                                        a.w_stride ? a.w_stride : a.d_in * a.ldb, MODE == FORWARD ? BK : a.BN);
+                                                                        a.w_stride ? a.w_stride : a.d_in * a.ldb, MODE == FORWARD ? BK : pair ? a.BN / 2 : a.BN);
         in_bulk |= ok ? 2 : 0;
     }
     return in_bulk;
@@ -579,7 +657,23 @@ int32_t launch_linear(rtma_ctx* ctx, int32_t dtype, LinearArgs& a, int cls, cuda
     bool* configured = ctx->linear_configured + MODE * 4;
     KernelScope ks(ctx, cls, stream);
     const bool bf16 = dtype == RTMA_BF16;
-    a.in_bulk = bulk_maps<MODE>(a, bf16);
+    // Pairs of blocks where the contraction is deep: each then brings half of the right operand, which comes from the L2 cache again for
+    // every tile (bf16, alone / in pairs: 500,000 x 512 -> 512 285 / 270 us, 30,000 rows 35 / 27; 1M x 256 -> 256 181 / 170, 30,000 rows
+    // 17 / 14).  Short contractions are drains, which a pair's blocks wait for together: 1M x 64 -> 256 123 / 133.
+    bool pair = false;
+    if constexpr (MODE != WEIGHT_GRADIENT) pair = a.BN == 256 && (MODE == FORWARD ? a.d_in : a.d_out) >= 256 && tiles >= ctx->sm_count;
+    a.in_bulk = bulk_maps<MODE>(a, bf16, pair);
+    if constexpr (MODE != WEIGHT_GRADIENT) {
+        if (pair && a.in_bulk == 3) {
+            a.tile_rows = 2 * BM;
+            a.tiles = a.n / a.tile_rows + a.G;
+            const int64_t blocks = 2 * a.tiles * a.n_tiles, places = ctx->sm_count & ~1;
+            bool* once = ctx->linear_configured + 12 + (MODE == FORWARD ? 0 : 2);
+            return bf16 ? launch_form<__nv_bfloat16, MODE, PAIR>(ctx, a, (unsigned)std::min(blocks, places), once[0], stream)
+                        : launch_form<__half, MODE, PAIR>(ctx, a, (unsigned)std::min(blocks, places), once[1], stream);
+        }
+        if (pair) a.in_bulk = 0;  // (the right operand's map is one for pairs)
+    }
     if (a.in_bulk == 3)
         return bf16 ? launch_form<__nv_bfloat16, MODE, BULK>(ctx, a, grid, configured[0], stream) : launch_form<__half, MODE, BULK>(ctx, a, grid, configured[1], stream);
     return bf16 ? launch_form<__nv_bfloat16, MODE, COPIES>(ctx, a, grid, configured[2], stream) : launch_form<__half, MODE, COPIES>(ctx, a, grid, configured[3], stream);

@@ -51,9 +51,11 @@ struct Shared {
     alignas(16) float bias[8 * 128];  // of every drain warp's columns
 };
 
+// CLUSTER: the barrier may be signalled from the pair's other block
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, Shared& sh, int* error_word) {
     for (uint32_t i = 0; i < tc::WAIT_POLLS; ++i) {
-        if (tc::mbar_try_wait(bar, parity)) return true;
+        if (CLUSTER ? tc::mbar_try_wait_cluster(bar, parity) : tc::mbar_try_wait(bar, parity)) return true;
         if ((i & 1023u) == 1023u && *reinterpret_cast<volatile int*>(&sh.abort)) break;
     }
     *reinterpret_cast<volatile int*>(&sh.abort) = 1;
@@ -61,8 +63,9 @@ __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, Shared&
     return false;
 }
 
-// A role's walk over a block's tiles and their stages.
-template <int MODE, int BM, int BK>
+// A role's walk over a block's tiles and their stages.  PAIR: two blocks of a cluster share tiles of 2 BM rows, of which each sees its
+// own BM (the second none or fewer where the part ends).
+template <int MODE, int BM, int BK, bool PAIR = false>
 struct Walk {
     int tile, part, row_tile, m0, n0;  // part: set before `at`, to one that is not behind the tile's
     int64_t row0;     // first row of the tile
@@ -88,12 +91,16 @@ struct Walk {
         const int64_t inside = (int64_t)(row_tile - sh.tile_start[part]) * sh.tile_rows;
         row0 = sh.begin[part] + inside;
         rows = (int)min((int64_t)sh.rows[part] - inside, (int64_t)sh.tile_rows);
+        if (PAIR) {
+            row0 += BM * (blockIdx.x & 1);
+            rows -= BM * (int)(blockIdx.x & 1);
+        }
         k_end = MODE == FORWARD ? a.d_in : MODE == INPUT_GRADIENT ? a.d_out : rows;
         k0 = 0;
         return true;
     }
     __device__ __forceinline__ bool first(const LinearArgs& a, const Shared& sh) {
-        tile = blockIdx.x;
+        tile = blockIdx.x >> PAIR;
         part = 0;
         return at(a, sh);
     }
@@ -103,11 +110,11 @@ struct Walk {
             k0 += BK;
             return true;
         }
-        tile += gridDim.x;
+        tile += gridDim.x >> PAIR;
         return at(a, sh);
     }
     __device__ __forceinline__ bool next_tile(const LinearArgs& a, const Shared& sh) {
-        tile += gridDim.x;
+        tile += gridDim.x >> PAIR;
         return at(a, sh);
     }
 };
@@ -241,9 +248,12 @@ struct Outlet {
 // The bias of a warp's columns (chunks c, c + step, ... of 32), in shared memory.
 template <class T>
 struct BiasHolder {
-    float* at;  // 16-byte boundary
-    __device__ __forceinline__ void fetch(const LinearArgs& a, int part, int n0, int c, int step, int chunks, int lane) const {
+    float* at;                 // 16-byte boundary
+    const T* held = nullptr;   // of which columns: a block's tiles have the same ones most of the time
+    __device__ __forceinline__ void fetch(const LinearArgs& a, int part, int n0, int c, int step, int chunks, int lane) {
         const T* bias = static_cast<const T*>(a.bias) + part * a.bias_stride + n0;
+        if (bias == held) return;
+        held = bias;
         __syncwarp();
         for (int chunk = c, i = 0; chunk < chunks; chunk += step, ++i) {
             const int col = 32 * chunk + lane;
