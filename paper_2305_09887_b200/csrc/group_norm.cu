@@ -23,6 +23,7 @@ struct NormArgs {
     int G, C, groups, per_set, units, rows_at_once, pitch;  // per_set = C / groups; units of eight channels; rows a block works on at a time;
                                                            // lanes of a row where warps keep rows to themselves (0: they do not)
     bool straddles;  // sets share units, two at most
+    bool wide;       // sets of more than a warp's lanes
     int tile_rows;
     int64_t tiles;   // at most so many
     int act;
@@ -306,20 +307,36 @@ struct Run {
     }
 };
 
-// ---- rows of up to 512 channels whose sets are runs of lanes ---------------------------------------
-// A row lies in `pitch` lanes (a power of two), eight channels each (NP times: channels 8 (lane + 32 p) ..); a set is the whole row or
-// a power of two of neighbouring lanes, so its sums are exchanged within a warp and nothing goes through shared memory.  RB rows
-// side by side hide one another's loads and shuffles.
-template <int N>
-__device__ __forceinline__ void set_sums(float (&x)[N], int lanes) {
-    for (int o = lanes >> 1; o > 0; o >>= 1) {
+// ---- rows whose sets are runs of lanes -------------------------------------------------------------
+// A row lies in `pitch` lanes (a power of two, 256 at most), eight channels each; a set is the whole row or a power of two of
+// neighbouring lanes, so its sums are exchanged within a warp, and only those of sets of more than 256 channels (WIDE) go through
+// shared memory.  RB rows side by side hide one another's loads and shuffles.
+// Sums over `lanes` lanes, in every lane.  WIDE: red, 8 floats per sum, is used by every other call.
+template <bool WIDE, int N>
+__device__ __forceinline__ void set_sums(float (&x)[N], int lanes, float* red) {
+    for (int o = (WIDE ? 32 : lanes) >> 1; o > 0; o >>= 1) {
 #pragma unroll
         for (int i = 0; i < N; ++i) x[i] += __shfl_xor_sync(0xffffffffu, x[i], o);
     }
+    if constexpr (WIDE) {
+        const int warp = threadIdx.x >> 5, first = warp & ~(lanes / 32 - 1);
+        if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) red[8 * i + warp] = x[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            x[i] = 0.f;
+            for (int w = first; w < first + lanes / 32; ++w) x[i] += red[8 * i + w];
+        }
+    }
 }
 
-template <class T, int NP, int RB, bool FULL>
+template <class T, bool FULL, bool WIDE>
 __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_kernel(const NormArgs a) {
+    constexpr int RB = 4;  // rows in flight
+    __shared__ float red[2][8 * RB];
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
     wait_for_kernel_before();
     number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums);
@@ -327,102 +344,76 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_kernel(const N
     const bool whole = a.groups == 1;
     const int lanes = whole ? pitch : a.per_set / 8, lanes_log = 31 - __clz(lanes);  // of a set
     const float inv = 1.f / (float)a.per_set;
-    const T* X = static_cast<const T*>(a.X);
-    T* Y = static_cast<T*>(a.Y);
-    int valid[NP];
-#pragma unroll
-    for (int p = 0; p < NP; ++p) valid[p] = max(0, min(8, a.C - 8 * (u + 32 * p)));
+    const int valid = max(0, min(8, a.C - 8 * u));
     for (int tile = blockIdx.x; tile < tile_start[a.G]; tile += gridDim.x) {
         const Run run(a, tile_start, tile);
-        f2 gam[NP][4], bet[NP][4];
-#pragma unroll
-        for (int p = 0; p < NP; ++p) {
-            load_params(a.gamma, a.gamma_stride, run.part, u + 32 * p, valid[p], 1.f, gam[p]);
-            load_params(a.beta, a.beta_stride, run.part, u + 32 * p, valid[p], 0.f, bet[p]);
-        }
+        f2 gam[4], bet[4];
+        load_params(a.gamma, a.gamma_stride, run.part, u, valid, 1.f, gam);
+        load_params(a.beta, a.beta_stride, run.part, u, valid, 0.f, bet);
         const float slope = a.slope ? __ldg(a.slope + run.part * a.slope_stride) : 0.f;
-        Eight<T> raw[RB][NP];  // the next rows are on their way while these are worked on
+        Eight<T> raw[RB];  // the next rows are on their way while these are worked on
         int left = (int)(run.end - run.begin), asked = left - y;  // rows from this step's first on; from this lane's next request on
-        const T* x = X + (run.begin + y) * a.ldx + 8 * u;
-        T* out = Y + (run.begin + y) * a.ldy + 8 * u;
+        const T* x = static_cast<const T*>(a.X) + (run.begin + y) * a.ldx + 8 * u;
+        T* out = static_cast<T*>(a.Y) + (run.begin + y) * a.ldy + 8 * u;
         int64_t r = run.begin + y;
         const int64_t x_step = rows_at_once * a.ldx, out_step = rows_at_once * a.ldy;
         auto request = [&]() {
 #pragma unroll
-            for (int b = 0; b < RB; ++b) {
-#pragma unroll
-                for (int p = 0; p < NP; ++p) load_unit<FULL>(raw[b][p], x + 256 * p, b * rows_at_once < asked, valid[p], a.vx);
-                x += x_step;
-            }
+            for (int b = 0; b < RB; ++b, x += x_step) load_unit<FULL>(raw[b], x, b * rows_at_once < asked, valid, a.vx);
             asked -= RB * rows_at_once;
         };
         request();
         for (; left > 0; left -= RB * rows_at_once) {  // the same number of times in every lane
-            f2 v[RB][NP][4];
-            float mean[RB * NP], rstd[RB * NP];
+            f2 v[RB][4];
+            float mean[RB], rstd[RB];
 #pragma unroll
-            for (int b = 0; b < RB; ++b)
-#pragma unroll
-                for (int p = 0; p < NP; ++p) pairs_of(raw[b][p], v[b][p]);
+            for (int b = 0; b < RB; ++b) pairs_of(raw[b], v[b]);
             request();
 #pragma unroll
-            for (int b = 0; b < RB; ++b) {
-#pragma unroll
-                for (int p = 0; p < NP; ++p)  // what is not there reads as zero
-                    mean[b * NP + p] = halves_sum(add2(add2(v[b][p][0], v[b][p][1]), add2(v[b][p][2], v[b][p][3])));
-                if (NP == 2 && whole) mean[b * NP] = mean[b * NP + NP - 1] = mean[b * NP] + mean[b * NP + NP - 1];
-            }
-            set_sums(mean, lanes);
+            for (int b = 0; b < RB; ++b) mean[b] = halves_sum(add2(add2(v[b][0], v[b][1]), add2(v[b][2], v[b][3])));  // what is not there reads as zero
+            set_sums<WIDE>(mean, lanes, red[0]);
 #pragma unroll
             for (int b = 0; b < RB; ++b) {
+                mean[b] *= inv;
+                const f2 minus = pack2(-mean[b], -mean[b]);
+                f2 q = 0ull;
 #pragma unroll
-                for (int p = 0; p < NP; ++p) {
-                    mean[b * NP + p] *= inv;
-                    const f2 minus = pack2(-mean[b * NP + p], -mean[b * NP + p]);
-                    f2 q = 0ull;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        v[b][p][i] = add2(v[b][p][i], minus);
-                        f2 t = v[b][p][i];
-                        if (!FULL && valid[p] < 8) {  // channels that are not there do not count
-                            float t0, t1;
-                            unpack2(t, t0, t1);
-                            t = pack2(2 * i < valid[p] ? t0 : 0.f, 2 * i + 1 < valid[p] ? t1 : 0.f);
-                        }
-                        q = fma2(t, t, q);
+                for (int i = 0; i < 4; ++i) {
+                    v[b][i] = add2(v[b][i], minus);
+                    f2 t = v[b][i];
+                    if (!FULL && valid < 8) {  // channels that are not there do not count
+                        float t0, t1;
+                        unpack2(t, t0, t1);
+                        t = pack2(2 * i < valid ? t0 : 0.f, 2 * i + 1 < valid ? t1 : 0.f);
                     }
-                    rstd[b * NP + p] = halves_sum(q);
+                    q = fma2(t, t, q);
                 }
-                if (NP == 2 && whole) rstd[b * NP] = rstd[b * NP + NP - 1] = rstd[b * NP] + rstd[b * NP + NP - 1];
+                rstd[b] = halves_sum(q);
             }
-            set_sums(rstd, lanes);
+            set_sums<WIDE>(rstd, lanes, red[1]);
 #pragma unroll
-            for (int i = 0; i < RB * NP; ++i) rstd[i] = inverse_root(fmaf(rstd[i], inv, a.eps));
+            for (int b = 0; b < RB; ++b) rstd[b] = inverse_root(fmaf(rstd[b], inv, a.eps));
 #pragma unroll
             for (int b = 0; b < RB; ++b, out += out_step, r += rows_at_once) {
-                if (y + b * rows_at_once >= left) continue;
-                const uint32_t id = a.drop.threshold ? id_of(a, r) : 0u;
+                if (y + b * rows_at_once >= left || (!FULL && valid == 0)) continue;
+                if (a.stats && (u & (lanes - 1)) == 0)
+                    *reinterpret_cast<float2*>(a.stats + 2 * (r * a.groups + (u >> lanes_log))) = make_float2(mean[b], rstd[b]);
+                const f2 r2 = pack2(rstd[b], rstd[b]);
 #pragma unroll
-                for (int p = 0; p < NP; ++p) {
-                    const int unit = u + 32 * p;
-                    if (!FULL && valid[p] == 0) continue;
-                    if (a.stats && (whole ? unit == 0 : (unit & (lanes - 1)) == 0))
-                        *reinterpret_cast<float2*>(a.stats + 2 * (r * a.groups + (whole ? 0 : unit >> lanes_log))) = make_float2(mean[b * NP + p], rstd[b * NP + p]);
-                    const f2 r2 = pack2(rstd[b * NP + p], rstd[b * NP + p]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) v[b][p][i] = fma2(mul2(v[b][p][i], r2), gam[p][i], bet[p][i]);
-                    activate(a.act, slope, v[b][p]);
-                    if (a.drop.threshold) drop_pairs(a.drop, id, unit, v[b][p]);
-                    store_unit<FULL>(out + 256 * p, v[b][p], valid[p], a.vy);
-                }
+                for (int i = 0; i < 4; ++i) v[b][i] = fma2(mul2(v[b][i], r2), gam[i], bet[i]);
+                activate(a.act, slope, v[b]);
+                if (a.drop.threshold) drop_pairs(a.drop, id_of(a, r), u, v[b]);
+                store_unit<FULL>(out, v[b], valid, a.vy);
             }
         }
     }
 }
 
-template <class T, int NP, int RB, bool FULL>
+template <class T, bool FULL, bool WIDE>
 __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_grad_kernel(const NormArgs a) {
+    constexpr int RB = 2;  // rows in flight
     __shared__ float shared[8 * NORM_THREADS];
+    __shared__ float red[2][16 * RB];
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
     wait_for_kernel_before();
     number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums);
@@ -430,111 +421,85 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_grad_kernel(co
     const bool whole = a.groups == 1;
     const int lanes = whole ? pitch : a.per_set / 8, lanes_log = 31 - __clz(lanes);
     const float inv = 1.f / (float)a.per_set;
-    const T* X = static_cast<const T*>(a.X);
-    const T* dY = static_cast<const T*>(a.dY);
-    T* Y = static_cast<T*>(a.Y);
-    int valid[NP];
-#pragma unroll
-    for (int p = 0; p < NP; ++p) valid[p] = max(0, min(8, a.C - 8 * (u + 32 * p)));
+    const int valid = max(0, min(8, a.C - 8 * u));
+    int turn = 0;
     for (int tile = blockIdx.x; tile < tile_start[a.G]; tile += gridDim.x) {
         const Run run(a, tile_start, tile);
-        f2 gam[NP][4], bet[NP][4], sb[NP][4], sg[NP][4];
+        f2 gam[4], bet[4], sb[4], sg[4];
         float ds = 0.f;
+        load_params(a.gamma, a.gamma_stride, run.part, u, valid, 1.f, gam);
+        load_params(a.beta, a.beta_stride, run.part, u, valid, 0.f, bet);
 #pragma unroll
-        for (int p = 0; p < NP; ++p) {
-            load_params(a.gamma, a.gamma_stride, run.part, u + 32 * p, valid[p], 1.f, gam[p]);
-            load_params(a.beta, a.beta_stride, run.part, u + 32 * p, valid[p], 0.f, bet[p]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sb[p][i] = sg[p][i] = 0ull;
-        }
+        for (int i = 0; i < 4; ++i) sb[i] = sg[i] = 0ull;
         const float slope = a.slope ? __ldg(a.slope + run.part * a.slope_stride) : 0.f;
-        Eight<T> rx[RB][NP], rd[RB][NP];
-        float2 rs[RB][NP];
+        Eight<T> rx[RB], rd[RB];
+        float2 rs[RB];
         int left = (int)(run.end - run.begin), asked = left - y;
-        const T* x = X + (run.begin + y) * a.ldx + 8 * u;
-        const T* dy = dY + (run.begin + y) * a.lddy + 8 * u;
-        const float* stat = a.stats + 2 * ((run.begin + y) * a.groups + (whole ? 0 : u >> lanes_log));
-        T* out = Y + (run.begin + y) * a.ldy + 8 * u;
+        const T* x = static_cast<const T*>(a.X) + (run.begin + y) * a.ldx + 8 * u;
+        const T* dy = static_cast<const T*>(a.dY) + (run.begin + y) * a.lddy + 8 * u;
+        const float* stat = a.stats + 2 * ((run.begin + y) * a.groups + (u >> lanes_log));
+        T* out = static_cast<T*>(a.Y) + (run.begin + y) * a.ldy + 8 * u;
         int64_t r = run.begin + y;
         const int64_t x_step = rows_at_once * a.ldx, dy_step = rows_at_once * a.lddy, out_step = rows_at_once * a.ldy;
         const int stat_step = 2 * rows_at_once * a.groups;
         auto request = [&]() {
 #pragma unroll
-            for (int b = 0; b < RB; ++b) {
+            for (int b = 0; b < RB; ++b, x += x_step, dy += dy_step, stat += stat_step) {
                 const bool here = b * rows_at_once < asked;
-#pragma unroll
-                for (int p = 0; p < NP; ++p) {
-                    load_unit<FULL>(rx[b][p], x + 256 * p, here, valid[p], a.vx);
-                    load_unit<FULL>(rd[b][p], dy + 256 * p, here, valid[p], a.vdy);
-                    rs[b][p] = here && (FULL || valid[p]) ? *reinterpret_cast<const float2*>(stat + (whole ? 0 : 2 * (32 >> lanes_log) * p)) : make_float2(0.f, 0.f);
-                }
-                x += x_step;
-                dy += dy_step;
-                stat += stat_step;
+                load_unit<FULL>(rx[b], x, here, valid, a.vx);
+                load_unit<FULL>(rd[b], dy, here, valid, a.vdy);
+                rs[b] = here && (FULL || valid) ? *reinterpret_cast<const float2*>(stat) : make_float2(0.f, 0.f);
             }
             asked -= RB * rows_at_once;
         };
         request();
         for (; left > 0; left -= RB * rows_at_once) {
-            f2 xh[RB][NP][4], du[RB][NP][4];
-            float s12[2 * RB * NP], rstd[RB][NP];  // sums over the set of gamma du, and of gamma du xhat
-            Standard<T> st[RB][NP];
+            f2 xh[RB][4], du[RB][4];
+            float s12[2 * RB], rstd[RB];  // sums over the set of gamma du, and of gamma du xhat
+            Standard<T> st[RB];
 #pragma unroll
-            for (int b = 0; b < RB; ++b)
-#pragma unroll
-                for (int p = 0; p < NP; ++p) {
-                    pairs_of(rx[b][p], xh[b][p]);
-                    pairs_of(rd[b][p], du[b][p]);
-                    st[b][p].set(rs[b][p].x, rs[b][p].y, rs[b][p].x, rs[b][p].y);
-                    rstd[b][p] = rs[b][p].y;
-                }
+            for (int b = 0; b < RB; ++b) {
+                pairs_of(rx[b], xh[b]);
+                pairs_of(rd[b], du[b]);
+                st[b].set(rs[b].x, rs[b].y, rs[b].x, rs[b].y);
+                rstd[b] = rs[b].y;
+            }
             request();
 #pragma unroll
             for (int b = 0; b < RB; ++b) {
-                const uint32_t id = a.drop.threshold && y + b * rows_at_once < left ? id_of(a, r + b * rows_at_once) : 0u;
+                if (a.drop.threshold) drop_pairs(a.drop, y + b * rows_at_once < left ? id_of(a, r + b * rows_at_once) : 0u, u, du[b]);
+                f2 pre[4];
 #pragma unroll
-                for (int p = 0; p < NP; ++p) {
-                    if (a.drop.threshold) drop_pairs(a.drop, id, u + 32 * p, du[b][p]);
-                    f2 pre[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        xh[b][p][i] = st[b][p](xh[b][p][i]);
-                        pre[i] = fma2(xh[b][p][i], gam[p][i], bet[p][i]);
-                    }
-                    ds += activate_back(a.act, slope, pre, du[b][p]);
-                    f2 t1 = 0ull, t2 = 0ull;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        sb[p][i] = add2(sb[p][i], du[b][p][i]);
-                        sg[p][i] = fma2(du[b][p][i], xh[b][p][i], sg[p][i]);
-                        du[b][p][i] = mul2(du[b][p][i], gam[p][i]);
-                        t1 = add2(t1, du[b][p][i]);
-                        t2 = fma2(du[b][p][i], xh[b][p][i], t2);
-                    }
-                    s12[2 * (b * NP + p)] = halves_sum(t1);
-                    s12[2 * (b * NP + p) + 1] = halves_sum(t2);
+                for (int i = 0; i < 4; ++i) {
+                    xh[b][i] = st[b](xh[b][i]);
+                    pre[i] = fma2(xh[b][i], gam[i], bet[i]);
                 }
-                if (NP == 2 && whole) {
-                    s12[2 * b * NP] = s12[2 * b * NP + 2 * (NP - 1)] = s12[2 * b * NP] + s12[2 * b * NP + 2 * (NP - 1)];
-                    s12[2 * b * NP + 1] = s12[2 * b * NP + 2 * NP - 1] = s12[2 * b * NP + 1] + s12[2 * b * NP + 2 * NP - 1];
+                ds += activate_back(a.act, slope, pre, du[b]);
+                f2 t1 = 0ull, t2 = 0ull;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    sb[i] = add2(sb[i], du[b][i]);
+                    sg[i] = fma2(du[b][i], xh[b][i], sg[i]);
+                    du[b][i] = mul2(du[b][i], gam[i]);
+                    t1 = add2(t1, du[b][i]);
+                    t2 = fma2(du[b][i], xh[b][i], t2);
                 }
+                s12[2 * b] = halves_sum(t1);
+                s12[2 * b + 1] = halves_sum(t2);
             }
-            set_sums(s12, lanes);
+            set_sums<WIDE>(s12, lanes, red[turn]);
+            turn ^= 1;
 #pragma unroll
             for (int b = 0; b < RB; ++b, out += out_step, r += rows_at_once) {
-                if (y + b * rows_at_once >= left) continue;
+                if (y + b * rows_at_once >= left || (!FULL && valid == 0)) continue;
+                const float n1 = -inv * s12[2 * b], n2 = -inv * s12[2 * b + 1];
+                const f2 m1 = pack2(n1, n1), m2 = pack2(n2, n2), r2 = pack2(rstd[b], rstd[b]);
 #pragma unroll
-                for (int p = 0; p < NP; ++p) {
-                    const float n1 = -inv * s12[2 * (b * NP + p)], n2 = -inv * s12[2 * (b * NP + p) + 1];
-                    const f2 m1 = pack2(n1, n1), m2 = pack2(n2, n2), r2 = pack2(rstd[b][p], rstd[b][p]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) du[b][p][i] = mul2(r2, fma2(xh[b][p][i], m2, add2(du[b][p][i], m1)));
-                    if (FULL || valid[p]) store_unit<FULL>(out + 256 * p, du[b][p], valid[p], a.vy);
-                }
+                for (int i = 0; i < 4; ++i) du[b][i] = mul2(r2, fma2(xh[b][i], m2, add2(du[b][i], m1)));
+                store_unit<FULL>(out, du[b], valid, a.vy);
             }
         }
-#pragma unroll
-        for (int p = 0; p < NP; ++p) leave_sums(a, tile, 8 * (u + 32 * p), y, pitch, rows_at_once, sb[p], sg[p], shared);
+        leave_sums(a, tile, 8 * u, y, pitch, rows_at_once, sb, sg, shared);
         leave_slope(a, tile, ds, shared);
     }
 }
@@ -1353,10 +1318,11 @@ NormArgs norm_args(const rtma_ctx* ctx, const rtma_norm_desc* d, int64_t n, int3
     a.rows_at_once = NORM_THREADS / a.units;
     // warps keep rows to themselves where a set is a power of two of lanes or the whole row, or two sets at most share a unit
     const int lanes = a.per_set / 8;
-    const bool of_lanes = d->groups == 1 || (a.per_set % 8 == 0 && lanes <= 32 && (lanes & (lanes - 1)) == 0);
+    const bool of_lanes = d->groups == 1 || (a.per_set % 8 == 0 && (lanes & (lanes - 1)) == 0);
     a.straddles = !of_lanes && a.per_set >= 8 && d->C <= 256;
-    if (d->scope == RTMA_SCOPE_ROW && d->C <= 512 && (of_lanes || a.straddles))
-        for (a.pitch = 1; a.pitch < std::min(a.units, 32);) a.pitch *= 2;
+    if (d->scope == RTMA_SCOPE_ROW && (of_lanes || a.straddles))
+        for (a.pitch = 1; a.pitch < a.units;) a.pitch *= 2;
+    a.wide = a.pitch > 32 && a.per_set > 256;
     cut_rows(a, ctx, 4);
     a.act = d->act;
     a.eps = d->eps;
@@ -1403,8 +1369,8 @@ extern "C" int32_t rtma_group_norm(rtma_ctx* ctx, const rtma_norm_desc* d, int64
         const bool full = full_units(a, d->dtype, false);
         auto kernel = !a.pitch ? NORM_KERNEL(norm_rows_kernel)
                       : a.straddles ? (full ? NORM_KERNEL(norm_straddle_rows_kernel, , true) : NORM_KERNEL(norm_straddle_rows_kernel, , false))
-                      : a.units <= 32 ? (full ? NORM_KERNEL(norm_warp_rows_kernel, , 1, 4, true) : NORM_KERNEL(norm_warp_rows_kernel, , 1, 4, false))
-                                      : (full ? NORM_KERNEL(norm_warp_rows_kernel, , 2, 2, true) : NORM_KERNEL(norm_warp_rows_kernel, , 2, 2, false));
+                      : a.wide ? (full ? NORM_KERNEL(norm_warp_rows_kernel, , true, true) : NORM_KERNEL(norm_warp_rows_kernel, , false, true))
+                               : (full ? NORM_KERNEL(norm_warp_rows_kernel, , true, false) : NORM_KERNEL(norm_warp_rows_kernel, , false, false));
         KernelScope ks(ctx, KC_POST, stream);
         launch_kernel(kernel, grid, NORM_THREADS, a.pitch ? 0 : smem, stream, a);
     } else {
@@ -1467,8 +1433,8 @@ extern "C" int32_t rtma_group_norm_grad(rtma_ctx* ctx, const rtma_norm_desc* d, 
             const bool full = full_units(a, d->dtype, true);
             auto kernel = !a.pitch ? NORM_KERNEL(norm_rows_grad_kernel)
                           : a.straddles ? (full ? NORM_KERNEL(norm_straddle_rows_grad_kernel, , true) : NORM_KERNEL(norm_straddle_rows_grad_kernel, , false))
-                          : a.units <= 32 ? (full ? NORM_KERNEL(norm_warp_rows_grad_kernel, , 1, 2, true) : NORM_KERNEL(norm_warp_rows_grad_kernel, , 1, 2, false))
-                                          : (full ? NORM_KERNEL(norm_warp_rows_grad_kernel, , 2, 1, true) : NORM_KERNEL(norm_warp_rows_grad_kernel, , 2, 1, false));
+                          : a.wide ? (full ? NORM_KERNEL(norm_warp_rows_grad_kernel, , true, true) : NORM_KERNEL(norm_warp_rows_grad_kernel, , false, true))
+                                   : (full ? NORM_KERNEL(norm_warp_rows_grad_kernel, , true, false) : NORM_KERNEL(norm_warp_rows_grad_kernel, , false, false));
             launch_kernel(kernel, (unsigned)tiles, NORM_THREADS, a.pitch ? 0 : smem, stream, a);
         } else {
             launch_kernel(full_units(a, d->dtype, true) ? NORM_KERNEL(norm_grad_sums_kernel, , true) : NORM_KERNEL(norm_grad_sums_kernel, , false), (unsigned)tiles, NORM_THREADS, 0, stream, a);

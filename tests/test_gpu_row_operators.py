@@ -116,6 +116,7 @@ NORM_CASES = [
     # sizes of the parts, C, groups
     ([1], 8, 1), ([1], 2, 1), ([7, 0, 1, 30], 64, 8), ([130, 3], 47, 47), ([130, 3], 47, 1), ([64, 200], 100, 4), ([33, 0], 90, 9),
     ([37, 0, 90], 240, 10), ([61, 5], 250, 2), ([3, 300], 54, 6), ([40, 1], 27, 3), ([200], 144, 16), ([9, 50], 300, 3), ([20, 30], 12, 3),
+    ([30, 7], 1536, 3), ([21], 1000, 1), ([40, 0, 9], 2048, 8), ([25, 3], 600, 1), ([90, 4], 64, 32), ([33], 36, 9), ([5, 70], 12, 12),
     ([50, 60], 256, 32), ([70], 512, 1), ([9, 12], 1024, 8), ([5, 9], 2048, 2), ([0, 0], 32, 4), ([2500], 24, 3), ([40, 50], 384, 1),
 ]
 
