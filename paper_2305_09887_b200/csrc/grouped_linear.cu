@@ -9,7 +9,7 @@
 // The tensor cores truncate when they accumulate, so a long sum drifts towards zero by half a step per addition.  The weight
 // gradient, whose result is fp32, therefore has its drain warps take the accumulator after every 128 rows and add it up in
 // registers, rounded to nearest.  The column sums of dY are a product as well, with a left operand of ones: added up by the drain
-// warps from shared memory they cost more than all else that these do (1M x 128 x 256 in fp16: 239 us then, 164 like this and with what came after).
+// warps from shared memory they cost more than all else that these do (1M x 128 x 256 in fp16: 239 us; like this and with what came after it 161).
 //
 // This file: 16-bit rows (fp32 ones are in grouped_split.cu).  Three ways of loading:
 //   COPIES  rows of an operand do not all lie on 16-byte boundaries: three or four groups of 4 warps with asynchronous copies of 8 or 4
@@ -17,6 +17,11 @@
 //   BULK    rows on 16-byte boundaries: one thread with bulk-tensor loads
 //   PAIR    the same on pairs of blocks (a cluster of two, MMAs of 256 rows) that bring half of the right operand each
 // then 8 drain warps (a quarter of the lanes, every second 32 columns each) and one warp that issues the MMAs.
+//
+// What bounds it: up to 256 terms the rows' bytes (dx of 2M x 256 -> 256 in bf16 324 us, 6.3 TB/s), above that the operands' way from the
+// L2 cache (500,000 x 512 -> 512 260 to 270 us, 1 PFLOP/s; 200,000 x 1024 -> 1024 356 us, 1.18); the weight gradient reads each row of X and dY
+// once per 128 columns of the other (1M x 256 x 256 in bf16 320 to 335 us), and shared memory, from which an MMA of 128 x 128 reads 128
+// bytes a clock; rows off 16-byte boundaries the copies (1M x 100 x 256 in fp16 200 to 230 us, 1M x 47 -> 90 in bf16 150).
 #include <algorithm>
 
 #include "grouped_linear.cuh"
@@ -541,7 +546,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Form<T, MODE, PAIR>:
 }
 
 // The slots of every part added up in order.  A block takes 128 neighbouring places of a slot, its warps every eighth slot each; the
-// row behind the weights is the bias's, whose partial sums lie in bias_rows rows.
+// row behind the weights is the bias's, whose partial sums lie in bias_rows rows (added up one after the other by one thread each they
+// took 414 us for 16 parts; so, the kernel takes 10).
 constexpr int REDUCE_THREADS = 256;
 __global__ void __launch_bounds__(REDUCE_THREADS) linear_reduce_kernel(const __grid_constant__ LinearArgs a) {
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
@@ -586,7 +592,7 @@ void cut_columns(LinearArgs& a, int N, int widest) {
     a.n_tiles = (int)ceil_div(N, a.BN);
 }
 
-// 16-bit matrices whose rows do not lie on 16-byte boundaries -> [part][d_in][ld] that do (ld: d_out rounded up to 8)
+// A few us: 16-bit matrices whose rows do not lie on 16-byte boundaries -> [part][d_in][ld] that do (ld: d_out rounded up to 8)
 __global__ void __launch_bounds__(256) pad_matrices_kernel(const __half* __restrict__ W, int64_t w_stride, int parts, int d_in, int d_out, int granule,
                                                            __half* __restrict__ out) {
     wait_for_kernel_before();
