@@ -406,7 +406,8 @@ int32_t rtma_group_norm(rtma_ctx* ctx, const rtma_norm_desc* desc, int64_t n, in
                         const float* beta, const float* slope, const int32_t* row_ids, void* Y,
                         int64_t ldy, float* stats, void* stream);
 /* The gradient, from the forward call's X and stats: dX of dY, and (each may be NULL) dgamma, dbeta
- * [C] and dslope [1] per part, with strides of their own; stride 0 with G > 1: summed over the parts.
+ * [C] and dslope [1] per part, with strides of their own (those of two parts must not overlap); stride 0
+ * with G > 1: summed over the parts.
  * At u = 0 ReLU and PReLU take the derivative of the negative side.  dX may be dY or X.        */
 int32_t rtma_group_norm_grad(rtma_ctx* ctx, const rtma_norm_desc* desc, int64_t n, int32_t G,
                              const int64_t* offsets, const void* X, int64_t ldx, const void* dY,

@@ -24,6 +24,7 @@ struct NormArgs {
                                                            // lanes of a row where warps keep rows to themselves (0: they do not)
     bool straddles;  // sets share units, two at most
     bool wide;       // sets of more than a warp's lanes
+    int within;      // sets of 1, 2 or 4 channels, which share units but do not straddle them; otherwise 0
     int tile_rows;
     int64_t tiles;   // at most so many
     int act;
@@ -162,8 +163,9 @@ __device__ __forceinline__ float lane_sum(float x, int lanes) {
 }
 
 // ---- statistics of a row ---------------------------------------------------------------------------
-// Any sets, of any size, through shared memory: those of less than eight channels that are more than one per row, and uneven ones in
-// rows of more than 256.  Far from memory's pace, for the block waits for all its rows twice: 1M x 64 in 32 sets, bf16, 435 us, gradient 645.
+// Any sets, of any size, through shared memory: those of 3, 5, 6 or 7 channels, and of other widths than a power of two times eight in rows
+// of more than 256.  Far from memory's pace, for the block waits for all its rows twice: 500,000 x 60 in 20 sets, bf16, 188 us,
+// gradient 300; 500,000 x 300 in 3 sets, fp16, 853 and 1408.
 __device__ __forceinline__ int row_pitch(const NormArgs& a) { return a.units * 8; }
 
 template <class T>
@@ -730,6 +732,166 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_straddle_rows_grad_kerne
     }
 }
 
+// ---- rows whose sets lie within units --------------------------------------------------------------
+// Sets of P = 1, 2 or 4 channels: a lane has all of a set, nothing is exchanged.  (Channels that are not there are whole sets.)
+// 1M x 64 in 32 sets, bf16, 127 us, gradient 130 (through shared memory 435 and 645); 200,000 x 128 in 32 sets, fp32, 47 and 73.
+template <int P>
+__device__ __forceinline__ void sums_within(f2 (&x)[4]) {  // every channel's set's sum
+#pragma unroll
+    for (int i = 0; i < 4; i += P == 4 ? 2 : 1) {
+        if constexpr (P >= 2) {
+            const float s = halves_sum(P == 4 ? add2(x[i], x[i + (P == 4)]) : x[i]);
+            x[i] = x[i + (P == 4)] = pack2(s, s);
+        }
+    }
+}
+
+template <class T, int P, bool FULL>
+__global__ void __launch_bounds__(NORM_THREADS, 2) norm_unit_rows_kernel(const NormArgs a) {
+    constexpr int RB = 2;  // rows in flight
+    __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
+    wait_for_kernel_before();
+    number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums);
+    const int pitch = a.pitch, u = threadIdx.x & (pitch - 1), y = threadIdx.x / pitch, rows_at_once = NORM_THREADS / pitch;
+    const int valid = max(0, min(8, a.C - 8 * u));
+    const f2 inv = pack2(1.f / P, 1.f / P), minus = pack2(-1.f, -1.f);
+    for (int tile = blockIdx.x; tile < tile_start[a.G]; tile += gridDim.x) {
+        const Run run(a, tile_start, tile);
+        f2 gam[4], bet[4];
+        load_params(a.gamma, a.gamma_stride, run.part, u, valid, 1.f, gam);
+        load_params(a.beta, a.beta_stride, run.part, u, valid, 0.f, bet);
+        const float slope = a.slope ? __ldg(a.slope + run.part * a.slope_stride) : 0.f;
+        Eight<T> raw[RB];
+        int left = (int)(run.end - run.begin) - y, asked = left;
+        const T* x = static_cast<const T*>(a.X) + (run.begin + y) * a.ldx + 8 * u;
+        T* out = static_cast<T*>(a.Y) + (run.begin + y) * a.ldy + 8 * u;
+        int64_t r = run.begin + y;
+        const int64_t x_step = rows_at_once * a.ldx, out_step = rows_at_once * a.ldy;
+        auto request = [&]() {
+#pragma unroll
+            for (int b = 0; b < RB; ++b, x += x_step) load_unit<FULL>(raw[b], x, b * rows_at_once < asked && valid, valid, a.vx);
+            asked -= RB * rows_at_once;
+        };
+        request();
+        for (; left > 0; left -= RB * rows_at_once) {
+            f2 v[RB][4];
+#pragma unroll
+            for (int b = 0; b < RB; ++b) pairs_of(raw[b], v[b]);
+            request();
+#pragma unroll
+            for (int b = 0; b < RB; ++b, out += out_step, r += rows_at_once) {
+                if (b * rows_at_once >= left || valid == 0) continue;
+                f2 mean[4], q[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mean[i] = v[b][i];
+                sums_within<P>(mean);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    mean[i] = mul2(mean[i], inv);
+                    v[b][i] = fma2(mean[i], minus, v[b][i]);
+                    q[i] = mul2(v[b][i], v[b][i]);
+                }
+                sums_within<P>(q);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float q0, q1;
+                    unpack2(q[i], q0, q1);
+                    q[i] = pack2(inverse_root(fmaf(q0, 1.f / P, a.eps)), inverse_root(fmaf(q1, 1.f / P, a.eps)));
+                }
+                if (a.stats) {
+                    float2* st = reinterpret_cast<float2*>(a.stats) + r * a.groups + 8 / P * u;
+#pragma unroll
+                    for (int j = 0; j < 8; j += P) {
+                        float m0, m1, s0, s1;
+                        unpack2(mean[j / 2], m0, m1);
+                        unpack2(q[j / 2], s0, s1);
+                        if (j < valid) st[j / P] = make_float2(j & 1 ? m1 : m0, j & 1 ? s1 : s0);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[b][i] = fma2(mul2(v[b][i], q[i]), gam[i], bet[i]);
+                activate(a.act, slope, v[b]);
+                if (a.drop.threshold) drop_pairs(a.drop, id_of(a, r), u, v[b]);
+                store_unit<FULL>(out, v[b], valid, a.vy);
+            }
+        }
+    }
+}
+
+template <class T, int P, bool FULL>
+__global__ void __launch_bounds__(NORM_THREADS, 2) norm_unit_rows_grad_kernel(const NormArgs a) {
+    __shared__ float shared[8 * NORM_THREADS];
+    __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
+    wait_for_kernel_before();
+    number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums);
+    const int pitch = a.pitch, u = threadIdx.x & (pitch - 1), y = threadIdx.x / pitch, rows_at_once = NORM_THREADS / pitch;
+    const int valid = max(0, min(8, a.C - 8 * u));
+    const f2 minus_inv = pack2(-1.f / P, -1.f / P);
+    for (int tile = blockIdx.x; tile < tile_start[a.G]; tile += gridDim.x) {
+        const Run run(a, tile_start, tile);
+        f2 gam[4], bet[4], sb[4], sg[4];
+        float ds = 0.f;
+        load_params(a.gamma, a.gamma_stride, run.part, u, valid, 1.f, gam);
+        load_params(a.beta, a.beta_stride, run.part, u, valid, 0.f, bet);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sb[i] = sg[i] = 0ull;
+        const float slope = a.slope ? __ldg(a.slope + run.part * a.slope_stride) : 0.f;
+        Eight<T> rx, rd;
+        float2 rs[8 / P];
+        int left = (int)(run.end - run.begin) - y, asked = left;
+        const T* x = static_cast<const T*>(a.X) + (run.begin + y) * a.ldx + 8 * u;
+        const T* dy = static_cast<const T*>(a.dY) + (run.begin + y) * a.lddy + 8 * u;
+        const float2* stat = reinterpret_cast<const float2*>(a.stats) + (run.begin + y) * a.groups + 8 / P * u;
+        T* out = static_cast<T*>(a.Y) + (run.begin + y) * a.ldy + 8 * u;
+        int64_t r = run.begin + y;
+        const int64_t x_step = rows_at_once * a.ldx, dy_step = rows_at_once * a.lddy, out_step = rows_at_once * a.ldy;
+        auto request = [&]() {
+            const bool here = asked > 0 && valid;
+            load_unit<FULL>(rx, x, here, valid, a.vx);
+            load_unit<FULL>(rd, dy, here, valid, a.vdy);
+#pragma unroll
+            for (int j = 0; j < 8 / P; ++j) rs[j] = here && j * P < valid ? stat[j] : make_float2(0.f, 0.f);
+            x += x_step;
+            dy += dy_step;
+            stat += rows_at_once * a.groups;
+            asked -= rows_at_once;
+        };
+        request();
+        for (; left > 0; left -= rows_at_once, out += out_step, r += rows_at_once) {
+            f2 xh[4], du[4], rstd[4], pre[4], t1[4], t2[4];
+            pairs_of(rx, xh);
+            pairs_of(rd, du);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 s0 = rs[2 * i / P], s1 = rs[(2 * i + 1) / P];
+                Standard<T> st;
+                st.set(s0.x, s0.y, s1.x, s1.y);
+                rstd[i] = pack2(s0.y, s1.y);
+                xh[i] = st(xh[i]);
+                pre[i] = fma2(xh[i], gam[i], bet[i]);
+            }
+            request();
+            if (a.drop.threshold) drop_pairs(a.drop, id_of(a, r), u, du);
+            ds += activate_back(a.act, slope, pre, du);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                sb[i] = add2(sb[i], du[i]);
+                sg[i] = fma2(du[i], xh[i], sg[i]);
+                t1[i] = du[i] = mul2(du[i], gam[i]);
+                t2[i] = mul2(du[i], xh[i]);
+            }
+            sums_within<P>(t1);
+            sums_within<P>(t2);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                du[i] = mul2(rstd[i], fma2(xh[i], mul2(t2[i], minus_inv), fma2(t1[i], minus_inv, du[i])));
+            if (valid) store_unit<FULL>(out, du, valid, a.vy);
+        }
+        leave_sums(a, tile, 8 * u, y, pitch, rows_at_once, sb, sg, shared);
+        leave_slope(a, tile, ds, shared);
+    }
+}
+
 template <class T>
 __global__ void __launch_bounds__(NORM_THREADS) norm_rows_grad_kernel(const NormArgs a) {
     extern __shared__ float shared[];
@@ -1287,6 +1449,8 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_reduce_parts_kernel(const N
 
 template <class K>
 K by_type(int32_t dtype, K f32, K bf16, K f16) { return dtype == RTMA_F32 ? f32 : dtype == RTMA_BF16 ? bf16 : f16; }
+// of sets within units
+#define NORM_KERNEL_WITHIN(name, full) (a.within == 1 ? NORM_KERNEL(name, , 1, full) : a.within == 2 ? NORM_KERNEL(name, , 2, full) : NORM_KERNEL(name, , 4, full))
 #define NORM_KERNEL(name, ...) by_type(d->dtype, &name<float __VA_ARGS__>, &name<__nv_bfloat16 __VA_ARGS__>, &name<__half __VA_ARGS__>)
 
 // Runs of rows, per_sm for every SM: twice as many as run at a time, so that all SMs end together.  A few rows per thread at least.
@@ -1299,7 +1463,7 @@ void cut_rows(NormArgs& a, const rtma_ctx* ctx, int per_sm) {
 // Whether every unit of eight channels is there in full, on the boundary of one load: then no load or store asks.
 bool full_units(const NormArgs& a, int32_t dtype, bool gradient) {
     const int most = dtype == RTMA_F32 ? 32 : 16;
-    const bool pieces = a.pitch == 0 || a.straddles || (a.units & (a.units - 1)) == 0;  // (straddling sets) no lane of a row is idle
+    const bool pieces = a.pitch == 0 || a.straddles || a.within || (a.units & (a.units - 1)) == 0;  // no lane of a row is idle, or the kernel asks
     return a.C % 8 == 0 && pieces && a.vx >= most && a.vy >= most && (!gradient || a.vdy >= most);
 }
 
@@ -1332,7 +1496,9 @@ NormArgs norm_args(const rtma_ctx* ctx, const rtma_norm_desc* d, int64_t n, int3
     const int lanes = a.per_set / 8;
     const bool of_lanes = d->groups == 1 || (a.per_set % 8 == 0 && (lanes & (lanes - 1)) == 0);
     a.straddles = !of_lanes && a.per_set >= 8 && d->C <= 256;
-    if (d->scope == RTMA_SCOPE_ROW && (of_lanes || a.straddles))
+    a.within = a.per_set == 1 || a.per_set == 2 || a.per_set == 4 ? a.per_set : 0;
+    if (d->groups == 1) a.within = 0;
+    if (d->scope == RTMA_SCOPE_ROW && (of_lanes || a.straddles || a.within))
         for (a.pitch = 1; a.pitch < a.units;) a.pitch *= 2;
     a.wide = a.pitch > 32 && a.per_set > 256;
     cut_rows(a, ctx, 4);
@@ -1380,6 +1546,7 @@ extern "C" int32_t rtma_group_norm(rtma_ctx* ctx, const rtma_norm_desc* d, int64
         const size_t smem = sizeof(float) * a.rows_at_once * (8 * a.units + 2 * (size_t)a.groups);
         const bool full = full_units(a, d->dtype, false);
         auto kernel = !a.pitch ? NORM_KERNEL(norm_rows_kernel)
+                      : a.within ? (full ? NORM_KERNEL_WITHIN(norm_unit_rows_kernel, true) : NORM_KERNEL_WITHIN(norm_unit_rows_kernel, false))
                       : a.straddles ? (full ? NORM_KERNEL(norm_straddle_rows_kernel, , true) : NORM_KERNEL(norm_straddle_rows_kernel, , false))
                       : a.wide ? (full ? NORM_KERNEL(norm_warp_rows_kernel, , true, true) : NORM_KERNEL(norm_warp_rows_kernel, , false, true))
                                : (full ? NORM_KERNEL(norm_warp_rows_kernel, , true, false) : NORM_KERNEL(norm_warp_rows_kernel, , false, false));
@@ -1417,6 +1584,9 @@ extern "C" int32_t rtma_group_norm_grad(rtma_ctx* ctx, const rtma_norm_desc* d, 
     if (n > 0 && (!X || !dY || !stats || !dX)) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "rtma_group_norm_grad: null pointer");
     if (ldx < d->C || lddy < d->C || lddx < d->C)
         return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "rtma_group_norm_grad: rows of %d channels lie closer than that", d->C);
+    const auto overlap = [&](const float* p, int64_t stride) { return p && G > 1 && stride != 0 && stride < d->C && stride > -d->C; };
+    if (overlap(dgamma, dgamma_stride) || overlap(dbeta, dbeta_stride))
+        return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "rtma_group_norm_grad: gradients of %d channels lie closer than that", d->C);
     if (dslope && d->act != RTMA_ACT_PRELU) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "rtma_group_norm_grad: a slope's gradient without PReLU");
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     DeviceScope on(ctx->device);
@@ -1444,6 +1614,7 @@ extern "C" int32_t rtma_group_norm_grad(rtma_ctx* ctx, const rtma_norm_desc* d, 
             const size_t smem = sizeof(float2) * (8 * NORM_THREADS + (size_t)a.rows_at_once * a.groups);
             const bool full = full_units(a, d->dtype, true);
             auto kernel = !a.pitch ? NORM_KERNEL(norm_rows_grad_kernel)
+                          : a.within ? (full ? NORM_KERNEL_WITHIN(norm_unit_rows_grad_kernel, true) : NORM_KERNEL_WITHIN(norm_unit_rows_grad_kernel, false))
                           : a.straddles ? (full ? NORM_KERNEL(norm_straddle_rows_grad_kernel, , true) : NORM_KERNEL(norm_straddle_rows_grad_kernel, , false))
                           : a.wide ? (full ? NORM_KERNEL(norm_warp_rows_grad_kernel, , true, true) : NORM_KERNEL(norm_warp_rows_grad_kernel, , false, true))
                                    : (full ? NORM_KERNEL(norm_warp_rows_grad_kernel, , true, false) : NORM_KERNEL(norm_warp_rows_grad_kernel, , false, false));

@@ -726,6 +726,7 @@ def test_refusals(ctx):
         (binding.RtmaError, lambda: ctx.group_norm(torch.ones(2, 2049, device="cuda"), None, 1)),
         (ValueError, lambda: ctx.group_norm_grad(x, x, torch.ones(10, 2, 2, device="cuda"), off, 4, g)),
         (binding.RtmaError, lambda: ctx.group_norm_grad(x, x, torch.ones(10, 4, 2, device="cuda"), off, 4, g, dslope=torch.ones(2, device="cuda"))),
+        (binding.RtmaError, lambda: ctx.group_norm_grad(x, x, torch.ones(10, 4, 2, device="cuda"), off, 4, g, dgamma=torch.ones(20, device="cuda").as_strided((2, 16), (4, 1)))),
     ]
     for i, (error, call) in enumerate(refused):
         with pytest.raises(error):
