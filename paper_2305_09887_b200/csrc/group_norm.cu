@@ -1260,10 +1260,11 @@ __global__ void __launch_bounds__(NORM_THREADS, FULL ? 3 : 2) norm_apply_kernel(
 }
 
 // The gradient of part scope in two passes, as the sums over a part have to be complete before any of its rows: 500,000 x 256 in
-// bf16 with SiLU 126 us for the sums, 8 for joining them, 150 for the rows, which work out du again (storing it would cost as many bytes).
+// bf16 with SiLU 262 us, 8 of them for joining the sums; the rows' pass works out du again (storing it would cost as many bytes).  Bound by
+// the loads on their way: with two rows of 16-bit values in flight instead of four 281 us, without an activation 254 (four: 226).
 template <class T, bool FULL>
 __global__ void __launch_bounds__(NORM_THREADS, 2) norm_grad_sums_kernel(const NormArgs a) {
-    constexpr int RB = 2;  // rows in flight
+    constexpr int RB = 8 / sizeof(T);  // rows in flight
     __shared__ float shared[8 * NORM_THREADS];
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
     wait_for_kernel_before();
@@ -1325,7 +1326,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_grad_sums_kernel(const N
 
 template <class T, bool FULL>
 __global__ void __launch_bounds__(NORM_THREADS, 2) norm_grad_apply_kernel(const NormArgs a) {
-    constexpr int RB = 2;
+    constexpr int RB = 8 / sizeof(T);  // rows in flight
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
     __shared__ float2 of_set[NORM_MAX_CHANNELS];
     wait_for_kernel_before();
