@@ -23,7 +23,7 @@ struct NormArgs {
     int G, C, groups, per_set, units, rows_at_once, pitch;  // per_set = C / groups; units of eight channels; rows a block works on at a time;
                                                            // lanes of a row where warps keep rows to themselves (0: they do not)
     bool straddles;  // sets share units, two at most
-    bool wide;       // sets of more than a warp's lanes
+    bool wide;       // a set's lanes are in several warps, or may be
     int within;      // sets of 1, 2 or 4 channels, which share units but do not straddle them; otherwise 0
     int tile_rows;
     int64_t tiles;   // at most so many
@@ -163,9 +163,8 @@ __device__ __forceinline__ float lane_sum(float x, int lanes) {
 }
 
 // ---- statistics of a row ---------------------------------------------------------------------------
-// Any sets, of any size, through shared memory: those of 3, 5, 6 or 7 channels, and of other widths than a power of two times eight in rows
-// of more than 256.  Far from memory's pace, for the block waits for all its rows twice: 500,000 x 60 in 20 sets, bf16, 188 us,
-// gradient 300; 500,000 x 300 in 3 sets, fp16, 853 and 1408.
+// Any sets, of any size, through shared memory; called for those of 3, 5, 6 or 7 channels.  Far from memory's pace, for the block waits for
+// all its rows twice: 500,000 x 60 in 20 sets, bf16, 188 us, gradient 300.
 __device__ __forceinline__ int row_pitch(const NormArgs& a) { return a.units * 8; }
 
 template <class T>
@@ -511,14 +510,16 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_grad_kernel(co
     }
 }
 
-// ---- rows of up to 256 channels whose sets share units ---------------------------------------------
+// ---- rows whose sets share units ---------------------------------------------
 // Sets of eight channels or more that do not end with a unit: a unit's channels belong to one set or to two.  A row lies in `pitch`
 // lanes as above; a set's sum grows from lane to lane in a scan that starts anew where a set begins, is complete in the lane with the
-// set's last channel and fetched from there.  Bound by instructions: 1M x 100 in 4 sets, fp16, 227 us, gradient 283 (through shared memory,
-// by the kernels for all other sets, 550 and 990); 1M x 240 in 10 sets, fp32, 369 and 582.
+// set's last channel and fetched from there.  WIDE: rows of more than 256 channels; the warps' scans are joined in shared memory.  Bound by instructions: 1M x 100 in 4 sets, fp16, 227 us, gradient 283 (through shared memory,
+// by the kernels for all other sets, 550 and 990); 1M x 240 in 10 sets, fp32, 369 and 582.  WIDE by its barriers, too: 500,000 x 300 in
+// 3 sets, fp16, 745 and 888 (853 and 1408), x 384 in 8 sets, fp32, 703 and 787.
 struct Straddle {
     int set, first;   // set of the unit's first channel, how many of its channels are in it
     bool begins, two; // the set begins with the unit; another one begins within it
+    int start;        // the lane where the unit's first set begins
     int back;         // lanes from where the unit's last set begins
     int end0, end1;   // lanes where the two sums are complete
     __device__ __forceinline__ Straddle(const NormArgs& a, int u) {
@@ -528,6 +529,7 @@ struct Straddle {
         const int c0 = set * a.per_set;
         first = there ? min(8, c0 + a.per_set - c) : 8;
         begins = !there || c == c0;
+        start = there ? c0 >> 3 : u;
         two = first < 8 && c + first < a.C;
         back = begins || first < 8 ? 0 : u - (c0 >> 3);
         end0 = there ? (c0 + a.per_set - 1) >> 3 : u;
@@ -547,31 +549,61 @@ struct Straddle {
             hi += (2 * i < first ? 0.f : x) + (2 * i + 1 < first ? 0.f : y);
         }
     }
-    // ... become the sets' sums
-    template <int N>
-    __device__ __forceinline__ void join(float (&lo)[N], float (&hi)[N], int pitch, int far) const {
+    // ... become the sets' sums.  WIDE: ends is 8 floats per sum, sums NORM_THREADS; everything before is read when a call is through.
+    template <bool WIDE, int N>
+    __device__ __forceinline__ void join(float (&lo)[N], float (&hi)[N], int u, int pitch, int far, float* ends, float* sums) const {
+        const int width = WIDE ? 32 : pitch, lane = u & 31, within = WIDE ? min(back, lane) : back;
         float open[N];  // of the set that goes on behind the unit
 #pragma unroll
         for (int i = 0; i < N; ++i) open[i] = first < 8 ? hi[i] : lo[i];
-        for (int o = 1; o <= far; o <<= 1) {
+        for (int o = 1; o <= far && o < 32; o <<= 1) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float x = __shfl_up_sync(0xffffffffu, open[i], o, pitch);
-                if (o <= back) open[i] += x;
+                const float x = __shfl_up_sync(0xffffffffu, open[i], o, width);
+                if (o <= within) open[i] += x;
             }
+        }
+        const int warp = threadIdx.x >> 5, mine = u >> 5, row = warp - mine;  // of the block, of the row; the row's first
+        if constexpr (WIDE) {
+            if (lane == 31) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) ends[8 * i + warp] = open[i];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                for (int w = (u - back) >> 5; w < mine; ++w) open[i] += ends[8 * i + row + w];
         }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float before = __shfl_up_sync(0xffffffffu, open[i], 1, pitch), all = begins ? lo[i] : before + lo[i];
-            lo[i] = __shfl_sync(0xffffffffu, all, end0, pitch);
-            hi[i] = __shfl_sync(0xffffffffu, all, end1, pitch);
+            float before = __shfl_up_sync(0xffffffffu, open[i], 1, width);
+            if (WIDE && lane == 0) {
+                before = 0.f;
+                for (int w = start >> 5; w < mine; ++w) before += ends[8 * i + row + w];
+            }
+            const float all = begins ? lo[i] : before + lo[i];
+            if constexpr (WIDE) {
+                sums[NORM_THREADS * i + threadIdx.x] = all;
+            } else {
+                lo[i] = __shfl_sync(0xffffffffu, all, end0, pitch);
+                hi[i] = __shfl_sync(0xffffffffu, all, end1, pitch);
+            }
+        }
+        if constexpr (WIDE) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                lo[i] = sums[NORM_THREADS * i + threadIdx.x - u + end0];
+                hi[i] = sums[NORM_THREADS * i + threadIdx.x - u + end1];
+            }
         }
     }
 };
 
-template <class T, bool FULL>
+template <class T, bool FULL, bool WIDE>
 __global__ void __launch_bounds__(NORM_THREADS, 2) norm_straddle_rows_kernel(const NormArgs a) {
     constexpr int RB = 2;  // rows in flight
+    __shared__ float ends[WIDE ? 8 * RB : 1], sums[WIDE ? NORM_THREADS * RB : 1];
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
     wait_for_kernel_before();
     number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums);
@@ -606,7 +638,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_straddle_rows_kernel(con
                 sets.part(v[b], mean0[b], mean1[b]);  // (what is not there reads as zero)
             }
             request();
-            sets.join(mean0, mean1, pitch, far);
+            sets.join<WIDE>(mean0, mean1, u, pitch, far, ends, sums);
 #pragma unroll
             for (int b = 0; b < RB; ++b) {
                 mean0[b] *= inv;
@@ -621,7 +653,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_straddle_rows_kernel(con
                 }
                 sets.part(q, rstd0[b], rstd1[b]);
             }
-            sets.join(rstd0, rstd1, pitch, far);
+            sets.join<WIDE>(rstd0, rstd1, u, pitch, far, ends, sums);
 #pragma unroll
             for (int b = 0; b < RB; ++b, out += out_step, r += rows_at_once) {
                 rstd0[b] = inverse_root(fmaf(rstd0[b], inv, a.eps));
@@ -642,9 +674,10 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_straddle_rows_kernel(con
     }
 }
 
-template <class T, bool FULL>
+template <class T, bool FULL, bool WIDE>
 __global__ void __launch_bounds__(NORM_THREADS, 2) norm_straddle_rows_grad_kernel(const NormArgs a) {
     constexpr int RB = 1;  // rows in flight: two do not fit the registers (1M x 100 in 4 sets, fp16: 320 us instead of 283)
+    __shared__ float ends[WIDE ? 16 * RB : 1], sums[WIDE ? 2 * NORM_THREADS * RB : 1];
     __shared__ float shared[8 * NORM_THREADS];
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
     wait_for_kernel_before();
@@ -715,7 +748,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_straddle_rows_grad_kerne
                 sets.part(t, lo[2 * b + 1], hi[2 * b + 1]);
             }
             request();
-            sets.join(lo, hi, pitch, far);
+            sets.join<WIDE>(lo, hi, u, pitch, far, ends, sums);
 #pragma unroll
             for (int b = 0; b < RB; ++b, out += out_step, r += rows_at_once) {
                 if (y + b * rows_at_once >= left || valid == 0) continue;
@@ -1496,12 +1529,12 @@ NormArgs norm_args(const rtma_ctx* ctx, const rtma_norm_desc* d, int64_t n, int3
     // warps keep rows to themselves where a set is a power of two of lanes or the whole row, or two sets at most share a unit
     const int lanes = a.per_set / 8;
     const bool of_lanes = d->groups == 1 || (a.per_set % 8 == 0 && (lanes & (lanes - 1)) == 0);
-    a.straddles = !of_lanes && a.per_set >= 8 && d->C <= 256;
+    a.straddles = !of_lanes && a.per_set >= 8;
     a.within = a.per_set == 1 || a.per_set == 2 || a.per_set == 4 ? a.per_set : 0;
     if (d->groups == 1) a.within = 0;
     if (d->scope == RTMA_SCOPE_ROW && (of_lanes || a.straddles || a.within))
         for (a.pitch = 1; a.pitch < a.units;) a.pitch *= 2;
-    a.wide = a.pitch > 32 && a.per_set > 256;
+    a.wide = a.pitch > 32 && (a.straddles || a.per_set > 256);
     cut_rows(a, ctx, 4);
     a.act = d->act;
     a.eps = d->eps;
@@ -1548,7 +1581,8 @@ extern "C" int32_t rtma_group_norm(rtma_ctx* ctx, const rtma_norm_desc* d, int64
         const bool full = full_units(a, d->dtype, false);
         auto kernel = !a.pitch ? NORM_KERNEL(norm_rows_kernel)
                       : a.within ? (full ? NORM_KERNEL_WITHIN(norm_unit_rows_kernel, true) : NORM_KERNEL_WITHIN(norm_unit_rows_kernel, false))
-                      : a.straddles ? (full ? NORM_KERNEL(norm_straddle_rows_kernel, , true) : NORM_KERNEL(norm_straddle_rows_kernel, , false))
+                      : a.straddles && a.wide ? (full ? NORM_KERNEL(norm_straddle_rows_kernel, , true, true) : NORM_KERNEL(norm_straddle_rows_kernel, , false, true))
+                      : a.straddles ? (full ? NORM_KERNEL(norm_straddle_rows_kernel, , true, false) : NORM_KERNEL(norm_straddle_rows_kernel, , false, false))
                       : a.wide ? (full ? NORM_KERNEL(norm_warp_rows_kernel, , true, true) : NORM_KERNEL(norm_warp_rows_kernel, , false, true))
                                : (full ? NORM_KERNEL(norm_warp_rows_kernel, , true, false) : NORM_KERNEL(norm_warp_rows_kernel, , false, false));
         KernelScope ks(ctx, KC_POST, stream);
@@ -1616,7 +1650,8 @@ extern "C" int32_t rtma_group_norm_grad(rtma_ctx* ctx, const rtma_norm_desc* d, 
             const bool full = full_units(a, d->dtype, true);
             auto kernel = !a.pitch ? NORM_KERNEL(norm_rows_grad_kernel)
                           : a.within ? (full ? NORM_KERNEL_WITHIN(norm_unit_rows_grad_kernel, true) : NORM_KERNEL_WITHIN(norm_unit_rows_grad_kernel, false))
-                          : a.straddles ? (full ? NORM_KERNEL(norm_straddle_rows_grad_kernel, , true) : NORM_KERNEL(norm_straddle_rows_grad_kernel, , false))
+                          : a.straddles && a.wide ? (full ? NORM_KERNEL(norm_straddle_rows_grad_kernel, , true, true) : NORM_KERNEL(norm_straddle_rows_grad_kernel, , false, true))
+                          : a.straddles ? (full ? NORM_KERNEL(norm_straddle_rows_grad_kernel, , true, false) : NORM_KERNEL(norm_straddle_rows_grad_kernel, , false, false))
                           : a.wide ? (full ? NORM_KERNEL(norm_warp_rows_grad_kernel, , true, true) : NORM_KERNEL(norm_warp_rows_grad_kernel, , false, true))
                                    : (full ? NORM_KERNEL(norm_warp_rows_grad_kernel, , true, false) : NORM_KERNEL(norm_warp_rows_grad_kernel, , false, false));
             launch_kernel(kernel, (unsigned)tiles, NORM_THREADS, a.pitch ? 0 : smem, stream, a);

@@ -116,6 +116,7 @@ NORM_CASES = [
     # sizes of the parts, C, groups
     ([1], 8, 1), ([1], 2, 1), ([7, 0, 1, 30], 64, 8), ([130, 3], 47, 47), ([130, 3], 47, 1), ([64, 200], 100, 4), ([33, 0], 90, 9),
     ([37, 0, 90], 240, 10), ([61, 5], 250, 2), ([3, 300], 54, 6), ([40, 1], 27, 3), ([200], 144, 16), ([9, 50], 300, 3), ([20, 30], 12, 3),
+    ([50, 3], 384, 2), ([41], 384, 32), ([30, 1], 2040, 3), ([17, 40], 1020, 17), ([25], 1100, 100), ([19, 2], 700, 2),
     ([30, 7], 1536, 3), ([21], 1000, 1), ([40, 0, 9], 2048, 8), ([25, 3], 600, 1), ([90, 4], 64, 32), ([33], 36, 9), ([5, 70], 12, 12),
     ([50, 60], 256, 32), ([70], 512, 1), ([9, 12], 1024, 8), ([5, 9], 2048, 2), ([0, 0], 32, 4), ([2500], 24, 3), ([40, 50], 384, 1),
 ]
@@ -503,6 +504,39 @@ def test_a_captured_product_keeps_its_laid_out_matrices():
     torch.cuda.synchronize()
     assert torch.equal(y, ctx.grouped_linear(x, None, W))
     ctx.check()
+
+
+@pytest.mark.parametrize("direction", ["y", "dx"])
+def test_deep_products_in_a_graph_and_on_two_streams(direction):
+    """Deep contractions of 16-bit rows run on pairs of blocks; the same bits in a graph, and beside another context's."""
+    one, two = binding.Context(0), binding.Context(0)
+    o, off = offsets_of([12_000, 0, 300, 17_701])
+    x = torch.randn(o[-1], 512, generator=gen(1)).bfloat16().cuda()
+    W = (torch.randn(4, 512, 512, generator=gen(2)) / 20).bfloat16().cuda()
+    b = torch.randn(4, 512, generator=gen(3)).bfloat16().cuda()
+    call = (lambda c, **k: c.grouped_linear(x, off, W, b, **k)) if direction == "y" else (lambda c, **k: c.grouped_linear_dx(x, off, W, **k))
+    want = call(one).clone()
+    x32, W32 = x.float(), W.float()
+    want32 = two.grouped_linear(x32, off, W32).clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call(one)
+    out.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    outs, outs32 = [torch.empty_like(want) for _ in range(6)], [torch.empty_like(want32) for _ in range(6)]
+    torch.cuda.synchronize()
+    for a, c in zip(outs, outs32):
+        call(one, out=a, stream=streams[0])
+        two.grouped_linear(x32, off, W32, out=c, stream=streams[1])
+        call(two, out=a, stream=streams[1])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, want) for a in outs) and all(torch.equal(c, want32) for c in outs32)
+    one.check()
+    two.check()
 
 
 def test_more_than_two_to_the_31_elements(ctx):
