@@ -389,8 +389,8 @@ int32_t rtma_grouped_linear_dw(rtma_ctx* ctx, int32_t dtype, int64_t n, int32_t 
  * within all rows of its part.  act: none, ReLU, PReLU (one slope per part, slope [G] with
  * slope_stride), SiLU.  Dropout as rtma_dropout with p, seed and row_ids (NULL: the row's number).
  *   gamma, beta  [C] per part or NULL (1 and 0).   C <= 2048.
- *   stats        [n or G][groups][2] (mean, 1 / sqrt(var + eps)): kept for the gradient; NULL: not
- *                kept.  An empty part's are (0, 1 / sqrt(eps)).
+ *   stats        [n or G][groups][2] (mean, 1 / sqrt(var + eps)), on an 8-byte boundary: kept for the
+ *                gradient; NULL: not kept.  An empty part's are (0, 1 / sqrt(eps)).
  * Y may be X.                                                                                  */
 enum { RTMA_SCOPE_ROW = 0, RTMA_SCOPE_PART = 1 };
 enum { RTMA_ACT_NONE = 0, RTMA_ACT_RELU = 1, RTMA_ACT_PRELU = 2, RTMA_ACT_SILU = 3 };

@@ -569,7 +569,8 @@ class Context:
                    row_ids=None, out=None, stats=None, stream=None):
         """dropout(act(gamma_g xhat + beta_g)) over X [n, C], xhat normalised within sets of C / groups neighbouring channels of a
         row (scope "row") or of all rows of a part ("part").  gamma, beta [G, C] or [C] float32, slope [G] or one value (act
-        "prelu"); dropout as in `dropout`.  Returns (Y, stats [n or G, groups, 2] float32: mean, 1 / std); Y may be X (out=X)."""
+        "prelu"); dropout as in `dropout`.  Returns (Y, stats [n or G, groups, 2] float32: mean, 1 / std); Y may be X (out=X).
+        Statistics that are handed in (here and to group_norm_grad) lie on an 8-byte boundary."""
         x, ldx = self._rows(X, "X")
         off, G, desc, gm, bt, sl, ids = self._norm(X, offsets, groups, gamma, beta, slope, scope, act, eps, p, seed, row_ids)
         n = X.shape[0]

@@ -1501,7 +1501,8 @@ bool full_units(const NormArgs& a, int32_t dtype, bool gradient) {
     return a.C % 8 == 0 && pieces && a.vx >= most && a.vy >= most && (!gradient || a.vdy >= most);
 }
 
-int32_t check_norm(rtma_ctx* ctx, const char* who, const rtma_norm_desc* d, int64_t n, int32_t G, const int64_t* offsets, const float* slope) {
+int32_t check_norm(rtma_ctx* ctx, const char* who, const rtma_norm_desc* d, int64_t n, int32_t G, const int64_t* offsets, const float* slope,
+                   const float* stats) {
     if (!d) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: null descriptor", who);
     RTMA_TRY(check_parts(ctx, who, n, G, offsets));
     if (d->dtype < RTMA_F32 || d->dtype > RTMA_F16) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: dtype=%d", who, d->dtype);
@@ -1512,6 +1513,8 @@ int32_t check_norm(rtma_ctx* ctx, const char* who, const rtma_norm_desc* d, int6
     if (d->act == RTMA_ACT_PRELU && !slope) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: PReLU without a slope", who);
     if (!(d->eps > 0.f) || std::isinf(d->eps)) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: eps=%g", who, (double)d->eps);
     if (!(d->p >= 0.0 && d->p <= 1.0)) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: p=%g outside [0,1]", who, d->p);
+    if (reinterpret_cast<uintptr_t>(stats) % sizeof(float2))  // (mean, 1 / std) are read and written as one
+        return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: stats do not lie on an 8-byte boundary", who);
     return RTMA_OK;
 }
 
@@ -1557,7 +1560,7 @@ extern "C" int32_t rtma_group_norm(rtma_ctx* ctx, const rtma_norm_desc* d, int64
                                    const float* gamma, const float* beta, const float* slope, const int32_t* row_ids, void* Y, int64_t ldy,
                                    float* stats, void* stream_) {
     if (!ctx) return RTMA_ERR_INVALID_ARG;
-    RTMA_TRY(check_norm(ctx, "rtma_group_norm", d, n, G, offsets, slope));
+    RTMA_TRY(check_norm(ctx, "rtma_group_norm", d, n, G, offsets, slope, stats));
     if (n > 0 && (!X || !Y)) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "rtma_group_norm: null pointer");
     if (ldx < d->C || ldy < d->C) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "rtma_group_norm: rows of %d channels lie closer than that", d->C);
     const bool rows = d->scope == RTMA_SCOPE_ROW;
@@ -1615,7 +1618,7 @@ extern "C" int32_t rtma_group_norm_grad(rtma_ctx* ctx, const rtma_norm_desc* d, 
                                         const int32_t* row_ids, void* dX, int64_t lddx, float* dgamma, int64_t dgamma_stride, float* dbeta,
                                         int64_t dbeta_stride, float* dslope, int64_t dslope_stride, void* stream_) {
     if (!ctx) return RTMA_ERR_INVALID_ARG;
-    RTMA_TRY(check_norm(ctx, "rtma_group_norm_grad", d, n, G, offsets, slope));
+    RTMA_TRY(check_norm(ctx, "rtma_group_norm_grad", d, n, G, offsets, slope, stats));
     if (n > 0 && (!X || !dY || !stats || !dX)) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "rtma_group_norm_grad: null pointer");
     if (ldx < d->C || lddy < d->C || lddx < d->C)
         return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "rtma_group_norm_grad: rows of %d channels lie closer than that", d->C);
