@@ -33,20 +33,37 @@ struct LinearArgs {
     int64_t ldo;
     float *dW, *db;
     int64_t dw_stride, db_stride;
-    int32_t* chunk_rows;       // dw: where the rows of a row tile are left for the reduction
+    uint32_t* chunk_rows;      // dw: where the rows of a row tile are left for the reduction
     int* error_word;
     CUtensorMap map_a, map_b;  // operands that are fetched by bulk-tensor loads
     CUtensorMap map_o;         // the result (dw: the slots, one below the other)
 };
 
 #ifdef __CUDACC__
+// Chunks of a part's rows.  Unsigned: a part has up to 2^31 - 1 rows, which with a chunk added to them no longer fit a signed number;
+// a chunk smaller than the largest part, the only ones asked about, fits an unsigned one.
+__host__ __device__ __forceinline__ uint32_t chunks_in(uint32_t rows, uint32_t chunk) { return (rows + chunk - 1) / chunk; }
+// The smallest chunk, of `least` rows or more and a multiple of `step`, of which all parts have not more than `tiles`; by bisection.
+// most: rows of the largest part; count(c): chunks of c rows in all parts.  `tiles` is at least the number of parts.
+template <class Count>
+__host__ __device__ __forceinline__ uint32_t fit_chunk(uint32_t least, uint32_t most, uint32_t step, int64_t tiles, Count count) {
+    uint32_t lo = least / step, hi = (most + step - 1) / step;  // hi fits: a chunk a part
+    if (hi < lo) hi = lo;
+    while (lo < hi) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (count(mid * step) <= tiles) hi = mid;
+        else lo = mid + 1;
+    }
+    return lo * step;
+}
+
 struct Shared {
     uint64_t full[MAX_STAGES], empty[MAX_STAGES];
     uint64_t acc_full[2], acc_empty[2];
     uint32_t tmem_base;
     int abort;
     int32_t warp_sums[32];
-    int32_t tile_rows;
+    uint32_t tile_rows;
     int32_t tile_start[RTMA_MAX_GROUPS + 1], begin[RTMA_MAX_GROUPS], rows[RTMA_MAX_GROUPS];
     alignas(16) float bias[8 * 128];  // of every drain warp's columns
 };
@@ -88,7 +105,7 @@ struct Walk {
         }
         n0 = rest * a.BN;
         while (row_tile >= sh.tile_start[part + 1]) ++part;  // tiles come in ascending order
-        const int64_t inside = (int64_t)(row_tile - sh.tile_start[part]) * sh.tile_rows;
+        const int64_t inside = (row_tile - sh.tile_start[part]) * (int64_t)sh.tile_rows;
         row0 = sh.begin[part] + inside;
         rows = (int)min((int64_t)sh.rows[part] - inside, (int64_t)sh.tile_rows);
         if (PAIR) {
@@ -131,28 +148,24 @@ __device__ __forceinline__ void lay_out(const LinearArgs& a, Shared& sh) {
     if (MODE == WEIGHT_GRADIENT) {
         __syncthreads();
         if (threadIdx.x < 32) {
-            // The smallest chunks (multiples of STEP rows) of which there are not more than `tiles`, which fills the blocks that run at
-            // a time evenly, whatever the parts' sizes; by bisection.
+            // Chunks of which there are not more than `tiles` fill the blocks that run at a time evenly, whatever the parts' sizes.
             const int lane = threadIdx.x;
             int most = 1;
             for (int g = lane; g < a.G; g += 32) most = max(most, sh.rows[g]);
             for (int o = 16; o > 0; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
-            int lo = (int)min(a.tile_rows, (int64_t)1 << 30) / STEP, hi = max((most + STEP - 1) / STEP, lo);  // hi fits: a tile a part
-            while (lo < hi) {
-                const int mid = (lo + hi) / 2, rows = mid * STEP;
+            const uint32_t rows = fit_chunk((uint32_t)a.tile_rows, (uint32_t)most, STEP, a.tiles, [&](uint32_t chunk) {
                 int64_t count = 0;
-                for (int g = lane; g < a.G; g += 32) count += (sh.rows[g] + rows - 1) / rows;
+                for (int g = lane; g < a.G; g += 32) count += chunks_in((uint32_t)sh.rows[g], chunk);
                 for (int o = 16; o > 0; o >>= 1) count += __shfl_xor_sync(0xffffffffu, count, o);
-                if (count <= a.tiles) hi = mid;
-                else lo = mid + 1;
-            }
+                return count;
+            });
             if (lane == 0) {
-                sh.tile_rows = lo * STEP;
-                if (blockIdx.x == 0) *a.chunk_rows = lo * STEP;
+                sh.tile_rows = rows;
+                if (blockIdx.x == 0) *a.chunk_rows = rows;
             }
         }
     } else if (threadIdx.x == 0) {
-        sh.tile_rows = (int32_t)a.tile_rows;
+        sh.tile_rows = (uint32_t)a.tile_rows;
     }
     __syncthreads();
     number_tiles(a.offsets, a.n, a.G, sh.tile_rows, a.tiles, sh.tile_start, sh.warp_sums, a.span);
