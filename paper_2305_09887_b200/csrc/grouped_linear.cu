@@ -778,7 +778,7 @@ extern "C" int32_t rtma_grouped_linear_dw(rtma_ctx* ctx, int32_t dtype, int64_t 
     a.go = 32;
     const int64_t slot_rows = a.tiles * (d_in + a.bias_rows);
     RTMA_TRY(prepare_row_call(ctx, 256 + sizeof(float) * slot_rows * a.ldo, stream));
-    a.chunk_rows = reinterpret_cast<uint32_t*>(ctx->arena);
+    a.chunk_rows = reinterpret_cast<int32_t*>(ctx->arena);
     a.out = ctx->arena + 256;
     a.vo = dtype != RTMA_F32 && slot_rows < (int64_t(1) << 31) && make_store_map(&a.map_o, RTMA_F32, a.out, slot_rows, a.ldo, a.ldo);
     if (n > 0) RTMA_TRY(launch_linear<WEIGHT_GRADIENT>(ctx, dtype, a, KC_GEMM_WGRAD, stream));

@@ -33,7 +33,7 @@ struct LinearArgs {
     int64_t ldo;
     float *dW, *db;
     int64_t dw_stride, db_stride;
-    uint32_t* chunk_rows;      // dw: where the rows of a row tile are left for the reduction
+    int32_t* chunk_rows;       // dw: where the rows of a row tile are left for the reduction
     int* error_word;
     CUtensorMap map_a, map_b;  // operands that are fetched by bulk-tensor loads
     CUtensorMap map_o;         // the result (dw: the slots, one below the other)
@@ -63,7 +63,7 @@ struct Shared {
     uint32_t tmem_base;
     int abort;
     int32_t warp_sums[32];
-    uint32_t tile_rows;
+    int32_t tile_rows;
     int32_t tile_start[RTMA_MAX_GROUPS + 1], begin[RTMA_MAX_GROUPS], rows[RTMA_MAX_GROUPS];
     alignas(16) float bias[8 * 128];  // of every drain warp's columns
 };
@@ -105,7 +105,7 @@ struct Walk {
         }
         n0 = rest * a.BN;
         while (row_tile >= sh.tile_start[part + 1]) ++part;  // tiles come in ascending order
-        const int64_t inside = (row_tile - sh.tile_start[part]) * (int64_t)sh.tile_rows;
+        const int64_t inside = (int64_t)(row_tile - sh.tile_start[part]) * sh.tile_rows;
         row0 = sh.begin[part] + inside;
         rows = (int)min((int64_t)sh.rows[part] - inside, (int64_t)sh.tile_rows);
         if (PAIR) {
@@ -153,7 +153,8 @@ __device__ __forceinline__ void lay_out(const LinearArgs& a, Shared& sh) {
             int most = 1;
             for (int g = lane; g < a.G; g += 32) most = max(most, sh.rows[g]);
             for (int o = 16; o > 0; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
-            const uint32_t rows = fit_chunk((uint32_t)a.tile_rows, (uint32_t)most, STEP, a.tiles, [&](uint32_t chunk) {
+            // (2^31 rows are no chunk: with fewer than 256 parts there are twice as many tiles, unless rows are so wide that 2^31 of them fit no memory.)
+            const int32_t rows = (int32_t)fit_chunk((uint32_t)a.tile_rows, (uint32_t)most, STEP, a.tiles, [&](uint32_t chunk) {
                 int64_t count = 0;
                 for (int g = lane; g < a.G; g += 32) count += chunks_in((uint32_t)sh.rows[g], chunk);
                 for (int o = 16; o > 0; o >>= 1) count += __shfl_xor_sync(0xffffffffu, count, o);
@@ -165,7 +166,7 @@ __device__ __forceinline__ void lay_out(const LinearArgs& a, Shared& sh) {
             }
         }
     } else if (threadIdx.x == 0) {
-        sh.tile_rows = (uint32_t)a.tile_rows;
+        sh.tile_rows = (int32_t)a.tile_rows;
     }
     __syncthreads();
     number_tiles(a.offsets, a.n, a.G, sh.tile_rows, a.tiles, sh.tile_start, sh.warp_sums, a.span);
