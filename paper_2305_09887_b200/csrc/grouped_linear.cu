@@ -714,6 +714,7 @@ int32_t run_rows(rtma_ctx* ctx, const char* who, bool transposed, int32_t dtype,
     cut_columns(a, N, dtype == RTMA_F32 ? SPLIT_COLUMNS : 256);
     a.d_in = d_in; a.d_out = d_out;
     a.A = A; a.lda = lda; a.B = W; a.ldb = d_out; a.w_stride = w_stride; a.bias = b; a.bias_stride = b_stride;
+    a.bias_overlaps = G > 1 && b_stride != 0 && b_stride < d_out && b_stride > -d_out;
     a.va = row_granule(A, lda, es);
     a.vb = std::min(row_granule(W, d_out, es), row_granule(nullptr, w_stride, es));
     a.out = out; a.ldo = ldo;

@@ -28,6 +28,7 @@ struct LinearArgs {
     bool vo;                   // the result can leave by bulk-tensor stores: map_o holds
     const void* bias;
     int64_t bias_stride;
+    bool bias_overlaps;        // of two parts: an address then does not say which columns lie there
     int bias_rows;             // dw: partial sums of the bias gradient in a slot, one row per warp that adds them up
     void* out;                 // dw: the slots, [row tile][d_in + bias_rows][ldo]
     int64_t ldo;
@@ -266,7 +267,7 @@ struct BiasHolder {
     const T* held = nullptr;   // of which columns: a block's tiles have the same ones most of the time
     __device__ __forceinline__ void fetch(const LinearArgs& a, int part, int n0, int c, int step, int chunks, int lane) {
         const T* bias = static_cast<const T*>(a.bias) + part * a.bias_stride + n0;
-        if (bias == held) return;
+        if (bias == held && !a.bias_overlaps) return;
         held = bias;
         __syncwarp();
         for (int chunk = c, i = 0; chunk < chunks; chunk += step, ++i) {

@@ -23,3 +23,20 @@ def test_weight_gradient_of_nearly_two_to_the_31_rows(ctx):
     for got in (dw, db):
         assert abs(got.item() - n) <= 600 * 2 * U * n
     ctx.check()
+
+
+@pytest.mark.parametrize("dtype,d_out,stride", [(torch.float32, 300, 112), (torch.float32, 300, 224), (torch.bfloat16, 600, 416), (torch.float16, 600, 208)])
+def test_parameters_of_parts_that_overlap(ctx, dtype, d_out, stride):
+    """Parameters are only read, so those of two parts may share memory (strides smaller than a part's): columns of one part's bias that
+    another part has at the same address are still that part's, and as many as it has."""
+    G, d_in = 9, 16
+    g = torch.Generator().manual_seed(d_out + stride)
+    sizes = torch.randint(3_000, 14_000, (G,), generator=g)
+    off = torch.cat([torch.zeros(1, dtype=torch.int64), sizes.cumsum(0)]).cuda()
+    x = torch.randn(int(off[-1]), d_in, generator=g).to(dtype).cuda()
+    flat = torch.randn(G * max(stride, 5) + d_in * d_out, generator=g).to(dtype).cuda()
+    bias = flat.as_strided((G, d_out), (stride, 1))
+    W = flat.as_strided((G, d_in, d_out), (5, d_out, 1))
+    assert torch.equal(ctx.grouped_linear(x, off, W, bias), ctx.grouped_linear(x, off, W.contiguous(), bias.contiguous()))
+    dy = torch.randn(len(x), d_out, generator=g).to(dtype).cuda()
+    assert torch.equal(ctx.grouped_linear_dx(dy, off, W), ctx.grouped_linear_dx(dy, off, W.contiguous()))
