@@ -451,8 +451,9 @@ class Context:
             raise ValueError("offsets must be a contiguous vector of one more value than there are parts")
         return offsets.data_ptr(), size[0] - 1
 
-    def _of_parts(self, t, name, dtype, G, shape):
-        """(pointer, distance between parts) of a parameter: [G, *shape], or *shape for one that all parts share."""
+    def _of_parts(self, t, name, dtype, G, shape, result=False):
+        """(pointer, distance between parts) of a parameter: [G, *shape], or *shape for one that all parts share.  A result's distance is
+        not 0 (an expanded view): every part's would be written to the same place."""
         if t is None:
             return None, 0
         if t.dtype != dtype:
@@ -462,6 +463,8 @@ class Context:
         if len(size) == len(shape) + 1 and size[0] == G:
             if G > 1:
                 between = steps[0]
+                if result and between == 0:
+                    raise RtmaError(f"{name} must have memory of its own for every part, got an expanded view")
             size, steps = size[1:], steps[1:]
         step, packed = 1, size == shape
         for k in range(len(shape) - 1, -1, -1):
@@ -526,8 +529,8 @@ class Context:
         for t, name, rank in ((dw, "dw", 2), (db, "db", 1)):
             if t is not None and t.dim() != rank + len(lead):
                 raise ValueError(f"{name} has {t.dim()} dimensions with shared={shared}")
-        w, ws = self._of_parts(dw, "dw", torch.float32, G, (d_in, d_out))
-        b, bs = self._of_parts(db, "db", torch.float32, G, (d_out,))
+        w, ws = self._of_parts(dw, "dw", torch.float32, G, (d_in, d_out), result=True)
+        b, bs = self._of_parts(db, "db", torch.float32, G, (d_out,), result=True)
         self._check(self._lib.rtma_grouped_linear_dw(self._h, ROW_TYPES[X.dtype], n, G, off, d_in, d_out, x, ldx, g, ldg, w, ws, b, bs,
                                                      self._stream(stream)), "rtma_grouped_linear_dw")
         return dw, db
@@ -546,14 +549,17 @@ class Context:
                         gs, bs, ss)
         return off, G, desc, gm, bt, sl, self._ids(row_ids, n)
 
-    def _slope(self, t, name, G):
+    def _slope(self, t, name, G, result=False):
         if t.dtype != torch.float32:
             raise TypeError(f"{name} must be {torch.float32}, got {t.dtype}")
         self._here(t, name)
         size = tuple(t.shape)
         if size not in ((), (1,), (G,)):
             raise ValueError(f"{name} must be [{G}] or a single value")
-        return t.data_ptr(), t.stride(0) if size == (G,) and G > 1 else 0
+        between = t.stride(0) if size == (G,) and G > 1 else 0
+        if result and size == (G,) and G > 1 and between == 0:
+            raise RtmaError(f"{name} must have memory of its own for every part, got an expanded view")
+        return t.data_ptr(), between
 
     def _ids(self, row_ids, n):
         if row_ids is None:
@@ -603,11 +609,11 @@ class Context:
         dgamma = new(gamma) if dgamma is None and gamma is not None else dgamma
         dbeta = new(beta) if dbeta is None and beta is not None else dbeta
         dslope = new(slope) if dslope is None and act == "prelu" else dslope
-        dg, dgs = self._of_parts(dgamma, "dgamma", torch.float32, G, (C,))
-        db, dbs = self._of_parts(dbeta, "dbeta", torch.float32, G, (C,))
+        dg, dgs = self._of_parts(dgamma, "dgamma", torch.float32, G, (C,), result=True)
+        db, dbs = self._of_parts(dbeta, "dbeta", torch.float32, G, (C,), result=True)
         ds, dss = None, 0
         if dslope is not None:
-            ds, dss = self._slope(dslope, "dslope", G)
+            ds, dss = self._slope(dslope, "dslope", G, result=True)
         self._check(self._lib.rtma_group_norm_grad(self._h, desc, n, G, off, x, ldx, g, ldg, st, gm, bt, sl, ids, dx, lddx, dg, dgs, db, dbs,
                                                    ds, dss, self._stream(stream)), "rtma_group_norm_grad")
         return out, dgamma, dbeta, dslope

@@ -4,6 +4,7 @@ The C calls are made on a context that has no device: what passes the checks of 
 without a launch.
 """
 import ctypes
+import math
 import os
 import subprocess
 
@@ -55,3 +56,63 @@ def test_statistics_off_8_byte_boundaries(lib, handle, scope, off):
                    lib.rtma_group_norm_grad(handle, desc, n, 1, None, x, C, x, C, st, None, None, None, None, x, C, None, 0, None, 0, None, 0, None)):
         assert (status == INVALID_ARG) == (off % 8 != 0)
         assert ("8-byte boundary" in error_of(lib, handle)) == (off % 8 != 0)
+
+
+class Recorder:
+    """Stands in for the library: takes every call, remembers its name and arguments."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append((name, args))
+            return 0
+        return call
+
+
+@pytest.fixture
+def ctx():
+    """A binding context whose tensors live on the CPU and whose library does nothing."""
+    c = binding.Context.__new__(binding.Context)
+    c._lib, c._h = Recorder(), None
+    c.device = torch.device("cpu")
+    c._index = -1
+    c._stream = lambda stream: 0
+    return c
+
+
+G, D_IN, D_OUT, N = 3, 8, 4, 10
+OFF = torch.tensor([0, 2, 5, 10])
+
+
+def grads(ctx, **results):
+    x, dy = torch.ones(N, D_IN), torch.ones(N, D_OUT)
+    return ctx.grouped_linear_dw(x, dy, OFF, **results)
+
+
+def norm_grads(ctx, **results):
+    x, st = torch.ones(N, D_IN), torch.ones(N, 2, 2)
+    p = torch.ones(G, D_IN)
+    return ctx.group_norm_grad(x, x, st, OFF, 2, p, p, act="prelu", slope=torch.ones(G), **results)
+
+
+@pytest.mark.parametrize("call,name,part,distance", [(grads, "dw", (D_IN, D_OUT), 12), (grads, "db", (D_OUT,), 14), (norm_grads, "dgamma", (D_IN,), 17),
+                                                     (norm_grads, "dbeta", (D_IN,), 19), (norm_grads, "dslope", (), 21)])
+def test_results_that_are_expanded_views(ctx, call, name, part, distance):
+    """Every part's result would go to one place (the C call sums over the parts where their distance is 0)."""
+    alone = dict(bias=False) if name == "dw" else {}
+    with pytest.raises(binding.RtmaError, match=f"{name} must have memory of its own"):
+        call(ctx, **alone, **{name: torch.ones(part).expand(G, *part)})
+    assert not ctx._lib.calls
+    call(ctx, **alone, **{name: torch.ones(G, *part)})
+    (_, args), = ctx._lib.calls
+    assert args[distance] == math.prod(part)
+
+
+def test_one_result_for_all_parts_and_of_one_part(ctx):
+    """Neither is an expanded view: a result without a leading dimension is the sum, a single part's distance is not used."""
+    ctx.grouped_linear_dw(torch.ones(N, D_IN), torch.ones(N, D_OUT), OFF, shared=True, dw=torch.ones(D_IN, D_OUT), db=torch.ones(D_OUT))
+    ctx.grouped_linear_dw(torch.ones(N, D_IN), torch.ones(N, D_OUT), None, dw=torch.ones(D_IN, D_OUT).expand(1, D_IN, D_OUT), bias=False)
+    norm_grads(ctx, dgamma=torch.ones(D_IN), dbeta=torch.ones(D_IN), dslope=torch.ones(1))
+    assert len(ctx._lib.calls) == 3
