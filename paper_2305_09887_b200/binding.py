@@ -608,7 +608,7 @@ class Context:
         new = lambda like: torch.empty(like.shape, dtype=torch.float32, device=self.device)  # noqa: E731
         dgamma = new(gamma) if dgamma is None and gamma is not None else dgamma
         dbeta = new(beta) if dbeta is None and beta is not None else dbeta
-        dslope = new(slope) if dslope is None and act == "prelu" else dslope
+        dslope = new(slope) if dslope is None and act == "prelu" and slope is not None else dslope
         dg, dgs = self._of_parts(dgamma, "dgamma", torch.float32, G, (C,), result=True)
         db, dbs = self._of_parts(dbeta, "dbeta", torch.float32, G, (C,), result=True)
         ds, dss = None, 0

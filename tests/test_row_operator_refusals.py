@@ -116,3 +116,13 @@ def test_one_result_for_all_parts_and_of_one_part(ctx):
     ctx.grouped_linear_dw(torch.ones(N, D_IN), torch.ones(N, D_OUT), None, dw=torch.ones(D_IN, D_OUT).expand(1, D_IN, D_OUT), bias=False)
     norm_grads(ctx, dgamma=torch.ones(D_IN), dbeta=torch.ones(D_IN), dslope=torch.ones(1))
     assert len(ctx._lib.calls) == 3
+
+
+def test_prelu_without_a_slope(lib, handle, ctx):
+    """Forward and gradient say what is missing."""
+    ctx._lib, ctx._h = lib, handle
+    lib.rtma_last_error.restype = ctypes.c_char_p
+    x, st = torch.ones(N, D_IN), torch.ones(N, 2, 2)
+    for call in (lambda: ctx.group_norm(x, OFF, 2, act="prelu"), lambda: ctx.group_norm_grad(x, x, st, OFF, 2, act="prelu")):
+        with pytest.raises(binding.RtmaError, match="PReLU without a slope"):
+            call()
