@@ -126,3 +126,4 @@ def test_prelu_without_a_slope(lib, handle, ctx):
     for call in (lambda: ctx.group_norm(x, OFF, 2, act="prelu"), lambda: ctx.group_norm_grad(x, x, st, OFF, 2, act="prelu")):
         with pytest.raises(binding.RtmaError, match="PReLU without a slope"):
             call()
+    ctx._h = None  # it is not this binding's to destroy
