@@ -40,3 +40,23 @@ def test_parameters_of_parts_that_overlap(ctx, dtype, d_out, stride):
     assert torch.equal(ctx.grouped_linear(x, off, W, bias), ctx.grouped_linear(x, off, W.contiguous(), bias.contiguous()))
     dy = torch.randn(len(x), d_out, generator=g).to(dtype).cuda()
     assert torch.equal(ctx.grouped_linear_dx(dy, off, W), ctx.grouped_linear_dx(dy, off, W.contiguous()))
+
+
+NORM_KINDS = [(64, 8), (64, 32), (60, 20), (100, 4), (384, 1), (300, 3), (1024, 2)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("C,groups", NORM_KINDS)
+def test_norm_of_equal_values_far_from_zero(ctx, dtype, C, groups):
+    """x - mean is 0 whatever 1 / std is: y is beta, and gamma's gradient 0 however many rows there are."""
+    n = 5_000
+    x = torch.full((n, C), 1000.0, dtype=dtype, device="cuda")
+    g = torch.Generator().manual_seed(C)
+    gamma, beta = torch.randn(C, generator=g).cuda(), torch.randn(C, generator=g).cuda()
+    dy = torch.ones_like(x)
+    y, st = ctx.group_norm(x, None, groups, gamma, beta, scope="part")
+    assert torch.equal(y, beta.to(dtype).expand(n, C)) and (st[..., 0] == 1000).all()
+    for scope, rows in (("part", 1), ("row", n)):
+        stats = st.expand(rows, groups, 2).contiguous()
+        _, dg, db, _ = ctx.group_norm_grad(x, dy, stats, None, groups, gamma, beta, scope=scope)
+        assert not dg.any() and (db == n).all()
