@@ -386,7 +386,9 @@ int32_t rtma_grouped_linear_dw(rtma_ctx* ctx, int32_t dtype, int64_t n, int32_t 
  *   xhat = (x - mean) / sqrt(var + eps), u = gamma_g xhat + beta_g, y = dropout(act(u))
  * The C channels are cut into `groups` sets of C / groups neighbours.  scope RTMA_SCOPE_ROW: mean and
  * (biased) variance of a set within its row (groups = 1 is Layer Normalization); RTMA_SCOPE_PART:
- * within all rows of its part.  act: none, ReLU, PReLU (one slope per part, slope [G] with
+ * within all rows of its part.  Where the squares of the differences from a mean do not fit fp32 (values
+ * above about 1e19), 1 / sqrt(var + eps) and xhat are 0; where a set's values cannot be added up, NaN.
+ * act: none, ReLU, PReLU (one slope per part, slope [G] with
  * slope_stride), SiLU.  Dropout as rtma_dropout with p, seed and row_ids (NULL: the row's number).
  *   gamma, beta  [C] per part or NULL (1 and 0).   C <= 2048.
  *   stats        [n or G][groups][2] (mean, 1 / sqrt(var + eps)), on an 8-byte boundary: kept for the

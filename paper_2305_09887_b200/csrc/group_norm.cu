@@ -291,10 +291,11 @@ __device__ __forceinline__ void leave_slope(const NormArgs& a, int tile, float d
     __syncthreads();
 }
 
-// 1 / sqrt(x) for x >= eps > 0: the approximation and a Newton step, within a unit in the last place
+// 1 / sqrt(x) for x >= eps > 0: the approximation and a Newton step, within a unit in the last place (x y first: half of a number
+// below 2^-126 loses bits).  0 for an infinite x, a variance that does not fit fp32.
 __device__ __forceinline__ float inverse_root(float x) {
     const float y = rsqrtf(x);
-    return y * fmaf(-0.5f * x * y, y, 1.5f);
+    return x < __int_as_float(0x7f800000) ? y * fmaf(x * y, -0.5f * y, 1.5f) : y;
 }
 
 // A run of rows of one part.
@@ -1086,7 +1087,7 @@ __global__ void __launch_bounds__(NORM_THREADS, FULL ? 3 : 2) norm_stats_kernel(
                     }
                     const f2 d = fma2(mean[i], minus, s);
                     mean[i] = fma2(d, share2, mean[i]);
-                    m2[i] = fma2(mul2(d, d), weight2, q);
+                    m2[i] = fma2(mul2(d, weight2), d, q);  // (in this order: a weight of 0 makes any finite d 0)
                 }
                 count += BATCH;
             }
@@ -1101,7 +1102,7 @@ __global__ void __launch_bounds__(NORM_THREADS, FULL ? 3 : 2) norm_stats_kernel(
                 for (int i = 0; i < 4; ++i) {
                     const f2 d = fma2(mean[i], minus, v[i]);
                     mean[i] = fma2(d, share2, mean[i]);
-                    m2[i] = fma2(mul2(d, d), weight2, m2[i]);
+                    m2[i] = fma2(mul2(d, weight2), d, m2[i]);
                 }
                 count += 1.f;
             }
@@ -1339,7 +1340,11 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_grad_sums_kernel(const N
             }
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sg[i] = mul2(sg[i], pack2(rstd[2 * i], rstd[2 * i + 1]));
+        for (int i = 0; i < 4; ++i) {
+            float s0, s1;
+            unpack2(sg[i], s0, s1);
+            sg[i] = pack2(rstd[2 * i] == 0.f ? 0.f : s0 * rstd[2 * i], rstd[2 * i + 1] == 0.f ? 0.f : s1 * rstd[2 * i + 1]);  // (sums may be infinite)
+        }
         leave_sums(a, tile, 8 * at.u, at.active ? at.y : NORM_THREADS, a.units, a.rows_at_once, sb, sg, shared);
         leave_slope(a, tile, ds, shared);
     }

@@ -60,3 +60,42 @@ def test_norm_of_equal_values_far_from_zero(ctx, dtype, C, groups):
         stats = st.expand(rows, groups, 2).contiguous()
         _, dg, db, _ = ctx.group_norm_grad(x, dy, stats, None, groups, gamma, beta, scope=scope)
         assert not dg.any() and (db == n).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("scope", ["row", "part"])
+@pytest.mark.parametrize("C,groups", NORM_KINDS)
+def test_norm_of_values_whose_squares_do_not_fit(ctx, dtype, scope, C, groups):
+    """1 / std is 0 then, so that y is beta, and no gradient comes through; other rows (parts) are not touched."""
+    g = torch.Generator().manual_seed(C)
+    n, half = 120, 60
+    x = torch.randn(n, C, generator=g).to(dtype).cuda()
+    gamma, beta = torch.randn(2, C, generator=g).cuda(), torch.randn(2, C, generator=g).cuda()
+    dy = torch.randn(n, C, generator=g).to(dtype).cuda()
+    off = torch.tensor([0, half, n], dtype=torch.int64, device="cuda")
+    clean, _ = ctx.group_norm(x, off, groups, gamma, beta, scope=scope)
+    x[half:] = (x[half:].float() * 1e25).to(dtype)
+    y, st = ctx.group_norm(x, off, groups, gamma, beta, scope=scope)
+    assert torch.equal(y[:half], clean[:half])
+    assert torch.equal(y[half:], beta[1].to(dtype).expand(n - half, C))
+    huge = st[half:] if scope == "row" else st[1:]
+    # (two rounded values of a row's set may be equal: such a set has no squares to speak of)
+    sets = x[half:].view(half, groups, C // groups) if scope == "row" else x[half:].view(half, groups, C // groups).transpose(0, 1).reshape(1, groups, -1)
+    equal = sets.amax(2) == sets.amin(2)
+    assert (huge[..., 1] == 0)[~equal].all() and (huge[..., 0].abs() < 1e26).all()
+    dx, dg, db, _ = ctx.group_norm_grad(x, dy, st, off, groups, gamma, beta, scope=scope)
+    assert not dx[half:].view(half, groups, -1)[~equal.expand(half, groups)].any() and not dg[1].any() and dx.isfinite().all()
+    want = dy[half:].to(F64).sum(0)
+    assert ((db[1].to(F64) - want).abs() <= n * 2 * U * dy[half:].to(F64).abs().sum(0)).all()
+
+
+@pytest.mark.parametrize("scope", ["row", "part"])
+@pytest.mark.parametrize("C,groups", NORM_KINDS)
+@pytest.mark.parametrize("eps", [1e-42, 1e-30])
+def test_norm_of_equal_values_with_a_tiny_eps(ctx, scope, C, groups, eps):
+    """1 / sqrt(eps), of an eps below the smallest normal number too: three roundings, and that of eps itself."""
+    x = torch.full((40, C), 2.0, device="cuda")
+    y, st = ctx.group_norm(x, None, groups, scope=scope, eps=eps)
+    want = torch.tensor(eps).to(F64).item() ** -0.5
+    assert not y.any() and (st[..., 0] == 2).all()
+    assert ((st[..., 1].to(F64) / want - 1).abs() <= 4 * 2 * U).all()
