@@ -189,7 +189,10 @@ def partition_static(n: int, group_id, seed: int, M: int, device: int = 0, strea
 
 class Context:
     """One library context on one CUDA device.  Calls are enqueued on the given (or the
-    current torch) stream and share the context's scratch, so keep them stream-ordered."""
+    current torch) stream and share the context's scratch, so keep them stream-ordered.  Results that a call makes
+    are allocated on the current stream: where `stream` is another one, order it behind the current one.  The operators on
+    rows allocate theirs on `stream`, as under torch.cuda.stream(stream): order the use on another one behind it, and
+    record_stream a result that is freed before that use has ended."""
 
     def __init__(self, device: int = 0, workspace_bytes: int = 0, checked: bool = False):
         if not torch.cuda.is_available():
@@ -476,6 +479,14 @@ class Context:
             raise ValueError(f"{name} must be [{G}, {', '.join(map(str, shape))}] or {list(shape)}, contiguous within a part")
         return t.data_ptr(), between
 
+    def _new(self, shape, dtype, stream):
+        """Memory for a result, of the stream that the call is for: from the current stream's it might still be in use there, for something
+        that has been freed, when `stream` writes to it."""
+        if stream is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(torch.cuda.ExternalStream(_stream_handle(stream), device=self.device)):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+
     def _stream(self, stream):
         return torch._C._cuda_getCurrentRawStream(self._index) if stream is None else _stream_handle(stream)
 
@@ -490,7 +501,7 @@ class Context:
         w, ws = self._of_parts(W, "W", X.dtype, G, (d_in, d_out))
         b, bs = self._of_parts(bias, "bias", X.dtype, G, (d_out,))
         if out is None:
-            out = torch.empty(n, d_out, dtype=X.dtype, device=self.device)
+            out = self._new((n, d_out), X.dtype, stream)
         y, ldy = self._rows(out, "out", X.dtype, (n, d_out))
         self._check(self._lib.rtma_grouped_linear(self._h, ROW_TYPES[X.dtype], n, G, off, d_in, d_out, x, ldx, w, ws, b, bs, y, ldy,
                                                   self._stream(stream)), "rtma_grouped_linear")
@@ -504,7 +515,7 @@ class Context:
         d_in = W.shape[-2]
         w, ws = self._of_parts(W, "W", dY.dtype, G, (d_in, d_out))
         if out is None:
-            out = torch.empty(n, d_in, dtype=dY.dtype, device=self.device)
+            out = self._new((n, d_in), dY.dtype, stream)
         x, ldx = self._rows(out, "out", dY.dtype, (n, d_in))
         self._check(self._lib.rtma_grouped_linear_dx(self._h, ROW_TYPES[dY.dtype], n, G, off, d_in, d_out, g, ldg, w, ws, x, ldx,
                                                      self._stream(stream)), "rtma_grouped_linear_dx")
@@ -523,9 +534,9 @@ class Context:
         off, G = self._parts(offsets)
         lead = () if shared else (G,)
         if dw is None:
-            dw = torch.empty(*lead, d_in, d_out, dtype=torch.float32, device=self.device)
+            dw = self._new((*lead, d_in, d_out), torch.float32, stream)
         if db is None and bias:
-            db = torch.empty(*lead, d_out, dtype=torch.float32, device=self.device)
+            db = self._new((*lead, d_out), torch.float32, stream)
         for t, name, rank in ((dw, "dw", 2), (db, "db", 1)):
             if t is not None and t.dim() != rank + len(lead):
                 raise ValueError(f"{name} has {t.dim()} dimensions with shared={shared}")
@@ -581,11 +592,11 @@ class Context:
         off, G, desc, gm, bt, sl, ids = self._norm(X, offsets, groups, gamma, beta, slope, scope, act, eps, p, seed, row_ids)
         n = X.shape[0]
         if out is None:
-            out = torch.empty_like(X, memory_format=torch.contiguous_format)
+            out = self._new(X.shape, X.dtype, stream)
         y, ldy = self._rows(out, "out", X.dtype, X.shape)
         shape = (n if scope == "row" else G, int(groups), 2)
         if stats is None:
-            stats = torch.empty(shape, dtype=torch.float32, device=self.device)
+            stats = self._new(shape, torch.float32, stream)
             st = stats.data_ptr()
         else:
             st = self._of_parts(stats, "stats", torch.float32, 1, shape)[0]
@@ -603,9 +614,9 @@ class Context:
         g, ldg = self._rows(dY, "dY", X.dtype, (n, C))
         st = self._of_parts(stats, "stats", torch.float32, 1, (n if scope == "row" else G, int(groups), 2))[0]
         if out is None:
-            out = torch.empty_like(X, memory_format=torch.contiguous_format)
+            out = self._new(X.shape, X.dtype, stream)
         dx, lddx = self._rows(out, "out", X.dtype, (n, C))
-        new = lambda like: torch.empty(like.shape, dtype=torch.float32, device=self.device)  # noqa: E731
+        new = lambda like: self._new(like.shape, torch.float32, stream)  # noqa: E731
         dgamma = new(gamma) if dgamma is None and gamma is not None else dgamma
         dbeta = new(beta) if dbeta is None and beta is not None else dbeta
         dslope = new(slope) if dslope is None and act == "prelu" and slope is not None else dslope
@@ -626,7 +637,7 @@ class Context:
         r, ldr = (None, 0) if residual is None else self._rows(residual, "residual", X.dtype, (n, d))
         ids = self._ids(row_ids, n)
         if out is None:
-            out = torch.empty_like(X, memory_format=torch.contiguous_format)
+            out = self._new(X.shape, X.dtype, stream)
         y, ldy = self._rows(out, "out", X.dtype, X.shape)
         self._check(self._lib.rtma_dropout(self._h, ROW_TYPES[X.dtype], n, d, x, ldx, ids, r, ldr, float(p), int(seed) & (2**64 - 1), y, ldy,
                                            self._stream(stream)), "rtma_dropout")

@@ -99,3 +99,20 @@ def test_norm_of_equal_values_with_a_tiny_eps(ctx, scope, C, groups, eps):
     want = torch.tensor(eps).to(F64).item() ** -0.5
     assert not y.any() and (st[..., 0] == 2).all()
     assert ((st[..., 1].to(F64) / want - 1).abs() <= 4 * 2 * U).all()
+
+
+def test_a_result_is_not_in_memory_that_another_stream_still_writes(ctx):
+    """A tensor is freed while its stream has yet to write it; a call on another stream, which runs first, keeps out of its memory."""
+    n, d = 4096, 1024
+    x = torch.randn(n, d, device="cuda")
+    want = ctx.dropout(x, 0.5, 3)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        freed = torch.empty(n, d, device="cuda")
+        torch.cuda._sleep(100_000_000)
+        freed.fill_(7)
+        del freed
+        y = ctx.dropout(x, 0.5, 3, stream=side)
+        torch.cuda.synchronize()
+        assert torch.equal(y, want)

@@ -3,10 +3,12 @@
 The C calls are made on a context that has no device: what passes the checks of its arguments ends in RTMA_ERR_CUDA or behind them,
 without a launch.
 """
+import contextlib
 import ctypes
 import math
 import os
 import subprocess
+import types
 
 import pytest
 import torch
@@ -127,3 +129,35 @@ def test_prelu_without_a_slope(lib, handle, ctx):
         with pytest.raises(binding.RtmaError, match="PReLU without a slope"):
             call()
     ctx._h = None  # it is not this binding's to destroy
+
+
+def every_call(ctx, **k):
+    x, dy, W, st = torch.ones(N, D_IN), torch.ones(N, D_OUT), torch.ones(G, D_IN, D_OUT), torch.ones(N, 2, 2)
+    p = torch.ones(G, D_IN)
+    yield ctx.grouped_linear(x, OFF, W, **k)
+    yield ctx.grouped_linear_dx(dy, OFF, W, **k)
+    yield ctx.grouped_linear_dw(x, dy, OFF, **k)
+    yield ctx.group_norm(x, OFF, 2, p, p, **k)
+    yield ctx.group_norm_grad(x, x, st, OFF, 2, p, p, act="prelu", slope=torch.ones(G), **k)
+    yield ctx.dropout(x, 0.5, 1, **k)
+
+
+@pytest.mark.parametrize("stream", [None, 77, types.SimpleNamespace(cuda_stream=77)])
+def test_results_are_allocated_on_the_stream_that_writes_them(ctx, monkeypatch, stream):
+    """Memory of the current stream's might still be in use there, for something that has been freed."""
+    on, made = [], []
+
+    @contextlib.contextmanager
+    def current(s):
+        on.append(s)
+        yield
+        on.pop()
+
+    real = torch.empty
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, device=None: handle)
+    monkeypatch.setattr(torch.cuda, "stream", current)
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: (made.append(on[-1] if on else None), real(*a, **k))[1])
+    monkeypatch.setattr(torch, "empty_like", lambda t, **k: torch.empty(t.shape, dtype=t.dtype))
+    results = list(every_call(ctx, stream=stream))
+    assert len(results) == 6 and not on
+    assert made == [None if stream is None else 77] * 11  # Y; dX; dW, db; Y, stats; dX and three gradients; Y
