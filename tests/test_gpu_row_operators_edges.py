@@ -116,3 +116,47 @@ def test_a_result_is_not_in_memory_that_another_stream_still_writes(ctx):
         y = ctx.dropout(x, 0.5, 3, stream=side)
         torch.cuda.synchronize()
         assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("direction", ["y", "dx"])
+def test_deep_products_beside_another_contexts(direction):
+    """Products on pairs of blocks while another context's run on another stream: every one its own result, all of them right."""
+    one, two = binding.Context(0), binding.Context(0)
+    g = torch.Generator().manual_seed(4)
+    off = torch.tensor([0, 12_000, 12_000, 12_300, 30_001], device="cuda")
+    x = torch.randn(30_001, 512, generator=g).bfloat16().cuda()
+    W = (torch.randn(4, 512, 512, generator=g) / 20).bfloat16().cuda()
+    call = (lambda c, **k: c.grouped_linear(x, off, W, **k)) if direction == "y" else (lambda c, **k: c.grouped_linear_dx(x, off, W, **k))
+    want = call(one).clone()
+    W64 = W.double() if direction == "y" else W.double().mT
+    for k in range(4):
+        r = slice(int(off[k]), int(off[k + 1]))
+        exact, size = x[r].double() @ W64[k], x[r].double().abs() @ W64[k].abs()
+        assert ((want[r].double() - exact).abs() <= 2.0 ** -8 * 1.001 * exact.abs() + (512 + 16) * 2 * U * size).all()
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    outs = [[torch.zeros_like(want) for _ in range(6)] for _ in streams]
+    torch.cuda.synchronize()
+    for k in range(6):
+        for c, s, o in zip((one, two), streams, outs):
+            call(c, out=o[k], stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for side in outs for o in side)
+    one.check()
+    two.check()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("sign", [False, True])
+def test_the_longest_contractions(ctx, dtype, sign):
+    """16,384 terms.  Sums of 16-bit rows stay in the accumulator, truncated every 16 terms (a step, 2^-23 of the sum so far at most, towards zero):
+    with terms of one sign that is a drift of up to 1024 steps, a quarter of a rounding to fp16."""
+    K, N, n = 16384, 40, 300
+    g = torch.Generator().manual_seed(5)
+    draw = (lambda *s: torch.randn(*s, generator=g)) if sign else (lambda *s: torch.rand(*s, generator=g) + 0.5)
+    x, W = draw(n, K).to(dtype).cuda(), (draw(K, N) / 128).to(dtype).cuda()
+    tiny = torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps
+    for got, a, b in ((ctx.grouped_linear(x, None, W), x, W), (ctx.grouped_linear_dx(x, None, W.mT.contiguous()), x, W)):
+        exact, size = a.double() @ b.double(), a.double().abs() @ b.double().abs()
+        # sums within 16 terms are exact or truncated as well: 2 steps for each of the K / 16 additions
+        tol = torch.finfo(dtype).eps / 2 * 1.001 * exact.abs() + tiny + (2 * K / 16 + 16) * 2 * U * size
+        assert ((got.double() - exact).abs() <= tol).all()
