@@ -70,7 +70,7 @@ extern "C" int32_t rtma_dropout(rtma_ctx* ctx, int32_t dtype, int64_t n, int32_t
     RTMA_CUDA(ctx, on.status);
     RTMA_TRY(prepare_row_call(ctx, 0, stream));
     const size_t es = row_type_bytes(dtype);
-    DropoutArgs a{X, residual, Y, n, ldx, ldr, ldy, d, (d + 7) / 8, row_granule(X, ldx, es), row_granule(residual, ldr, es),
+    DropoutArgs a{X, residual, Y, n, ldx, ldr, ldy, d, (int)ceil_div(d, 8), row_granule(X, ldx, es), row_granule(residual, ldr, es),
                   row_granule(Y, ldy, es), drop_args(p, seed, row_ids)};
     const int64_t blocks = ceil_div(n * a.units, 256);
     const unsigned grid = (unsigned)(blocks < (int64_t)ctx->sm_count * 32 ? blocks : (int64_t)ctx->sm_count * 32);

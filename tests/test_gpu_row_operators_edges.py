@@ -1,5 +1,6 @@
 """The operators on the rows of many parts where their arguments are at an end: the most rows, expanded and overlapping tensors,
 runs of rows of every length, values whose squares do not fit.  Tolerances as in test_gpu_row_operators.py."""
+import numpy as np
 import pytest
 import torch
 
@@ -160,3 +161,25 @@ def test_the_longest_contractions(ctx, dtype, sign):
         # sums within 16 terms are exact or truncated as well: 2 steps for each of the K / 16 additions
         tol = torch.finfo(dtype).eps / 2 * 1.001 * exact.abs() + tiny + (2 * K / 16 + 16) * 2 * U * size
         assert ((got.double() - exact).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("d", [2 ** 31 - 1, 2 ** 31 - 9])
+def test_dropout_of_the_widest_row(ctx, d):
+    """One row of as many columns as an int32 counts: the mask of its last columns, and nothing behind them."""
+    def step(z):
+        z = z + np.uint64(0x9E3779B97F4A7C15)
+        z = (z ^ (z >> np.uint64(30))) * np.uint64(0xBF58476D1CE4E5B9)
+        z = (z ^ (z >> np.uint64(27))) * np.uint64(0x94D049BB133111EB)
+        return z ^ (z >> np.uint64(31))
+
+    x = torch.ones(1, d + 9, dtype=torch.float16, device="cuda")[:, :d]
+    y = torch.full((1, d + 9), 7.0, dtype=torch.float16, device="cuda")
+    ctx.dropout(x, 0.5, 11, out=y[:, :d])
+    assert (y[:, d:] == 7).all()
+    last = 4096
+    first = (d - last) // 4 * 4
+    with np.errstate(over="ignore"):
+        key = step(np.array([11], dtype=np.uint64))[0]
+        col = np.arange(first, d, dtype=np.uint64)
+        lane = (step(key ^ (col // np.uint64(4))) >> (np.uint64(16) * (col % np.uint64(4)))) & np.uint64(0xFFFF)
+    assert torch.equal(y[0, first:d].cpu(), torch.from_numpy(lane >= 32768).half() * 2)
