@@ -18,6 +18,7 @@ LIB_CHECKED_PATH = os.path.join(_PKG, "librtma_checked.so")   # built with -DRTM
 MAX_PARTS = 64
 MAX_LAYERS = 8
 MAX_GROUPS = 512
+MAX_INT32 = 2**31 - 1
 
 EXPORTS = (
     "rtma_create", "rtma_destroy", "rtma_last_error", "rtma_workspace_bytes", "rtma_partition", "rtma_partition_grouped",
@@ -433,6 +434,8 @@ class Context:
         if len(size) != 2 or (shape is not None and size != shape):
             raise ValueError(f"{name} must be a matrix{'' if shape is None else ' of ' + str(tuple(shape))}, got {tuple(size)}")
         n, d = size
+        if d > MAX_INT32:  # ctypes would cut it down without a word
+            raise ValueError(f"{name} has rows of {d} values, {MAX_INT32} are the most")
         ld, inner = t.stride()
         if inner != 1 and d > 1:
             raise ValueError(f"the values of a row of {name} must be adjacent")
@@ -452,6 +455,8 @@ class Context:
         size = offsets.shape
         if len(size) != 1 or size[0] < 2 or not offsets.is_contiguous():
             raise ValueError("offsets must be a contiguous vector of one more value than there are parts")
+        if size[0] > MAX_INT32:
+            raise ValueError(f"offsets of {size[0] - 1} parts, {MAX_GROUPS} are the most")
         return offsets.data_ptr(), size[0] - 1
 
     def _of_parts(self, t, name, dtype, G, shape, result=False):
@@ -549,6 +554,8 @@ class Context:
     def _norm(self, X, offsets, groups, gamma, beta, slope, scope, act, eps, p, seed, row_ids):
         if scope not in SCOPES or act not in ACTIVATIONS:
             raise ValueError(f"scope={scope!r} (of {list(SCOPES)}), act={act!r} (of {list(ACTIVATIONS)})")
+        if abs(groups) > MAX_INT32:
+            raise ValueError(f"{groups} sets of channels")
         off, G = self._parts(offsets)
         n, C = X.shape
         gm, gs = self._of_parts(gamma, "gamma", torch.float32, G, (C,))

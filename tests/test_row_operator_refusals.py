@@ -161,3 +161,30 @@ def test_results_are_allocated_on_the_stream_that_writes_them(ctx, monkeypatch, 
     results = list(every_call(ctx, stream=stream))
     assert len(results) == 6 and not on
     assert made == [None if stream is None else 77] * 11  # Y; dX; dW, db; Y, stats; dX and three gradients; Y
+
+
+WIDE = 2 ** 32 + 8  # 8 in 32 bits
+
+
+def meta(*shape, dtype=torch.float16):
+    return torch.empty(shape, dtype=dtype, device="meta")
+
+
+@pytest.mark.parametrize("call", [
+    lambda c: c.dropout(meta(1, WIDE), 0.5, 1),
+    lambda c: c.dropout(meta(1, 2 ** 31), 0.5, 1),
+    lambda c: c.grouped_linear(meta(1, WIDE), None, meta(WIDE, 4)),
+    lambda c: c.grouped_linear(meta(1, 4), None, meta(4, WIDE), out=meta(1, WIDE)),
+    lambda c: c.grouped_linear_dx(meta(1, WIDE), None, meta(4, WIDE)),
+    lambda c: c.grouped_linear_dx(meta(1, 4), None, meta(WIDE, 4), out=meta(1, WIDE)),
+    lambda c: c.grouped_linear_dw(meta(1, WIDE), meta(1, 4), None, dw=meta(1, WIDE, 4, dtype=torch.float32)),
+    lambda c: c.grouped_linear_dw(meta(1, 4), meta(1, WIDE), None, dw=meta(1, 4, WIDE, dtype=torch.float32)),
+    lambda c: c.group_norm(meta(1, WIDE), None, 8, out=meta(1, WIDE), stats=meta(1, 8, 2, dtype=torch.float32)),
+    lambda c: c.group_norm(meta(1, 8), None, 2 ** 32 + 8, stats=meta(1, 2 ** 32 + 8, 2, dtype=torch.float32)),
+    lambda c: c.group_norm(meta(1, 8), meta(2 ** 32 + 2, dtype=torch.int64), 8),
+])
+def test_sizes_of_more_than_31_bits(ctx, call):
+    """The C calls take them as int32; ctypes would cut them down without a word."""
+    with pytest.raises((ValueError, binding.RtmaError)):
+        call(ctx)
+    assert not ctx._lib.calls
