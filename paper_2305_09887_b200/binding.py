@@ -487,8 +487,6 @@ class Context:
     def _new(self, shape, dtype, stream):
         """Memory for a result, of the stream that the call is for: from the current stream's it might still be in use there, for something
         that has been freed, when `stream` writes to it."""
-        if stream is None:
-            return torch.empty(shape, dtype=dtype, device=self.device)
         with torch.cuda.stream(torch.cuda.ExternalStream(_stream_handle(stream), device=self.device)):
             return torch.empty(shape, dtype=dtype, device=self.device)
 
@@ -506,7 +504,7 @@ class Context:
         w, ws = self._of_parts(W, "W", X.dtype, G, (d_in, d_out))
         b, bs = self._of_parts(bias, "bias", X.dtype, G, (d_out,))
         if out is None:
-            out = self._new((n, d_out), X.dtype, stream)
+            out = torch.empty(n, d_out, dtype=X.dtype, device=self.device) if stream is None else self._new((n, d_out), X.dtype, stream)
         y, ldy = self._rows(out, "out", X.dtype, (n, d_out))
         self._check(self._lib.rtma_grouped_linear(self._h, ROW_TYPES[X.dtype], n, G, off, d_in, d_out, x, ldx, w, ws, b, bs, y, ldy,
                                                   self._stream(stream)), "rtma_grouped_linear")
@@ -520,7 +518,7 @@ class Context:
         d_in = W.shape[-2]
         w, ws = self._of_parts(W, "W", dY.dtype, G, (d_in, d_out))
         if out is None:
-            out = self._new((n, d_in), dY.dtype, stream)
+            out = torch.empty(n, d_in, dtype=dY.dtype, device=self.device) if stream is None else self._new((n, d_in), dY.dtype, stream)
         x, ldx = self._rows(out, "out", dY.dtype, (n, d_in))
         self._check(self._lib.rtma_grouped_linear_dx(self._h, ROW_TYPES[dY.dtype], n, G, off, d_in, d_out, g, ldg, w, ws, x, ldx,
                                                      self._stream(stream)), "rtma_grouped_linear_dx")
@@ -539,9 +537,9 @@ class Context:
         off, G = self._parts(offsets)
         lead = () if shared else (G,)
         if dw is None:
-            dw = self._new((*lead, d_in, d_out), torch.float32, stream)
+            dw = torch.empty(*lead, d_in, d_out, dtype=torch.float32, device=self.device) if stream is None else self._new((*lead, d_in, d_out), torch.float32, stream)
         if db is None and bias:
-            db = self._new((*lead, d_out), torch.float32, stream)
+            db = torch.empty(*lead, d_out, dtype=torch.float32, device=self.device) if stream is None else self._new((*lead, d_out), torch.float32, stream)
         for t, name, rank in ((dw, "dw", 2), (db, "db", 1)):
             if t is not None and t.dim() != rank + len(lead):
                 raise ValueError(f"{name} has {t.dim()} dimensions with shared={shared}")
@@ -599,11 +597,11 @@ class Context:
         off, G, desc, gm, bt, sl, ids = self._norm(X, offsets, groups, gamma, beta, slope, scope, act, eps, p, seed, row_ids)
         n = X.shape[0]
         if out is None:
-            out = self._new(X.shape, X.dtype, stream)
+            out = torch.empty_like(X, memory_format=torch.contiguous_format) if stream is None else self._new(X.shape, X.dtype, stream)
         y, ldy = self._rows(out, "out", X.dtype, X.shape)
         shape = (n if scope == "row" else G, int(groups), 2)
         if stats is None:
-            stats = self._new(shape, torch.float32, stream)
+            stats = torch.empty(shape, dtype=torch.float32, device=self.device) if stream is None else self._new(shape, torch.float32, stream)
             st = stats.data_ptr()
         else:
             st = self._of_parts(stats, "stats", torch.float32, 1, shape)[0]
@@ -621,9 +619,12 @@ class Context:
         g, ldg = self._rows(dY, "dY", X.dtype, (n, C))
         st = self._of_parts(stats, "stats", torch.float32, 1, (n if scope == "row" else G, int(groups), 2))[0]
         if out is None:
-            out = self._new(X.shape, X.dtype, stream)
+            out = torch.empty_like(X, memory_format=torch.contiguous_format) if stream is None else self._new(X.shape, X.dtype, stream)
         dx, lddx = self._rows(out, "out", X.dtype, (n, C))
-        new = lambda like: self._new(like.shape, torch.float32, stream)  # noqa: E731
+        if stream is None:
+            new = lambda like: torch.empty(like.shape, dtype=torch.float32, device=self.device)  # noqa: E731
+        else:
+            new = lambda like: self._new(like.shape, torch.float32, stream)  # noqa: E731
         dgamma = new(gamma) if dgamma is None and gamma is not None else dgamma
         dbeta = new(beta) if dbeta is None and beta is not None else dbeta
         dslope = new(slope) if dslope is None and act == "prelu" and slope is not None else dslope
@@ -644,7 +645,7 @@ class Context:
         r, ldr = (None, 0) if residual is None else self._rows(residual, "residual", X.dtype, (n, d))
         ids = self._ids(row_ids, n)
         if out is None:
-            out = self._new(X.shape, X.dtype, stream)
+            out = torch.empty_like(X, memory_format=torch.contiguous_format) if stream is None else self._new(X.shape, X.dtype, stream)
         y, ldy = self._rows(out, "out", X.dtype, X.shape)
         self._check(self._lib.rtma_dropout(self._h, ROW_TYPES[X.dtype], n, d, x, ldx, ids, r, ldr, float(p), int(seed) & (2**64 - 1), y, ldy,
                                            self._stream(stream)), "rtma_dropout")
