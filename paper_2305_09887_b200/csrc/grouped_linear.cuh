@@ -41,21 +41,20 @@ struct LinearArgs {
 };
 
 #ifdef __CUDACC__
-// Chunks of a part's rows.  Unsigned: a part has up to 2^31 - 1 rows, which with a chunk added to them no longer fit a signed number;
-// a chunk smaller than the largest part, the only ones asked about, fits an unsigned one.
-__host__ __device__ __forceinline__ uint32_t chunks_in(uint32_t rows, uint32_t chunk) { return (rows + chunk - 1) / chunk; }
-// The smallest chunk, of `least` rows or more and a multiple of `step`, of which all parts have not more than `tiles`; by bisection.
-// most: rows of the largest part; count(c): chunks of c rows in all parts.  `tiles` is at least the number of parts.
+// Rows in whole steps of STEP: up to 2^31 - 1 of them with a chunk added do not fit 31 bits, their steps do.
+template <int STEP>
+__host__ __device__ __forceinline__ int steps_of(int rows) { return (int)(((uint32_t)rows + (STEP - 1)) / STEP); }
+// The smallest chunk, of `least` steps or more, of which all parts have not more than `tiles`; by bisection.  most: steps of the largest
+// part; count(c): chunks of c steps in all parts.  `tiles` is at least the number of parts.
 template <class Count>
-__host__ __device__ __forceinline__ uint32_t fit_chunk(uint32_t least, uint32_t most, uint32_t step, int64_t tiles, Count count) {
-    uint32_t lo = least / step, hi = (most + step - 1) / step;  // hi fits: a chunk a part
-    if (hi < lo) hi = lo;
+__host__ __device__ __forceinline__ int fit_chunk(int least, int most, int64_t tiles, Count count) {
+    int lo = least, hi = most > least ? most : least;  // hi fits: a chunk a part
     while (lo < hi) {
-        const uint32_t mid = (lo + hi) / 2;
-        if (count(mid * step) <= tiles) hi = mid;
+        const int mid = (lo + hi) / 2;
+        if (count(mid) <= tiles) hi = mid;
         else lo = mid + 1;
     }
-    return lo * step;
+    return lo;
 }
 
 struct Shared {
@@ -154,13 +153,14 @@ __device__ __forceinline__ void lay_out(const LinearArgs& a, Shared& sh) {
             int most = 1;
             for (int g = lane; g < a.G; g += 32) most = max(most, sh.rows[g]);
             for (int o = 16; o > 0; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
-            // (2^31 rows are no chunk: with fewer than 256 parts there are twice as many tiles, unless rows are so wide that 2^31 of them fit no memory.)
-            const int32_t rows = (int32_t)fit_chunk((uint32_t)a.tile_rows, (uint32_t)most, STEP, a.tiles, [&](uint32_t chunk) {
+            const int chunk = fit_chunk((int)a.tile_rows / STEP, steps_of<STEP>(most), a.tiles, [&](int steps) {
                 int64_t count = 0;
-                for (int g = lane; g < a.G; g += 32) count += chunks_in((uint32_t)sh.rows[g], chunk);
+                for (int g = lane; g < a.G; g += 32) count += (steps_of<STEP>(sh.rows[g]) + steps - 1) / steps;
                 for (int o = 16; o > 0; o >>= 1) count += __shfl_xor_sync(0xffffffffu, count, o);
                 return count;
             });
+            // (2^31 rows are no chunk: with fewer than 256 parts there are twice as many tiles, unless rows are so wide that 2^31 of them fit no memory.)
+            const int32_t rows = chunk * STEP;
             if (lane == 0) {
                 sh.tile_rows = rows;
                 if (blockIdx.x == 0) *a.chunk_rows = rows;

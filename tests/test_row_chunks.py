@@ -12,14 +12,18 @@ from paper_2305_09887_b200 import build
 LEAST, MOST = 256, 2 ** 31 - 1
 SOURCE = """
 #include "grouped_linear.cuh"
-extern "C" uint32_t fit(int parts, const uint32_t* rows, uint32_t least, uint32_t step, int64_t tiles) {
-    uint32_t most = 1;
+template <int STEP>
+int64_t fit_rows(int parts, const int32_t* rows, int64_t least, int64_t tiles) {
+    int most = 1;
     for (int g = 0; g < parts; ++g) most = rows[g] > most ? rows[g] : most;
-    return grouped::fit_chunk(least, most, step, tiles, [&](uint32_t chunk) {
+    return (int64_t)STEP * grouped::fit_chunk((int)least / STEP, grouped::steps_of<STEP>(most), tiles, [&](int steps) {
         int64_t count = 0;
-        for (int g = 0; g < parts; ++g) count += grouped::chunks_in(rows[g], chunk);
+        for (int g = 0; g < parts; ++g) count += (grouped::steps_of<STEP>(rows[g]) + steps - 1) / steps;
         return count;
     });
+}
+extern "C" int64_t fit(int parts, const int32_t* rows, int64_t least, int step, int64_t tiles) {
+    return step == 32 ? fit_rows<32>(parts, rows, least, tiles) : fit_rows<64>(parts, rows, least, tiles);
 }
 """
 
@@ -32,9 +36,9 @@ def fit(tmp_path_factory):
         f.write(SOURCE)
     subprocess.run([build._nvcc()] + build.NVCC_FLAGS + ["-shared", source, "-o", shared], check=True)
     call = ctypes.CDLL(shared).fit
-    call.restype = ctypes.c_uint32
-    call.argtypes = [ctypes.c_int, ctypes.POINTER(ctypes.c_uint32), ctypes.c_uint32, ctypes.c_uint32, ctypes.c_int64]
-    return lambda rows, step, tiles: call(len(rows), (ctypes.c_uint32 * len(rows))(*rows), LEAST, step, tiles)
+    call.restype = ctypes.c_int64
+    call.argtypes = [ctypes.c_int, ctypes.POINTER(ctypes.c_int32), ctypes.c_int64, ctypes.c_int, ctypes.c_int64]
+    return lambda rows, step, tiles: call(len(rows), (ctypes.c_int32 * len(rows))(*rows), LEAST, step, tiles)
 
 
 def check(fit, rows, step, tiles):
