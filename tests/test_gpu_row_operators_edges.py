@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+import row_reference as ref
 from paper_2305_09887_b200 import binding
 
 pytestmark = pytest.mark.gpu
@@ -183,3 +184,22 @@ def test_dropout_of_the_widest_row(ctx, d):
         col = np.arange(first, d, dtype=np.uint64)
         lane = (step(key ^ (col // np.uint64(4))) >> (np.uint64(16) * (col % np.uint64(4)))) & np.uint64(0xFFFF)
     assert torch.equal(y[0, first:d].cpu(), torch.from_numpy(lane >= 32768).half() * 2)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("deviations", [0.0, 60.0, 63.9, 64.1, 70.0, 500.0])
+def test_norm_of_a_part_with_means_on_both_sides_of_the_folding(ctx, dtype, deviations):
+    """The mean folded into the shift, 2^-24 of up to 64 deviations off, or subtracted: both within a few roundings of the result, and mixed within a row."""
+    n, C, groups = 30_000, 64, 8
+    g = torch.Generator().manual_seed(6)
+    x = torch.randn(n, C, generator=g)
+    x[:, :24] += deviations  # three of the eight sets
+    x = x.to(dtype).cuda()
+    gamma, beta = torch.randn(C, generator=g).cuda(), torch.randn(C, generator=g).cuda()
+    y, st = ctx.group_norm(x, None, groups, gamma, beta, scope="part")
+    want, stats, u, xhat = ref.group_norm(x.to(F64), [0, n], groups, gamma.to(F64)[None], beta.to(F64)[None], "part", "none", None, 1e-5)
+    # statistics: sums at most 8 (channels) + 16 + 240 steps deep, three roundings each; the folding: 64 deviations at 2^-24, times gamma
+    size, rstd = x.to(F64).abs().view(n, groups, 8).amax(dim=(0, 2)), stats[0, :, 1]
+    tol_x = (3 * U * 270 * (size * rstd)).repeat_interleave(8) + 3 * U * 270 * xhat.abs() + 64 * U
+    tol = gamma.to(F64).abs() * tol_x + 4 * U * (want.abs() + beta.to(F64).abs()) + torch.finfo(dtype).eps / 2 * 1.001 * want.abs() + 2.0 ** -24
+    assert ((y.to(F64) - want).abs() <= tol).all()
