@@ -116,7 +116,7 @@ __device__ __forceinline__ float activate_back(int act, float slope, const f2 (&
 
 // (x - mean) * rstd of a pair.  The difference first, so that a mean much larger than the deviation costs no digits: with the mean
 // folded into x rstd + (-mean rstd) a set of equal values, whose rstd is 1 / sqrt(eps), is off by half a step of mean rstd.  The
-// subtraction costs the row gradient of 16-bit rows 2 % (1M x 256 in one set 314 -> 319 us).
+// subtraction costs the row gradient of 16-bit rows 2 % (1M x 256 in one set 314 -> 320 us).
 struct Standard {
     f2 r, m;
     __device__ __forceinline__ void set(float mean0, float rstd0, float mean1, float rstd1) {
@@ -315,9 +315,10 @@ struct Run {
 // A row lies in `pitch` lanes (a power of two, 256 at most), eight channels each; a set is the whole row or a power of two of
 // neighbouring lanes, so its sums are exchanged within a warp, and only those of sets of more than 256 channels (WIDE) go through
 // shared memory.  RB rows side by side hide one another's loads and shuffles.  Reads each row once; bound by instructions (two sums
-// exchanged per row, the activation) at 4.7 to 6 TB/s: 2M x 128 in bf16 with ReLU 205 us, 200,000 x 1024 in 8 sets fp32 with SiLU 280;
-// gradients of 200,000 x 256 in 8 sets, fp32 with dropout, 132 us and of 1M x 256 in bf16 314.  With up to 16 channels a lane instead
-// (and shared memory above 512) these two and 500,000 x 512 took 132, 405 and 466 us.
+// exchanged per row, the activation) at 4.7 to 6 TB/s: 2M x 128 in bf16 with ReLU 185 us, 200,000 x 1024 in 8 sets fp32 with SiLU 280;
+// gradients of 200,000 x 256 in 8 sets, fp32 with dropout, 132 us and of 1M x 256 in bf16 320 (two rows of three kinds fill the 128 registers:
+// of fp32 rows 56 bytes a thread are spilled, 64 with WIDE, 104 and 152 where units are not whole; 16-bit rows spill nothing).  With up to 16
+// channels a lane instead (and shared memory above 512) these two and 500,000 x 512 took 132, 405 and 466 us.
 // Sums over `lanes` lanes, in every lane.  WIDE: red, 8 floats per sum, is used by every other call.
 template <bool WIDE, int N>
 __device__ __forceinline__ void set_sums(float (&x)[N], int lanes, float* red) {
@@ -514,7 +515,8 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_warp_rows_grad_kernel(co
 // ---- rows whose sets share units ---------------------------------------------
 // Sets of eight channels or more that do not end with a unit: a unit's channels belong to one set or to two.  A row lies in `pitch`
 // lanes as above; a set's sum grows from lane to lane in a scan that starts anew where a set begins, is complete in the lane with the
-// set's last channel and fetched from there.  WIDE: rows of more than 256 channels; the warps' scans are joined in shared memory.  Bound by instructions: 1M x 100 in 4 sets, fp16, 227 us, gradient 283 (through shared memory,
+// set's last channel and fetched from there.  WIDE: rows of more than 256 channels; the warps' scans are joined in shared memory.
+// Bound by instructions: 1M x 100 in 4 sets, fp16, 230 us, gradient 287 (through shared memory,
 // by the kernels for all other sets, 550 and 990); 1M x 240 in 10 sets, fp32, 369 and 582.  WIDE by its barriers, too: 500,000 x 300 in
 // 3 sets, fp16, 745 and 888 (853 and 1408), x 384 in 8 sets, fp32, 703 and 787.
 struct Straddle {
@@ -677,7 +679,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_straddle_rows_kernel(con
 
 template <class T, bool FULL, bool WIDE>
 __global__ void __launch_bounds__(NORM_THREADS, 2) norm_straddle_rows_grad_kernel(const NormArgs a) {
-    constexpr int RB = 1;  // rows in flight: two do not fit the registers (1M x 100 in 4 sets, fp16: 320 us instead of 283)
+    constexpr int RB = 1;  // rows in flight: two do not fit the registers (1M x 100 in 4 sets, fp16: 320 us instead of 287)
     __shared__ float ends[WIDE ? 16 * RB : 1], sums[WIDE ? 2 * NORM_THREADS * RB : 1];
     __shared__ float shared[8 * NORM_THREADS];
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
@@ -766,7 +768,8 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_straddle_rows_grad_kerne
 
 // ---- rows whose sets lie within units --------------------------------------------------------------
 // Sets of P = 1, 2 or 4 channels: a lane has all of a set, nothing is exchanged.  (Channels that are not there are whole sets.)
-// 1M x 64 in 32 sets, bf16, 127 us, gradient 130 (through shared memory 435 and 645); 200,000 x 128 in 32 sets, fp32, 47 and 73.
+// 1M x 64 in 32 sets, bf16, 117 to 127 us, gradient 130 (through shared memory 435 and 645); 200,000 x 128 in 32 sets, fp32, 47 and 73.
+// (Of the gradient's forms only that of single fp32 channels in rows that are not whole units spills: 32 bytes a thread.)
 template <int P>
 __device__ __forceinline__ void sums_within(f2 (&x)[4]) {  // every channel's set's sum
 #pragma unroll
@@ -1201,7 +1204,7 @@ __device__ __forceinline__ void load_part_stats(const NormArgs& a, int part, con
     }
 }
 
-// The second pass of part scope; 2M x 128 in bf16 with SiLU: 160 us.  (Rows backwards, so that it starts with what the first pass read
+// The second pass of part scope; 2M x 128 in bf16 with SiLU: 160 us (4 bytes a thread are spilled).  (Rows backwards, so that it starts with what the first pass read
 // last, and loads and stores past the cache changed nothing: it is not memory alone that bounds it.)
 
 // minus the mean, rstd gamma and beta of a thread's channels
@@ -1303,7 +1306,8 @@ __global__ void __launch_bounds__(NORM_THREADS, FULL ? 3 : 2) norm_apply_kernel(
 
 // The gradient of part scope in two passes, as the sums over a part have to be complete before any of its rows: 500,000 x 256 in
 // bf16 with SiLU 262 us, 8 of them for joining the sums; the rows' pass works out du again (storing it would cost as many bytes).  Bound by
-// the loads on their way: with two rows of 16-bit values in flight instead of four 281 us, without an activation 254 (four: 226).
+// the loads on their way: with two rows of 16-bit values in flight instead of four 281 us, without an activation 254 (four: 226).  The first
+// kernel spills 32 bytes a thread of 16-bit rows and 16 of fp32 ones (up to 52 where units are not whole), the second 12 and 8 (up to 36).
 template <class T, bool FULL>
 __global__ void __launch_bounds__(NORM_THREADS, 2) norm_grad_sums_kernel(const NormArgs a) {
     constexpr int RB = 8 / sizeof(T);  // rows in flight

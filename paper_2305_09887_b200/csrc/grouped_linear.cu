@@ -18,10 +18,13 @@
 //   PAIR    the same on pairs of blocks (a cluster of two, MMAs of 256 rows) that bring half of the right operand each
 // then 8 drain warps (a quarter of the lanes, every second 32 columns each) and one warp that issues the MMAs.
 //
-// What bounds it: up to 256 terms the rows' bytes (dx of 2M x 256 -> 256 in bf16 324 us, 6.3 TB/s), above that the operands' way from the
-// L2 cache (500,000 x 512 -> 512 260 to 270 us, 1 PFLOP/s; 200,000 x 1024 -> 1024 356 us, 1.18); the weight gradient reads each row of X and dY
+// What bounds it: up to 256 terms the rows' bytes (dx of 2M x 256 -> 256 in bf16 324 us, 6.3 TB/s).  Above that waiting for operands, though no
+// unit is full: of 100,000 x 512 -> 512 on pairs (59 us under the profiler) the tensor pipes are busy for 43 %, the L2 cache for 34 %,
+// memory for 35 % (500,000 rows 260 to 270 us, 1 PFLOP/s; 200,000 x 1024 -> 1024 356 us, 1.18).  The weight gradient reads each row of X and dY
 // once per 128 columns of the other (1M x 256 x 256 in bf16 320 to 335 us), and shared memory, from which an MMA of 128 x 128 reads 128
-// bytes a clock; rows off 16-byte boundaries the copies (1M x 100 x 256 in fp16 200 to 230 us, 1M x 47 -> 90 in bf16 150).
+// bytes a clock.  Rows off 16-byte boundaries: the copies (1M x 100 x 256 in fp16 200 to 230 us, 1M x 47 -> 90 in bf16 150); of that weight
+// gradient with 500,000 rows shared memory's data path is busy for 50 %, instructions are issued in 48 % of the cycles, tensor pipes 28 %.
+// Its kernel is the one here that spills: 256 bytes a thread at 72 registers (80 sums and 8 loaded values in a drain warp's lane).
 #include <algorithm>
 
 #include "grouped_linear.cuh"
@@ -665,7 +668,8 @@ int32_t launch_linear(rtma_ctx* ctx, int32_t dtype, LinearArgs& a, int cls, cuda
     const bool bf16 = dtype == RTMA_BF16;
     // Pairs of blocks where the contraction is deep: each then brings half of the right operand, which comes from the L2 cache again for
     // every tile (bf16, alone / in pairs: 500,000 x 512 -> 512 285 / 270 us, 30,000 rows 35 / 27; 1M x 256 -> 256 181 / 170, 30,000 rows
-    // 17 / 14).  Short contractions are drains, which a pair's blocks wait for together: 1M x 64 -> 256 123 / 133.
+    // 17 / 14).  Short contractions are drains, which a pair's blocks wait for together: 1M x 64 -> 256 123 / 133.  A pair's block brings 128
+    // columns, so tiles of other widths (384 columns are two of 192, 600 three of 208) never pair.
     bool pair = false;
     if constexpr (MODE != WEIGHT_GRADIENT) pair = a.BN == 256 && (MODE == FORWARD ? a.d_in : a.d_out) >= 256 && tiles >= ctx->sm_count;
     a.in_bulk = bulk_maps<MODE>(a, bf16, pair);

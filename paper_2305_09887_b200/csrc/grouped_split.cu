@@ -13,7 +13,9 @@
 // 256 x 47 gradient of as many rows (two: 103).
 //
 // Bound by the chain of these steps, not by the six MMAs (47 us) or the bytes (48) of the first: 200,000 x 128 -> 256 125 us, its dx 133, the
-// gradient of 256 x 256 295 (90 TFLOP/s of fp32 products).
+// gradient of 256 x 256 295 (90 TFLOP/s of fp32 products).  Of the first, shared memory's data path is busy for 62 % of the cycles, the
+// tensor pipes for 29 %, memory for 24 %, and instructions are issued in 35 %; of the 256 x 47 gradient 46, 15, 34 and 46 %.  The dx kernels
+// spill 16 bytes a thread, the others nothing.
 #include "grouped_linear.cuh"
 
 RTMA_BOUNDS_TU()
