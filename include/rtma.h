@@ -363,8 +363,9 @@ enum { RTMA_F32 = 0, RTMA_BF16 = 1, RTMA_F16 = 2 };
 /* Y[r] = X[r] W_g + b_g for the rows r of part g.  W_g [d_in][d_out] row-major at W + g * w_stride,
  * b_g [d_out] at b + g * b_stride (b may be NULL).  X [n][ldx], Y [n][ldy]; they must not overlap.
  * Of fp32 rows the products are fp32 ones (no TF32): each factor is used as three bf16 numbers that
- * add up to it, and only what is below 2^-22 of a product is left out; a value of X that is not
- * finite makes its row of Y not finite, possibly NaN where fp32 arithmetic gives an infinity.
+ * add up to it (to within 2^-133, the smallest of them, which values below 2^-110 feel), and only what
+ * is below 2^-22 of a product is left out; a value of X that is not finite makes its row of Y not
+ * finite, possibly NaN where fp32 arithmetic gives an infinity.
  * Sums of fp32 rows are rounded to nearest every 32 terms.  Sums of 16-bit rows, here and in _dx, stay
  * in the tensor cores' accumulators, which truncate: towards zero by up to a step (2^-23) for every 16
  * terms; for terms of one sign 3e-6 of the sum at 512 terms and 1e-4 at 16,384 were measured, a fifth of

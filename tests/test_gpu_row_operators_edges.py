@@ -203,3 +203,24 @@ def test_norm_of_a_part_with_means_on_both_sides_of_the_folding(ctx, dtype, devi
     tol_x = (3 * U * 270 * (size * rstd)).repeat_interleave(8) + 3 * U * 270 * xhat.abs() + 64 * U
     tol = gamma.to(F64).abs() * tol_x + 4 * U * (want.abs() + beta.to(F64).abs()) + torch.finfo(dtype).eps / 2 * 1.001 * want.abs() + 2.0 ** -24
     assert ((y.to(F64) - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("exponent", [-100, -110, -115, -120, -126, -130])
+def test_fp32_products_of_tiny_values(ctx, exponent):
+    """A factor's three bf16 numbers add up to it to within the smallest of them, 2^-133 (the last is cut off, the second rounded: once each)."""
+    g = torch.Generator().manual_seed(9)
+    K, n = 64, 300
+    small = ((torch.rand(n, K, generator=g) + 0.5).to(F64) * 2.0 ** exponent).float().cuda()
+    W = (torch.rand(K, 40, generator=g) + 0.5).cuda()
+    ones = torch.ones(n, 40, device="cuda")
+
+    def check(got, a, b, tiny_is_a, steps):
+        a, b = a.to(F64), b.to(F64)
+        size = a.abs() @ b.abs()
+        lost = 2 * 2.0 ** -133 * (torch.ones_like(a) @ b.abs() if tiny_is_a else a.abs() @ torch.ones_like(b))
+        assert ((got.to(F64) - a @ b).abs() <= (steps + 16) * 2 * U * size + lost + 2.0 ** -149).all()
+
+    check(ctx.grouped_linear(small, None, W), small, W, True, K)
+    check(ctx.grouped_linear_dx(small, None, W.mT.contiguous()), small, W, True, K)
+    check(ctx.grouped_linear(ones[:, :K // 2].contiguous(), None, small[:K // 2].contiguous()), ones[:, :K // 2], small[:K // 2], False, K)
+    check(ctx.grouped_linear_dw(small, ones, None)[0][0], small.mT, ones, True, n)
