@@ -527,7 +527,7 @@ class Context:
     def grouped_linear_dw(self, X, dY, offsets, shared=False, dw=None, db=None, bias=True, stream=None):
         """(dW, db) of grouped_linear in float32: dW_g = sum_r X[r]^T dY[r], db_g = sum_r dY[r]; [G, d_in, d_out] and [G, d_out],
         or summed over all parts without the leading G (shared).  dw, db: where to write them (views of a replica's gradients,
-        for instance).  bias=False: dW alone, db is None."""
+        for instance; memory of its own for every part, no expanded views).  bias=False: dW alone, db is None."""
         x, ldx = self._rows(X, "X")
         n, d_in = X.shape
         g, ldg = self._rows(dY, "dY", X.dtype)
@@ -612,7 +612,7 @@ class Context:
     def group_norm_grad(self, X, dY, stats, offsets, groups, gamma=None, beta=None, scope="row", act="none", slope=None, eps=1e-5, p=0.0,
                         seed=0, row_ids=None, out=None, dgamma=None, dbeta=None, dslope=None, stream=None):
         """(dX, dgamma, dbeta, dslope) of group_norm from its X, its stats and dY; the parameters' gradients in float32, in the
-        parameters' shape (summed over the parts for a shared one), None for a parameter that is None."""
+        parameters' shape (summed over the parts for a shared one; no expanded views), None for a parameter that is None."""
         x, ldx = self._rows(X, "X")
         off, G, desc, gm, bt, sl, ids = self._norm(X, offsets, groups, gamma, beta, slope, scope, act, eps, p, seed, row_ids)
         n, C = X.shape

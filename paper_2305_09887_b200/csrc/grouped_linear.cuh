@@ -16,7 +16,7 @@ struct LinearArgs {
     const int64_t* offsets;
     int64_t n;
     int G, span;
-    int64_t tile_rows, tiles;  // rows of a row tile (forward, dx: 128; dw: at least, see fit_chunks), row tiles at most
+    int64_t tile_rows, tiles;  // rows of a row tile (forward, dx: 128; dw: at least, see fit_chunk), row tiles at most
     int m_tiles, n_tiles;      // tiles of one row tile: m_tiles (dw) x n_tiles
     int BN;
     int d_in, d_out;
