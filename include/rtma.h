@@ -425,6 +425,34 @@ int32_t rtma_group_norm_grad(rtma_ctx* ctx, const rtma_norm_desc* desc, int64_t 
                              float* dgamma, int64_t dgamma_stride, float* dbeta, int64_t dbeta_stride,
                              float* dslope, int64_t dslope_stride, void* stream);
 
+/* A whole layer on the rows r of part g:
+ *   Y[r] = residual[r] + act(X[r] W_g + b_g)                                         gated = 0
+ *   Y[r] = residual[r] + act(X[r] V_g + c_g) * (X[r] U_g + d_g), W_g = [V_g | U_g], b_g = [c_g | d_g]   gated = 1
+ * W_g [d_in][d_out], or [d_in][2 d_out] of a gated layer (2 d_out <= RTMA_MAX_WIDTH); b (may be NULL) likewise; both of the rows' type.
+ * act and slope (PReLU: one per part) as in rtma_group_norm; any of them gates.  The product is held in fp32 up to
+ * the one rounding of Y; sums as in rtma_grouped_linear.  residual [n][ldr] may be NULL, and may be Y.  X and Y must not overlap. */
+typedef struct {
+    int32_t dtype, d_in, d_out, act, gated;
+    int32_t grad_dtype; /* of dW and db: RTMA_F32 or dtype */
+    int64_t w_stride, b_stride, slope_stride;
+} rtma_layer_desc;
+int32_t rtma_grouped_layer(rtma_ctx* ctx, const rtma_layer_desc* desc, int64_t n, int32_t G, const int64_t* offsets,
+                           const void* X, int64_t ldx, const void* W, const void* b, const float* slope,
+                           const void* residual, int64_t ldr, void* Y, int64_t ldy, void* stream);
+/* Its gradient from the inputs alone; nothing is kept from the forward call (Z = X W + b is worked out again).  The residual's gradient
+ * is dY itself.
+ *   dZ [n][lddz]  of the rows' type, d_out (gated: 2 d_out) values: receives the gradient of Z, rounded to that type, from which the rest
+ *                 is formed.  May be dY if not gated.  Not used (may be NULL) by a layer with neither activation nor gate: dZ is dY.
+ *   dX            = dZ W_g^T (NULL: not wanted).  It overlaps neither X nor dZ.
+ *   dW, db        as in rtma_grouped_linear_dw with dZ in dY's place (each may be NULL; db only with dW), in grad_dtype, rounded once.
+ *   dslope        float, PReLU only (may be NULL): sum of dY min(Z, 0) (gated: of dY U min(V, 0)); stride 0 with G > 1: over all parts.
+ * At Z = 0 ReLU and PReLU take the derivative of the negative side.                            */
+int32_t rtma_grouped_layer_grad(rtma_ctx* ctx, const rtma_layer_desc* desc, int64_t n, int32_t G, const int64_t* offsets,
+                                const void* X, int64_t ldx, const void* W, const void* b, const float* slope,
+                                const void* dY, int64_t lddy, void* dZ, int64_t lddz, void* dX, int64_t lddx, void* dW,
+                                int64_t dw_stride, void* db, int64_t db_stride, float* dslope, int64_t dslope_stride,
+                                void* stream);
+
 /* Y = residual + dropout(X) for n rows of d values (residual NULL: none).  The mask is never stored:
  * element (row id v, column j) is dropped iff 16 bits of a hash are below t = floor(65536 p + 1/2),
  *   h = S(S(seed) ^ ((uint64)(uint32)v << 32 | j / 4)), S = one SplitMix64 step, bits 16 (j mod 4) ..
@@ -436,6 +464,24 @@ int32_t rtma_group_norm_grad(rtma_ctx* ctx, const rtma_norm_desc* desc, int64_t 
 int32_t rtma_dropout(rtma_ctx* ctx, int32_t dtype, int64_t n, int32_t d, const void* X, int64_t ldx,
                      const int32_t* row_ids, const void* residual, int64_t ldr, double p, uint64_t seed,
                      void* Y, int64_t ldy, void* stream);
+
+/* The norm of every part's gradients over all their tensors, and the gradients scaled down to a largest norm:
+ *   norms[g] = sqrt(sum over the tensors of the sum of x^2 over part g's share),  out = c_g x,  c_g = min(1, max_norm / norms[g])
+ * grads: HOST array of `count` tensors.  Part g's share of a tensor are the `size` values from grad + g * grad_stride on (elements;
+ * G = 1: whole tensors); one_norm: norms[0] over all parts instead, for all of them.  Its result goes to out + g * out_stride, in the gradient's type or in RTMA_F32
+ * (out NULL: not wanted; out == grad, with the same type and stride: in place, and then not written where c_g is 1).  So 16-bit
+ * gradients of the calls above can go, clipped, to the places in grads [M][P] that rtma_sgd_aggregate takes.
+ * norms [G] float (device) or NULL.  0 <= max_norm (infinity: nothing is clipped).  A part whose norm is not finite keeps its
+ * gradients as they are or (zero_nonfinite) gets zeros, so that its step does nothing.  Squares are summed in 64 bits: values whose squares do
+ * not fit fp32 are no matter.  Results must not overlap other tensors.                          */
+typedef struct {
+    const void* grad;
+    void* out;
+    int64_t size, grad_stride, out_stride;
+    int32_t dtype, out_dtype;
+} rtma_gradient;
+int32_t rtma_clip_gradients(rtma_ctx* ctx, int32_t count, const rtma_gradient* grads, int32_t G, int32_t one_norm,
+                            double max_norm, int32_t zero_nonfinite, float* norms, void* stream);
 
 /* ---- R2: aggregation (Algorithm 1, phi = plain average; Algorithm 2, overwrite) ---------
  * Wbar[j] = (1/M) sum_i params[i][j]; every replica is overwritten with Wbar; global_out

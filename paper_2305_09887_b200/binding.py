@@ -8,7 +8,9 @@ CUDA device is present the calls raise.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
+import struct
 
 import torch
 
@@ -29,6 +31,7 @@ EXPORTS = (
     "rtma_link_steps", "rtma_set_workspace_limit", "rtma_local_steps_gathered", "rtma_bounds_checked", "rtma_sample_hop",
     "rtma_set_dense_aggregation", "rtma_selftest_chunks", "rtma_grouped_linear", "rtma_grouped_linear_dx",
     "rtma_grouped_linear_dw", "rtma_group_norm", "rtma_group_norm_grad", "rtma_dropout",
+    "rtma_grouped_layer", "rtma_grouped_layer_grad", "rtma_clip_gradients",
 )
 KERNEL_CLASSES = 21
 
@@ -66,6 +69,13 @@ class NormDesc(ctypes.Structure):
                 ("gamma_stride", ctypes.c_int64), ("beta_stride", ctypes.c_int64), ("slope_stride", ctypes.c_int64)]
 
 
+class LayerDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("d_in", ctypes.c_int32), ("d_out", ctypes.c_int32), ("act", ctypes.c_int32), ("gated", ctypes.c_int32),
+                ("grad_dtype", ctypes.c_int32), ("w_stride", ctypes.c_int64), ("b_stride", ctypes.c_int64), ("slope_stride", ctypes.c_int64)]
+
+
+GRADIENT = struct.Struct("<QQqqqii")  # rtma_gradient
+
 ROW_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 SCOPES = {"row": 0, "part": 1}
 ACTIVATIONS = {"none": 0, "relu": 1, "prelu": 2, "silu": 3}
@@ -98,6 +108,10 @@ def load_library(checked: bool = False):
         norm = [vp, ctypes.POINTER(NormDesc), i64, i32, vp, vp, i64]
         lib.rtma_group_norm.argtypes = norm + [vp, vp, vp, vp, vp, i64, vp, vp]
         lib.rtma_group_norm_grad.argtypes = norm + [vp, i64, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+        layer = [vp, ctypes.POINTER(LayerDesc), i64, i32, vp, vp, i64, vp, vp, vp]
+        lib.rtma_grouped_layer.argtypes = layer + [vp, i64, vp, i64, vp]
+        lib.rtma_grouped_layer_grad.argtypes = layer + [vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+        lib.rtma_clip_gradients.argtypes = [vp, i32, ctypes.c_char_p, i32, i32, ctypes.c_double, i32, vp, vp]
         lib.rtma_dropout.argtypes = [vp, i32, i64, i32, vp, i64, vp, vp, i64, ctypes.c_double, u64, vp, i64, vp]
         _libs[path] = lib
     return _libs[path]
@@ -650,6 +664,161 @@ class Context:
         self._check(self._lib.rtma_dropout(self._h, ROW_TYPES[X.dtype], n, d, x, ldx, ids, r, ldr, float(p), int(seed) & (2**64 - 1), y, ldy,
                                            self._stream(stream)), "rtma_dropout")
         return out
+
+    # ---- whole layers and their step ---------------------------------------------------
+    def _layer(self, X, offsets, W, bias, act, slope, gated, grad_dtype):
+        if act not in ACTIVATIONS:
+            raise ValueError(f"act={act!r} (of {list(ACTIVATIONS)})")
+        x, ldx = self._rows(X, "X")
+        off, G = self._parts(offsets)
+        n, d_in = X.shape
+        wide = W.shape[-1]
+        if gated and wide % 2:
+            raise ValueError(f"W has {wide} columns: a gated layer's are two matrices of equal width")
+        if wide > MAX_INT32:
+            raise ValueError(f"W has rows of {wide} values")
+        w, ws = self._of_parts(W, "W", X.dtype, G, (d_in, wide))
+        b, bs = self._of_parts(bias, "bias", X.dtype, G, (wide,))
+        sl, ss = (None, 0) if slope is None else self._slope(slope, "slope", G)
+        d_out = wide // 2 if gated else wide
+        desc = LayerDesc(ROW_TYPES[X.dtype], d_in, d_out, ACTIVATIONS[act], 1 if gated else 0, ROW_TYPES[grad_dtype or X.dtype], ws, bs, ss)
+        return (desc, n, G, off, x, ldx, w, b, sl), d_out
+
+    def _empty(self, shape, dtype, stream):
+        return torch.empty(shape, dtype=dtype, device=self.device) if stream is None else self._new(shape, dtype, stream)
+
+    def _forward(self, X, offsets, W, bias, act, slope, residual, out, stream, gated):
+        args, d_out = self._layer(X, offsets, W, bias, act, slope, gated, None)
+        n = X.shape[0]
+        r, ldr = (None, 0) if residual is None else self._rows(residual, "residual", X.dtype, (n, d_out))
+        if out is None:
+            out = self._empty((n, d_out), X.dtype, stream)
+        y, ldy = self._rows(out, "out", X.dtype, (n, d_out))
+        self._check(self._lib.rtma_grouped_layer(self._h, *args, r, ldr, y, ldy, self._stream(stream)), "rtma_grouped_layer")
+        return out
+
+    def _gradient(self, X, dY, offsets, W, bias, act, slope, need_dx, need_dw, grad_dtype, out, dz, dw, db, dslope, stream, gated):
+        if dw is not None:
+            grad_dtype = dw.dtype
+        elif grad_dtype is None:
+            grad_dtype = X.dtype
+        if grad_dtype not in (X.dtype, torch.float32):
+            raise TypeError(f"gradients of the parameters must be {X.dtype} or {torch.float32}, got {grad_dtype}")
+        args, d_out = self._layer(X, offsets, W, bias, act, slope, gated, grad_dtype)
+        n, d_in = X.shape
+        G, wide = args[2], W.shape[-1]
+        g, ldg = self._rows(dY, "dY", X.dtype, (n, d_out))
+        if dz is None and (gated or act != "none"):
+            dz = self._empty((n, wide), X.dtype, stream)
+        z, ldz = (None, 0) if dz is None else self._rows(dz, "dz", X.dtype, (n, wide))
+        if need_dx and out is None:
+            out = self._empty((n, d_in), X.dtype, stream)
+        x, ldx = (None, 0) if out is None else self._rows(out, "out", X.dtype, (n, d_in))
+        if need_dw and dw is None:
+            dw = self._empty(W.shape, grad_dtype, stream)
+        if need_dw and db is None and bias is not None:
+            db = self._empty(bias.shape, grad_dtype, stream)
+        if dslope is None and act == "prelu" and slope is not None and need_dw:
+            dslope = self._empty(slope.shape, torch.float32, stream)
+        for t, like, name in ((dw, W, "dw"), (db, bias, "db")):
+            if t is not None and like is not None and t.shape != like.shape:
+                raise ValueError(f"{name} must be {list(like.shape)}, got {list(t.shape)}")
+        w, ws = self._of_parts(dw, "dw", grad_dtype, G, (d_in, wide), result=True)
+        b, bs = self._of_parts(db, "db", grad_dtype, G, (wide,), result=True)
+        sl, ss = (None, 0) if dslope is None else self._slope(dslope, "dslope", G, result=True)
+        self._check(self._lib.rtma_grouped_layer_grad(self._h, *args, g, ldg, z, ldz, x, ldx, w, ws, b, bs, sl, ss, self._stream(stream)),
+                    "rtma_grouped_layer_grad")
+        return out, dw, db, dslope
+
+    def grouped_linear_act(self, X, offsets, W, bias=None, act="none", slope=None, residual=None, out=None, stream=None):
+        """Y[r] = residual[r] + act(X[r] W_g + b_g) for the rows r of part g: X [n, d_in], W [G, d_in, d_out] (or [d_in, d_out] for all
+        parts), bias [G, d_out] (or [d_out]), act one of ACTIVATIONS, slope [G] or one value (float32, act "prelu"), residual
+        [n, d_out].  The product is rounded once, behind all of it.  Returns Y [n, d_out], which may be residual (out=residual)."""
+        return self._forward(X, offsets, W, bias, act, slope, residual, out, stream, False)
+
+    def grouped_linear_act_grad(self, X, dY, offsets, W, bias=None, act="none", slope=None, need_dx=True, need_dw=True, grad_dtype=None, out=None,
+                                dz=None, dw=None, db=None, dslope=None, stream=None):
+        """(dX, dW, db, dslope) of grouped_linear_act from its inputs and dY (the residual's gradient is dY itself); what lies in
+        front of the activation is worked out again.  dW and db have the parameters' shape (summed over the parts for shared ones) and
+        grad_dtype: the rows' type, or float32; dslope float32.  None for a parameter that is None, and for what is not wanted
+        (need_dx, need_dw).  dz [n, d_out]: where the gradient in front of the activation is put, rounded to the rows' type, as
+        the operand of the two products (it may be dY; a new one otherwise; act "none" has none)."""
+        return self._gradient(X, dY, offsets, W, bias, act, slope, need_dx, need_dw, grad_dtype, out, dz, dw, db, dslope, stream, False)
+
+    def grouped_gated_linear(self, X, offsets, W, bias=None, act="silu", slope=None, residual=None, out=None, stream=None):
+        """H[r] = residual[r] + act(X[r] V_g + c_g) * (X[r] U_g + d_g): the gated half of a feed-forward block.  W [G, d_in, 2 f] (or
+        [d_in, 2 f]) holds V in its first f columns and U in the others, bias [G, 2 f] likewise; the rest as in grouped_linear_act.
+        Both products stay on the chip; H [n, f] is rounded once."""
+        return self._forward(X, offsets, W, bias, act, slope, residual, out, stream, True)
+
+    def grouped_gated_linear_grad(self, X, dH, offsets, W, bias=None, act="silu", slope=None, need_dx=True, need_dw=True, grad_dtype=None, out=None,
+                                  dz=None, dw=None, db=None, dslope=None, stream=None):
+        """(dX, dW, db, dslope) of grouped_gated_linear from its inputs and dH; both products are worked out again.  dz [n, 2 f]: as in
+        grouped_linear_act_grad, the gradients of both, side by side."""
+        return self._gradient(X, dH, offsets, W, bias, act, slope, need_dx, need_dw, grad_dtype, out, dz, dw, db, dslope, stream, True)
+
+    def _share(self, t, parts, name):
+        """(pointer, values of a part, distance between parts)."""
+        if t.dtype not in ROW_TYPES:
+            raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+        self._here(t, name)
+        size = t.shape
+        if parts > 1 and (not size or size[0] != parts):
+            raise ValueError(f"{name} must be [{parts}, ...], got {list(size)}")
+        values = t.numel()
+        if t.is_contiguous():
+            return t.data_ptr(), values // parts, values // parts
+        if parts > 1 and (values == 0 or t[0].is_contiguous()):
+            return t.data_ptr(), values // parts, t.stride(0)
+        raise ValueError(f"{name} must be contiguous{' within a part' if parts > 1 else ''}")
+
+    def _clip(self, grads, outs, max_norm, parts, zero_nonfinite, stream):
+        parts, one = int(parts), 0
+        if parts < 1 or parts > MAX_GROUPS:
+            raise ValueError(f"parts={parts} outside [1, {MAX_GROUPS}]")
+        shares = parts
+        if parts == 1 and not all(t.is_contiguous() for t in (*grads, *(o for o in outs if o is not None))):
+            # one norm over tensors whose first dimension is a row of its own in something larger
+            lead = {t.shape[0] if t.dim() else 1 for t in grads}
+            if len(lead) == 1 and 0 < next(iter(lead)) <= MAX_GROUPS:
+                shares, one = lead.pop(), 1
+        table = bytearray(GRADIENT.size * len(grads))
+        for i, (t, o) in enumerate(zip(grads, outs)):
+            p, size, between = self._share(t, shares, f"gradient {i}")
+            kind = ROW_TYPES[t.dtype]
+            if o is None:
+                q, apart, out_kind = 0, 0, kind
+            elif o is t:
+                q, apart, out_kind = p, between, kind
+            else:
+                if o.shape != t.shape or o.dtype not in (t.dtype, torch.float32):
+                    raise ValueError(f"result {i} must be {list(t.shape)}, {t.dtype} or {torch.float32}, got {list(o.shape)}, {o.dtype}")
+                q, _, apart = self._share(o, shares, f"result {i}")
+                out_kind = ROW_TYPES[o.dtype]
+            if o is not None and shares > 1 and apart == 0 and size:
+                raise RtmaError(f"result {i} must have memory of its own for every part, got an expanded view")
+            GRADIENT.pack_into(table, GRADIENT.size * i, p, q, size, between, apart, kind, out_kind)
+        norms = self._empty((parts,), torch.float32, stream)
+        self._check(self._lib.rtma_clip_gradients(self._h, len(grads), bytes(table), shares, one, float(max_norm), 1 if zero_nonfinite else 0, norms.data_ptr(),
+                                                  self._stream(stream)), "rtma_clip_gradients")
+        return norms
+
+    def clip_gradients(self, grads, max_norm, parts=1, out=None, zero_nonfinite=False, stream=None):
+        """Scales the tensors `grads` down so that their norm, over all of them together, is max_norm at most; returns the norms [parts]
+        float32 from before.  parts = G: every tensor is [G, ...] and every part has a norm and a scale of its own.  Tensors are contiguous,
+        or contiguous within a part.  In place, or into the tensors `out` of the same shapes, of the gradient's type or float32 (for
+        instance views of the grads [M, P] that sgd_aggregate takes); an entry that is None is only part of the norm.  Where a norm is not
+        finite the gradients stay as they are or (zero_nonfinite) become zeros."""
+        grads = list(grads)
+        outs = grads if out is None else list(out)
+        if len(outs) != len(grads):
+            raise ValueError(f"{len(grads)} gradients and {len(outs)} results")
+        return self._clip(grads, outs, max_norm, parts, zero_nonfinite, stream)
+
+    def gradient_norms(self, grads, parts=1, stream=None):
+        """The norms [parts] float32 of clip_gradients alone."""
+        grads = list(grads)
+        return self._clip(grads, [None] * len(grads), math.inf, parts, False, stream)
 
     # ---- R2 -------------------------------------------------------------------------
     def aggregate(self, params, global_out=None, stream=None):

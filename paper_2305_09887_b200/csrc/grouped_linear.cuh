@@ -20,6 +20,7 @@ struct LinearArgs {
     int m_tiles, n_tiles;      // tiles of one row tile: m_tiles (dw) x n_tiles
     int BN;
     int d_in, d_out;
+    int up;                    // two matrices side by side: columns from one to the other
     const void *A, *B;         // rows; matrices (forward, dx) or rows (dw)
     int64_t lda, ldb, w_stride;
     int va, vb;                // granules of the rows (bytes)
@@ -32,7 +33,7 @@ struct LinearArgs {
     int bias_rows;             // dw: partial sums of the bias gradient in a slot, one row per warp that adds them up
     void* out;                 // dw: the slots, [row tile][d_in + bias_rows][ldo]
     int64_t ldo;
-    float *dW, *db;
+    void *dW, *db;             // dw: in float, or in the rows' type
     int64_t dw_stride, db_stride;
     int32_t* chunk_rows;       // dw: where the rows of a row tile are left for the reduction
     int* error_word;
@@ -197,8 +198,8 @@ struct Outlet {
     int at = 0;
     __device__ __forceinline__ static int swizzle(int row) { return (row >> 1) & 3; }
     // row0, c: place in the map; rows, cols: how much is this tile's; whole: all columns of the matrix from c on are, and end on a
-    // 16-byte boundary (a store's box is cut off at the edge of the matrix only in steps of 16 bytes)
-    __device__ __forceinline__ void put(const LinearArgs& a, const float (&v)[32], int64_t row0, int c, int rows, int cols, bool whole, O* out, int64_t ldo, int lane) {
+    // 16-byte boundary (a store's box is cut off at the edge of the matrix only in steps of 16 bytes); aligned: column c lies on one
+    __device__ __forceinline__ void put(const LinearArgs& a, const float (&v)[32], int64_t row0, int c, int rows, int cols, bool whole, O* out, int64_t ldo, int lane, bool aligned = true) {
         constexpr int WIDE = ROW / sizeof(O), PIECE = 16 / sizeof(O);
 #pragma unroll
         for (int c0 = 0; c0 < 32; c0 += WIDE) {
@@ -218,7 +219,7 @@ struct Outlet {
                 }
                 store_16(slab + lane * ROW + ((q ^ swizzle(lane)) << 4), x);
             }
-            const bool bulk = a.vo && rows == 32 && (cols - c0 >= WIDE || whole);
+            const bool bulk = a.vo && aligned && rows == 32 && (cols - c0 >= WIDE || whole);
             if (bulk) tc::fence_proxy_async_smem();
             __syncwarp();
             if (bulk) {
@@ -298,3 +299,12 @@ struct BiasHolder {
 constexpr int SPLIT_COLUMNS = 128, SPLIT_DW_COLUMNS = 64, SPLIT_BIAS_ROWS = 8, SPLIT_BLOCKS_PER_SM = 2;
 size_t split_planes_bytes(const grouped::LinearArgs& a);
 int32_t launch_split(rtma_ctx* ctx, int mode, grouped::LinearArgs& a, void* planes, int cls, cudaStream_t stream);
+
+// Products with the matrices of the parts, and the gradient of these, for calls that are made of several (grouped_linear.cu).  scratch:
+// only says how much the call would take.  The gradients come in out_dtype.
+int32_t grouped_rows(rtma_ctx* ctx, const char* who, bool transposed, int32_t dtype, int64_t n, int32_t G, const int64_t* offsets, int32_t d_in, int32_t d_out,
+                     const void* A, int64_t lda, const void* W, int64_t w_stride, const void* b, int64_t b_stride, void* out, int64_t ldo, size_t* scratch,
+                     cudaStream_t stream);
+int32_t grouped_dw(rtma_ctx* ctx, const char* who, int32_t dtype, int64_t n, int32_t G, const int64_t* offsets, int32_t d_in, int32_t d_out, const void* X,
+                   int64_t ldx, const void* dY, int64_t lddy, int32_t out_dtype, void* dW, int64_t dw_stride, void* db, int64_t db_stride, size_t* scratch,
+                   cudaStream_t stream);

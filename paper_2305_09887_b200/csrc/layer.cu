@@ -1,0 +1,416 @@
+// Layers over the rows of many parts, on the tensor cores:
+//   Y[r] = R[r] + act(X[r] W_g + b_g)                          gated: H[r] = R[r] + act(X[r] V_g + c_g) * (X[r] U_g + d_g)
+// for the rows r of part g, W_g = [V_g | U_g] in a gated layer, and the first step of their gradients,
+//   dZ[r] = dY[r] act'(Z[r])                                   gated: dZ[r] = [dH u act'(v) | dH act(v)]
+// with Z = X W + b worked out again from the inputs: kept from the forward pass it would cost a write there and a read here, which is
+// more than the product as long as the contraction has fewer terms than about 600 (16-bit rows).  dX = dZ W^T and dW = X^T dZ are then the
+// grouped products of grouped_linear.cu.
+//
+// One kernel body (grouped_rows.cuh) for all four: the product stays in tensor memory and goes through the layer in the registers of
+// the warps that drain it.  A tile of a gated layer has the same columns of both matrices, so that a lane finds both factors of a result in its own
+// row.  dZ is rounded to the rows' type: it is an operand of 16-bit products.
+//
+// This file: 16-bit rows, and the calls.  fp32 rows are in layer_split.cu.
+#include <algorithm>
+
+#include "grouped_rows.cuh"
+#include "layer.cuh"
+
+RTMA_BOUNDS_TU()
+
+namespace {
+
+using namespace grouped;
+
+// 32 values of a lane's row as they are stored; those that do not exist read as zero.
+template <class T>
+struct Side {
+    Eight<T> e[4];
+    __device__ __forceinline__ void load(const T* p, int valid, int granule) {
+        if (valid >= 32 && granule == 32) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                uint4 &x = e[2 * i].w[0], &y = e[2 * i + 1].w[0];
+                asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                             : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w), "=r"(y.x), "=r"(y.y), "=r"(y.z), "=r"(y.w)
+                             : "l"(p + 16 * i));
+            }
+        } else if (granule >= 16 && valid % 8 == 0) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                e[i].w[0] = make_uint4(0u, 0u, 0u, 0u);
+                if (8 * i < valid) asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(e[i].w[0].x), "=r"(e[i].w[0].y), "=r"(e[i].w[0].z), "=r"(e[i].w[0].w) : "l"(p + 8 * i));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e[i].load(p + 8 * i, max(0, min(8, valid - 8 * i)), granule);
+        }
+    }
+};
+
+// What a drain warp does with its rows (a quarter of the tile's) and every second 32 columns of a tile.
+template <class F, bool GRADIENT>
+__device__ __forceinline__ void drain_layer(const LayerArgs& a, Shared& sh, uint32_t slabs) {
+    typedef typename F::T T;
+    constexpr bool GATED = F::GATED;
+    constexpr bool AHEAD = F::LOADING != COPIES;  // the next columns' rows are requested before these are worked on (with fewer registers they are not)
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, half = warp >> 2;
+    Outlet<T, F::OUT_SLABS> outlet{slabs + warp * F::OUT_BYTES};
+    LayerBias bias{sh.bias + 128 * warp};
+    const uint32_t tmem = sh.tmem_base + ((uint32_t)(32 * quarter) << 16);
+    const int chunks = (a.BN + 31) / 32, mine = (chunks - half + 1) / 2;
+    int slope_part = -1;
+    float slope = 0.f;
+    typename F::Walks w;
+    tc::RingAt acc;
+    for (bool more = w.first(a, sh); more; more = w.next_tile(a, sh)) {
+        const int rows = min(32, w.rows - 32 * quarter);
+        const int64_t row0 = w.row0 + 32 * quarter;
+        auto column = [&](int chunk) { return w.n0 + 32 * chunk; };
+        auto columns = [&](int chunk) { return min(min(32, a.BN - 32 * chunk), a.width - column(chunk)); };
+        if (a.bias) {
+            if constexpr (GATED)
+                bias.fetch(a, w.part, w.n0, 2 * mine, lane, static_cast<const T*>(nullptr),
+                           [&](int i) { return column(half + (i & ~1)) + (i & 1 ? a.width : 0); }, [&](int i) { return columns(half + (i & ~1)); });
+            else
+                bias.fetch(a, w.part, w.n0, mine, lane, static_cast<const T*>(nullptr), [&](int i) { return column(half + 2 * i); }, [&](int i) { return columns(half + 2 * i); });
+        }
+        if (a.slope && w.part != slope_part) {
+            slope_part = w.part;
+            slope = __ldg(a.slope + w.part * a.slope_stride);
+        }
+        const T* const from = static_cast<const T*>(a.side) + (row0 + lane) * a.lds;
+        Side<T> side, next;
+        auto request = [&](int chunk, Side<T>& to) {
+            if ((GRADIENT || a.side) && chunk < chunks) to.load(from + column(chunk), lane < rows ? max(0, columns(chunk)) : 0, a.gs);
+        };
+        if (AHEAD) request(half, next);
+        float slope_sum = 0.f;
+        if (!wait_for<F::PAIRED>(&sh.acc_full[acc.s], acc.phase, sh, a.error_word)) return;
+        __syncwarp();
+        tc::tc_fence_after_sync();
+        for (int chunk = half, i = 0; chunk < chunks; chunk += 2, ++i) {
+            if (AHEAD) {
+                side = next;
+                request(chunk + 2, next);
+            } else {
+                request(chunk, side);
+            }
+            float v[32], u[GATED ? 32 : 1];
+            if constexpr (GATED) {
+                uint32_t x[32], y[32];
+                tc::tmem_load_issue(tmem + acc.s * F::ACC_COLUMNS + 32 * chunk, x);
+                tc::tmem_load_issue(tmem + acc.s * F::ACC_COLUMNS + 128 + 32 * chunk, y);
+                tc::tmem_load_wait(x);
+                tc::tmem_load_wait(y);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    v[j] = __uint_as_float(x[j]);
+                    u[j] = __uint_as_float(y[j]);
+                }
+            } else {
+                tc::tmem_load_32x32(tmem + acc.s * F::ACC_COLUMNS + 32 * chunk, v);
+            }
+            const int cols = columns(chunk);
+            float ds = 0.f;
+            auto eight = [&](auto Q) {
+                constexpr int q = decltype(Q)::value;
+                f2 z[4], d[4];
+                eight_of<q>(v, z);
+                if (a.bias) bias.add(z, GATED ? 2 * i : i, q);
+                if (GRADIENT && a.slope_slots) cut_eight(z, cols - 8 * q);
+                if (GRADIENT || a.side) pairs_of(side.e[q], d);
+                if constexpr (GATED) {
+                    f2 y[4];
+                    eight_of<q>(u, y);
+                    if (a.bias) bias.add(y, 2 * i + 1, q);
+                    if (GRADIENT && a.slope_slots) cut_eight(y, cols - 8 * q);
+                    if constexpr (GRADIENT) {
+                        f2 dv[4], du[4];
+                        ds += gate_back(a.act, slope, z, y, d, dv, du);
+                        eight_to<q>(dv, v);
+                        eight_to<q>(du, u);
+                    } else {
+                        activate(a.act, slope, z);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) z[j] = a.side ? fma2(z[j], y[j], d[j]) : mul2(z[j], y[j]);
+                        eight_to<q>(z, v);
+                    }
+                } else if constexpr (GRADIENT) {
+                    ds += activate_back(a.act, slope, z, d);
+                    eight_to<q>(d, v);
+                } else {
+                    activate(a.act, slope, z);
+                    if (a.side) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) z[j] = add2(z[j], d[j]);
+                    }
+                    eight_to<q>(z, v);
+                }
+            };
+            eight(std::integral_constant<int, 0>());
+            eight(std::integral_constant<int, 1>());
+            eight(std::integral_constant<int, 2>());
+            eight(std::integral_constant<int, 3>());
+            if (lane < rows) slope_sum += ds;  // (what the accumulator has for rows that are not there may be anything)
+            const int c = column(chunk);
+            if (rows > 0 && cols > 0) {
+                constexpr int PIECE = 16 / (int)sizeof(T);
+                T* const out = static_cast<T*>(a.out) + row0 * a.ldo + c;
+                if constexpr (GATED && GRADIENT) {
+                    outlet.put(a, v, row0, c, rows, cols, false, out, a.ldo, lane);
+                    outlet.put(a, u, row0, a.width + c, rows, cols, c + cols == a.width && a.width % PIECE == 0, out + a.width, a.ldo, lane, a.width % PIECE == 0);
+                } else {
+                    outlet.put(a, v, row0, c, rows, cols, c + cols == a.width && a.width % PIECE == 0, out, a.ldo, lane);
+                }
+            }
+        }
+        tc::tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) {  // (a pair's warps all report to the first block)
+            if constexpr (F::PAIRED) tc::mbar_arrive_remote(tc::leader_addr(&sh.acc_empty[acc.s]));
+            else tc::mbar_arrive(&sh.acc_empty[acc.s]);
+        }
+        acc.advance(2);
+        if (GRADIENT && a.slope_slots) {
+            for (int o = 16; o > 0; o >>= 1) slope_sum += __shfl_xor_sync(0xffffffffu, slope_sum, o);
+            const int64_t tile = F::PAIRED ? 2 * (int64_t)w.tile + (blockIdx.x & 1) : w.tile;
+            if (lane == 0) a.slope_slots[tile * a.slope_warps + warp] = slope_sum;
+        }
+    }
+    outlet.finish(lane);
+}
+
+template <class T, int LOADING, bool GATED, bool GRADIENT>
+__global__ void __launch_bounds__(Form<T, FORWARD, LOADING, GATED>::THREADS, 1) layer_kernel(const __grid_constant__ LayerArgs a) {
+    typedef Form<T, FORWARD, LOADING, GATED> F;
+    __shared__ Shared sh;
+    linear_body<F>(a, sh, [&](uint32_t slabs) { drain_layer<F, GRADIENT>(a, sh, slabs); });
+}
+template <class T, bool GATED, bool GRADIENT>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Form<T, FORWARD, PAIR, GATED>::THREADS, 1) layer_pair_kernel(const __grid_constant__ LayerArgs a) {
+    typedef Form<T, FORWARD, PAIR, GATED> F;
+    __shared__ Shared sh;
+    linear_body<F>(a, sh, [&](uint32_t slabs) { drain_layer<F, GRADIENT>(a, sh, slabs); });
+}
+
+// 16-bit matrices -> [part][d_in][halves * up] on 16-byte boundaries, up: width rounded up to 8
+__global__ void __launch_bounds__(256) lay_out_matrices_kernel(const __half* __restrict__ W, int64_t w_stride, int parts, int d_in, int width, int halves, int granule,
+                                                               __half* __restrict__ out) {
+    wait_for_kernel_before();
+    const int units = (width + 7) / 8;
+    const int64_t total = (int64_t)parts * d_in * halves * units;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t run = i / units, row = run / halves, part = row / d_in;  // run: a row of one matrix
+        const int u = (int)(i - run * units), h = (int)(run - row * halves);
+        Eight<__half> x;
+        x.load(W + part * w_stride + ((row - part * d_in) * halves + h) * width + 8 * u, min(8, width - 8 * u), granule);
+        *reinterpret_cast<uint4*>(out + 8 * i) = x.w[0];
+    }
+}
+
+// What the warps of all tiles have of the slopes' gradients, added up in order; one block for every part, or one for all (shared).
+__global__ void __launch_bounds__(256) slope_reduce_kernel(const int64_t* offsets, int64_t n, int G, int64_t tile_rows, int64_t tiles, int64_t per_tile,
+                                                           const float* __restrict__ slots, bool shared, float* dslope, int64_t stride) {
+    __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
+    __shared__ double red[8];
+    wait_for_kernel_before();
+    number_tiles(offsets, n, G, tile_rows, tiles, tile_start, warp_sums);
+    const int part = blockIdx.x;
+    const int64_t from = shared ? 0 : tile_start[part] * per_tile, to = tile_start[shared ? G : part + 1] * per_tile;
+    double s = 0.0;
+#pragma unroll 4
+    for (int64_t i = from + threadIdx.x; i < to; i += 256) s += slots[i];
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int k = 1; k < 8; ++k) s += red[k];
+        dslope[part * stride] = (float)s;
+    }
+}
+
+template <class T, int LOADING, bool GATED, bool GRADIENT>
+int32_t launch_form(rtma_ctx* ctx, const LayerArgs& a, unsigned grid, bool& configured, cudaStream_t stream) {
+    typedef Form<T, FORWARD, LOADING, GATED> F;
+    void (*kernel)(LayerArgs);
+    if constexpr (LOADING == PAIR) kernel = layer_pair_kernel<T, GATED, GRADIENT>;
+    else kernel = layer_kernel<T, LOADING, GATED, GRADIENT>;
+    if (!configured) {
+        RTMA_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, F::DYNAMIC_BYTES));
+        configured = true;
+    }
+    launch_kernel(kernel, grid, F::THREADS, F::DYNAMIC_BYTES, stream, a);
+    RTMA_LAUNCH_CHECK(ctx);
+    return RTMA_OK;
+}
+
+template <class T, int LOADING>
+int32_t launch_kind(rtma_ctx* ctx, const LayerArgs& a, bool gated, bool gradient, unsigned grid, cudaStream_t stream) {
+    bool* once = ctx->layer_configured + ((std::is_same<T, __half>::value ? 1 : 0) * 3 + LOADING) * 4;
+    if (gated) return gradient ? launch_form<T, LOADING, true, true>(ctx, a, grid, once[3], stream) : launch_form<T, LOADING, true, false>(ctx, a, grid, once[2], stream);
+    return gradient ? launch_form<T, LOADING, false, true>(ctx, a, grid, once[1], stream) : launch_form<T, LOADING, false, false>(ctx, a, grid, once[0], stream);
+}
+
+// The layer's kernel on 16-bit rows.  room: scratch for the laid-out matrices.
+int32_t launch_layer(rtma_ctx* ctx, LayerArgs& a, bool bf16, bool gated, bool gradient, char* room, int cls, cudaStream_t stream) {
+    const int halves = gated ? 2 : 1;
+    if (room) {
+        const int parts = a.w_stride ? a.G : 1;
+        const int64_t blocks = ceil_div((int64_t)parts * a.d_in * halves * ceil_div(a.width, 8), 256);
+        KernelScope ks(ctx, KC_WEIGHT_PREP, stream);
+        launch_kernel(lay_out_matrices_kernel, (unsigned)std::min<int64_t>(blocks, 16 * ctx->sm_count), 256, 0, stream, static_cast<const __half*>(a.B), a.w_stride, parts,
+                      a.d_in, a.width, halves, std::min(a.vb, row_granule(nullptr, a.width, 2)), reinterpret_cast<__half*>(room));
+        RTMA_LAUNCH_CHECK(ctx);
+        a.B = room;
+        a.up = (int)ceil_div(a.width, 8) * 8;
+        a.ldb = halves * a.up;
+        a.w_stride = a.w_stride ? a.d_in * a.ldb : 0;
+        a.vb = 16;
+    }
+    const int64_t tiles = a.tiles * a.n_tiles;
+    if (tiles >= (int64_t(1) << 30)) return rtma_fail(ctx, RTMA_ERR_OVERFLOW, "grouped layer: %lld tiles", (long long)tiles);
+    a.in_bulk = 2;
+    if (!make_tensor_map_16bit(&a.map_b, bf16, a.B, a.w_stride ? a.G : 1, a.d_in, gated ? a.up + a.width : a.width, a.ldb, a.w_stride ? a.w_stride : a.d_in * a.ldb, BK))
+        return rtma_fail(ctx, RTMA_ERR_CUDA, "grouped layer: no tensor map for %d matrices of %d x %d", a.w_stride ? a.G : 1, a.d_in, a.width);
+    if (a.va >= 16 && make_tensor_map_16bit(&a.map_a, bf16, a.A, 1, a.n, a.d_in, a.lda, a.n * a.lda, BM)) a.in_bulk |= 1;
+    KernelScope ks(ctx, cls, stream);
+    // pairs of blocks by the rule of the plain products: deep contractions, whole tiles
+    if (a.in_bulk == 3 && a.BN == (gated ? 128 : 256) && a.d_in >= 256 && tiles >= ctx->sm_count) {
+        a.tile_rows = 2 * BM;
+        a.tiles = a.n / a.tile_rows + a.G;
+        const unsigned grid = (unsigned)std::min<int64_t>(2 * a.tiles * a.n_tiles, ctx->sm_count & ~1);
+        return bf16 ? launch_kind<__nv_bfloat16, PAIR>(ctx, a, gated, gradient, grid, stream) : launch_kind<__half, PAIR>(ctx, a, gated, gradient, grid, stream);
+    }
+    const unsigned grid = (unsigned)std::min<int64_t>(tiles, ctx->sm_count);
+    if (a.in_bulk == 3)
+        return bf16 ? launch_kind<__nv_bfloat16, BULK>(ctx, a, gated, gradient, grid, stream) : launch_kind<__half, BULK>(ctx, a, gated, gradient, grid, stream);
+    return bf16 ? launch_kind<__nv_bfloat16, COPIES>(ctx, a, gated, gradient, grid, stream) : launch_kind<__half, COPIES>(ctx, a, gated, gradient, grid, stream);
+}
+
+int32_t check_layer(rtma_ctx* ctx, const char* who, const rtma_layer_desc* d, int64_t n, int32_t G, const int64_t* offsets, const float* slope) {
+    if (!d) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: null description", who);
+    RTMA_TRY(check_parts(ctx, who, n, G, offsets));
+    if (d->dtype < RTMA_F32 || d->dtype > RTMA_F16) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: dtype=%d", who, d->dtype);
+    if (d->act < RTMA_ACT_NONE || d->act > RTMA_ACT_SILU) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: act=%d", who, d->act);
+    if (d->act == RTMA_ACT_PRELU && !slope) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: PReLU without a slope", who);
+    const int64_t wide = d->gated ? 2 * (int64_t)d->d_out : d->d_out;
+    if (d->d_in < 1 || d->d_out < 1 || d->d_in > RTMA_MAX_WIDTH || wide > RTMA_MAX_WIDTH)
+        return rtma_fail(ctx, RTMA_ERR_UNSUPPORTED, "%s: %d x %lld outside [1,%d]", who, d->d_in, (long long)wide, RTMA_MAX_WIDTH);
+    return RTMA_OK;
+}
+
+// The arguments of the layer's kernel and the scratch that it takes (lay: the matrices have to be laid out).
+void describe(rtma_ctx* ctx, LayerArgs& a, const rtma_layer_desc* d, int64_t n, int32_t G, const int64_t* offsets, const void* X, int64_t ldx, const void* W, const void* b,
+              const float* slope, size_t* bytes) {
+    const size_t es = row_type_bytes(d->dtype);
+    const int wide = d->gated ? 2 * d->d_out : d->d_out;
+    a.error_word = ctx->error_word;
+    a.offsets = offsets; a.n = n; a.G = G; a.span = 1;
+    a.tile_rows = BM;
+    a.tiles = n / BM + G;
+    a.m_tiles = 1;
+    a.d_in = d->d_in; a.d_out = a.width = a.up = d->d_out;
+    a.A = X; a.lda = ldx; a.B = W; a.ldb = wide; a.w_stride = d->w_stride;
+    a.bias = b; a.bias_stride = d->b_stride;
+    a.va = row_granule(X, ldx, es);
+    a.vb = std::min(row_granule(W, wide, es), row_granule(nullptr, d->w_stride, es));
+    a.act = d->act;
+    a.slope = d->act == RTMA_ACT_PRELU ? slope : nullptr; a.slope_stride = d->slope_stride;
+    a.slope_warps = 8;
+    if (d->dtype == RTMA_F32) {
+        describe_layer_split(a, d->gated != 0);
+        *bytes = layer_split_bytes(a, d->gated != 0);
+        return;
+    }
+    const int widest = d->gated ? 128 : 256;
+    a.n_tiles = (int)ceil_div(a.width, widest);
+    a.BN = (int)ceil_div(ceil_div(a.width, a.n_tiles), 16) * 16;
+    a.n_tiles = (int)ceil_div(a.width, a.BN);
+    const bool lay = a.vb < 16 || a.w_stride < 0 || (d->gated && a.width % 8);
+    *bytes = lay ? (size_t)2 * (a.w_stride ? G : 1) * a.d_in * (d->gated ? 2 : 1) * ceil_div(a.width, 8) * 8 : 0;
+}
+
+}  // namespace
+
+extern "C" int32_t rtma_grouped_layer(rtma_ctx* ctx, const rtma_layer_desc* d, int64_t n, int32_t G, const int64_t* offsets, const void* X, int64_t ldx, const void* W,
+                                      const void* b, const float* slope, const void* residual, int64_t ldr, void* Y, int64_t ldy, void* stream_) {
+    const char* who = "rtma_grouped_layer";
+    if (!ctx) return RTMA_ERR_INVALID_ARG;
+    RTMA_TRY(check_layer(ctx, who, d, n, G, offsets, slope));
+    if (n == 0) return RTMA_OK;
+    if (!X || !W || !Y) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: null pointer", who);
+    if (ldx < d->d_in || ldy < d->d_out || (residual && ldr < d->d_out))
+        return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: rows of %d and %d values lie closer than that", who, d->d_in, d->d_out);
+    if (X == Y) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: the result must not overlap the rows", who);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    DeviceScope on(ctx->device);
+    RTMA_CUDA(ctx, on.status);
+    const size_t es = row_type_bytes(d->dtype);
+    LayerArgs a{};
+    size_t bytes = 0;
+    describe(ctx, a, d, n, G, offsets, X, ldx, W, b, slope, &bytes);
+    a.side = residual; a.lds = ldr; a.gs = residual ? row_granule(residual, ldr, es) : 0;
+    a.out = Y; a.ldo = ldy;
+    a.go = row_granule(Y, ldy, es);
+    a.vo = d->dtype != RTMA_F32 && a.go >= 16 && make_store_map(&a.map_o, d->dtype, Y, n, d->d_out, ldy);
+    RTMA_TRY(prepare_row_call(ctx, bytes, stream));
+    if (d->dtype == RTMA_F32) return launch_layer_split(ctx, a, d->gated != 0, false, ctx->arena, KC_GEMM_FWD, stream);
+    return launch_layer(ctx, a, d->dtype == RTMA_BF16, d->gated != 0, false, bytes ? ctx->arena : nullptr, KC_GEMM_FWD, stream);
+}
+
+extern "C" int32_t rtma_grouped_layer_grad(rtma_ctx* ctx, const rtma_layer_desc* d, int64_t n, int32_t G, const int64_t* offsets, const void* X, int64_t ldx, const void* W,
+                                           const void* b, const float* slope, const void* dY, int64_t lddy, void* dZ, int64_t lddz, void* dX, int64_t lddx, void* dW,
+                                           int64_t dw_stride, void* db, int64_t db_stride, float* dslope, int64_t dslope_stride, void* stream_) {
+    const char* who = "rtma_grouped_layer_grad";
+    if (!ctx) return RTMA_ERR_INVALID_ARG;
+    RTMA_TRY(check_layer(ctx, who, d, n, G, offsets, slope));
+    const bool gated = d->gated != 0, plain = !gated && d->act == RTMA_ACT_NONE;  // plain: dZ is dY
+    const int wide = gated ? 2 * d->d_out : d->d_out;
+    if (n > 0 && (!X || !W || !dY || (!plain && !dZ))) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: null pointer", who);
+    if (db && !dW) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: the bias gradient comes with the weights'", who);
+    if (dslope && d->act != RTMA_ACT_PRELU) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: a slope's gradient without PReLU", who);
+    if (d->grad_dtype != d->dtype && d->grad_dtype != RTMA_F32) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: gradients of the parameters in type %d", who, d->grad_dtype);
+    if (ldx < d->d_in || lddy < d->d_out || (!plain && lddz < wide) || (dX && lddx < d->d_in))
+        return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: rows of %d and %d values lie closer than that", who, d->d_in, wide);
+    if (!plain && n > 0 && (dZ == X || (dZ == dY && (gated || lddz != lddy)) || dZ == dX))
+        return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: dZ must not overlap other rows", who);
+    if (n > 0 && dX && (dX == X || (dX == dY && plain))) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: dX must not overlap rows that are still read", who);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    DeviceScope on(ctx->device);
+    RTMA_CUDA(ctx, on.status);
+    const size_t es = row_type_bytes(d->dtype);
+    const void* dz = plain ? dY : dZ;
+    const int64_t ldz = plain ? lddy : lddz;
+    LayerArgs a{};
+    size_t matrices = 0, slots = 0, rows_bytes = 0, dw_bytes = 0;
+    describe(ctx, a, d, n, G, offsets, X, ldx, W, b, slope, &matrices);
+    matrices = ArenaCursor::granule(matrices);
+    if (dslope) slots = sizeof(float) * (size_t)(a.tiles * a.n_tiles + 2 * (int64_t)G * a.n_tiles) * 8;
+    // all scratch at once: inside a capture nothing is enqueued unless everything fits
+    if (dX) RTMA_TRY(grouped_rows(ctx, who, true, d->dtype, n, G, offsets, d->d_in, wide, dz, ldz, W, d->w_stride, nullptr, 0, dX, lddx, &rows_bytes, stream));
+    if (dW)
+        RTMA_TRY(grouped_dw(ctx, who, d->dtype, n, G, offsets, d->d_in, wide, X, ldx, dz, ldz, d->grad_dtype, dW, dw_stride, db, db_stride, &dw_bytes, stream));
+    RTMA_TRY(prepare_row_call(ctx, std::max(plain ? 0 : matrices + slots, std::max(rows_bytes, dw_bytes)), stream));
+    if (!plain && n > 0) {
+        a.side = dY; a.lds = lddy; a.gs = row_granule(dY, lddy, es);
+        a.out = dZ; a.ldo = lddz;
+        a.go = row_granule(dZ, lddz, es);
+        a.g2 = std::min(a.go, row_granule(nullptr, d->d_out, es));
+        a.vo = d->dtype != RTMA_F32 && a.go >= 16 && make_store_map(&a.map_o, d->dtype, dZ, n, wide, lddz);
+        a.slope_slots = dslope ? reinterpret_cast<float*>(ctx->arena + matrices) : nullptr;
+        if (d->dtype == RTMA_F32) RTMA_TRY(launch_layer_split(ctx, a, gated, true, ctx->arena, KC_GEMM_FWD, stream));
+        else RTMA_TRY(launch_layer(ctx, a, d->dtype == RTMA_BF16, gated, true, matrices ? ctx->arena : nullptr, KC_GEMM_FWD, stream));
+    }
+    if (dslope) {
+        const bool shared = G > 1 && dslope_stride == 0;
+        const int64_t per_tile = (int64_t)a.n_tiles * a.slope_warps * (a.tile_rows / BM);
+        KernelScope ks(ctx, KC_REDUCE_SGD, stream);
+        launch_kernel(slope_reduce_kernel, shared ? 1u : (unsigned)G, 256, 0, stream, offsets, n, G, a.tile_rows, a.tiles, per_tile,
+                      const_cast<const float*>(a.slope_slots), shared, dslope, dslope_stride);
+        RTMA_LAUNCH_CHECK(ctx);
+    }
+    if (dX) RTMA_TRY(grouped_rows(ctx, who, true, d->dtype, n, G, offsets, d->d_in, wide, dz, ldz, W, d->w_stride, nullptr, 0, dX, lddx, nullptr, stream));
+    if (dW) RTMA_TRY(grouped_dw(ctx, who, d->dtype, n, G, offsets, d->d_in, wide, X, ldx, dz, ldz, d->grad_dtype, dW, dw_stride, db, db_stride, nullptr, stream));
+    return RTMA_OK;
+}
