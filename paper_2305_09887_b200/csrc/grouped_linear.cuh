@@ -193,67 +193,81 @@ __device__ __forceinline__ void add_eight(float (&sums)[8], const float (&v)[8])
 // not this tile's, and rows off the 16-byte boundaries, are written by the lanes.
 template <class O, int SLABS>
 struct Outlet {
-    static constexpr int ROW = 64;
+    static constexpr int ROW = 64, WIDE = ROW / (int)sizeof(O), PIECE = 16 / (int)sizeof(O);
     uint32_t slabs;
     int at = 0;
     __device__ __forceinline__ static int swizzle(int row) { return (row >> 1) & 3; }
-    // row0, c: place in the map; rows, cols: how much is this tile's; whole: all columns of the matrix from c on are, and end on a
-    // 16-byte boundary (a store's box is cut off at the edge of the matrix only in steps of 16 bytes); aligned: column c lies on one
-    __device__ __forceinline__ void put(const LinearArgs& a, const float (&v)[32], int64_t row0, int c, int rows, int cols, bool whole, O* out, int64_t ldo, int lane, bool aligned = true) {
-        constexpr int WIDE = ROW / sizeof(O), PIECE = 16 / sizeof(O);
+    // The next slab, once its last store has read it.
+    __device__ __forceinline__ uint32_t open(int lane) const {
+        if (lane == 0) tc::tma_store_wait_read_but<SLABS - 1>();
+        __syncwarp();
+        return slabs + at * 32 * ROW;
+    }
+    // The one after it, which is closed after it.
+    __device__ __forceinline__ uint32_t open_second(int lane) const {
+        if (lane == 0) tc::tma_store_wait_read_but<SLABS - 2>();
+        __syncwarp();
+        return slabs + (at + 1 == SLABS ? 0 : at + 1) * 32 * ROW;
+    }
+    // Piece q (16 bytes) of this lane's row; pack_piece: what it holds.
+    __device__ __forceinline__ static void piece(uint32_t slab, int lane, int q, uint4 x) { store_16(slab + lane * ROW + ((q ^ swizzle(lane)) << 4), x); }
+    __device__ __forceinline__ static uint4 pack_piece(const float* v) {
+        if constexpr (sizeof(O) == 4) {
+            return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        } else {
+            const O* tag = nullptr;
+            return make_uint4(narrow2(v[0], v[1], tag), narrow2(v[2], v[3], tag), narrow2(v[4], v[5], tag), narrow2(v[6], v[7], tag));
+        }
+    }
+    // The slab's WIDE columns, of which cols are this tile's, to the matrix.  row0, c: place in the map; whole: all columns of the matrix from
+    // c on are this tile's, and end on a 16-byte boundary (a store's box is cut off at the edge of the matrix only in steps of 16 bytes);
+    // aligned: column c lies on one.  out: the address of (row0, c).
+    __device__ __forceinline__ void close(const LinearArgs& a, uint32_t slab, int64_t row0, int c, int rows, int cols, bool whole, O* out, int64_t ldo, int lane, bool aligned = true) {
+        const bool bulk = a.vo && aligned && rows == 32 && (cols >= WIDE || whole);
+        if (bulk) tc::fence_proxy_async_smem();
+        __syncwarp();
+        if (bulk) {
+            if (lane == 0) {
+                asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
+                             ::"l"(reinterpret_cast<uint64_t>(&a.map_o)), "r"(slab), "r"(c), "r"((int32_t)row0)
+                             : "memory");
+            }
+        } else {
+            // single values, eight rows (16 in fp32) under way: one at a time, this took longer than all else
+            const int x = lane % WIDE;
+            constexpr int TOGETHER = 8;
+            for (int r0 = lane / WIDE; r0 < rows; r0 += TOGETHER * (32 / WIDE)) {
+                O y[TOGETHER];
+#pragma unroll
+                for (int i = 0; i < TOGETHER; ++i) {
+                    const int r = r0 + i * (32 / WIDE);
+                    const uint32_t from = slab + r * ROW + (((x / PIECE) ^ swizzle(r)) << 4) + (x % PIECE) * (int)sizeof(O);
+                    if constexpr (sizeof(O) == 4) {
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(y[i]) : "r"(from) : "memory");
+                    } else {
+                        unsigned short bits;
+                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(bits) : "r"(from) : "memory");
+                        y[i] = *reinterpret_cast<O*>(&bits);
+                    }
+                }
+                O* to = out + r0 * ldo + x;
+#pragma unroll
+                for (int i = 0; i < TOGETHER; ++i, to += (32 / WIDE) * ldo)
+                    if (r0 + i * (32 / WIDE) < rows && x < cols) *to = y[i];
+            }
+        }
+        if (lane == 0) tc::tma_store_commit();  // a group for every slab, empty or not
+        at = at + 1 == SLABS ? 0 : at + 1;
+    }
+    // 32 columns of which cols are this tile's
+    __device__ __forceinline__ void put(const LinearArgs& a, const float (&v)[32], int64_t row0, int c, int rows, int cols, bool whole, O* out, int64_t ldo, int lane) {
 #pragma unroll
         for (int c0 = 0; c0 < 32; c0 += WIDE) {
             if (c0 >= cols) break;
-            const uint32_t slab = slabs + at * 32 * ROW;
-            if (lane == 0) tc::tma_store_wait_read_but<SLABS - 1>();  // the slab's last store has read it
-            __syncwarp();
+            const uint32_t slab = open(lane);
 #pragma unroll
-            for (int q = 0; q < ROW / 16; ++q) {
-                const int e = c0 + q * PIECE;
-                uint4 x;
-                if constexpr (sizeof(O) == 4) {
-                    x = make_uint4(__float_as_uint(v[e]), __float_as_uint(v[e + 1]), __float_as_uint(v[e + 2]), __float_as_uint(v[e + 3]));
-                } else {
-                    const O* tag = nullptr;
-                    x = make_uint4(narrow2(v[e], v[e + 1], tag), narrow2(v[e + 2], v[e + 3], tag), narrow2(v[e + 4], v[e + 5], tag), narrow2(v[e + 6], v[e + 7], tag));
-                }
-                store_16(slab + lane * ROW + ((q ^ swizzle(lane)) << 4), x);
-            }
-            const bool bulk = a.vo && aligned && rows == 32 && (cols - c0 >= WIDE || whole);
-            if (bulk) tc::fence_proxy_async_smem();
-            __syncwarp();
-            if (bulk) {
-                if (lane == 0) {
-                    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
-                                 ::"l"(reinterpret_cast<uint64_t>(&a.map_o)), "r"(slab), "r"(c + c0), "r"((int32_t)row0)
-                                 : "memory");
-                }
-            } else {
-                // single values, eight rows (16 in fp32) under way: one at a time, this took longer than all else
-                const int x = lane % WIDE;
-                constexpr int TOGETHER = 8;
-                for (int r0 = lane / WIDE; r0 < rows; r0 += TOGETHER * (32 / WIDE)) {
-                    O y[TOGETHER];
-#pragma unroll
-                    for (int i = 0; i < TOGETHER; ++i) {
-                        const int r = r0 + i * (32 / WIDE);
-                        const uint32_t from = slab + r * ROW + (((x / PIECE) ^ swizzle(r)) << 4) + (x % PIECE) * (int)sizeof(O);
-                        if constexpr (sizeof(O) == 4) {
-                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(y[i]) : "r"(from) : "memory");
-                        } else {
-                            unsigned short bits;
-                            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(bits) : "r"(from) : "memory");
-                            y[i] = *reinterpret_cast<O*>(&bits);
-                        }
-                    }
-                    O* to = out + r0 * ldo + c0 + x;
-#pragma unroll
-                    for (int i = 0; i < TOGETHER; ++i, to += (32 / WIDE) * ldo)
-                        if (r0 + i * (32 / WIDE) < rows && c0 + x < cols) *to = y[i];
-                }
-            }
-            if (lane == 0) tc::tma_store_commit();  // a group for every slab, empty or not
-            at = at + 1 == SLABS ? 0 : at + 1;
+            for (int q = 0; q < ROW / 16; ++q) piece(slab, lane, q, pack_piece(v + c0 + q * PIECE));
+            close(a, slab, row0, c + c0, rows, cols - c0, whole, out + c0, ldo, lane);
         }
     }
     __device__ __forceinline__ void finish(int lane) const {

@@ -21,7 +21,7 @@ constexpr int BM = 128, BK = 64;
 constexpr int DRAIN_REGISTERS = 104, LOAD_REGISTERS = 64, MULTIPLY_REGISTERS = 40;
 constexpr int SLAB_BYTES = 32 * 128;       // 32 rows of 64 16-bit values
 
-template <class T_, int MODE_, int LOADING_, bool GATED_ = false>
+template <class T_, int MODE_, int LOADING_, bool GATED_ = false, int DRAIN_WARPS_ = 8>
 struct Form {
     typedef T_ T;
     static constexpr int MODE = MODE_, LOADING = LOADING_;
@@ -34,8 +34,8 @@ struct Form {
     // the results of a tile leave while the next is drained, which is worth more than another stage
     static constexpr int RING_BYTES = (MODE == WEIGHT_GRADIENT ? 160 : 144) * 1024;
     static constexpr int STAGES = RING_BYTES / STAGE_BYTES;
-    static constexpr int DRAIN_WARPS = 8;
-    static constexpr int OUT_SLABS = MODE == WEIGHT_GRADIENT ? 2 : 4;                  // of a drain warp: 32 rows of 64 bytes on their way out
+    static constexpr int DRAIN_WARPS = DRAIN_WARPS_;
+    static constexpr int OUT_SLABS = MODE == WEIGHT_GRADIENT ? 2 : 32 / DRAIN_WARPS;   // of a drain warp: 32 rows of 64 bytes on their way out
     static constexpr int OUT_BYTES = OUT_SLABS * 32 * 64;
     static constexpr int ACC_STAGES = MODE == WEIGHT_GRADIENT ? 2 : 1 << 20;           // after so many the accumulator is drained (or at a tile's end)
     static constexpr int ACC_COLUMNS = 256;                                            // dw: 128 of the product, 128 of the column sums
@@ -48,6 +48,10 @@ struct Form {
     static constexpr int LOAD_WARPS = 4 * LOAD_GROUPS;
     using Walks = Walk<MODE, BM, BK, PAIRED>;
     static constexpr int THREADS = 32 * (DRAIN_WARPS + LOAD_WARPS + 4);
+    // Registers go over to the warps that drain: from those that copy, or (16 drain warps: 640 threads at 96, 512 x 104 + 128 x 64 = 640 x 96)
+    // from the multiplier's four
+    static constexpr bool MOVES = LOADING == COPIES || DRAIN_WARPS == 16;
+    static constexpr int MULTIPLY = LOADING == COPIES ? MULTIPLY_REGISTERS : 64;
 };
 
 // Where the eight values of slab i that a loading thread (row 0..31 of the slab, unit 0..7 of the row) brings come from, and how
@@ -412,7 +416,7 @@ __device__ __forceinline__ void linear_body(const LinearArgs& a, S& sh, Drain dr
     tc::tc_fence_after_sync();
     const int rank = F::PAIRED ? (int)tc::cluster_rank() : 0;
     if (warp < F::DRAIN_WARPS) {
-        if constexpr (LOADING == COPIES) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(DRAIN_REGISTERS));
+        if constexpr (F::MOVES) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(DRAIN_REGISTERS));
         drain(slabs);
     } else if (warp < MULTIPLIER) {
         if constexpr (LOADING == COPIES) {
@@ -421,7 +425,7 @@ __device__ __forceinline__ void linear_body(const LinearArgs& a, S& sh, Drain dr
             copy_role<F>(a, sh, ring_bytes, t & 127, t >> 7);
         }
     } else {
-        if constexpr (LOADING == COPIES) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(MULTIPLY_REGISTERS));
+        if constexpr (F::MOVES) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(F::MULTIPLY));
         if (warp == MULTIPLIER && rank == 0) multiply_role<F>(a, sh, ring, ones);
         if constexpr (LOADING == BULK)
             if (warp == MULTIPLIER + 1) bulk_role<F>(a, sh, ring_bytes, lane);

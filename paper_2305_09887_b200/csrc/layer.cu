@@ -10,7 +10,7 @@
 // the warps that drain it.  A tile of a gated layer has the same columns of both matrices, so that a lane finds both factors of a result in its own
 // row.  dZ is rounded to the rows' type: it is an operand of 16-bit products.
 //
-// This file: 16-bit rows, and the calls.  fp32 rows are in layer_split.cu.
+// This file: the calls.  The kernels of 16-bit rows are in layer_kernels.cuh, those of fp32 rows in layer_split.cu.
 #include <algorithm>
 
 #include "grouped_rows.cuh"
@@ -21,178 +21,6 @@ RTMA_BOUNDS_TU()
 namespace {
 
 using namespace grouped;
-
-// 32 values of a lane's row as they are stored; those that do not exist read as zero.
-template <class T>
-struct Side {
-    Eight<T> e[4];
-    __device__ __forceinline__ void load(const T* p, int valid, int granule) {
-        if (valid >= 32 && granule == 32) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                uint4 &x = e[2 * i].w[0], &y = e[2 * i + 1].w[0];
-                asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                             : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w), "=r"(y.x), "=r"(y.y), "=r"(y.z), "=r"(y.w)
-                             : "l"(p + 16 * i));
-            }
-        } else if (granule >= 16 && valid % 8 == 0) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                e[i].w[0] = make_uint4(0u, 0u, 0u, 0u);
-                if (8 * i < valid) asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(e[i].w[0].x), "=r"(e[i].w[0].y), "=r"(e[i].w[0].z), "=r"(e[i].w[0].w) : "l"(p + 8 * i));
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) e[i].load(p + 8 * i, max(0, min(8, valid - 8 * i)), granule);
-        }
-    }
-};
-
-// What a drain warp does with its rows (a quarter of the tile's) and every second 32 columns of a tile.
-template <class F, bool GRADIENT>
-__device__ __forceinline__ void drain_layer(const LayerArgs& a, Shared& sh, uint32_t slabs) {
-    typedef typename F::T T;
-    constexpr bool GATED = F::GATED;
-    constexpr bool AHEAD = F::LOADING != COPIES;  // the next columns' rows are requested before these are worked on (with fewer registers they are not)
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, half = warp >> 2;
-    Outlet<T, F::OUT_SLABS> outlet{slabs + warp * F::OUT_BYTES};
-    LayerBias bias{sh.bias + 128 * warp};
-    const uint32_t tmem = sh.tmem_base + ((uint32_t)(32 * quarter) << 16);
-    const int chunks = (a.BN + 31) / 32, mine = (chunks - half + 1) / 2;
-    int slope_part = -1;
-    float slope = 0.f;
-    typename F::Walks w;
-    tc::RingAt acc;
-    for (bool more = w.first(a, sh); more; more = w.next_tile(a, sh)) {
-        const int rows = min(32, w.rows - 32 * quarter);
-        const int64_t row0 = w.row0 + 32 * quarter;
-        auto column = [&](int chunk) { return w.n0 + 32 * chunk; };
-        auto columns = [&](int chunk) { return min(min(32, a.BN - 32 * chunk), a.width - column(chunk)); };
-        if (a.bias) {
-            if constexpr (GATED)
-                bias.fetch(a, w.part, w.n0, 2 * mine, lane, static_cast<const T*>(nullptr),
-                           [&](int i) { return column(half + (i & ~1)) + (i & 1 ? a.width : 0); }, [&](int i) { return columns(half + (i & ~1)); });
-            else
-                bias.fetch(a, w.part, w.n0, mine, lane, static_cast<const T*>(nullptr), [&](int i) { return column(half + 2 * i); }, [&](int i) { return columns(half + 2 * i); });
-        }
-        if (a.slope && w.part != slope_part) {
-            slope_part = w.part;
-            slope = __ldg(a.slope + w.part * a.slope_stride);
-        }
-        const T* const from = static_cast<const T*>(a.side) + (row0 + lane) * a.lds;
-        Side<T> side, next;
-        auto request = [&](int chunk, Side<T>& to) {
-            if ((GRADIENT || a.side) && chunk < chunks) to.load(from + column(chunk), lane < rows ? max(0, columns(chunk)) : 0, a.gs);
-        };
-        if (AHEAD) request(half, next);
-        float slope_sum = 0.f;
-        if (!wait_for<F::PAIRED>(&sh.acc_full[acc.s], acc.phase, sh, a.error_word)) return;
-        __syncwarp();
-        tc::tc_fence_after_sync();
-        for (int chunk = half, i = 0; chunk < chunks; chunk += 2, ++i) {
-            if (AHEAD) {
-                side = next;
-                request(chunk + 2, next);
-            } else {
-                request(chunk, side);
-            }
-            float v[32], u[GATED ? 32 : 1];
-            if constexpr (GATED) {
-                uint32_t x[32], y[32];
-                tc::tmem_load_issue(tmem + acc.s * F::ACC_COLUMNS + 32 * chunk, x);
-                tc::tmem_load_issue(tmem + acc.s * F::ACC_COLUMNS + 128 + 32 * chunk, y);
-                tc::tmem_load_wait(x);
-                tc::tmem_load_wait(y);
-#pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    v[j] = __uint_as_float(x[j]);
-                    u[j] = __uint_as_float(y[j]);
-                }
-            } else {
-                tc::tmem_load_32x32(tmem + acc.s * F::ACC_COLUMNS + 32 * chunk, v);
-            }
-            const int cols = columns(chunk);
-            float ds = 0.f;
-            auto eight = [&](auto Q) {
-                constexpr int q = decltype(Q)::value;
-                f2 z[4], d[4];
-                eight_of<q>(v, z);
-                if (a.bias) bias.add(z, GATED ? 2 * i : i, q);
-                if (GRADIENT && a.slope_slots) cut_eight(z, cols - 8 * q);
-                if (GRADIENT || a.side) pairs_of(side.e[q], d);
-                if constexpr (GATED) {
-                    f2 y[4];
-                    eight_of<q>(u, y);
-                    if (a.bias) bias.add(y, 2 * i + 1, q);
-                    if (GRADIENT && a.slope_slots) cut_eight(y, cols - 8 * q);
-                    if constexpr (GRADIENT) {
-                        f2 dv[4], du[4];
-                        ds += gate_back(a.act, slope, z, y, d, dv, du);
-                        eight_to<q>(dv, v);
-                        eight_to<q>(du, u);
-                    } else {
-                        activate(a.act, slope, z);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) z[j] = a.side ? fma2(z[j], y[j], d[j]) : mul2(z[j], y[j]);
-                        eight_to<q>(z, v);
-                    }
-                } else if constexpr (GRADIENT) {
-                    ds += activate_back(a.act, slope, z, d);
-                    eight_to<q>(d, v);
-                } else {
-                    activate(a.act, slope, z);
-                    if (a.side) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) z[j] = add2(z[j], d[j]);
-                    }
-                    eight_to<q>(z, v);
-                }
-            };
-            eight(std::integral_constant<int, 0>());
-            eight(std::integral_constant<int, 1>());
-            eight(std::integral_constant<int, 2>());
-            eight(std::integral_constant<int, 3>());
-            if (lane < rows) slope_sum += ds;  // (what the accumulator has for rows that are not there may be anything)
-            const int c = column(chunk);
-            if (rows > 0 && cols > 0) {
-                constexpr int PIECE = 16 / (int)sizeof(T);
-                T* const out = static_cast<T*>(a.out) + row0 * a.ldo + c;
-                if constexpr (GATED && GRADIENT) {
-                    outlet.put(a, v, row0, c, rows, cols, false, out, a.ldo, lane);
-                    outlet.put(a, u, row0, a.width + c, rows, cols, c + cols == a.width && a.width % PIECE == 0, out + a.width, a.ldo, lane, a.width % PIECE == 0);
-                } else {
-                    outlet.put(a, v, row0, c, rows, cols, c + cols == a.width && a.width % PIECE == 0, out, a.ldo, lane);
-                }
-            }
-        }
-        tc::tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) {  // (a pair's warps all report to the first block)
-            if constexpr (F::PAIRED) tc::mbar_arrive_remote(tc::leader_addr(&sh.acc_empty[acc.s]));
-            else tc::mbar_arrive(&sh.acc_empty[acc.s]);
-        }
-        acc.advance(2);
-        if (GRADIENT && a.slope_slots) {
-            for (int o = 16; o > 0; o >>= 1) slope_sum += __shfl_xor_sync(0xffffffffu, slope_sum, o);
-            const int64_t tile = F::PAIRED ? 2 * (int64_t)w.tile + (blockIdx.x & 1) : w.tile;
-            if (lane == 0) a.slope_slots[tile * a.slope_warps + warp] = slope_sum;
-        }
-    }
-    outlet.finish(lane);
-}
-
-template <class T, int LOADING, bool GATED, bool GRADIENT>
-__global__ void __launch_bounds__(Form<T, FORWARD, LOADING, GATED>::THREADS, 1) layer_kernel(const __grid_constant__ LayerArgs a) {
-    typedef Form<T, FORWARD, LOADING, GATED> F;
-    __shared__ Shared sh;
-    linear_body<F>(a, sh, [&](uint32_t slabs) { drain_layer<F, GRADIENT>(a, sh, slabs); });
-}
-template <class T, bool GATED, bool GRADIENT>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Form<T, FORWARD, PAIR, GATED>::THREADS, 1) layer_pair_kernel(const __grid_constant__ LayerArgs a) {
-    typedef Form<T, FORWARD, PAIR, GATED> F;
-    __shared__ Shared sh;
-    linear_body<F>(a, sh, [&](uint32_t slabs) { drain_layer<F, GRADIENT>(a, sh, slabs); });
-}
 
 // 16-bit matrices -> [part][d_in][halves * up] on 16-byte boundaries, up: width rounded up to 8
 __global__ void __launch_bounds__(256) lay_out_matrices_kernel(const __half* __restrict__ W, int64_t w_stride, int parts, int d_in, int width, int halves, int granule,
@@ -230,28 +58,6 @@ __global__ void __launch_bounds__(256) slope_reduce_kernel(const int64_t* offset
     }
 }
 
-template <class T, int LOADING, bool GATED, bool GRADIENT>
-int32_t launch_form(rtma_ctx* ctx, const LayerArgs& a, unsigned grid, bool& configured, cudaStream_t stream) {
-    typedef Form<T, FORWARD, LOADING, GATED> F;
-    void (*kernel)(LayerArgs);
-    if constexpr (LOADING == PAIR) kernel = layer_pair_kernel<T, GATED, GRADIENT>;
-    else kernel = layer_kernel<T, LOADING, GATED, GRADIENT>;
-    if (!configured) {
-        RTMA_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, F::DYNAMIC_BYTES));
-        configured = true;
-    }
-    launch_kernel(kernel, grid, F::THREADS, F::DYNAMIC_BYTES, stream, a);
-    RTMA_LAUNCH_CHECK(ctx);
-    return RTMA_OK;
-}
-
-template <class T, int LOADING>
-int32_t launch_kind(rtma_ctx* ctx, const LayerArgs& a, bool gated, bool gradient, unsigned grid, cudaStream_t stream) {
-    bool* once = ctx->layer_configured + ((std::is_same<T, __half>::value ? 1 : 0) * 3 + LOADING) * 4;
-    if (gated) return gradient ? launch_form<T, LOADING, true, true>(ctx, a, grid, once[3], stream) : launch_form<T, LOADING, true, false>(ctx, a, grid, once[2], stream);
-    return gradient ? launch_form<T, LOADING, false, true>(ctx, a, grid, once[1], stream) : launch_form<T, LOADING, false, false>(ctx, a, grid, once[0], stream);
-}
-
 // The layer's kernel on 16-bit rows.  room: scratch for the laid-out matrices.
 int32_t launch_layer(rtma_ctx* ctx, LayerArgs& a, bool bf16, bool gated, bool gradient, char* room, int cls, cudaStream_t stream) {
     const int halves = gated ? 2 : 1;
@@ -274,18 +80,17 @@ int32_t launch_layer(rtma_ctx* ctx, LayerArgs& a, bool bf16, bool gated, bool gr
     if (!make_tensor_map_16bit(&a.map_b, bf16, a.B, a.w_stride ? a.G : 1, a.d_in, gated ? a.up + a.width : a.width, a.ldb, a.w_stride ? a.w_stride : a.d_in * a.ldb, BK))
         return rtma_fail(ctx, RTMA_ERR_CUDA, "grouped layer: no tensor map for %d matrices of %d x %d", a.w_stride ? a.G : 1, a.d_in, a.width);
     if (a.va >= 16 && make_tensor_map_16bit(&a.map_a, bf16, a.A, 1, a.n, a.d_in, a.lda, a.n * a.lda, BM)) a.in_bulk |= 1;
+    auto launch = bf16 ? launch_layer_bf16 : launch_layer_f16;
     KernelScope ks(ctx, cls, stream);
     // pairs of blocks by the rule of the plain products: deep contractions, whole tiles
     if (a.in_bulk == 3 && a.BN == (gated ? 128 : 256) && a.d_in >= 256 && tiles >= ctx->sm_count) {
         a.tile_rows = 2 * BM;
         a.tiles = a.n / a.tile_rows + a.G;
         const unsigned grid = (unsigned)std::min<int64_t>(2 * a.tiles * a.n_tiles, ctx->sm_count & ~1);
-        return bf16 ? launch_kind<__nv_bfloat16, PAIR>(ctx, a, gated, gradient, grid, stream) : launch_kind<__half, PAIR>(ctx, a, gated, gradient, grid, stream);
+        return launch(ctx, a, PAIR, gated, gradient, grid, stream);
     }
-    const unsigned grid = (unsigned)std::min<int64_t>(tiles, ctx->sm_count);
-    if (a.in_bulk == 3)
-        return bf16 ? launch_kind<__nv_bfloat16, BULK>(ctx, a, gated, gradient, grid, stream) : launch_kind<__half, BULK>(ctx, a, gated, gradient, grid, stream);
-    return bf16 ? launch_kind<__nv_bfloat16, COPIES>(ctx, a, gated, gradient, grid, stream) : launch_kind<__half, COPIES>(ctx, a, gated, gradient, grid, stream);
+    if (a.in_bulk != 3) a.slope_warps = 8;
+    return launch(ctx, a, a.in_bulk == 3 ? BULK : COPIES, gated, gradient, (unsigned)std::min<int64_t>(tiles, ctx->sm_count), stream);
 }
 
 int32_t check_layer(rtma_ctx* ctx, const char* who, const rtma_layer_desc* d, int64_t n, int32_t G, const int64_t* offsets, const float* slope) {
@@ -317,7 +122,7 @@ void describe(rtma_ctx* ctx, LayerArgs& a, const rtma_layer_desc* d, int64_t n, 
     a.vb = std::min(row_granule(W, wide, es), row_granule(nullptr, d->w_stride, es));
     a.act = d->act;
     a.slope = d->act == RTMA_ACT_PRELU ? slope : nullptr; a.slope_stride = d->slope_stride;
-    a.slope_warps = 8;
+    a.slope_warps = 16;
     if (d->dtype == RTMA_F32) {
         describe_layer_split(a, d->gated != 0);
         *bytes = layer_split_bytes(a, d->gated != 0);
@@ -386,7 +191,7 @@ extern "C" int32_t rtma_grouped_layer_grad(rtma_ctx* ctx, const rtma_layer_desc*
     size_t matrices = 0, slots = 0, rows_bytes = 0, dw_bytes = 0;
     describe(ctx, a, d, n, G, offsets, X, ldx, W, b, slope, &matrices);
     matrices = ArenaCursor::granule(matrices);
-    if (dslope) slots = sizeof(float) * (size_t)(a.tiles * a.n_tiles + 2 * (int64_t)G * a.n_tiles) * 8;
+    if (dslope) slots = sizeof(float) * (size_t)(a.tiles * a.n_tiles + 2 * (int64_t)G * a.n_tiles) * a.slope_warps;
     // all scratch at once: inside a capture nothing is enqueued unless everything fits
     if (dX) RTMA_TRY(grouped_rows(ctx, who, true, d->dtype, n, G, offsets, d->d_in, wide, dz, ldz, W, d->w_stride, nullptr, 0, dX, lddx, &rows_bytes, stream));
     if (dW)

@@ -18,6 +18,7 @@ struct LayerArgs : LinearArgs {
     int g2;               // granule of the result's second half (gradient of a gated layer)
     float* slope_slots;   // gradient, PReLU: what every warp that drains a tile has of the slope's gradient, [tile][slope_warps]
     int slope_warps;
+    int step_rows, step_rest;  // from a block's tile to its next: row tiles, and tiles of columns beside them
 };
 
 #ifdef __CUDACC__
@@ -31,14 +32,14 @@ struct LayerBias {
         if (of_part == part && of_n0 == n0) return;
         part = of_part;
         n0 = of_n0;
-        const T* bias = static_cast<const T*>(a.bias) + part * a.bias_stride;
+        const T* bias = static_cast<const T*>(a.bias) + part * a.bias_stride;  // (none: zeros)
         __syncwarp();
-        for (int i = 0; i < chunks; ++i) at[32 * i + lane] = lane < edge(i) ? to_f32(bias[column(i) + lane]) : 0.f;
+        for (int i = 0; i < chunks; ++i) at[32 * i + lane] = a.bias && lane < edge(i) ? to_f32(bias[column(i) + lane]) : 0.f;
         __syncwarp();
     }
-    // eight of them, added to v
-    __device__ __forceinline__ void add(f2 (&v)[4], int i, int q) const {
-        const float4* b = reinterpret_cast<const float4*>(at + 32 * i + 8 * q);
+    // eight of them, from the one numbered j on, added to v
+    __device__ __forceinline__ void add(f2 (&v)[4], int j) const {
+        const float4* b = reinterpret_cast<const float4*>(at + j);
         const float4 x = b[0], y = b[1];
         v[0] = add2(v[0], pack2(x.x, x.y));
         v[1] = add2(v[1], pack2(x.z, x.w));
@@ -47,16 +48,6 @@ struct LayerBias {
     }
 };
 
-template <int Q>
-__device__ __forceinline__ void eight_of(const float (&v)[32], f2 (&x)[4]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = pack2(v[8 * Q + 2 * i], v[8 * Q + 2 * i + 1]);
-}
-template <int Q>
-__device__ __forceinline__ void eight_to(const f2 (&x)[4], float (&v)[32]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) unpack2(x[i], v[8 * Q + 2 * i], v[8 * Q + 2 * i + 1]);
-}
 // Values from `valid` on become zero: tensor memory may hold anything in columns that are not the tile's, and a sum must not see it.
 __device__ __forceinline__ void cut_eight(f2 (&x)[4], int valid) {
     if (valid >= 8) return;
@@ -67,6 +58,61 @@ __device__ __forceinline__ void cut_eight(f2 (&x)[4], int valid) {
         x[i] = pack2(2 * i < valid ? a : 0.f, 2 * i + 1 < valid ? b : 0.f);
     }
 }
+
+// Eight of a lane's results.  z (and y, a gated layer's second factors): sums of the products, bias j.. added here; d: the row that is read
+// beside them (beside).  summed: the slope's gradient is wanted.  z (and y) become what is stored; returns the slope's gradient.  valid: how many are the tile's.
+template <bool GATED, bool GRADIENT>
+__device__ __forceinline__ float eight_results(int act, bool beside, const LayerBias& bias, int j, int j2, float slope, bool summed, int valid, f2 (&z)[4], f2 (&y)[4], const f2 (&d)[4]) {
+    float ds = 0.f;
+    bias.add(z, j);
+    if constexpr (GATED) bias.add(y, j2);
+    if constexpr (GRADIENT) {
+        if (act == RTMA_ACT_PRELU && summed) {
+            cut_eight(z, valid);
+            if constexpr (GATED) cut_eight(y, valid);
+        }
+        if constexpr (GATED) {
+            f2 dz[4], dy[4];
+            ds = gate_back(act, slope, z, y, d, dz, dy);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                z[i] = dz[i];
+                y[i] = dy[i];
+            }
+        } else {
+            f2 dz[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dz[i] = d[i];
+            ds = activate_back(act, slope, z, dz);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[i] = dz[i];
+        }
+    } else {
+        activate(act, slope, z);
+        if constexpr (GATED) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[i] = beside ? fma2(z[i], y[i], d[i]) : mul2(z[i], y[i]);
+        } else if (beside) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[i] = add2(z[i], d[i]);
+        }
+    }
+    return ds;
+}
+// f of the activation (and of whether rows are read beside the sums) as constants
+template <bool GRADIENT, class Call>
+__device__ __forceinline__ void with_activation(const LayerArgs& a, Call f) {
+    auto beside = [&](auto ACT) {
+        if (GRADIENT || a.side) f(ACT, std::true_type());
+        else f(ACT, std::false_type());
+    };
+    switch (a.act) {
+        case RTMA_ACT_NONE: beside(std::integral_constant<int, RTMA_ACT_NONE>()); break;
+        case RTMA_ACT_RELU: beside(std::integral_constant<int, RTMA_ACT_RELU>()); break;
+        case RTMA_ACT_PRELU: beside(std::integral_constant<int, RTMA_ACT_PRELU>()); break;
+        default: beside(std::integral_constant<int, RTMA_ACT_SILU>()); break;
+    }
+}
 #endif
 
 }  // namespace grouped
@@ -75,3 +121,6 @@ __device__ __forceinline__ void cut_eight(f2 (&x)[4], int valid) {
 size_t layer_split_bytes(const grouped::LayerArgs& a, bool gated);
 void describe_layer_split(grouped::LayerArgs& a, bool gated);  // tiles
 int32_t launch_layer_split(rtma_ctx* ctx, grouped::LayerArgs& a, bool gated, bool gradient, void* planes, int cls, cudaStream_t stream);
+// 16-bit rows: the kernel of one way of loading (grouped_rows.cuh).
+int32_t launch_layer_bf16(rtma_ctx* ctx, grouped::LayerArgs& a, int loading, bool gated, bool gradient, unsigned grid, cudaStream_t stream);
+int32_t launch_layer_f16(rtma_ctx* ctx, grouped::LayerArgs& a, int loading, bool gated, bool gradient, unsigned grid, cudaStream_t stream);

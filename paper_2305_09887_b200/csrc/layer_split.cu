@@ -46,8 +46,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS_PER_SM) layer_split_kernel(con
         // the columns of total[h]: results, or (gated) what they are made of
         auto column = [&](int h) { return GATED ? (out.n0 + out_c) / 2 : out.n0 + out_c + 32 * h; };
         auto columns = [&](int h) { return GATED ? min(32, a.width - column(0)) : min(min(32, a.BN - out_c - 32 * h), a.width - column(h)); };
-        if (a.bias)
-            bias.fetch(a, out.part, out.n0, 2, lane, static_cast<const float*>(nullptr), [&](int h) { return column(h) + (GATED && h ? a.width : 0); }, columns);
+        bias.fetch(a, out.part, out.n0, 2, lane, static_cast<const float*>(nullptr), [&](int h) { return column(h) + (GATED && h ? a.width : 0); }, columns);
         const float slope = a.slope ? __ldg(a.slope + out.part * a.slope_stride) : 0.f;
         float slope_sum = 0.f;
 #pragma unroll
@@ -56,49 +55,26 @@ __global__ void __launch_bounds__(THREADS, BLOCKS_PER_SM) layer_split_kernel(con
             if (rows <= 0 || cols <= 0) continue;
             const float* const from = static_cast<const float*>(a.side) + (row0 + lane) * a.lds + c;
             float ds = 0.f;
-            auto eight = [&](auto Q) {
-                constexpr int q = decltype(Q)::value;
-                f2 z[4], d[4];
-                eight_of<q>(total[h], z);
-                if (a.bias) bias.add(z, GATED ? 0 : h, q);
-                if (GRADIENT && a.slope_slots) cut_eight(z, cols - 8 * q);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                f2 z[4], y[4], d[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    z[k] = pack2(total[h][8 * q + 2 * k], total[h][8 * q + 2 * k + 1]);
+                    if constexpr (GATED) y[k] = pack2(total[1][8 * q + 2 * k], total[1][8 * q + 2 * k + 1]);
+                }
                 if (GRADIENT || a.side) {
                     Eight<float> e;
                     e.load(from + 8 * q, lane < rows ? max(0, min(8, cols - 8 * q)) : 0, a.gs);
                     pairs_of(e, d);
                 }
-                if constexpr (GATED) {
-                    f2 y[4];
-                    eight_of<q>(total[1], y);
-                    if (a.bias) bias.add(y, 1, q);
-                    if (GRADIENT && a.slope_slots) cut_eight(y, cols - 8 * q);
-                    if constexpr (GRADIENT) {
-                        f2 dv[4], du[4];
-                        ds += gate_back(a.act, slope, z, y, d, dv, du);
-                        eight_to<q>(dv, total[0]);
-                        eight_to<q>(du, total[1]);
-                    } else {
-                        activate(a.act, slope, z);
+                ds += eight_results<GATED, GRADIENT>(a.act, a.side != nullptr, bias, (GATED ? 0 : 32 * h) + 8 * q, 32 + 8 * q, slope, a.slope_slots != nullptr, cols - 8 * q, z, y, d);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) z[j] = a.side ? fma2(z[j], y[j], d[j]) : mul2(z[j], y[j]);
-                        eight_to<q>(z, total[0]);
-                    }
-                } else if constexpr (GRADIENT) {
-                    ds += activate_back(a.act, slope, z, d);
-                    eight_to<q>(d, total[h]);
-                } else {
-                    activate(a.act, slope, z);
-                    if (a.side) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) z[j] = add2(z[j], d[j]);
-                    }
-                    eight_to<q>(z, total[h]);
+                for (int k = 0; k < 4; ++k) {
+                    unpack2(z[k], total[h][8 * q + 2 * k], total[h][8 * q + 2 * k + 1]);
+                    if constexpr (GATED && GRADIENT) unpack2(y[k], total[1][8 * q + 2 * k], total[1][8 * q + 2 * k + 1]);
                 }
-            };
-            eight(std::integral_constant<int, 0>());
-            eight(std::integral_constant<int, 1>());
-            eight(std::integral_constant<int, 2>());
-            eight(std::integral_constant<int, 3>());
+            }
             if (lane < rows) slope_sum += ds;
             float* const to = static_cast<float*>(a.out) + row0 * a.ldo + c;
             put_rows(to, a.ldo, a.go, total[h], rows, cols, lane);
