@@ -13,7 +13,6 @@
 // This file: the calls.  The kernels of 16-bit rows are in layer_kernels.cuh, those of fp32 rows in layer_split.cu.
 #include <algorithm>
 
-#include "grouped_rows.cuh"
 #include "layer.cuh"
 
 RTMA_BOUNDS_TU()
@@ -21,6 +20,8 @@ RTMA_BOUNDS_TU()
 namespace {
 
 using namespace grouped;
+
+constexpr int BM = 128, BK = 64;  // of the kernels on 16-bit rows
 
 // 16-bit matrices -> [part][d_in][halves * up] on 16-byte boundaries, up: width rounded up to 8
 __global__ void __launch_bounds__(256) lay_out_matrices_kernel(const __half* __restrict__ W, int64_t w_stride, int parts, int d_in, int width, int halves, int granule,
@@ -34,6 +35,63 @@ __global__ void __launch_bounds__(256) lay_out_matrices_kernel(const __half* __r
         Eight<__half> x;
         x.load(W + part * w_stride + ((row - part * d_in) * halves + h) * width + 8 * u, min(8, width - 8 * u), granule);
         *reinterpret_cast<uint4*>(out + 8 * i) = x.w[0];
+    }
+}
+
+struct SumsArgs {
+    const int64_t* offsets;
+    int64_t n, tile_rows, tiles;
+    int G, places, n_tiles, columns;  // columns: 0 if their sums are not wanted
+    int width, real_width;            // of one of dZ's halves, with and without what was rounded up
+    const float *column_slots, *slope_slots;
+    void* db;
+    float* dslope;
+    int64_t db_stride, dslope_stride;
+    bool shared, slope_shared;
+    // a column's place in the bias, or -1
+    __device__ __forceinline__ int place_of(int column) const {
+        const int second = column >= width ? 1 : 0, c = column - second * width;
+        return c < real_width ? second * real_width + c : -1;
+    }
+};
+
+// What pairs of blocks leave of sums over rows (layer_pairs.cuh), added up in order: a block for 32 columns of dZ and a part (or all parts:
+// shared), the last of a part for its slope's gradient.
+template <class O>
+__global__ void __launch_bounds__(256) layer_sums_kernel(const __grid_constant__ SumsArgs a) {
+    __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
+    __shared__ double red[256];
+    wait_for_kernel_before();
+    number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const bool of_slope = (int)blockIdx.x * 32 >= a.columns, shared = of_slope ? a.slope_shared : a.shared;
+    if ((int)blockIdx.y > 0 && shared) return;
+    const int column = 32 * blockIdx.x + lane, first = shared ? 0 : blockIdx.y, last = shared ? a.G : first + 1;
+    const int64_t tiles = tile_start[a.G];
+    double s = 0.0;
+    for (int part = first; part < last; ++part) {
+        const int from = tile_start[part], to = tile_start[part + 1];
+        if (from == to) continue;
+        // the places whose tiles [tiles i / places, tiles (i + 1) / places) are among the part's
+        int i = (int)((int64_t)from * a.places / tiles);
+        while ((int)(tiles * (i + 1) / a.places) <= from) ++i;
+        for (; i < a.places && (int)(tiles * i / a.places) < to; ++i) {
+            if ((int)(tiles * i / a.places) == (int)(tiles * (i + 1) / a.places)) continue;
+            const int64_t slot = 8 * (int64_t)(i + part);
+            if (!of_slope) s += column < a.columns ? a.column_slots[(slot + warp) * a.columns + column] : 0.f;
+            else
+                for (int k = threadIdx.x; k < 32 * a.n_tiles; k += 256) s += a.slope_slots[slot * 4 * a.n_tiles + k];
+        }
+    }
+    red[threadIdx.x] = s;
+    __syncthreads();
+    if (!of_slope) {
+        if (warp) return;
+        for (int k = 1; k < 8; ++k) s += red[32 * k + lane];
+        if (column < a.columns && a.place_of(column) >= 0) static_cast<O*>(a.db)[blockIdx.y * a.db_stride + a.place_of(column)] = from_f32<O>((float)s);
+    } else if (threadIdx.x == 0) {
+        for (int k = 1; k < 256; ++k) s += red[k];
+        a.dslope[blockIdx.y * a.dslope_stride] = (float)s;
     }
 }
 
@@ -79,18 +137,15 @@ int32_t launch_layer(rtma_ctx* ctx, LayerArgs& a, bool bf16, bool gated, bool gr
     a.in_bulk = 2;
     if (!make_tensor_map_16bit(&a.map_b, bf16, a.B, a.w_stride ? a.G : 1, a.d_in, gated ? a.up + a.width : a.width, a.ldb, a.w_stride ? a.w_stride : a.d_in * a.ldb, BK))
         return rtma_fail(ctx, RTMA_ERR_CUDA, "grouped layer: no tensor map for %d matrices of %d x %d", a.w_stride ? a.G : 1, a.d_in, a.width);
-    if (a.va >= 16 && make_tensor_map_16bit(&a.map_a, bf16, a.A, 1, a.n, a.d_in, a.lda, a.n * a.lda, BM)) a.in_bulk |= 1;
-    auto launch = bf16 ? launch_layer_bf16 : launch_layer_f16;
-    KernelScope ks(ctx, cls, stream);
-    // pairs of blocks by the rule of the plain products: deep contractions, whole tiles
-    if (a.in_bulk == 3 && a.BN == (gated ? 128 : 256) && a.d_in >= 256 && tiles >= ctx->sm_count) {
-        a.tile_rows = 2 * BM;
-        a.tiles = a.n / a.tile_rows + a.G;
-        const unsigned grid = (unsigned)std::min<int64_t>(2 * a.tiles * a.n_tiles, ctx->sm_count & ~1);
-        return launch(ctx, a, PAIR, gated, gradient, grid, stream);
+    if (a.va >= 16) {
+        if (make_tensor_map_16bit(&a.map_a, bf16, a.A, 1, a.n, a.d_in, a.lda, a.n * a.lda, BM)) a.in_bulk |= 1;
+        else if (a.places) return rtma_fail(ctx, RTMA_ERR_CUDA, "grouped layer: no tensor map for rows of %d values", a.d_in);
     }
-    if (a.in_bulk != 3) a.slope_warps = 8;
-    return launch(ctx, a, a.in_bulk == 3 ? BULK : COPIES, gated, gradient, (unsigned)std::min<int64_t>(tiles, ctx->sm_count), stream);
+    if (a.places && a.side && !make_store_map(&a.map_side, bf16 ? RTMA_BF16 : RTMA_F16, a.side, a.n, a.width, a.lds))
+        return rtma_fail(ctx, RTMA_ERR_CUDA, "grouped layer: no tensor map for rows of %d values", a.width);
+    KernelScope ks(ctx, cls, stream);
+    const unsigned grid = a.places ? 2u * a.places * a.n_tiles : (unsigned)std::min<int64_t>(tiles, ctx->sm_count);
+    return (bf16 ? launch_layer_bf16 : launch_layer_f16)(ctx, a, a.places != 0, gated, gradient, grid, stream);
 }
 
 int32_t check_layer(rtma_ctx* ctx, const char* who, const rtma_layer_desc* d, int64_t n, int32_t G, const int64_t* offsets, const float* slope) {
@@ -107,7 +162,7 @@ int32_t check_layer(rtma_ctx* ctx, const char* who, const rtma_layer_desc* d, in
 
 // The arguments of the layer's kernel and the scratch that it takes (lay: the matrices have to be laid out).
 void describe(rtma_ctx* ctx, LayerArgs& a, const rtma_layer_desc* d, int64_t n, int32_t G, const int64_t* offsets, const void* X, int64_t ldx, const void* W, const void* b,
-              const float* slope, size_t* bytes) {
+              const float* slope, const void* side, int64_t lds, size_t* bytes) {
     const size_t es = row_type_bytes(d->dtype);
     const int wide = d->gated ? 2 * d->d_out : d->d_out;
     a.error_word = ctx->error_word;
@@ -122,16 +177,27 @@ void describe(rtma_ctx* ctx, LayerArgs& a, const rtma_layer_desc* d, int64_t n, 
     a.vb = std::min(row_granule(W, wide, es), row_granule(nullptr, d->w_stride, es));
     a.act = d->act;
     a.slope = d->act == RTMA_ACT_PRELU ? slope : nullptr; a.slope_stride = d->slope_stride;
-    a.slope_warps = 16;
+    a.slope_warps = 8;
+    a.side = side; a.lds = lds; a.gs = side ? row_granule(side, lds, es) : 0;
     if (d->dtype == RTMA_F32) {
         describe_layer_split(a, d->gated != 0);
         *bytes = layer_split_bytes(a, d->gated != 0);
         return;
     }
-    const int widest = d->gated ? 128 : 256;
+    a.bias_up = a.bias_width = a.width;
+    // Rows on 16-byte boundaries: pairs of blocks, as long as there are pairs for all tiles of columns
+    const int widest = d->gated ? 128 : 256, pairs = ctx->sm_count / 2;
     a.n_tiles = (int)ceil_div(a.width, widest);
-    a.BN = (int)ceil_div(ceil_div(a.width, a.n_tiles), 16) * 16;
-    a.n_tiles = (int)ceil_div(a.width, a.BN);
+    if (a.va >= 16 && (!side || a.gs >= 16) && a.n_tiles <= pairs) {
+        a.half = (int)ceil_div(ceil_div(a.width, a.n_tiles), d->gated ? 16 : 32) * 16;
+        a.n_tiles = (int)ceil_div(a.width, d->gated ? a.half : 2 * a.half);
+        a.tile_rows = 2 * BM;
+        a.tiles = n / a.tile_rows + G;
+        a.places = (int)std::min<int64_t>(pairs / a.n_tiles, a.tiles);
+    } else {
+        a.BN = (int)ceil_div(ceil_div(a.width, a.n_tiles), 16) * 16;
+        a.n_tiles = (int)ceil_div(a.width, a.BN);
+    }
     const bool lay = a.vb < 16 || a.w_stride < 0 || (d->gated && a.width % 8);
     *bytes = lay ? (size_t)2 * (a.w_stride ? G : 1) * a.d_in * (d->gated ? 2 : 1) * ceil_div(a.width, 8) * 8 : 0;
 }
@@ -154,8 +220,7 @@ extern "C" int32_t rtma_grouped_layer(rtma_ctx* ctx, const rtma_layer_desc* d, i
     const size_t es = row_type_bytes(d->dtype);
     LayerArgs a{};
     size_t bytes = 0;
-    describe(ctx, a, d, n, G, offsets, X, ldx, W, b, slope, &bytes);
-    a.side = residual; a.lds = ldr; a.gs = residual ? row_granule(residual, ldr, es) : 0;
+    describe(ctx, a, d, n, G, offsets, X, ldx, W, b, slope, residual, ldr, &bytes);
     a.out = Y; a.ldo = ldy;
     a.go = row_granule(Y, ldy, es);
     a.vo = d->dtype != RTMA_F32 && a.go >= 16 && make_store_map(&a.map_o, d->dtype, Y, n, d->d_out, ldy);
@@ -174,6 +239,9 @@ extern "C" int32_t rtma_grouped_layer_grad(rtma_ctx* ctx, const rtma_layer_desc*
     const int wide = gated ? 2 * d->d_out : d->d_out;
     if (n > 0 && (!X || !W || !dY || (!plain && !dZ))) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: null pointer", who);
     if (db && !dW) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: the bias gradient comes with the weights'", who);
+    if (G > 1 && db && (db_stride == 0) != (dw_stride == 0))
+        return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: either both gradients are one for all parts or neither", who);
+    if (G > 1 && db && db_stride != 0 && db_stride < wide && db_stride > -wide) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: gradients of the parts overlap", who);
     if (dslope && d->act != RTMA_ACT_PRELU) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: a slope's gradient without PReLU", who);
     if (d->grad_dtype != d->dtype && d->grad_dtype != RTMA_F32) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: gradients of the parameters in type %d", who, d->grad_dtype);
     if (ldx < d->d_in || lddy < d->d_out || (!plain && lddz < wide) || (dX && lddx < d->d_in))
@@ -189,33 +257,54 @@ extern "C" int32_t rtma_grouped_layer_grad(rtma_ctx* ctx, const rtma_layer_desc*
     const int64_t ldz = plain ? lddy : lddz;
     LayerArgs a{};
     size_t matrices = 0, slots = 0, rows_bytes = 0, dw_bytes = 0;
-    describe(ctx, a, d, n, G, offsets, X, ldx, W, b, slope, &matrices);
+    describe(ctx, a, d, n, G, offsets, X, ldx, W, b, slope, dY, lddy, &matrices);
     matrices = ArenaCursor::granule(matrices);
-    if (dslope) slots = sizeof(float) * (size_t)(a.tiles * a.n_tiles + 2 * (int64_t)G * a.n_tiles) * a.slope_warps;
+    const bool pairs = !plain && n > 0 && a.places != 0, sums = pairs && db;  // the bias gradient comes with dZ
+    size_t column_bytes = 0;
+    if (pairs) {
+        a.columns = wide;
+        const size_t rows = 8 * (size_t)(a.places + G);
+        column_bytes = sums ? ArenaCursor::granule(rows * wide * sizeof(float)) : 0;
+        slots = column_bytes + (dslope ? rows * a.n_tiles * 4 * sizeof(float) : 0);
+    } else if (dslope) {
+        slots = sizeof(float) * (size_t)(a.tiles * a.n_tiles) * a.slope_warps;
+    }
     // all scratch at once: inside a capture nothing is enqueued unless everything fits
     if (dX) RTMA_TRY(grouped_rows(ctx, who, true, d->dtype, n, G, offsets, d->d_in, wide, dz, ldz, W, d->w_stride, nullptr, 0, dX, lddx, &rows_bytes, stream));
     if (dW)
-        RTMA_TRY(grouped_dw(ctx, who, d->dtype, n, G, offsets, d->d_in, wide, X, ldx, dz, ldz, d->grad_dtype, dW, dw_stride, db, db_stride, &dw_bytes, stream));
+        RTMA_TRY(grouped_dw(ctx, who, d->dtype, n, G, offsets, d->d_in, wide, X, ldx, dz, ldz, d->grad_dtype, dW, dw_stride, sums ? nullptr : db, db_stride, &dw_bytes, stream));
     RTMA_TRY(prepare_row_call(ctx, std::max(plain ? 0 : matrices + slots, std::max(rows_bytes, dw_bytes)), stream));
     if (!plain && n > 0) {
-        a.side = dY; a.lds = lddy; a.gs = row_granule(dY, lddy, es);
         a.out = dZ; a.ldo = lddz;
         a.go = row_granule(dZ, lddz, es);
         a.g2 = std::min(a.go, row_granule(nullptr, d->d_out, es));
         a.vo = d->dtype != RTMA_F32 && a.go >= 16 && make_store_map(&a.map_o, d->dtype, dZ, n, wide, lddz);
-        a.slope_slots = dslope ? reinterpret_cast<float*>(ctx->arena + matrices) : nullptr;
+        a.column_slots = sums ? reinterpret_cast<float*>(ctx->arena + matrices) : nullptr;
+        a.slope_slots = dslope ? reinterpret_cast<float*>(ctx->arena + matrices + column_bytes) : nullptr;
         if (d->dtype == RTMA_F32) RTMA_TRY(launch_layer_split(ctx, a, gated, true, ctx->arena, KC_GEMM_FWD, stream));
         else RTMA_TRY(launch_layer(ctx, a, d->dtype == RTMA_BF16, gated, true, matrices ? ctx->arena : nullptr, KC_GEMM_FWD, stream));
     }
-    if (dslope) {
-        const bool shared = G > 1 && dslope_stride == 0;
-        const int64_t per_tile = (int64_t)a.n_tiles * a.slope_warps * (a.tile_rows / BM);
+    const bool slope_shared = G > 1 && dslope_stride == 0;
+    if (pairs && (sums || dslope)) {
+        SumsArgs m{};
+        m.offsets = offsets; m.n = n; m.tile_rows = a.tile_rows; m.tiles = a.tiles;
+        m.G = G; m.places = a.places; m.n_tiles = a.n_tiles; m.columns = sums ? wide : 0;
+        m.width = a.width; m.real_width = d->d_out;
+        m.column_slots = a.column_slots; m.slope_slots = a.slope_slots;
+        m.db = db; m.dslope = dslope; m.db_stride = db_stride; m.dslope_stride = dslope_stride;
+        m.shared = G > 1 && db_stride == 0; m.slope_shared = slope_shared;
+        void (*kernel)(SumsArgs) = d->grad_dtype == RTMA_F32 ? layer_sums_kernel<float> : d->grad_dtype == RTMA_BF16 ? layer_sums_kernel<__nv_bfloat16> : layer_sums_kernel<__half>;
         KernelScope ks(ctx, KC_REDUCE_SGD, stream);
-        launch_kernel(slope_reduce_kernel, shared ? 1u : (unsigned)G, 256, 0, stream, offsets, n, G, a.tile_rows, a.tiles, per_tile,
-                      const_cast<const float*>(a.slope_slots), shared, dslope, dslope_stride);
+        launch_kernel(kernel, dim3((unsigned)(ceil_div(m.columns, 32) + (dslope ? 1 : 0)), (unsigned)G), 256, 0, stream, m);
+        RTMA_LAUNCH_CHECK(ctx);
+    } else if (dslope) {
+        const int64_t per_tile = (int64_t)a.n_tiles * a.slope_warps;
+        KernelScope ks(ctx, KC_REDUCE_SGD, stream);
+        launch_kernel(slope_reduce_kernel, slope_shared ? 1u : (unsigned)G, 256, 0, stream, offsets, n, G, a.tile_rows, a.tiles, per_tile,
+                      const_cast<const float*>(a.slope_slots), slope_shared, dslope, dslope_stride);
         RTMA_LAUNCH_CHECK(ctx);
     }
     if (dX) RTMA_TRY(grouped_rows(ctx, who, true, d->dtype, n, G, offsets, d->d_in, wide, dz, ldz, W, d->w_stride, nullptr, 0, dX, lddx, nullptr, stream));
-    if (dW) RTMA_TRY(grouped_dw(ctx, who, d->dtype, n, G, offsets, d->d_in, wide, X, ldx, dz, ldz, d->grad_dtype, dW, dw_stride, db, db_stride, nullptr, stream));
+    if (dW) RTMA_TRY(grouped_dw(ctx, who, d->dtype, n, G, offsets, d->d_in, wide, X, ldx, dz, ldz, d->grad_dtype, dW, dw_stride, sums ? nullptr : db, db_stride, nullptr, stream));
     return RTMA_OK;
 }

@@ -19,6 +19,13 @@ struct LayerArgs : LinearArgs {
     float* slope_slots;   // gradient, PReLU: what every warp that drains a tile has of the slope's gradient, [tile][slope_warps]
     int slope_warps;
     int step_rows, step_rest;  // from a block's tile to its next: row tiles, and tiles of columns beside them
+    // pairs of blocks (layer_pairs.cuh)
+    int half;             // columns that each block of a pair brings of the matrix (gated: of one of the two)
+    int places;           // pairs that share a tile's columns
+    int bias_up, bias_width;  // as width and the distance of the two matrices, in the bias (width may be rounded up)
+    CUtensorMap map_side;
+    float* column_slots;  // gradient: sums of dZ's columns, [8 (places + parts)][columns]
+    int columns;
 };
 
 #ifdef __CUDACC__
@@ -121,6 +128,6 @@ __device__ __forceinline__ void with_activation(const LayerArgs& a, Call f) {
 size_t layer_split_bytes(const grouped::LayerArgs& a, bool gated);
 void describe_layer_split(grouped::LayerArgs& a, bool gated);  // tiles
 int32_t launch_layer_split(rtma_ctx* ctx, grouped::LayerArgs& a, bool gated, bool gradient, void* planes, int cls, cudaStream_t stream);
-// 16-bit rows: the kernel of one way of loading (grouped_rows.cuh).
-int32_t launch_layer_bf16(rtma_ctx* ctx, grouped::LayerArgs& a, int loading, bool gated, bool gradient, unsigned grid, cudaStream_t stream);
-int32_t launch_layer_f16(rtma_ctx* ctx, grouped::LayerArgs& a, int loading, bool gated, bool gradient, unsigned grid, cudaStream_t stream);
+// 16-bit rows: pairs of blocks with the matrix resident (up to 256 terms) or not; rows on any boundary.
+int32_t launch_layer_bf16(rtma_ctx* ctx, grouped::LayerArgs& a, bool pairs, bool gated, bool gradient, unsigned grid, cudaStream_t stream);
+int32_t launch_layer_f16(rtma_ctx* ctx, grouped::LayerArgs& a, bool pairs, bool gated, bool gradient, unsigned grid, cudaStream_t stream);

@@ -1,6 +1,12 @@
-// Whole layers on rows of bf16 (layer.cu); a file of its own for each type because it takes long to compile.
+// Whole layers (layer.cu) on rows of bf16; a file of its own for each type because it takes long to compile.
 #include "layer_kernels.cuh"
+#include "layer_pairs.cuh"
 
-int32_t launch_layer_bf16(rtma_ctx* ctx, grouped::LayerArgs& a, int loading, bool gated, bool gradient, unsigned grid, cudaStream_t stream) {
-    return launch_of_type<__nv_bfloat16>(ctx, a, loading, gated, gradient, grid, stream);
+RTMA_BOUNDS_TU()
+
+int32_t launch_layer_bf16(rtma_ctx* ctx, LayerArgs& a, bool pairs, bool gated, bool gradient, unsigned grid, cudaStream_t stream) {
+    if (!pairs) return launch_copies<__nv_bfloat16>(ctx, a, gated, gradient, grid, stream);
+    const bool resident = a.d_in <= RESIDENT_TERMS;
+    if (gated) return resident ? launch_pairs<__nv_bfloat16, true, true>(ctx, a, gradient, grid, stream) : launch_pairs<__nv_bfloat16, true, false>(ctx, a, gradient, grid, stream);
+    return resident ? launch_pairs<__nv_bfloat16, false, true>(ctx, a, gradient, grid, stream) : launch_pairs<__nv_bfloat16, false, false>(ctx, a, gradient, grid, stream);
 }

@@ -1,10 +1,8 @@
-// The kernels of whole layers on 16-bit rows (layer.cu), for one type of rows: what the warps that drain the accumulators do.
+// The kernel of whole layers (layer.cu) on 16-bit rows off 16-byte boundaries, or not many of them: what the warps that drain do.
 #pragma once
 
 #include "grouped_rows.cuh"
 #include "layer.cuh"
-
-RTMA_BOUNDS_TU()
 
 namespace {
 
@@ -46,15 +44,14 @@ struct TileAt {
         if (row_tile >= sh.tile_start[a.G]) return false;
         while (row_tile >= sh.tile_start[part + 1]) ++part;  // tiles come in ascending order
         n0 = rest * a.BN;
-        const int64_t inside = (int64_t)(row_tile - sh.tile_start[part]) * (F::PAIRED ? 2 * BM : BM) + (F::PAIRED ? BM * (int)(blockIdx.x & 1) : 0);
+        const int64_t inside = (int64_t)(row_tile - sh.tile_start[part]) * (BM);
         row0 = sh.begin[part] + inside;
         rows = (int)min(sh.rows[part] - inside, (int64_t)BM);
         return true;
     }
     __device__ __forceinline__ bool first(const LayerArgs& a, const Shared& sh) {
-        const int block = blockIdx.x >> F::PAIRED;
-        row_tile = block / a.n_tiles;
-        rest = block - row_tile * a.n_tiles;
+        row_tile = blockIdx.x / a.n_tiles;
+        rest = blockIdx.x - row_tile * a.n_tiles;
         part = 0;
         return at(a, sh);
     }
@@ -71,13 +68,13 @@ struct TileAt {
 
 // What a drain warp does: its rows (a quarter of the tile's) of every SLICES-th 32 columns.  The rows read beside the accumulators are
 // requested 32 columns ahead, from the next tile where these are a tile's last.
-template <class F, bool GRADIENT, int ACT, int BESIDE>
+template <class F, bool GRADIENT>
 __device__ __forceinline__ void drain_layer(const LayerArgs& a, Shared& sh, uint32_t slabs) {
     typedef typename F::T T;
     typedef Outlet<T, F::OUT_SLABS> Out;
     constexpr bool GATED = F::GATED;
-    const int act = ACT >= 0 ? ACT : a.act;
-    const bool beside = BESIDE >= 0 ? BESIDE : GRADIENT || a.side;
+    const int act = a.act;
+    const bool beside = GRADIENT || a.side;
     constexpr int SLICES = F::DRAIN_WARPS / 4, PIECE = 16 / (int)sizeof(T);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, slice = warp >> 2;
     Out outlet{slabs + warp * F::OUT_BYTES};
@@ -119,7 +116,7 @@ __device__ __forceinline__ void drain_layer(const LayerArgs& a, Shared& sh, uint
             slope = __ldg(a.slope + w.part * a.slope_stride);
         }
         float slope_sum = 0.f;
-        if (!wait_for<F::PAIRED>(&sh.acc_full[acc.s], acc.phase, sh, a.error_word)) return;
+        if (!wait_for(&sh.acc_full[acc.s], acc.phase, sh, a.error_word)) return;
         __syncwarp();
         tc::tc_fence_after_sync();
         for (int i = 0; i < mine; ++i) {
@@ -172,75 +169,43 @@ __device__ __forceinline__ void drain_layer(const LayerArgs& a, Shared& sh, uint
         }
         tc::tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) {  // (a pair's warps all report to the first block)
-            if constexpr (F::PAIRED) tc::mbar_arrive_remote(tc::leader_addr(&sh.acc_empty[acc.s]));
-            else tc::mbar_arrive(&sh.acc_empty[acc.s]);
-        }
+        if (lane == 0) tc::mbar_arrive(&sh.acc_empty[acc.s]);
         acc.advance(2);
         if (GRADIENT && act == RTMA_ACT_PRELU && a.slope_slots) {
             for (int o = 16; o > 0; o >>= 1) slope_sum += __shfl_xor_sync(0xffffffffu, slope_sum, o);
-            const int64_t tile = F::PAIRED ? 2 * (int64_t)w.tile(a) + (blockIdx.x & 1) : w.tile(a);
-            if (lane == 0) a.slope_slots[tile * a.slope_warps + warp] = slope_sum;
+            if (lane == 0) a.slope_slots[(int64_t)w.tile(a) * a.slope_warps + warp] = slope_sum;
         }
     }
     outlet.finish(lane);
 }
 
-// Copies leave the registers of a block to fewer warps.
-template <class T, int LOADING, bool GATED>
-using LayerForm = Form<T, FORWARD, LOADING, GATED, LOADING == COPIES ? 8 : 16>;
-
-// The activation as a constant: the eight kinds share a kernel (a switch for every eight results cost a quarter of the time).  Where rows are
-// copied, which has other bounds, it is looked up.
-template <class F, bool GRADIENT>
-__device__ __forceinline__ void layer_body(const LayerArgs& a, Shared& sh) {
-    linear_body<F>(a, sh, [&](uint32_t slabs) {
-        if constexpr (F::LOADING == COPIES) drain_layer<F, GRADIENT, -1, -1>(a, sh, slabs);
-        else with_activation<GRADIENT>(a, [&](auto act, auto beside) { drain_layer<F, GRADIENT, decltype(act)::value, decltype(beside)::value>(a, sh, slabs); });
-    });
-}
-
-template <class T, int LOADING, bool GATED, bool GRADIENT>
-__global__ void __launch_bounds__(LayerForm<T, LOADING, GATED>::THREADS, 1) layer_kernel(const __grid_constant__ LayerArgs a) {
-    __shared__ Shared sh;
-    layer_body<LayerForm<T, LOADING, GATED>, GRADIENT>(a, sh);
-}
 template <class T, bool GATED, bool GRADIENT>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LayerForm<T, PAIR, GATED>::THREADS, 1) layer_pair_kernel(const __grid_constant__ LayerArgs a) {
+__global__ void __launch_bounds__(Form<T, FORWARD, COPIES, GATED>::THREADS, 1) layer_copies_kernel(const __grid_constant__ LayerArgs a) {
+    typedef Form<T, FORWARD, COPIES, GATED> F;
     __shared__ Shared sh;
-    layer_body<LayerForm<T, PAIR, GATED>, GRADIENT>(a, sh);
+    linear_body<F>(a, sh, [&](uint32_t slabs) { drain_layer<F, GRADIENT>(a, sh, slabs); });
 }
 
-template <class T, int LOADING, bool GATED, bool GRADIENT>
-int32_t launch_form(rtma_ctx* ctx, LayerArgs& a, unsigned grid, bool& configured, cudaStream_t stream) {
-    typedef LayerForm<T, LOADING, GATED> F;
-    const int blocks = (int)grid >> F::PAIRED;
-    a.step_rows = blocks / a.n_tiles;
-    a.step_rest = blocks % a.n_tiles;
-    void (*kernel)(LayerArgs);
-    if constexpr (LOADING == PAIR) kernel = layer_pair_kernel<T, GATED, GRADIENT>;
-    else kernel = layer_kernel<T, LOADING, GATED, GRADIENT>;
+template <class T, bool GATED, bool GRADIENT>
+int32_t launch_copies_form(rtma_ctx* ctx, LayerArgs& a, unsigned grid, bool& configured, cudaStream_t stream) {
+    typedef Form<T, FORWARD, COPIES, GATED> F;
+    void (*kernel)(LayerArgs) = layer_copies_kernel<T, GATED, GRADIENT>;
     if (!configured) {
         RTMA_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, F::DYNAMIC_BYTES));
         configured = true;
     }
+    a.step_rows = (int)grid / a.n_tiles;
+    a.step_rest = (int)grid % a.n_tiles;
     launch_kernel(kernel, grid, F::THREADS, F::DYNAMIC_BYTES, stream, a);
     RTMA_LAUNCH_CHECK(ctx);
     return RTMA_OK;
 }
 
-template <class T, int LOADING>
-int32_t launch_kind(rtma_ctx* ctx, LayerArgs& a, bool gated, bool gradient, unsigned grid, cudaStream_t stream) {
-    bool* once = ctx->layer_configured + ((std::is_same<T, __half>::value ? 1 : 0) * 3 + LOADING) * 4;
-    if (gated) return gradient ? launch_form<T, LOADING, true, true>(ctx, a, grid, once[3], stream) : launch_form<T, LOADING, true, false>(ctx, a, grid, once[2], stream);
-    return gradient ? launch_form<T, LOADING, false, true>(ctx, a, grid, once[1], stream) : launch_form<T, LOADING, false, false>(ctx, a, grid, once[0], stream);
-}
-
 template <class T>
-int32_t launch_of_type(rtma_ctx* ctx, LayerArgs& a, int loading, bool gated, bool gradient, unsigned grid, cudaStream_t stream) {
-    return loading == PAIR ? launch_kind<T, PAIR>(ctx, a, gated, gradient, grid, stream)
-           : loading == BULK ? launch_kind<T, BULK>(ctx, a, gated, gradient, grid, stream)
-                             : launch_kind<T, COPIES>(ctx, a, gated, gradient, grid, stream);
+int32_t launch_copies(rtma_ctx* ctx, LayerArgs& a, bool gated, bool gradient, unsigned grid, cudaStream_t stream) {
+    bool* once = ctx->layer_configured + 16 + (std::is_same<T, __half>::value ? 4 : 0);
+    if (gated) return gradient ? launch_copies_form<T, true, true>(ctx, a, grid, once[3], stream) : launch_copies_form<T, true, false>(ctx, a, grid, once[2], stream);
+    return gradient ? launch_copies_form<T, false, true>(ctx, a, grid, once[1], stream) : launch_copies_form<T, false, false>(ctx, a, grid, once[0], stream);
 }
 
 }  // namespace
