@@ -271,8 +271,10 @@ extern "C" int32_t rtma_grouped_layer_grad(rtma_ctx* ctx, const rtma_layer_desc*
     }
     // all scratch at once: inside a capture nothing is enqueued unless everything fits
     if (dX) RTMA_TRY(grouped_rows(ctx, who, true, d->dtype, n, G, offsets, d->d_in, wide, dz, ldz, W, d->w_stride, nullptr, 0, dX, lddx, &rows_bytes, stream));
+    const bool by_pairs = d->dtype != RTMA_F32 && row_granule(X, ldx, es) >= 16 && row_granule(dz, ldz, es) >= 16;
+    auto weights = by_pairs ? layer_dw : grouped_dw;
     if (dW)
-        RTMA_TRY(grouped_dw(ctx, who, d->dtype, n, G, offsets, d->d_in, wide, X, ldx, dz, ldz, d->grad_dtype, dW, dw_stride, sums ? nullptr : db, db_stride, &dw_bytes, stream));
+        RTMA_TRY(weights(ctx, who, d->dtype, n, G, offsets, d->d_in, wide, X, ldx, dz, ldz, d->grad_dtype, dW, dw_stride, sums ? nullptr : db, db_stride, &dw_bytes, stream));
     RTMA_TRY(prepare_row_call(ctx, std::max(plain ? 0 : matrices + slots, std::max(rows_bytes, dw_bytes)), stream));
     if (!plain && n > 0) {
         a.out = dZ; a.ldo = lddz;
@@ -305,6 +307,6 @@ extern "C" int32_t rtma_grouped_layer_grad(rtma_ctx* ctx, const rtma_layer_desc*
         RTMA_LAUNCH_CHECK(ctx);
     }
     if (dX) RTMA_TRY(grouped_rows(ctx, who, true, d->dtype, n, G, offsets, d->d_in, wide, dz, ldz, W, d->w_stride, nullptr, 0, dX, lddx, nullptr, stream));
-    if (dW) RTMA_TRY(grouped_dw(ctx, who, d->dtype, n, G, offsets, d->d_in, wide, X, ldx, dz, ldz, d->grad_dtype, dW, dw_stride, sums ? nullptr : db, db_stride, nullptr, stream));
+    if (dW) RTMA_TRY(weights(ctx, who, d->dtype, n, G, offsets, d->d_in, wide, X, ldx, dz, ldz, d->grad_dtype, dW, dw_stride, sums ? nullptr : db, db_stride, nullptr, stream));
     return RTMA_OK;
 }

@@ -131,3 +131,6 @@ int32_t launch_layer_split(rtma_ctx* ctx, grouped::LayerArgs& a, bool gated, boo
 // 16-bit rows: pairs of blocks with the matrix resident (up to 256 terms) or not; rows on any boundary.
 int32_t launch_layer_bf16(rtma_ctx* ctx, grouped::LayerArgs& a, bool pairs, bool gated, bool gradient, unsigned grid, cudaStream_t stream);
 int32_t launch_layer_f16(rtma_ctx* ctx, grouped::LayerArgs& a, bool pairs, bool gated, bool gradient, unsigned grid, cudaStream_t stream);
+// The weight gradient of 16-bit rows on 16-byte boundaries (layer_wgrad.cu); as grouped_dw.
+int32_t layer_dw(rtma_ctx* ctx, const char* who, int32_t dtype, int64_t n, int32_t G, const int64_t* offsets, int32_t d_in, int32_t d_out, const void* X, int64_t ldx,
+                 const void* dZ, int64_t lddz, int32_t out_dtype, void* dW, int64_t dw_stride, void* db, int64_t db_stride, size_t* scratch, cudaStream_t stream);

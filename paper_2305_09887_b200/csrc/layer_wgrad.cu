@@ -1,0 +1,426 @@
+// The weight gradient of a layer (layer.cu) over 16-bit rows on 16-byte boundaries: dW_g = X_g^T dZ_g, db_g = the column sums of dZ_g.
+//
+// Pairs of blocks (MMAs of 256 x up to 256 over 64 rows a stage); rows run across both operands, so that both come as they lie.  The wider
+// of X and dZ is the left operand (256 of its columns a tile), the other one's up to 256 columns the right one, whichever wastes less.  The
+// parts' rows are cut into chunks as in grouped_linear.cu, one slot of fp32 sums for each, added up by a second kernel.
+//
+// The tensor cores truncate when they accumulate: sixteen warps take the accumulator after every 128 rows and add it up in registers, rounded to
+// nearest, 64 columns of a row in a lane (16 warps, not 8, because of these sums).  The column sums of dZ are taken from a stage that the
+// MMAs are done with, by two warps with mma.sync against ones; as a product of 128 x 128 tiles with ones, as in grouped_linear.cu, they cost as many MMAs as
+// the weights' do.
+#include <algorithm>
+
+#include "grouped_rows.cuh"
+#include "layer.cuh"
+
+RTMA_BOUNDS_TU()
+
+namespace {
+
+using namespace grouped;
+
+constexpr int LEFT = 256, STAGES = 6, STAGE_BYTES = 2 * 128 * 128, DRAIN_WARPS = 16, THREADS = 32 * (DRAIN_WARPS + 4);
+constexpr int DYNAMIC_BYTES = 1024 + STAGES * STAGE_BYTES;
+constexpr int ACC_STAGES = 2;  // of 64 rows, after which the accumulator is taken
+constexpr int DW_WAVES = 2;    // tiles for every pair that runs at a time
+constexpr int SUMS_REGISTERS = 104, OTHER_REGISTERS = 64;  // 512 x 104 + 128 x 64 = 640 x 96
+
+struct GradArgs : LinearArgs {  // A, map_a: the left operand, B, map_b: the right one
+    int left, right;   // their widths
+    bool swapped;      // dZ is the left one
+    int half;          // columns of the right one that a block brings
+    bool sums;         // of dZ's columns are wanted
+    float* slots;      // [row tile][d_in + 1][ldo]
+};
+
+struct GradShared : Shared {
+    uint64_t free[STAGES];  // stages whose columns have been summed
+};
+
+struct GradWalk {
+    int tile, row_tile, part, m0, n0, k_end, k0;
+    int64_t row0;
+    __device__ __forceinline__ bool at(const GradArgs& a, const GradShared& sh) {
+        const int per = a.m_tiles * a.n_tiles;
+        row_tile = tile / per;
+        if (row_tile >= sh.tile_start[a.G]) return false;
+        const int rest = tile - row_tile * per;
+        m0 = rest / a.n_tiles;
+        n0 = (rest - m0 * a.n_tiles) * 2 * a.half;
+        m0 *= LEFT;
+        while (row_tile >= sh.tile_start[part + 1]) ++part;  // tiles come in ascending order
+        const int64_t inside = (int64_t)(row_tile - sh.tile_start[part]) * sh.tile_rows;
+        row0 = sh.begin[part] + inside;
+        k_end = (int)min((int64_t)sh.rows[part] - inside, (int64_t)sh.tile_rows);
+        k0 = 0;
+        return true;
+    }
+    __device__ __forceinline__ bool first(const GradArgs& a, const GradShared& sh) {
+        tile = blockIdx.x >> 1;
+        part = 0;
+        return at(a, sh);
+    }
+    __device__ __forceinline__ bool next_tile(const GradArgs& a, const GradShared& sh) {
+        tile += gridDim.x >> 1;
+        return at(a, sh);
+    }
+    __device__ __forceinline__ bool last_stage() const { return k0 + BK >= k_end; }
+    __device__ __forceinline__ bool next(const GradArgs& a, const GradShared& sh) {  // the next stage
+        if (!last_stage()) {
+            k0 += BK;
+            return true;
+        }
+        return next_tile(a, sh);
+    }
+    // whether this tile's block sums columns of dZ: once for each, in the first tile of X's columns
+    __device__ __forceinline__ bool sums(const GradArgs& a) const { return a.sums && (a.swapped ? n0 : m0) == 0; }
+};
+
+// One warp.  Rows behind the end of a chunk belong to another part: the last stage's rows are copied by the lanes, with zeros behind them.
+template <class T>
+__device__ __forceinline__ void grad_producer(const GradArgs& a, GradShared& sh, uint8_t* ring, int rank, int lane) {
+    if (lane == 0) {
+        tc::prefetch_tensormap(&a.map_a);
+        tc::prefetch_tensormap(&a.map_b);
+    }
+    const int atoms = (a.half + 63) / 64;
+    GradWalk w;
+    tc::RingAt at;
+    int filled = 0;  // stages, STAGES at most
+    bool ok = true;
+    for (bool more = w.first(a, sh); more; more = w.next(a, sh), at.advance(STAGES)) {
+        uint64_t* released = a.sums ? &sh.free[at.s] : &sh.empty[at.s];
+        if (!wait_for<true>(released, at.phase ^ 1u, sh, a.error_word)) {
+            ok = false;
+            break;
+        }
+        filled = min(filled + 1, STAGES);
+        uint8_t* stage = ring + at.s * STAGE_BYTES;
+        const uint32_t bar = tc::leader_addr(&sh.full[at.s]);
+        const int m = w.m0 + 128 * rank, n = w.n0 + a.half * rank;
+        if (w.k0 + BK > w.k_end) {
+            const T *A = static_cast<const T*>(a.A), *B = static_cast<const T*>(a.B);
+            for (int j = lane; j < (2 + atoms) * 512; j += 32) {
+                const int atom = j >> 9, row = j >> 3 & 63, unit = j & 7, k = w.k0 + row;
+                const bool is_left = atom < 2;
+                const int c = is_left ? m + 64 * atom + 8 * unit : n + 64 * (atom - 2) + 8 * unit, width = is_left ? a.left : a.right;
+                const int valid = k < w.k_end ? max(0, min(8, width - c)) : 0;
+                const T* p = is_left ? A : B;
+                if (valid) p += (w.row0 + k) * (is_left ? a.lda : a.ldb) + c;
+                copy<16>(tc::smem_u32(stage) + atom * 2 * SLAB_BYTES + row * 128 + ((unit ^ (row & 7)) << 4), p, valid * (int)sizeof(T));
+            }
+            copies_done();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive_cluster(bar);
+        } else if (lane == 0) {
+            if (rank == 0) tc::mbar_arrive_expect_tx(&sh.full[at.s], 2 * (2 + atoms) * 2 * SLAB_BYTES);
+            else tc::mbar_arrive_remote(bar);
+            for (int i = 0; i < 2; ++i) tc::tma_load_3d_pair(stage + i * 2 * SLAB_BYTES, &a.map_a, bar, m + 64 * i, (int)w.row0 + w.k0, 0);
+            for (int i = 0; i < atoms; ++i) tc::tma_load_3d_pair(stage + (2 + i) * 2 * SLAB_BYTES, &a.map_b, bar, n + 64 * i, (int)w.row0 + w.k0, 0);
+        }
+        __syncwarp();
+    }
+    // No signal stays under way (see the pairs of grouped_rows.cuh).
+    for (int i = 0; i < filled; ++i) {
+        const int back = filled - i, s = (at.s - back + STAGES) % STAGES;
+        const uint32_t parity = s < at.s ? at.phase : at.phase ^ 1u;
+        if (!ok || !wait_for<true>(a.sums ? &sh.free[s] : &sh.empty[s], parity, sh, a.error_word)) {
+            ok = false;
+            if (rank == 0)
+                for (uint32_t k = 0; k < (1u << 14) && !tc::mbar_try_wait_cluster(&sh.full[s], parity); ++k) {}
+        }
+    }
+}
+
+template <class T>
+__device__ __forceinline__ void grad_multiplier(const GradArgs& a, GradShared& sh, uint32_t ring) {
+    const uint32_t format = std::is_same<T, __half>::value ? 0u : 1u;  // fp16 or bf16 operands, fp32 sums
+    const uint32_t idesc = (1u << 4) | (format << 7) | (format << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(2 * a.half >> 3) << 17) | ((uint32_t)(LEFT >> 4) << 24);
+    const uint64_t desc = tc::smem_desc_sw128(0, 2 * SLAB_BYTES, 1024);  // atoms of 64 columns lie two slabs apart
+    GradWalk w;
+    tc::RingAt at, acc;
+    int held = 0;  // stages in the accumulator
+    for (bool more = w.first(a, sh); more; more = w.next(a, sh)) {
+        if (held == 0 && !wait_for<true>(&sh.acc_empty[acc.s], acc.phase ^ 1u, sh, a.error_word)) return;
+        if (!wait_for<true>(&sh.full[at.s], at.phase, sh, a.error_word)) return;
+        tc::tc_fence_after_sync();
+        __syncwarp();
+        const uint32_t d = sh.tmem_base + acc.s * 256, stage = ring + at.s * STAGE_BYTES;
+        const uint64_t da = desc + (stage >> 4), db = da + (4 * SLAB_BYTES >> 4);
+        const int steps = (min(BK, w.k_end - w.k0) + 15) >> 4;
+#pragma unroll
+        for (int k = 0; k < BK / 16; ++k)
+            if (k < steps) tc::mma_pair_by_warp(d, da + 128 * k, db + 128 * k, idesc, k || held ? 1u : 0u);
+        tc::commit_pair_by_warp(&sh.empty[at.s]);
+        at.advance(STAGES);
+        if (++held == ACC_STAGES || w.last_stage()) {
+            held = 0;
+            tc::commit_pair_by_warp(&sh.acc_full[acc.s]);
+            acc.advance(2);
+        }
+    }
+}
+
+// Two warps: the column sums of dZ, 64 columns each (which: the first or the second), of each stage that the MMAs have read.
+template <class T>
+__device__ __forceinline__ void grad_sums(const GradArgs& a, GradShared& sh, uint32_t ring, int rank, int which, int lane) {
+    const uint32_t one = std::is_same<T, __half>::value ? 0x3C003C00u : 0x3F803F80u;
+    const int columns = (a.swapped ? 128 : a.half) - 64 * which;  // of dZ in this block
+    GradWalk w;
+    tc::RingAt at;
+    float c[4][4];  // c[m][0]: column 16 m + lane / 4, c[m][2]: the one 8 behind it
+    auto clear = [&]() {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) c[i >> 2][i & 3] = 0.f;
+    };
+    clear();
+    for (bool more = w.first(a, sh); more; more = w.next(a, sh)) {
+        if (!wait_for<true>(&sh.empty[at.s], at.phase, sh, a.error_word)) return;
+        __syncwarp();
+        if (w.sums(a)) {
+            const uint32_t from = ring + at.s * STAGE_BYTES + (a.swapped ? 0 : 4 * SLAB_BYTES) + which * 2 * SLAB_BYTES;
+            const int steps = (min(BK, w.k_end - w.k0) + 15) >> 4;
+            for (int k = 0; k < steps; ++k) {
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    if (16 * m >= columns) break;
+                    // four 8 x 8 blocks: columns 16 m .. + 7 and + 8 .. + 15 of rows 16 k .. + 7, then of rows + 8 .. + 15
+                    const int row = 16 * k + 8 * (lane >> 4) + (lane & 7), unit = 2 * m + (lane >> 3 & 1);
+                    uint32_t x[4];
+                    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                                 : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3])
+                                 : "r"(from + row * 128 + ((unit ^ (row & 7)) << 4))
+                                 : "memory");
+                    if constexpr (std::is_same<T, __half>::value)
+                        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %8}, {%0, %1, %2, %3};"
+                                     : "+f"(c[m][0]), "+f"(c[m][1]), "+f"(c[m][2]), "+f"(c[m][3])
+                                     : "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(one));
+                    else
+                        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %8}, {%0, %1, %2, %3};"
+                                     : "+f"(c[m][0]), "+f"(c[m][1]), "+f"(c[m][2]), "+f"(c[m][3])
+                                     : "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(one));
+                }
+            }
+        }
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&sh.free[at.s]);
+        at.advance(STAGES);
+        if (w.last_stage() && w.sums(a)) {
+            const int first = (a.swapped ? w.m0 + 128 * rank : w.n0 + a.half * rank) + 64 * which;
+            float* to = a.slots + ((int64_t)w.row_tile * (a.d_in + 1) + a.d_in) * a.ldo;
+            if ((lane & 3) == 0) {
+#pragma unroll
+                for (int m = 0; m < 4; ++m)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int j = 16 * m + 8 * h + (lane >> 2);
+                        if (j < columns && first + j < a.d_out) to[first + j] = c[m][2 * h];
+                    }
+            }
+            clear();
+        }
+    }
+}
+
+__device__ __forceinline__ void grad_drain(const GradArgs& a, GradShared& sh, int rank) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, slice = warp >> 2;
+    const uint32_t tmem = sh.tmem_base + ((uint32_t)(32 * quarter) << 16) + 64 * slice;
+    const bool mine = 64 * slice < 2 * a.half;
+    GradWalk w;
+    tc::RingAt acc;
+    for (bool more = w.first(a, sh); more; more = w.next_tile(a, sh)) {
+        f2 total[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) total[j] = pack2(0.f, 0.f);
+        for (int k0 = 0; k0 < w.k_end; k0 += ACC_STAGES * BK) {
+            if (!wait_for<true>(&sh.acc_full[acc.s], acc.phase, sh, a.error_word)) return;
+            __syncwarp();
+            tc::tc_fence_after_sync();
+            if (mine) {
+                const uint32_t from = tmem + acc.s * 256;
+                uint32_t x[2][8];
+                tc::tmem_load_issue_8(from, x[0]);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    tc::tmem_load_wait_8(x[q & 1]);
+                    if (q < 7) tc::tmem_load_issue_8(from + 8 * (q + 1), x[(q + 1) & 1]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) total[4 * q + j] = add2(total[4 * q + j], pack2(__uint_as_float(x[q & 1][2 * j]), __uint_as_float(x[q & 1][2 * j + 1])));
+                }
+            }
+            tc::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive_remote(tc::leader_addr(&sh.acc_empty[acc.s]));  // (a pair's warps all report to the first block)
+            acc.advance(2);
+        }
+        const int m = w.m0 + 128 * rank + 32 * quarter + lane, n = w.n0 + 64 * slice;
+        const int cols = min(64, min(2 * a.half - 64 * slice, a.right - n));
+        if (m < a.left && cols > 0) {
+            float* const slot = a.slots + (int64_t)w.row_tile * (a.d_in + 1) * a.ldo;
+            if (a.swapped) {  // a lane's column of dZ: neighbours beside one another
+                float* to = slot + (int64_t)n * a.ldo + m;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    float x, y;
+                    unpack2(total[j], x, y);
+                    if (2 * j < cols) to[0] = x;
+                    if (2 * j + 1 < cols) to[a.ldo] = y;
+                    to += 2 * a.ldo;
+                }
+            } else {  // a lane's row of dW (the slots' rows are padded to 32 bytes)
+                float* to = slot + (int64_t)m * a.ldo + n;
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    float v[8];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) unpack2(total[4 * q + j], v[2 * j], v[2 * j + 1]);
+                    if (8 * q < cols)
+                        asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to + 8 * q), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]),
+                                     "f"(v[6]), "f"(v[7])
+                                     : "memory");
+                }
+            }
+        }
+    }
+}
+
+template <class T>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) layer_wgrad_kernel(const __grid_constant__ GradArgs a) {
+    static_assert(DYNAMIC_BYTES + sizeof(GradShared) <= SMEM_MOST && STAGES <= MAX_STAGES, "shared memory of a block");
+    extern __shared__ uint8_t raw[];
+    __shared__ GradShared sh;
+    uint8_t* const ring_bytes = raw + ((1024u - (tc::smem_u32(raw) & 1023u)) & 1023u);
+    const uint32_t ring = tc::smem_u32(ring_bytes);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) {
+            tc::mbar_init(&sh.full[s], 2);  // both blocks'
+            tc::mbar_init(&sh.empty[s], 1);
+            tc::mbar_init(&sh.free[s], 2);
+        }
+        for (int b = 0; b < 2; ++b) {
+            tc::mbar_init(&sh.acc_full[b], 1);
+            tc::mbar_init(&sh.acc_empty[b], 2 * DRAIN_WARPS);
+        }
+        sh.abort = 0;
+        tc::fence_barrier_init();
+    }
+    if (warp == DRAIN_WARPS) {
+        tc::tmem_alloc_pair(&sh.tmem_base, 512);
+        tc::tmem_relinquish_pair();
+    }
+    wait_for_kernel_before();
+    lay_out<WEIGHT_GRADIENT, THREADS, BK>(a, sh);
+    tc::tc_fence_before_sync();
+    __syncthreads();
+    tc::cluster_sync();  // both blocks' barriers and tensor memory exist before either is signalled
+    tc::tc_fence_after_sync();
+    const int rank = (int)tc::cluster_rank();
+    if (warp < DRAIN_WARPS) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SUMS_REGISTERS));
+        grad_drain(a, sh, rank);
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGISTERS));
+        if (warp == DRAIN_WARPS && rank == 0) grad_multiplier<T>(a, sh, ring);
+        if (warp == DRAIN_WARPS + 1) grad_producer<T>(a, sh, ring_bytes, rank, lane);
+        if (warp >= DRAIN_WARPS + 2 && a.sums) grad_sums<T>(a, sh, ring, rank, warp - DRAIN_WARPS - 2, lane);
+    }
+    __syncwarp();
+    if (*reinterpret_cast<volatile int*>(&sh.abort)) __nanosleep(1000000);  // a wait ran out: copies and MMAs under way land before the block ends
+    tc::tc_fence_before_sync();
+    __syncthreads();
+    tc::cluster_sync();  // neither block leaves while the other may still signal it or read its operands
+    if (warp == DRAIN_WARPS) {
+        tc::tc_fence_after_sync();
+        tc::tmem_dealloc_pair(sh.tmem_base, 512);
+    }
+}
+
+// The slots of every part added up in order, four neighbouring values a thread; blocks take many, because each has to number the tiles first (a block
+// for every 128 values took 105 us for 16 parts of 256 x 1,024).
+template <class O>
+__global__ void __launch_bounds__(256) layer_wgrad_reduce_kernel(const __grid_constant__ GradArgs a) {
+    __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
+    wait_for_kernel_before();
+    number_tiles(a.offsets, a.n, a.G, a.n ? *a.chunk_rows : 1, a.tiles, tile_start, warp_sums, a.span);
+    const int part = blockIdx.y, from = tile_start[part], count = tile_start[part + 1] - from, quads = (int)a.ldo / 4;
+    const int64_t slot = (a.d_in + 1) * a.ldo, all = (int64_t)(a.d_in + (a.sums ? 1 : 0)) * quads;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int row = (int)(i / quads), col = 4 * (int)(i - (int64_t)row * quads);
+        const float* p = a.slots + from * slot + 4 * i;
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int t = 0; t < count; ++t, p += slot) {
+            const float4 v = *reinterpret_cast<const float4*>(p);
+            s.x += v.x;
+            s.y += v.y;
+            s.z += v.z;
+            s.w += v.w;
+        }
+        O* to = (row < a.d_in ? static_cast<O*>(a.dW) + part * a.dw_stride + (int64_t)row * a.d_out : static_cast<O*>(a.db) + part * a.db_stride) + col;
+        if (col < a.d_out) to[0] = from_f32<O>(s.x);
+        if (col + 1 < a.d_out) to[1] = from_f32<O>(s.y);
+        if (col + 2 < a.d_out) to[2] = from_f32<O>(s.z);
+        if (col + 3 < a.d_out) to[3] = from_f32<O>(s.w);
+    }
+}
+
+}  // namespace
+
+int32_t layer_dw(rtma_ctx* ctx, const char* who, int32_t dtype, int64_t n, int32_t G, const int64_t* offsets, int32_t d_in, int32_t d_out, const void* X, int64_t ldx,
+                 const void* dZ, int64_t lddz, int32_t out_dtype, void* dW, int64_t dw_stride, void* db, int64_t db_stride, size_t* scratch, cudaStream_t stream) {
+    const int64_t weights = (int64_t)d_in * d_out;
+    const bool shared = G > 1 && dw_stride == 0, bf16 = dtype == RTMA_BF16;
+    if (G > 1 && !shared && dw_stride < weights && dw_stride > -weights) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: gradients of the parts overlap", who);
+    GradArgs a{};
+    a.error_word = ctx->error_word;
+    a.offsets = offsets; a.n = n;
+    a.G = shared ? 1 : G;
+    a.span = shared ? G : 1;
+    a.d_in = d_in; a.d_out = d_out;
+    // MMAs of either orientation, in columns of the right operand
+    const int64_t as_left = ceil_div(d_in, LEFT) * ceil_div(d_out, 32), swapped = ceil_div(d_out, LEFT) * ceil_div(d_in, 32);
+    a.swapped = swapped <= as_left;
+    a.left = a.swapped ? d_out : d_in; a.right = a.swapped ? d_in : d_out;
+    a.A = a.swapped ? dZ : X; a.lda = a.swapped ? lddz : ldx;
+    a.B = a.swapped ? X : dZ; a.ldb = a.swapped ? ldx : lddz;
+    a.m_tiles = (int)ceil_div(a.left, LEFT);
+    a.n_tiles = (int)ceil_div(a.right, 256);
+    a.half = (int)ceil_div(ceil_div(a.right, a.n_tiles), 32) * 16;
+    a.n_tiles = (int)ceil_div(a.right, 2 * a.half);
+    const int pairs = ctx->sm_count / 2;
+    a.tile_rows = 256;
+    a.tiles = std::min(std::max<int64_t>(a.G, (int64_t)DW_WAVES * pairs / ((int64_t)a.m_tiles * a.n_tiles)), n / a.tile_rows + a.G);
+    a.ldo = ceil_div(d_out, 8) * 8;
+    a.dW = dW; a.dw_stride = dw_stride; a.db = db; a.db_stride = db_stride;
+    a.sums = db != nullptr;
+    const size_t bytes = 256 + sizeof(float) * (size_t)a.tiles * (d_in + 1) * a.ldo;
+    if (scratch) {
+        *scratch = bytes;
+        return RTMA_OK;
+    }
+    RTMA_TRY(prepare_row_call(ctx, bytes, stream));
+    a.chunk_rows = reinterpret_cast<int32_t*>(ctx->arena);
+    a.slots = reinterpret_cast<float*>(ctx->arena + 256);
+    if (n > 0) {
+        const int64_t tiles = a.tiles * a.m_tiles * a.n_tiles;
+        if (tiles >= (int64_t(1) << 30)) return rtma_fail(ctx, RTMA_ERR_OVERFLOW, "%s: %lld tiles", who, (long long)tiles);
+        if (!make_tensor_map_16bit(&a.map_a, bf16, a.A, 1, n, a.left, a.lda, n * a.lda, BK) || !make_tensor_map_16bit(&a.map_b, bf16, a.B, 1, n, a.right, a.ldb, n * a.ldb, BK))
+            return rtma_fail(ctx, RTMA_ERR_CUDA, "%s: no tensor map for rows of %d and %d values", who, d_in, d_out);
+        void (*kernel)(GradArgs) = bf16 ? layer_wgrad_kernel<__nv_bfloat16> : layer_wgrad_kernel<__half>;
+        bool& configured = ctx->layer_configured[bf16 ? 32 : 33];
+        if (!configured) {
+            RTMA_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, DYNAMIC_BYTES));
+            configured = true;
+        }
+        KernelScope ks(ctx, KC_GEMM_WGRAD, stream);
+        launch_kernel(kernel, (unsigned)(2 * std::min<int64_t>(tiles, pairs)), THREADS, DYNAMIC_BYTES, stream, a);
+        RTMA_LAUNCH_CHECK(ctx);
+    }
+    KernelScope ks(ctx, KC_REDUCE_SGD, stream);
+    void (*reduce)(GradArgs) = out_dtype == RTMA_F32 ? layer_wgrad_reduce_kernel<float> : bf16 ? layer_wgrad_reduce_kernel<__nv_bfloat16> : layer_wgrad_reduce_kernel<__half>;
+    const int64_t blocks = ceil_div((int64_t)(d_in + 1) * a.ldo / 4, 256);
+    launch_kernel(reduce, dim3((unsigned)std::min<int64_t>(blocks, std::max(1, 8 * ctx->sm_count / a.G)), (unsigned)a.G), 256, 0, stream, a);
+    RTMA_LAUNCH_CHECK(ctx);
+    return RTMA_OK;
+}
