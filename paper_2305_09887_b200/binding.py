@@ -708,9 +708,10 @@ class Context:
         n, d_in = X.shape
         G, wide = args[2], W.shape[-1]
         g, ldg = self._rows(dY, "dY", X.dtype, (n, d_out))
+        columns = (2 if gated else 1) * (d_out if X.dtype == torch.float32 else (d_out + 7) // 8 * 8)
         if dz is None and (gated or act != "none"):
-            dz = self._empty((n, wide), X.dtype, stream)
-        z, ldz = (None, 0) if dz is None else self._rows(dz, "dz", X.dtype, (n, wide))
+            dz = self._empty((n, columns), X.dtype, stream)
+        z, ldz = (None, 0) if dz is None else self._rows(dz, "dz", X.dtype, (n, columns))
         if need_dx and out is None:
             out = self._empty((n, d_in), X.dtype, stream)
         x, ldx = (None, 0) if out is None else self._rows(out, "out", X.dtype, (n, d_in))
@@ -742,7 +743,8 @@ class Context:
         front of the activation is worked out again.  dW and db have the parameters' shape (summed over the parts for shared ones) and
         grad_dtype: the rows' type, or float32; dslope float32.  None for a parameter that is None, and for what is not wanted
         (need_dx, need_dw).  dz [n, d_out]: where the gradient in front of the activation is put, rounded to the rows' type, as
-        the operand of the two products (it may be dY; a new one otherwise; act "none" has none)."""
+        the operand of the two products (a new one otherwise; act "none" has none); of 16-bit rows on 16-byte boundaries and with d_out
+        rounded up to a multiple of 8, zeros behind; it may be dY where nothing is rounded up."""
         return self._gradient(X, dY, offsets, W, bias, act, slope, need_dx, need_dw, grad_dtype, out, dz, dw, db, dslope, stream, False)
 
     def grouped_gated_linear(self, X, offsets, W, bias=None, act="silu", slope=None, residual=None, out=None, stream=None):
@@ -754,7 +756,7 @@ class Context:
     def grouped_gated_linear_grad(self, X, dH, offsets, W, bias=None, act="silu", slope=None, need_dx=True, need_dw=True, grad_dtype=None, out=None,
                                   dz=None, dw=None, db=None, dslope=None, stream=None):
         """(dX, dW, db, dslope) of grouped_gated_linear from its inputs and dH; both products are worked out again.  dz [n, 2 f]: as in
-        grouped_linear_act_grad, the gradients of both, side by side."""
+        grouped_linear_act_grad, the gradients of both side by side (each rounded up to a multiple of 8 columns)."""
         return self._gradient(X, dH, offsets, W, bias, act, slope, need_dx, need_dw, grad_dtype, out, dz, dw, db, dslope, stream, True)
 
     def _share(self, t, parts, name):

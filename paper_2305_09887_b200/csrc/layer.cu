@@ -10,7 +10,7 @@
 // the warps that drain it.  A tile of a gated layer has the same columns of both matrices, so that a lane finds both factors of a result in its own
 // row.  dZ is rounded to the rows' type: it is an operand of 16-bit products.
 //
-// This file: the calls.  The kernels of 16-bit rows are in layer_kernels.cuh, those of fp32 rows in layer_split.cu.
+// This file: the calls.  Those of 16-bit rows are in layer_pairs.cuh and layer_wgrad.cu, those of fp32 rows in layer_split.cu.
 #include <algorithm>
 
 #include "layer.cuh"
@@ -21,20 +21,79 @@ namespace {
 
 using namespace grouped;
 
-constexpr int BM = 128, BK = 64;  // of the kernels on 16-bit rows
+constexpr int PAIR_ROWS = 256;  // of a tile of the kernels on 16-bit rows
 
-// 16-bit matrices -> [part][d_in][halves * up] on 16-byte boundaries, up: width rounded up to 8
-__global__ void __launch_bounds__(256) lay_out_matrices_kernel(const __half* __restrict__ W, int64_t w_stride, int parts, int d_in, int width, int halves, int granule,
-                                                               __half* __restrict__ out) {
+// 16-bit rows on any boundary -> rows on 16-byte ones, zeros behind each up to a multiple of 8 values.  Row r lies at src + (r / group) *
+// group_stride + (r % group) * ld.
+struct AlignJob {
+    const uint16_t* src;
+    uint16_t* dst;
+    int64_t rows, group, group_stride, ld;
+    int d, granule;
+};
+struct AlignArgs {
+    AlignJob job[3];
+};
+constexpr int ALIGN_BYTES = 16384;
+
+// A block brings neighbouring rows as the 16-byte words that they lie in, and cuts them up in shared memory.  Memory's time (200,000 x 100: 15 us), where
+// the products' own copies of such rows, for every tile of columns again, cost more than the products (200,000 x 100 -> 2 x 266 in fp16: 222 us).
+__global__ void __launch_bounds__(256) align_rows_kernel(const __grid_constant__ AlignArgs args) {
+    __shared__ uint4 words[ALIGN_BYTES / 16 + 2];
     wait_for_kernel_before();
-    const int units = (width + 7) / 8;
-    const int64_t total = (int64_t)parts * d_in * halves * units;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t run = i / units, row = run / halves, part = row / d_in;  // run: a row of one matrix
-        const int u = (int)(i - run * units), h = (int)(run - row * halves);
-        Eight<__half> x;
-        x.load(W + part * w_stride + ((row - part * d_in) * halves + h) * width + 8 * u, min(8, width - 8 * u), granule);
-        *reinterpret_cast<uint4*>(out + 8 * i) = x.w[0];
+    const AlignJob& a = args.job[blockIdx.y];
+    if (!a.rows) return;
+    const int units = (a.d + 7) / 8;
+    const int together = a.ld <= 2 * (int64_t)a.d && a.ld * 2 <= ALIGN_BYTES ? (int)min(a.group, ALIGN_BYTES / (a.ld * 2)) : 0;  // rows at a time
+    if (!together) {
+        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.rows * units; i += (int64_t)gridDim.x * 256) {
+            const int64_t row = i / units, part = row / a.group;
+            const int u = (int)(i - row * units);
+            Eight<__half> x;
+            x.load(reinterpret_cast<const __half*>(a.src) + part * a.group_stride + (row - part * a.group) * a.ld + 8 * u, min(8, a.d - 8 * u), a.granule);
+            *reinterpret_cast<uint4*>(a.dst + 8 * i) = x.w[0];
+        }
+        return;
+    }
+    const int64_t per_group = (a.group + together - 1) / together, all = a.rows / a.group * per_group;
+    for (int64_t c = blockIdx.x; c < all; c += gridDim.x) {
+        const int64_t part = c / per_group, row0 = (c - part * per_group) * together;
+        const int rows = (int)min((int64_t)together, a.group - row0);
+        const uintptr_t from = reinterpret_cast<uintptr_t>(a.src + part * a.group_stride + row0 * a.ld), to = from + 2 * ((rows - 1) * a.ld + a.d), base = from & ~(uintptr_t)15;
+        const int count = (int)((to - base + 15) / 16);
+        for (int i = threadIdx.x; i < count; i += 256) {
+            const uintptr_t p = base + 16 * (uintptr_t)i;
+            uint4 x;
+            if (p >= from && p + 16 <= to) {
+                x = *reinterpret_cast<const uint4*>(p);
+            } else {
+                uint32_t w[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uintptr_t e = p + 4 * k;
+                    const uint32_t lo = e >= from && e < to ? *reinterpret_cast<const uint16_t*>(e) : 0u, hi = e + 2 >= from && e + 2 < to ? *reinterpret_cast<const uint16_t*>(e + 2) : 0u;
+                    w[k] = lo | hi << 16;
+                }
+                x = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+            words[i] = x;
+        }
+        __syncthreads();
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(words);
+        const int shift = (int)(from - base) / 2, ld = (int)a.ld;  // in values
+        uint4* out = reinterpret_cast<uint4*>(a.dst) + (part * a.group + row0) * units;
+        for (int i = threadIdx.x; i < rows * units; i += 256) {
+            const int row = i / units, u = i - row * units, at = shift + row * ld + 8 * u, valid = a.d - 8 * u;
+            uint32_t x[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int e = at + 2 * k;
+                x[k] = 2 * k < valid ? __funnelshift_r(w[e >> 1], w[(e >> 1) + 1], 16 * (e & 1)) : 0u;
+                if (2 * k + 1 >= valid) x[k] &= 0xFFFFu;
+            }
+            out[i] = make_uint4(x[0], x[1], x[2], x[3]);
+        }
+        __syncthreads();
     }
 }
 
@@ -116,38 +175,6 @@ __global__ void __launch_bounds__(256) slope_reduce_kernel(const int64_t* offset
     }
 }
 
-// The layer's kernel on 16-bit rows.  room: scratch for the laid-out matrices.
-int32_t launch_layer(rtma_ctx* ctx, LayerArgs& a, bool bf16, bool gated, bool gradient, char* room, int cls, cudaStream_t stream) {
-    const int halves = gated ? 2 : 1;
-    if (room) {
-        const int parts = a.w_stride ? a.G : 1;
-        const int64_t blocks = ceil_div((int64_t)parts * a.d_in * halves * ceil_div(a.width, 8), 256);
-        KernelScope ks(ctx, KC_WEIGHT_PREP, stream);
-        launch_kernel(lay_out_matrices_kernel, (unsigned)std::min<int64_t>(blocks, 16 * ctx->sm_count), 256, 0, stream, static_cast<const __half*>(a.B), a.w_stride, parts,
-                      a.d_in, a.width, halves, std::min(a.vb, row_granule(nullptr, a.width, 2)), reinterpret_cast<__half*>(room));
-        RTMA_LAUNCH_CHECK(ctx);
-        a.B = room;
-        a.up = (int)ceil_div(a.width, 8) * 8;
-        a.ldb = halves * a.up;
-        a.w_stride = a.w_stride ? a.d_in * a.ldb : 0;
-        a.vb = 16;
-    }
-    const int64_t tiles = a.tiles * a.n_tiles;
-    if (tiles >= (int64_t(1) << 30)) return rtma_fail(ctx, RTMA_ERR_OVERFLOW, "grouped layer: %lld tiles", (long long)tiles);
-    a.in_bulk = 2;
-    if (!make_tensor_map_16bit(&a.map_b, bf16, a.B, a.w_stride ? a.G : 1, a.d_in, gated ? a.up + a.width : a.width, a.ldb, a.w_stride ? a.w_stride : a.d_in * a.ldb, BK))
-        return rtma_fail(ctx, RTMA_ERR_CUDA, "grouped layer: no tensor map for %d matrices of %d x %d", a.w_stride ? a.G : 1, a.d_in, a.width);
-    if (a.va >= 16) {
-        if (make_tensor_map_16bit(&a.map_a, bf16, a.A, 1, a.n, a.d_in, a.lda, a.n * a.lda, BM)) a.in_bulk |= 1;
-        else if (a.places) return rtma_fail(ctx, RTMA_ERR_CUDA, "grouped layer: no tensor map for rows of %d values", a.d_in);
-    }
-    if (a.places && a.side && !make_store_map(&a.map_side, bf16 ? RTMA_BF16 : RTMA_F16, a.side, a.n, a.width, a.lds))
-        return rtma_fail(ctx, RTMA_ERR_CUDA, "grouped layer: no tensor map for rows of %d values", a.width);
-    KernelScope ks(ctx, cls, stream);
-    const unsigned grid = a.places ? 2u * a.places * a.n_tiles : (unsigned)std::min<int64_t>(tiles, ctx->sm_count);
-    return (bf16 ? launch_layer_bf16 : launch_layer_f16)(ctx, a, a.places != 0, gated, gradient, grid, stream);
-}
-
 int32_t check_layer(rtma_ctx* ctx, const char* who, const rtma_layer_desc* d, int64_t n, int32_t G, const int64_t* offsets, const float* slope) {
     if (!d) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: null description", who);
     RTMA_TRY(check_parts(ctx, who, n, G, offsets));
@@ -160,46 +187,114 @@ int32_t check_layer(rtma_ctx* ctx, const char* who, const rtma_layer_desc* d, in
     return RTMA_OK;
 }
 
-// The arguments of the layer's kernel and the scratch that it takes (lay: the matrices have to be laid out).
-void describe(rtma_ctx* ctx, LayerArgs& a, const rtma_layer_desc* d, int64_t n, int32_t G, const int64_t* offsets, const void* X, int64_t ldx, const void* W, const void* b,
-              const float* slope, const void* side, int64_t lds, size_t* bytes) {
+// A layer of 16-bit rows: what is laid out on 16-byte boundaries first, where in the scratch, and the tiles.  Rows that lie so already
+// are used where they are.
+struct Plan16 {
+    int halves, up, n_tiles, half, places;
+    int64_t tiles;
+    bool lay_x, lay_side, lay_w;
+    size_t x_at, side_at, w_at, end;  // in the scratch
+};
+
+int32_t columns_of(const rtma_layer_desc* d) { return d->dtype == RTMA_F32 ? d->d_out : (d->d_out + 7) / 8 * 8; }
+
+// padded: results and matrices with columns_of the layer's width, as the gradient has them
+Plan16 plan_16(const rtma_ctx* ctx, const rtma_layer_desc* d, int64_t n, int32_t G, const void* X, int64_t ldx, const void* W, const void* side, int64_t lds, bool padded) {
+    Plan16 p{};
+    p.halves = d->gated ? 2 : 1;
+    p.lay_x = row_granule(X, ldx, 2) < 16;
+    // (a gradient that is dZ itself is an operand whole, and what lies behind its rows is not zero)
+    p.lay_side = side && (row_granule(side, lds, 2) < 16 || (padded && !d->gated && d->act == RTMA_ACT_NONE && d->d_out % 8));
+    p.lay_w = row_granule(W, (int64_t)p.halves * d->d_out, 2) < 16 || row_granule(nullptr, d->w_stride, 2) < 16 || d->w_stride < 0 || (d->d_out % 8 && (d->gated || padded));
+    p.up = p.lay_w ? columns_of(d) : d->d_out;
+    ArenaCursor room(nullptr);
+    p.x_at = room.used;
+    if (p.lay_x) room.take<uint16_t>((size_t)n * ((d->d_in + 7) / 8 * 8));
+    p.side_at = room.used;
+    if (p.lay_side) room.take<uint16_t>((size_t)n * columns_of(d));
+    p.w_at = room.used;
+    if (p.lay_w) room.take<uint16_t>((size_t)(d->w_stride ? G : 1) * d->d_in * p.halves * p.up);
+    p.end = room.used;
+    // Columns in equal tiles: 256 of a pair of blocks at most (128 of either matrix)
+    const int width = padded ? columns_of(d) : d->d_out, pairs = ctx->sm_count / 2;
+    p.n_tiles = (int)ceil_div(width, 256 / p.halves);
+    p.half = (int)ceil_div(ceil_div(width, p.n_tiles), d->gated ? 16 : 32) * 16;
+    p.n_tiles = (int)ceil_div(width, d->gated ? p.half : 2 * p.half);
+    p.tiles = n / PAIR_ROWS + G;
+    p.places = (int)std::min<int64_t>(std::max(1, pairs / p.n_tiles), p.tiles);
+    return p;
+}
+
+// Lays out what has to be and points X, side and W there.
+int32_t lay_out_16(rtma_ctx* ctx, const Plan16& p, const rtma_layer_desc* d, int64_t n, int32_t G, const void*& X, int64_t& ldx, const void*& side, int64_t& lds, const void*& W,
+                   int64_t& w_stride, cudaStream_t stream) {
+    if (!p.lay_x && !p.lay_side && !p.lay_w) return RTMA_OK;
+    AlignArgs args{};
+    auto job = [&](AlignJob& j, const void* src, size_t at, int64_t rows, int64_t group, int64_t group_stride, int64_t ld, int width) {
+        j.src = static_cast<const uint16_t*>(src);
+        j.dst = reinterpret_cast<uint16_t*>(ctx->arena + at);
+        j.rows = rows; j.group = group; j.group_stride = group_stride; j.ld = ld; j.d = width;
+        j.granule = std::min(row_granule(src, ld, 2), row_granule(nullptr, group_stride, 2));
+    };
+    if (p.lay_x) {
+        job(args.job[0], X, p.x_at, n, n, 0, ldx, d->d_in);
+        X = args.job[0].dst;
+        ldx = (d->d_in + 7) / 8 * 8;
+    }
+    if (p.lay_side) {
+        job(args.job[1], side, p.side_at, n, n, 0, lds, d->d_out);
+        side = args.job[1].dst;
+        lds = columns_of(d);
+    }
+    if (p.lay_w) {
+        const int64_t rows = (int64_t)d->d_in * p.halves;
+        job(args.job[2], W, p.w_at, (w_stride ? G : 1) * rows, rows, w_stride, d->d_out, d->d_out);
+        W = args.job[2].dst;
+        w_stride = w_stride ? rows * p.up : 0;
+    }
+    int64_t blocks = 1;
+    for (const AlignJob& j : args.job) blocks = std::max(blocks, ceil_div(j.rows * ((j.d + 7) / 8), 1024));
+    KernelScope ks(ctx, KC_WEIGHT_PREP, stream);
+    launch_kernel(align_rows_kernel, dim3((unsigned)std::min<int64_t>(blocks, 8 * ctx->sm_count), 3), 256, 0, stream, args);
+    RTMA_LAUNCH_CHECK(ctx);
+    return RTMA_OK;
+}
+
+// What all kernels of a layer take.
+LayerArgs layer_args(const rtma_ctx* ctx, const rtma_layer_desc* d, int64_t n, int32_t G, const int64_t* offsets, const void* X, int64_t ldx, const void* W, int64_t w_stride,
+                     const void* b, const float* slope, const void* side, int64_t lds, void* out, int64_t ldo) {
     const size_t es = row_type_bytes(d->dtype);
-    const int wide = d->gated ? 2 * d->d_out : d->d_out;
+    LayerArgs a{};
     a.error_word = ctx->error_word;
     a.offsets = offsets; a.n = n; a.G = G; a.span = 1;
-    a.tile_rows = BM;
-    a.tiles = n / BM + G;
     a.m_tiles = 1;
-    a.d_in = d->d_in; a.d_out = a.width = a.up = d->d_out;
-    a.A = X; a.lda = ldx; a.B = W; a.ldb = wide; a.w_stride = d->w_stride;
+    a.d_in = d->d_in; a.d_out = a.width = a.up = a.bias_up = a.bias_width = d->d_out;
+    a.A = X; a.lda = ldx; a.B = W; a.ldb = (d->gated ? 2 : 1) * (int64_t)d->d_out; a.w_stride = w_stride;
     a.bias = b; a.bias_stride = d->b_stride;
-    a.va = row_granule(X, ldx, es);
-    a.vb = std::min(row_granule(W, wide, es), row_granule(nullptr, d->w_stride, es));
     a.act = d->act;
     a.slope = d->act == RTMA_ACT_PRELU ? slope : nullptr; a.slope_stride = d->slope_stride;
-    a.slope_warps = 8;
     a.side = side; a.lds = lds; a.gs = side ? row_granule(side, lds, es) : 0;
-    if (d->dtype == RTMA_F32) {
-        describe_layer_split(a, d->gated != 0);
-        *bytes = layer_split_bytes(a, d->gated != 0);
-        return;
-    }
-    a.bias_up = a.bias_width = a.width;
-    // Rows on 16-byte boundaries: pairs of blocks, as long as there are pairs for all tiles of columns
-    const int widest = d->gated ? 128 : 256, pairs = ctx->sm_count / 2;
-    a.n_tiles = (int)ceil_div(a.width, widest);
-    if (a.va >= 16 && (!side || a.gs >= 16) && a.n_tiles <= pairs) {
-        a.half = (int)ceil_div(ceil_div(a.width, a.n_tiles), d->gated ? 16 : 32) * 16;
-        a.n_tiles = (int)ceil_div(a.width, d->gated ? a.half : 2 * a.half);
-        a.tile_rows = 2 * BM;
-        a.tiles = n / a.tile_rows + G;
-        a.places = (int)std::min<int64_t>(pairs / a.n_tiles, a.tiles);
-    } else {
-        a.BN = (int)ceil_div(ceil_div(a.width, a.n_tiles), 16) * 16;
-        a.n_tiles = (int)ceil_div(a.width, a.BN);
-    }
-    const bool lay = a.vb < 16 || a.w_stride < 0 || (d->gated && a.width % 8);
-    *bytes = lay ? (size_t)2 * (a.w_stride ? G : 1) * a.d_in * (d->gated ? 2 : 1) * ceil_div(a.width, 8) * 8 : 0;
+    a.out = out; a.ldo = ldo;
+    a.go = row_granule(out, ldo, es);
+    return a;
+}
+
+// The layer's kernel on 16-bit rows that lie on 16-byte boundaries; width: columns of the result (of each of its halves).
+int32_t launch_16(rtma_ctx* ctx, LayerArgs& a, const Plan16& p, const rtma_layer_desc* d, bool gradient, int width, cudaStream_t stream) {
+    const bool bf16 = d->dtype == RTMA_BF16, gated = d->gated != 0;
+    a.up = p.up;
+    a.ldb = p.halves * (int64_t)p.up;
+    a.tile_rows = PAIR_ROWS;
+    a.tiles = p.tiles;
+    a.n_tiles = p.n_tiles; a.half = p.half; a.places = p.places;
+    a.width = width;
+    a.vo = a.go >= 16 && make_store_map(&a.map_o, d->dtype, a.out, a.n, gradient ? p.halves * width : width, a.ldo);
+    if (!make_tensor_map_16bit(&a.map_b, bf16, a.B, a.w_stride ? a.G : 1, a.d_in, a.ldb, a.ldb, a.w_stride ? a.w_stride : a.d_in * a.ldb, 64) ||
+        !make_tensor_map_16bit(&a.map_a, bf16, a.A, 1, a.n, a.d_in, a.lda, a.n * a.lda, PAIR_ROWS / 2) ||
+        (a.side && !make_store_map(&a.map_side, d->dtype, a.side, a.n, d->d_out, a.lds)))
+        return rtma_fail(ctx, RTMA_ERR_CUDA, "grouped layer: no tensor map for rows of %d and %d values", a.d_in, d->d_out);
+    KernelScope ks(ctx, KC_GEMM_FWD, stream);
+    return (bf16 ? launch_layer_bf16 : launch_layer_f16)(ctx, a, gated, gradient, 2u * p.places * p.n_tiles, stream);
 }
 
 }  // namespace
@@ -217,16 +312,18 @@ extern "C" int32_t rtma_grouped_layer(rtma_ctx* ctx, const rtma_layer_desc* d, i
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     DeviceScope on(ctx->device);
     RTMA_CUDA(ctx, on.status);
-    const size_t es = row_type_bytes(d->dtype);
-    LayerArgs a{};
-    size_t bytes = 0;
-    describe(ctx, a, d, n, G, offsets, X, ldx, W, b, slope, residual, ldr, &bytes);
-    a.out = Y; a.ldo = ldy;
-    a.go = row_granule(Y, ldy, es);
-    a.vo = d->dtype != RTMA_F32 && a.go >= 16 && make_store_map(&a.map_o, d->dtype, Y, n, d->d_out, ldy);
-    RTMA_TRY(prepare_row_call(ctx, bytes, stream));
-    if (d->dtype == RTMA_F32) return launch_layer_split(ctx, a, d->gated != 0, false, ctx->arena, KC_GEMM_FWD, stream);
-    return launch_layer(ctx, a, d->dtype == RTMA_BF16, d->gated != 0, false, bytes ? ctx->arena : nullptr, KC_GEMM_FWD, stream);
+    int64_t w_stride = d->w_stride;
+    if (d->dtype == RTMA_F32) {
+        LayerArgs a = layer_args(ctx, d, n, G, offsets, X, ldx, W, w_stride, b, slope, residual, ldr, Y, ldy);
+        describe_layer_split(a, d->gated != 0);
+        RTMA_TRY(prepare_row_call(ctx, layer_split_bytes(a, d->gated != 0), stream));
+        return launch_layer_split(ctx, a, d->gated != 0, false, ctx->arena, KC_GEMM_FWD, stream);
+    }
+    const Plan16 p = plan_16(ctx, d, n, G, X, ldx, W, residual, ldr, false);
+    RTMA_TRY(prepare_row_call(ctx, p.end, stream));
+    RTMA_TRY(lay_out_16(ctx, p, d, n, G, X, ldx, residual, ldr, W, w_stride, stream));
+    LayerArgs a = layer_args(ctx, d, n, G, offsets, X, ldx, W, w_stride, b, slope, residual, ldr, Y, ldy);
+    return launch_16(ctx, a, p, d, false, d->d_out, stream);
 }
 
 extern "C" int32_t rtma_grouped_layer_grad(rtma_ctx* ctx, const rtma_layer_desc* d, int64_t n, int32_t G, const int64_t* offsets, const void* X, int64_t ldx, const void* W,
@@ -235,78 +332,79 @@ extern "C" int32_t rtma_grouped_layer_grad(rtma_ctx* ctx, const rtma_layer_desc*
     const char* who = "rtma_grouped_layer_grad";
     if (!ctx) return RTMA_ERR_INVALID_ARG;
     RTMA_TRY(check_layer(ctx, who, d, n, G, offsets, slope));
-    const bool gated = d->gated != 0, plain = !gated && d->act == RTMA_ACT_NONE;  // plain: dZ is dY
-    const int wide = gated ? 2 * d->d_out : d->d_out;
+    const bool gated = d->gated != 0, plain = !gated && d->act == RTMA_ACT_NONE, wide_type = d->dtype == RTMA_F32;  // plain: dZ is dY
+    const int real = gated ? 2 * d->d_out : d->d_out, wide = (gated ? 2 : 1) * columns_of(d);
     if (n > 0 && (!X || !W || !dY || (!plain && !dZ))) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: null pointer", who);
     if (db && !dW) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: the bias gradient comes with the weights'", who);
-    if (G > 1 && db && (db_stride == 0) != (dw_stride == 0))
-        return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: either both gradients are one for all parts or neither", who);
-    if (G > 1 && db && db_stride != 0 && db_stride < wide && db_stride > -wide) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: gradients of the parts overlap", who);
     if (dslope && d->act != RTMA_ACT_PRELU) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: a slope's gradient without PReLU", who);
     if (d->grad_dtype != d->dtype && d->grad_dtype != RTMA_F32) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: gradients of the parameters in type %d", who, d->grad_dtype);
     if (ldx < d->d_in || lddy < d->d_out || (!plain && lddz < wide) || (dX && lddx < d->d_in))
         return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: rows of %d and %d values lie closer than that", who, d->d_in, wide);
-    if (!plain && n > 0 && (dZ == X || (dZ == dY && (gated || lddz != lddy)) || dZ == dX))
-        return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: dZ must not overlap other rows", who);
+    if (!plain && n > 0) {
+        if (dZ == X || dZ == dX || (dZ == dY && (gated || lddz != lddy || wide != real))) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: dZ must not overlap other rows", who);
+        if (!wide_type && row_granule(dZ, lddz, 2) < 16) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: rows of dZ off 16-byte boundaries", who);
+    }
     if (n > 0 && dX && (dX == X || (dX == dY && plain))) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: dX must not overlap rows that are still read", who);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     DeviceScope on(ctx->device);
     RTMA_CUDA(ctx, on.status);
-    const size_t es = row_type_bytes(d->dtype);
+    int64_t w_stride = d->w_stride;
     const void* dz = plain ? dY : dZ;
-    const int64_t ldz = plain ? lddy : lddz;
-    LayerArgs a{};
-    size_t matrices = 0, slots = 0, rows_bytes = 0, dw_bytes = 0;
-    describe(ctx, a, d, n, G, offsets, X, ldx, W, b, slope, dY, lddy, &matrices);
-    matrices = ArenaCursor::granule(matrices);
-    const bool pairs = !plain && n > 0 && a.places != 0, sums = pairs && db;  // the bias gradient comes with dZ
-    size_t column_bytes = 0;
-    if (pairs) {
+    int64_t ldz = plain ? lddy : lddz;
+    // All scratch at once: inside a capture nothing is enqueued unless everything fits.
+    const Plan16 p = wide_type ? Plan16{} : plan_16(ctx, d, n, G, X, ldx, W, dY, lddy, true);
+    LayerArgs a = layer_args(ctx, d, n, G, offsets, X, ldx, W, w_stride, b, slope, dY, lddy, dZ, lddz);
+    size_t slots_at = p.end, slot_bytes = 0, column_bytes = 0, rows_bytes = 0, dw_bytes = 0;
+    const bool column_sums = db && !wide_type && !plain && n > 0;  // the bias gradient comes with dZ
+    if (wide_type) {
+        describe_layer_split(a, gated);
+        slots_at = plain ? 0 : ArenaCursor::granule(layer_split_bytes(a, gated));
+        if (dslope) slot_bytes = sizeof(float) * (size_t)a.tiles * a.n_tiles * a.slope_warps;
+        if (dX) RTMA_TRY(grouped_rows(ctx, who, true, d->dtype, n, G, offsets, d->d_in, wide, dz, ldz, W, w_stride, nullptr, 0, dX, lddx, &rows_bytes, stream));
+        if (dW) RTMA_TRY(grouped_dw(ctx, who, d->dtype, n, G, offsets, d->d_in, wide, X, ldx, dz, ldz, d->grad_dtype, dW, dw_stride, db, db_stride, &dw_bytes, stream));
+    } else {
+        const size_t rows = 8 * (size_t)(p.places + G);
+        if (column_sums) column_bytes = ArenaCursor::granule(sizeof(float) * rows * wide);
+        slot_bytes = column_bytes + (dslope ? sizeof(float) * rows * 4 * p.n_tiles : 0);
+        if (dW) RTMA_TRY(layer_dw(ctx, who, d, n, G, offsets, X, ldx, dz, ldz, dW, dw_stride, db, db_stride, !column_sums, p.end, &dw_bytes, stream));
+    }
+    RTMA_TRY(prepare_row_call(ctx, std::max(slots_at + slot_bytes, std::max(rows_bytes, dw_bytes)), stream));
+    const int64_t slope_parts = G > 1 && dslope_stride == 0 ? 1 : G;
+    if (n > 0) {
+        if (!wide_type) {
+            RTMA_TRY(lay_out_16(ctx, p, d, n, G, X, ldx, dY, lddy, W, w_stride, stream));
+            a = layer_args(ctx, d, n, G, offsets, X, ldx, W, w_stride, b, slope, dY, lddy, dZ, lddz);
+            if (plain) {
+                dz = dY;
+                ldz = lddy;
+            }
+        }
+        a.column_slots = column_sums ? reinterpret_cast<float*>(ctx->arena + slots_at) : nullptr;
         a.columns = wide;
-        const size_t rows = 8 * (size_t)(a.places + G);
-        column_bytes = sums ? ArenaCursor::granule(rows * wide * sizeof(float)) : 0;
-        slots = column_bytes + (dslope ? rows * a.n_tiles * 4 * sizeof(float) : 0);
-    } else if (dslope) {
-        slots = sizeof(float) * (size_t)(a.tiles * a.n_tiles) * a.slope_warps;
+        a.slope_slots = dslope ? reinterpret_cast<float*>(ctx->arena + slots_at + column_bytes) : nullptr;
+        if (!plain) RTMA_TRY(wide_type ? launch_layer_split(ctx, a, gated, true, ctx->arena, KC_GEMM_FWD, stream) : launch_16(ctx, a, p, d, true, columns_of(d), stream));
     }
-    // all scratch at once: inside a capture nothing is enqueued unless everything fits
-    if (dX) RTMA_TRY(grouped_rows(ctx, who, true, d->dtype, n, G, offsets, d->d_in, wide, dz, ldz, W, d->w_stride, nullptr, 0, dX, lddx, &rows_bytes, stream));
-    const bool by_pairs = d->dtype != RTMA_F32 && row_granule(X, ldx, es) >= 16 && row_granule(dz, ldz, es) >= 16;
-    auto weights = by_pairs ? layer_dw : grouped_dw;
-    if (dW)
-        RTMA_TRY(weights(ctx, who, d->dtype, n, G, offsets, d->d_in, wide, X, ldx, dz, ldz, d->grad_dtype, dW, dw_stride, sums ? nullptr : db, db_stride, &dw_bytes, stream));
-    RTMA_TRY(prepare_row_call(ctx, std::max(plain ? 0 : matrices + slots, std::max(rows_bytes, dw_bytes)), stream));
-    if (!plain && n > 0) {
-        a.out = dZ; a.ldo = lddz;
-        a.go = row_granule(dZ, lddz, es);
-        a.g2 = std::min(a.go, row_granule(nullptr, d->d_out, es));
-        a.vo = d->dtype != RTMA_F32 && a.go >= 16 && make_store_map(&a.map_o, d->dtype, dZ, n, wide, lddz);
-        a.column_slots = sums ? reinterpret_cast<float*>(ctx->arena + matrices) : nullptr;
-        a.slope_slots = dslope ? reinterpret_cast<float*>(ctx->arena + matrices + column_bytes) : nullptr;
-        if (d->dtype == RTMA_F32) RTMA_TRY(launch_layer_split(ctx, a, gated, true, ctx->arena, KC_GEMM_FWD, stream));
-        else RTMA_TRY(launch_layer(ctx, a, d->dtype == RTMA_BF16, gated, true, matrices ? ctx->arena : nullptr, KC_GEMM_FWD, stream));
-    }
-    const bool slope_shared = G > 1 && dslope_stride == 0;
-    if (pairs && (sums || dslope)) {
-        SumsArgs m{};
-        m.offsets = offsets; m.n = n; m.tile_rows = a.tile_rows; m.tiles = a.tiles;
-        m.G = G; m.places = a.places; m.n_tiles = a.n_tiles; m.columns = sums ? wide : 0;
-        m.width = a.width; m.real_width = d->d_out;
-        m.column_slots = a.column_slots; m.slope_slots = a.slope_slots;
-        m.db = db; m.dslope = dslope; m.db_stride = db_stride; m.dslope_stride = dslope_stride;
-        m.shared = G > 1 && db_stride == 0; m.slope_shared = slope_shared;
-        void (*kernel)(SumsArgs) = d->grad_dtype == RTMA_F32 ? layer_sums_kernel<float> : d->grad_dtype == RTMA_BF16 ? layer_sums_kernel<__nv_bfloat16> : layer_sums_kernel<__half>;
+    if (wide_type ? dslope != nullptr : column_sums || dslope) {
         KernelScope ks(ctx, KC_REDUCE_SGD, stream);
-        launch_kernel(kernel, dim3((unsigned)(ceil_div(m.columns, 32) + (dslope ? 1 : 0)), (unsigned)G), 256, 0, stream, m);
-        RTMA_LAUNCH_CHECK(ctx);
-    } else if (dslope) {
-        const int64_t per_tile = (int64_t)a.n_tiles * a.slope_warps;
-        KernelScope ks(ctx, KC_REDUCE_SGD, stream);
-        launch_kernel(slope_reduce_kernel, slope_shared ? 1u : (unsigned)G, 256, 0, stream, offsets, n, G, a.tile_rows, a.tiles, per_tile,
-                      const_cast<const float*>(a.slope_slots), slope_shared, dslope, dslope_stride);
+        if (wide_type) {
+            const float* slots = a.slope_slots;
+            launch_kernel(slope_reduce_kernel, (unsigned)slope_parts, 256, 0, stream, offsets, n, G, a.tile_rows, a.tiles, (int64_t)a.n_tiles * a.slope_warps, slots,
+                          slope_parts != G, dslope, dslope_stride);
+        } else {
+            SumsArgs m{};
+            m.offsets = offsets; m.n = n; m.tile_rows = PAIR_ROWS; m.tiles = p.tiles;
+            m.G = G; m.places = p.places; m.n_tiles = p.n_tiles; m.columns = column_sums ? wide : 0;
+            m.width = columns_of(d); m.real_width = d->d_out;
+            m.column_slots = a.column_slots; m.slope_slots = a.slope_slots;
+            m.db = db; m.dslope = dslope; m.db_stride = db_stride; m.dslope_stride = dslope_stride;
+            m.shared = G > 1 && db_stride == 0; m.slope_shared = slope_parts != G;
+            void (*kernel)(SumsArgs) = d->grad_dtype == RTMA_F32 ? layer_sums_kernel<float> : d->dtype == RTMA_BF16 ? layer_sums_kernel<__nv_bfloat16> : layer_sums_kernel<__half>;
+            launch_kernel(kernel, dim3((unsigned)(ceil_div(m.columns, 32) + (dslope ? 1 : 0)), (unsigned)G), 256, 0, stream, m);
+        }
         RTMA_LAUNCH_CHECK(ctx);
     }
-    if (dX) RTMA_TRY(grouped_rows(ctx, who, true, d->dtype, n, G, offsets, d->d_in, wide, dz, ldz, W, d->w_stride, nullptr, 0, dX, lddx, nullptr, stream));
-    if (dW) RTMA_TRY(weights(ctx, who, d->dtype, n, G, offsets, d->d_in, wide, X, ldx, dz, ldz, d->grad_dtype, dW, dw_stride, sums ? nullptr : db, db_stride, nullptr, stream));
-    return RTMA_OK;
+    if (dX) RTMA_TRY(grouped_rows(ctx, who, true, d->dtype, n, G, offsets, d->d_in, wide_type || !p.lay_w ? real : wide, dz, ldz, W, w_stride, nullptr, 0, dX, lddx, nullptr, stream));
+    if (!dW) return RTMA_OK;
+    if (wide_type) return grouped_dw(ctx, who, d->dtype, n, G, offsets, d->d_in, wide, X, ldx, dz, ldz, d->grad_dtype, dW, dw_stride, db, db_stride, nullptr, stream);
+    return layer_dw(ctx, who, d, n, G, offsets, X, ldx, dz, ldz, dW, dw_stride, db, db_stride, !column_sums, p.end, nullptr, stream);
 }

@@ -16,9 +16,9 @@ struct LayerArgs : LinearArgs {
     int64_t lds;
     int gs;               // granule of these rows
     int g2;               // granule of the result's second half (gradient of a gated layer)
-    float* slope_slots;   // gradient, PReLU: what every warp that drains a tile has of the slope's gradient, [tile][slope_warps]
+    float* slope_slots;   // gradient, PReLU: what every warp that drains a tile has of the slope's gradient, [tile][slope_warps]; pairs of
+                          // blocks: [place + part][block of the pair, quarter of its rows][tile of columns][slice]
     int slope_warps;
-    int step_rows, step_rest;  // from a block's tile to its next: row tiles, and tiles of columns beside them
     // pairs of blocks (layer_pairs.cuh)
     int half;             // columns that each block of a pair brings of the matrix (gated: of one of the two)
     int places;           // pairs that share a tile's columns
@@ -128,9 +128,11 @@ __device__ __forceinline__ void with_activation(const LayerArgs& a, Call f) {
 size_t layer_split_bytes(const grouped::LayerArgs& a, bool gated);
 void describe_layer_split(grouped::LayerArgs& a, bool gated);  // tiles
 int32_t launch_layer_split(rtma_ctx* ctx, grouped::LayerArgs& a, bool gated, bool gradient, void* planes, int cls, cudaStream_t stream);
-// 16-bit rows: pairs of blocks with the matrix resident (up to 256 terms) or not; rows on any boundary.
-int32_t launch_layer_bf16(rtma_ctx* ctx, grouped::LayerArgs& a, bool pairs, bool gated, bool gradient, unsigned grid, cudaStream_t stream);
-int32_t launch_layer_f16(rtma_ctx* ctx, grouped::LayerArgs& a, bool pairs, bool gated, bool gradient, unsigned grid, cudaStream_t stream);
-// The weight gradient of 16-bit rows on 16-byte boundaries (layer_wgrad.cu); as grouped_dw.
-int32_t layer_dw(rtma_ctx* ctx, const char* who, int32_t dtype, int64_t n, int32_t G, const int64_t* offsets, int32_t d_in, int32_t d_out, const void* X, int64_t ldx,
-                 const void* dZ, int64_t lddz, int32_t out_dtype, void* dW, int64_t dw_stride, void* db, int64_t db_stride, size_t* scratch, cudaStream_t stream);
+// 16-bit rows on 16-byte boundaries (layer_pairs.cuh).
+int32_t launch_layer_bf16(rtma_ctx* ctx, grouped::LayerArgs& a, bool gated, bool gradient, unsigned grid, cudaStream_t stream);
+int32_t launch_layer_f16(rtma_ctx* ctx, grouped::LayerArgs& a, bool gated, bool gradient, unsigned grid, cudaStream_t stream);
+// The weight gradient of 16-bit rows on 16-byte boundaries (layer_wgrad.cu), from dZ with its halves as wide as the layer rounded up to 8; in the
+// scratch from `at` on.  sums: db is formed here.  scratch: only says how much of it the
+// call takes, from its start.
+int32_t layer_dw(rtma_ctx* ctx, const char* who, const rtma_layer_desc* d, int64_t n, int32_t G, const int64_t* offsets, const void* X, int64_t ldx, const void* dZ,
+                 int64_t lddz, void* dW, int64_t dw_stride, void* db, int64_t db_stride, bool sums, size_t at, size_t* scratch, cudaStream_t stream);

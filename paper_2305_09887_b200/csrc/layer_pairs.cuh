@@ -10,9 +10,9 @@
 // leave from; read by the lanes, each from a row of its own, it cost twice its time from memory (gradient of 500,000 x 256 -> 256: 178 us,
 // 99 without these reads).
 //
-// Gradient: the column sums of dZ (the bias gradient) are products with ones as well, by mma.sync from the slab: adding them up by the lanes would
-// cost more than the activation.  They and the slope's gradient stay in registers until the part changes, and are left in a slot of
-// (place of the pair + part), which no two share.
+// Gradient: the column sums of dZ (the bias gradient) are products with ones, by mma.sync from the slab: added up by the lanes they would cost more
+// than the activation (here 5 us of 367 for 500,000 x 256 -> 2 x 512, in the weight gradient's kernel, whose tensor cores are busier, 64 and more).  They
+// and the slope's gradient stay in registers until the part changes, and are left in a slot of (place of the pair + part), which no two share.
 #pragma once
 
 #include "grouped_rows.cuh"
@@ -300,12 +300,12 @@ __device__ __forceinline__ void pair_drain(const LayerArgs& a, PairShared& sh, u
                 if constexpr (GATED && GRADIENT) {
 #pragma unroll
                     for (int k = 0; k < 4; ++k) unpack2(y[k], v[2 * k], v[2 * k + 1]);
-                    p = Out::pack_piece(v);
-                    if (rows < 32 && lane >= rows) p = make_uint4(0u, 0u, 0u, 0u);
                     if (q == 0) {  // the last second half has been read
                         if (lane == 0) tc::tma_store_wait_read_but<0>();
                         __syncwarp();
                     }
+                    p = Out::pack_piece(v);
+                    if (rows < 32 && lane >= rows) p = make_uint4(0u, 0u, 0u, 0u);
                     Out::piece(other, lane, q, p);
                 }
                 if (BESIDE && q == 0) {  // what comes next, into the slab that the columns before these have left
@@ -340,7 +340,8 @@ __device__ __forceinline__ void pair_drain(const LayerArgs& a, PairShared& sh, u
         if (lane == 0) tc::mbar_arrive_remote(tc::leader_addr(&sh.acc_empty[acc.s]));  // (a pair's warps all report to the first block)
         acc.advance(2);
         if (GRADIENT && w.part_ends(sh)) {
-            const int64_t slot = 8 * ((int64_t)(blockIdx.x >> 1) / a.n_tiles + part) + 4 * rank + quarter;
+            const int pair = blockIdx.x >> 1, place = pair / a.n_tiles;
+            const int64_t slot = 8 * (int64_t)(place + part) + 4 * rank + quarter;
             if (a.column_slots) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
@@ -356,7 +357,7 @@ __device__ __forceinline__ void pair_drain(const LayerArgs& a, PairShared& sh, u
             }
             if (ACT == RTMA_ACT_PRELU && a.slope_slots) {
                 for (int o = 16; o > 0; o >>= 1) slope_sum += __shfl_xor_sync(0xffffffffu, slope_sum, o);
-                if (lane == 0) a.slope_slots[(slot * a.n_tiles + (blockIdx.x >> 1) % a.n_tiles) * 4 + slice] = slope_sum;
+                if (lane == 0) a.slope_slots[(slot * a.n_tiles + (pair - place * a.n_tiles)) * 4 + slice] = slope_sum;
             }
             clear();
         }

@@ -106,6 +106,11 @@ int plane_columns(const LayerArgs& a, bool gated) { return gated ? (int)ceil_div
 size_t layer_split_bytes(const LayerArgs& a, bool gated) { return (size_t)3 * 2 * (a.w_stride ? a.G : 1) * a.d_in * plane_columns(a, gated); }
 
 void describe_layer_split(LayerArgs& a, bool gated) {
+    a.va = row_granule(a.A, a.lda, 4);
+    a.vb = std::min(row_granule(a.B, a.ldb, 4), row_granule(nullptr, a.w_stride, 4));
+    a.g2 = std::min(a.go, row_granule(nullptr, a.width, 4));
+    a.tile_rows = BM;
+    a.tiles = a.n / BM + a.G;
     const int N = gated ? plane_columns(a, true) : a.width;
     a.n_tiles = (int)ceil_div(N, SPLIT_COLUMNS);
     a.BN = gated ? std::min(N, SPLIT_COLUMNS) : (int)ceil_div(ceil_div(N, a.n_tiles), 16) * 16;

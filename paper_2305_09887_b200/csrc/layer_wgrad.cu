@@ -5,8 +5,8 @@
 // parts' rows are cut into chunks as in grouped_linear.cu, one slot of fp32 sums for each, added up by a second kernel.
 //
 // The tensor cores truncate when they accumulate: sixteen warps take the accumulator after every 128 rows and add it up in registers, rounded to
-// nearest, 64 columns of a row in a lane (16 warps, not 8, because of these sums).  The column sums of dZ are taken from a stage that the
-// MMAs are done with, by two warps with mma.sync against ones; as a product of 128 x 128 tiles with ones, as in grouped_linear.cu, they cost as many MMAs as
+// nearest, 64 columns of a row in a lane (16 warps, not 8, because of these sums).  The same warps take the column
+// sums of dZ from the stages; as products with ones by mma.sync these held the MMAs up (500,000 x 256 x 1,024 in bf16: 415 us, 284 without the sums), as a product of 128 x 128 tiles with ones, as in grouped_linear.cu, they cost as many MMAs as
 // the weights' do.
 #include <algorithm>
 
@@ -30,11 +30,13 @@ struct GradArgs : LinearArgs {  // A, map_a: the left operand, B, map_b: the rig
     bool swapped;      // dZ is the left one
     int half;          // columns of the right one that a block brings
     bool sums;         // of dZ's columns are wanted
-    float* slots;      // [row tile][d_in + 1][ldo]
+    float* slots;      // [row tile][d_in + 2][ldo], two sums of dZ's columns behind the weights
+    int width, real_width;  // of dZ's halves, with and without what was rounded up
+    int real_out;      // columns of dW
 };
 
 struct GradShared : Shared {
-    uint64_t free[STAGES];  // stages whose columns have been summed
+    uint64_t ready[STAGES], free[STAGES];  // stages that have come, in either block; whose columns have been summed
 };
 
 struct GradWalk {
@@ -89,8 +91,7 @@ __device__ __forceinline__ void grad_producer(const GradArgs& a, GradShared& sh,
     int filled = 0;  // stages, STAGES at most
     bool ok = true;
     for (bool more = w.first(a, sh); more; more = w.next(a, sh), at.advance(STAGES)) {
-        uint64_t* released = a.sums ? &sh.free[at.s] : &sh.empty[at.s];
-        if (!wait_for<true>(released, at.phase ^ 1u, sh, a.error_word)) {
+        if (!wait_for<true>(&sh.empty[at.s], at.phase ^ 1u, sh, a.error_word) || (a.sums && !wait_for(&sh.free[at.s], at.phase ^ 1u, sh, a.error_word))) {
             ok = false;
             break;
         }
@@ -124,7 +125,7 @@ __device__ __forceinline__ void grad_producer(const GradArgs& a, GradShared& sh,
     for (int i = 0; i < filled; ++i) {
         const int back = filled - i, s = (at.s - back + STAGES) % STAGES;
         const uint32_t parity = s < at.s ? at.phase : at.phase ^ 1u;
-        if (!ok || !wait_for<true>(a.sums ? &sh.free[s] : &sh.empty[s], parity, sh, a.error_word)) {
+        if (!ok || !wait_for<true>(&sh.empty[s], parity, sh, a.error_word) || (a.sums && !wait_for(&sh.free[s], parity, sh, a.error_word))) {
             ok = false;
             if (rank == 0)
                 for (uint32_t k = 0; k < (1u << 14) && !tc::mbar_try_wait_cluster(&sh.full[s], parity); ++k) {}
@@ -145,6 +146,7 @@ __device__ __forceinline__ void grad_multiplier(const GradArgs& a, GradShared& s
         if (!wait_for<true>(&sh.full[at.s], at.phase, sh, a.error_word)) return;
         tc::tc_fence_after_sync();
         __syncwarp();
+        if (a.sums) tc::commit_pair_by_warp(&sh.ready[at.s]);  // (both blocks learn of the stage when the one before has been multiplied)
         const uint32_t d = sh.tmem_base + acc.s * 256, stage = ring + at.s * STAGE_BYTES;
         const uint64_t da = desc + (stage >> 4), db = da + (4 * SLAB_BYTES >> 4);
         const int steps = (min(BK, w.k_end - w.k0) + 15) >> 4;
@@ -161,78 +163,64 @@ __device__ __forceinline__ void grad_multiplier(const GradArgs& a, GradShared& s
     }
 }
 
-// Two warps: the column sums of dZ, 64 columns each (which: the first or the second), of each stage that the MMAs have read.
+// Column sums of dZ, beside the MMAs: the drain warps take 16 columns of half of a stage's rows each.
 template <class T>
-__device__ __forceinline__ void grad_sums(const GradArgs& a, GradShared& sh, uint32_t ring, int rank, int which, int lane) {
-    const uint32_t one = std::is_same<T, __half>::value ? 0x3C003C00u : 0x3F803F80u;
-    const int columns = (a.swapped ? 128 : a.half) - 64 * which;  // of dZ in this block
-    GradWalk w;
-    tc::RingAt at;
-    float c[4][4];  // c[m][0]: column 16 m + lane / 4, c[m][2]: the one 8 behind it
-    auto clear = [&]() {
+struct ColumnSums {
+    f2 of[2];  // of columns lane / 4 and 8 behind it, of a lane's rows: even ones, odd ones
+    __device__ __forceinline__ void clear() { of[0] = of[1] = pack2(0.f, 0.f); }
+    __device__ __forceinline__ void add(uint32_t columns, int which, int lane, int rows) {  // columns: of dZ in the stage; which: of the 16 warps
+        const int m = which >> 1;
+        // four 8 x 8 blocks of 16 x 16 values: columns .. + 7 and + 8 .. + 15 of rows .. + 7, then of rows + 8 .. + 15
+        const uint32_t from = columns + (m >> 2) * 2 * SLAB_BYTES + (32 * (which & 1) + 8 * (lane >> 4) + (lane & 7)) * 128 + (((2 * (m & 3) + (lane >> 3 & 1)) ^ (lane & 7)) << 4);
+        uint32_t x[2][4];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) c[i >> 2][i & 3] = 0.f;
-    };
-    clear();
-    for (bool more = w.first(a, sh); more; more = w.next(a, sh)) {
-        if (!wait_for<true>(&sh.empty[at.s], at.phase, sh, a.error_word)) return;
-        __syncwarp();
-        if (w.sums(a)) {
-            const uint32_t from = ring + at.s * STAGE_BYTES + (a.swapped ? 0 : 4 * SLAB_BYTES) + which * 2 * SLAB_BYTES;
-            const int steps = (min(BK, w.k_end - w.k0) + 15) >> 4;
-            for (int k = 0; k < steps; ++k) {
+        for (int k = 0; k < 2; ++k)
+            asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(x[k][0]), "=r"(x[k][1]), "=r"(x[k][2]), "=r"(x[k][3])
+                         : "r"(from + 2048 * k)
+                         : "memory");
 #pragma unroll
-                for (int m = 0; m < 4; ++m) {
-                    if (16 * m >= columns) break;
-                    // four 8 x 8 blocks: columns 16 m .. + 7 and + 8 .. + 15 of rows 16 k .. + 7, then of rows + 8 .. + 15
-                    const int row = 16 * k + 8 * (lane >> 4) + (lane & 7), unit = 2 * m + (lane >> 3 & 1);
-                    uint32_t x[4];
-                    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
-                                 : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3])
-                                 : "r"(from + row * 128 + ((unit ^ (row & 7)) << 4))
-                                 : "memory");
-                    if constexpr (std::is_same<T, __half>::value)
-                        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %8}, {%0, %1, %2, %3};"
-                                     : "+f"(c[m][0]), "+f"(c[m][1]), "+f"(c[m][2]), "+f"(c[m][3])
-                                     : "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(one));
-                    else
-                        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %8}, {%0, %1, %2, %3};"
-                                     : "+f"(c[m][0]), "+f"(c[m][1]), "+f"(c[m][2]), "+f"(c[m][3])
-                                     : "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(one));
-                }
+        for (int k = 0; k < 2; ++k) {
+            if (32 * (which & 1) + 16 * k >= rows) break;  // (rows behind the last are zeros up to 64 if there are any)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float a, b;
+                widen2(x[k][i], a, b, static_cast<const T*>(nullptr));
+                of[i & 1] = add2(of[i & 1], pack2(a, b));
             }
-        }
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&sh.free[at.s]);
-        at.advance(STAGES);
-        if (w.last_stage() && w.sums(a)) {
-            const int first = (a.swapped ? w.m0 + 128 * rank : w.n0 + a.half * rank) + 64 * which;
-            float* to = a.slots + ((int64_t)w.row_tile * (a.d_in + 1) + a.d_in) * a.ldo;
-            if ((lane & 3) == 0) {
-#pragma unroll
-                for (int m = 0; m < 4; ++m)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int j = 16 * m + 8 * h + (lane >> 2);
-                        if (j < columns && first + j < a.d_out) to[first + j] = c[m][2 * h];
-                    }
-            }
-            clear();
         }
     }
-}
+    __device__ __forceinline__ float total(int h) const {  // of all lanes' rows
+        float s = halves_sum(of[h]);
+        s += __shfl_xor_sync(0xffffffffu, s, 1);
+        return s + __shfl_xor_sync(0xffffffffu, s, 2);
+    }
+};
 
-__device__ __forceinline__ void grad_drain(const GradArgs& a, GradShared& sh, int rank) {
+template <class T>
+__device__ __forceinline__ void grad_drain(const GradArgs& a, GradShared& sh, uint32_t ring, int rank) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, slice = warp >> 2;
     const uint32_t tmem = sh.tmem_base + ((uint32_t)(32 * quarter) << 16) + 64 * slice;
     const bool mine = 64 * slice < 2 * a.half;
     GradWalk w;
-    tc::RingAt acc;
+    tc::RingAt acc, at;
+    ColumnSums<T> sums;
     for (bool more = w.first(a, sh); more; more = w.next_tile(a, sh)) {
+        sums.clear();
         f2 total[32];
 #pragma unroll
         for (int j = 0; j < 32; ++j) total[j] = pack2(0.f, 0.f);
         for (int k0 = 0; k0 < w.k_end; k0 += ACC_STAGES * BK) {
+            if (a.sums) {
+                for (int k = k0; k < min(k0 + ACC_STAGES * BK, w.k_end); k += BK) {
+                    if (!wait_for<true>(&sh.ready[at.s], at.phase, sh, a.error_word)) return;
+                    __syncwarp();
+                    if (w.sums(a)) sums.add(ring + at.s * STAGE_BYTES + (a.swapped ? 0 : 4 * SLAB_BYTES), warp, lane, w.k_end - k);
+                    __syncwarp();
+                    if (lane == 0) tc::mbar_arrive(&sh.free[at.s]);
+                    at.advance(STAGES);
+                }
+            }
             if (!wait_for<true>(&sh.acc_full[acc.s], acc.phase, sh, a.error_word)) return;
             __syncwarp();
             tc::tc_fence_after_sync();
@@ -253,10 +241,20 @@ __device__ __forceinline__ void grad_drain(const GradArgs& a, GradShared& sh, in
             if (lane == 0) tc::mbar_arrive_remote(tc::leader_addr(&sh.acc_empty[acc.s]));  // (a pair's warps all report to the first block)
             acc.advance(2);
         }
+        if (w.sums(a)) {
+            const int of_block = a.swapped ? 128 : a.half, first = a.swapped ? w.m0 + 128 * rank : w.n0 + a.half * rank;
+            float* const to = a.slots + ((int64_t)w.row_tile * (a.d_in + 2) + a.d_in + (warp & 1)) * a.ldo + first;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float s = sums.total(h);
+                const int j = 16 * (warp >> 1) + 8 * h + (lane >> 2);
+                if ((lane & 3) == 0 && j < of_block && first + j < a.d_out) to[j] = s;
+            }
+        }
         const int m = w.m0 + 128 * rank + 32 * quarter + lane, n = w.n0 + 64 * slice;
         const int cols = min(64, min(2 * a.half - 64 * slice, a.right - n));
         if (m < a.left && cols > 0) {
-            float* const slot = a.slots + (int64_t)w.row_tile * (a.d_in + 1) * a.ldo;
+            float* const slot = a.slots + (int64_t)w.row_tile * (a.d_in + 2) * a.ldo;
             if (a.swapped) {  // a lane's column of dZ: neighbours beside one another
                 float* to = slot + (int64_t)n * a.ldo + m;
 #pragma unroll
@@ -296,7 +294,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) layer_wg
         for (int s = 0; s < STAGES; ++s) {
             tc::mbar_init(&sh.full[s], 2);  // both blocks'
             tc::mbar_init(&sh.empty[s], 1);
-            tc::mbar_init(&sh.free[s], 2);
+            tc::mbar_init(&sh.ready[s], 1);
+            tc::mbar_init(&sh.free[s], DRAIN_WARPS);
         }
         for (int b = 0; b < 2; ++b) {
             tc::mbar_init(&sh.acc_full[b], 1);
@@ -318,12 +317,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) layer_wg
     const int rank = (int)tc::cluster_rank();
     if (warp < DRAIN_WARPS) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SUMS_REGISTERS));
-        grad_drain(a, sh, rank);
+        grad_drain<T>(a, sh, ring, rank);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGISTERS));
         if (warp == DRAIN_WARPS && rank == 0) grad_multiplier<T>(a, sh, ring);
         if (warp == DRAIN_WARPS + 1) grad_producer<T>(a, sh, ring_bytes, rank, lane);
-        if (warp >= DRAIN_WARPS + 2 && a.sums) grad_sums<T>(a, sh, ring, rank, warp - DRAIN_WARPS - 2, lane);
     }
     __syncwarp();
     if (*reinterpret_cast<volatile int*>(&sh.abort)) __nanosleep(1000000);  // a wait ran out: copies and MMAs under way land before the block ends
@@ -343,35 +341,45 @@ __global__ void __launch_bounds__(256) layer_wgrad_reduce_kernel(const __grid_co
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
     wait_for_kernel_before();
     number_tiles(a.offsets, a.n, a.G, a.n ? *a.chunk_rows : 1, a.tiles, tile_start, warp_sums, a.span);
+    auto add = [](float4& s, const float4 v) {
+        s.x += v.x;
+        s.y += v.y;
+        s.z += v.z;
+        s.w += v.w;
+    };
     const int part = blockIdx.y, from = tile_start[part], count = tile_start[part + 1] - from, quads = (int)a.ldo / 4;
-    const int64_t slot = (a.d_in + 1) * a.ldo, all = (int64_t)(a.d_in + (a.sums ? 1 : 0)) * quads;
+    const int64_t slot = (a.d_in + 2) * a.ldo, all = (int64_t)(a.d_in + (a.sums ? 1 : 0)) * quads;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
         const int row = (int)(i / quads), col = 4 * (int)(i - (int64_t)row * quads);
         const float* p = a.slots + from * slot + 4 * i;
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-        for (int t = 0; t < count; ++t, p += slot) {
-            const float4 v = *reinterpret_cast<const float4*>(p);
-            s.x += v.x;
-            s.y += v.y;
-            s.z += v.z;
-            s.w += v.w;
+        for (int t = 0; t < count; ++t, p += slot) add(s, *reinterpret_cast<const float4*>(p));
+        if (row == a.d_in) {  // the other half's
+            p = a.slots + from * slot + 4 * i + a.ldo;
+            for (int t = 0; t < count; ++t, p += slot) add(s, *reinterpret_cast<const float4*>(p));
         }
-        O* to = (row < a.d_in ? static_cast<O*>(a.dW) + part * a.dw_stride + (int64_t)row * a.d_out : static_cast<O*>(a.db) + part * a.db_stride) + col;
-        if (col < a.d_out) to[0] = from_f32<O>(s.x);
-        if (col + 1 < a.d_out) to[1] = from_f32<O>(s.y);
-        if (col + 2 < a.d_out) to[2] = from_f32<O>(s.z);
-        if (col + 3 < a.d_out) to[3] = from_f32<O>(s.w);
+        O* to = row < a.d_in ? static_cast<O*>(a.dW) + part * a.dw_stride + (int64_t)row * a.real_out : static_cast<O*>(a.db) + part * a.db_stride;
+        const int second = col >= a.width ? 1 : 0, c = col - second * a.width;  // (halves are multiples of 8)
+        to += second * a.real_width + c;
+        if (c < a.real_width) to[0] = from_f32<O>(s.x);
+        if (c + 1 < a.real_width) to[1] = from_f32<O>(s.y);
+        if (c + 2 < a.real_width) to[2] = from_f32<O>(s.z);
+        if (c + 3 < a.real_width) to[3] = from_f32<O>(s.w);
     }
 }
 
 }  // namespace
 
-int32_t layer_dw(rtma_ctx* ctx, const char* who, int32_t dtype, int64_t n, int32_t G, const int64_t* offsets, int32_t d_in, int32_t d_out, const void* X, int64_t ldx,
-                 const void* dZ, int64_t lddz, int32_t out_dtype, void* dW, int64_t dw_stride, void* db, int64_t db_stride, size_t* scratch, cudaStream_t stream) {
-    const int64_t weights = (int64_t)d_in * d_out;
-    const bool shared = G > 1 && dw_stride == 0, bf16 = dtype == RTMA_BF16;
-    if (G > 1 && !shared && dw_stride < weights && dw_stride > -weights) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: gradients of the parts overlap", who);
+int32_t layer_dw(rtma_ctx* ctx, const char* who, const rtma_layer_desc* d, int64_t n, int32_t G, const int64_t* offsets, const void* X, int64_t ldx, const void* dZ,
+                 int64_t lddz, void* dW, int64_t dw_stride, void* db, int64_t db_stride, bool sums, size_t at, size_t* scratch, cudaStream_t stream) {
+    const int halves = d->gated ? 2 : 1, width = (int)ceil_div(d->d_out, 8) * 8, d_in = d->d_in, d_out = halves * width, real_out = halves * d->d_out;
+    const int64_t weights = (int64_t)d_in * real_out;
+    const bool shared = G > 1 && dw_stride == 0, bf16 = d->dtype == RTMA_BF16;
+    if (G > 1 && db && (db_stride == 0) != shared)
+        return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: either both gradients are one for all parts or neither", who);
+    if (G > 1 && !shared && ((dw_stride < weights && dw_stride > -weights) || (db && db_stride < real_out && db_stride > -real_out)))
+        return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: gradients of the parts overlap", who);
     GradArgs a{};
     a.error_word = ctx->error_word;
     a.offsets = offsets; a.n = n;
@@ -391,17 +399,18 @@ int32_t layer_dw(rtma_ctx* ctx, const char* who, int32_t dtype, int64_t n, int32
     const int pairs = ctx->sm_count / 2;
     a.tile_rows = 256;
     a.tiles = std::min(std::max<int64_t>(a.G, (int64_t)DW_WAVES * pairs / ((int64_t)a.m_tiles * a.n_tiles)), n / a.tile_rows + a.G);
-    a.ldo = ceil_div(d_out, 8) * 8;
+    a.ldo = d_out;
+    a.width = width; a.real_width = d->d_out; a.real_out = real_out;
     a.dW = dW; a.dw_stride = dw_stride; a.db = db; a.db_stride = db_stride;
-    a.sums = db != nullptr;
-    const size_t bytes = 256 + sizeof(float) * (size_t)a.tiles * (d_in + 1) * a.ldo;
+    a.sums = db && sums;
+    const size_t bytes = at + 256 + sizeof(float) * (size_t)a.tiles * (d_in + 2) * a.ldo;
     if (scratch) {
         *scratch = bytes;
         return RTMA_OK;
     }
     RTMA_TRY(prepare_row_call(ctx, bytes, stream));
-    a.chunk_rows = reinterpret_cast<int32_t*>(ctx->arena);
-    a.slots = reinterpret_cast<float*>(ctx->arena + 256);
+    a.chunk_rows = reinterpret_cast<int32_t*>(ctx->arena + at);
+    a.slots = reinterpret_cast<float*>(ctx->arena + at + 256);
     if (n > 0) {
         const int64_t tiles = a.tiles * a.m_tiles * a.n_tiles;
         if (tiles >= (int64_t(1) << 30)) return rtma_fail(ctx, RTMA_ERR_OVERFLOW, "%s: %lld tiles", who, (long long)tiles);
@@ -418,7 +427,7 @@ int32_t layer_dw(rtma_ctx* ctx, const char* who, int32_t dtype, int64_t n, int32
         RTMA_LAUNCH_CHECK(ctx);
     }
     KernelScope ks(ctx, KC_REDUCE_SGD, stream);
-    void (*reduce)(GradArgs) = out_dtype == RTMA_F32 ? layer_wgrad_reduce_kernel<float> : bf16 ? layer_wgrad_reduce_kernel<__nv_bfloat16> : layer_wgrad_reduce_kernel<__half>;
+    void (*reduce)(GradArgs) = d->grad_dtype == RTMA_F32 ? layer_wgrad_reduce_kernel<float> : bf16 ? layer_wgrad_reduce_kernel<__nv_bfloat16> : layer_wgrad_reduce_kernel<__half>;
     const int64_t blocks = ceil_div((int64_t)(d_in + 1) * a.ldo / 4, 256);
     launch_kernel(reduce, dim3((unsigned)std::min<int64_t>(blocks, std::max(1, 8 * ctx->sm_count / a.G)), (unsigned)a.G), 256, 0, stream, a);
     RTMA_LAUNCH_CHECK(ctx);

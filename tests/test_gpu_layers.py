@@ -98,7 +98,8 @@ class Case:
     def check_gradient(self, ctx, grad_dtype=None):
         n = self.X.shape[0]
         out = rows_of(torch.full((n - 2, self.d_in), 7.0, device="cuda"), self.dtype, 3)
-        dz = rows_of(torch.full((n - 2, self.wide), 7.0, device="cuda"), self.dtype)
+        up = self.d_out if self.dtype == torch.float32 else (self.d_out + 7) // 8 * 8  # 16-bit halves are rounded up, with zeros behind
+        dz = rows_of(torch.full((n - 2, self.wide // self.d_out * up), 7.0, device="cuda"), self.dtype)
         out[n - 2:] = dz[n - 2:] = 7.0
         made = self.gated or self.act != "none"
         dx, dw, db, dslope = self.gradient(ctx, out=out, dz=dz if made else None, grad_dtype=grad_dtype)
@@ -109,7 +110,10 @@ class Case:
         for g, a, b, want in self.parts(grad=True):
             assert_close(dx[a:b], want.dx, want.dx_off, f"dX of part {g}")
             if made:
-                assert_close(dz[a:b], want.dz, want.dz_off, f"dZ of part {g}")
+                for h in range(self.wide // self.d_out):
+                    real = slice(h * self.d_out, (h + 1) * self.d_out)
+                    assert_close(dz[a:b, h * up:h * up + self.d_out], want.dz[:, real], want.dz_off[:, real], f"dZ of part {g}")
+                    assert not dz[a:b, h * up + self.d_out:(h + 1) * up].any()
             if self.slope is not None:
                 assert_close(dslope[g], want.dslope, want.dslope_off + rounding(want.dslope, torch.float32), f"dslope of part {g}")
             if self.shared:

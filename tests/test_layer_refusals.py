@@ -62,7 +62,7 @@ def calls(lib, handle, **more):
     (dict(dtype=3), "dtype=3", 3), (dict(act=4), "act=4", 3), (dict(act=-1), "act=-1", 3), (dict(act=2), "PReLU without a slope", 3),
     (dict(d_in=0), "outside", 3), (dict(d_out=16385, ldy=20000, ldz=20000), "outside", 3), (dict(gated=1, d_out=8193, ldy=9000, ldz=20000), "outside", 3),
     (dict(n=-1), "outside", 3), (dict(n=2**31), "outside", 3), (dict(G=0), "outside", 3), (dict(G=513), "outside", 3), (dict(G=2), "without offsets", 3),
-    (dict(ldx=7), "closer", 3), (dict(ldy=15), "closer", 3), (dict(r=64, ldr=15), "closer", 1), (dict(ldz=15), "closer", 2), (dict(gated=1, ldz=31), "closer", 2),
+    (dict(ldx=7), "closer", 3), (dict(ldy=15), "closer", 3), (dict(r=64, ldr=15), "closer", 1), (dict(ldz=15), "closer", 2), (dict(ldz=20), "16-byte", 2), (dict(z=66), "16-byte", 2), (dict(d_out=15, dy=64, z=64, ldy=16, ldz=16), "overlap", 2), (dict(gated=1, ldz=31), "closer", 2),
     (dict(dx=64, lddx=7), "closer", 2), (dict(x=None), "null", 3), (dict(w=None), "null", 3), (dict(z=None), "null", 2), (dict(dslope=64), "without PReLU", 2),
     (dict(db=64), "comes with", 2), (dict(grad_dtype=2), "type 2", 2), (dict(x=64, y=64), "overlap", 1), (dict(x=64, z=64), "overlap", 2), (dict(x=64, dx=64), "overlap", 2),
     (dict(gated=1, ldz=32, dy=64, z=64), "overlap", 2), (dict(dy=64, z=64, ldz=17), "overlap", 2), (dict(z=64, dx=64), "overlap", 2), (dict(act=0, dy=64, dx=64), "overlap", 2),
