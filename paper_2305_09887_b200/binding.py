@@ -759,22 +759,21 @@ class Context:
         grouped_linear_act_grad, the gradients of both side by side (each rounded up to a multiple of 8 columns)."""
         return self._gradient(X, dH, offsets, W, bias, act, slope, need_dx, need_dw, grad_dtype, out, dz, dw, db, dslope, stream, True)
 
-    def _share(self, t, parts, name):
-        """(pointer, values of a part, distance between parts)."""
-        if t.dtype not in ROW_TYPES:
-            raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
-        self._here(t, name)
-        size = t.shape
-        if parts > 1 and (not size or size[0] != parts):
-            raise ValueError(f"{name} must be [{parts}, ...], got {list(size)}")
-        values = t.numel()
+    def _share(self, t, size, parts, name):
+        """(pointer, distance between the parts) of a tensor's shares, [parts, ...] or whole."""
+        if t.get_device() != self._index:
+            self._here(t, name)
         if t.is_contiguous():
-            return t.data_ptr(), values // parts, values // parts
-        if parts > 1 and (values == 0 or t[0].is_contiguous()):
-            return t.data_ptr(), values // parts, t.stride(0)
-        raise ValueError(f"{name} must be contiguous{' within a part' if parts > 1 else ''}")
+            return t.data_ptr(), t.numel() // parts
+        want, steps = 1, t.stride()
+        for k in range(len(size) - 1, 0, -1):
+            if steps[k] != want and size[k] != 1 or parts == 1:
+                raise ValueError(f"{name} must be contiguous{' within a part' if parts > 1 else ''}")
+            want *= size[k]
+        return t.data_ptr(), steps[0]
 
     def _clip(self, grads, outs, max_norm, parts, zero_nonfinite, stream):
+        # (Every tensor's checks are what a small call costs on the host: see _here.)
         parts, one = int(parts), 0
         if parts < 1 or parts > MAX_GROUPS:
             raise ValueError(f"parts={parts} outside [1, {MAX_GROUPS}]")
@@ -784,24 +783,30 @@ class Context:
             lead = {t.shape[0] if t.dim() else 1 for t in grads}
             if len(lead) == 1 and 0 < next(iter(lead)) <= MAX_GROUPS:
                 shares, one = lead.pop(), 1
-        table = bytearray(GRADIENT.size * len(grads))
+        fields, share = [], self._share
         for i, (t, o) in enumerate(zip(grads, outs)):
-            p, size, between = self._share(t, shares, f"gradient {i}")
-            kind = ROW_TYPES[t.dtype]
-            if o is None:
-                q, apart, out_kind = 0, 0, kind
-            elif o is t:
+            kind, size = ROW_TYPES.get(t.dtype), t.shape
+            if kind is None:
+                raise TypeError(f"gradient {i} must be float32, bfloat16 or float16, got {t.dtype}")
+            if shares > 1 and (not size or size[0] != shares):
+                raise ValueError(f"gradient {i} must be [{shares}, ...], got {list(size)}")
+            p, between = share(t, size, shares, "a gradient")
+            values = t.numel() // shares
+            if o is t:
                 q, apart, out_kind = p, between, kind
+            elif o is None:
+                q, apart, out_kind = 0, 0, kind
             else:
-                if o.shape != t.shape or o.dtype not in (t.dtype, torch.float32):
-                    raise ValueError(f"result {i} must be {list(t.shape)}, {t.dtype} or {torch.float32}, got {list(o.shape)}, {o.dtype}")
-                q, _, apart = self._share(o, shares, f"result {i}")
-                out_kind = ROW_TYPES[o.dtype]
-            if o is not None and shares > 1 and apart == 0 and size:
+                out_kind = ROW_TYPES.get(o.dtype)
+                if o.shape != size or (out_kind != kind and out_kind != 0):
+                    raise ValueError(f"result {i} must be {list(size)}, {t.dtype} or {torch.float32}, got {list(o.shape)}, {o.dtype}")
+                q, apart = share(o, size, shares, "a result")
+            if apart == 0 and o is not None and shares > 1 and values:
                 raise RtmaError(f"result {i} must have memory of its own for every part, got an expanded view")
-            GRADIENT.pack_into(table, GRADIENT.size * i, p, q, size, between, apart, kind, out_kind)
+            fields += (p, q, values, between, apart, kind, out_kind)
+        table = struct.pack("<" + GRADIENT.format[1:] * len(grads), *fields)
         norms = self._empty((parts,), torch.float32, stream)
-        self._check(self._lib.rtma_clip_gradients(self._h, len(grads), bytes(table), shares, one, float(max_norm), 1 if zero_nonfinite else 0, norms.data_ptr(),
+        self._check(self._lib.rtma_clip_gradients(self._h, len(grads), table, shares, one, float(max_norm), 1 if zero_nonfinite else 0, norms.data_ptr(),
                                                   self._stream(stream)), "rtma_clip_gradients")
         return norms
 

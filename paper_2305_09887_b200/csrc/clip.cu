@@ -79,44 +79,86 @@ __device__ __forceinline__ double squares(const float (&v)[8]) {
     return d;
 }
 
-// Eight values of a piece for thread t in step `step`: neighbouring ones where rows lie on 16-byte boundaries (VECTOR), otherwise every
-// THREADS-th, so that a warp's are neighbours.
-template <bool VECTOR, class T>
-__device__ __forceinline__ void load_step(const T* p, int64_t length, int64_t step, float (&v)[8]) {
-    if constexpr (VECTOR) {
-        const int64_t at = 8 * (step * THREADS + threadIdx.x);
-        const int valid = (int)max((int64_t)0, min((int64_t)8, length - at));
-        Eight<T> e;
-        e.load(p + (valid ? at : 0), valid, 16);
-        e.values(v);
-    } else {
-        const int64_t at = 8 * step * THREADS + threadIdx.x;
+// Eight values of a piece for a thread in a step: neighbouring ones where gradients and results lie on boundaries of eight values (VECTOR),
+// otherwise every THREADS-th, so that a warp's are neighbours.  WHOLE: all of the step's values exist.
+template <bool VECTOR, bool WHOLE, class T>
+struct Step {
+    Eight<T> e;
+    T one[VECTOR ? 1 : 8];
+    __device__ __forceinline__ void load(const T* p, int64_t length, int64_t step) {
+        if constexpr (VECTOR) {
+            const int64_t at = 8 * (step * THREADS + threadIdx.x);
+            if constexpr (WHOLE) {
+                load_unit<true>(e, p + at, true, 8, 32);
+            } else {
+                const int valid = (int)max((int64_t)0, min((int64_t)8, length - at));
+                e.load(p + (valid ? at : 0), valid, 8 * (int)sizeof(T));
+            }
+        } else {
+            const int64_t at = 8 * step * THREADS + threadIdx.x;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = at + j * THREADS < length ? to_f32(p[at + j * THREADS]) : 0.f;
+            for (int j = 0; j < 8; ++j) one[j] = WHOLE || at + j * THREADS < length ? p[at + j * THREADS] : from_f32<T>(0.f);
+        }
     }
-}
-template <bool VECTOR, class T>
-__device__ __forceinline__ void store_step(T* p, int64_t length, int64_t step, const float (&v)[8]) {
-    if constexpr (VECTOR) {
-        const int64_t at = 8 * (step * THREADS + threadIdx.x);
-        if (at < length) store_eight(p + at, v, (int)min((int64_t)8, length - at), 16);
-    } else {
-        const int64_t at = 8 * step * THREADS + threadIdx.x;
+    __device__ __forceinline__ void values(float (&v)[8]) const {
+        if constexpr (VECTOR) {
+            e.values(v);
+        } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (at + j * THREADS < length) p[at + j * THREADS] = from_f32<T>(v[j]);
+            for (int j = 0; j < 8; ++j) v[j] = to_f32(one[j]);
+        }
     }
-}
-__device__ __forceinline__ bool on_16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+    // results are not read again here: they leave the L2 cache to the gradients
+    template <class O>
+    __device__ __forceinline__ static void store(O* p, int64_t length, int64_t step, const float (&v)[8]) {
+        if constexpr (VECTOR) {
+            const int64_t at = 8 * (step * THREADS + threadIdx.x);
+            if constexpr (WHOLE) {
+                if constexpr (sizeof(O) == 4) {  // whole sectors: two stores of 16 bytes each took 30 us more of the 250 for 151M bf16 values
+                    asm volatile("st.global.cs.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p + at), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]),
+                                 "f"(v[7])
+                                 : "memory");
+                } else {
+                    const O* tag = nullptr;
+                    __stcs(reinterpret_cast<uint4*>(p + at), make_uint4(narrow2(v[0], v[1], tag), narrow2(v[2], v[3], tag), narrow2(v[4], v[5], tag), narrow2(v[6], v[7], tag)));
+                }
+            } else if (at < length) {
+                store_eight(p + at, v, (int)min((int64_t)8, length - at), 8 * (int)sizeof(O));
+            }
+        } else {
+            const int64_t at = 8 * step * THREADS + threadIdx.x;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (WHOLE || at + j * THREADS < length) p[at + j * THREADS] = from_f32<O>(v[j]);
+        }
+    }
+};
+// on a boundary of eight values
+template <class T>
+__device__ __forceinline__ bool on_eight(const T* p) { return (reinterpret_cast<uintptr_t>(p) & (8 * sizeof(T) - 1)) == 0; }
+
+constexpr int TOGETHER = 4;  // steps of which all loads are under way at a time
 
 template <bool VECTOR, class T>
 __device__ __forceinline__ double piece_squares(const T* p, int64_t length) {
     double s = 0.0;
-    const int64_t steps = (length + 8 * THREADS - 1) / (8 * THREADS);
-#pragma unroll 4
-    for (int64_t i = 0; i < steps; ++i) {
-        float v[8];
-        load_step<VECTOR>(p, length, i, v);
+    const int64_t whole = length / (8 * THREADS);
+    int64_t i = 0;
+    float v[8];
+    for (; i + TOGETHER <= whole; i += TOGETHER) {
+        Step<VECTOR, true, T> step[TOGETHER];
+#pragma unroll
+        for (int k = 0; k < TOGETHER; ++k) step[k].load(p, length, i + k);
+#pragma unroll
+        for (int k = 0; k < TOGETHER; ++k) {
+            step[k].values(v);
+            s += squares(v);
+        }
+    }
+    for (; i * 8 * THREADS < length; ++i) {
+        Step<VECTOR, false, T> step;
+        step.load(p, length, i);
+        step.values(v);
         s += squares(v);
     }
     return s;
@@ -135,7 +177,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS_PER_SM) squares_kernel(const _
         auto sum = [&](auto tag) {
             typedef decltype(tag) T;
             const T* p = static_cast<const T*>(t.grad) + from;
-            return on_16(p) ? piece_squares<true>(p, piece.length) : piece_squares<false>(p, piece.length);
+            return on_eight(p) ? piece_squares<true>(p, piece.length) : piece_squares<false>(p, piece.length);
         };
         const int type = t.types & 3;
         double s = type == RTMA_F32 ? sum(0.f) : type == RTMA_BF16 ? sum(__nv_bfloat16()) : sum(__half());
@@ -165,18 +207,36 @@ __device__ __forceinline__ Scale scale_of(const ClipArgs<MOST>& a, int part, dou
     return x;
 }
 
-template <bool VECTOR, class T, class O>
-__device__ __forceinline__ void piece_scaled(const T* p, O* out, int64_t length, const Scale& x) {
-    const int64_t steps = (length + 8 * THREADS - 1) / (8 * THREADS);
+__device__ __forceinline__ void scale_eight(const Scale& x, float (&v)[8]) {
+    if (x.all) return;
     const float c = (float)x.c;
     const bool tiny = x.c < 1e-30;  // of which fp32 has fewer bits, or none
-#pragma unroll 2
-    for (int64_t i = 0; i < steps; ++i) {
-        float v[8];
-        load_step<VECTOR>(p, length, i, v);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = x.all ? v[j] : x.none ? 0.f : tiny ? (float)(v[j] * x.c) : v[j] * c;
-        store_step<VECTOR>(out, length, i, v);
+    for (int j = 0; j < 8; ++j) v[j] = x.none ? 0.f : tiny ? (float)(v[j] * x.c) : v[j] * c;
+}
+
+template <bool VECTOR, class T, class O>
+__device__ __forceinline__ void piece_scaled(const T* p, O* out, int64_t length, const Scale& x) {
+    const int64_t whole = length / (8 * THREADS);
+    int64_t i = 0;
+    float v[8];
+    for (; i + TOGETHER <= whole; i += TOGETHER) {
+        Step<VECTOR, true, T> step[TOGETHER];
+#pragma unroll
+        for (int k = 0; k < TOGETHER; ++k) step[k].load(p, length, i + k);
+#pragma unroll
+        for (int k = 0; k < TOGETHER; ++k) {
+            step[k].values(v);
+            scale_eight(x, v);
+            step[k].store(out, length, i + k, v);
+        }
+    }
+    for (; i * 8 * THREADS < length; ++i) {
+        Step<VECTOR, false, T> step;
+        step.load(p, length, i);
+        step.values(v);
+        scale_eight(x, v);
+        step.store(out, length, i, v);
     }
 }
 
@@ -204,7 +264,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS_PER_SM) scale_kernel(const __g
             typedef decltype(out_tag) O;
             const T* p = static_cast<const T*>(t.grad) + from;
             O* out = static_cast<O*>(t.out) + to;
-            if (on_16(p) && on_16(out)) piece_scaled<true>(p, out, piece.length, x);
+            if (on_eight(p) && on_eight(out)) piece_scaled<true>(p, out, piece.length, x);
             else piece_scaled<false>(p, out, piece.length, x);
         };
         const int type = t.types & 3;
