@@ -441,8 +441,8 @@ int32_t rtma_grouped_layer(rtma_ctx* ctx, const rtma_layer_desc* desc, int64_t n
                            const void* residual, int64_t ldr, void* Y, int64_t ldy, void* stream);
 /* Its gradient from the inputs alone; nothing is kept from the forward call (Z = X W + b is worked out again).  The residual's gradient
  * is dY itself.
- *   dZ [n][lddz]  of the rows' type: receives the gradient of Z, rounded to that type, from which the rest is formed.  Of 16-bit rows it lies on
- *                 16-byte boundaries, and d_out (of a gated layer each of its halves) is rounded up to a multiple of 8 values, zeros behind.
+ *   dZ [n][lddz]  of the rows' type: receives the gradient of Z, rounded to that type, from which the rest is formed.  Its rows lie on 16-byte
+ *                 boundaries, and d_out (of a gated layer each of its halves) is rounded up to a multiple of 8 values, zeros behind.
  *                 May be dY if not gated and not rounded up.  Not used (may be NULL) by a layer with neither activation nor gate: dZ is dY.
  *   dX            = dZ W_g^T (NULL: not wanted).  It overlaps neither X nor dZ.
  *   dW, db        as in rtma_grouped_linear_dw with dZ in dY's place (each may be NULL; db only with dW), in grad_dtype, rounded once.

@@ -708,7 +708,7 @@ class Context:
         n, d_in = X.shape
         G, wide = args[2], W.shape[-1]
         g, ldg = self._rows(dY, "dY", X.dtype, (n, d_out))
-        columns = (2 if gated else 1) * (d_out if X.dtype == torch.float32 else (d_out + 7) // 8 * 8)
+        columns = (2 if gated else 1) * ((d_out + 7) // 8 * 8)
         if dz is None and (gated or act != "none"):
             dz = self._empty((n, columns), X.dtype, stream)
         z, ldz = (None, 0) if dz is None else self._rows(dz, "dz", X.dtype, (n, columns))
@@ -743,8 +743,8 @@ class Context:
         front of the activation is worked out again.  dW and db have the parameters' shape (summed over the parts for shared ones) and
         grad_dtype: the rows' type, or float32; dslope float32.  None for a parameter that is None, and for what is not wanted
         (need_dx, need_dw).  dz [n, d_out]: where the gradient in front of the activation is put, rounded to the rows' type, as
-        the operand of the two products (a new one otherwise; act "none" has none); of 16-bit rows on 16-byte boundaries and with d_out
-        rounded up to a multiple of 8, zeros behind; it may be dY where nothing is rounded up."""
+        the operand of the two products (a new one otherwise; act "none" has none), its rows on 16-byte boundaries and d_out rounded up
+        to a multiple of 8, zeros behind; it may be dY where nothing is rounded up."""
         return self._gradient(X, dY, offsets, W, bias, act, slope, need_dx, need_dw, grad_dtype, out, dz, dw, db, dslope, stream, False)
 
     def grouped_gated_linear(self, X, offsets, W, bias=None, act="silu", slope=None, residual=None, out=None, stream=None):

@@ -178,11 +178,13 @@ __global__ void __launch_bounds__(REDUCE_THREADS) linear_reduce_kernel(const __g
     if (share || row > a.d_in || (row == a.d_in && !a.db)) return;
 #pragma unroll
     for (int k = 1; k < 8; ++k) add(red[k][lane]);
-    O* to = row < a.d_in ? static_cast<O*>(a.dW) + part * a.dw_stride + (int64_t)row * a.d_out + col : static_cast<O*>(a.db) + part * a.db_stride + col;
-    if (col < a.d_out) to[0] = from_f32<O>(s.x);
-    if (col + 1 < a.d_out) to[1] = from_f32<O>(s.y);
-    if (col + 2 < a.d_out) to[2] = from_f32<O>(s.z);
-    if (col + 3 < a.d_out) to[3] = from_f32<O>(s.w);
+    const int run = col / a.fold, c = col - run * a.fold, real = a.d_out / a.fold * a.fold_real;
+    O* to = (row < a.d_in ? static_cast<O*>(a.dW) + part * a.dw_stride + (int64_t)row * real : static_cast<O*>(a.db) + part * a.db_stride) + run * a.fold_real + c;
+    const int left = min(a.fold_real - c, a.d_out - col);
+    if (left > 0) to[0] = from_f32<O>(s.x);
+    if (left > 1) to[1] = from_f32<O>(s.y);
+    if (left > 2) to[2] = from_f32<O>(s.z);
+    if (left > 3) to[3] = from_f32<O>(s.w);
 }
 
 // Columns in equal tiles of a multiple of 16.
@@ -339,17 +341,18 @@ int32_t grouped_rows(rtma_ctx* ctx, const char* who, bool transposed, int32_t dt
 }
 
 int32_t grouped_dw(rtma_ctx* ctx, const char* who, int32_t dtype, int64_t n, int32_t G, const int64_t* offsets, int32_t d_in, int32_t d_out, const void* X,
-                   int64_t ldx, const void* dY, int64_t lddy, int32_t out_dtype, void* dW, int64_t dw_stride, void* db, int64_t db_stride, size_t* scratch,
+                   int64_t ldx, const void* dY, int64_t lddy, int fold, int fold_real, int32_t out_dtype, void* dW, int64_t dw_stride, void* db, int64_t db_stride, size_t* scratch,
                    cudaStream_t stream) {
     if (!ctx) return RTMA_ERR_INVALID_ARG;
     RTMA_TRY(check_linear(ctx, who, dtype, n, G, offsets, d_in, d_out));
     if (!dW || (n > 0 && (!X || !dY))) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: null pointer", who);
     if (ldx < d_in || lddy < d_out) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: rows of %d and %d values lie closer than that", who, d_in, d_out);
-    const int64_t weights = (int64_t)d_in * d_out;
+    const int real_out = d_out / fold * fold_real;
+    const int64_t weights = (int64_t)d_in * real_out;
     const bool shared = G > 1 && dw_stride == 0;
     if (G > 1 && db && (db_stride == 0) != shared)
         return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: either both gradients are one for all parts or neither", who);
-    if (G > 1 && !shared && ((dw_stride < weights && dw_stride > -weights) || (db && db_stride < d_out && db_stride > -d_out)))
+    if (G > 1 && !shared && ((dw_stride < weights && dw_stride > -weights) || (db && db_stride < real_out && db_stride > -real_out)))
         return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: gradients of the parts overlap", who);
     DeviceScope on(ctx->device);
     RTMA_CUDA(ctx, on.status);
@@ -370,6 +373,7 @@ int32_t grouped_dw(rtma_ctx* ctx, const char* who, int32_t dtype, int64_t n, int
     a.va = row_granule(X, ldx, es);
     a.vb = row_granule(dY, lddy, es);
     a.dW = dW; a.dw_stride = dw_stride; a.db = db; a.db_stride = db_stride;
+    a.fold = fold; a.fold_real = fold_real;
     a.ldo = ceil_div(d_out, 8) * 8;
     a.go = 32;
     const int64_t slot_rows = a.tiles * (d_in + a.bias_rows);
@@ -408,6 +412,6 @@ extern "C" int32_t rtma_grouped_linear_dx(rtma_ctx* ctx, int32_t dtype, int64_t 
 extern "C" int32_t rtma_grouped_linear_dw(rtma_ctx* ctx, int32_t dtype, int64_t n, int32_t G, const int64_t* offsets, int32_t d_in, int32_t d_out,
                                           const void* X, int64_t ldx, const void* dY, int64_t lddy, float* dW, int64_t dw_stride, float* db,
                                           int64_t db_stride, void* stream) {
-    return grouped_dw(ctx, "rtma_grouped_linear_dw", dtype, n, G, offsets, d_in, d_out, X, ldx, dY, lddy, RTMA_F32, dW, dw_stride, db, db_stride, nullptr,
+    return grouped_dw(ctx, "rtma_grouped_linear_dw", dtype, n, G, offsets, d_in, d_out, X, ldx, dY, lddy, d_out, d_out, RTMA_F32, dW, dw_stride, db, db_stride, nullptr,
                       static_cast<cudaStream_t>(stream));
 }

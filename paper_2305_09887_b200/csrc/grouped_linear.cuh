@@ -35,6 +35,7 @@ struct LinearArgs {
     int64_t ldo;
     void *dW, *db;             // dw: in float, or in the rows' type
     int64_t dw_stride, db_stride;
+    int fold, fold_real;       // dw: dY's columns are runs of `fold`, of which the first fold_real are dW's
     int32_t* chunk_rows;       // dw: where the rows of a row tile are left for the reduction
     int* error_word;
     CUtensorMap map_a, map_b;  // operands that are fetched by bulk-tensor loads
@@ -315,10 +316,10 @@ size_t split_planes_bytes(const grouped::LinearArgs& a);
 int32_t launch_split(rtma_ctx* ctx, int mode, grouped::LinearArgs& a, void* planes, int cls, cudaStream_t stream);
 
 // Products with the matrices of the parts, and the gradient of these, for calls that are made of several (grouped_linear.cu).  scratch:
-// only says how much the call would take.  The gradients come in out_dtype.
+// only says how much the call would take.  The gradients come in out_dtype; of every `fold` columns of dY the first fold_real have one.
 int32_t grouped_rows(rtma_ctx* ctx, const char* who, bool transposed, int32_t dtype, int64_t n, int32_t G, const int64_t* offsets, int32_t d_in, int32_t d_out,
                      const void* A, int64_t lda, const void* W, int64_t w_stride, const void* b, int64_t b_stride, void* out, int64_t ldo, size_t* scratch,
                      cudaStream_t stream);
 int32_t grouped_dw(rtma_ctx* ctx, const char* who, int32_t dtype, int64_t n, int32_t G, const int64_t* offsets, int32_t d_in, int32_t d_out, const void* X,
-                   int64_t ldx, const void* dY, int64_t lddy, int32_t out_dtype, void* dW, int64_t dw_stride, void* db, int64_t db_stride, size_t* scratch,
+                   int64_t ldx, const void* dY, int64_t lddy, int fold, int fold_real, int32_t out_dtype, void* dW, int64_t dw_stride, void* db, int64_t db_stride, size_t* scratch,
                    cudaStream_t stream);

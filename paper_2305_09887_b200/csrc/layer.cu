@@ -97,6 +97,8 @@ __global__ void __launch_bounds__(256) align_rows_kernel(const __grid_constant__
     }
 }
 
+constexpr int MOST_PLACES = 256;  // pairs of blocks on a GPU at most
+
 struct SumsArgs {
     const int64_t* offsets;
     int64_t n, tile_rows, tiles;
@@ -120,6 +122,7 @@ template <class O>
 __global__ void __launch_bounds__(256) layer_sums_kernel(const __grid_constant__ SumsArgs a) {
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
     __shared__ double red[256];
+    __shared__ int32_t place_start[MOST_PLACES + 1];
     wait_for_kernel_before();
     number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -127,15 +130,17 @@ __global__ void __launch_bounds__(256) layer_sums_kernel(const __grid_constant__
     if ((int)blockIdx.y > 0 && shared) return;
     const int column = 32 * blockIdx.x + lane, first = shared ? 0 : blockIdx.y, last = shared ? a.G : first + 1;
     const int64_t tiles = tile_start[a.G];
+    for (int i = threadIdx.x; i <= a.places; i += 256) place_start[i] = (int)(tiles * i / a.places);
+    __syncthreads();
     double s = 0.0;
     for (int part = first; part < last; ++part) {
         const int from = tile_start[part], to = tile_start[part + 1];
         if (from == to) continue;
-        // the places whose tiles [tiles i / places, tiles (i + 1) / places) are among the part's
         int i = (int)((int64_t)from * a.places / tiles);
-        while ((int)(tiles * (i + 1) / a.places) <= from) ++i;
-        for (; i < a.places && (int)(tiles * i / a.places) < to; ++i) {
-            if ((int)(tiles * i / a.places) == (int)(tiles * (i + 1) / a.places)) continue;
+        while (place_start[i + 1] <= from) ++i;
+#pragma unroll 4
+        for (; i < a.places; ++i) {
+            if (place_start[i] >= to || place_start[i] == place_start[i + 1]) continue;  // (not among the part's; without tiles, which has left no slot)
             const int64_t slot = 8 * (int64_t)(i + part);
             if (!of_slope) s += column < a.columns ? a.column_slots[(slot + warp) * a.columns + column] : 0.f;
             else
@@ -154,27 +159,6 @@ __global__ void __launch_bounds__(256) layer_sums_kernel(const __grid_constant__
     }
 }
 
-// What the warps of all tiles have of the slopes' gradients, added up in order; one block for every part, or one for all (shared).
-__global__ void __launch_bounds__(256) slope_reduce_kernel(const int64_t* offsets, int64_t n, int G, int64_t tile_rows, int64_t tiles, int64_t per_tile,
-                                                           const float* __restrict__ slots, bool shared, float* dslope, int64_t stride) {
-    __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
-    __shared__ double red[8];
-    wait_for_kernel_before();
-    number_tiles(offsets, n, G, tile_rows, tiles, tile_start, warp_sums);
-    const int part = blockIdx.x;
-    const int64_t from = shared ? 0 : tile_start[part] * per_tile, to = tile_start[shared ? G : part + 1] * per_tile;
-    double s = 0.0;
-#pragma unroll 4
-    for (int64_t i = from + threadIdx.x; i < to; i += 256) s += slots[i];
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int k = 1; k < 8; ++k) s += red[k];
-        dslope[part * stride] = (float)s;
-    }
-}
-
 int32_t check_layer(rtma_ctx* ctx, const char* who, const rtma_layer_desc* d, int64_t n, int32_t G, const int64_t* offsets, const float* slope) {
     if (!d) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: null description", who);
     RTMA_TRY(check_parts(ctx, who, n, G, offsets));
@@ -187,48 +171,75 @@ int32_t check_layer(rtma_ctx* ctx, const char* who, const rtma_layer_desc* d, in
     return RTMA_OK;
 }
 
-// A layer of 16-bit rows: what is laid out on 16-byte boundaries first, where in the scratch, and the tiles.  Rows that lie so already
-// are used where they are.
-struct Plan16 {
-    int halves, up, n_tiles, half, places;
+// What is laid out first, where in the scratch, and the tiles.  Rows that lie on 16-byte boundaries are used where they are.
+struct Plan {
+    bool f32, lay_x, lay_side, lay_w;
+    int halves, up;               // up: columns from one of the laid out matrices to the other
+    int ld, ldt;                  // fp32: of the planes of the matrices, and of their transposes
+    size_t x_at, side_at, w_at, wt_at, end;
+    int n_tiles, half, places;
     int64_t tiles;
-    bool lay_x, lay_side, lay_w;
-    size_t x_at, side_at, w_at, end;  // in the scratch
 };
 
-int32_t columns_of(const rtma_layer_desc* d) { return d->dtype == RTMA_F32 ? d->d_out : (d->d_out + 7) / 8 * 8; }
+int columns_of(const rtma_layer_desc* d) { return (d->d_out + 7) / 8 * 8; }
 
-// padded: results and matrices with columns_of the layer's width, as the gradient has them
-Plan16 plan_16(const rtma_ctx* ctx, const rtma_layer_desc* d, int64_t n, int32_t G, const void* X, int64_t ldx, const void* W, const void* side, int64_t lds, bool padded) {
-    Plan16 p{};
+// Pairs of blocks on N columns: equal tiles of 256 at most in steps of `step`.
+void cut_tiles(const rtma_ctx* ctx, int N, int step, int64_t tiles, int& n_tiles, int& half, int& places) {
+    n_tiles = (int)ceil_div(N, 256);
+    half = (int)ceil_div(ceil_div(N, n_tiles), step) * step / 2;
+    n_tiles = (int)ceil_div(N, 2 * half);
+    places = (int)std::min<int64_t>(std::min(MOST_PLACES, std::max(1, ctx->sm_count / 2 / n_tiles)), tiles);
+}
+
+// gradient: dZ and what it is multiplied by have columns_of the layer's width.
+Plan make_plan(const rtma_ctx* ctx, const rtma_layer_desc* d, int64_t n, int32_t G, const void* X, int64_t ldx, const void* W, const void* side, int64_t lds, bool gradient) {
+    Plan p{};
+    const bool plain = !d->gated && d->act == RTMA_ACT_NONE;
+    const size_t es = row_type_bytes(d->dtype);
+    const int64_t parts = d->w_stride ? G : 1;
+    const int width = gradient && !plain ? columns_of(d) : d->d_out;
+    p.f32 = d->dtype == RTMA_F32;
     p.halves = d->gated ? 2 : 1;
-    p.lay_x = row_granule(X, ldx, 2) < 16;
-    // (a gradient that is dZ itself is an operand whole, and what lies behind its rows is not zero)
-    p.lay_side = side && (row_granule(side, lds, 2) < 16 || (padded && !d->gated && d->act == RTMA_ACT_NONE && d->d_out % 8));
-    p.lay_w = row_granule(W, (int64_t)p.halves * d->d_out, 2) < 16 || row_granule(nullptr, d->w_stride, 2) < 16 || d->w_stride < 0 || (d->d_out % 8 && (d->gated || padded));
-    p.up = p.lay_w ? columns_of(d) : d->d_out;
+    p.lay_x = row_granule(X, ldx, es) < 16;
+    // (16-bit: a gradient that is dZ itself is an operand whole, and what lies behind its rows is not zero)
+    p.lay_side = side && (row_granule(side, lds, es) < 16 || (!p.f32 && gradient && plain && d->d_out % 8));
     ArenaCursor room(nullptr);
     p.x_at = room.used;
-    if (p.lay_x) room.take<uint16_t>((size_t)n * ((d->d_in + 7) / 8 * 8));
+    if (p.lay_x) room.take<char>(es * n * ((d->d_in + 7) / 8 * 8));
     p.side_at = room.used;
-    if (p.lay_side) room.take<uint16_t>((size_t)n * columns_of(d));
-    p.w_at = room.used;
-    if (p.lay_w) room.take<uint16_t>((size_t)(d->w_stride ? G : 1) * d->d_in * p.halves * p.up);
-    p.end = room.used;
-    // Columns in equal tiles: 256 of a pair of blocks at most (128 of either matrix)
-    const int width = padded ? columns_of(d) : d->d_out, pairs = ctx->sm_count / 2;
-    p.n_tiles = (int)ceil_div(width, 256 / p.halves);
-    p.half = (int)ceil_div(ceil_div(width, p.n_tiles), d->gated ? 16 : 32) * 16;
-    p.n_tiles = (int)ceil_div(width, d->gated ? p.half : 2 * p.half);
+    if (p.lay_side) room.take<char>(es * n * columns_of(d));
+    p.w_at = p.wt_at = room.used;
     p.tiles = n / PAIR_ROWS + G;
-    p.places = (int)std::min<int64_t>(std::max(1, pairs / p.n_tiles), p.tiles);
+    if (p.f32) {
+        p.up = plain ? d->d_out : columns_of(d);
+        p.ld = d->gated ? (width + 31) / 32 * 64 : (width + 7) / 8 * 8;
+        p.ldt = (d->d_in + 7) / 8 * 8;
+        room.take<uint16_t>(3 * (size_t)parts * d->d_in * p.ld);
+        p.wt_at = room.used;
+        if (gradient) room.take<uint16_t>(3 * (size_t)parts * p.halves * p.up * p.ldt);
+        cut_tiles(ctx, p.ld, d->gated ? 64 : 32, p.tiles, p.n_tiles, p.half, p.places);
+    } else {
+        p.lay_w = row_granule(W, (int64_t)p.halves * d->d_out, 2) < 16 || row_granule(nullptr, d->w_stride, 2) < 16 || d->w_stride < 0 || (d->d_out % 8 && (d->gated || gradient));
+        p.up = p.lay_w ? columns_of(d) : d->d_out;
+        if (p.lay_w) room.take<uint16_t>((size_t)parts * d->d_in * p.halves * p.up);
+        const int columns = gradient ? columns_of(d) : d->d_out;
+        if (d->gated) {  // as many of either matrix
+            cut_tiles(ctx, 2 * columns, 32, p.tiles, p.n_tiles, p.half, p.places);
+            p.n_tiles = (int)ceil_div(columns, p.half);
+            p.places = (int)std::min<int64_t>(std::min(MOST_PLACES, std::max(1, ctx->sm_count / 2 / p.n_tiles)), p.tiles);
+        } else {
+            cut_tiles(ctx, columns, 32, p.tiles, p.n_tiles, p.half, p.places);
+        }
+    }
+    p.end = room.used;
     return p;
 }
 
 // Lays out what has to be and points X, side and W there.
-int32_t lay_out_16(rtma_ctx* ctx, const Plan16& p, const rtma_layer_desc* d, int64_t n, int32_t G, const void*& X, int64_t& ldx, const void*& side, int64_t& lds, const void*& W,
-                   int64_t& w_stride, cudaStream_t stream) {
+int32_t lay_out_rows(rtma_ctx* ctx, const Plan& p, const rtma_layer_desc* d, int64_t n, int32_t G, const void*& X, int64_t& ldx, const void*& side, int64_t& lds, const void*& W,
+                     int64_t& w_stride, cudaStream_t stream) {
     if (!p.lay_x && !p.lay_side && !p.lay_w) return RTMA_OK;
+    const int values = (int)row_type_bytes(d->dtype) / 2;  // 16-bit ones in one of the rows'
     AlignArgs args{};
     auto job = [&](AlignJob& j, const void* src, size_t at, int64_t rows, int64_t group, int64_t group_stride, int64_t ld, int width) {
         j.src = static_cast<const uint16_t*>(src);
@@ -236,15 +247,16 @@ int32_t lay_out_16(rtma_ctx* ctx, const Plan16& p, const rtma_layer_desc* d, int
         j.rows = rows; j.group = group; j.group_stride = group_stride; j.ld = ld; j.d = width;
         j.granule = std::min(row_granule(src, ld, 2), row_granule(nullptr, group_stride, 2));
     };
+    auto rounded = [&](int width) { return (int64_t)((values * width + 7) / 8 * 8) / values; };
     if (p.lay_x) {
-        job(args.job[0], X, p.x_at, n, n, 0, ldx, d->d_in);
+        job(args.job[0], X, p.x_at, n, n, 0, values * ldx, values * d->d_in);
         X = args.job[0].dst;
-        ldx = (d->d_in + 7) / 8 * 8;
+        ldx = rounded(d->d_in);
     }
     if (p.lay_side) {
-        job(args.job[1], side, p.side_at, n, n, 0, lds, d->d_out);
+        job(args.job[1], side, p.side_at, n, n, 0, values * lds, values * d->d_out);
         side = args.job[1].dst;
-        lds = columns_of(d);
+        lds = rounded(d->d_out);
     }
     if (p.lay_w) {
         const int64_t rows = (int64_t)d->d_in * p.halves;
@@ -260,41 +272,59 @@ int32_t lay_out_16(rtma_ctx* ctx, const Plan16& p, const rtma_layer_desc* d, int
     return RTMA_OK;
 }
 
-// What all kernels of a layer take.
-LayerArgs layer_args(const rtma_ctx* ctx, const rtma_layer_desc* d, int64_t n, int32_t G, const int64_t* offsets, const void* X, int64_t ldx, const void* W, int64_t w_stride,
-                     const void* b, const float* slope, const void* side, int64_t lds, void* out, int64_t ldo) {
+// What all kernels of a layer take.  width: columns of the result (of each of its halves).
+LayerArgs layer_args(const rtma_ctx* ctx, const Plan& p, const rtma_layer_desc* d, int64_t n, int32_t G, const int64_t* offsets, const void* X, int64_t ldx, const void* W,
+                     int64_t w_stride, const void* b, const float* slope, const void* side, int64_t lds, void* out, int64_t ldo, int width) {
     const size_t es = row_type_bytes(d->dtype);
     LayerArgs a{};
     a.error_word = ctx->error_word;
     a.offsets = offsets; a.n = n; a.G = G; a.span = 1;
     a.m_tiles = 1;
-    a.d_in = d->d_in; a.d_out = a.width = a.up = a.bias_up = a.bias_width = d->d_out;
-    a.A = X; a.lda = ldx; a.B = W; a.ldb = (d->gated ? 2 : 1) * (int64_t)d->d_out; a.w_stride = w_stride;
+    a.tile_rows = PAIR_ROWS; a.tiles = p.tiles;
+    a.n_tiles = p.n_tiles; a.half = p.half; a.places = p.places;
+    a.d_in = d->d_in; a.d_out = a.bias_up = a.bias_width = d->d_out;
+    a.width = width;
+    a.up = p.up;
+    a.A = X; a.lda = ldx; a.B = p.f32 ? ctx->arena + p.w_at : W; a.ldb = p.f32 ? p.ld : p.halves * (int64_t)p.up; a.w_stride = w_stride;
     a.bias = b; a.bias_stride = d->b_stride;
     a.act = d->act;
     a.slope = d->act == RTMA_ACT_PRELU ? slope : nullptr; a.slope_stride = d->slope_stride;
-    a.side = side; a.lds = lds; a.gs = side ? row_granule(side, lds, es) : 0;
+    a.side = side; a.lds = lds;
     a.out = out; a.ldo = ldo;
     a.go = row_granule(out, ldo, es);
     return a;
 }
 
-// The layer's kernel on 16-bit rows that lie on 16-byte boundaries; width: columns of the result (of each of its halves).
-int32_t launch_16(rtma_ctx* ctx, LayerArgs& a, const Plan16& p, const rtma_layer_desc* d, bool gradient, int width, cudaStream_t stream) {
+// The layer's kernel; columns: of the whole result.
+int32_t launch_layer(rtma_ctx* ctx, LayerArgs& a, const Plan& p, const rtma_layer_desc* d, bool gradient, int columns, cudaStream_t stream) {
     const bool bf16 = d->dtype == RTMA_BF16, gated = d->gated != 0;
-    a.up = p.up;
-    a.ldb = p.halves * (int64_t)p.up;
-    a.tile_rows = PAIR_ROWS;
-    a.tiles = p.tiles;
-    a.n_tiles = p.n_tiles; a.half = p.half; a.places = p.places;
-    a.width = width;
-    a.vo = a.go >= 16 && make_store_map(&a.map_o, d->dtype, a.out, a.n, gradient ? p.halves * width : width, a.ldo);
+    const unsigned grid = 2u * p.places * p.n_tiles;
+    a.vo = a.go >= 16 && make_store_map(&a.map_o, d->dtype, a.out, a.n, columns, a.ldo);
+    if (p.f32) return launch_layer_f32(ctx, a, gated, gradient, KC_GEMM_FWD, grid, stream);
     if (!make_tensor_map_16bit(&a.map_b, bf16, a.B, a.w_stride ? a.G : 1, a.d_in, a.ldb, a.ldb, a.w_stride ? a.w_stride : a.d_in * a.ldb, 64) ||
         !make_tensor_map_16bit(&a.map_a, bf16, a.A, 1, a.n, a.d_in, a.lda, a.n * a.lda, PAIR_ROWS / 2) ||
         (a.side && !make_store_map(&a.map_side, d->dtype, a.side, a.n, d->d_out, a.lds)))
         return rtma_fail(ctx, RTMA_ERR_CUDA, "grouped layer: no tensor map for rows of %d and %d values", a.d_in, d->d_out);
     KernelScope ks(ctx, KC_GEMM_FWD, stream);
-    return (bf16 ? launch_layer_bf16 : launch_layer_f16)(ctx, a, gated, gradient, 2u * p.places * p.n_tiles, stream);
+    return (bf16 ? launch_layer_bf16 : launch_layer_f16)(ctx, a, gated, gradient, grid, stream);
+}
+
+// dX of fp32 rows: the rows dz times the transposed matrices' planes, by the layer's kernel without anything behind the product.
+int32_t rows_gradient_f32(rtma_ctx* ctx, const Plan& p, const rtma_layer_desc* d, int64_t n, int32_t G, const int64_t* offsets, const void* dz, int64_t ldz, void* dX, int64_t lddx,
+                          cudaStream_t stream) {
+    rtma_layer_desc t{};
+    t.dtype = RTMA_F32; t.d_in = p.halves * p.up; t.d_out = d->d_in; t.act = RTMA_ACT_NONE;
+    t.w_stride = d->w_stride;
+    Plan q{};
+    q.f32 = true;
+    q.halves = 1; q.up = d->d_in;
+    q.ld = p.ldt;
+    q.w_at = p.wt_at;
+    q.tiles = p.tiles;
+    cut_tiles(ctx, q.ld, 32, q.tiles, q.n_tiles, q.half, q.places);
+    LayerArgs a = layer_args(ctx, q, &t, n, G, offsets, dz, ldz, nullptr, t.w_stride, nullptr, nullptr, nullptr, 0, dX, lddx, d->d_in);
+    a.vo = a.go >= 16 && make_store_map(&a.map_o, RTMA_F32, dX, n, d->d_in, lddx);
+    return launch_layer_f32(ctx, a, false, false, KC_GEMM_DGRAD, 2u * q.places * q.n_tiles, stream);
 }
 
 }  // namespace
@@ -313,17 +343,13 @@ extern "C" int32_t rtma_grouped_layer(rtma_ctx* ctx, const rtma_layer_desc* d, i
     DeviceScope on(ctx->device);
     RTMA_CUDA(ctx, on.status);
     int64_t w_stride = d->w_stride;
-    if (d->dtype == RTMA_F32) {
-        LayerArgs a = layer_args(ctx, d, n, G, offsets, X, ldx, W, w_stride, b, slope, residual, ldr, Y, ldy);
-        describe_layer_split(a, d->gated != 0);
-        RTMA_TRY(prepare_row_call(ctx, layer_split_bytes(a, d->gated != 0), stream));
-        return launch_layer_split(ctx, a, d->gated != 0, false, ctx->arena, KC_GEMM_FWD, stream);
-    }
-    const Plan16 p = plan_16(ctx, d, n, G, X, ldx, W, residual, ldr, false);
+    const Plan p = make_plan(ctx, d, n, G, X, ldx, W, residual, ldr, false);
     RTMA_TRY(prepare_row_call(ctx, p.end, stream));
-    RTMA_TRY(lay_out_16(ctx, p, d, n, G, X, ldx, residual, ldr, W, w_stride, stream));
-    LayerArgs a = layer_args(ctx, d, n, G, offsets, X, ldx, W, w_stride, b, slope, residual, ldr, Y, ldy);
-    return launch_16(ctx, a, p, d, false, d->d_out, stream);
+    if (p.f32)
+        RTMA_TRY(split_matrices(ctx, static_cast<const float*>(W), w_stride, w_stride ? G : 1, d->d_in, d->d_out, p.halves, p.up, ctx->arena + p.w_at, p.ld, nullptr, 0, stream));
+    RTMA_TRY(lay_out_rows(ctx, p, d, n, G, X, ldx, residual, ldr, W, w_stride, stream));
+    LayerArgs a = layer_args(ctx, p, d, n, G, offsets, X, ldx, W, w_stride, b, slope, residual, ldr, Y, ldy, d->d_out);
+    return launch_layer(ctx, a, p, d, false, d->d_out, stream);
 }
 
 extern "C" int32_t rtma_grouped_layer_grad(rtma_ctx* ctx, const rtma_layer_desc* d, int64_t n, int32_t G, const int64_t* offsets, const void* X, int64_t ldx, const void* W,
@@ -332,79 +358,69 @@ extern "C" int32_t rtma_grouped_layer_grad(rtma_ctx* ctx, const rtma_layer_desc*
     const char* who = "rtma_grouped_layer_grad";
     if (!ctx) return RTMA_ERR_INVALID_ARG;
     RTMA_TRY(check_layer(ctx, who, d, n, G, offsets, slope));
-    const bool gated = d->gated != 0, plain = !gated && d->act == RTMA_ACT_NONE, wide_type = d->dtype == RTMA_F32;  // plain: dZ is dY
-    const int real = gated ? 2 * d->d_out : d->d_out, wide = (gated ? 2 : 1) * columns_of(d);
+    const bool gated = d->gated != 0, plain = !gated && d->act == RTMA_ACT_NONE, f32 = d->dtype == RTMA_F32;  // plain: dZ is dY
+    const int halves = gated ? 2 : 1, width = plain && f32 ? d->d_out : columns_of(d), wide = halves * width;  // of dZ
     if (n > 0 && (!X || !W || !dY || (!plain && !dZ))) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: null pointer", who);
     if (db && !dW) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: the bias gradient comes with the weights'", who);
     if (dslope && d->act != RTMA_ACT_PRELU) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: a slope's gradient without PReLU", who);
     if (d->grad_dtype != d->dtype && d->grad_dtype != RTMA_F32) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: gradients of the parameters in type %d", who, d->grad_dtype);
     if (ldx < d->d_in || lddy < d->d_out || (!plain && lddz < wide) || (dX && lddx < d->d_in))
-        return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: rows of %d and %d values lie closer than that", who, d->d_in, wide);
+        return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: rows of %d and %d values lie closer than that", who, d->d_in, plain ? d->d_out : wide);
     if (!plain && n > 0) {
-        if (dZ == X || dZ == dX || (dZ == dY && (gated || lddz != lddy || wide != real))) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: dZ must not overlap other rows", who);
-        if (!wide_type && row_granule(dZ, lddz, 2) < 16) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: rows of dZ off 16-byte boundaries", who);
+        if (dZ == X || dZ == dX || (dZ == dY && (gated || lddz != lddy || width != d->d_out))) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: dZ must not overlap other rows", who);
+        if (row_granule(dZ, lddz, row_type_bytes(d->dtype)) < 16) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: rows of dZ off 16-byte boundaries", who);
     }
     if (n > 0 && dX && (dX == X || (dX == dY && plain))) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: dX must not overlap rows that are still read", who);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     DeviceScope on(ctx->device);
     RTMA_CUDA(ctx, on.status);
     int64_t w_stride = d->w_stride;
-    const void* dz = plain ? dY : dZ;
+    const void *dz = plain ? dY : dZ, *x0 = X, *dz0 = dz;  // x0, dz0: as the caller has them, outside of the scratch
     int64_t ldz = plain ? lddy : lddz;
+    const int64_t ldx0 = ldx, ldz0 = ldz;
     // All scratch at once: inside a capture nothing is enqueued unless everything fits.
-    const Plan16 p = wide_type ? Plan16{} : plan_16(ctx, d, n, G, X, ldx, W, dY, lddy, true);
-    LayerArgs a = layer_args(ctx, d, n, G, offsets, X, ldx, W, w_stride, b, slope, dY, lddy, dZ, lddz);
-    size_t slots_at = p.end, slot_bytes = 0, column_bytes = 0, rows_bytes = 0, dw_bytes = 0;
-    const bool column_sums = db && !wide_type && !plain && n > 0;  // the bias gradient comes with dZ
-    if (wide_type) {
-        describe_layer_split(a, gated);
-        slots_at = plain ? 0 : ArenaCursor::granule(layer_split_bytes(a, gated));
-        if (dslope) slot_bytes = sizeof(float) * (size_t)a.tiles * a.n_tiles * a.slope_warps;
-        if (dX) RTMA_TRY(grouped_rows(ctx, who, true, d->dtype, n, G, offsets, d->d_in, wide, dz, ldz, W, w_stride, nullptr, 0, dX, lddx, &rows_bytes, stream));
-        if (dW) RTMA_TRY(grouped_dw(ctx, who, d->dtype, n, G, offsets, d->d_in, wide, X, ldx, dz, ldz, d->grad_dtype, dW, dw_stride, db, db_stride, &dw_bytes, stream));
-    } else {
-        const size_t rows = 8 * (size_t)(p.places + G);
-        if (column_sums) column_bytes = ArenaCursor::granule(sizeof(float) * rows * wide);
-        slot_bytes = column_bytes + (dslope ? sizeof(float) * rows * 4 * p.n_tiles : 0);
-        if (dW) RTMA_TRY(layer_dw(ctx, who, d, n, G, offsets, X, ldx, dz, ldz, dW, dw_stride, db, db_stride, !column_sums, p.end, &dw_bytes, stream));
-    }
-    RTMA_TRY(prepare_row_call(ctx, std::max(slots_at + slot_bytes, std::max(rows_bytes, dw_bytes)), stream));
-    const int64_t slope_parts = G > 1 && dslope_stride == 0 ? 1 : G;
+    const Plan p = make_plan(ctx, d, n, G, X, ldx, W, dY, lddy, true);
+    const bool column_sums = db && !f32 && !plain && n > 0;  // the bias gradient comes with dZ
+    const size_t slot_rows = 8 * (size_t)(p.places + G), column_bytes = column_sums ? ArenaCursor::granule(sizeof(float) * slot_rows * wide) : 0,
+                 slot_bytes = column_bytes + (dslope ? sizeof(float) * slot_rows * 4 * p.n_tiles : 0);
+    size_t dw_bytes = 0;
+    auto weights = [&](size_t* scratch) {
+        return f32 ? grouped_dw(ctx, who, d->dtype, n, G, offsets, d->d_in, wide, x0, ldx0, dz0, ldz0, width, d->d_out, RTMA_F32, dW, dw_stride, db, db_stride, scratch, stream)
+                   : layer_dw(ctx, who, d, n, G, offsets, X, ldx, dz, ldz, dW, dw_stride, db, db_stride, !column_sums, p.end, scratch, stream);
+    };
+    if (dW) RTMA_TRY(weights(&dw_bytes));
+    RTMA_TRY(prepare_row_call(ctx, std::max(p.end + slot_bytes, dw_bytes), stream));
     if (n > 0) {
-        if (!wide_type) {
-            RTMA_TRY(lay_out_16(ctx, p, d, n, G, X, ldx, dY, lddy, W, w_stride, stream));
-            a = layer_args(ctx, d, n, G, offsets, X, ldx, W, w_stride, b, slope, dY, lddy, dZ, lddz);
-            if (plain) {
-                dz = dY;
-                ldz = lddy;
-            }
-        }
-        a.column_slots = column_sums ? reinterpret_cast<float*>(ctx->arena + slots_at) : nullptr;
-        a.columns = wide;
-        a.slope_slots = dslope ? reinterpret_cast<float*>(ctx->arena + slots_at + column_bytes) : nullptr;
-        if (!plain) RTMA_TRY(wide_type ? launch_layer_split(ctx, a, gated, true, ctx->arena, KC_GEMM_FWD, stream) : launch_16(ctx, a, p, d, true, columns_of(d), stream));
-    }
-    if (wide_type ? dslope != nullptr : column_sums || dslope) {
-        KernelScope ks(ctx, KC_REDUCE_SGD, stream);
-        if (wide_type) {
-            const float* slots = a.slope_slots;
-            launch_kernel(slope_reduce_kernel, (unsigned)slope_parts, 256, 0, stream, offsets, n, G, a.tile_rows, a.tiles, (int64_t)a.n_tiles * a.slope_warps, slots,
-                          slope_parts != G, dslope, dslope_stride);
+        if (f32 && (dX || !plain))
+            RTMA_TRY(split_matrices(ctx, static_cast<const float*>(W), w_stride, w_stride ? G : 1, d->d_in, d->d_out, p.halves, p.up, plain ? nullptr : ctx->arena + p.w_at, p.ld,
+                                    dX ? ctx->arena + p.wt_at : nullptr, p.ldt, stream));
+        RTMA_TRY(lay_out_rows(ctx, p, d, n, G, X, ldx, dY, lddy, W, w_stride, stream));
+        if (plain) {
+            dz = dY;
+            ldz = lddy;
         } else {
-            SumsArgs m{};
-            m.offsets = offsets; m.n = n; m.tile_rows = PAIR_ROWS; m.tiles = p.tiles;
-            m.G = G; m.places = p.places; m.n_tiles = p.n_tiles; m.columns = column_sums ? wide : 0;
-            m.width = columns_of(d); m.real_width = d->d_out;
-            m.column_slots = a.column_slots; m.slope_slots = a.slope_slots;
-            m.db = db; m.dslope = dslope; m.db_stride = db_stride; m.dslope_stride = dslope_stride;
-            m.shared = G > 1 && db_stride == 0; m.slope_shared = slope_parts != G;
-            void (*kernel)(SumsArgs) = d->grad_dtype == RTMA_F32 ? layer_sums_kernel<float> : d->dtype == RTMA_BF16 ? layer_sums_kernel<__nv_bfloat16> : layer_sums_kernel<__half>;
-            launch_kernel(kernel, dim3((unsigned)(ceil_div(m.columns, 32) + (dslope ? 1 : 0)), (unsigned)G), 256, 0, stream, m);
+            LayerArgs a = layer_args(ctx, p, d, n, G, offsets, X, ldx, W, w_stride, b, slope, dY, lddy, dZ, lddz, width);
+            a.column_slots = column_sums ? reinterpret_cast<float*>(ctx->arena + p.end) : nullptr;
+            a.columns = wide;
+            a.slope_slots = dslope ? reinterpret_cast<float*>(ctx->arena + p.end + column_bytes) : nullptr;
+            RTMA_TRY(launch_layer(ctx, a, p, d, true, wide, stream));
         }
+    }
+    if (column_sums || dslope) {
+        SumsArgs m{};
+        m.offsets = offsets; m.n = n; m.tile_rows = PAIR_ROWS; m.tiles = p.tiles;
+        m.G = G; m.places = p.places; m.n_tiles = p.n_tiles; m.columns = column_sums ? wide : 0;
+        m.width = width; m.real_width = d->d_out;
+        m.column_slots = reinterpret_cast<const float*>(ctx->arena + p.end); m.slope_slots = reinterpret_cast<const float*>(ctx->arena + p.end + column_bytes);
+        m.db = db; m.dslope = dslope; m.db_stride = db_stride; m.dslope_stride = dslope_stride;
+        m.shared = G > 1 && db_stride == 0; m.slope_shared = G > 1 && dslope_stride == 0;
+        void (*kernel)(SumsArgs) = d->grad_dtype == RTMA_F32 ? layer_sums_kernel<float> : d->dtype == RTMA_BF16 ? layer_sums_kernel<__nv_bfloat16> : layer_sums_kernel<__half>;
+        KernelScope ks(ctx, KC_REDUCE_SGD, stream);
+        launch_kernel(kernel, dim3((unsigned)(ceil_div(m.columns, 32) + (dslope ? 1 : 0)), (unsigned)G), 256, 0, stream, m);
         RTMA_LAUNCH_CHECK(ctx);
     }
-    if (dX) RTMA_TRY(grouped_rows(ctx, who, true, d->dtype, n, G, offsets, d->d_in, wide_type || !p.lay_w ? real : wide, dz, ldz, W, w_stride, nullptr, 0, dX, lddx, nullptr, stream));
-    if (!dW) return RTMA_OK;
-    if (wide_type) return grouped_dw(ctx, who, d->dtype, n, G, offsets, d->d_in, wide, X, ldx, dz, ldz, d->grad_dtype, dW, dw_stride, db, db_stride, nullptr, stream);
-    return layer_dw(ctx, who, d, n, G, offsets, X, ldx, dz, ldz, dW, dw_stride, db, db_stride, !column_sums, p.end, nullptr, stream);
+    if (dX && n > 0)
+        RTMA_TRY(f32 ? rows_gradient_f32(ctx, p, d, n, G, offsets, dz, ldz, dX, lddx, stream)
+                     : grouped_rows(ctx, who, true, d->dtype, n, G, offsets, d->d_in, p.halves * p.up, dz, ldz, W, w_stride, nullptr, 0, dX, lddx, nullptr, stream));
+    return dW ? weights(nullptr) : RTMA_OK;
 }

@@ -14,12 +14,8 @@ struct LayerArgs : LinearArgs {
     int64_t slope_stride;
     const void* side;     // rows read on the way out: the residual branch (or none), or the result's gradient
     int64_t lds;
-    int gs;               // granule of these rows
-    int g2;               // granule of the result's second half (gradient of a gated layer)
-    float* slope_slots;   // gradient, PReLU: what every warp that drains a tile has of the slope's gradient, [tile][slope_warps]; pairs of
-                          // blocks: [place + part][block of the pair, quarter of its rows][tile of columns][slice]
-    int slope_warps;
-    // pairs of blocks (layer_pairs.cuh)
+    float* slope_slots;   // gradient, PReLU: what the warps that drain have of the slope's gradient, [place + part][block of the pair,
+                          // quarter of its rows][tile of columns][slice]
     int half;             // columns that each block of a pair brings of the matrix (gated: of one of the two)
     int places;           // pairs that share a tile's columns
     int bias_up, bias_width;  // as width and the distance of the two matrices, in the bias (width may be rounded up)
@@ -29,6 +25,40 @@ struct LayerArgs : LinearArgs {
 };
 
 #ifdef __CUDACC__
+constexpr int PAIR_BM = 128;  // rows of a tile that a block of a pair has
+// A pair's walk down its row tiles; rows and row0 are the block's own.
+struct PairWalk {
+    int t, end, part, left;  // left: rows of the part from the tile's first on
+    int64_t first_row;
+    __device__ __forceinline__ bool open(const LayerArgs& a, const Shared& sh) {
+        const int64_t tiles = sh.tile_start[a.G];
+        const int place = (blockIdx.x >> 1) / a.n_tiles;
+        t = (int)(tiles * place / a.places);
+        end = (int)(tiles * (place + 1) / a.places);
+        if (t >= end) return false;
+        part = part_of_tile(sh.tile_start, a.G, t);
+        return at(sh);
+    }
+    __device__ __forceinline__ bool at(const Shared& sh) {
+        const int inside = (t - sh.tile_start[part]) * 2 * PAIR_BM;
+        first_row = (int64_t)sh.begin[part] + inside;
+        left = sh.rows[part] - inside;
+        return true;
+    }
+    __device__ __forceinline__ bool next(const Shared& sh) {
+        if (++t >= end) return false;
+        if (t >= sh.tile_start[part + 1]) {
+            do ++part;
+            while (t >= sh.tile_start[part + 1]);
+            return at(sh);
+        }
+        first_row += 2 * PAIR_BM;
+        left -= 2 * PAIR_BM;
+        return true;
+    }
+    __device__ __forceinline__ bool part_ends(const Shared& sh) const { return t + 1 >= end || t + 1 >= sh.tile_start[part + 1]; }
+};
+
 // The bias of a warp's columns in shared memory: 32 at a time, `chunks` of them.  Held for as long as part and column stay.
 struct LayerBias {
     float* at;  // 16-byte boundary
@@ -124,10 +154,12 @@ __device__ __forceinline__ void with_activation(const LayerArgs& a, Call f) {
 
 }  // namespace grouped
 
-// fp32 rows: the matrices are laid out in planes (scratch), the two of a gated layer by turns of 32 columns.
-size_t layer_split_bytes(const grouped::LayerArgs& a, bool gated);
-void describe_layer_split(grouped::LayerArgs& a, bool gated);  // tiles
-int32_t launch_layer_split(rtma_ctx* ctx, grouped::LayerArgs& a, bool gated, bool gradient, void* planes, int cls, cudaStream_t stream);
+// fp32 rows on 16-byte boundaries (layer_f32.cu).  a.B: planes that the matrices have been split into, of a.ldb columns.
+int32_t launch_layer_f32(rtma_ctx* ctx, grouped::LayerArgs& a, bool gated, bool gradient, int cls, unsigned grid, cudaStream_t stream);
+// The matrices [part][d_in][halves * width] as planes [part][3][d_in][ld], the halves by turns of 32 columns, and (transposed not NULL) as planes
+// [part][3][halves * up][ldt] of their transposes, zeros for what `up` has above width.
+int32_t split_matrices(rtma_ctx* ctx, const float* W, int64_t w_stride, int parts, int d_in, int width, int halves, int up, void* planes, int ld, void* transposed, int ldt,
+                       cudaStream_t stream);
 // 16-bit rows on 16-byte boundaries (layer_pairs.cuh).
 int32_t launch_layer_bf16(rtma_ctx* ctx, grouped::LayerArgs& a, bool gated, bool gradient, unsigned grid, cudaStream_t stream);
 int32_t launch_layer_f16(rtma_ctx* ctx, grouped::LayerArgs& a, bool gated, bool gradient, unsigned grid, cudaStream_t stream);

@@ -45,39 +45,6 @@ struct PairShared : Shared {
     uint64_t side[16][2];            // slabs that rows read beside the accumulators have come to
 };
 
-// A pair's walk down its row tiles; rows and row0 are the block's own.
-struct PairWalk {
-    int t, end, part, left;  // left: rows of the part from the tile's first on
-    int64_t first_row;
-    __device__ __forceinline__ bool open(const LayerArgs& a, const PairShared& sh) {
-        const int64_t tiles = sh.tile_start[a.G];
-        const int place = (blockIdx.x >> 1) / a.n_tiles;
-        t = (int)(tiles * place / a.places);
-        end = (int)(tiles * (place + 1) / a.places);
-        if (t >= end) return false;
-        part = part_of_tile(sh.tile_start, a.G, t);
-        return at(sh);
-    }
-    __device__ __forceinline__ bool at(const PairShared& sh) {
-        const int inside = (t - sh.tile_start[part]) * 2 * BM;
-        first_row = (int64_t)sh.begin[part] + inside;
-        left = sh.rows[part] - inside;
-        return true;
-    }
-    __device__ __forceinline__ bool next(const PairShared& sh) {
-        if (++t >= end) return false;
-        if (t >= sh.tile_start[part + 1]) {
-            do ++part;
-            while (t >= sh.tile_start[part + 1]);
-            return at(sh);
-        }
-        first_row += 2 * BM;
-        left -= 2 * BM;
-        return true;
-    }
-    __device__ __forceinline__ bool part_ends(const PairShared& sh) const { return t + 1 >= end || t + 1 >= sh.tile_start[part + 1]; }
-};
-
 template <class F>
 __device__ __forceinline__ void pair_producer(const LayerArgs& a, PairShared& sh, uint8_t* ring, uint8_t* held, int rank) {
     tc::prefetch_tensormap(&a.map_a);

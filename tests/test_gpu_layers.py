@@ -98,7 +98,7 @@ class Case:
     def check_gradient(self, ctx, grad_dtype=None):
         n = self.X.shape[0]
         out = rows_of(torch.full((n - 2, self.d_in), 7.0, device="cuda"), self.dtype, 3)
-        up = self.d_out if self.dtype == torch.float32 else (self.d_out + 7) // 8 * 8  # 16-bit halves are rounded up, with zeros behind
+        up = (self.d_out + 7) // 8 * 8  # halves are rounded up, with zeros behind
         dz = rows_of(torch.full((n - 2, self.wide // self.d_out * up), 7.0, device="cuda"), self.dtype)
         out[n - 2:] = dz[n - 2:] = 7.0
         made = self.gated or self.act != "none"
