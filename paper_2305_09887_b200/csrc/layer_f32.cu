@@ -4,7 +4,7 @@
 // then added up in registers, rounded to nearest (grouped_split.cu says why).  Pairs of blocks (MMAs of 256 rows by up to 256 columns), each step
 // with warps of its own, so that the MMAs wait for none of them:
 //   one warp   bulk-tensor loads of the rows as they are (three stages) and of the matrix's planes, which are split once a call (two)
-//   two warps  split a stage's rows into planes
+//   six warps  split a stage's rows into planes (two took twice the MMAs' time)
 //   one warp   MMAs
 //   16 warps   take 64 columns of 32 rows of the accumulator after every stage, and a finished tile through the layer, 16 columns at a time
 // In turn, all steps by the same warps and two blocks on an SM as in grouped_split.cu, 200,000 x 256 -> 256 with a residual branch took 327 us.
@@ -22,12 +22,12 @@ namespace {
 
 using namespace grouped;
 
-constexpr int BM = PAIR_BM, BK = 32, DRAIN_WARPS = 16, THREADS = 32 * (DRAIN_WARPS + 4), SPLIT_WARPS = 2;
+constexpr int BM = PAIR_BM, BK = 32, DRAIN_WARPS = 16, SPLIT_WARPS = 6, THREADS = 32 * (DRAIN_WARPS + 2 + SPLIT_WARPS);
 constexpr int RAW_STAGES = 3, RAW_BYTES = BM * BK * 4, STAGES = 2;
 constexpr int A_PLANE = BM * BK * 2, W_ATOM = 3 * 64 * BK * 2;  // a plane of the rows; three planes of 64 columns
 constexpr int A_BYTES = 3 * A_PLANE, W_BYTES = 2 * W_ATOM, SLAB = 32 * 64, SLABS = 2;
 constexpr int DYNAMIC_BYTES = 1024 + RAW_STAGES * RAW_BYTES + STAGES * (A_BYTES + W_BYTES) + DRAIN_WARPS * SLABS * SLAB;
-constexpr int DRAIN_REGISTERS = 104, OTHER_REGISTERS = 64;  // 512 x 104 + 128 x 64 = 640 x 96
+constexpr int DRAIN_REGISTERS = 96, OTHER_REGISTERS = 48;  // 512 x 96 + 256 x 48 = 768 x 80
 
 struct F32Shared : Shared {
     uint64_t raw_full[RAW_STAGES], raw_free[RAW_STAGES];
@@ -94,7 +94,7 @@ __device__ __forceinline__ void f32_producer(const LayerArgs& a, F32Shared& sh, 
     }
 }
 
-// A warp's half of a stage's rows: units of eight terms, two at a time.
+// A warp's share of a stage's rows: units of eight terms.
 __device__ __forceinline__ void f32_splitter(const LayerArgs& a, F32Shared& sh, uint32_t raw, uint32_t planes, int which, int lane) {
     StageWalk w;
     tc::RingAt at, raw_at;
@@ -104,29 +104,21 @@ __device__ __forceinline__ void f32_splitter(const LayerArgs& a, F32Shared& sh, 
         __syncwarp();
         const uint32_t from = raw + raw_at.s * RAW_BYTES, to = planes + at.s * A_BYTES;
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-            uint4 x[2][2];
+        for (int i = 0; i < (BM * 4 + 32 * SPLIT_WARPS - 1) / (32 * SPLIT_WARPS); ++i) {
+            const int j = 32 * (SPLIT_WARPS * i + which) + lane, row = j >> 2, unit = j & 3;
+            if (32 * SPLIT_WARPS * (i + 1) > BM * 4 && j >= BM * 4) break;  // (a warp as a whole)
+            const uint4 lo = load_16(from + row * 128 + (((2 * unit) ^ (row & 7)) << 4)), hi = load_16(from + row * 128 + (((2 * unit + 1) ^ (row & 7)) << 4));
+            const uint32_t v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+            uint4 p[3];
+            split_eight(v, p);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int row = 64 * which + 8 * (i + j) + (lane >> 2), unit = lane & 3;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) x[j][h] = load_16(from + row * 128 + (((2 * unit + h) ^ (row & 7)) << 4));
-            }
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int row = 64 * which + 8 * (i + j) + (lane >> 2), unit = lane & 3;
-                const uint32_t v[8] = {x[j][0].x, x[j][0].y, x[j][0].z, x[j][0].w, x[j][1].x, x[j][1].y, x[j][1].z, x[j][1].w};
-                uint4 p[3];
-                split_eight(v, p);
-#pragma unroll
-                for (int k = 0; k < 3; ++k) store_16(to + k * A_PLANE + row * 64 + ((unit ^ (row >> 1 & 3)) << 4), p[k]);
-            }
+            for (int k = 0; k < 3; ++k) store_16(to + k * A_PLANE + row * 64 + ((unit ^ (row >> 1 & 3)) << 4), p[k]);
         }
         tc::fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
             tc::mbar_arrive(&sh.raw_free[raw_at.s]);
-            tc::mbar_arrive_cluster(tc::leader_addr(&sh.full[at.s]));
+            tc::mbar_arrive_remote(tc::leader_addr(&sh.full[at.s]));  // (each block's planes are read by its own tensor cores: the fence has made them visible)
         }
         raw_at.advance(RAW_STAGES);
         at.advance(STAGES);
@@ -206,6 +198,8 @@ __device__ __forceinline__ void f32_drain(const LayerArgs& a, F32Shared& sh, uin
             __syncwarp();
             request(0);
             request(1);
+            if (lane >= 2 && lane < mine)  // the others come to the L2 cache meanwhile
+                asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];" ::"l"(reinterpret_cast<uint64_t>(&a.map_side)), "r"(c0 + 16 * lane), "r"((int)row0) : "memory");
         }
         if (w.part != part) {
             part = w.part;
@@ -281,14 +275,13 @@ __device__ __forceinline__ void f32_drain(const LayerArgs& a, F32Shared& sh, uin
                     }
                     Out::piece(slab, lane, 2 * q, Out::pack_piece(v));
                     Out::piece(slab, lane, 2 * q + 1, Out::pack_piece(v + 4));
+                    if (BESIDE && !GATED && q == 0 && j >= 1 && j < ITEMS - 1) {  // the rows beside the next 16 results, into the slab that the last ones have left
+                        if (lane == 0) tc::tma_store_wait_read_but<0>();
+                        __syncwarp();
+                        request(j + 1);
+                    }
                 }
                 store(j, slab, 0);
-                if (BESIDE && !GATED && j == 1 && mine > 2) {
-                    if (lane == 0) tc::tma_store_wait_read_but<0>();
-                    __syncwarp();
-                    request(2);
-                    request(3);
-                }
             }
             if constexpr (GATED && GRADIENT) {  // the second halves, kept until the slabs are free again
                 if (lane == 0) tc::tma_store_wait_read_but<0>();
