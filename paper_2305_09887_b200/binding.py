@@ -783,24 +783,29 @@ class Context:
             lead = {t.shape[0] if t.dim() else 1 for t in grads}
             if len(lead) == 1 and 0 < next(iter(lead)) <= MAX_GROUPS:
                 shares, one = lead.pop(), 1
-        fields, share = [], self._share
+        fields, share, kinds, index = [], self._share, ROW_TYPES.get, self._index
         for i, (t, o) in enumerate(zip(grads, outs)):
-            kind, size = ROW_TYPES.get(t.dtype), t.shape
+            kind, size = kinds(t.dtype), t.shape
             if kind is None:
                 raise TypeError(f"gradient {i} must be float32, bfloat16 or float16, got {t.dtype}")
             if shares > 1 and (not size or size[0] != shares):
                 raise ValueError(f"gradient {i} must be [{shares}, ...], got {list(size)}")
-            p, between = share(t, size, shares, "a gradient")
             values = t.numel() // shares
+            whole = t.is_contiguous() and t.get_device() == index
+            p, between = (t.data_ptr(), values) if whole else share(t, size, shares, f"gradient {i}")
             if o is t:
                 q, apart, out_kind = p, between, kind
             elif o is None:
                 q, apart, out_kind = 0, 0, kind
             else:
-                out_kind = ROW_TYPES.get(o.dtype)
+                out_kind = kinds(o.dtype)
                 if o.shape != size or (out_kind != kind and out_kind != 0):
                     raise ValueError(f"result {i} must be {list(size)}, {t.dtype} or {torch.float32}, got {list(o.shape)}, {o.dtype}")
-                q, apart = share(o, size, shares, "a result")
+                steps = o.stride()
+                if whole and shares > 1 and steps[1:] == t.stride()[1:] and o.get_device() == index:
+                    q, apart = o.data_ptr(), steps[0]
+                else:
+                    q, apart = share(o, size, shares, f"result {i}")
             if apart == 0 and o is not None and shares > 1 and values:
                 raise RtmaError(f"result {i} must have memory of its own for every part, got an expanded view")
             fields += (p, q, values, between, apart, kind, out_kind)

@@ -39,7 +39,7 @@ constexpr int ALIGN_BYTES = 16384;
 // A block brings neighbouring rows as the 16-byte words that they lie in, and cuts them up in shared memory.  Memory's time (200,000 x 100: 15 us), where
 // the products' own copies of such rows, for every tile of columns again, cost more than the products (200,000 x 100 -> 2 x 266 in fp16: 222 us).
 __global__ void __launch_bounds__(256) align_rows_kernel(const __grid_constant__ AlignArgs args) {
-    __shared__ uint4 words[ALIGN_BYTES / 16 + 2];
+    __shared__ uint4 words[ALIGN_BYTES / 16 + 258];  // (a row's last words are read beyond it, and dropped)
     wait_for_kernel_before();
     const AlignJob& a = args.job[blockIdx.y];
     if (!a.rows) return;
@@ -56,43 +56,76 @@ __global__ void __launch_bounds__(256) align_rows_kernel(const __grid_constant__
         return;
     }
     const int64_t per_group = (a.group + together - 1) / together, all = a.rows / a.group * per_group;
-    for (int64_t c = blockIdx.x; c < all; c += gridDim.x) {
-        const int64_t part = c / per_group, row0 = (c - part * per_group) * together;
-        const int rows = (int)min((int64_t)together, a.group - row0);
-        const uintptr_t from = reinterpret_cast<uintptr_t>(a.src + part * a.group_stride + row0 * a.ld), to = from + 2 * ((rows - 1) * a.ld + a.d), base = from & ~(uintptr_t)15;
-        const int count = (int)((to - base + 15) / 16);
-        for (int i = threadIdx.x; i < count; i += 256) {
-            const uintptr_t p = base + 16 * (uintptr_t)i;
-            uint4 x;
-            if (p >= from && p + 16 <= to) {
-                x = *reinterpret_cast<const uint4*>(p);
-            } else {
+    constexpr int LOADS = ALIGN_BYTES / 16 / 256 + 1;
+    struct Chunk {
+        int64_t row0;  // of all rows
+        int rows;
+        uintptr_t from, to, base;
+    };
+    auto chunk = [&](int64_t c) {
+        const int64_t part = c / per_group, first = (c - part * per_group) * together;
+        Chunk k;
+        k.row0 = part * a.group + first;
+        k.rows = (int)min((int64_t)together, a.group - first);
+        k.from = reinterpret_cast<uintptr_t>(a.src + part * a.group_stride + first * a.ld);
+        k.to = k.from + 2 * ((k.rows - 1) * a.ld + a.d);
+        k.base = k.from & ~(uintptr_t)15;
+        return k;
+    };
+    uint4 x[LOADS];
+    auto bring = [&](const Chunk& k) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const uintptr_t p = k.base + 16 * (uintptr_t)(threadIdx.x + 256 * i);
+            if (p >= k.from && p + 16 <= k.to) {
+                x[i] = *reinterpret_cast<const uint4*>(p);
+            } else if (p < k.to) {  // a word that is not the rows' alone
                 uint32_t w[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uintptr_t e = p + 4 * k;
-                    const uint32_t lo = e >= from && e < to ? *reinterpret_cast<const uint16_t*>(e) : 0u, hi = e + 2 >= from && e + 2 < to ? *reinterpret_cast<const uint16_t*>(e + 2) : 0u;
-                    w[k] = lo | hi << 16;
+                for (int h = 0; h < 4; ++h) {
+                    const uintptr_t e = p + 4 * h;
+                    const uint32_t lo = e >= k.from && e < k.to ? *reinterpret_cast<const uint16_t*>(e) : 0u, hi = e + 2 >= k.from && e + 2 < k.to ? *reinterpret_cast<const uint16_t*>(e + 2) : 0u;
+                    w[h] = lo | hi << 16;
                 }
-                x = make_uint4(w[0], w[1], w[2], w[3]);
+                x[i] = make_uint4(w[0], w[1], w[2], w[3]);
             }
-            words[i] = x;
         }
-        __syncthreads();
-        const uint32_t* w = reinterpret_cast<const uint32_t*>(words);
-        const int shift = (int)(from - base) / 2, ld = (int)a.ld;  // in values
-        uint4* out = reinterpret_cast<uint4*>(a.dst) + (part * a.group + row0) * units;
-        for (int i = threadIdx.x; i < rows * units; i += 256) {
-            const int row = i / units, u = i - row * units, at = shift + row * ld + 8 * u, valid = a.d - 8 * u;
-            uint32_t x[4];
+    };
+    int64_t c = blockIdx.x;
+    if (c >= all) return;
+    Chunk now = chunk(c);
+    bring(now);
+    const int ld = (int)a.ld, per_row = 4 * units, rows_on = 256 / per_row, on = 256 - rows_on * per_row;  // in values; in words of 4 bytes
+    for (;;) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int e = at + 2 * k;
-                x[k] = 2 * k < valid ? __funnelshift_r(w[e >> 1], w[(e >> 1) + 1], 16 * (e & 1)) : 0u;
-                if (2 * k + 1 >= valid) x[k] &= 0xFFFFu;
-            }
-            out[i] = make_uint4(x[0], x[1], x[2], x[3]);
+        for (int i = 0; i < LOADS; ++i)
+            if (now.base + 16 * (uintptr_t)(threadIdx.x + 256 * i) < now.to) words[threadIdx.x + 256 * i] = x[i];
+        __syncthreads();
+        const Chunk these = now;
+        c += gridDim.x;
+        const bool more = c < all;
+        if (more) {  // the next ones are on their way while these are cut up
+            now = chunk(c);
+            bring(now);
         }
+        // 4 bytes a thread, so that a warp reads and writes neighbouring ones
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(words);
+        const int shift = (int)(these.from - these.base) / 2;
+        uint32_t* out = reinterpret_cast<uint32_t*>(a.dst) + these.row0 * per_row;
+        int row = threadIdx.x / per_row, column = threadIdx.x - row * per_row;
+        for (int i = threadIdx.x; i < these.rows * per_row; i += 256) {
+            const int e = shift + row * ld + 2 * column, valid = a.d - 2 * column;
+            uint32_t v = __funnelshift_r(w[e >> 1], w[(e >> 1) + 1], 16 * (e & 1));
+            if (valid < 2) v = valid == 1 ? v & 0xFFFFu : 0u;
+            out[i] = v;
+            row += rows_on;
+            column += on;
+            if (column >= per_row) {
+                column -= per_row;
+                ++row;
+            }
+        }
+        if (!more) return;
         __syncthreads();
     }
 }
@@ -118,44 +151,53 @@ struct SumsArgs {
 
 // What pairs of blocks leave of sums over rows (layer_pairs.cuh), added up in order: a block for 32 columns of dZ and a part (or all parts:
 // shared), the last of a part for its slope's gradient.
+constexpr int SUMS_THREADS = 1024;
 template <class O>
-__global__ void __launch_bounds__(256) layer_sums_kernel(const __grid_constant__ SumsArgs a) {
-    __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
-    __shared__ double red[256];
-    __shared__ int32_t place_start[MOST_PLACES + 1];
+__global__ void __launch_bounds__(SUMS_THREADS) layer_sums_kernel(const __grid_constant__ SumsArgs a) {
+    __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32], place_start[MOST_PLACES + 1];
+    __shared__ double red[SUMS_THREADS];
     wait_for_kernel_before();
     number_tiles(a.offsets, a.n, a.G, a.tile_rows, a.tiles, tile_start, warp_sums);
+    const int64_t tiles = tile_start[a.G];
+    for (int i = threadIdx.x; i <= a.places; i += SUMS_THREADS) place_start[i] = (int)(tiles * i / a.places);
+    __syncthreads();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const bool of_slope = (int)blockIdx.x * 32 >= a.columns, shared = of_slope ? a.slope_shared : a.shared;
     if ((int)blockIdx.y > 0 && shared) return;
     const int column = 32 * blockIdx.x + lane, first = shared ? 0 : blockIdx.y, last = shared ? a.G : first + 1;
-    const int64_t tiles = tile_start[a.G];
-    for (int i = threadIdx.x; i <= a.places; i += 256) place_start[i] = (int)(tiles * i / a.places);
-    __syncthreads();
     double s = 0.0;
     for (int part = first; part < last; ++part) {
         const int from = tile_start[part], to = tile_start[part + 1];
         if (from == to) continue;
-        int i = (int)((int64_t)from * a.places / tiles);
+        // the places whose tiles are among the part's; those without tiles have left no slot
+        int i = (int)((int64_t)from * a.places / tiles), end;
         while (place_start[i + 1] <= from) ++i;
+        for (end = i + 1; end < a.places && place_start[end] < to;) ++end;
+        if (!of_slope) {  // eight warps for the sums of a slot, every fourth slot
+            const float* p = a.column_slots + (8 * (int64_t)(i + part) + (warp & 7)) * a.columns + min(column, a.columns - 1);
 #pragma unroll 4
-        for (; i < a.places; ++i) {
-            if (place_start[i] >= to || place_start[i] == place_start[i + 1]) continue;  // (not among the part's; without tiles, which has left no slot)
-            const int64_t slot = 8 * (int64_t)(i + part);
-            if (!of_slope) s += column < a.columns ? a.column_slots[(slot + warp) * a.columns + column] : 0.f;
-            else
-                for (int k = threadIdx.x; k < 32 * a.n_tiles; k += 256) s += a.slope_slots[slot * 4 * a.n_tiles + k];
+            for (int k = i + (warp >> 3); k < end; k += 4) {
+                const float v = p[8 * (int64_t)(k - i) * a.columns];
+                s += place_start[k] != place_start[k + 1] ? v : 0.f;
+            }
+        } else {
+            const int per = 32 * a.n_tiles;
+            for (int k = threadIdx.x; k < (end - i) * per; k += SUMS_THREADS) {
+                const int at = i + k / per;
+                if (place_start[at] != place_start[at + 1]) s += a.slope_slots[(int64_t)(i + part) * per + k];
+            }
         }
     }
     red[threadIdx.x] = s;
     __syncthreads();
+    if (warp) return;
+#pragma unroll 8
+    for (int k = 1; k < SUMS_THREADS / 32; ++k) s += red[32 * k + lane];
     if (!of_slope) {
-        if (warp) return;
-        for (int k = 1; k < 8; ++k) s += red[32 * k + lane];
         if (column < a.columns && a.place_of(column) >= 0) static_cast<O*>(a.db)[blockIdx.y * a.db_stride + a.place_of(column)] = from_f32<O>((float)s);
-    } else if (threadIdx.x == 0) {
-        for (int k = 1; k < 256; ++k) s += red[k];
-        a.dslope[blockIdx.y * a.dslope_stride] = (float)s;
+    } else {
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        if (lane == 0) a.dslope[blockIdx.y * a.dslope_stride] = (float)s;
     }
 }
 
@@ -416,7 +458,7 @@ extern "C" int32_t rtma_grouped_layer_grad(rtma_ctx* ctx, const rtma_layer_desc*
         m.shared = G > 1 && db_stride == 0; m.slope_shared = G > 1 && dslope_stride == 0;
         void (*kernel)(SumsArgs) = d->grad_dtype == RTMA_F32 ? layer_sums_kernel<float> : d->dtype == RTMA_BF16 ? layer_sums_kernel<__nv_bfloat16> : layer_sums_kernel<__half>;
         KernelScope ks(ctx, KC_REDUCE_SGD, stream);
-        launch_kernel(kernel, dim3((unsigned)(ceil_div(m.columns, 32) + (dslope ? 1 : 0)), (unsigned)G), 256, 0, stream, m);
+        launch_kernel(kernel, dim3((unsigned)(ceil_div(m.columns, 32) + (dslope ? 1 : 0)), (unsigned)G), SUMS_THREADS, 0, stream, m);
         RTMA_LAUNCH_CHECK(ctx);
     }
     if (dX && n > 0)

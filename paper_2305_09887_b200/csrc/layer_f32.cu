@@ -322,6 +322,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) layer_f3
     uint8_t* const w_planes = raw + RAW_STAGES * RAW_BYTES;
     const uint32_t a_planes = tc::smem_u32(w_planes) + STAGES * W_BYTES, slabs = a_planes + STAGES * A_BYTES;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x >= 32 && threadIdx.x < 32 + DRAIN_WARPS * SLABS) {
+        tc::mbar_init(&sh.side[(threadIdx.x - 32) / SLABS][threadIdx.x % SLABS], 1);
+        tc::fence_barrier_init();
+    }
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
             tc::mbar_init(&sh.full[s], 1 + 2 * SPLIT_WARPS);  // the planes of the matrix; both blocks' rows
@@ -333,7 +337,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) layer_f3
             tc::mbar_init(&sh.raw_full[s], 1);
             tc::mbar_init(&sh.raw_free[s], SPLIT_WARPS);
         }
-        for (int i = 0; i < DRAIN_WARPS * SLABS; ++i) tc::mbar_init(&sh.side[i / SLABS][i % SLABS], 1);
         sh.abort = 0;
         tc::fence_barrier_init();
     }

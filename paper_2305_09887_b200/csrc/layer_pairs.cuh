@@ -296,7 +296,8 @@ __device__ __forceinline__ void pair_drain(const LayerArgs& a, PairShared& sh, u
                     add_columns<T>(other, lane, sums[1]);
                 }
             } else {
-                outlet.close(a, slab, row0, c, rows, cols, whole, out, a.ldo, lane);
+                if (!GRADIENT && !a.vo && a.go >= 4 && cols % 2 == 0) outlet.close_words(a, slab, rows, cols, out, a.ldo, lane);
+                else outlet.close(a, slab, row0, c, rows, cols, whole, out, a.ldo, lane);
                 if constexpr (GRADIENT)
                     if (a.column_slots) add_columns<T>(slab, lane, sums[i]);
             }
@@ -341,6 +342,10 @@ __device__ __forceinline__ void pair_body(const LayerArgs& a) {
     uint8_t* const held_bytes = ring_bytes + F::RING_BYTES;
     const uint32_t ring = tc::smem_u32(ring_bytes), held = ring + F::RING_BYTES, slabs = held + F::HELD_BYTES;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x >= 32 && threadIdx.x < 64) {
+        tc::mbar_init(&sh.side[threadIdx.x >> 1 & 15][threadIdx.x & 1], 1);
+        tc::fence_barrier_init();
+    }
     if (threadIdx.x == 0) {
         for (int s = 0; s < F::STAGES; ++s) {
             tc::mbar_init(&sh.full[s], 1);
@@ -352,7 +357,6 @@ __device__ __forceinline__ void pair_body(const LayerArgs& a) {
         }
         tc::mbar_init(&sh.held_full, 1);
         tc::mbar_init(&sh.held_empty, 1);
-        for (int i = 0; i < 32; ++i) tc::mbar_init(&sh.side[i >> 1][i & 1], 1);
         sh.abort = 0;
         tc::fence_barrier_init();
     }

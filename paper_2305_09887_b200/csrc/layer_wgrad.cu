@@ -339,6 +339,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) layer_wg
 template <class O>
 __global__ void __launch_bounds__(256) layer_wgrad_reduce_kernel(const __grid_constant__ GradArgs a) {
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32];
+    __shared__ float4 red[8][32];
     wait_for_kernel_before();
     number_tiles(a.offsets, a.n, a.G, a.n ? *a.chunk_rows : 1, a.tiles, tile_start, warp_sums, a.span);
     auto add = [](float4& s, const float4 v) {
@@ -349,16 +350,28 @@ __global__ void __launch_bounds__(256) layer_wgrad_reduce_kernel(const __grid_co
     };
     const int part = blockIdx.y, from = tile_start[part], count = tile_start[part + 1] - from, quads = (int)a.ldo / 4;
     const int64_t slot = (a.d_in + 2) * a.ldo, all = (int64_t)(a.d_in + (a.sums ? 1 : 0)) * quads;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-        const int row = (int)(i / quads), col = 4 * (int)(i - (int64_t)row * quads);
-        const float* p = a.slots + from * slot + 4 * i;
+    // where there are many slots and few quads, eight warps share the slots of 32 quads; otherwise every thread has a quad of its own
+    const int shares = count >= 8 && gridDim.x * 32 >= all ? 8 : 1, share = shares > 1 ? threadIdx.x >> 5 : 0, together = 256 / shares;
+    for (int64_t base = (int64_t)blockIdx.x * together; base < all; base += (int64_t)gridDim.x * together) {
+        const int64_t i = base + (shares > 1 ? threadIdx.x & 31 : threadIdx.x);
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        const int row = (int)(i / quads), col = 4 * (int)(i - (int64_t)row * quads);
+        if (i < all) {
+            const float* p = a.slots + from * slot + 4 * i;
 #pragma unroll 4
-        for (int t = 0; t < count; ++t, p += slot) add(s, *reinterpret_cast<const float4*>(p));
-        if (row == a.d_in) {  // the other half's
-            p = a.slots + from * slot + 4 * i + a.ldo;
-            for (int t = 0; t < count; ++t, p += slot) add(s, *reinterpret_cast<const float4*>(p));
+            for (int t = share; t < count; t += shares) add(s, *reinterpret_cast<const float4*>(p + t * slot));
+            if (row == a.d_in)  // the other half of the rows'
+                for (int t = share; t < count; t += shares) add(s, *reinterpret_cast<const float4*>(p + t * slot + a.ldo));
         }
+        if (shares > 1) {
+            __syncthreads();
+            red[share][threadIdx.x & 31] = s;
+            __syncthreads();
+            if (share) continue;
+#pragma unroll
+            for (int k = 1; k < 8; ++k) add(s, red[k][threadIdx.x & 31]);
+        }
+        if (i >= all) continue;
         O* to = row < a.d_in ? static_cast<O*>(a.dW) + part * a.dw_stride + (int64_t)row * a.real_out : static_cast<O*>(a.db) + part * a.db_stride;
         const int second = col >= a.width ? 1 : 0, c = col - second * a.width;  // (halves are multiples of 8)
         to += second * a.real_width + c;
@@ -428,7 +441,7 @@ int32_t layer_dw(rtma_ctx* ctx, const char* who, const rtma_layer_desc* d, int64
     }
     KernelScope ks(ctx, KC_REDUCE_SGD, stream);
     void (*reduce)(GradArgs) = d->grad_dtype == RTMA_F32 ? layer_wgrad_reduce_kernel<float> : bf16 ? layer_wgrad_reduce_kernel<__nv_bfloat16> : layer_wgrad_reduce_kernel<__half>;
-    const int64_t blocks = ceil_div((int64_t)(d_in + 1) * a.ldo / 4, 256);
+    const int64_t blocks = ceil_div((int64_t)(d_in + 1) * a.ldo / 4, 32);
     launch_kernel(reduce, dim3((unsigned)std::min<int64_t>(blocks, std::max(1, 8 * ctx->sm_count / a.G)), (unsigned)a.G), 256, 0, stream, a);
     RTMA_LAUNCH_CHECK(ctx);
     return RTMA_OK;
