@@ -9,7 +9,7 @@
 namespace grouped {
 
 enum Mode { FORWARD, INPUT_GRADIENT, WEIGHT_GRADIENT };
-constexpr int MAX_STAGES = 6;
+constexpr int MAX_STAGES = 6, MAX_ACCUMULATORS = 3;
 constexpr int SMEM_MOST = 232448;  // bytes a block can have
 
 struct LinearArgs {
@@ -20,7 +20,6 @@ struct LinearArgs {
     int m_tiles, n_tiles;      // tiles of one row tile: m_tiles (dw) x n_tiles
     int BN;
     int d_in, d_out;
-    int up;                    // two matrices side by side: columns from one to the other
     const void *A, *B;         // rows; matrices (forward, dx) or rows (dw)
     int64_t lda, ldb, w_stride;
     int va, vb;                // granules of the rows (bytes)
@@ -33,9 +32,8 @@ struct LinearArgs {
     int bias_rows;             // dw: partial sums of the bias gradient in a slot, one row per warp that adds them up
     void* out;                 // dw: the slots, [row tile][d_in + bias_rows][ldo]
     int64_t ldo;
-    void *dW, *db;             // dw: in float, or in the rows' type
+    float *dW, *db;
     int64_t dw_stride, db_stride;
-    int fold, fold_real;       // dw: dY's columns are runs of `fold`, of which the first fold_real are dW's
     int32_t* chunk_rows;       // dw: where the rows of a row tile are left for the reduction
     int* error_word;
     CUtensorMap map_a, map_b;  // operands that are fetched by bulk-tensor loads
@@ -61,7 +59,7 @@ __host__ __device__ __forceinline__ int fit_chunk(int least, int most, int64_t t
 
 struct Shared {
     uint64_t full[MAX_STAGES], empty[MAX_STAGES];
-    uint64_t acc_full[2], acc_empty[2];
+    uint64_t acc_full[MAX_ACCUMULATORS], acc_empty[MAX_ACCUMULATORS];
     uint32_t tmem_base;
     int abort;
     int32_t warp_sums[32];
@@ -340,12 +338,3 @@ struct BiasHolder {
 constexpr int SPLIT_COLUMNS = 128, SPLIT_DW_COLUMNS = 64, SPLIT_BIAS_ROWS = 8, SPLIT_BLOCKS_PER_SM = 2;
 size_t split_planes_bytes(const grouped::LinearArgs& a);
 int32_t launch_split(rtma_ctx* ctx, int mode, grouped::LinearArgs& a, void* planes, int cls, cudaStream_t stream);
-
-// Products with the matrices of the parts, and the gradient of these, for calls that are made of several (grouped_linear.cu).  scratch:
-// only says how much the call would take.  The gradients come in out_dtype; of every `fold` columns of dY the first fold_real have one.
-int32_t grouped_rows(rtma_ctx* ctx, const char* who, bool transposed, int32_t dtype, int64_t n, int32_t G, const int64_t* offsets, int32_t d_in, int32_t d_out,
-                     const void* A, int64_t lda, const void* W, int64_t w_stride, const void* b, int64_t b_stride, void* out, int64_t ldo, size_t* scratch,
-                     cudaStream_t stream);
-int32_t grouped_dw(rtma_ctx* ctx, const char* who, int32_t dtype, int64_t n, int32_t G, const int64_t* offsets, int32_t d_in, int32_t d_out, const void* X,
-                   int64_t ldx, const void* dY, int64_t lddy, int fold, int fold_real, int32_t out_dtype, void* dW, int64_t dw_stride, void* db, int64_t db_stride, size_t* scratch,
-                   cudaStream_t stream);

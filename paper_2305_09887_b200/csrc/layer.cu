@@ -417,9 +417,8 @@ extern "C" int32_t rtma_grouped_layer_grad(rtma_ctx* ctx, const rtma_layer_desc*
     DeviceScope on(ctx->device);
     RTMA_CUDA(ctx, on.status);
     int64_t w_stride = d->w_stride;
-    const void *dz = plain ? dY : dZ, *x0 = X, *dz0 = dz;  // x0, dz0: as the caller has them, outside of the scratch
+    const void* dz = plain ? dY : dZ;
     int64_t ldz = plain ? lddy : lddz;
-    const int64_t ldx0 = ldx, ldz0 = ldz;
     // All scratch at once: inside a capture nothing is enqueued unless everything fits.
     const Plan p = make_plan(ctx, d, n, G, X, ldx, W, dY, lddy, true);
     const bool column_sums = db && !f32 && !plain && n > 0;  // the bias gradient comes with dZ
@@ -427,8 +426,7 @@ extern "C" int32_t rtma_grouped_layer_grad(rtma_ctx* ctx, const rtma_layer_desc*
                  slot_bytes = column_bytes + (dslope ? sizeof(float) * slot_rows * 4 * p.n_tiles : 0);
     size_t dw_bytes = 0;
     auto weights = [&](size_t* scratch) {
-        return f32 ? grouped_dw(ctx, who, d->dtype, n, G, offsets, d->d_in, wide, x0, ldx0, dz0, ldz0, width, d->d_out, RTMA_F32, dW, dw_stride, db, db_stride, scratch, stream)
-                   : layer_dw(ctx, who, d, n, G, offsets, X, ldx, dz, ldz, dW, dw_stride, db, db_stride, !column_sums, p.end, scratch, stream);
+        return layer_dw(ctx, who, d, n, G, offsets, X, ldx, dz, ldz, width, dW, dw_stride, db, db_stride, !column_sums, p.end, scratch, stream);
     };
     if (dW) RTMA_TRY(weights(&dw_bytes));
     RTMA_TRY(prepare_row_call(ctx, std::max(p.end + slot_bytes, dw_bytes), stream));
@@ -463,6 +461,6 @@ extern "C" int32_t rtma_grouped_layer_grad(rtma_ctx* ctx, const rtma_layer_desc*
     }
     if (dX && n > 0)
         RTMA_TRY(f32 ? rows_gradient_f32(ctx, p, d, n, G, offsets, dz, ldz, dX, lddx, stream)
-                     : grouped_rows(ctx, who, true, d->dtype, n, G, offsets, d->d_in, p.halves * p.up, dz, ldz, W, w_stride, nullptr, 0, dX, lddx, nullptr, stream));
+                     : rtma_grouped_linear_dx(ctx, d->dtype, n, G, offsets, d->d_in, p.halves * p.up, dz, ldz, W, w_stride, dX, lddx, stream));
     return dW ? weights(nullptr) : RTMA_OK;
 }

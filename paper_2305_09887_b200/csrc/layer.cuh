@@ -9,6 +9,7 @@ namespace grouped {
 
 struct LayerArgs : LinearArgs {
     int width;            // columns of the result (of each of a gated layer's two matrices)
+    int up;               // columns from one of the two matrices to the other
     int act;
     const float* slope;
     int64_t slope_stride;
@@ -25,7 +26,8 @@ struct LayerArgs : LinearArgs {
 };
 
 #ifdef __CUDACC__
-constexpr int PAIR_BM = 128;  // rows of a tile that a block of a pair has
+constexpr int PAIR_BM = 128;            // rows of a tile that a block of a pair has
+constexpr int SLAB_BYTES = 32 * 128;    // of an operand: 32 rows of 64 16-bit values
 // A pair's walk down its row tiles; rows and row0 are the block's own.
 struct PairWalk {
     int t, end, part, left;  // left: rows of the part from the tile's first on
@@ -163,8 +165,7 @@ int32_t split_matrices(rtma_ctx* ctx, const float* W, int64_t w_stride, int part
 // 16-bit rows on 16-byte boundaries (layer_pairs.cuh).
 int32_t launch_layer_bf16(rtma_ctx* ctx, grouped::LayerArgs& a, bool gated, bool gradient, unsigned grid, cudaStream_t stream);
 int32_t launch_layer_f16(rtma_ctx* ctx, grouped::LayerArgs& a, bool gated, bool gradient, unsigned grid, cudaStream_t stream);
-// The weight gradient of 16-bit rows on 16-byte boundaries (layer_wgrad.cu), from dZ with its halves as wide as the layer rounded up to 8; in the
-// scratch from `at` on.  sums: db is formed here.  scratch: only says how much of it the
-// call takes, from its start.
+// The weight gradient of rows on 16-byte boundaries (layer_wgrad.cu), from dZ with halves of `width` columns; in the scratch from `at` on.  sums: db is formed
+// here.  scratch: only says how much of it the call takes, from its start.
 int32_t layer_dw(rtma_ctx* ctx, const char* who, const rtma_layer_desc* d, int64_t n, int32_t G, const int64_t* offsets, const void* X, int64_t ldx, const void* dZ,
-                 int64_t lddz, void* dW, int64_t dw_stride, void* db, int64_t db_stride, bool sums, size_t at, size_t* scratch, cudaStream_t stream);
+                 int64_t lddz, int width, void* dW, int64_t dw_stride, void* db, int64_t db_stride, bool sums, size_t at, size_t* scratch, cudaStream_t stream);

@@ -15,13 +15,13 @@
 // and the slope's gradient stay in registers until the part changes, and are left in a slot of (place of the pair + part), which no two share.
 #pragma once
 
-#include "grouped_rows.cuh"
 #include "layer.cuh"
 
 namespace {
 
 using namespace grouped;
 
+constexpr int BM = PAIR_BM, BK = 64;
 constexpr int RESIDENT_TERMS = 256;  // of the contraction, up to which the matrix stays in shared memory
 
 template <class T_, bool GATED_, bool GRADIENT_, bool RESIDENT_>

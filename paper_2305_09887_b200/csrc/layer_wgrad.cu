@@ -10,8 +10,8 @@
 // the weights' do.
 #include <algorithm>
 
-#include "grouped_rows.cuh"
 #include "layer.cuh"
+#include "split.cuh"
 
 RTMA_BOUNDS_TU()
 
@@ -19,10 +19,15 @@ namespace {
 
 using namespace grouped;
 
-constexpr int LEFT = 256, STAGES = 6, STAGE_BYTES = 2 * 128 * 128, DRAIN_WARPS = 16, THREADS = 32 * (DRAIN_WARPS + 4);
+constexpr int LEFT = 256, BK = 64, STAGES = 6, STAGE_BYTES = 2 * 128 * 128, DRAIN_WARPS = 16, THREADS = 32 * (DRAIN_WARPS + 4);
 constexpr int DYNAMIC_BYTES = 1024 + STAGES * STAGE_BYTES;
 constexpr int ACC_STAGES = 2;  // of 64 rows, after which the accumulator is taken
 constexpr int DW_WAVES = 2;    // tiles for every pair that runs at a time
+// fp32 rows: 32 of them a stage, 64 columns of the right operand in a block
+constexpr int F32_BK = 32, F32_HALF = 64, RAW_STAGES = 3, RAW_BYTES = F32_BK * (128 + F32_HALF) * 4, F32_STAGES = 3, ATOM_BYTES = 3 * F32_BK * 64 * 2;
+constexpr int F32_DRAIN_WARPS = 8, SPLIT_WARPS = 12, F32_THREADS = 32 * (F32_DRAIN_WARPS + 4 + SPLIT_WARPS);
+constexpr int F32_DYNAMIC_BYTES = 1024 + RAW_STAGES * RAW_BYTES + F32_STAGES * 3 * ATOM_BYTES;
+constexpr int F32_OTHER_REGISTERS = 64;  // 256 x 104 + 512 x 64 = 59,392 of 768 x 80
 constexpr int SUMS_REGISTERS = 104, OTHER_REGISTERS = 64;  // 512 x 104 + 128 x 64 = 640 x 96
 
 struct GradArgs : LinearArgs {  // A, map_a: the left operand, B, map_b: the right one
@@ -30,19 +35,27 @@ struct GradArgs : LinearArgs {  // A, map_a: the left operand, B, map_b: the rig
     bool swapped;      // dZ is the left one
     int half;          // columns of the right one that a block brings
     bool sums;         // of dZ's columns are wanted
-    float* slots;      // [row tile][d_in + 2][ldo], two sums of dZ's columns behind the weights
+    int sum_rows;      // sums of dZ's columns in a slot, behind the weights: of as many shares of the rows
+    float* slots;      // [row tile][d_in + sum_rows][ldo]
     int width, real_width;  // of dZ's halves, with and without what was rounded up
     int real_out;      // columns of dW
+    void *to_w, *to_b; // dW and db, in float or in the rows' type
 };
+
+template <int SIZE>
+__device__ __forceinline__ void copy(uint32_t dst, const void* src, int bytes) {  // the rest of the SIZE bytes becomes zero
+    asm volatile("cp.async.cg.shared.global [%0], [%1], %3, %2;" ::"r"(dst), "l"(src), "r"(bytes), "n"(SIZE) : "memory");
+}
 
 struct GradShared : Shared {
     uint64_t ready[STAGES], free[STAGES];  // stages that have come, in either block; whose columns have been summed
 };
 
+template <int STEP>
 struct GradWalk {
     int tile, row_tile, part, m0, n0, k_end, k0;
     int64_t row0;
-    __device__ __forceinline__ bool at(const GradArgs& a, const GradShared& sh) {
+    __device__ __forceinline__ bool at(const GradArgs& a, const Shared& sh) {
         const int per = a.m_tiles * a.n_tiles;
         row_tile = tile / per;
         if (row_tile >= sh.tile_start[a.G]) return false;
@@ -57,19 +70,19 @@ struct GradWalk {
         k0 = 0;
         return true;
     }
-    __device__ __forceinline__ bool first(const GradArgs& a, const GradShared& sh) {
+    __device__ __forceinline__ bool first(const GradArgs& a, const Shared& sh) {
         tile = blockIdx.x >> 1;
         part = 0;
         return at(a, sh);
     }
-    __device__ __forceinline__ bool next_tile(const GradArgs& a, const GradShared& sh) {
+    __device__ __forceinline__ bool next_tile(const GradArgs& a, const Shared& sh) {
         tile += gridDim.x >> 1;
         return at(a, sh);
     }
-    __device__ __forceinline__ bool last_stage() const { return k0 + BK >= k_end; }
-    __device__ __forceinline__ bool next(const GradArgs& a, const GradShared& sh) {  // the next stage
+    __device__ __forceinline__ bool last_stage() const { return k0 + STEP >= k_end; }
+    __device__ __forceinline__ bool next(const GradArgs& a, const Shared& sh) {  // the next stage
         if (!last_stage()) {
-            k0 += BK;
+            k0 += STEP;
             return true;
         }
         return next_tile(a, sh);
@@ -86,7 +99,7 @@ __device__ __forceinline__ void grad_producer(const GradArgs& a, GradShared& sh,
         tc::prefetch_tensormap(&a.map_b);
     }
     const int atoms = (a.half + 63) / 64;
-    GradWalk w;
+    GradWalk<BK> w;
     tc::RingAt at;
     int filled = 0;  // stages, STAGES at most
     bool ok = true;
@@ -110,7 +123,8 @@ __device__ __forceinline__ void grad_producer(const GradArgs& a, GradShared& sh,
                 if (valid) p += (w.row0 + k) * (is_left ? a.lda : a.ldb) + c;
                 copy<16>(tc::smem_u32(stage) + atom * 2 * SLAB_BYTES + row * 128 + ((unit ^ (row & 7)) << 4), p, valid * (int)sizeof(T));
             }
-            copies_done();
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            tc::fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) tc::mbar_arrive_cluster(bar);
         } else if (lane == 0) {
@@ -138,7 +152,7 @@ __device__ __forceinline__ void grad_multiplier(const GradArgs& a, GradShared& s
     const uint32_t format = std::is_same<T, __half>::value ? 0u : 1u;  // fp16 or bf16 operands, fp32 sums
     const uint32_t idesc = (1u << 4) | (format << 7) | (format << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(2 * a.half >> 3) << 17) | ((uint32_t)(LEFT >> 4) << 24);
     const uint64_t desc = tc::smem_desc_sw128(0, 2 * SLAB_BYTES, 1024);  // atoms of 64 columns lie two slabs apart
-    GradWalk w;
+    GradWalk<BK> w;
     tc::RingAt at, acc;
     int held = 0;  // stages in the accumulator
     for (bool more = w.first(a, sh); more; more = w.next(a, sh)) {
@@ -197,35 +211,27 @@ struct ColumnSums {
     }
 };
 
-template <class T>
-__device__ __forceinline__ void grad_drain(const GradArgs& a, GradShared& sh, uint32_t ring, int rank) {
+// before(w, k0): what is done before the accumulator of the rows from k0 on is waited for; after(w): at the end of a tile.
+// RING, SPACING: of accumulators and their columns.  TURNED: of every 64 columns of an operand the upper 32 lie with the halves of each eight the other way
+// around (see grad_f32_splitter).
+template <int STEP, int TAKEN, int RING, int SPACING, bool TURNED, class S, class Before, class After>
+__device__ __forceinline__ void grad_drain(const GradArgs& a, S& sh, int rank, Before before, After after) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, slice = warp >> 2;
     const uint32_t tmem = sh.tmem_base + ((uint32_t)(32 * quarter) << 16) + 64 * slice;
     const bool mine = 64 * slice < 2 * a.half;
-    GradWalk w;
-    tc::RingAt acc, at;
-    ColumnSums<T> sums;
+    GradWalk<STEP> w;
+    tc::RingAt acc;
     for (bool more = w.first(a, sh); more; more = w.next_tile(a, sh)) {
-        sums.clear();
         f2 total[32];
 #pragma unroll
         for (int j = 0; j < 32; ++j) total[j] = pack2(0.f, 0.f);
-        for (int k0 = 0; k0 < w.k_end; k0 += ACC_STAGES * BK) {
-            if (a.sums) {
-                for (int k = k0; k < min(k0 + ACC_STAGES * BK, w.k_end); k += BK) {
-                    if (!wait_for<true>(&sh.ready[at.s], at.phase, sh, a.error_word)) return;
-                    __syncwarp();
-                    if (w.sums(a)) sums.add(ring + at.s * STAGE_BYTES + (a.swapped ? 0 : 4 * SLAB_BYTES), warp, lane, w.k_end - k);
-                    __syncwarp();
-                    if (lane == 0) tc::mbar_arrive(&sh.free[at.s]);
-                    at.advance(STAGES);
-                }
-            }
+        for (int k0 = 0; k0 < w.k_end; k0 += TAKEN) {
+            if (!before(w, k0)) return;
             if (!wait_for<true>(&sh.acc_full[acc.s], acc.phase, sh, a.error_word)) return;
             __syncwarp();
             tc::tc_fence_after_sync();
             if (mine) {
-                const uint32_t from = tmem + acc.s * 256;
+                const uint32_t from = tmem + acc.s * SPACING;
                 uint32_t x[2][8];
                 tc::tmem_load_issue_8(from, x[0]);
 #pragma unroll
@@ -239,22 +245,25 @@ __device__ __forceinline__ void grad_drain(const GradArgs& a, GradShared& sh, ui
             tc::tc_fence_before_sync();
             __syncwarp();
             if (lane == 0) tc::mbar_arrive_remote(tc::leader_addr(&sh.acc_empty[acc.s]));  // (a pair's warps all report to the first block)
-            acc.advance(2);
+            acc.advance(RING);
         }
-        if (w.sums(a)) {
-            const int of_block = a.swapped ? 128 : a.half, first = a.swapped ? w.m0 + 128 * rank : w.n0 + a.half * rank;
-            float* const to = a.slots + ((int64_t)w.row_tile * (a.d_in + 2) + a.d_in + (warp & 1)) * a.ldo + first;
+        after(w);
+        const int m = w.m0 + 128 * rank + 32 * quarter + (TURNED && (quarter & 1) ? lane ^ 4 : lane), n = w.n0 + 64 * slice;
+        const int cols = min(64, min(2 * a.half - 64 * slice, a.right - n));
+        if constexpr (TURNED) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float s = sums.total(h);
-                const int j = 16 * (warp >> 1) + 8 * h + (lane >> 2);
-                if ((lane & 3) == 0 && j < of_block && first + j < a.d_out) to[j] = s;
+            for (int q = 0; q < 8; ++q) {
+                if ((64 * slice + 8 * q) % a.half < 32) continue;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const f2 t = total[4 * q + j];
+                    total[4 * q + j] = total[4 * q + 2 + j];
+                    total[4 * q + 2 + j] = t;
+                }
             }
         }
-        const int m = w.m0 + 128 * rank + 32 * quarter + lane, n = w.n0 + 64 * slice;
-        const int cols = min(64, min(2 * a.half - 64 * slice, a.right - n));
         if (m < a.left && cols > 0) {
-            float* const slot = a.slots + (int64_t)w.row_tile * (a.d_in + 2) * a.ldo;
+            float* const slot = a.slots + (int64_t)w.row_tile * (a.d_in + a.sum_rows) * a.ldo;
             if (a.swapped) {  // a lane's column of dZ: neighbours beside one another
                 float* to = slot + (int64_t)n * a.ldo + m;
 #pragma unroll
@@ -317,7 +326,35 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) layer_wg
     const int rank = (int)tc::cluster_rank();
     if (warp < DRAIN_WARPS) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SUMS_REGISTERS));
-        grad_drain<T>(a, sh, ring, rank);
+        tc::RingAt at;
+        ColumnSums<T> sums;
+        sums.clear();
+        grad_drain<BK, ACC_STAGES * BK, 2, 256, false>(
+            a, sh, rank,
+            [&](const GradWalk<BK>& w, int k0) {
+                if (!a.sums) return true;
+                for (int k = k0; k < min(k0 + ACC_STAGES * BK, w.k_end); k += BK) {
+                    if (!wait_for<true>(&sh.ready[at.s], at.phase, sh, a.error_word)) return false;
+                    __syncwarp();
+                    if (w.sums(a)) sums.add(ring + at.s * STAGE_BYTES + (a.swapped ? 0 : 4 * SLAB_BYTES), warp, lane, w.k_end - k);
+                    __syncwarp();
+                    if (lane == 0) tc::mbar_arrive(&sh.free[at.s]);
+                    at.advance(STAGES);
+                }
+                return true;
+            },
+            [&](const GradWalk<BK>& w) {
+                if (!w.sums(a)) return;
+                const int of_block = a.swapped ? 128 : a.half, first = a.swapped ? w.m0 + 128 * rank : w.n0 + a.half * rank;
+                float* const to = a.slots + ((int64_t)w.row_tile * (a.d_in + a.sum_rows) + a.d_in + (warp & 1)) * a.ldo + first;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float s = sums.total(h);
+                    const int j = 16 * (warp >> 1) + 8 * h + (lane >> 2);
+                    if ((lane & 3) == 0 && j < of_block && first + j < a.d_out) to[j] = s;
+                }
+                sums.clear();
+            });
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGISTERS));
         if (warp == DRAIN_WARPS && rank == 0) grad_multiplier<T>(a, sh, ring);
@@ -329,6 +366,190 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) layer_wg
     __syncthreads();
     tc::cluster_sync();  // neither block leaves while the other may still signal it or read its operands
     if (warp == DRAIN_WARPS) {
+        tc::tc_fence_after_sync();
+        tc::tmem_dealloc_pair(sh.tmem_base, 512);
+    }
+}
+
+// ---- fp32 rows ----------------------------------------------------------------------------------
+// Six MMAs a product on three bf16 numbers a value, a fresh accumulator for every 32 rows (layer_f32.cu); tiles of 256 x 128.  Splitting is what bounds
+// it: twelve warps do it, four for every 64 columns, always the same ones, so that they add up dZ's columns on the way.
+struct GradF32Shared : Shared {
+    uint64_t raw_full[RAW_STAGES], raw_free[RAW_STAGES];
+};
+
+__device__ __forceinline__ void grad_f32_producer(const GradArgs& a, GradF32Shared& sh, uint8_t* raw, int rank) {
+    tc::prefetch_tensormap(&a.map_a);
+    tc::prefetch_tensormap(&a.map_b);
+    const int boxes = (a.half + 31) / 32;
+    GradWalk<F32_BK> w;
+    tc::RingAt at;
+    for (bool more = w.first(a, sh); more; more = w.next(a, sh), at.advance(RAW_STAGES)) {
+        if (!wait_for(&sh.raw_free[at.s], at.phase ^ 1u, sh, a.error_word)) return;
+        uint8_t* stage = raw + at.s * RAW_BYTES;
+        uint64_t* bar = &sh.raw_full[at.s];
+        tc::mbar_arrive_expect_tx(bar, (4 + boxes) * 4096);
+        const int row = (int)w.row0 + w.k0;
+        for (int i = 0; i < 4; ++i) tc::tma_load_3d(stage + 4096 * i, &a.map_a, bar, 2 * (w.m0 + 128 * rank + 32 * i), row, 0);
+        for (int i = 0; i < boxes; ++i) tc::tma_load_3d(stage + 4096 * (4 + i), &a.map_b, bar, 2 * (w.n0 + a.half * rank + 32 * i), row, 0);
+    }
+}
+
+// which: 4 * atom (two of the left operand, one of the right one) + quarter of the rows.  A thread has eight columns of a row; those of an atom's upper 32
+// read the halves of their eight the other way around, so that no two of eight threads are in one bank, and leave them so: the results' columns are
+// put right once a tile.
+__device__ __forceinline__ void grad_f32_splitter(const GradArgs& a, GradF32Shared& sh, uint32_t raw, uint32_t planes, int rank, int which, int lane) {
+    const int atom = which >> 2, unit = lane & 7, turned = unit >> 2;
+    const bool of_dz = (atom < 2) == a.swapped;
+    GradWalk<F32_BK> w;
+    tc::RingAt at, raw_at;
+    int filled = 0;  // stages, F32_STAGES at most
+    float sums[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sums[j] = 0.f;
+    for (bool more = w.first(a, sh); more; more = w.next(a, sh)) {
+        if (!wait_for(&sh.raw_full[raw_at.s], raw_at.phase, sh, a.error_word)) return;
+        if (!wait_for<true>(&sh.empty[at.s], at.phase ^ 1u, sh, a.error_word)) return;
+        __syncwarp();
+        const uint32_t from = raw + raw_at.s * RAW_BYTES + (2 * atom + turned) * 4096, to = planes + (3 * at.s + atom) * ATOM_BYTES;
+        uint32_t v[2][8];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int row = 8 * (which & 3) + 4 * i + (lane >> 3);
+            const uint32_t line = from + row * 128;
+            const uint4 x = load_16(line + (((2 * (unit & 3) + turned) ^ (row & 7)) << 4)), y = load_16(line + (((2 * (unit & 3) + 1 - turned) ^ (row & 7)) << 4));
+            v[i][0] = x.x; v[i][1] = x.y; v[i][2] = x.z; v[i][3] = x.w;
+            v[i][4] = y.x; v[i][5] = y.y; v[i][6] = y.z; v[i][7] = y.w;
+        }
+        if (w.k0 + F32_BK > w.k_end) {  // rows behind the chunk are another part's
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[i][j] = w.k0 + 8 * (which & 3) + 4 * i + (lane >> 3) < w.k_end ? v[i][j] : 0u;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int row = 8 * (which & 3) + 4 * i + (lane >> 3);
+            if (of_dz) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sums[j] += __uint_as_float(v[i][j]);
+            }
+            uint4 p[3];
+            split_eight(v[i], p);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) store_16(to + k * (ATOM_BYTES / 3) + row * 128 + ((unit ^ (row & 7)) << 4), p[k]);
+        }
+        tc::fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+            tc::mbar_arrive(&sh.raw_free[raw_at.s]);
+            tc::mbar_arrive_remote(tc::leader_addr(&sh.full[at.s]));  // (each block's planes are read by its own tensor cores: the fence has made them visible)
+        }
+        raw_at.advance(RAW_STAGES);
+        at.advance(F32_STAGES);
+        filled = min(filled + 1, F32_STAGES);
+        if (w.last_stage() && of_dz) {
+            const int left = a.swapped ? 128 - 64 * atom : a.half, first = a.swapped ? w.m0 + 128 * rank + 64 * atom : w.n0 + a.half * rank;
+            float* const to_sums = a.slots + ((int64_t)w.row_tile * (a.d_in + a.sum_rows) + a.d_in + (which & 3)) * a.ldo + first;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float s = sums[j] + __shfl_xor_sync(0xffffffffu, sums[j], 8);
+                s += __shfl_xor_sync(0xffffffffu, s, 16);
+                const int c = 8 * unit + (j ^ (4 * turned));
+                if (w.sums(a) && lane < 8 && c < left && first + c < a.d_out) to_sums[c] = s;
+                sums[j] = 0.f;
+            }
+        }
+    }
+    // No signal stays under way: the last stages are waited for.
+    for (int i = 0; i < filled; ++i) {
+        const int back = filled - i, s = (at.s - back + F32_STAGES) % F32_STAGES;
+        if (!wait_for<true>(&sh.empty[s], s < at.s ? at.phase : at.phase ^ 1u, sh, a.error_word)) return;
+    }
+}
+
+__device__ __forceinline__ void grad_f32_multiplier(const GradArgs& a, GradF32Shared& sh, uint32_t planes) {
+    const uint32_t idesc = tc::idesc_bf16(LEFT, 2 * a.half, true, true);
+    constexpr uint32_t plane = ATOM_BYTES / 3 >> 4;
+    const uint64_t desc = tc::smem_desc_sw128(0, ATOM_BYTES, 1024);
+    GradWalk<F32_BK> w;
+    tc::RingAt at;
+    for (bool more = w.first(a, sh); more; more = w.next(a, sh)) {
+        if (!wait_for<true>(&sh.acc_empty[at.s], at.phase ^ 1u, sh, a.error_word)) return;
+        if (!wait_for<true>(&sh.full[at.s], at.phase, sh, a.error_word)) return;
+        tc::tc_fence_after_sync();
+        __syncwarp();
+        const uint32_t d = sh.tmem_base + at.s * 128;
+        const uint64_t da = desc + ((planes + 3 * at.s * ATOM_BYTES) >> 4), db = da + (2 * ATOM_BYTES >> 4);
+        tc::mma_pair_by_warp(d, da + 2 * plane, db, idesc, 0u);
+        tc::mma_pair_by_warp(d, da, db + 2 * plane, idesc, 1u);
+        tc::mma_pair_by_warp(d, da + plane, db + plane, idesc, 1u);
+        tc::mma_pair_by_warp(d, da + plane, db, idesc, 1u);
+        tc::mma_pair_by_warp(d, da, db + plane, idesc, 1u);
+        if (w.k_end - w.k0 > 16) {  // 16 rows further
+            const uint64_t x = da + 128, y = db + 128;
+            tc::mma_pair_by_warp(d, x + 2 * plane, y, idesc, 1u);
+            tc::mma_pair_by_warp(d, x, y + 2 * plane, idesc, 1u);
+            tc::mma_pair_by_warp(d, x + plane, y + plane, idesc, 1u);
+            tc::mma_pair_by_warp(d, x + plane, y, idesc, 1u);
+            tc::mma_pair_by_warp(d, x, y + plane, idesc, 1u);
+            tc::mma_pair_by_warp(d, x, y, idesc, 1u);
+        }
+        tc::mma_pair_by_warp(d, da, db, idesc, 1u);
+        tc::commit_pair_by_warp(&sh.empty[at.s]);
+        tc::commit_pair_by_warp(&sh.acc_full[at.s]);
+        at.advance(F32_STAGES);
+    }
+}
+
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F32_THREADS, 1) layer_wgrad_f32_kernel(const __grid_constant__ GradArgs a) {
+    static_assert(F32_DYNAMIC_BYTES + sizeof(GradF32Shared) <= SMEM_MOST, "shared memory of a block");
+    extern __shared__ uint8_t bytes[];
+    __shared__ GradF32Shared sh;
+    uint8_t* const raw = bytes + ((1024u - (tc::smem_u32(bytes) & 1023u)) & 1023u);
+    const uint32_t planes = tc::smem_u32(raw) + RAW_STAGES * RAW_BYTES;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr int DRAINS = F32_DRAIN_WARPS;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < F32_STAGES; ++s) {
+            tc::mbar_init(&sh.full[s], 2 * SPLIT_WARPS);
+            tc::mbar_init(&sh.empty[s], 1);
+            tc::mbar_init(&sh.acc_full[s], 1);
+            tc::mbar_init(&sh.acc_empty[s], 2 * DRAINS);
+        }
+        for (int s = 0; s < RAW_STAGES; ++s) {
+            tc::mbar_init(&sh.raw_full[s], 1);
+            tc::mbar_init(&sh.raw_free[s], SPLIT_WARPS);
+        }
+        sh.abort = 0;
+        tc::fence_barrier_init();
+    }
+    if (warp == DRAINS) {
+        tc::tmem_alloc_pair(&sh.tmem_base, 512);
+        tc::tmem_relinquish_pair();
+    }
+    wait_for_kernel_before();
+    lay_out<WEIGHT_GRADIENT, F32_THREADS, F32_BK>(a, sh);
+    tc::tc_fence_before_sync();
+    __syncthreads();
+    tc::cluster_sync();  // both blocks' barriers and tensor memory exist before either is signalled
+    tc::tc_fence_after_sync();
+    const int rank = (int)tc::cluster_rank();
+    if (warp < DRAINS) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SUMS_REGISTERS));
+        grad_drain<F32_BK, F32_BK, F32_STAGES, 128, true>(a, sh, rank, [](const GradWalk<F32_BK>&, int) { return true; }, [](const GradWalk<F32_BK>&) {});
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(F32_OTHER_REGISTERS));
+        if (warp == DRAINS && rank == 0) grad_f32_multiplier(a, sh, planes);
+        if (warp == DRAINS + 1 && lane == 0) grad_f32_producer(a, sh, raw, rank);
+        if (warp >= DRAINS + 4) grad_f32_splitter(a, sh, tc::smem_u32(raw), planes, rank, warp - DRAINS - 4, lane);
+    }
+    __syncwarp();
+    if (*reinterpret_cast<volatile int*>(&sh.abort)) __nanosleep(1000000);  // a wait ran out: copies and MMAs under way land before the block ends
+    tc::tc_fence_before_sync();
+    __syncthreads();
+    tc::cluster_sync();  // neither block leaves while the other may still signal it or read its operands
+    if (warp == DRAINS) {
         tc::tc_fence_after_sync();
         tc::tmem_dealloc_pair(sh.tmem_base, 512);
     }
@@ -349,7 +570,7 @@ __global__ void __launch_bounds__(256) layer_wgrad_reduce_kernel(const __grid_co
         s.w += v.w;
     };
     const int part = blockIdx.y, from = tile_start[part], count = tile_start[part + 1] - from, quads = (int)a.ldo / 4;
-    const int64_t slot = (a.d_in + 2) * a.ldo, all = (int64_t)(a.d_in + (a.sums ? 1 : 0)) * quads;
+    const int64_t slot = (a.d_in + a.sum_rows) * a.ldo, all = (int64_t)(a.d_in + (a.sums ? 1 : 0)) * quads;
     // where there are many slots and few quads, eight warps share the slots of 32 quads; otherwise every thread has a quad of its own
     const int shares = count >= 8 && gridDim.x * 32 >= all ? 8 : 1, share = shares > 1 ? threadIdx.x >> 5 : 0, together = 256 / shares;
     for (int64_t base = (int64_t)blockIdx.x * together; base < all; base += (int64_t)gridDim.x * together) {
@@ -360,8 +581,9 @@ __global__ void __launch_bounds__(256) layer_wgrad_reduce_kernel(const __grid_co
             const float* p = a.slots + from * slot + 4 * i;
 #pragma unroll 4
             for (int t = share; t < count; t += shares) add(s, *reinterpret_cast<const float4*>(p + t * slot));
-            if (row == a.d_in)  // the other half of the rows'
-                for (int t = share; t < count; t += shares) add(s, *reinterpret_cast<const float4*>(p + t * slot + a.ldo));
+            if (row == a.d_in)  // the other shares of the rows
+                for (int k = 1; k < a.sum_rows; ++k)
+                    for (int t = share; t < count; t += shares) add(s, *reinterpret_cast<const float4*>(p + t * slot + k * a.ldo));
         }
         if (shares > 1) {
             __syncthreads();
@@ -372,8 +594,8 @@ __global__ void __launch_bounds__(256) layer_wgrad_reduce_kernel(const __grid_co
             for (int k = 1; k < 8; ++k) add(s, red[k][threadIdx.x & 31]);
         }
         if (i >= all) continue;
-        O* to = row < a.d_in ? static_cast<O*>(a.dW) + part * a.dw_stride + (int64_t)row * a.real_out : static_cast<O*>(a.db) + part * a.db_stride;
-        const int second = col >= a.width ? 1 : 0, c = col - second * a.width;  // (halves are multiples of 8)
+        O* to = row < a.d_in ? static_cast<O*>(a.to_w) + part * a.dw_stride + (int64_t)row * a.real_out : static_cast<O*>(a.to_b) + part * a.db_stride;
+        const int second = a.d_out > a.width && col >= a.width ? 1 : 0, c = col - second * a.width;  // (of two halves each is a multiple of 8)
         to += second * a.real_width + c;
         if (c < a.real_width) to[0] = from_f32<O>(s.x);
         if (c + 1 < a.real_width) to[1] = from_f32<O>(s.y);
@@ -385,10 +607,10 @@ __global__ void __launch_bounds__(256) layer_wgrad_reduce_kernel(const __grid_co
 }  // namespace
 
 int32_t layer_dw(rtma_ctx* ctx, const char* who, const rtma_layer_desc* d, int64_t n, int32_t G, const int64_t* offsets, const void* X, int64_t ldx, const void* dZ,
-                 int64_t lddz, void* dW, int64_t dw_stride, void* db, int64_t db_stride, bool sums, size_t at, size_t* scratch, cudaStream_t stream) {
-    const int halves = d->gated ? 2 : 1, width = (int)ceil_div(d->d_out, 8) * 8, d_in = d->d_in, d_out = halves * width, real_out = halves * d->d_out;
+                 int64_t lddz, int width, void* dW, int64_t dw_stride, void* db, int64_t db_stride, bool sums, size_t at, size_t* scratch, cudaStream_t stream) {
+    const int halves = d->gated ? 2 : 1, d_in = d->d_in, d_out = halves * width, real_out = halves * d->d_out;
     const int64_t weights = (int64_t)d_in * real_out;
-    const bool shared = G > 1 && dw_stride == 0, bf16 = d->dtype == RTMA_BF16;
+    const bool shared = G > 1 && dw_stride == 0, bf16 = d->dtype == RTMA_BF16, f32 = d->dtype == RTMA_F32;
     if (G > 1 && db && (db_stride == 0) != shared)
         return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: either both gradients are one for all parts or neither", who);
     if (G > 1 && !shared && ((dw_stride < weights && dw_stride > -weights) || (db && db_stride < real_out && db_stride > -real_out)))
@@ -406,17 +628,19 @@ int32_t layer_dw(rtma_ctx* ctx, const char* who, const rtma_layer_desc* d, int64
     a.A = a.swapped ? dZ : X; a.lda = a.swapped ? lddz : ldx;
     a.B = a.swapped ? X : dZ; a.ldb = a.swapped ? ldx : lddz;
     a.m_tiles = (int)ceil_div(a.left, LEFT);
-    a.n_tiles = (int)ceil_div(a.right, 256);
+    const int widest = f32 ? 2 * F32_HALF : 256;  // columns of the right operand in a tile
+    a.n_tiles = (int)ceil_div(a.right, widest);
     a.half = (int)ceil_div(ceil_div(a.right, a.n_tiles), 32) * 16;
     a.n_tiles = (int)ceil_div(a.right, 2 * a.half);
     const int pairs = ctx->sm_count / 2;
     a.tile_rows = 256;
     a.tiles = std::min(std::max<int64_t>(a.G, (int64_t)DW_WAVES * pairs / ((int64_t)a.m_tiles * a.n_tiles)), n / a.tile_rows + a.G);
-    a.ldo = d_out;
+    a.ldo = ceil_div(d_out, 8) * 8;
     a.width = width; a.real_width = d->d_out; a.real_out = real_out;
-    a.dW = dW; a.dw_stride = dw_stride; a.db = db; a.db_stride = db_stride;
+    a.to_w = dW; a.dw_stride = dw_stride; a.to_b = db; a.db_stride = db_stride;
     a.sums = db && sums;
-    const size_t bytes = at + 256 + sizeof(float) * (size_t)a.tiles * (d_in + 2) * a.ldo;
+    a.sum_rows = f32 ? 4 : 2;
+    const size_t bytes = at + 256 + sizeof(float) * (size_t)a.tiles * (d_in + a.sum_rows) * a.ldo;
     if (scratch) {
         *scratch = bytes;
         return RTMA_OK;
@@ -427,16 +651,20 @@ int32_t layer_dw(rtma_ctx* ctx, const char* who, const rtma_layer_desc* d, int64
     if (n > 0) {
         const int64_t tiles = a.tiles * a.m_tiles * a.n_tiles;
         if (tiles >= (int64_t(1) << 30)) return rtma_fail(ctx, RTMA_ERR_OVERFLOW, "%s: %lld tiles", who, (long long)tiles);
-        if (!make_tensor_map_16bit(&a.map_a, bf16, a.A, 1, n, a.left, a.lda, n * a.lda, BK) || !make_tensor_map_16bit(&a.map_b, bf16, a.B, 1, n, a.right, a.ldb, n * a.ldb, BK))
+        // fp32 rows as twice as many 16-bit values, in boxes of 32 of them and as many rows
+        const int values = f32 ? 2 : 1, box = f32 ? F32_BK : BK;
+        if (!make_tensor_map_16bit(&a.map_a, f32 || bf16, a.A, 1, n, values * (uint64_t)a.left, values * a.lda, values * n * a.lda, box) ||
+            !make_tensor_map_16bit(&a.map_b, f32 || bf16, a.B, 1, n, values * (uint64_t)a.right, values * a.ldb, values * n * a.ldb, box))
             return rtma_fail(ctx, RTMA_ERR_CUDA, "%s: no tensor map for rows of %d and %d values", who, d_in, d_out);
-        void (*kernel)(GradArgs) = bf16 ? layer_wgrad_kernel<__nv_bfloat16> : layer_wgrad_kernel<__half>;
-        bool& configured = ctx->layer_configured[bf16 ? 32 : 33];
+        void (*kernel)(GradArgs) = f32 ? layer_wgrad_f32_kernel : bf16 ? layer_wgrad_kernel<__nv_bfloat16> : layer_wgrad_kernel<__half>;
+        const int bytes_of = f32 ? F32_DYNAMIC_BYTES : DYNAMIC_BYTES;
+        bool& configured = ctx->layer_configured[32 + d->dtype];
         if (!configured) {
-            RTMA_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, DYNAMIC_BYTES));
+            RTMA_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes_of));
             configured = true;
         }
         KernelScope ks(ctx, KC_GEMM_WGRAD, stream);
-        launch_kernel(kernel, (unsigned)(2 * std::min<int64_t>(tiles, pairs)), THREADS, DYNAMIC_BYTES, stream, a);
+        launch_kernel(kernel, (unsigned)(2 * std::min<int64_t>(tiles, pairs)), f32 ? F32_THREADS : THREADS, bytes_of, stream, a);
         RTMA_LAUNCH_CHECK(ctx);
     }
     KernelScope ks(ctx, KC_REDUCE_SGD, stream);
