@@ -2,15 +2,16 @@
 //   Y[r] = R[r] + act(X[r] W_g + b_g)                          gated: H[r] = R[r] + act(X[r] V_g + c_g) * (X[r] U_g + d_g)
 // for the rows r of part g, W_g = [V_g | U_g] in a gated layer, and the first step of their gradients,
 //   dZ[r] = dY[r] act'(Z[r])                                   gated: dZ[r] = [dH u act'(v) | dH act(v)]
-// with Z = X W + b worked out again from the inputs: kept from the forward pass it would cost a write there and a read here, which is
-// more than the product as long as the contraction has fewer terms than about 600 (16-bit rows).  dX = dZ W^T and dW = X^T dZ are then the
-// grouped products of grouped_linear.cu.
+// with Z = X W + b worked out again from the inputs.  Kept from the forward pass, Z would cost a write there and a read here: of 16-bit rows
+// that is more than the product as long as the contraction has fewer than about 600 terms, and nothing of the forward pass has to be kept.
+// dX = dZ W^T and dW = X^T dZ are products of their own, and dZ, an operand of these, is rounded to the rows' type.
 //
-// One kernel body (grouped_rows.cuh) for all four: the product stays in tensor memory and goes through the layer in the registers of
-// the warps that drain it.  A tile of a gated layer has the same columns of both matrices, so that a lane finds both factors of a result in its own
-// row.  dZ is rounded to the rows' type: it is an operand of 16-bit products.
+// The product stays in tensor memory and goes through the layer in the registers of the warps that drain it.  A tile of a gated layer has the same columns
+// of both matrices, so that a lane finds both factors of a result in its own row.  Rows off 16-byte boundaries, and matrices whose rows lie so, are laid
+// out on such boundaries first: one way through the products for all rows.
 //
-// This file: the calls.  Those of 16-bit rows are in layer_pairs.cuh and layer_wgrad.cu, those of fp32 rows in layer_split.cu.
+// This file: the calls and what is laid out.  The layers' kernels: layer_pairs.cuh (16-bit rows), layer_f32.cu; the weight gradients': layer_wgrad.cu; dX of
+// 16-bit rows is a call of grouped_linear.cu.
 #include <algorithm>
 
 #include "layer.cuh"
@@ -21,7 +22,7 @@ namespace {
 
 using namespace grouped;
 
-constexpr int PAIR_ROWS = 256;  // of a tile of the kernels on 16-bit rows
+constexpr int PAIR_ROWS = 2 * PAIR_BM;  // of a pair's tile
 
 // 16-bit rows on any boundary -> rows on 16-byte ones, zeros behind each up to a multiple of 8 values.  Row r lies at src + (r / group) *
 // group_stride + (r % group) * ld.
@@ -36,8 +37,9 @@ struct AlignArgs {
 };
 constexpr int ALIGN_BYTES = 16384;
 
-// A block brings neighbouring rows as the 16-byte words that they lie in, and cuts them up in shared memory.  Memory's time (200,000 x 100: 15 us), where
-// the products' own copies of such rows, for every tile of columns again, cost more than the products (200,000 x 100 -> 2 x 266 in fp16: 222 us).
+// A block brings neighbouring rows as the 16-byte words that they lie in, and cuts them up in shared memory while the next ones come (200,000 x 100 in
+// fp16 25 us, 3.2 TB/s: instructions; 300,000 x 100 and x 47 44 us).  Copied by the products for every tile of columns again, such rows cost
+// more than the products: 200,000 x 100 -> 2 x 266 222 us, like this 81 and 25.
 __global__ void __launch_bounds__(256) align_rows_kernel(const __grid_constant__ AlignArgs args) {
     __shared__ uint4 words[ALIGN_BYTES / 16 + 258];  // (a row's last words are read beyond it, and dropped)
     wait_for_kernel_before();
@@ -151,7 +153,7 @@ struct SumsArgs {
 
 // What pairs of blocks leave of sums over rows (layer_pairs.cuh), added up in order: a block for 32 columns of dZ and a part (or all parts:
 // shared), the last of a part for its slope's gradient.
-constexpr int SUMS_THREADS = 1024;
+constexpr int SUMS_THREADS = 512;
 template <class O>
 __global__ void __launch_bounds__(SUMS_THREADS) layer_sums_kernel(const __grid_constant__ SumsArgs a) {
     __shared__ int32_t tile_start[RTMA_MAX_GROUPS + 1], warp_sums[32], place_start[MOST_PLACES + 1];
@@ -173,10 +175,10 @@ __global__ void __launch_bounds__(SUMS_THREADS) layer_sums_kernel(const __grid_c
         int i = (int)((int64_t)from * a.places / tiles), end;
         while (place_start[i + 1] <= from) ++i;
         for (end = i + 1; end < a.places && place_start[end] < to;) ++end;
-        if (!of_slope) {  // eight warps for the sums of a slot, every fourth slot
+        if (!of_slope) {  // eight warps for the sums of a slot, every second slot
             const float* p = a.column_slots + (8 * (int64_t)(i + part) + (warp & 7)) * a.columns + min(column, a.columns - 1);
 #pragma unroll 4
-            for (int k = i + (warp >> 3); k < end; k += 4) {
+            for (int k = i + (warp >> 3); k < end; k += SUMS_THREADS / 256) {
                 const float v = p[8 * (int64_t)(k - i) * a.columns];
                 s += place_start[k] != place_start[k + 1] ? v : 0.f;
             }

@@ -1,13 +1,13 @@
-// The weight gradient of a layer (layer.cu) over 16-bit rows on 16-byte boundaries: dW_g = X_g^T dZ_g, db_g = the column sums of dZ_g.
+// The weight gradient of a layer (layer.cu) from rows on 16-byte boundaries: dW_g = X_g^T dZ_g, db_g = the column sums of dZ_g.
 //
-// Pairs of blocks (MMAs of 256 x up to 256 over 64 rows a stage); rows run across both operands, so that both come as they lie.  The wider
-// of X and dZ is the left operand (256 of its columns a tile), the other one's up to 256 columns the right one, whichever wastes less.  The
-// parts' rows are cut into chunks as in grouped_linear.cu, one slot of fp32 sums for each, added up by a second kernel.
+// Pairs of blocks (MMAs of 256 x up to 256 over 64 rows a stage); rows run across both operands, so that both come as they lie.  The
+// left operand (256 columns a tile) is X or dZ, whichever makes fewer MMAs; every stage's 32 KB a block come from the L2 cache, which is what
+// bounds it: 500,000 x 256 x 1,024 in bf16 281 us (0.93 PFLOP/s; memory's share of it 213), 500,000 x 256 x 256 95 us; as tiles of 128 x 128 in
+// grouped_linear.cu 456 and 127.  The parts' rows are cut into chunks as there, one slot of fp32 sums for each, added up by a second kernel.
 //
 // The tensor cores truncate when they accumulate: sixteen warps take the accumulator after every 128 rows and add it up in registers, rounded to
-// nearest, 64 columns of a row in a lane (16 warps, not 8, because of these sums).  The same warps take the column
-// sums of dZ from the stages; as products with ones by mma.sync these held the MMAs up (500,000 x 256 x 1,024 in bf16: 415 us, 284 without the sums), as a product of 128 x 128 tiles with ones, as in grouped_linear.cu, they cost as many MMAs as
-// the weights' do.
+// nearest, 64 columns of a row in a lane.  The same warps take dZ's column sums from the stages where no kernel before has (layers without activation
+// or gate: 500,000 x 256 x 1,024 351 us; as products with ones by mma.sync, which the MMAs wait for, 415).
 #include <algorithm>
 
 #include "layer.cuh"
@@ -373,7 +373,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) layer_wg
 
 // ---- fp32 rows ----------------------------------------------------------------------------------
 // Six MMAs a product on three bf16 numbers a value, a fresh accumulator for every 32 rows (layer_f32.cu); tiles of 256 x 128.  Splitting is what bounds
-// it: twelve warps do it, four for every 64 columns, always the same ones, so that they add up dZ's columns on the way.
+// it (100,000 x 128 x 512: 94 us, 75 with nothing split; eight warps with fewer registers and tiles of twice the width 150): twelve warps do it, four for
+// every 64 columns, always the same ones, so that they add up dZ's columns on the way.  56 bytes a thread are spilled, of warps that drain.
 struct GradF32Shared : Shared {
     uint64_t raw_full[RAW_STAGES], raw_free[RAW_STAGES];
 };
@@ -404,9 +405,9 @@ __device__ __forceinline__ void grad_f32_splitter(const GradArgs& a, GradF32Shar
     GradWalk<F32_BK> w;
     tc::RingAt at, raw_at;
     int filled = 0;  // stages, F32_STAGES at most
-    float sums[8];
+    float sums[8], total[8];  // a lane's columns; sums of 16 stages are added to total, so that not every value meets a long sum
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sums[j] = 0.f;
+    for (int j = 0; j < 8; ++j) sums[j] = total[j] = 0.f;
     for (bool more = w.first(a, sh); more; more = w.next(a, sh)) {
         if (!wait_for(&sh.raw_full[raw_at.s], raw_at.phase, sh, a.error_word)) return;
         if (!wait_for<true>(&sh.empty[at.s], at.phase ^ 1u, sh, a.error_word)) return;
@@ -448,16 +449,23 @@ __device__ __forceinline__ void grad_f32_splitter(const GradArgs& a, GradF32Shar
         raw_at.advance(RAW_STAGES);
         at.advance(F32_STAGES);
         filled = min(filled + 1, F32_STAGES);
+        if (of_dz && (w.last_stage() || (w.k0 / F32_BK) % 16 == 15)) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                total[j] += sums[j];
+                sums[j] = 0.f;
+            }
+        }
         if (w.last_stage() && of_dz) {
             const int left = a.swapped ? 128 - 64 * atom : a.half, first = a.swapped ? w.m0 + 128 * rank + 64 * atom : w.n0 + a.half * rank;
             float* const to_sums = a.slots + ((int64_t)w.row_tile * (a.d_in + a.sum_rows) + a.d_in + (which & 3)) * a.ldo + first;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                float s = sums[j] + __shfl_xor_sync(0xffffffffu, sums[j], 8);
+                float s = total[j] + __shfl_xor_sync(0xffffffffu, total[j], 8);
                 s += __shfl_xor_sync(0xffffffffu, s, 16);
                 const int c = 8 * unit + (j ^ (4 * turned));
                 if (w.sums(a) && lane < 8 && c < left && first + c < a.d_out) to_sums[c] = s;
-                sums[j] = 0.f;
+                total[j] = 0.f;
             }
         }
     }
@@ -570,30 +578,11 @@ __global__ void __launch_bounds__(256) layer_wgrad_reduce_kernel(const __grid_co
         s.w += v.w;
     };
     const int part = blockIdx.y, from = tile_start[part], count = tile_start[part + 1] - from, quads = (int)a.ldo / 4;
-    const int64_t slot = (a.d_in + a.sum_rows) * a.ldo, all = (int64_t)(a.d_in + (a.sums ? 1 : 0)) * quads;
-    // where there are many slots and few quads, eight warps share the slots of 32 quads; otherwise every thread has a quad of its own
-    const int shares = count >= 8 && gridDim.x * 32 >= all ? 8 : 1, share = shares > 1 ? threadIdx.x >> 5 : 0, together = 256 / shares;
-    for (int64_t base = (int64_t)blockIdx.x * together; base < all; base += (int64_t)gridDim.x * together) {
-        const int64_t i = base + (shares > 1 ? threadIdx.x & 31 : threadIdx.x);
-        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        const int row = (int)(i / quads), col = 4 * (int)(i - (int64_t)row * quads);
-        if (i < all) {
-            const float* p = a.slots + from * slot + 4 * i;
-#pragma unroll 4
-            for (int t = share; t < count; t += shares) add(s, *reinterpret_cast<const float4*>(p + t * slot));
-            if (row == a.d_in)  // the other shares of the rows
-                for (int k = 1; k < a.sum_rows; ++k)
-                    for (int t = share; t < count; t += shares) add(s, *reinterpret_cast<const float4*>(p + t * slot + k * a.ldo));
-        }
-        if (shares > 1) {
-            __syncthreads();
-            red[share][threadIdx.x & 31] = s;
-            __syncthreads();
-            if (share) continue;
-#pragma unroll
-            for (int k = 1; k < 8; ++k) add(s, red[k][threadIdx.x & 31]);
-        }
-        if (i >= all) continue;
+    const int64_t slot = (a.d_in + a.sum_rows) * a.ldo;
+    const int all = (a.d_in + (a.sums ? 1 : 0)) * quads;
+    const float* const slots = a.slots + from * slot;
+    auto put = [&](int i, float4 s) {
+        const int row = i / quads, col = 4 * (i - row * quads);
         O* to = row < a.d_in ? static_cast<O*>(a.to_w) + part * a.dw_stride + (int64_t)row * a.real_out : static_cast<O*>(a.to_b) + part * a.db_stride;
         const int second = a.d_out > a.width && col >= a.width ? 1 : 0, c = col - second * a.width;  // (of two halves each is a multiple of 8)
         to += second * a.real_width + c;
@@ -601,6 +590,31 @@ __global__ void __launch_bounds__(256) layer_wgrad_reduce_kernel(const __grid_co
         if (c + 1 < a.real_width) to[1] = from_f32<O>(s.y);
         if (c + 2 < a.real_width) to[2] = from_f32<O>(s.z);
         if (c + 3 < a.real_width) to[3] = from_f32<O>(s.w);
+    };
+    // a quad's sums over every `step`-th slot from `first` on; the bias's over the shares of the rows, too
+    auto sum = [&](int i, int first, int step) {
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        const int shares = i >= a.d_in * quads ? a.sum_rows : 1;
+        for (int k = 0; k < shares; ++k) {
+            const float* p = slots + first * slot + 4 * (int64_t)i + k * a.ldo;
+#pragma unroll 4
+            for (int t = first; t < count; t += step, p += step * slot) add(s, *reinterpret_cast<const float4*>(p));
+        }
+        return s;
+    };
+    // where there are many slots and few quads, eight warps share the slots of 32 quads; otherwise every thread has a quad of its own
+    if (count >= 8 && (int)gridDim.x * 32 >= all) {
+        const int lane = threadIdx.x & 31, share = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (i < all) s = sum(i, share, 8);
+        red[share][lane] = s;
+        __syncthreads();
+        if (share || i >= all) return;
+#pragma unroll
+        for (int k = 1; k < 8; ++k) add(s, red[k][lane]);
+        put(i, s);
+    } else {
+        for (int i = blockIdx.x * 256 + threadIdx.x; i < all; i += gridDim.x * 256) put(i, sum(i, 0, 1));
     }
 }
 
