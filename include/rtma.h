@@ -474,7 +474,7 @@ int32_t rtma_dropout(rtma_ctx* ctx, int32_t dtype, int64_t n, int32_t d, const v
  * gradients of the calls above can go, clipped, to the places in grads [M][P] that rtma_sgd_aggregate takes.
  * norms [G] float (device) or NULL.  0 <= max_norm (infinity: nothing is clipped).  A part whose norm is not finite keeps its
  * gradients as they are or (zero_nonfinite) gets zeros, so that its step does nothing.  Squares are summed in 64 bits: values whose squares do
- * not fit fp32 are no matter.  Results must not overlap other tensors.                          */
+ * not fit fp32 are no matter.  Results must not overlap other tensors: one that starts where another, or another's gradient, does is refused. */
 typedef struct {
     const void* grad;
     void* out;

@@ -819,7 +819,7 @@ class Context:
         """Scales the tensors `grads` down so that their norm, over all of them together, is max_norm at most; returns the norms [parts]
         float32 from before.  parts = G: every tensor is [G, ...] and every part has a norm and a scale of its own.  Tensors are contiguous,
         or contiguous within a part.  In place, or into the tensors `out` of the same shapes, of the gradient's type or float32 (for
-        instance views of the grads [M, P] that sgd_aggregate takes); an entry that is None is only part of the norm.  Where a norm is not
+        instance views of the grads [M, P] that sgd_aggregate takes); an entry that is None is only part of the norm; no tensor twice.  Where a norm is not
         finite the gradients stay as they are or (zero_nonfinite) become zeros."""
         grads = list(grads)
         outs = grads if out is None else list(out)

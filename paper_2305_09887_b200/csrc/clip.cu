@@ -9,6 +9,9 @@
 // Squares are added up in fp32 eight at a time, then in 64 bits; eight whose sum leaves the range of fp32 (or is so small that
 // squares got lost) are squared in 64 bits.  So the norm neither overflows nor underflows before its own value does.
 #include <algorithm>
+#include <memory>
+#include <new>
+#include <utility>
 
 #include "rows.cuh"
 
@@ -341,6 +344,30 @@ int32_t clip(rtma_ctx* ctx, const rtma_gradient* grads, int32_t count, int32_t G
     return RTMA_OK;
 }
 
+// A result that is another's, or another's gradient, would be read after it has been written, or before.
+int32_t check_results(rtma_ctx* ctx, const char* who, int32_t count, const rtma_gradient* grads) {
+    typedef std::pair<const void*, int32_t> Place;
+    Place few[2 * FEW];
+    std::unique_ptr<Place[]> many;
+    Place* places = few;
+    if (count > FEW) {
+        many.reset(new (std::nothrow) Place[2 * (size_t)count]);
+        if (!(places = many.get())) return rtma_fail(ctx, RTMA_ERR_WORKSPACE, "%s: no host memory for %d gradients", who, count);
+    }
+    size_t used = 0;
+    for (int32_t i = 0; i < count; ++i) {
+        const rtma_gradient& t = grads[i];
+        if (!t.out || !t.size) continue;
+        places[used++] = Place(t.out, i);
+        if (t.out != t.grad) places[used++] = Place(t.grad, -1);
+    }
+    std::sort(places, places + used);
+    for (size_t k = 1; k < used; ++k)
+        if (places[k].first == places[k - 1].first && places[k].second >= 0)
+            return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: the result of gradient %d lies where another result or gradient does", who, places[k].second);
+    return RTMA_OK;
+}
+
 }  // namespace
 
 extern "C" int32_t rtma_clip_gradients(rtma_ctx* ctx, int32_t count, const rtma_gradient* grads, int32_t G, int32_t one_norm, double max_norm, int32_t zero_nonfinite,
@@ -362,6 +389,7 @@ extern "C" int32_t rtma_clip_gradients(rtma_ctx* ctx, int32_t count, const rtma_
             return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: result %d lies on its gradient in another form", who, i);
         total += (double)t.size;
     }
+    RTMA_TRY(check_results(ctx, who, count, grads));
     // Pieces: 24 for every SM or so, of 2,048 values or more (a step of a block)
     constexpr int64_t STEP = 8 * THREADS;
     if (total * G >= 9e15) return rtma_fail(ctx, RTMA_ERR_OVERFLOW, "%s: %g values", who, total * G);

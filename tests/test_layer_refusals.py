@@ -173,3 +173,21 @@ def test_the_table_of_gradients(ctx):
     assert first == (grads[0].data_ptr(), flat.data_ptr() + 12, 12, 12, 50, 1, 0)
     assert second == (grads[1].data_ptr(), 0, 7, 50, 0, 0, 0)
     assert binding.GRADIENT.size == 48
+
+
+@pytest.mark.parametrize("count", [2, 30])
+@pytest.mark.parametrize("grads,outs", [((1024, 1024), (1024, 1024)), ((1024, 2048), (4096, 4096)), ((1024, 2048), (2048, 4096)), ((1024, 2048), (4096, 1024))])
+def test_a_tensor_listed_twice(lib, handle, grads, outs, count):
+    """Two results at one place, or one where another's gradient still has to be read."""
+    rows = [(1 << 20, 0, 10)] * (count - 2) + [(g, o, 10) for g, o in zip(grads, outs)]
+    table = b"".join(struct.pack("<QQqqqii", g, o, size, 10, 10, 1, 1) for g, o, size in rows)
+    assert lib.rtma_clip_gradients(handle, count, table, 1, 0, 1.0, 0, None, None) == -1
+    assert f"the result of gradient {count - 1}" in error_of(lib, handle) or f"the result of gradient {count - 2}" in error_of(lib, handle)
+
+
+def test_a_gradient_twice_where_nothing_is_written_to_it(lib, handle):
+    """One gradient with two results, or one that is only part of the norm besides, passes the checks (and then finds no device)."""
+    for rows in ([(1024, 2048), (1024, 4096)], [(1024, 1024), (1024, 0)]):
+        table = b"".join(struct.pack("<QQqqqii", g, o, 10, 10, 10, 1, 1) for g, o in rows)
+        assert lib.rtma_clip_gradients(handle, 2, table, 1, 0, 1.0, 0, None, None) < 0
+        assert "result" not in error_of(lib, handle)
