@@ -258,32 +258,6 @@ struct Outlet {
         if (lane == 0) tc::tma_store_commit();  // a group for every slab, empty or not
         at = at + 1 == SLABS ? 0 : at + 1;
     }
-    // As close, of 16-bit values on boundaries of 4 or 8 bytes (a.go): by words of so many.
-    __device__ __forceinline__ void close_words(const LinearArgs& a, uint32_t slab, int rows, int cols, O* out, int64_t ldo, int lane) {
-        static_assert(sizeof(O) == 2, "16-bit values");
-        __syncwarp();
-        if (a.go >= 8 && cols % 4 == 0) {
-            const int word = lane & 7;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int r = 4 * i + (lane >> 3);
-                uint2 x;
-                asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x.x), "=r"(x.y) : "r"(slab + r * ROW + (((word >> 1) ^ swizzle(r)) << 4) + (word & 1) * 8) : "memory");
-                if (r < rows && 4 * word < cols) *reinterpret_cast<uint2*>(out + r * ldo + 4 * word) = x;
-            }
-        } else {
-            const int word = lane & 15;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int r = 2 * i + (lane >> 4);
-                uint32_t x;
-                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(slab + r * ROW + (((word >> 2) ^ swizzle(r)) << 4) + (word & 3) * 4) : "memory");
-                if (r < rows && 2 * word < cols) *reinterpret_cast<uint32_t*>(out + r * ldo + 2 * word) = x;
-            }
-        }
-        if (lane == 0) tc::tma_store_commit();  // a group for every slab, empty or not
-        at = at + 1 == SLABS ? 0 : at + 1;
-    }
     // 32 columns of which cols are this tile's
     __device__ __forceinline__ void put(const LinearArgs& a, const float (&v)[32], int64_t row0, int c, int rows, int cols, bool whole, O* out, int64_t ldo, int lane) {
 #pragma unroll

@@ -1,5 +1,5 @@
 // What the kernels of whole layers share: products of rows whose results go through an activation, a gate or a residual branch on
-// their way out (layer.cu: 16-bit rows, layer_split.cu: fp32 rows).
+// their way out (layer.cu: layer_pairs.cuh and layer_f32.cu; layer_wgrad.cu takes parts of them).
 #pragma once
 
 #include "activation.cuh"

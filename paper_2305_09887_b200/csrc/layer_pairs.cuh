@@ -24,6 +24,7 @@ namespace {
 using namespace grouped;
 
 constexpr int BM = PAIR_BM, BK = 64;
+constexpr int SUMMED_TILES = 64;     // after which the column sums go to their slots: tensor cores truncate, by 2^-23 of the sum at most for 16 rows
 constexpr int RESIDENT_TERMS = 256;  // of the contraction, up to which the matrix stays in shared memory
 
 template <class T_, bool GATED_, bool GRADIENT_, bool RESIDENT_>
@@ -298,8 +299,7 @@ __device__ __forceinline__ void pair_drain(const LayerArgs& a, PairShared& sh, u
                     add_columns<T>(other, lane, sums[1]);
                 }
             } else {
-                if (!GRADIENT && !a.vo && a.go >= 4 && cols % 2 == 0) outlet.close_words(a, slab, rows, cols, out, a.ldo, lane);
-                else outlet.close(a, slab, row0, c, rows, cols, whole, out, a.ldo, lane);
+                outlet.close(a, slab, row0, c, rows, cols, whole, out, a.ldo, lane);
                 if constexpr (GRADIENT)
                     if (a.column_slots) add_columns<T>(slab, lane, sums[i]);
             }
@@ -309,8 +309,11 @@ __device__ __forceinline__ void pair_drain(const LayerArgs& a, PairShared& sh, u
         __syncwarp();
         if (lane == 0) tc::mbar_arrive_remote(tc::leader_addr(&sh.acc_empty[acc.s]));  // (a pair's warps all report to the first block)
         acc.advance(2);
-        if (GRADIENT && w.part_ends(sh)) {
+        if (GRADIENT && (w.part_ends(sh) || w.t % SUMMED_TILES == SUMMED_TILES - 1)) {
             const int pair = blockIdx.x >> 1, place = pair / a.n_tiles;
+            // the part's first tile here; again: the slots hold sums of tiles before these
+            const int first = max((int)((int64_t)sh.tile_start[a.G] * place / a.places), sh.tile_start[part]);
+            const bool again = first / SUMMED_TILES < w.t / SUMMED_TILES;
             const int64_t slot = 8 * (int64_t)(place + part) + 4 * rank + quarter;
             if (a.column_slots) {
 #pragma unroll
@@ -321,13 +324,14 @@ __device__ __forceinline__ void pair_drain(const LayerArgs& a, PairShared& sh, u
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const int j = 8 * k + (lane >> 2);
-                        if (j < cols) to[j] = sums[i][k >> 1][2 * (k & 1)];
+                        if (j < cols) to[j] = sums[i][k >> 1][2 * (k & 1)] + (again ? to[j] : 0.f);
                     }
                 }
             }
             if (ACT == RTMA_ACT_PRELU && a.slope_slots) {
                 for (int o = 16; o > 0; o >>= 1) slope_sum += __shfl_xor_sync(0xffffffffu, slope_sum, o);
-                if (lane == 0) a.slope_slots[(slot * a.n_tiles + (pair - place * a.n_tiles)) * 4 + slice] = slope_sum;
+                float* const to = a.slope_slots + (slot * a.n_tiles + (pair - place * a.n_tiles)) * 4 + slice;
+                if (lane == 0) *to = slope_sum + (again ? *to : 0.f);
             }
             clear();
         }

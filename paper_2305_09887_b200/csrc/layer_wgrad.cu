@@ -135,7 +135,8 @@ __device__ __forceinline__ void grad_producer(const GradArgs& a, GradShared& sh,
         }
         __syncwarp();
     }
-    // No signal stays under way (see the pairs of grouped_rows.cuh).
+    // No signal stays under way: every stage filled is waited for until both blocks have it back or, after a give-up, until its loads have
+    // landed (the first block, for both).
     for (int i = 0; i < filled; ++i) {
         const int back = filled - i, s = (at.s - back + STAGES) % STAGES;
         const uint32_t parity = s < at.s ? at.phase : at.phase ^ 1u;
