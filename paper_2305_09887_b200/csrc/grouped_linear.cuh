@@ -9,7 +9,7 @@
 namespace grouped {
 
 enum Mode { FORWARD, INPUT_GRADIENT, WEIGHT_GRADIENT };
-constexpr int MAX_STAGES = 6, MAX_ACCUMULATORS = 3;
+constexpr int MAX_STAGES = 6, MAX_ACCUMULATORS = 4;
 constexpr int SMEM_MOST = 232448;  // bytes a block can have
 
 struct LinearArgs {
@@ -151,9 +151,19 @@ __device__ __forceinline__ void lay_out(const LinearArgs& a, Shared& sh) {
             // Chunks of which there are not more than `tiles` fill the blocks that run at a time evenly, whatever the parts' sizes.
             const int lane = threadIdx.x;
             int most = 1;
-            for (int g = lane; g < a.G; g += 32) most = max(most, sh.rows[g]);
-            for (int o = 16; o > 0; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
-            const int chunk = fit_chunk((int)a.tile_rows / STEP, steps_of<STEP>(most), a.tiles, [&](int steps) {
+            int64_t all = 0;
+            for (int g = lane; g < a.G; g += 32) {
+                most = max(most, sh.rows[g]);
+                all += steps_of<STEP>(sh.rows[g]);
+            }
+            for (int o = 16; o > 0; o >>= 1) {
+                most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+                all += __shfl_xor_sync(0xffffffffu, all, o);
+            }
+            // c steps make all / c chunks or more, and less than G above that: between these bounds lies what is looked for (in a few steps: of 8 parts 3 of 12)
+            const int least = max((int)a.tile_rows / STEP, (int)((all + a.tiles - 1) / a.tiles));
+            const int fits = a.tiles > a.G ? (int)min((int64_t)steps_of<STEP>(most), (all + a.tiles - a.G - 1) / (a.tiles - a.G)) : steps_of<STEP>(most);
+            const int chunk = fit_chunk(least, fits, a.tiles, [&](int steps) {
                 int64_t count = 0;
                 for (int g = lane; g < a.G; g += 32) count += (steps_of<STEP>(sh.rows[g]) + steps - 1) / steps;
                 for (int o = 16; o > 0; o >>= 1) count += __shfl_xor_sync(0xffffffffu, count, o);

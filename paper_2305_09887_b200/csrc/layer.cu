@@ -38,8 +38,8 @@ struct AlignArgs {
 constexpr int ALIGN_BYTES = 16384;
 
 // A block brings neighbouring rows as the 16-byte words that they lie in, and cuts them up in shared memory while the next ones come (200,000 x 100 in
-// fp16 25 us, 3.2 TB/s: instructions; 300,000 x 100 and x 47 44 us).  Copied by the products for every tile of columns again, such rows cost
-// more than the products: 200,000 x 100 -> 2 x 266 222 us, like this 81 and 25.
+// fp16 24 us; 300,000 x 100 and x 47 37 us, 4 TB/s: instructions, of which they issue 64 % of what they can).  Copied by the products for every tile of columns again, such rows cost
+// more than the products: 200,000 x 100 -> 2 x 266 222 us, like this 81 and 24.
 __global__ void __launch_bounds__(256) align_rows_kernel(const __grid_constant__ AlignArgs args) {
     __shared__ uint4 words[ALIGN_BYTES / 16 + 258];  // (a row's last words are read beyond it, and dropped)
     wait_for_kernel_before();
@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(256) align_rows_kernel(const __grid_constant__
     if (c >= all) return;
     Chunk now = chunk(c);
     bring(now);
-    const int ld = (int)a.ld, per_row = 4 * units, rows_on = 256 / per_row, on = 256 - rows_on * per_row;  // in values; in words of 4 bytes
+    const int ld = (int)a.ld, rows_on = 256 / units, on = 256 - rows_on * units;
     for (;;) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i)
@@ -110,20 +110,29 @@ __global__ void __launch_bounds__(256) align_rows_kernel(const __grid_constant__
             now = chunk(c);
             bring(now);
         }
-        // 4 bytes a thread, so that a warp reads and writes neighbouring ones
-        const uint32_t* w = reinterpret_cast<const uint32_t*>(words);
+        // 16 bytes a thread: two words, of which the row's place in them says which five halves are wanted
         const int shift = (int)(these.from - these.base) / 2;
-        uint32_t* out = reinterpret_cast<uint32_t*>(a.dst) + these.row0 * per_row;
-        int row = threadIdx.x / per_row, column = threadIdx.x - row * per_row;
-        for (int i = threadIdx.x; i < these.rows * per_row; i += 256) {
-            const int e = shift + row * ld + 2 * column, valid = a.d - 2 * column;
-            uint32_t v = __funnelshift_r(w[e >> 1], w[(e >> 1) + 1], 16 * (e & 1));
-            if (valid < 2) v = valid == 1 ? v & 0xFFFFu : 0u;
-            out[i] = v;
+        uint4* out = reinterpret_cast<uint4*>(a.dst) + these.row0 * units;
+        int row = threadIdx.x / units, unit = threadIdx.x - row * units;
+        for (int i = threadIdx.x; i < these.rows * units; i += 256) {
+            const int e = shift + row * ld + 8 * unit, valid = a.d - 8 * unit;
+            const uint4 lo = words[e >> 3], hi = words[(e >> 3) + 1];
+            uint32_t w[7] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z};
+            if (e & 4) {
+                w[0] = w[2]; w[1] = w[3]; w[2] = w[4]; w[3] = w[5]; w[4] = w[6]; w[5] = hi.w;
+            }
+#pragma unroll
+            for (int k = 0; k < 5; ++k) w[k] = e & 2 ? w[k + 1] : w[k];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                w[k] = __funnelshift_r(w[k], w[k + 1], 16 * (e & 1));
+                if (valid < 2 * k + 2) w[k] = valid == 2 * k + 1 ? w[k] & 0xFFFFu : 0u;
+            }
+            out[i] = make_uint4(w[0], w[1], w[2], w[3]);
             row += rows_on;
-            column += on;
-            if (column >= per_row) {
-                column -= per_row;
+            unit += on;
+            if (unit >= units) {
+                unit -= units;
                 ++row;
             }
         }
@@ -140,6 +149,8 @@ struct SumsArgs {
     int G, places, n_tiles, columns;  // columns: 0 if their sums are not wanted
     int width, real_width;            // of one of dZ's halves, with and without what was rounded up
     const float *column_slots, *slope_slots;
+    int64_t slots_up;  // as LayerArgs'
+    int groups_log;
     void* db;
     float* dslope;
     int64_t db_stride, dslope_stride;
@@ -178,9 +189,10 @@ __global__ void __launch_bounds__(SUMS_THREADS) layer_sums_kernel(const __grid_c
         if (!of_slope) {  // eight warps for the sums of a slot, every second slot
             const float* p = a.column_slots + (8 * (int64_t)(i + part) + (warp & 7)) * a.columns + min(column, a.columns - 1);
 #pragma unroll 4
-            for (int k = i + (warp >> 3); k < end; k += SUMS_THREADS / 256) {
-                const float v = p[8 * (int64_t)(k - i) * a.columns];
-                s += place_start[k] != place_start[k + 1] ? v : 0.f;
+            for (int x = warp >> 3; x < (end - i) << a.groups_log; x += SUMS_THREADS / 256) {
+                const int k = x >> a.groups_log, group = x - (k << a.groups_log);
+                const float v = p[(group * a.slots_up + 8 * (int64_t)k) * a.columns];
+                s += place_start[i + k] != place_start[i + k + 1] ? v : 0.f;
             }
         } else {
             const int per = 32 * a.n_tiles;
@@ -424,7 +436,8 @@ extern "C" int32_t rtma_grouped_layer_grad(rtma_ctx* ctx, const rtma_layer_desc*
     // All scratch at once: inside a capture nothing is enqueued unless everything fits.
     const Plan p = make_plan(ctx, d, n, G, X, ldx, W, dY, lddy, true);
     const bool column_sums = db && !f32 && !plain && n > 0;  // the bias gradient comes with dZ
-    const size_t slot_rows = 8 * (size_t)(p.places + G), column_bytes = column_sums ? ArenaCursor::granule(sizeof(float) * slot_rows * wide) : 0,
+    const Turns turns(gated ? p.half : 2 * p.half, 2 * p.half);
+    const size_t slot_rows = 8 * (size_t)(p.places + G), column_bytes = column_sums ? ArenaCursor::granule(sizeof(float) * slot_rows * turns.groups * wide) : 0,
                  slot_bytes = column_bytes + (dslope ? sizeof(float) * slot_rows * 4 * p.n_tiles : 0);
     size_t dw_bytes = 0;
     auto weights = [&](size_t* scratch) {
@@ -444,6 +457,7 @@ extern "C" int32_t rtma_grouped_layer_grad(rtma_ctx* ctx, const rtma_layer_desc*
             LayerArgs a = layer_args(ctx, p, d, n, G, offsets, X, ldx, W, w_stride, b, slope, dY, lddy, dZ, lddz, width);
             a.column_slots = column_sums ? reinterpret_cast<float*>(ctx->arena + p.end) : nullptr;
             a.columns = wide;
+            a.slots_up = (int64_t)slot_rows;
             a.slope_slots = dslope ? reinterpret_cast<float*>(ctx->arena + p.end + column_bytes) : nullptr;
             RTMA_TRY(launch_layer(ctx, a, p, d, true, wide, stream));
         }
@@ -452,6 +466,7 @@ extern "C" int32_t rtma_grouped_layer_grad(rtma_ctx* ctx, const rtma_layer_desc*
         SumsArgs m{};
         m.offsets = offsets; m.n = n; m.tile_rows = PAIR_ROWS; m.tiles = p.tiles;
         m.G = G; m.places = p.places; m.n_tiles = p.n_tiles; m.columns = column_sums ? wide : 0;
+        m.groups_log = turns.groups == 4 ? 2 : turns.groups - 1; m.slots_up = (int64_t)slot_rows;
         m.width = width; m.real_width = d->d_out;
         m.column_slots = reinterpret_cast<const float*>(ctx->arena + p.end); m.slope_slots = reinterpret_cast<const float*>(ctx->arena + p.end + column_bytes);
         m.db = db; m.dslope = dslope; m.db_stride = db_stride; m.dslope_stride = dslope_stride;

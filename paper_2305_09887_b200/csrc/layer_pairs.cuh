@@ -109,6 +109,7 @@ __device__ __forceinline__ void pair_multiplier(const LayerArgs& a, PairShared& 
     const uint32_t format = std::is_same<typename F::T, __half>::value ? 0u : 1u;  // fp16 or bf16 operands, fp32 sums
     const uint32_t idesc = (1u << 4) | (format << 7) | (format << 10) | (1u << 16) | ((uint32_t)(2 * a.half >> 3) << 17) | ((uint32_t)(2 * BM >> 4) << 24);
     const uint64_t desc = tc::smem_desc_sw128(0, 2 * SLAB_BYTES, 1024);  // atoms of 64 columns lie two slabs apart
+    const Turns turns(F::GATED ? a.half : 2 * a.half, 2 * a.half);
     PairWalk w;
     tc::RingAt at, acc;
     int part = -1;
@@ -119,7 +120,7 @@ __device__ __forceinline__ void pair_multiplier(const LayerArgs& a, PairShared& 
             if (!wait_for<true>(&sh.held_full, changes++ & 1u, sh, a.error_word)) return;
         }
         if (!wait_for<true>(&sh.acc_empty[acc.s], acc.phase ^ 1u, sh, a.error_word)) return;
-        const uint32_t d = sh.tmem_base + acc.s * 256;
+        const uint32_t d = sh.tmem_base + acc.s * turns.spacing;
         for (int k = 0; k < blocks; ++k) {
             if (!wait_for<true>(&sh.full[at.s], at.phase, sh, a.error_word)) return;
             tc::tc_fence_after_sync();
@@ -134,7 +135,7 @@ __device__ __forceinline__ void pair_multiplier(const LayerArgs& a, PairShared& 
             at.advance(F::STAGES);
         }
         tc::commit_pair_by_warp(&sh.acc_full[acc.s]);
-        acc.advance(2);
+        acc.advance(turns.buffers);
         if (F::RESIDENT && w.part_ends(sh)) tc::commit_pair_by_warp(&sh.held_empty);
     }
 }
@@ -171,7 +172,9 @@ __device__ __forceinline__ void pair_drain(const LayerArgs& a, PairShared& sh, u
     typedef Outlet<T, F::SLABS> Out;
     constexpr bool GATED = F::GATED, GRADIENT = F::GRADIENT;
     constexpr int ITEMS = GATED ? 1 : 2, PIECE = 16 / (int)sizeof(T);  // chunks of 32 columns a tile for a warp, at most
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, slice = warp >> 2;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3;
+    const Turns turns(GATED ? a.half : 2 * a.half, 2 * a.half);
+    const int slice = (warp >> 2) % turns.slices, group = (warp >> 2) / turns.slices;
     slabs += warp * F::OUT_BYTES;
     LayerBias bias{sh.bias + 64 * warp};
     uint64_t* const side = sh.side[warp];
@@ -184,10 +187,12 @@ __device__ __forceinline__ void pair_drain(const LayerArgs& a, PairShared& sh, u
     PairWalk w, ahead;
     bool more = w.open(a, sh), ahead_more = more && BESIDE && mine > 0;
     ahead = w;
+    const int start = w.t;
+    auto is_mine = [&](const PairWalk& x) { return (x.t - start & turns.groups - 1) == group; };
     int ahead_item = 0;
     // The rows beside the next 32 columns that are this warp's, into slab n & 1, whose last store has to have been read.
     auto request = [&](uint32_t n) {
-        while (ahead_more && ahead.left <= above) ahead_more = ahead.next(sh);  // (a tile that ends above this warp's rows)
+        while (ahead_more && (ahead.left <= above || !is_mine(ahead))) ahead_more = ahead.next(sh);  // (a tile that ends above this warp's rows)
         if (!ahead_more) return;
         if (lane == 0) {
             uint64_t* bar = &side[n & 1];
@@ -227,9 +232,9 @@ __device__ __forceinline__ void pair_drain(const LayerArgs& a, PairShared& sh, u
         tc::tc_fence_after_sync();
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            if (rows <= 0 || i >= mine) break;
+            if (rows <= 0 || i >= mine || !is_mine(w)) break;
             const int c = column(i), cols = columns(i);
-            const uint32_t from = tmem + acc.s * 256 + 32 * (slice + 4 * i);
+            const uint32_t from = tmem + acc.s * turns.spacing + 32 * (slice + 4 * i);
             const uint32_t slab = slabs + (n & 1) * F::SLAB, other = slabs + 2 * F::SLAB;
             uint32_t x[2][8], x2[2][8];
             tc::tmem_load_issue_8(from, x[0]);
@@ -308,18 +313,18 @@ __device__ __forceinline__ void pair_drain(const LayerArgs& a, PairShared& sh, u
         tc::tc_fence_before_sync();
         __syncwarp();
         if (lane == 0) tc::mbar_arrive_remote(tc::leader_addr(&sh.acc_empty[acc.s]));  // (a pair's warps all report to the first block)
-        acc.advance(2);
+        acc.advance(turns.buffers);
         if (GRADIENT && (w.part_ends(sh) || w.t % SUMMED_TILES == SUMMED_TILES - 1)) {
             const int pair = blockIdx.x >> 1, place = pair / a.n_tiles;
             // the part's first tile here; again: the slots hold sums of tiles before these
             const int first = max((int)((int64_t)sh.tile_start[a.G] * place / a.places), sh.tile_start[part]);
             const bool again = first / SUMMED_TILES < w.t / SUMMED_TILES;
-            const int64_t slot = 8 * (int64_t)(place + part) + 4 * rank + quarter;
+            const int64_t slot = 8 * (int64_t)(place + part) + 4 * rank + quarter;  // (of the first group)
             if (a.column_slots) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     if ((lane & 3) || (GATED ? mine < 1 : i >= mine)) continue;
-                    float* const to = a.column_slots + slot * a.columns + (GATED ? column(0) + (i ? a.width : 0) : column(i));
+                    float* const to = a.column_slots + (group * a.slots_up + slot) * a.columns + (GATED ? column(0) + (i ? a.width : 0) : column(i));
                     const int cols = GATED ? columns(0) : columns(i);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
@@ -330,7 +335,7 @@ __device__ __forceinline__ void pair_drain(const LayerArgs& a, PairShared& sh, u
             }
             if (ACT == RTMA_ACT_PRELU && a.slope_slots) {
                 for (int o = 16; o > 0; o >>= 1) slope_sum += __shfl_xor_sync(0xffffffffu, slope_sum, o);
-                float* const to = a.slope_slots + (slot * a.n_tiles + (pair - place * a.n_tiles)) * 4 + slice;
+                float* const to = a.slope_slots + (slot * a.n_tiles + (pair - place * a.n_tiles)) * 4 + (warp >> 2);
                 if (lane == 0) *to = slope_sum + (again ? *to : 0.f);
             }
             clear();
@@ -357,7 +362,7 @@ __device__ __forceinline__ void pair_body(const LayerArgs& a) {
             tc::mbar_init(&sh.full[s], 1);
             tc::mbar_init(&sh.empty[s], 1);
         }
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < 4; ++b) {
             tc::mbar_init(&sh.acc_full[b], 1);
             tc::mbar_init(&sh.acc_empty[b], 2 * F::DRAIN_WARPS);  // the first block counts the warps of both
         }

@@ -6,7 +6,7 @@
 // grouped_linear.cu 456 and 127.  The parts' rows are cut into chunks as there, one slot of fp32 sums for each, added up by a second kernel.
 //
 // The tensor cores truncate when they accumulate: sixteen warps take the accumulator after every 128 rows and add it up in registers, rounded to
-// nearest, 64 columns of a row in a lane.  The same warps take dZ's column sums from the stages where no kernel before has (layers without activation
+// nearest, a quarter of a row's columns in a lane.  The same warps take dZ's column sums from the stages where no kernel before has (layers without activation
 // or gate: 500,000 x 256 x 1,024 351 us; as products with ones by mma.sync, which the MMAs wait for, 415).
 #include <algorithm>
 
@@ -33,7 +33,7 @@ constexpr int SUMS_REGISTERS = 104, OTHER_REGISTERS = 64;  // 512 x 104 + 128 x 
 struct GradArgs : LinearArgs {  // A, map_a: the left operand, B, map_b: the right one
     int left, right;   // their widths
     bool swapped;      // dZ is the left one
-    int half;          // columns of the right one that a block brings
+    int left_half, half;  // columns that a block brings, of the left one 64 or 128
     bool sums;         // of dZ's columns are wanted
     int sum_rows;      // sums of dZ's columns in a slot, behind the weights: of as many shares of the rows
     float* slots;      // [row tile][d_in + sum_rows][ldo]
@@ -62,7 +62,7 @@ struct GradWalk {
         const int rest = tile - row_tile * per;
         m0 = rest / a.n_tiles;
         n0 = (rest - m0 * a.n_tiles) * 2 * a.half;
-        m0 *= LEFT;
+        m0 *= 2 * a.left_half;
         while (row_tile >= sh.tile_start[part + 1]) ++part;  // tiles come in ascending order
         const int64_t inside = (int64_t)(row_tile - sh.tile_start[part]) * sh.tile_rows;
         row0 = sh.begin[part] + inside;
@@ -91,14 +91,14 @@ struct GradWalk {
     __device__ __forceinline__ bool sums(const GradArgs& a) const { return a.sums && (a.swapped ? n0 : m0) == 0; }
 };
 
-// One warp.  Rows behind the end of a chunk belong to another part: the last stage's rows are copied by the lanes, with zeros behind them.
-template <class T>
+// A warp for either operand (500,000 x 256 x 1,024: one for both 321 us, these two 293).  Rows behind the end of a chunk belong to
+// another part: the last stage's rows are copied by the lanes, with zeros behind them.
+template <class T, bool RIGHT>
 __device__ __forceinline__ void grad_producer(const GradArgs& a, GradShared& sh, uint8_t* ring, int rank, int lane) {
-    if (lane == 0) {
-        tc::prefetch_tensormap(&a.map_a);
-        tc::prefetch_tensormap(&a.map_b);
-    }
-    const int atoms = (a.half + 63) / 64;
+    const CUtensorMap* const map = RIGHT ? &a.map_b : &a.map_a;
+    if (lane == 0) tc::prefetch_tensormap(map);
+    const int atoms = RIGHT ? (a.half + 63) / 64 : a.left_half / 64, up = (RIGHT ? a.half : a.left_half) * rank, width = RIGHT ? a.right : a.left;
+    ring += RIGHT ? 4 * SLAB_BYTES : 0;
     GradWalk<BK> w;
     tc::RingAt at;
     int filled = 0;  // stages, STAGES at most
@@ -111,27 +111,23 @@ __device__ __forceinline__ void grad_producer(const GradArgs& a, GradShared& sh,
         filled = min(filled + 1, STAGES);
         uint8_t* stage = ring + at.s * STAGE_BYTES;
         const uint32_t bar = tc::leader_addr(&sh.full[at.s]);
-        const int m = w.m0 + 128 * rank, n = w.n0 + a.half * rank;
+        const int first = (RIGHT ? w.n0 : w.m0) + up;
         if (w.k0 + BK > w.k_end) {
-            const T *A = static_cast<const T*>(a.A), *B = static_cast<const T*>(a.B);
-            for (int j = lane; j < (2 + atoms) * 512; j += 32) {
-                const int atom = j >> 9, row = j >> 3 & 63, unit = j & 7, k = w.k0 + row;
-                const bool is_left = atom < 2;
-                const int c = is_left ? m + 64 * atom + 8 * unit : n + 64 * (atom - 2) + 8 * unit, width = is_left ? a.left : a.right;
+            const int64_t ld = RIGHT ? a.ldb : a.lda;
+            const T* const from = static_cast<const T*>(RIGHT ? a.B : a.A);
+            for (int j = lane; j < atoms * 512; j += 32) {
+                const int atom = j >> 9, row = j >> 3 & 63, unit = j & 7, k = w.k0 + row, c = first + 64 * atom + 8 * unit;
                 const int valid = k < w.k_end ? max(0, min(8, width - c)) : 0;
-                const T* p = is_left ? A : B;
-                if (valid) p += (w.row0 + k) * (is_left ? a.lda : a.ldb) + c;
-                copy<16>(tc::smem_u32(stage) + atom * 2 * SLAB_BYTES + row * 128 + ((unit ^ (row & 7)) << 4), p, valid * (int)sizeof(T));
+                copy<16>(tc::smem_u32(stage) + atom * 2 * SLAB_BYTES + row * 128 + ((unit ^ (row & 7)) << 4), valid ? from + (w.row0 + k) * ld + c : from, valid * (int)sizeof(T));
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
             tc::fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) tc::mbar_arrive_cluster(bar);
         } else if (lane == 0) {
-            if (rank == 0) tc::mbar_arrive_expect_tx(&sh.full[at.s], 2 * (2 + atoms) * 2 * SLAB_BYTES);
+            if (rank == 0) tc::mbar_arrive_expect_tx(&sh.full[at.s], 2 * atoms * 2 * SLAB_BYTES);
             else tc::mbar_arrive_remote(bar);
-            for (int i = 0; i < 2; ++i) tc::tma_load_3d_pair(stage + i * 2 * SLAB_BYTES, &a.map_a, bar, m + 64 * i, (int)w.row0 + w.k0, 0);
-            for (int i = 0; i < atoms; ++i) tc::tma_load_3d_pair(stage + (2 + i) * 2 * SLAB_BYTES, &a.map_b, bar, n + 64 * i, (int)w.row0 + w.k0, 0);
+            for (int i = 0; i < atoms; ++i) tc::tma_load_3d_pair(stage + i * 2 * SLAB_BYTES, map, bar, first + 64 * i, (int)w.row0 + w.k0, 0);
         }
         __syncwarp();
     }
@@ -148,6 +144,9 @@ __device__ __forceinline__ void grad_producer(const GradArgs& a, GradShared& sh,
     }
 }
 
+// Of 512 columns: the way from the MMAs to the warps that drain and back takes longer than narrow tiles' MMAs do.
+__device__ __forceinline__ int accumulators(const GradArgs& a) { return 2 * a.half <= 512 / MAX_ACCUMULATORS ? MAX_ACCUMULATORS : 2; }
+
 template <class T>
 __device__ __forceinline__ void grad_multiplier(const GradArgs& a, GradShared& sh, uint32_t ring) {
     const uint32_t format = std::is_same<T, __half>::value ? 0u : 1u;  // fp16 or bf16 operands, fp32 sums
@@ -155,6 +154,7 @@ __device__ __forceinline__ void grad_multiplier(const GradArgs& a, GradShared& s
     const uint64_t desc = tc::smem_desc_sw128(0, 2 * SLAB_BYTES, 1024);  // atoms of 64 columns lie two slabs apart
     GradWalk<BK> w;
     tc::RingAt at, acc;
+    const int ring_of_acc = accumulators(a);
     int held = 0;  // stages in the accumulator
     for (bool more = w.first(a, sh); more; more = w.next(a, sh)) {
         if (held == 0 && !wait_for<true>(&sh.acc_empty[acc.s], acc.phase ^ 1u, sh, a.error_word)) return;
@@ -162,7 +162,7 @@ __device__ __forceinline__ void grad_multiplier(const GradArgs& a, GradShared& s
         tc::tc_fence_after_sync();
         __syncwarp();
         if (a.sums) tc::commit_pair_by_warp(&sh.ready[at.s]);  // (both blocks learn of the stage when the one before has been multiplied)
-        const uint32_t d = sh.tmem_base + acc.s * 256, stage = ring + at.s * STAGE_BYTES;
+        const uint32_t d = sh.tmem_base + acc.s * (512 / ring_of_acc), stage = ring + at.s * STAGE_BYTES;
         const uint64_t da = desc + (stage >> 4), db = da + (4 * SLAB_BYTES >> 4);
         const int steps = (min(BK, w.k_end - w.k0) + 15) >> 4;
 #pragma unroll
@@ -173,7 +173,7 @@ __device__ __forceinline__ void grad_multiplier(const GradArgs& a, GradShared& s
         if (++held == ACC_STAGES || w.last_stage()) {
             held = 0;
             tc::commit_pair_by_warp(&sh.acc_full[acc.s]);
-            acc.advance(2);
+            acc.advance(ring_of_acc);
         }
     }
 }
@@ -213,13 +213,13 @@ struct ColumnSums {
 };
 
 // before(w, k0): what is done before the accumulator of the rows from k0 on is waited for; after(w): at the end of a tile.
-// RING, SPACING: of accumulators and their columns.  TURNED: of every 64 columns of an operand the upper 32 lie with the halves of each eight the other way
+// spacing: columns from one accumulator to the next.  TURNED: of every 64 columns of an operand the upper 32 lie with the halves of each eight the other way
 // around (see grad_f32_splitter).
-template <int STEP, int TAKEN, int RING, int SPACING, bool TURNED, class S, class Before, class After>
-__device__ __forceinline__ void grad_drain(const GradArgs& a, S& sh, int rank, Before before, After after) {
+template <int STEP, int TAKEN, int SLICES, bool TURNED, class S, class Before, class After>
+__device__ __forceinline__ void grad_drain(const GradArgs& a, S& sh, int rank, int accumulators, int spacing, Before before, After after) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, slice = warp >> 2;
-    const uint32_t tmem = sh.tmem_base + ((uint32_t)(32 * quarter) << 16) + 64 * slice;
-    const bool mine = 64 * slice < 2 * a.half;
+    const int per = 2 * a.half / SLICES;  // columns of a warp: a multiple of 8, 64 at most
+    const uint32_t tmem = sh.tmem_base + ((uint32_t)(32 * quarter) << 16) + per * slice;
     GradWalk<STEP> w;
     tc::RingAt acc;
     for (bool more = w.first(a, sh); more; more = w.next_tile(a, sh)) {
@@ -231,30 +231,30 @@ __device__ __forceinline__ void grad_drain(const GradArgs& a, S& sh, int rank, B
             if (!wait_for<true>(&sh.acc_full[acc.s], acc.phase, sh, a.error_word)) return;
             __syncwarp();
             tc::tc_fence_after_sync();
-            if (mine) {
-                const uint32_t from = tmem + acc.s * SPACING;
-                uint32_t x[2][8];
-                tc::tmem_load_issue_8(from, x[0]);
+            const uint32_t from = tmem + acc.s * spacing;
+            uint32_t x[2][8];
+            tc::tmem_load_issue_8(from, x[0]);
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    tc::tmem_load_wait_8(x[q & 1]);
-                    if (q < 7) tc::tmem_load_issue_8(from + 8 * (q + 1), x[(q + 1) & 1]);
+            for (int q = 0; q < 8; ++q) {
+                tc::tmem_load_wait_8(x[q & 1]);
+                const bool last = q == 7 || 8 * (q + 1) >= per;
+                if (!last) tc::tmem_load_issue_8(from + 8 * (q + 1), x[(q + 1) & 1]);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) total[4 * q + j] = add2(total[4 * q + j], pack2(__uint_as_float(x[q & 1][2 * j]), __uint_as_float(x[q & 1][2 * j + 1])));
-                }
+                for (int j = 0; j < 4; ++j) total[4 * q + j] = add2(total[4 * q + j], pack2(__uint_as_float(x[q & 1][2 * j]), __uint_as_float(x[q & 1][2 * j + 1])));
+                if (last) break;
             }
             tc::tc_fence_before_sync();
             __syncwarp();
             if (lane == 0) tc::mbar_arrive_remote(tc::leader_addr(&sh.acc_empty[acc.s]));  // (a pair's warps all report to the first block)
-            acc.advance(RING);
+            acc.advance(accumulators);
         }
         after(w);
-        const int m = w.m0 + 128 * rank + 32 * quarter + (TURNED && (quarter & 1) ? lane ^ 4 : lane), n = w.n0 + 64 * slice;
-        const int cols = min(64, min(2 * a.half - 64 * slice, a.right - n));
+        const int m = w.m0 + a.left_half * rank + 32 * quarter + (TURNED && (quarter & 1) ? lane ^ 4 : lane), n = w.n0 + per * slice;
+        const int cols = min(per, a.right - n);
         if constexpr (TURNED) {
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
-                if ((64 * slice + 8 * q) % a.half < 32) continue;
+                if ((per * slice + 8 * q) % a.half < 32) continue;
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const f2 t = total[4 * q + j];
@@ -263,7 +263,7 @@ __device__ __forceinline__ void grad_drain(const GradArgs& a, S& sh, int rank, B
                 }
             }
         }
-        if (m < a.left && cols > 0) {
+        if (32 * quarter < a.left_half && m < a.left && cols > 0) {
             float* const slot = a.slots + (int64_t)w.row_tile * (a.d_in + a.sum_rows) * a.ldo;
             if (a.swapped) {  // a lane's column of dZ: neighbours beside one another
                 float* to = slot + (int64_t)n * a.ldo + m;
@@ -302,12 +302,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) layer_wg
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
-            tc::mbar_init(&sh.full[s], 2);  // both blocks'
+            tc::mbar_init(&sh.full[s], 4);  // both blocks', of either operand
             tc::mbar_init(&sh.empty[s], 1);
             tc::mbar_init(&sh.ready[s], 1);
             tc::mbar_init(&sh.free[s], DRAIN_WARPS);
         }
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < MAX_ACCUMULATORS; ++b) {
             tc::mbar_init(&sh.acc_full[b], 1);
             tc::mbar_init(&sh.acc_empty[b], 2 * DRAIN_WARPS);
         }
@@ -330,8 +330,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) layer_wg
         tc::RingAt at;
         ColumnSums<T> sums;
         sums.clear();
-        grad_drain<BK, ACC_STAGES * BK, 2, 256, false>(
-            a, sh, rank,
+        grad_drain<BK, ACC_STAGES * BK, DRAIN_WARPS / 4, false>(
+            a, sh, rank, accumulators(a), 512 / accumulators(a),
             [&](const GradWalk<BK>& w, int k0) {
                 if (!a.sums) return true;
                 for (int k = k0; k < min(k0 + ACC_STAGES * BK, w.k_end); k += BK) {
@@ -346,7 +346,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) layer_wg
             },
             [&](const GradWalk<BK>& w) {
                 if (!w.sums(a)) return;
-                const int of_block = a.swapped ? 128 : a.half, first = a.swapped ? w.m0 + 128 * rank : w.n0 + a.half * rank;
+                const int of_block = a.swapped ? a.left_half : a.half, first = a.swapped ? w.m0 + a.left_half * rank : w.n0 + a.half * rank;
                 float* const to = a.slots + ((int64_t)w.row_tile * (a.d_in + a.sum_rows) + a.d_in + (warp & 1)) * a.ldo + first;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -359,7 +359,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) layer_wg
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGISTERS));
         if (warp == DRAIN_WARPS && rank == 0) grad_multiplier<T>(a, sh, ring);
-        if (warp == DRAIN_WARPS + 1) grad_producer<T>(a, sh, ring_bytes, rank, lane);
+        if (warp == DRAIN_WARPS + 1) grad_producer<T, false>(a, sh, ring_bytes, rank, lane);
+        if (warp == DRAIN_WARPS + 2) grad_producer<T, true>(a, sh, ring_bytes, rank, lane);
     }
     __syncwarp();
     if (*reinterpret_cast<volatile int*>(&sh.abort)) __nanosleep(1000000);  // a wait ran out: copies and MMAs under way land before the block ends
@@ -375,7 +376,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) layer_wg
 // ---- fp32 rows ----------------------------------------------------------------------------------
 // Six MMAs a product on three bf16 numbers a value, a fresh accumulator for every 32 rows (layer_f32.cu); tiles of 256 x 128.  Splitting is what bounds
 // it (100,000 x 128 x 512: 94 us, 75 with nothing split; eight warps with fewer registers and tiles of twice the width 150): twelve warps do it, four for
-// every 64 columns, always the same ones, so that they add up dZ's columns on the way.  56 bytes a thread are spilled, of warps that drain.
+// every 64 columns, always the same ones, so that they add up dZ's columns on the way.  40 bytes a thread are spilled, of warps that drain.
 struct GradF32Shared : Shared {
     uint64_t raw_full[RAW_STAGES], raw_free[RAW_STAGES];
 };
@@ -383,16 +384,16 @@ struct GradF32Shared : Shared {
 __device__ __forceinline__ void grad_f32_producer(const GradArgs& a, GradF32Shared& sh, uint8_t* raw, int rank) {
     tc::prefetch_tensormap(&a.map_a);
     tc::prefetch_tensormap(&a.map_b);
-    const int boxes = (a.half + 31) / 32;
+    const int left_boxes = a.left_half / 32, boxes = (a.half + 31) / 32;
     GradWalk<F32_BK> w;
     tc::RingAt at;
     for (bool more = w.first(a, sh); more; more = w.next(a, sh), at.advance(RAW_STAGES)) {
         if (!wait_for(&sh.raw_free[at.s], at.phase ^ 1u, sh, a.error_word)) return;
         uint8_t* stage = raw + at.s * RAW_BYTES;
         uint64_t* bar = &sh.raw_full[at.s];
-        tc::mbar_arrive_expect_tx(bar, (4 + boxes) * 4096);
+        tc::mbar_arrive_expect_tx(bar, (left_boxes + boxes) * 4096);
         const int row = (int)w.row0 + w.k0;
-        for (int i = 0; i < 4; ++i) tc::tma_load_3d(stage + 4096 * i, &a.map_a, bar, 2 * (w.m0 + 128 * rank + 32 * i), row, 0);
+        for (int i = 0; i < left_boxes; ++i) tc::tma_load_3d(stage + 4096 * i, &a.map_a, bar, 2 * (w.m0 + a.left_half * rank + 32 * i), row, 0);
         for (int i = 0; i < boxes; ++i) tc::tma_load_3d(stage + 4096 * (4 + i), &a.map_b, bar, 2 * (w.n0 + a.half * rank + 32 * i), row, 0);
     }
 }
@@ -458,7 +459,7 @@ __device__ __forceinline__ void grad_f32_splitter(const GradArgs& a, GradF32Shar
             }
         }
         if (w.last_stage() && of_dz) {
-            const int left = a.swapped ? 128 - 64 * atom : a.half, first = a.swapped ? w.m0 + 128 * rank + 64 * atom : w.n0 + a.half * rank;
+            const int left = a.swapped ? a.left_half - 64 * atom : a.half, first = a.swapped ? w.m0 + a.left_half * rank + 64 * atom : w.n0 + a.half * rank;
             float* const to_sums = a.slots + ((int64_t)w.row_tile * (a.d_in + a.sum_rows) + a.d_in + (which & 3)) * a.ldo + first;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -546,7 +547,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(F32_THREADS, 1) laye
     const int rank = (int)tc::cluster_rank();
     if (warp < DRAINS) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SUMS_REGISTERS));
-        grad_drain<F32_BK, F32_BK, F32_STAGES, 128, true>(a, sh, rank, [](const GradWalk<F32_BK>&, int) { return true; }, [](const GradWalk<F32_BK>&) {});
+        grad_drain<F32_BK, F32_BK, F32_DRAIN_WARPS / 4, true>(a, sh, rank, F32_STAGES, 128, [](const GradWalk<F32_BK>&, int) { return true; }, [](const GradWalk<F32_BK>&) {});
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(F32_OTHER_REGISTERS));
         if (warp == DRAINS && rank == 0) grad_f32_multiplier(a, sh, planes);
@@ -637,12 +638,14 @@ int32_t layer_dw(rtma_ctx* ctx, const char* who, const rtma_layer_desc* d, int64
     a.span = shared ? G : 1;
     a.d_in = d_in; a.d_out = d_out;
     // MMAs of either orientation, in columns of the right operand
-    const int64_t as_left = ceil_div(d_in, LEFT) * ceil_div(d_out, 32), swapped = ceil_div(d_out, LEFT) * ceil_div(d_in, 32);
+    auto tile = [](int columns) { return columns > LEFT / 2 ? LEFT : LEFT / 2; };  // of half of the columns both blocks bring a half: rows of few bytes are what loads take long for
+    const int64_t as_left = ceil_div(d_in, tile(d_in)) * ceil_div(d_out, 32), swapped = ceil_div(d_out, tile(d_out)) * ceil_div(d_in, 32);
     a.swapped = swapped <= as_left;
     a.left = a.swapped ? d_out : d_in; a.right = a.swapped ? d_in : d_out;
     a.A = a.swapped ? dZ : X; a.lda = a.swapped ? lddz : ldx;
     a.B = a.swapped ? X : dZ; a.ldb = a.swapped ? ldx : lddz;
-    a.m_tiles = (int)ceil_div(a.left, LEFT);
+    a.left_half = tile(a.left) / 2;
+    a.m_tiles = (int)ceil_div(a.left, 2 * a.left_half);
     const int widest = f32 ? 2 * F32_HALF : 256;  // columns of the right operand in a tile
     a.n_tiles = (int)ceil_div(a.right, widest);
     a.half = (int)ceil_div(ceil_div(a.right, a.n_tiles), 32) * 16;

@@ -14,7 +14,7 @@ MOST = {
     "layer_bf16.cu": {},
     "layer_f16.cu": {},
     "layer_f32.cu": {"layer_f32_kernelILb0ELb0E": 196, "layer_f32_kernelILb0ELb1E": 108, "layer_f32_kernelILb1ELb0E": 88, "layer_f32_kernelILb1ELb1E": 260},
-    "layer_wgrad.cu": {"layer_wgrad_f32_kernel": 56},
+    "layer_wgrad.cu": {"layer_wgrad_f32_kernel": 40},
     "clip.cu": {},
 }
 
