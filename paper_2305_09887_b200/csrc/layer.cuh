@@ -88,11 +88,11 @@ struct LayerBias {
     }
 };
 
-// Narrow tiles of 16-bit rows: where columns leave warps without any, groups of warps take tiles by turns, out of four accumulators instead of two (300,000 x 100 -> 47,
-// first step of the gradient 46 -> 41 us).
+// Narrow tiles: where columns leave warps without any, groups of warps take tiles by turns, out of four accumulators instead of two (fp16 300,000 x 100 ->
+// 47, first step of the gradient 46 -> 41 us; fp32 700,000 x 64 -> 2 125 -> 99, 64 -> 64 135 -> 105).
 struct Turns {
-    int groups, slices, buffers, spacing;  // slices: warps for each quarter of the rows that share a tile's columns, 32 each (64 of more than 128)
-    // wide: columns that are drained, columns: of the accumulator
+    int groups, slices, buffers, spacing;  // slices: warps for each quarter of the rows that share a tile's columns
+    // wide: columns of a tile, of which a warp takes 32 (or every fourth 32) of its rows (fp32: half of the columns, as a warp takes 64), columns: of its accumulator
     __host__ __device__ Turns(int wide, int columns) {
         slices = wide <= 32 ? 1 : wide <= 64 ? 2 : 4;
         groups = 4 / slices;

@@ -9,7 +9,7 @@
 //   16 warps   take 64 columns of 32 rows of the accumulator after every stage, and a finished tile through the layer, 16 columns at a time
 // 200,000 x 256 -> 256 with a residual branch 170 us, of which the MMAs take 105 (1.5 PFLOP/s of bf16): a tile's results and what is read beside them
 // leave and come in one go, while the MMAs can be two stages ahead only.  All steps in turn by the same warps, two blocks on an SM as in
-// grouped_split.cu, took 327.  Spilled, by the warps that drain: 88 to 260 bytes a thread, once a tile.
+// grouped_split.cu, took 327.  Spilled, by the warps that drain: 120 to 304 bytes a thread, once a tile.
 //
 // The two matrices of a gated layer lie by turns of 32 columns in the planes: the 64 columns of a warp are then 32 results, and a lane has both
 // factors of each of its own.
@@ -134,14 +134,15 @@ __device__ __forceinline__ uint64_t describe(uint32_t lbo, uint32_t sbo, bool na
 __device__ __forceinline__ void f32_multiplier(const LayerArgs& a, F32Shared& sh, uint32_t rows, uint32_t planes) {
     const uint32_t idesc = tc::idesc_bf16(2 * BM, 2 * a.half, false, true);
     constexpr uint32_t ap = A_PLANE >> 4, wp = 64 * BK * 2 >> 4;  // from one plane to the next
+    const Turns turns(a.half, 2 * a.half);
     StageWalk w;
-    tc::RingAt at;
+    tc::RingAt at, acc;
     for (bool more = w.open(a, sh); more; more = w.next(sh)) {
-        if (!wait_for<true>(&sh.acc_empty[at.s], at.phase ^ 1u, sh, a.error_word)) return;
+        if (!wait_for<true>(&sh.acc_empty[acc.s], acc.phase ^ 1u, sh, a.error_word)) return;
         if (!wait_for<true>(&sh.full[at.s], at.phase, sh, a.error_word)) return;
         tc::tc_fence_after_sync();
         __syncwarp();
-        const uint32_t d = sh.tmem_base + at.s * 256;
+        const uint32_t d = sh.tmem_base + acc.s * turns.spacing;
         const uint64_t da = describe(16, 512, true) + ((rows + at.s * A_BYTES) >> 4), db = describe(W_ATOM, 1024, false) + ((planes + at.s * W_BYTES) >> 4);
         const bool two = a.d_in - BK * w.k > 16;
         tc::mma_pair_by_warp(d, da + 2 * ap, db, idesc, 0u);
@@ -160,7 +161,8 @@ __device__ __forceinline__ void f32_multiplier(const LayerArgs& a, F32Shared& sh
         }
         tc::mma_pair_by_warp(d, da, db, idesc, 1u);
         tc::commit_pair_by_warp(&sh.empty[at.s]);
-        tc::commit_pair_by_warp(&sh.acc_full[at.s]);
+        tc::commit_pair_by_warp(&sh.acc_full[acc.s]);
+        acc.advance(turns.buffers);
         at.advance(STAGES);
     }
 }
@@ -169,7 +171,9 @@ template <bool GATED, bool GRADIENT, int ACT, bool BESIDE>
 __device__ __forceinline__ void f32_drain(const LayerArgs& a, F32Shared& sh, uint32_t slabs, int rank) {
     typedef Outlet<float, SLABS> Out;
     constexpr int ITEMS = GATED ? 2 : 4;  // of 16 results a row
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, slice = warp >> 2;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3;
+    const Turns turns(a.half, 2 * a.half);
+    const int slice = (warp >> 2) % turns.slices, group = (warp >> 2) / turns.slices;
     slabs += warp * SLABS * SLAB;
     LayerBias bias{sh.bias + 64 * warp};
     uint64_t* const side = sh.side[warp];
@@ -181,11 +185,11 @@ __device__ __forceinline__ void f32_drain(const LayerArgs& a, F32Shared& sh, uin
     tc::RingAt acc;
     uint32_t n = 0;  // slabs of 16 results that this warp has been through
     float slope = 0.f, slope_sum = 0.f;
-    int part = -1;
-    for (bool more = w.open(a, sh); more; more = w.next(sh)) {
+    int part = -1, turn = 0;
+    for (bool more = w.open(a, sh); more; more = w.next(sh), turn = turn + 1 & turns.groups - 1) {
         const int rows = min(32, w.left - above);
         const int64_t row0 = w.first_row + above;
-        const bool some = rows > 0 && mine > 0;
+        const bool some = rows > 0 && mine > 0 && turn == group;
         // the rows beside 16 results, into slab (n + j) & 1, whose last store has to have been read
         auto request = [&](int j) {
             if (j >= mine || lane) return;
@@ -217,7 +221,7 @@ __device__ __forceinline__ void f32_drain(const LayerArgs& a, F32Shared& sh, uin
             __syncwarp();
             tc::tc_fence_after_sync();
             if (some) {
-                const uint32_t from = tmem + acc.s * 256;
+                const uint32_t from = tmem + acc.s * turns.spacing;
                 uint32_t x[2][8];
                 tc::tmem_load_issue_8(from, x[0]);
 #pragma unroll
@@ -231,7 +235,7 @@ __device__ __forceinline__ void f32_drain(const LayerArgs& a, F32Shared& sh, uin
             tc::tc_fence_before_sync();
             __syncwarp();
             if (lane == 0) tc::mbar_arrive_remote(tc::leader_addr(&sh.acc_empty[acc.s]));  // (a pair's warps all report to the first block)
-            acc.advance(STAGES);
+            acc.advance(turns.buffers);
         }
         if (some) {
             float ds = 0.f;
@@ -308,7 +312,7 @@ __device__ __forceinline__ void f32_drain(const LayerArgs& a, F32Shared& sh, uin
         if (GRADIENT && ACT == RTMA_ACT_PRELU && a.slope_slots && w.part_ends(sh)) {
             for (int o = 16; o > 0; o >>= 1) slope_sum += __shfl_xor_sync(0xffffffffu, slope_sum, o);
             const int64_t slot = 8 * (int64_t)(place + part) + 4 * rank + quarter;
-            if (lane == 0) a.slope_slots[(slot * a.n_tiles + (pair - place * a.n_tiles)) * 4 + slice] = slope_sum;
+            if (lane == 0) a.slope_slots[(slot * a.n_tiles + (pair - place * a.n_tiles)) * 4 + (warp >> 2)] = slope_sum;
             slope_sum = 0.f;
         }
     }
@@ -332,8 +336,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) layer_f3
         for (int s = 0; s < STAGES; ++s) {
             tc::mbar_init(&sh.full[s], 1 + 2 * SPLIT_WARPS);  // the planes of the matrix; both blocks' rows
             tc::mbar_init(&sh.empty[s], 1);
-            tc::mbar_init(&sh.acc_full[s], 1);
-            tc::mbar_init(&sh.acc_empty[s], 2 * DRAIN_WARPS);
+        }
+        for (int b = 0; b < MAX_ACCUMULATORS; ++b) {
+            tc::mbar_init(&sh.acc_full[b], 1);
+            tc::mbar_init(&sh.acc_empty[b], 2 * DRAIN_WARPS);
         }
         for (int s = 0; s < RAW_STAGES; ++s) {
             tc::mbar_init(&sh.raw_full[s], 1);

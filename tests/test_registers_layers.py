@@ -13,7 +13,7 @@ MOST = {
     "layer.cu": {},
     "layer_bf16.cu": {},
     "layer_f16.cu": {},
-    "layer_f32.cu": {"layer_f32_kernelILb0ELb0E": 196, "layer_f32_kernelILb0ELb1E": 108, "layer_f32_kernelILb1ELb0E": 88, "layer_f32_kernelILb1ELb1E": 260},
+    "layer_f32.cu": {"layer_f32_kernelILb0ELb0E": 224, "layer_f32_kernelILb0ELb1E": 120, "layer_f32_kernelILb1ELb0E": 132, "layer_f32_kernelILb1ELb1E": 304},
     "layer_wgrad.cu": {"layer_wgrad_f32_kernel": 40},
     "clip.cu": {},
 }
