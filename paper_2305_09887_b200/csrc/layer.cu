@@ -436,7 +436,7 @@ extern "C" int32_t rtma_grouped_layer_grad(rtma_ctx* ctx, const rtma_layer_desc*
     // All scratch at once: inside a capture nothing is enqueued unless everything fits.
     const Plan p = make_plan(ctx, d, n, G, X, ldx, W, dY, lddy, true);
     const bool column_sums = db && !f32 && !plain && n > 0;  // the bias gradient comes with dZ
-    const Turns turns(gated ? p.half : 2 * p.half, 2 * p.half);
+    const Turns turns = Turns::of_pairs(gated, true, p.half);
     const size_t slot_rows = 8 * (size_t)(p.places + G), column_bytes = column_sums ? ArenaCursor::granule(sizeof(float) * slot_rows * turns.groups * wide) : 0,
                  slot_bytes = column_bytes + (dslope ? sizeof(float) * slot_rows * 4 * p.n_tiles : 0);
     size_t dw_bytes = 0;

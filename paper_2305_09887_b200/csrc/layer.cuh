@@ -92,13 +92,16 @@ struct LayerBias {
 // 47, first step of the gradient 46 -> 41 us; fp32 700,000 x 64 -> 2 125 -> 99, 64 -> 64 135 -> 105).
 struct Turns {
     int groups, slices, buffers, spacing;  // slices: warps for each quarter of the rows that share a tile's columns
-    // wide: columns of a tile, of which a warp takes 32 (or every fourth 32) of its rows (fp32: half of the columns, as a warp takes 64), columns: of its accumulator
-    __host__ __device__ Turns(int wide, int columns) {
+    // wide: columns of a tile, of which a warp takes 32 (or every fourth 32) of its rows (fp32: half of the columns, as a warp takes 64)
+    __host__ __device__ explicit Turns(int wide) {
         slices = wide <= 32 ? 1 : wide <= 64 ? 2 : 4;
         groups = 4 / slices;
-        buffers = columns <= 128 ? 4 : 2;
+        buffers = groups > 1 ? 4 : 2;
         spacing = 512 / buffers;
     }
+    // 16-bit rows.  Not for the gradient of gated layers: the registers that it takes cost 500,000 x 256 -> 2 x 512 387 -> 412 us
+    // without any turn taken
+    __host__ __device__ static Turns of_pairs(bool gated, bool gradient, int half) { return Turns(gated ? (gradient ? 256 : half) : 2 * half); }
 };
 
 // Values from `valid` on become zero: tensor memory may hold anything in columns that are not the tile's, and a sum must not see it.

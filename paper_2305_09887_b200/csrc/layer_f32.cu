@@ -134,7 +134,7 @@ __device__ __forceinline__ uint64_t describe(uint32_t lbo, uint32_t sbo, bool na
 __device__ __forceinline__ void f32_multiplier(const LayerArgs& a, F32Shared& sh, uint32_t rows, uint32_t planes) {
     const uint32_t idesc = tc::idesc_bf16(2 * BM, 2 * a.half, false, true);
     constexpr uint32_t ap = A_PLANE >> 4, wp = 64 * BK * 2 >> 4;  // from one plane to the next
-    const Turns turns(a.half, 2 * a.half);
+    const Turns turns(a.half);
     StageWalk w;
     tc::RingAt at, acc;
     for (bool more = w.open(a, sh); more; more = w.next(sh)) {
@@ -172,7 +172,7 @@ __device__ __forceinline__ void f32_drain(const LayerArgs& a, F32Shared& sh, uin
     typedef Outlet<float, SLABS> Out;
     constexpr int ITEMS = GATED ? 2 : 4;  // of 16 results a row
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3;
-    const Turns turns(a.half, 2 * a.half);
+    const Turns turns(a.half);
     const int slice = (warp >> 2) % turns.slices, group = (warp >> 2) / turns.slices;
     slabs += warp * SLABS * SLAB;
     LayerBias bias{sh.bias + 64 * warp};

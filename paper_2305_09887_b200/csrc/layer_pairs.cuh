@@ -109,7 +109,7 @@ __device__ __forceinline__ void pair_multiplier(const LayerArgs& a, PairShared& 
     const uint32_t format = std::is_same<typename F::T, __half>::value ? 0u : 1u;  // fp16 or bf16 operands, fp32 sums
     const uint32_t idesc = (1u << 4) | (format << 7) | (format << 10) | (1u << 16) | ((uint32_t)(2 * a.half >> 3) << 17) | ((uint32_t)(2 * BM >> 4) << 24);
     const uint64_t desc = tc::smem_desc_sw128(0, 2 * SLAB_BYTES, 1024);  // atoms of 64 columns lie two slabs apart
-    const Turns turns(F::GATED ? a.half : 2 * a.half, 2 * a.half);
+    const Turns turns = Turns::of_pairs(F::GATED, F::GRADIENT, a.half);
     PairWalk w;
     tc::RingAt at, acc;
     int part = -1;
@@ -166,15 +166,16 @@ __device__ __forceinline__ void add_columns(uint32_t slab, int lane, float (&c)[
         }
 }
 
-template <class F, int ACT, bool BESIDE>
+// NARROW: by turns.
+template <class F, int ACT, bool BESIDE, bool NARROW>
 __device__ __forceinline__ void pair_drain(const LayerArgs& a, PairShared& sh, uint32_t slabs, int rank) {
     typedef typename F::T T;
     typedef Outlet<T, F::SLABS> Out;
     constexpr bool GATED = F::GATED, GRADIENT = F::GRADIENT;
     constexpr int ITEMS = GATED ? 1 : 2, PIECE = 16 / (int)sizeof(T);  // chunks of 32 columns a tile for a warp, at most
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3;
-    const Turns turns(GATED ? a.half : 2 * a.half, 2 * a.half);
-    const int slice = (warp >> 2) % turns.slices, group = (warp >> 2) / turns.slices;
+    const Turns turns = NARROW ? Turns::of_pairs(GATED, GRADIENT, a.half) : Turns(256);
+    const int slice = NARROW ? (warp >> 2) % turns.slices : warp >> 2, group = NARROW ? (warp >> 2) / turns.slices : 0;
     slabs += warp * F::OUT_BYTES;
     LayerBias bias{sh.bias + 64 * warp};
     uint64_t* const side = sh.side[warp];
@@ -188,7 +189,7 @@ __device__ __forceinline__ void pair_drain(const LayerArgs& a, PairShared& sh, u
     bool more = w.open(a, sh), ahead_more = more && BESIDE && mine > 0;
     ahead = w;
     const int start = w.t;
-    auto is_mine = [&](const PairWalk& x) { return (x.t - start & turns.groups - 1) == group; };
+    auto is_mine = [&](const PairWalk& x) { return !NARROW || (x.t - start & turns.groups - 1) == group; };
     int ahead_item = 0;
     // The rows beside the next 32 columns that are this warp's, into slab n & 1, whose last store has to have been read.
     auto request = [&](uint32_t n) {
@@ -384,7 +385,12 @@ __device__ __forceinline__ void pair_body(const LayerArgs& a) {
     const int rank = (int)tc::cluster_rank();
     if (warp < F::DRAIN_WARPS) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(PAIR_DRAIN_REGISTERS));
-        with_activation<F::GRADIENT>(a, [&](auto act, auto beside) { pair_drain<F, decltype(act)::value, decltype(beside)::value>(a, sh, slabs, rank); });
+        auto drain = [&](auto narrow) {
+            with_activation<F::GRADIENT>(a, [&](auto act, auto beside) { pair_drain<F, decltype(act)::value, decltype(beside)::value, decltype(narrow)::value>(a, sh, slabs, rank); });
+        };
+        if constexpr (F::GATED && F::GRADIENT) drain(std::false_type());
+        else if (Turns::of_pairs(F::GATED, F::GRADIENT, a.half).groups > 1) drain(std::true_type());
+        else drain(std::false_type());
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PAIR_OTHER_REGISTERS));
         if (warp == F::DRAIN_WARPS && rank == 0) pair_multiplier<F>(a, sh, ring, held);

@@ -2,7 +2,7 @@
 //
 // Pairs of blocks (MMAs of 256 x up to 256 over 64 rows a stage); rows run across both operands, so that both come as they lie.  The
 // left operand (256 columns a tile) is X or dZ, whichever makes fewer MMAs; every stage's 32 KB a block come from the L2 cache, which is what
-// bounds it: 500,000 x 256 x 1,024 in bf16 281 us (0.93 PFLOP/s; memory's share of it 213), 500,000 x 256 x 256 95 us; as tiles of 128 x 128 in
+// bounds it: 500,000 x 256 x 1,024 in bf16 278 us (0.94 PFLOP/s; 7.4 TB/s from that cache), 500,000 x 256 x 256 106 us (100 without its launch; 4.8 TB/s from memory); as tiles of 128 x 128 in
 // grouped_linear.cu 456 and 127.  The parts' rows are cut into chunks as there, one slot of fp32 sums for each, added up by a second kernel.
 //
 // The tensor cores truncate when they accumulate: sixteen warps take the accumulator after every 128 rows and add it up in registers, rounded to
@@ -91,7 +91,7 @@ struct GradWalk {
     __device__ __forceinline__ bool sums(const GradArgs& a) const { return a.sums && (a.swapped ? n0 : m0) == 0; }
 };
 
-// A warp for either operand (500,000 x 256 x 1,024: one for both 321 us, these two 293).  Rows behind the end of a chunk belong to
+// A warp for either operand (500,000 x 256 x 1,024: one for both 286 us, these two 278).  Rows behind the end of a chunk belong to
 // another part: the last stage's rows are copied by the lanes, with zeros behind them.
 template <class T, bool RIGHT>
 __device__ __forceinline__ void grad_producer(const GradArgs& a, GradShared& sh, uint8_t* ring, int rank, int lane) {

@@ -152,3 +152,17 @@ def test_most_parts_clipped(ctx):
     norms = ctx.clip_gradients([t], 3.0, parts=binding.MAX_GROUPS)
     assert ((norms.double() - want).abs() <= 8 * 2.0**-24 * want).all()
     assert (t.double().norm(dim=1) <= 3.0 * (1 + 2.0**-22)).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_stream_of_its_own(dtype):
+    """stream=: everything the call makes and launches is on that stream."""
+    ctx, stream = binding.Context(0), torch.cuda.Stream()
+    case = Case(dtype, [5000, 0, 700], 100, 90, "prelu", True, seed=97)
+    want = [t.clone() for t in (case.forward(ctx), *case.gradient(ctx))]
+    stream.wait_stream(torch.cuda.current_stream())
+    got = (case.forward(ctx, stream=stream), *case.gradient(ctx, stream=stream))
+    stream.synchronize()
+    a, b = case.o[0], case.o[-1]
+    for x, y in zip(got, want):
+        assert torch.equal(x[a:b], y[a:b]) if x.shape[0] == case.X.shape[0] else torch.equal(x, y)
