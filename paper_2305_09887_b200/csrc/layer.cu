@@ -38,8 +38,8 @@ struct AlignArgs {
 constexpr int ALIGN_BYTES = 16384;
 
 // A block brings neighbouring rows as the 16-byte words that they lie in, and cuts them up in shared memory while the next ones come (200,000 x 100 in
-// fp16 24 us; 300,000 x 100 and x 47 37 us, 4.8 TB/s: instructions, of which they issue 64 % of what they can).  Copied by the products for every tile of columns again, such rows cost
-// more than the products: 200,000 x 100 -> 2 x 266 222 us, like this 81 and 24.
+// fp16 24 us; 300,000 x 100 and x 47 37 us, 4.8 TB/s: instructions, of which they issue 64 % of what they can).  Copied by the products for every
+// tile of columns again, such rows cost more than the products: 200,000 x 100 -> 2 x 266 222 us, like this 81 and 24.
 __global__ void __launch_bounds__(256) align_rows_kernel(const __grid_constant__ AlignArgs args) {
     __shared__ uint4 words[ALIGN_BYTES / 16 + 258];  // (a row's last words are read beyond it, and dropped)
     wait_for_kernel_before();

@@ -2,8 +2,8 @@
 //
 // Pairs of blocks (MMAs of 256 x up to 256 over 64 rows a stage); rows run across both operands, so that both come as they lie.  The
 // left operand (256 columns a tile) is X or dZ, whichever makes fewer MMAs; every stage's 32 KB a block come from the L2 cache, which is what
-// bounds it: 500,000 x 256 x 1,024 in bf16 278 us (0.94 PFLOP/s; 7.4 TB/s from that cache), 500,000 x 256 x 256 106 us (100 without its launch; 4.8 TB/s from memory); as tiles of 128 x 128 in
-// grouped_linear.cu 456 and 127.  The parts' rows are cut into chunks as there, one slot of fp32 sums for each, added up by a second kernel.
+// bounds it: 500,000 x 256 x 1,024 in bf16 278 us (0.94 PFLOP/s; 7.4 TB/s from that cache), 500,000 x 256 x 256 106 us (4.8 TB/s from memory);
+// as tiles of 128 x 128 in grouped_linear.cu 456 and 127.  The parts' rows are cut into chunks as there, one slot of fp32 sums for each, added up by a second kernel.
 //
 // The tensor cores truncate when they accumulate: sixteen warps take the accumulator after every 128 rows and add it up in registers, rounded to
 // nearest, a quarter of a row's columns in a lane.  The same warps take dZ's column sums from the stages where no kernel before has (layers without activation
