@@ -765,10 +765,12 @@ class Context:
             self._here(t, name)
         if t.is_contiguous():
             return t.data_ptr(), t.numel() // parts
+        if parts == 1:  # whole: of one dimension, too, there is no distance between values
+            raise ValueError(f"{name} must be contiguous")
         want, steps = 1, t.stride()
         for k in range(len(size) - 1, 0, -1):
-            if steps[k] != want and size[k] != 1 or parts == 1:
-                raise ValueError(f"{name} must be contiguous{' within a part' if parts > 1 else ''}")
+            if steps[k] != want and size[k] != 1:
+                raise ValueError(f"{name} must be contiguous within a part")
             want *= size[k]
         return t.data_ptr(), steps[0]
 
@@ -818,7 +820,8 @@ class Context:
     def clip_gradients(self, grads, max_norm, parts=1, out=None, zero_nonfinite=False, stream=None):
         """Scales the tensors `grads` down so that their norm, over all of them together, is max_norm at most; returns the norms [parts]
         float32 from before.  parts = G: every tensor is [G, ...] and every part has a norm and a scale of its own.  Tensors are contiguous,
-        or contiguous within a part.  In place, or into the tensors `out` of the same shapes, of the gradient's type or float32 (for
+        or contiguous within a part (of one part: within an index of the first dimension, where that is equally long in all of them, MAX_GROUPS at
+        most; others that are not contiguous are refused).  In place, or into the tensors `out` of the same shapes, of the gradient's type or float32 (for
         instance views of the grads [M, P] that sgd_aggregate takes); an entry that is None is only part of the norm; no tensor twice.  Where a norm is not
         finite the gradients stay as they are or (zero_nonfinite) become zeros."""
         grads = list(grads)
