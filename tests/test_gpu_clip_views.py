@@ -3,6 +3,7 @@ import pytest
 import torch
 
 from paper_2305_09887_b200 import binding
+from layer_reference import rounding
 from test_gpu_clip import NORM, TYPES
 from test_gpu_layers import normal
 
@@ -35,6 +36,6 @@ def test_a_column(ctx, dtype, rows, beside):
     assert torch.equal(whole[:, ::2], before[:, ::2])
     near = before[:, 1].contiguous()
     ctx.clip_gradients([near], 0.5)
-    # (the sums of squares are put together in another order: two factors in fp32 that are a step apart, and one rounding of the type)
-    most = (2 * NORM + 2.0**-22 + torch.finfo(dtype).eps) * near.double().abs()
+    # (the sums of squares are put together in another order: two factors in fp32 that are a step apart, and a rounding to the type each)
+    most = (2 * NORM + 2.0**-22) * near.double().abs() + 2 * rounding(near.double(), dtype)
     assert ((column.double() - near.double()).abs() <= most).all()
