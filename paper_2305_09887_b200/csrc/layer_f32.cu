@@ -120,7 +120,7 @@ __device__ __forceinline__ void f32_splitter(const LayerArgs& a, F32Shared& sh, 
         __syncwarp();
         if (lane == 0) {
             tc::mbar_arrive(&sh.raw_free[raw_at.s]);
-            tc::mbar_arrive_remote(tc::leader_addr(&sh.full[at.s]));  // (each block's planes are read by its own tensor cores: the fence has made them visible)
+            tc::mbar_arrive_written(tc::leader_addr(&sh.full[at.s]));
         }
         raw_at.advance(RAW_STAGES);
         at.advance(STAGES);
