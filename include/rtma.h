@@ -445,7 +445,8 @@ int32_t rtma_grouped_layer(rtma_ctx* ctx, const rtma_layer_desc* desc, int64_t n
  *                 boundaries, and d_out (of a gated layer each of its halves) is rounded up to a multiple of 8 values, zeros behind.
  *                 May be dY if not gated and not rounded up.  Not used (may be NULL) by a layer with neither activation nor gate: dZ is dY.
  *   dX            = dZ W_g^T (NULL: not wanted).  It overlaps neither X nor dZ.
- *   dW, db        as in rtma_grouped_linear_dw with dZ in dY's place (each may be NULL; db only with dW), in grad_dtype, rounded once.
+ *   dW, db        as in rtma_grouped_linear_dw with dZ in dY's place (each may be NULL; db only with dW), in grad_dtype, rounded once.  Either
+ *                 can be one for all parts without the other.
  *   dslope        float, PReLU only (may be NULL): sum of dY min(Z, 0) (gated: of dY U min(V, 0)); stride 0 with G > 1: over all parts.
  * At Z = 0 ReLU and PReLU take the derivative of the negative side.                            */
 int32_t rtma_grouped_layer_grad(rtma_ctx* ctx, const rtma_layer_desc* desc, int64_t n, int32_t G, const int64_t* offsets,

@@ -40,6 +40,8 @@ struct GradArgs : LinearArgs {  // A, map_a: the left operand, B, map_b: the rig
     int width, real_width;  // of dZ's halves, with and without what was rounded up
     int real_out;      // columns of dW
     void *to_w, *to_b; // dW and db, in float or in the rows' type
+    int first_row, rows;  // of the slots, which a reduction adds up: d_in of dW, then db
+    bool all_parts;       // over all parts
 };
 
 template <int SIZE>
@@ -575,12 +577,12 @@ __global__ void __launch_bounds__(256) layer_wgrad_reduce_kernel(const __grid_co
         s.z += v.z;
         s.w += v.w;
     };
-    const int part = blockIdx.y, from = tile_start[part], count = tile_start[part + 1] - from, quads = (int)a.ldo / 4;
+    const int part = blockIdx.y, from = a.all_parts ? 0 : tile_start[part], count = tile_start[a.all_parts ? a.G : part + 1] - from, quads = (int)a.ldo / 4;
     const int64_t slot = (a.d_in + a.sum_rows) * a.ldo;
-    const int all = (a.d_in + (a.sums ? 1 : 0)) * quads;
-    const float* const slots = a.slots + from * slot;
+    const int all = a.rows * quads;
+    const float* const slots = a.slots + from * slot + a.first_row * a.ldo;
     auto put = [&](int i, float4 s) {
-        const int row = i / quads, col = 4 * (i - row * quads);
+        const int at = i / quads, row = a.first_row + at, col = 4 * (i - at * quads);
         O* to = row < a.d_in ? static_cast<O*>(a.to_w) + part * a.dw_stride + (int64_t)row * a.real_out : static_cast<O*>(a.to_b) + part * a.db_stride;
         const int second = a.d_out > a.width && col >= a.width ? 1 : 0, c = col - second * a.width;  // (of two halves each is a multiple of 8)
         to += second * a.real_width + c;
@@ -592,7 +594,7 @@ __global__ void __launch_bounds__(256) layer_wgrad_reduce_kernel(const __grid_co
     // a quad's sums over every `step`-th slot from `first` on; the bias's over the shares of the rows, too
     auto sum = [&](int i, int first, int step) {
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        const int shares = i >= a.d_in * quads ? a.sum_rows : 1;
+        const int shares = i >= (a.d_in - a.first_row) * quads ? a.sum_rows : 1;
         for (int k = 0; k < shares; ++k) {
             const float* p = slots + first * slot + 4 * (int64_t)i + k * a.ldo;
 #pragma unroll 4
@@ -622,11 +624,12 @@ int32_t layer_dw(rtma_ctx* ctx, const char* who, const rtma_layer_desc* d, int64
                  int64_t lddz, int width, void* dW, int64_t dw_stride, void* db, int64_t db_stride, bool sums, size_t at, size_t* scratch, cudaStream_t stream) {
     const int halves = d->gated ? 2 : 1, d_in = d->d_in, d_out = halves * width, real_out = halves * d->d_out;
     const int64_t weights = (int64_t)d_in * real_out;
-    const bool shared = G > 1 && dw_stride == 0, bf16 = d->dtype == RTMA_BF16, f32 = d->dtype == RTMA_F32;
-    if (G > 1 && db && (db_stride == 0) != shared)
-        return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: either both gradients are one for all parts or neither", who);
-    if (G > 1 && !shared && ((dw_stride < weights && dw_stride > -weights) || (db && db_stride < real_out && db_stride > -real_out)))
-        return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: gradients of the parts overlap", who);
+    const bool bf16 = d->dtype == RTMA_BF16, f32 = d->dtype == RTMA_F32;
+    auto overlap = [G](int64_t stride, int64_t size) { return G > 1 && stride && stride < size && stride > -size; };
+    if (overlap(dw_stride, weights) || (db && overlap(db_stride, real_out))) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: gradients of the parts overlap", who);
+    // One gradient for all parts: their rows are cut into chunks as one.  Of weights and bias only one: cut part by part, and only what is for all of them
+    // is added up over all.
+    const bool mixed = G > 1 && db && sums && (dw_stride == 0) != (db_stride == 0), shared = G > 1 && dw_stride == 0 && !mixed;
     GradArgs a{};
     a.error_word = ctx->error_word;
     a.offsets = offsets; a.n = n;
@@ -683,8 +686,18 @@ int32_t layer_dw(rtma_ctx* ctx, const char* who, const rtma_layer_desc* d, int64
     }
     KernelScope ks(ctx, KC_REDUCE_SGD, stream);
     void (*reduce)(GradArgs) = d->grad_dtype == RTMA_F32 ? layer_wgrad_reduce_kernel<float> : bf16 ? layer_wgrad_reduce_kernel<__nv_bfloat16> : layer_wgrad_reduce_kernel<__half>;
-    const int64_t blocks = ceil_div((int64_t)(d_in + 1) * a.ldo / 4, 32);
-    launch_kernel(reduce, dim3((unsigned)std::min<int64_t>(blocks, std::max(1, 8 * ctx->sm_count / a.G)), (unsigned)a.G), 256, 0, stream, a);
+    auto add_up = [&](int first_row, int rows, bool all_parts) {
+        a.first_row = first_row; a.rows = rows; a.all_parts = all_parts;
+        const int parts = all_parts ? 1 : a.G;
+        launch_kernel(reduce, dim3((unsigned)std::min<int64_t>(ceil_div(rows * a.ldo / 4, 32), std::max(1, 8 * ctx->sm_count / parts)), (unsigned)parts), 256, 0, stream, a);
+    };
+    if (!mixed) {
+        add_up(0, d_in + (a.sums ? 1 : 0), false);
+    } else {
+        add_up(0, d_in, dw_stride == 0);
+        RTMA_LAUNCH_CHECK(ctx);
+        add_up(d_in, 1, db_stride == 0);
+    }
     RTMA_LAUNCH_CHECK(ctx);
     return RTMA_OK;
 }
