@@ -24,7 +24,7 @@ namespace {
 using namespace grouped;
 
 constexpr int BM = PAIR_BM, BK = 64;
-constexpr int SUMMED_TILES = 64;     // after which the column sums go to their slots: tensor cores truncate, by 2^-23 of the sum at most for 16 rows
+constexpr int SUMMED_TILES = 64;     // after which the sums of columns and slopes go to their slots, so that not every tile's meet a long sum
 constexpr int RESIDENT_TERMS = 256;  // of the contraction, up to which the matrix stays in shared memory
 
 template <class T_, bool GATED_, bool GRADIENT_, bool RESIDENT_>
@@ -140,14 +140,16 @@ __device__ __forceinline__ void pair_multiplier(const LayerArgs& a, PairShared& 
     }
 }
 
-// Sums of the 32 columns of a slab over its 32 rows, added to c: c[m][0] of lane l is column 16 m + l / 4, c[m][2] the one 8 behind it.
+// Sums of the 32 columns of a slab over its 32 rows, added to sums: sums[m][0] of lane l is column 16 m + l / 4, sums[m][1] the one 8 behind it.  Products
+// with ones; the tensor cores' accumulators, which truncate, hold no more than these 32 rows (their other halves are the same again).
 template <class T>
-__device__ __forceinline__ void add_columns(uint32_t slab, int lane, float (&c)[2][4]) {
+__device__ __forceinline__ void add_columns(uint32_t slab, int lane, float (&sums)[2][2]) {
     const uint32_t one = std::is_same<T, __half>::value ? 0x3C003C00u : 0x3F803F80u;
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+    for (int m = 0; m < 2; ++m) {
+        float c[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
+        for (int k = 0; k < 2; ++k) {
             // four 8 x 8 blocks: columns 16 m .. + 7 and + 8 .. + 15 of rows 16 k .. + 7, then of rows + 8 .. + 15
             const int row = 16 * k + 8 * (lane >> 4) + (lane & 7), q = 2 * m + (lane >> 3 & 1);
             uint32_t x[4];
@@ -157,13 +159,16 @@ __device__ __forceinline__ void add_columns(uint32_t slab, int lane, float (&c)[
                          : "memory");
             if constexpr (std::is_same<T, __half>::value)
                 asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %8}, {%0, %1, %2, %3};"
-                             : "+f"(c[m][0]), "+f"(c[m][1]), "+f"(c[m][2]), "+f"(c[m][3])
+                             : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                              : "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(one));
             else
                 asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %8}, {%0, %1, %2, %3};"
-                             : "+f"(c[m][0]), "+f"(c[m][1]), "+f"(c[m][2]), "+f"(c[m][3])
+                             : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                              : "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(one));
         }
+        sums[m][0] += c[0];
+        sums[m][1] += c[2];
+    }
 }
 
 // NARROW: by turns.
@@ -210,13 +215,13 @@ __device__ __forceinline__ void pair_drain(const LayerArgs& a, PairShared& sh, u
     uint32_t n = 0;  // 32 columns that this warp has been through
     request(0);
     tc::RingAt acc;
-    float slope = 0.f, slope_sum = 0.f, sums[GRADIENT ? 2 : 1][2][4];
+    float slope = 0.f, slope_sum = 0.f, sums[GRADIENT ? 2 : 1][2][2];
     int part = -1;
     auto clear = [&]() {
         slope_sum = 0.f;
         if constexpr (GRADIENT)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sums[i >> 3][i >> 2 & 1][i & 3] = 0.f;
+            for (int i = 0; i < 8; ++i) sums[i >> 2][i >> 1 & 1][i & 1] = 0.f;
     };
     clear();
     for (; more; more = w.next(sh)) {
@@ -330,7 +335,7 @@ __device__ __forceinline__ void pair_drain(const LayerArgs& a, PairShared& sh, u
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const int j = 8 * k + (lane >> 2);
-                        if (j < cols) to[j] = sums[i][k >> 1][2 * (k & 1)] + (again ? to[j] : 0.f);
+                        if (j < cols) to[j] = sums[i][k >> 1][k & 1] + (again ? to[j] : 0.f);
                     }
                 }
             }
