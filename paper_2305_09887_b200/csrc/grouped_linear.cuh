@@ -57,6 +57,17 @@ __host__ __device__ __forceinline__ int fit_chunk(int least, int most, int64_t t
     return lo;
 }
 
+// Between what that search has to look, in steps: c steps make all / c chunks or more, and less than G above that (in a few tries: of 8 parts 3 instead
+// of 12).  all: steps of all parts; longest: of the largest part; tile_rows: rows of a chunk at least.
+struct ChunkBounds {
+    int least, fits;
+};
+template <int STEP>
+__host__ __device__ __forceinline__ ChunkBounds chunk_bounds(int64_t all, int longest, int64_t tile_rows, int64_t tiles, int G) {
+    const int64_t least = tile_rows / STEP, even = (all + tiles - 1) / tiles, fits = tiles > G ? (all + tiles - G - 1) / (tiles - G) : longest;
+    return {(int)(even > least ? even : least), (int)(fits < longest ? fits : longest)};
+}
+
 struct Shared {
     uint64_t full[MAX_STAGES], empty[MAX_STAGES];
     uint64_t acc_full[MAX_ACCUMULATORS], acc_empty[MAX_ACCUMULATORS];
@@ -160,10 +171,8 @@ __device__ __forceinline__ void lay_out(const LinearArgs& a, Shared& sh) {
                 most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
                 all += __shfl_xor_sync(0xffffffffu, all, o);
             }
-            // c steps make all / c chunks or more, and less than G above that: between these bounds lies what is looked for (in a few steps: of 8 parts 3 of 12)
-            const int least = max((int)a.tile_rows / STEP, (int)((all + a.tiles - 1) / a.tiles));
-            const int fits = a.tiles > a.G ? (int)min((int64_t)steps_of<STEP>(most), (all + a.tiles - a.G - 1) / (a.tiles - a.G)) : steps_of<STEP>(most);
-            const int chunk = fit_chunk(least, fits, a.tiles, [&](int steps) {
+            const ChunkBounds bounds = chunk_bounds<STEP>(all, steps_of<STEP>(most), a.tile_rows, a.tiles, a.G);
+            const int chunk = fit_chunk(bounds.least, bounds.fits, a.tiles, [&](int steps) {
                 int64_t count = 0;
                 for (int g = lane; g < a.G; g += 32) count += (steps_of<STEP>(sh.rows[g]) + steps - 1) / steps;
                 for (int o = 16; o > 0; o >>= 1) count += __shfl_xor_sync(0xffffffffu, count, o);
