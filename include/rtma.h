@@ -430,7 +430,8 @@ int32_t rtma_group_norm_grad(rtma_ctx* ctx, const rtma_norm_desc* desc, int64_t 
  *   Y[r] = residual[r] + act(X[r] V_g + c_g) * (X[r] U_g + d_g), W_g = [V_g | U_g], b_g = [c_g | d_g]   gated = 1
  * W_g [d_in][d_out], or [d_in][2 d_out] of a gated layer (2 d_out <= RTMA_MAX_WIDTH); b (may be NULL) likewise; both of the rows' type.
  * act and slope (PReLU: one per part) as in rtma_group_norm; any of them gates.  The product is held in fp32 up to
- * the one rounding of Y; sums as in rtma_grouped_linear.  residual [n][ldr] may be NULL, and may be Y.  X and Y must not overlap. */
+ * the one rounding of Y; sums as in rtma_grouped_linear.  residual [n][ldr] may be NULL, and may be Y
+ * (then ldr = ldy).  Y overlaps neither X, W nor b; calls in which it starts where one of them does are refused. */
 typedef struct {
     int32_t dtype, d_in, d_out, act, gated;
     int32_t grad_dtype; /* of dW and db: RTMA_F32 or dtype */
@@ -449,6 +450,8 @@ int32_t rtma_grouped_layer(rtma_ctx* ctx, const rtma_layer_desc* desc, int64_t n
  *                 can be one for all parts without the other.  (db of 16-bit rows behind an activation or a gate: sums of 32 rows are formed
  *                 by the tensor cores, which truncate, by 2^-22 of them at most, and added up in fp32 rounded to nearest.)
  *   dslope        float, PReLU only (may be NULL): sum of dY min(Z, 0) (gated: of dY U min(V, 0)); stride 0 with G > 1: over all parts.
+ * Results overlap neither one another nor what is still read: dZ and dX lie in neither W nor b, dX may be dY where dZ is rows of its own, dW may be W, db b and dslope slope.
+ * Calls in which they start at such a place are refused.
  * At Z = 0 ReLU and PReLU take the derivative of the negative side.                            */
 int32_t rtma_grouped_layer_grad(rtma_ctx* ctx, const rtma_layer_desc* desc, int64_t n, int32_t G, const int64_t* offsets,
                                 const void* X, int64_t ldx, const void* W, const void* b, const float* slope,

@@ -394,7 +394,9 @@ extern "C" int32_t rtma_grouped_layer(rtma_ctx* ctx, const rtma_layer_desc* d, i
     if (!X || !W || !Y) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: null pointer", who);
     if (ldx < d->d_in || ldy < d->d_out || (residual && ldr < d->d_out))
         return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: rows of %d and %d values lie closer than that", who, d->d_in, d->d_out);
-    if (X == Y) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: the result must not overlap the rows", who);
+    if (X == Y || Y == W || Y == b) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: the result must not overlap the rows, the matrices or the bias", who);
+    // (rows of one that are other rows of the other would be read ahead, or after they have been written)
+    if (residual == Y && ldr != ldy && n > 1) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: a result in the residual branch's place must not overlap other rows of it", who);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     DeviceScope on(ctx->device);
     RTMA_CUDA(ctx, on.status);
@@ -427,6 +429,13 @@ extern "C" int32_t rtma_grouped_layer_grad(rtma_ctx* ctx, const rtma_layer_desc*
         if (row_granule(dZ, lddz, row_type_bytes(d->dtype)) < 16) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: rows of dZ off 16-byte boundaries", who);
     }
     if (n > 0 && dX && (dX == X || (dX == dY && plain))) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: dX must not overlap rows that are still read", who);
+    const void* const results[] = {plain || n == 0 ? nullptr : dZ, n == 0 ? nullptr : dX, dW, db, dslope};
+    for (int i = 0; i < 5; ++i) {
+        if (!results[i]) continue;
+        if (i < 2 && (results[i] == W || results[i] == b)) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: rows of a result must not overlap the matrices or the bias", who);
+        for (int j = 0; j < i; ++j)
+            if (results[i] == results[j]) return rtma_fail(ctx, RTMA_ERR_INVALID_ARG, "%s: results must not overlap one another", who);
+    }
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     DeviceScope on(ctx->device);
     RTMA_CUDA(ctx, on.status);
