@@ -699,6 +699,8 @@ class Context:
 
     def _gradient(self, X, dY, offsets, W, bias, act, slope, need_dx, need_dw, grad_dtype, out, dz, dw, db, dslope, stream, gated):
         if dw is not None:
+            if grad_dtype not in (None, dw.dtype):
+                raise TypeError(f"dw must be {grad_dtype}, got {dw.dtype}")
             grad_dtype = dw.dtype
         elif grad_dtype is None:
             grad_dtype = X.dtype
@@ -741,7 +743,7 @@ class Context:
                                 dz=None, dw=None, db=None, dslope=None, stream=None):
         """(dX, dW, db, dslope) of grouped_linear_act from its inputs and dY (the residual's gradient is dY itself); what lies in
         front of the activation is worked out again.  dW and db have the parameters' shape (summed over the parts for shared ones) and
-        grad_dtype: the rows' type, or float32; dslope float32.  None for a parameter that is None, and for what is not wanted
+        grad_dtype: the rows' type, or float32 (that of dw if it is given); dslope float32.  None for a parameter that is None, and for what is not wanted
         (need_dx, need_dw).  dz [n, d_out]: where the gradient in front of the activation is put, rounded to the rows' type, as
         the operand of the two products (a new one otherwise; act "none" has none), its rows on 16-byte boundaries and d_out rounded up
         to a multiple of 8, zeros behind; it may be dY where nothing is rounded up."""
