@@ -221,12 +221,6 @@ struct Outlet {
         __syncwarp();
         return slabs + at * 32 * ROW;
     }
-    // The one after it, which is closed after it.
-    __device__ __forceinline__ uint32_t open_second(int lane) const {
-        if (lane == 0) tc::tma_store_wait_read_but<SLABS - 2>();
-        __syncwarp();
-        return slabs + (at + 1 == SLABS ? 0 : at + 1) * 32 * ROW;
-    }
     // Piece q (16 bytes) of this lane's row; pack_piece: what it holds.
     __device__ __forceinline__ static void piece(uint32_t slab, int lane, int q, uint4 x) { store_16(slab + lane * ROW + ((q ^ swizzle(lane)) << 4), x); }
     __device__ __forceinline__ static uint4 pack_piece(const float* v) {
