@@ -4,7 +4,8 @@
 // Two passes over the gradients.  Every tensor's share of a part is cut into pieces of equal length, of which a few thousand keep all SMs
 // busy; the first pass leaves the sum of squares of every piece, the pieces of a part behind one another, and every block of the
 // second adds up those of its part itself, always in the same order, so that no kernel lies between the two and no block waits for another.
-// The second walks the pieces backwards: what the first has read last is still in the L2 cache.
+// The second walks the pieces backwards: what the first has read last may still be in the L2 cache (fp32 in eight parts, 90 MB of gradients: 66 us, forwards 71;
+// 180 MB 99, 101; 300 MB of bf16 into fp32 220 either way).
 //
 // Squares are added up in fp32 eight at a time, then in 64 bits; eight whose sum leaves the range of fp32 (or is so small that
 // squares got lost) are squared in 64 bits.  So the norm neither overflows nor underflows before its own value does.
