@@ -448,7 +448,7 @@ int32_t rtma_grouped_layer(rtma_ctx* ctx, const rtma_layer_desc* desc, int64_t n
  *                 May be dY if not gated and not rounded up.  Not used (may be NULL) by a layer with neither activation nor gate: dZ is dY.
  *   dX            = dZ W_g^T (NULL: not wanted).  It overlaps neither X nor dZ.
  *   dW, db        as in rtma_grouped_linear_dw with dZ in dY's place (each may be NULL; db only with dW), in grad_dtype, rounded once.  Either
- *                 can be one for all parts without the other.  (db of 16-bit rows behind an activation or a gate: sums of 32 rows are formed
+ *                 can be one for all parts without the other (which may take scratch for a gradient of each part).  (db of 16-bit rows behind an activation or a gate: sums of 32 rows are formed
  *                 by the tensor cores, which truncate, by 2^-22 of them at most, and added up in fp32 rounded to nearest.)
  *   dslope        float, PReLU only (may be NULL): sum of dY min(Z, 0) (gated: of dY U min(V, 0)); stride 0 with G > 1: over all parts.
  * Results overlap neither one another nor what is still read: dZ and dX lie in neither W nor b, dX may be dY where dZ is rows of its own, dW may be W, db b and dslope slope.
